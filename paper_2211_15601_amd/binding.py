@@ -22,7 +22,11 @@ FS_GRAD_BROYDEN_J, FS_GRAD_EXACT_J = 0, 1
 
 EXPORTS = ["fs_create", "fs_destroy", "fs_set_params", "fs_set_tuning", "fs_set_list_order", "fs_set_spin_limit", "fs_precompute", "fs_init", "fs_solve", "fs_grad",
            "fs_dedupe", "fs_dedupe_noalloc", "fs_get_transforms", "fs_get_corr", "fs_microbench", "fs_set_timing", "fs_get_timing", "fs_last_error",
-           "fs_version"]
+           "fs_version",
+           "fs_tensors_create", "fs_tensors_destroy", "fs_tensors_update", "fs_tensors_set_stream", "fs_tensors_error",
+           "fs_grad_norm", "fs_grad_clip", "fs_adamw_step"]
+FS_FLOAT_FULL, FS_FLOAT_BRAIN, FS_FLOAT_HALF = 0, 1, 2
+FS_NORM_TWO, FS_NORM_MAX = 0, 1
 
 
 class GridDesc(ctypes.Structure):
@@ -36,6 +40,19 @@ class Params(ctypes.Structure):
                 ("init_mode", ctypes.c_int32), ("grad_mode", ctypes.c_int32),
                 ("corr_nx", ctypes.c_int32), ("corr_ny", ctypes.c_int32), ("corr_nz", ctypes.c_int32),
                 ("corr_k", ctypes.c_int32)]
+
+
+class Tensor(ctypes.Structure):
+    """fs_tensor of include/fastsnarf_train.h"""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("grad", "out", "param", "master", "exp_avg", "exp_avg_sq")] + \
+               [("n", ctypes.c_int64), ("grad_type", ctypes.c_int32), ("param_type", ctypes.c_int32),
+                ("lr_scale", ctypes.c_float), ("decay_scale", ctypes.c_float)]
+
+
+class AdamW(ctypes.Structure):
+    """fs_adamw of include/fastsnarf_train.h"""
+    _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay", "max_norm", "grad_scale")] + \
+               [("norm_given", ctypes.c_int32), ("skip_nonfinite", ctypes.c_int32), ("d_lr", ctypes.c_void_p)]
 
 
 class FsError(RuntimeError):
@@ -78,8 +95,17 @@ def load():
     L.fs_get_timing.argtypes = [vp, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i32)]
     L.fs_dedupe.argtypes = [vp, vp, vp, i64, i32, ctypes.c_float, vp, vp, vp, vp, i64]
     L.fs_dedupe_noalloc.argtypes = L.fs_dedupe.argtypes
+    L.fs_tensors_create.argtypes = [ctypes.POINTER(Tensor), i32, vp, ctypes.POINTER(vp)]
+    L.fs_tensors_destroy.argtypes = [vp]
+    L.fs_tensors_update.argtypes = [vp, ctypes.POINTER(Tensor), i32]
+    L.fs_tensors_set_stream.argtypes = [vp, vp]
+    L.fs_tensors_error.argtypes = [vp]
+    L.fs_tensors_error.restype = ctypes.c_char_p
+    L.fs_grad_norm.argtypes = [vp, i32, ctypes.c_double, vp]
+    L.fs_grad_clip.argtypes = [vp, i32, ctypes.c_double, ctypes.c_double, i32, vp]
+    L.fs_adamw_step.argtypes = [vp, ctypes.POINTER(AdamW), vp, vp]
     for name in EXPORTS:
-        if name not in ("fs_last_error", "fs_version"):
+        if name not in ("fs_last_error", "fs_version", "fs_tensors_error"):
             getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L

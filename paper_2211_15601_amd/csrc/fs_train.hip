@@ -1,0 +1,322 @@
+// C ABI of the calls on a list of tensors (see include/fastsnarf_train.h): argument checks, the list's copy on the device,
+// launches.  gfx950 only.
+#include "../../include/fastsnarf_train.h"
+#include "fs_train_kernels.hpp"
+
+#include <hip/hip_runtime.h>
+#include <algorithm>
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+#include <cstring>
+#include <new>
+
+using namespace fs;
+
+struct fs_tensors {
+    hipStream_t stream;
+    int device, n_cus;
+    int32_t asked;            // tensors as given
+    fs_tensor *given;         // [asked] of the last create or update
+    TensorD *host;            // [asked] those with elements, as they are on the device
+    // what the tensors as a whole have
+    bool params, moments;
+    ListD L;
+    char *mem;                // device: TensorD [asked], int [asked + 1], double [TRAIN_BLOCKS], ticket
+    double *partial;
+    unsigned *ticket;
+    const void *seen[8];      // words (d_norm, d_step, d_lr) that are known to be memory of the device, by address
+    char err[256];
+};
+
+namespace {
+
+fs_status fail(fs_tensors *t, fs_status s, const char *fmt, ...)
+{
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(t->err, sizeof t->err, fmt, ap);
+    va_end(ap);
+    return s;
+}
+
+fs_status launch_status(fs_tensors *t, const char *what)
+{
+    hipError_t e = hipGetLastError();
+    return e == hipSuccess ? FS_OK : fail(t, FS_E_DEVICE, "%s: %s", what, hipGetErrorString(e));
+}
+
+bool on_device(const fs_tensors *t, const void *p)
+{
+    hipPointerAttribute_t a;
+    if (hipPointerGetAttributes(&a, p) != hipSuccess) {
+        (void)hipGetLastError();
+        return false;
+    }
+    return (a.type == hipMemoryTypeDevice || a.type == hipMemoryTypeManaged) && a.device == t->device;
+}
+
+// Null (where that is allowed) or aligned to an element of `size` bytes, and memory of the list's device: asked only where the
+// pointer is not the one of the same place in the list before (`before`), which has been confirmed.
+bool array_ok(const fs_tensors *t, const void *p, const void *before, bool nullable, int size)
+{
+    if (!p) return nullable;
+    if (reinterpret_cast<uintptr_t>(p) % size) return false;
+    return p == before || on_device(t, p);
+}
+
+// A word that a call reads or writes.  The lookup in the runtime takes as long as a launch, and a program passes the same words again and
+// again, so those it has confirmed are remembered, as fastsnarf.hip does for its arrays.
+bool word_ok(fs_tensors *t, const void *p, int size)
+{
+    const uintptr_t u = reinterpret_cast<uintptr_t>(p);
+    if (!p || u % size) return false;
+    const int h = (int)((u >> 3 ^ u >> 9) & 7);
+    if (t->seen[h] == p) return true;
+    if (!on_device(t, p)) return false;
+    t->seen[h] = p;
+    return true;
+}
+
+bool apart(const void *a, const void *b, size_t bytes)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x + bytes <= y || y + bytes <= x;
+}
+
+bool type_ok(int32_t type) { return type == FS_FLOAT_FULL || type == FS_FLOAT_BRAIN || type == FS_FLOAT_HALF; }
+int size_of(int32_t type) { return type == FS_FLOAT_FULL ? 4 : 2; }
+static_assert(int(FS_FLOAT_FULL) == TYPE_F32 && int(FS_FLOAT_BRAIN) == TYPE_BF16 && int(FS_FLOAT_HALF) == TYPE_F16, "types");
+static_assert(int(FS_NORM_TWO) == KIND_TWO && int(FS_NORM_MAX) == KIND_MAX, "kinds");
+static_assert(sizeof(PutD) + 64 <= 4096, "kernel arguments");
+
+// Checks a list.  `before`: the list whose pointers are known to be memory of the device, or NULL.
+fs_status check_list(fs_tensors *t, const char *what, const fs_tensor *list, int32_t count, const fs_tensor *before)
+{
+    long long units = 0;
+    for (int32_t i = 0; i < count; ++i) {
+        const fs_tensor &x = list[i];
+        if (x.n < 0 || x.n > 1ll << 40) return fail(t, FS_E_SHAPE, "%s: tensor %d: n out of range", what, i);
+        if (x.n == 0) continue;
+        units += (x.n + UNIT - 1) / UNIT;
+        if (units >= 1ll << 31) return fail(t, FS_E_SHAPE, "%s: tensor %d: too many elements in all", what, i);
+        if (!type_ok(x.grad_type) || (x.param && !type_ok(x.param_type))) return fail(t, FS_E_ARG, "%s: tensor %d: bad type", what, i);
+        if (!std::isfinite(x.lr_scale) || !std::isfinite(x.decay_scale)) return fail(t, FS_E_ARG, "%s: tensor %d: lr_scale and decay_scale must be finite", what, i);
+        fs_tensor old = {};
+        if (before && before[i].n) old = before[i];
+        const int gs = size_of(x.grad_type), ps = size_of(x.param_type);
+        if (!array_ok(t, x.grad, old.grad, false, gs) || !array_ok(t, x.out, old.out, true, gs) || !array_ok(t, x.param, old.param, true, ps) ||
+            !array_ok(t, x.master, old.master, true, 4) || !array_ok(t, x.exp_avg, old.exp_avg, true, 4) || !array_ok(t, x.exp_avg_sq, old.exp_avg_sq, true, 4))
+            return fail(t, FS_E_ARG, "%s: tensor %d: arrays must be device pointers aligned to their elements (grad not NULL)", what, i);
+        if (x.out && x.out != x.grad && !apart(x.out, x.grad, (size_t)x.n * gs))
+            return fail(t, FS_E_ARG, "%s: tensor %d: out overlaps grad", what, i);
+    }
+    return FS_OK;
+}
+
+// Takes a checked list over: the host's copies, and the device's in the stream's order.
+fs_status put_list(fs_tensors *t, const char *what, const fs_tensor *list)
+{
+    int count = 0, units = 0;
+    t->params = t->moments = true;
+    for (int32_t i = 0; i < t->asked; ++i) {
+        const fs_tensor &x = t->given[i] = list[i];
+        if (x.n == 0) continue;
+        TensorD &d = t->host[count++];
+        d.grad = x.grad;
+        d.out = x.out ? x.out : x.grad;
+        d.param = x.param;
+        d.master = x.master;
+        d.m = x.exp_avg;
+        d.v = x.exp_avg_sq;
+        d.n = x.n;
+        d.first = units;
+        d.types = x.grad_type | x.param_type << 8;
+        d.lr_scale = x.lr_scale;
+        d.decay_scale = x.decay_scale;
+        units += (int)((x.n + UNIT - 1) / UNIT);
+        t->params = t->params && x.param;
+        t->moments = t->moments && x.exp_avg && x.exp_avg_sq;
+    }
+    t->L.count = count;
+    t->L.units = units;
+    for (int at = 0; at < count; at += PUT) {
+        PutD p;
+        const int n = std::min(PUT, count - at);
+        std::memcpy(p.t, t->host + at, n * sizeof(TensorD));
+        k_list_put<<<1, 64, 0, t->stream>>>(p, at, n, count, units, const_cast<TensorD *>(t->L.tensors), const_cast<int *>(t->L.first));
+    }
+    return launch_status(t, what);
+}
+
+fs_status on_current_device(fs_tensors *t, const char *what)
+{
+    int dev = -1;
+    if (hipGetDevice(&dev) != hipSuccess || dev != t->device) {
+        (void)hipGetLastError();
+        return fail(t, FS_E_DEVICE, "%s: the list's device must be the current one", what);
+    }
+    return FS_OK;
+}
+
+#define FS_TRAIN_BEGIN(t)                                                 \
+    do {                                                                  \
+        if (!(t)) return FS_E_ARG;                                        \
+        const fs_status begin_status = on_current_device((t), __func__);  \
+        if (begin_status != FS_OK) return begin_status;                   \
+    } while (0)
+
+// Every block takes a stretch of units; more blocks than the device holds at once only where the stretches are long.
+int blocks_for(const fs_tensors *t) { return std::max(1, std::min(t->L.units, 8 * t->n_cus)); }
+
+void launch_norm(fs_tensors *t, int32_t kind, double scale, float *d_norm)
+{
+    if (kind == FS_NORM_TWO) k_norm<KIND_TWO><<<blocks_for(t), 256, 0, t->stream>>>(t->L, scale, t->partial, t->ticket, d_norm);
+    else k_norm<KIND_MAX><<<blocks_for(t), 256, 0, t->stream>>>(t->L, scale, t->partial, t->ticket, d_norm);
+}
+
+bool scale_ok(double s) { return s > 0.0 && std::isfinite(s); }
+
+}  // namespace
+
+extern "C" {
+
+const char *fs_tensors_error(const fs_tensors *t) { return t ? t->err : "null list"; }
+
+fs_status fs_tensors_create(const fs_tensor *list, int32_t count, void *hip_stream, fs_tensors **out)
+{
+    if (out) *out = nullptr;
+    if (!out || (!list && count > 0)) return FS_E_ARG;
+    if (count < 0 || count > FS_MAX_TENSORS) return FS_E_SHAPE;
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess) {
+        (void)hipGetLastError();
+        return FS_E_DEVICE;
+    }
+    fs_tensors *t = new (std::nothrow) fs_tensors;
+    if (!t) return FS_E_ALLOC;
+    std::memset(t, 0, sizeof *t);
+    t->stream = static_cast<hipStream_t>(hip_stream);
+    t->device = dev;
+    t->asked = count;
+    t->given = new (std::nothrow) fs_tensor[count + 1];
+    t->host = new (std::nothrow) TensorD[count + 1];
+    fs_status s = t->given && t->host ? FS_OK : FS_E_ALLOC;
+    if (s == FS_OK) s = check_list(t, "fs_tensors_create", list, count, nullptr);
+    if (s == FS_OK) {
+        if (hipDeviceGetAttribute(&t->n_cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || t->n_cus < 1) t->n_cus = 256;
+        (void)hipGetLastError();
+        t->n_cus = std::min(t->n_cus, TRAIN_BLOCKS / 8);
+        const size_t at_first = (size_t)count * sizeof(TensorD), at_partial = (at_first + ((size_t)count + 1) * sizeof(int) + 15) / 16 * 16;
+        const size_t at_ticket = at_partial + TRAIN_BLOCKS * sizeof(double);
+        if (hipMalloc(reinterpret_cast<void **>(&t->mem), at_ticket + 16) != hipSuccess) {
+            (void)hipGetLastError();
+            t->mem = nullptr;
+            s = FS_E_ALLOC;
+        } else {
+            t->L.tensors = reinterpret_cast<TensorD *>(t->mem);
+            t->L.first = reinterpret_cast<int *>(t->mem + at_first);
+            t->partial = reinterpret_cast<double *>(t->mem + at_partial);
+            t->ticket = reinterpret_cast<unsigned *>(t->mem + at_ticket);
+            k_ticket_clear<<<1, 64, 0, t->stream>>>(t->ticket);
+            s = put_list(t, "fs_tensors_create", list);
+        }
+    }
+    if (s != FS_OK) {
+        if (t->mem) (void)hipFree(t->mem);
+        delete[] t->given;
+        delete[] t->host;
+        delete t;
+        return s;
+    }
+    *out = t;
+    return FS_OK;
+}
+
+fs_status fs_tensors_destroy(fs_tensors *t)
+{
+    if (!t) return FS_OK;
+    (void)hipStreamSynchronize(t->stream);
+    (void)hipFree(t->mem);
+    delete[] t->given;
+    delete[] t->host;
+    delete t;
+    return FS_OK;
+}
+
+fs_status fs_tensors_update(fs_tensors *t, const fs_tensor *list, int32_t count)
+{
+    FS_TRAIN_BEGIN(t);
+    if (count != t->asked) return fail(t, FS_E_SHAPE, "fs_tensors_update: the list has %d tensors, not %d", t->asked, count);
+    if (!list && count) return fail(t, FS_E_ARG, "fs_tensors_update: list is NULL");
+    const fs_status s = check_list(t, "fs_tensors_update", list, count, t->given);
+    return s == FS_OK ? put_list(t, "fs_tensors_update", list) : s;
+}
+
+fs_status fs_tensors_set_stream(fs_tensors *t, void *hip_stream)
+{
+    if (!t) return FS_E_ARG;
+    t->stream = static_cast<hipStream_t>(hip_stream);
+    return FS_OK;
+}
+
+fs_status fs_grad_norm(fs_tensors *t, int32_t kind, double grad_scale, float *d_norm)
+{
+    FS_TRAIN_BEGIN(t);
+    if (kind != FS_NORM_TWO && kind != FS_NORM_MAX) return fail(t, FS_E_ARG, "fs_grad_norm: bad kind");
+    if (!scale_ok(grad_scale)) return fail(t, FS_E_ARG, "fs_grad_norm: grad_scale must be positive and finite");
+    if (!word_ok(t, d_norm, 4)) return fail(t, FS_E_ARG, "fs_grad_norm: d_norm must be a device pointer");
+    launch_norm(t, kind, grad_scale, d_norm);
+    return launch_status(t, "fs_grad_norm");
+}
+
+fs_status fs_grad_clip(fs_tensors *t, int32_t kind, double max_norm, double grad_scale, int32_t norm_given, float *d_norm)
+{
+    FS_TRAIN_BEGIN(t);
+    if (norm_given != 0 && norm_given != 1) return fail(t, FS_E_ARG, "fs_grad_clip: norm_given must be 0 or 1");
+    if (!norm_given && kind != FS_NORM_TWO && kind != FS_NORM_MAX) return fail(t, FS_E_ARG, "fs_grad_clip: bad kind");
+    if (!(max_norm >= 0.0)) return fail(t, FS_E_ARG, "fs_grad_clip: max_norm must not be negative");
+    if (!scale_ok(grad_scale)) return fail(t, FS_E_ARG, "fs_grad_clip: grad_scale must be positive and finite");
+    if (!word_ok(t, d_norm, 4)) return fail(t, FS_E_ARG, "fs_grad_clip: d_norm must be a device pointer");
+    if (!norm_given) launch_norm(t, kind, grad_scale, d_norm);
+    if (t->L.units) k_clip<<<blocks_for(t), 256, 0, t->stream>>>(t->L, max_norm, grad_scale, d_norm);
+    return launch_status(t, "fs_grad_clip");
+}
+
+fs_status fs_adamw_step(fs_tensors *t, const fs_adamw *how, int64_t *d_step, float *d_norm)
+{
+    FS_TRAIN_BEGIN(t);
+    if (!how) return fail(t, FS_E_ARG, "fs_adamw_step: how is NULL");
+    const fs_adamw &h = *how;
+    if (!std::isfinite(h.lr) || !std::isfinite(h.weight_decay)) return fail(t, FS_E_ARG, "fs_adamw_step: lr and weight_decay must be finite");
+    if (!(h.beta1 >= 0.0 && h.beta1 < 1.0 && h.beta2 >= 0.0 && h.beta2 < 1.0)) return fail(t, FS_E_ARG, "fs_adamw_step: betas must be in [0, 1)");
+    if (!(h.eps >= 0.0) || !std::isfinite(h.eps)) return fail(t, FS_E_ARG, "fs_adamw_step: eps must be finite and not negative");
+    if (!(h.max_norm >= 0.0)) return fail(t, FS_E_ARG, "fs_adamw_step: max_norm must not be negative");
+    if (!scale_ok(h.grad_scale)) return fail(t, FS_E_ARG, "fs_adamw_step: grad_scale must be positive and finite");
+    if ((h.norm_given != 0 && h.norm_given != 1) || (h.skip_nonfinite != 0 && h.skip_nonfinite != 1))
+        return fail(t, FS_E_ARG, "fs_adamw_step: norm_given and skip_nonfinite must be 0 or 1");
+    if (!d_norm && (h.norm_given || h.skip_nonfinite || std::isfinite(h.max_norm)))
+        return fail(t, FS_E_ARG, "fs_adamw_step: d_norm is NULL, but a norm is asked for");
+    if (d_norm && !word_ok(t, d_norm, 4)) return fail(t, FS_E_ARG, "fs_adamw_step: d_norm must be a device pointer");
+    if (!word_ok(t, d_step, 8)) return fail(t, FS_E_ARG, "fs_adamw_step: d_step must be a device pointer");
+    if (h.d_lr && !word_ok(t, h.d_lr, 4)) return fail(t, FS_E_ARG, "fs_adamw_step: d_lr must be a device pointer or NULL");
+    if (!t->params || !t->moments) return fail(t, FS_E_STATE, "fs_adamw_step: tensors without param, exp_avg or exp_avg_sq");
+    if (d_norm && !h.norm_given) launch_norm(t, FS_NORM_TWO, h.grad_scale, d_norm);
+    AdamD A;
+    A.log_beta1 = std::log(h.beta1);
+    A.log_beta2 = std::log(h.beta2);
+    A.max_norm = h.max_norm;
+    A.scale = h.grad_scale;
+    A.lr = (float)h.lr;
+    A.beta1 = (float)h.beta1;
+    A.beta2 = (float)h.beta2;
+    A.rest1 = (float)(1.0 - h.beta1);
+    A.rest2 = (float)(1.0 - h.beta2);
+    A.eps = (float)h.eps;
+    A.decay = (float)h.weight_decay;
+    A.skip_nonfinite = h.skip_nonfinite;
+    k_adamw<<<blocks_for(t), 256, 0, t->stream>>>(t->L, A, h.d_lr, d_norm, reinterpret_cast<long long *>(d_step), t->ticket);
+    return launch_status(t, "fs_adamw_step");
+}
+
+}  // extern "C"

@@ -1,0 +1,321 @@
+"""What a training program does with its gradients, over the C ABI of include/fastsnarf_train.h: the global norm of a list of
+tensors, clipping, and the AdamW step.
+
+    norm = TensorList([p.grad for p in params]).clip_grads(1.0)          # as torch.nn.utils.clip_grad_norm_
+
+    opt = AdamW(params, lr=1e-3, weight_decay=0.01, max_norm=1.0)        # clips inside the step: no gradient is rewritten
+    loss.backward(); norm = opt.step(); opt.zero_grad()
+
+Tensors are float32, bfloat16 or float16 on one GPU, of any size and alignment, dense (any order of dimensions, without
+gaps); moments and masters are float32.  Results stay on the GPU and nothing waits for it.  Calls run on the stream that is current
+when they are made.  Argument marshalling only: the arithmetic runs in the HIP kernels.  There is no CPU fallback.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+from typing import Optional, Sequence
+
+import torch
+
+from . import binding
+
+_TYPES = {torch.float32: binding.FS_FLOAT_FULL, torch.bfloat16: binding.FS_FLOAT_BRAIN, torch.float16: binding.FS_FLOAT_HALF}
+_KINDS = {"l2": binding.FS_NORM_TWO, "max": binding.FS_NORM_MAX}
+
+
+def _dense(t: torch.Tensor) -> bool:
+    """Does the tensor's memory hold its elements one after another, in some order of the dimensions?"""
+    if t.is_contiguous():
+        return True
+    at = 1
+    for stride, size in sorted((st, sz) for st, sz in zip(t.stride(), t.shape) if sz != 1):
+        if stride != at:
+            return False
+        at *= size
+    return True
+
+
+def _order(t: torch.Tensor):
+    return [st for st, sz in zip(t.stride(), t.shape) if sz != 1]
+
+
+def _check(what: str, i: int, t: torch.Tensor, like: Optional[torch.Tensor], device, types):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{what}[{i}]: expected a tensor, got {type(t).__name__}")
+    if t.dtype not in types:
+        raise TypeError(f"{what}[{i}]: {t.dtype} is not supported here, expected {' or '.join(str(k) for k in types)}")
+    if t.device != device:
+        raise ValueError(f"{what}[{i}]: on {t.device}, the list is on {device}")
+    if like is None:
+        if t.layout != torch.strided or not _dense(t):
+            raise ValueError(f"{what}[{i}]: elements must lie one after another in memory (use .contiguous())")
+    elif t.shape != like.shape or (t.numel() and _order(t) != _order(like)):
+        raise ValueError(f"{what}[{i}]: shape {tuple(t.shape)} and strides {t.stride()}, expected {tuple(like.shape)} and {like.stride()}")
+
+
+def _check_apart(arrays):
+    """No two of the arrays may share memory: calls write some of them, block by block in no order."""
+    spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in arrays if t is not None and t.numel())
+    for (_, end), (begin, _) in zip(spans, spans[1:]):
+        if begin < end:
+            raise ValueError("tensors of the list overlap in memory")
+
+
+class _Handle:
+    """An fs_tensors, its host list and its stream.  Holds no tensors."""
+
+    def __init__(self, count: int, device: torch.device):
+        self.L = binding.load()
+        if device.type != "cuda":
+            raise ValueError(f"tensors must be on a GPU, got {device}")
+        self.device = device if device.index is not None else torch.device("cuda", torch.cuda.current_device())
+        self.count = count
+        self.list = (binding.Tensor * max(1, count))()
+        self._h = None
+
+    def put(self):
+        """Hands the list over: the first time, or after it has changed."""
+        if self._h is not None:
+            self.on_stream()
+            self.ret(self.L.fs_tensors_update(self._h, self.list, self.count))
+            return
+        h = ctypes.c_void_p()
+        with torch.cuda.device(self.device):
+            self._stream = torch.cuda.current_stream(self.device)
+            self._raw = self._stream.cuda_stream
+            st = self.L.fs_tensors_create(self.list, self.count, self._raw, ctypes.byref(h))
+        if st != binding.FS_OK:
+            raise binding.FsError(st, "fs_tensors_create failed")
+        self._h = h
+
+    def ret(self, st):
+        if st != binding.FS_OK:
+            raise binding.FsError(st, self.L.fs_tensors_error(self._h).decode())
+
+    def on_stream(self):
+        now = torch.cuda.current_stream(self.device)
+        if now.cuda_stream != self._raw:
+            # the list's scratch is one: this stream's calls come after those of the stream before.  A stream that records a graph cannot wait
+            # for work outside of it; torch.cuda.graph waits for the whole device before it records.
+            if not torch.cuda.is_current_stream_capturing():
+                now.wait_stream(self._stream)
+            self._stream, self._raw = now, now.cuda_stream
+            self.ret(self.L.fs_tensors_set_stream(self._h, self._raw))
+
+    def norm(self, norm):
+        """Where a call's norm goes or comes from."""
+        if norm is None:
+            return torch.empty(1, dtype=torch.float32, device=self.device)
+        _check("norm", 0, norm, None, self.device, [torch.float32])
+        if norm.numel() != 1:
+            raise ValueError("norm must have one element")
+        return norm
+
+    def __del__(self):
+        try:
+            if self._h is not None:
+                self.L.fs_tensors_destroy(self._h)
+                self._h = None
+        except Exception:
+            pass
+
+
+def _lists(n: int, **lists):
+    """Every argument as a list of n entries."""
+    out = []
+    for name, v in lists.items():
+        v = [None] * n if v is None else list(v)
+        if len(v) != n:
+            raise ValueError(f"{name}: {len(v)} entries, expected {n}")
+        out.append(v)
+    return out
+
+
+def _device_of(tensors, device=None) -> torch.device:
+    some = next((t for t in tensors if isinstance(t, torch.Tensor)), None)
+    return torch.device(device) if device is not None else some.device if some is not None else torch.device("cuda")
+
+
+def _places(tensors):
+    return [0 if t is None else t.data_ptr() for t in tensors]
+
+
+class TensorList:
+    """A list of gradients, and where their clipped values go (`outs`; without: in place).  Entries of `grads` may be None: they
+    are left out.  The list keeps references to the tensors, and notices when their memory has moved."""
+
+    def __init__(self, grads: Sequence[Optional[torch.Tensor]], outs: Optional[Sequence[Optional[torch.Tensor]]] = None, device=None):
+        self._grads = list(grads)
+        (self._outs,) = _lists(len(self._grads), outs=outs)
+        self._handle = _Handle(len(self._grads), _device_of(self._grads, device))
+        self._written = [o if o is not None else g for o, g in zip(self._outs, self._grads) if g is not None]
+        self._watched = self._grads + [o for o in self._outs if o is not None]
+        self._places = None
+        self._put()
+
+    def _put(self):
+        h = self._handle
+        for i, (g, o) in enumerate(zip(self._grads, self._outs)):
+            e = h.list[i]
+            e.n = 0
+            if g is None:
+                continue
+            _check("grads", i, g, None, h.device, _TYPES)
+            if o is not None:
+                _check("outs", i, o, g, h.device, [g.dtype])
+            e.grad, e.out, e.n, e.grad_type = g.data_ptr(), None if o is None else o.data_ptr(), g.numel(), _TYPES[g.dtype]
+        _check_apart(self._grads + [o for o, g in zip(self._outs, self._grads) if o is not None and g is not None and o.data_ptr() != g.data_ptr()])
+        self._places = None
+        h.put()
+        self._places = _places(self._watched)
+
+    def _ready(self):
+        if _places(self._watched) != self._places:
+            self._put()
+        self._handle.on_stream()
+
+    def grad_norm(self, kind: str = "l2", grad_scale: float = 1.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Global norm of the gradients times grad_scale, float32 [1]: "l2", or "max", the largest magnitude."""
+        h = self._handle
+        out = h.norm(out)
+        self._ready()
+        h.ret(h.L.fs_grad_norm(h._h, _kind(kind), grad_scale, out.data_ptr()))
+        return out
+
+    def clip_grads(self, max_norm: float, kind: str = "l2", grad_scale: float = 1.0, norm: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Gradients times grad_scale min(1, max_norm / (norm + 1e-6)).  Returns the norm; one that is given (of gradients that are
+        spread over several GPUs, say) is taken as it is."""
+        h = self._handle
+        d = h.norm(norm)
+        self._ready()
+        h.ret(h.L.fs_grad_clip(h._h, _kind(kind), max_norm, grad_scale, norm is not None, d.data_ptr()))
+        torch.autograd.graph.increment_version(self._written)
+        return d
+
+
+class AdamW:
+    """AdamW with decoupled weight decay over a list of parameters, one or two launches a step whatever their number.
+
+      params       float32, bfloat16 or float16 tensors on one GPU
+      grads        their gradients; without: each parameter's .grad at the time of the step (None: the parameter stays as it is)
+      lr           a number, or a float32 tensor of one element on the GPU that is read at every step (a schedule under graph capture)
+      max_norm     limit of the gradients' global 2-norm; None: no clipping
+      grad_scale   factor on all gradients before anything else (the inverse of a loss scale)
+      skip_nonfinite  a step whose norm is NaN or infinite changes nothing but the norm, and is not counted
+      masters      True: 16-bit parameters get float32 masters, which are what is updated; or a list (None: no master)
+      lr_scales, decay_scales   factors per parameter on lr and weight_decay
+      exp_avgs, exp_avg_sqs, step   state to go on from: float32 tensors like the parameters, and an int64 tensor of one element
+
+    State: .masters, .exp_avgs, .exp_avg_sqs, .step_count (updated in place), see state_dict()."""
+
+    def __init__(self, params: Sequence[torch.Tensor], grads=None, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2,
+                 max_norm: Optional[float] = None, grad_scale: float = 1.0, skip_nonfinite: bool = False, masters=None, lr_scales=None,
+                 decay_scales=None, exp_avgs=None, exp_avg_sqs=None, step: Optional[torch.Tensor] = None):
+        self.params = list(params)
+        n = len(self.params)
+        h = self._handle = _Handle(n, _device_of(self.params))
+        self.lr, self.betas, self.eps, self.weight_decay = lr, betas, eps, weight_decay
+        self.max_norm, self.grad_scale, self.skip_nonfinite = max_norm, grad_scale, skip_nonfinite
+        for i, p in enumerate(self.params):
+            _check("params", i, p, None, h.device, _TYPES)
+        if masters is True:
+            masters = [p.detach().to(torch.float32, memory_format=torch.preserve_format) if p.dtype != torch.float32 else None for p in self.params]
+        zeros = lambda: [torch.zeros_like(p, dtype=torch.float32, memory_format=torch.preserve_format, requires_grad=False) for p in self.params]
+        (self.masters,) = _lists(n, masters=masters or None)
+        self.exp_avgs, self.exp_avg_sqs = _lists(n, exp_avgs=zeros() if exp_avgs is None else exp_avgs, exp_avg_sqs=zeros() if exp_avg_sqs is None else exp_avg_sqs)
+        self._lr_scales, self._decay_scales = _lists(n, lr_scales=[1.0] * n if lr_scales is None else lr_scales,
+                                                     decay_scales=[1.0] * n if decay_scales is None else decay_scales)
+        for name, v in (("masters", self.masters), ("exp_avgs", self.exp_avgs), ("exp_avg_sqs", self.exp_avg_sqs)):
+            for i, (t, p) in enumerate(zip(v, self.params)):
+                if t is not None or name != "masters":
+                    _check(name, i, t, p, h.device, [torch.float32])
+        self.step_count = step if step is not None else torch.zeros(1, dtype=torch.int64, device=h.device)
+        _check("step", 0, self.step_count, None, h.device, [torch.int64])
+        if self.step_count.numel() != 1:
+            raise ValueError("step must have one element")
+        self._given = None
+        if grads is not None:
+            (self._given,) = _lists(n, grads=grads)
+        self._state = [t for t in self.masters + self.exp_avgs + self.exp_avg_sqs if t is not None]
+        self._written = self.params + self._state
+        _check_apart(self._written + (self._given or []))
+        self._straight = [p.is_contiguous() for p in self.params]
+        self._places = None
+        self._how = binding.AdamW()
+
+    def _put(self, grads, now):
+        h = self._handle
+        for i, (g, p) in enumerate(zip(grads, self.params)):
+            e = h.list[i]
+            e.n, e.lr_scale, e.decay_scale = 0, float(self._lr_scales[i]), float(self._decay_scales[i])
+            if g is None:
+                continue
+            _check("grads", i, g, p, h.device, _TYPES)
+            w = self.masters[i]
+            e.grad, e.param, e.master = g.data_ptr(), p.data_ptr(), None if w is None else w.data_ptr()
+            e.exp_avg, e.exp_avg_sq = self.exp_avgs[i].data_ptr(), self.exp_avg_sqs[i].data_ptr()
+            e.n, e.grad_type, e.param_type = p.numel(), _TYPES[g.dtype], _TYPES[p.dtype]
+        self._places = None
+        h.put()
+        self._places = now
+
+    @staticmethod
+    def _alike(g, p, straight):
+        return g is None or (g.dtype == p.dtype and (g.is_contiguous() if straight else _order(g) == _order(p)))
+
+    def step(self, norm: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+        """One step.  Returns the gradients' global norm, float32 [1] (None where neither max_norm nor skip_nonfinite asks for it); a
+        `norm` that is given is taken as it is (one over several GPUs, say)."""
+        h, how = self._handle, self._how
+        grads = self._given if self._given is not None else [p.grad for p in self.params]
+        now = _places(grads) + _places(self.params)
+        # gradients that are not held here may have been replaced by others at the same place
+        if now != self._places or (self._given is None and not all(self._alike(g, p, s) for g, p, s in zip(grads, self.params, self._straight))):
+            self._put(grads, now)
+        h.on_stream()
+        asked = norm is not None or self.max_norm is not None or self.skip_nonfinite
+        d = h.norm(norm) if asked else None
+        if isinstance(self.lr, torch.Tensor):
+            _check("lr", 0, self.lr, None, h.device, [torch.float32])
+            how.lr, how.d_lr = 0.0, self.lr.data_ptr()
+        else:
+            how.lr, how.d_lr = self.lr, None
+        how.beta1, how.beta2 = self.betas
+        how.eps, how.weight_decay, how.grad_scale = self.eps, self.weight_decay, self.grad_scale
+        how.max_norm = math.inf if self.max_norm is None else self.max_norm
+        how.norm_given, how.skip_nonfinite = norm is not None, bool(self.skip_nonfinite)
+        h.ret(h.L.fs_adamw_step(h._h, ctypes.byref(how), self.step_count.data_ptr(), d.data_ptr() if asked else None))
+        torch.autograd.graph.increment_version(self._written)
+        return d
+
+    def zero_grad(self, set_to_none: bool = False):
+        """Gradients to zero, in the memory that they have; or away with them (the next step then finds others)."""
+        grads = [g for g in (self._given if self._given is not None else [p.grad for p in self.params]) if g is not None]
+        if set_to_none and self._given is None:
+            for p in self.params:
+                p.grad = None
+        elif grads:
+            torch._foreach_zero_(grads)
+
+    def state_dict(self):
+        return {"step": self.step_count, "masters": self.masters, "exp_avgs": self.exp_avgs, "exp_avg_sqs": self.exp_avg_sqs}
+
+    def load_state_dict(self, state):
+        """Copies a state in; the parameters are the caller's to load."""
+        new = [state["masters"], state["exp_avgs"], state["exp_avg_sqs"]]
+        for name, mine, theirs in zip(("masters", "exp_avgs", "exp_avg_sqs"), (self.masters, self.exp_avgs, self.exp_avg_sqs), new):
+            if len(theirs) != len(mine) or any((a is None) != (b is None) or (a is not None and a.shape != b.shape) for a, b in zip(mine, theirs)):
+                raise ValueError(f"{name} do not fit")
+        with torch.no_grad():
+            for mine, theirs in zip((self.masters, self.exp_avgs, self.exp_avg_sqs), new):
+                for a, b in zip(mine, theirs):
+                    if a is not None:
+                        a.copy_(b)
+            self.step_count.copy_(state["step"])
+
+
+def _kind(kind):
+    if kind not in _KINDS:
+        raise ValueError(f"kind must be one of {', '.join(_KINDS)}, got {kind!r}")
+    return _KINDS[kind]
