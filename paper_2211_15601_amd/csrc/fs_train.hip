@@ -22,9 +22,9 @@ struct fs_tensors {
     // what the tensors as a whole have
     bool params, moments;
     ListD L;
-    char *mem;                // device: TensorD [asked], int [asked + 1], double [TRAIN_BLOCKS], ticket
+    char *mem;                // device: TensorD [asked], int [asked + 1], double [TRAIN_BLOCKS], unsigned [TICKETS]
     double *partial;
-    unsigned *ticket;
+    unsigned *tickets;
     const void *seen[8];      // words (d_norm, d_step, d_lr) that are known to be memory of the device, by address
     char err[256];
 };
@@ -171,8 +171,8 @@ int blocks_for(const fs_tensors *t) { return std::max(1, std::min(t->L.units, 8 
 
 void launch_norm(fs_tensors *t, int32_t kind, double scale, float *d_norm)
 {
-    if (kind == FS_NORM_TWO) k_norm<KIND_TWO><<<blocks_for(t), 256, 0, t->stream>>>(t->L, scale, t->partial, t->ticket, d_norm);
-    else k_norm<KIND_MAX><<<blocks_for(t), 256, 0, t->stream>>>(t->L, scale, t->partial, t->ticket, d_norm);
+    if (kind == FS_NORM_TWO) k_norm<KIND_TWO><<<blocks_for(t), 256, 0, t->stream>>>(t->L, scale, t->partial, t->tickets, d_norm);
+    else k_norm<KIND_MAX><<<blocks_for(t), 256, 0, t->stream>>>(t->L, scale, t->partial, t->tickets, d_norm);
 }
 
 bool scale_ok(double s) { return s > 0.0 && std::isfinite(s); }
@@ -207,9 +207,9 @@ fs_status fs_tensors_create(const fs_tensor *list, int32_t count, void *hip_stre
         if (hipDeviceGetAttribute(&t->n_cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || t->n_cus < 1) t->n_cus = 256;
         (void)hipGetLastError();
         t->n_cus = std::min(t->n_cus, TRAIN_BLOCKS / 8);
-        const size_t at_first = (size_t)count * sizeof(TensorD), at_partial = (at_first + ((size_t)count + 1) * sizeof(int) + 15) / 16 * 16;
-        const size_t at_ticket = at_partial + TRAIN_BLOCKS * sizeof(double);
-        if (hipMalloc(reinterpret_cast<void **>(&t->mem), at_ticket + 16) != hipSuccess) {
+        const size_t at_first = (size_t)count * sizeof(TensorD), at_partial = (at_first + ((size_t)count + 1) * sizeof(int) + 255) / 256 * 256;
+        const size_t at_tickets = at_partial + TRAIN_BLOCKS * sizeof(double);
+        if (hipMalloc(reinterpret_cast<void **>(&t->mem), at_tickets + TICKETS * sizeof(unsigned)) != hipSuccess) {
             (void)hipGetLastError();
             t->mem = nullptr;
             s = FS_E_ALLOC;
@@ -217,8 +217,8 @@ fs_status fs_tensors_create(const fs_tensor *list, int32_t count, void *hip_stre
             t->L.tensors = reinterpret_cast<TensorD *>(t->mem);
             t->L.first = reinterpret_cast<int *>(t->mem + at_first);
             t->partial = reinterpret_cast<double *>(t->mem + at_partial);
-            t->ticket = reinterpret_cast<unsigned *>(t->mem + at_ticket);
-            k_ticket_clear<<<1, 64, 0, t->stream>>>(t->ticket);
+            t->tickets = reinterpret_cast<unsigned *>(t->mem + at_tickets);
+            k_tickets_clear<<<1, 256, 0, t->stream>>>(t->tickets);
             s = put_list(t, "fs_tensors_create", list);
         }
     }
@@ -315,7 +315,7 @@ fs_status fs_adamw_step(fs_tensors *t, const fs_adamw *how, int64_t *d_step, flo
     A.eps = (float)h.eps;
     A.decay = (float)h.weight_decay;
     A.skip_nonfinite = h.skip_nonfinite;
-    k_adamw<<<blocks_for(t), 256, 0, t->stream>>>(t->L, A, h.d_lr, d_norm, reinterpret_cast<long long *>(d_step), t->ticket);
+    k_adamw<<<blocks_for(t), 256, 0, t->stream>>>(t->L, A, h.d_lr, d_norm, reinterpret_cast<long long *>(d_step), t->tickets);
     return launch_status(t, "fs_adamw_step");
 }
 

@@ -10,6 +10,8 @@ namespace fs {
 
 constexpr int UNIT = 2048;             // elements: 8 per thread
 constexpr int TRAIN_BLOCKS = 4096;     // at most; a partial sum for each
+constexpr int TICKET_GROUPS = 32, TICKET_STRIDE = 64;      // counters of last_block, each on lines of its own
+constexpr int TICKETS = (1 + TICKET_GROUPS) * TICKET_STRIDE;
 
 enum { TYPE_F32, TYPE_BF16, TYPE_F16 };
 enum { KIND_TWO, KIND_MAX };
@@ -43,9 +45,9 @@ __global__ __launch_bounds__(64) void k_list_put(PutD p, int at, int n, int coun
     if (i == 0 && at + n == count) first[count] = units;
 }
 
-__global__ void k_ticket_clear(unsigned *ticket)
+__global__ void k_tickets_clear(unsigned *tickets)
 {
-    if (threadIdx.x == 0) *ticket = 0u;
+    for (int i = threadIdx.x; i < TICKETS; i += blockDim.x) tickets[i] = 0u;
 }
 
 // ---- elements, four or eight at a time, aligned to the element only ----
@@ -141,15 +143,27 @@ __device__ __forceinline__ S block_join(S s)
     return join(join(wave[0], wave[1]), join(wave[2], wave[3]));
 }
 
-// True in every thread of the block that comes last, when all threads of all blocks have come here; `ticket` is 0 between kernels.
-__device__ __forceinline__ bool last_block(unsigned *ticket)
+// True in every thread of the block that comes last, when all threads of all blocks have come here.  Blocks count themselves in groups, the last
+// of a group counts it at the top: one counter serves a block in some 10 ns, so 2048 blocks that end together would stand 20 us in line at a
+// single one.  The counters are 0 between kernels.  What a block leaves for the last one it stores with agent-scope atomics, which go past the caches;
+// they are done when vmcnt is 0.  (A release at agent scope would write the whole L2 back and an acquire drop it, some 25 ns a block of 50 us in all.)
+__device__ __forceinline__ unsigned count_in(unsigned *counter, unsigned of)
 {
-    __shared__ bool last;
+    const unsigned before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (before != of - 1) return 0;
+    __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return 1;
+}
+
+__device__ __forceinline__ bool last_block(unsigned *tickets)
+{
+    __shared__ unsigned last;
     __syncthreads();
     if (threadIdx.x == 0) {
-        const unsigned before = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-        last = before == gridDim.x - 1;
-        if (last) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        const unsigned groups = min((unsigned)TICKET_GROUPS, gridDim.x), mine = blockIdx.x % groups;
+        last = count_in(tickets + (1 + mine) * TICKET_STRIDE, (gridDim.x - mine + groups - 1) / groups);
+        if (last) last = count_in(tickets, groups);
     }
     __syncthreads();
     return last;
@@ -189,7 +203,7 @@ __device__ __forceinline__ S sum_range(Global<T> g, long long begin, long long e
 }
 
 template <int KIND>
-__global__ __launch_bounds__(256) void k_norm(ListD L, double scale, double *__restrict__ partial, unsigned *__restrict__ ticket, float *__restrict__ norm)
+__global__ __launch_bounds__(256) void k_norm(ListD L, double scale, double *__restrict__ partial, unsigned *__restrict__ tickets, float *__restrict__ norm)
 {
     using S = typename Sum<KIND>::type;
     S s = 0;
@@ -203,7 +217,7 @@ __global__ __launch_bounds__(256) void k_norm(ListD L, double scale, double *__r
     s = block_join(s);
     S *part = reinterpret_cast<S *>(partial);
     if (threadIdx.x == 0) __hip_atomic_store(part + blockIdx.x, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (!last_block(ticket)) return;
+    if (!last_block(tickets)) return;
     s = 0;
     for (unsigned i = threadIdx.x; i < gridDim.x; i += 256) s = join(s, __hip_atomic_load(part + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
     s = block_join(s);
@@ -344,7 +358,7 @@ __device__ __forceinline__ void adam_types(const TensorD &t, long long begin, lo
 }
 
 __global__ __launch_bounds__(256) void k_adamw(ListD L, AdamD A, const float *__restrict__ lr, const float *__restrict__ norm,
-                                               long long *__restrict__ steps, unsigned *__restrict__ ticket)
+                                               long long *__restrict__ steps, unsigned *__restrict__ tickets)
 {
     if (A.skip_nonfinite && !(__builtin_fabsf(*norm) < __builtin_inff())) return;      // every block sees the same norm
     const long long before = *steps;
@@ -362,7 +376,7 @@ __global__ __launch_bounds__(256) void k_adamw(ListD L, AdamD A, const float *__
         }
     });
     // the counter moves on when every block has read it
-    if (last_block(ticket) && threadIdx.x == 0) *steps = before + 1;
+    if (last_block(tickets) && threadIdx.x == 0) *steps = before + 1;
 }
 
 }  // namespace fs
