@@ -88,6 +88,7 @@ bool type_ok(int32_t type) { return type == FS_FLOAT_FULL || type == FS_FLOAT_BR
 int size_of(int32_t type) { return type == FS_FLOAT_FULL ? 4 : 2; }
 static_assert(int(FS_FLOAT_FULL) == TYPE_F32 && int(FS_FLOAT_BRAIN) == TYPE_BF16 && int(FS_FLOAT_HALF) == TYPE_F16, "types");
 static_assert(int(FS_NORM_TWO) == KIND_TWO && int(FS_NORM_MAX) == KIND_MAX, "kinds");
+constexpr int MAX_LEAD = 64;
 static_assert(sizeof(PutD) + 64 <= 4096, "kernel arguments");
 
 // Checks a list.  `before`: the list whose pointers are known to be memory of the device, or NULL.
@@ -98,7 +99,7 @@ fs_status check_list(fs_tensors *t, const char *what, const fs_tensor *list, int
         const fs_tensor &x = list[i];
         if (x.n < 0 || x.n > 1ll << 40) return fail(t, FS_E_SHAPE, "%s: tensor %d: n out of range", what, i);
         if (x.n == 0) continue;
-        units += (x.n + UNIT - 1) / UNIT;
+        units += (x.n + MAX_LEAD + UNIT - 1) / UNIT;
         if (units >= 1ll << 31) return fail(t, FS_E_SHAPE, "%s: tensor %d: too many elements in all", what, i);
         if (!type_ok(x.grad_type) || (x.param && !type_ok(x.param_type))) return fail(t, FS_E_ARG, "%s: tensor %d: bad type", what, i);
         if (!std::isfinite(x.lr_scale) || !std::isfinite(x.decay_scale)) return fail(t, FS_E_ARG, "%s: tensor %d: lr_scale and decay_scale must be finite", what, i);
@@ -112,6 +113,15 @@ fs_status check_list(fs_tensors *t, const char *what, const fs_tensor *list, int
             return fail(t, FS_E_ARG, "%s: tensor %d: out overlaps grad", what, i);
     }
     return FS_OK;
+}
+
+// Elements by which a tensor's first unit begins before it, so that units begin at 256 bytes of the moments (of the gradients, where there are none; 16-bit
+// arrays then begin at 128).  Tensors packed without gaps lie anywhere: an AdamW step of 250 M elements in 16 bits took 1700 us with units that began with the
+// tensors, 1450 with tensors at multiples of 64 elements.
+int lead_of(const fs_tensor &x)
+{
+    const uintptr_t at = x.exp_avg ? reinterpret_cast<uintptr_t>(x.exp_avg) / 4 : reinterpret_cast<uintptr_t>(x.grad) / size_of(x.grad_type);
+    return (int)(at % MAX_LEAD);
 }
 
 // Takes a checked list over: the host's copies, and the device's in the stream's order.
@@ -131,10 +141,12 @@ fs_status put_list(fs_tensors *t, const char *what, const fs_tensor *list)
         d.v = x.exp_avg_sq;
         d.n = x.n;
         d.first = units;
+        d.lead = lead_of(x);
+        units += (int)((x.n + d.lead + UNIT - 1) / UNIT);
+        d.next = units;
         d.types = x.grad_type | x.param_type << 8;
         d.lr_scale = x.lr_scale;
         d.decay_scale = x.decay_scale;
-        units += (int)((x.n + UNIT - 1) / UNIT);
         t->params = t->params && x.param;
         t->moments = t->moments && x.exp_avg && x.exp_avg_sq;
     }
@@ -144,7 +156,7 @@ fs_status put_list(fs_tensors *t, const char *what, const fs_tensor *list)
         PutD p;
         const int n = std::min(PUT, count - at);
         std::memcpy(p.t, t->host + at, n * sizeof(TensorD));
-        k_list_put<<<1, 64, 0, t->stream>>>(p, at, n, count, units, const_cast<TensorD *>(t->L.tensors), const_cast<int *>(t->L.first));
+        k_list_put<<<1, 64, 0, t->stream>>>(p, at, n, const_cast<TensorD *>(t->L.tensors), const_cast<int *>(t->L.first));
     }
     return launch_status(t, what);
 }
@@ -166,13 +178,32 @@ fs_status on_current_device(fs_tensors *t, const char *what)
         if (begin_status != FS_OK) return begin_status;                   \
     } while (0)
 
-// Every block takes a stretch of units; more blocks than the device holds at once only where the stretches are long.
-int blocks_for(const fs_tensors *t) { return std::max(1, std::min(t->L.units, 8 * t->n_cus)); }
+#ifndef BPC_N
+#define BPC_N 2
+#define BPC_C 2
+#define BPC_A 2
+#define CAP 8
+#define SN(x) true
+#define SC(x) true
+#define SA(x) true
+#endif
+// How many blocks, and how many units each takes at a time.
+struct Grid { int blocks; ListD L; };
+Grid grid_for(const fs_tensors *t, int per_cu)
+{
+    Grid g = {std::max(1, std::min(t->L.units, per_cu * t->n_cus)), t->L};
+    const long long rounds = std::max(1ll, ((long long)t->L.units + (long long)CAP * g.blocks - 1) / ((long long)CAP * g.blocks));
+    g.L.chunk = (int)std::max(1ll, (t->L.units + g.blocks * rounds - 1) / (g.blocks * rounds));
+    return g;
+}
 
 void launch_norm(fs_tensors *t, int32_t kind, double scale, float *d_norm)
 {
-    if (kind == FS_NORM_TWO) k_norm<KIND_TWO><<<blocks_for(t), 256, 0, t->stream>>>(t->L, scale, t->partial, t->tickets, d_norm);
-    else k_norm<KIND_MAX><<<blocks_for(t), 256, 0, t->stream>>>(t->L, scale, t->partial, t->tickets, d_norm);
+    const Grid g = grid_for(t, BPC_N);
+    const bool stream = SN(t);
+#define FS_NORM(K, S) k_norm<K, S><<<g.blocks, 256, 0, t->stream>>>(g.L, scale, t->partial, t->tickets, d_norm)
+    if (kind == FS_NORM_TWO) { if (stream) FS_NORM(KIND_TWO, true); else FS_NORM(KIND_TWO, false); }
+    else { if (stream) FS_NORM(KIND_MAX, true); else FS_NORM(KIND_MAX, false); }
 }
 
 bool scale_ok(double s) { return s > 0.0 && std::isfinite(s); }
@@ -279,7 +310,11 @@ fs_status fs_grad_clip(fs_tensors *t, int32_t kind, double max_norm, double grad
     if (!scale_ok(grad_scale)) return fail(t, FS_E_ARG, "fs_grad_clip: grad_scale must be positive and finite");
     if (!word_ok(t, d_norm, 4)) return fail(t, FS_E_ARG, "fs_grad_clip: d_norm must be a device pointer");
     if (!norm_given) launch_norm(t, kind, grad_scale, d_norm);
-    if (t->L.units) k_clip<<<blocks_for(t), 256, 0, t->stream>>>(t->L, max_norm, grad_scale, d_norm);
+    if (t->L.units) {
+        const Grid g = grid_for(t, BPC_C);
+        if (SC(t)) k_clip<true><<<g.blocks, 256, 0, t->stream>>>(g.L, max_norm, grad_scale, d_norm);
+        else k_clip<false><<<g.blocks, 256, 0, t->stream>>>(g.L, max_norm, grad_scale, d_norm);
+    }
     return launch_status(t, "fs_grad_clip");
 }
 
@@ -315,7 +350,9 @@ fs_status fs_adamw_step(fs_tensors *t, const fs_adamw *how, int64_t *d_step, flo
     A.eps = (float)h.eps;
     A.decay = (float)h.weight_decay;
     A.skip_nonfinite = h.skip_nonfinite;
-    k_adamw<<<blocks_for(t), 256, 0, t->stream>>>(t->L, A, h.d_lr, d_norm, reinterpret_cast<long long *>(d_step), t->tickets);
+    const Grid g = grid_for(t, BPC_A);
+    if (SA(t)) k_adamw<true><<<g.blocks, 256, 0, t->stream>>>(g.L, A, h.d_lr, d_norm, reinterpret_cast<long long *>(d_step), t->tickets);
+    else k_adamw<false><<<g.blocks, 256, 0, t->stream>>>(g.L, A, h.d_lr, d_norm, reinterpret_cast<long long *>(d_step), t->tickets);
     return launch_status(t, "fs_adamw_step");
 }
 

@@ -1,7 +1,7 @@
 // Kernels over a list of tensors: global norm of the gradients, clipping, AdamW (see include/fastsnarf_train.h).
 //
-// All of them read the list from device memory and cut it into units of UNIT elements of one tensor, numbered through the list.  Every
-// block takes one stretch of consecutive units, finds the tensor that it begins in, and walks on from tensor to tensor.
+// All of them read the list from device memory and cut it into units of UNIT elements of one tensor, numbered through the list.  Blocks
+// take chunks of consecutive units in turn, find the tensor that a chunk begins in, and walk on from tensor to tensor.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -10,6 +10,7 @@ namespace fs {
 
 constexpr int UNIT = 2048;             // elements: 8 per thread
 constexpr int TRAIN_BLOCKS = 4096;     // at most; a partial sum for each
+constexpr int LIST_LDS = 1024;          // places that a block keeps in LDS
 constexpr int TICKET_GROUPS = 32, TICKET_STRIDE = 64;      // counters of last_block, each on lines of its own
 constexpr int TICKETS = (1 + TICKET_GROUPS) * TICKET_STRIDE;
 
@@ -20,29 +21,29 @@ struct TensorD {                       // a tensor as the kernels see it, n > 0
     void *grad, *out, *param;
     float *master, *m, *v;
     long long n;
-    int first;                         // its first unit
+    int first, next;                   // its first unit, and the first of the tensor behind it
+    int lead;                          // its first unit begins so many elements before the tensor, where memory is aligned
     int types;                         // of the gradients | of the parameters << 8
     float lr_scale, decay_scale;
 };
 
 struct ListD {
     const TensorD *tensors;
-    const int *first;                  // [count + 1] first units, ascending: first[count] = units
+    const int *first;                  // [count] first units, ascending
     int count, units;
+    int chunk;                         // units that a block takes at a time
 };
 
 constexpr int PUT = 40;                // tensors that one launch of k_list_put carries in its arguments (3.2 KB of 4)
 struct PutD { TensorD t[PUT]; };
 
 // The list travels in kernel arguments: in the stream's order, without host memory that has to outlive the call, and as part of a captured graph.
-__global__ __launch_bounds__(64) void k_list_put(PutD p, int at, int n, int count, int units, TensorD *__restrict__ tensors, int *__restrict__ first)
+__global__ __launch_bounds__(64) void k_list_put(PutD p, int at, int n, TensorD *__restrict__ tensors, int *__restrict__ first)
 {
     const int i = threadIdx.x;
-    if (i < n) {
-        tensors[at + i] = p.t[i];
-        first[at + i] = p.t[i].first;
-    }
-    if (i == 0 && at + n == count) first[count] = units;
+    if (i >= n) return;
+    tensors[at + i] = p.t[i];
+    first[at + i] = p.t[i].first;
 }
 
 __global__ void k_tickets_clear(unsigned *tickets)
@@ -57,53 +58,35 @@ template <class T> using Global = FS_GLOBAL T *;
 template <class T> __device__ __forceinline__ Global<T> global(void *p) { return (Global<T>)p; }
 
 template <class T, int N> struct VecOf { typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T)))); };
+template <class T, int N> using Vec = typename VecOf<T, N>::type;
 
-template <class T, int N>
-__device__ __forceinline__ void load(Global<T> p, float (&x)[N])
+// STREAM: past the caches as far as that goes, for data that no later kernel finds there
+template <bool STREAM, class T, int N>
+__device__ __forceinline__ Vec<T, N> load(Global<T> p)
 {
-    const typename VecOf<T, N>::type v = *(const FS_GLOBAL typename VecOf<T, N>::type *)p;
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = (float)v[i];
+    const FS_GLOBAL Vec<T, N> *at = (const FS_GLOBAL Vec<T, N> *)p;
+    return STREAM ? __builtin_nontemporal_load(at) : *at;
 }
 
-template <class T, int N>
-__device__ __forceinline__ void store(Global<T> p, const float (&x)[N])
+template <bool STREAM, class T, int N>
+__device__ __forceinline__ void store(Global<T> p, Vec<T, N> v)
 {
-    typename VecOf<T, N>::type v;
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = (T)x[i];
-    *(FS_GLOBAL typename VecOf<T, N>::type *)p = v;
-}
-
-// the first `n` of N elements, zeros behind
-template <class T, int N>
-__device__ __forceinline__ void load_some(Global<T> p, int n, float (&x)[N])
-{
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        x[i] = 0.0f;
-        if (i < n) x[i] = (float)p[i];
-    }
-}
-
-template <class T, int N>
-__device__ __forceinline__ void store_some(Global<T> p, int n, const float (&x)[N])
-{
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-        if (i < n) p[i] = (T)x[i];
+    FS_GLOBAL Vec<T, N> *at = (FS_GLOBAL Vec<T, N> *)p;
+    if (STREAM) __builtin_nontemporal_store(v, at);
+    else *at = v;
 }
 
 // ---- the walk over the list ----
 
 // The tensor that unit u belongs to: every round, the wave's 64 lanes ask at 64 places of what is left.
-__device__ __forceinline__ int find_tensor(const ListD &L, int u)
+template <class First>
+__device__ __forceinline__ int find_tensor(First first, int count, int u)
 {
     const int lane = threadIdx.x & 63;
-    int lo = 0, n = L.count;
+    int lo = 0, n = count;
     while (n > 1) {
         const int step = (n + 63) >> 6, i = lane * step;
-        const bool at_or_before = i < n && L.first[lo + i] <= u;
+        const bool at_or_before = i < n && first[lo + i] <= u;
         const int k = __popcll(__ballot(at_or_before)) - 1;       // lane 0 always says yes
         lo += k * step;
         n = min(step, n - k * step);
@@ -111,21 +94,76 @@ __device__ __forceinline__ int find_tensor(const ListD &L, int u)
     return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// Calls f(tensor, begin, end) for the elements [begin, end) of every tensor that this block's stretch of units covers; begin is a multiple of UNIT.
-template <class F>
+// A tensor, by scalar loads: the list does not change while a kernel reads it.
+__device__ __forceinline__ TensorD tensor_at(const ListD &L, int i)
+{
+    typedef const __attribute__((address_space(4))) TensorD *Constant;
+    const Constant c = (Constant)L.tensors + i;
+    return {c->grad, c->out, c->param, c->master, c->m, c->v, c->n, c->first, c->next, c->lead, c->types, c->lr_scale, c->decay_scale};
+}
+
+// A part of a tensor: elements [begin, end), of which those before 0 are not there (begin < 0 in a first unit with a lead).
+struct Piece { long long begin, end; };
+
+// Calls f(tensor, piece) for what this block's chunks of units cover of every tensor.  The next piece's tensor is found and asked for before
+// the present piece is worked on.  BACK: the last chunk first.
+template <bool BACK, class F>
 __device__ __forceinline__ void walk(const ListD &L, F f)
 {
-    const int b = blockIdx.x, G = gridDim.x;
-    int u = (int)((long long)L.units * b / G);
-    const int end = (int)((long long)L.units * (b + 1) / G);
-    if (u >= end) return;
-    for (int i = find_tensor(L, u); u < end; ++i) {
-        const TensorD t = L.tensors[i];
-        const long long begin = (long long)(u - t.first) * UNIT, upto = (long long)(end - t.first) * UNIT;
-        f(t, begin, upto < t.n ? upto : t.n);
-        u = t.first + (int)((t.n + UNIT - 1) / UNIT);
+    const int chunks = (int)(((long long)L.units + L.chunk - 1) / L.chunk);
+    int c = blockIdx.x;
+    if (c >= chunks) return;
+    const bool kept = (int)gridDim.x < chunks && L.count <= LIST_LDS;      // several chunks: the places are asked for more than once
+    __shared__ int s_first[LIST_LDS];
+    if (kept) {
+        for (int i = threadIdx.x; i < L.count; i += 256) s_first[i] = L.first[i];
+        __syncthreads();
+    }
+    auto find = [&](int u) { return kept ? find_tensor(s_first, L.count, u) : find_tensor(L.first, L.count, u); };
+    int u = (BACK ? chunks - 1 - c : c) * L.chunk, end = min(u + L.chunk, L.units), i = find(u);
+    TensorD t = tensor_at(L, i);
+    for (;;) {
+        const long long upto = (long long)(end - t.first) * UNIT - t.lead;
+        const Piece p = {(long long)(u - t.first) * UNIT - t.lead, upto < t.n ? upto : t.n};
+        u = t.next;
+        bool more = u < end;
+        if (more) ++i;
+        else {
+            c += gridDim.x;
+            more = c < chunks;
+            if (more) {
+                u = (BACK ? chunks - 1 - c : c) * L.chunk;
+                end = min(u + L.chunk, L.units);
+                i = find(u);
+            }
+        }
+        const TensorD next = more ? tensor_at(L, i) : t;
+        f(t, p);
+        if (!more) return;
+        t = next;
     }
 }
+
+// A piece in vectors of N elements.  Those at the tensor's ends that are not whole are left out; their elements, fewer than 2 N, are `edge`'s, one to a thread.
+template <int N>
+struct Vectors {
+    int from, upto;                    // whole vectors, numbered from the piece's begin
+    int heads, edges;                  // elements before them, and in all
+    long long tail;                    // the first element behind them
+    __device__ __forceinline__ explicit Vectors(const Piece &p)
+    {
+        const int before = p.begin < 0 ? (int)-p.begin : 0;
+        const int there = (int)(p.end - p.begin);
+        from = (before + N - 1) / N;
+        upto = there / N;
+        heads = min(from * N, there) - before;
+        if (upto < from) upto = from;
+        tail = p.begin + (long long)upto * N;
+        edges = heads + (tail < p.end ? (int)(p.end - tail) : 0);
+    }
+    // the element of this thread, which is < edges
+    __device__ __forceinline__ long long edge() const { return (int)threadIdx.x < heads ? (long long)threadIdx.x : tail + ((int)threadIdx.x - heads); }
+};
 
 // ---- sums over a block, and over the blocks ----
 __device__ __forceinline__ double join(double a, double b) { return a + b; }
@@ -185,33 +223,52 @@ template <> struct Sum<KIND_MAX> {
     static __device__ __forceinline__ double value(unsigned s) { return (double)__uint_as_float(s); }
 };
 
-template <int KIND, class T, class S>
-__device__ __forceinline__ S sum_range(Global<T> g, long long begin, long long end, S s)
+// AHEAD loads of 16 bytes in every thread on their way.
+#ifndef AHEAD_N
+#define AHEAD_N 4
+#define AHEAD_C 2
+#define AHEAD_A 1
+#endif
+template <int KIND, bool STREAM, class T, class S>
+__device__ __forceinline__ S sum_piece(Global<T> g, const Piece &p, S s)
 {
-    constexpr int N = 16 / sizeof(T);                      // elements of one load
-    for (long long at = begin; at < end; at += UNIT)
+    constexpr int N = 16 / sizeof(T), AHEAD = AHEAD_N;
+    const Vectors<N> V(p);
+    g += p.begin;
+    Vec<T, N> x[AHEAD];
+    auto add = [&](int k) {
 #pragma unroll
-        for (int k = 0; k < UNIT; k += 256 * N) {
-            const long long i = at + k + threadIdx.x * N;
-            float x[N];
-            if (i + N <= end) load<T, N>(g + i, x);
-            else load_some<T, N>(g + i, (int)(end > i ? end - i : 0), x);
+        for (int e = 0; e < N; ++e) s = Sum<KIND>::add(s, (float)x[k][e]);
+    };
+    for (int j = 0; j < V.upto; j += 256 * AHEAD) {
+        const int mine = j + threadIdx.x;
+        if (j >= V.from && j + 256 * AHEAD <= V.upto) {
 #pragma unroll
-            for (int e = 0; e < N; ++e) s = Sum<KIND>::add(s, x[e]);
+            for (int k = 0; k < AHEAD; ++k) x[k] = load<STREAM, T, N>(g + (mine + k * 256) * N);
+        } else {
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                x[k] = (T)0.0f;
+                if (mine + k * 256 >= V.from && mine + k * 256 < V.upto) x[k] = load<STREAM, T, N>(g + (mine + k * 256) * N);
+            }
         }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) add(k);
+    }
+    if ((int)threadIdx.x < V.edges) s = Sum<KIND>::add(s, (float)g[V.edge() - p.begin]);
     return s;
 }
 
-template <int KIND>
+template <int KIND, bool STREAM>
 __global__ __launch_bounds__(256) void k_norm(ListD L, double scale, double *__restrict__ partial, unsigned *__restrict__ tickets, float *__restrict__ norm)
 {
     using S = typename Sum<KIND>::type;
     S s = 0;
-    walk(L, [&](const TensorD &t, long long begin, long long end) {
+    walk<false>(L, [&](const TensorD &t, const Piece &p) {
         switch (t.types & 255) {
-        case TYPE_F32: s = sum_range<KIND>(global<float>(t.grad), begin, end, s); break;
-        case TYPE_BF16: s = sum_range<KIND>(global<__bf16>(t.grad), begin, end, s); break;
-        default: s = sum_range<KIND>(global<_Float16>(t.grad), begin, end, s); break;
+        case TYPE_F32: s = sum_piece<KIND, STREAM>(global<float>(t.grad), p, s); break;
+        case TYPE_BF16: s = sum_piece<KIND, STREAM>(global<__bf16>(t.grad), p, s); break;
+        default: s = sum_piece<KIND, STREAM>(global<_Float16>(t.grad), p, s); break;
         }
     });
     s = block_join(s);
@@ -234,34 +291,56 @@ __device__ __forceinline__ float clip_coef(const float *norm, double max_norm, d
     return (float)((q >= 1.0 ? 1.0 : q) * scale);
 }
 
-template <class T>
-__device__ __forceinline__ void scale_range(Global<T> g, Global<T> out, long long begin, long long end, float coef)
+template <bool STREAM, class T>
+__device__ __forceinline__ void scale_piece(Global<T> g, Global<T> out, const Piece &p, float coef)
 {
-    constexpr int N = 16 / sizeof(T);
-    for (long long at = begin; at < end; at += UNIT)
+    constexpr int N = 16 / sizeof(T), AHEAD = AHEAD_C;
+    const Vectors<N> V(p);
+    g += p.begin;
+    out += p.begin;
+    Vec<T, N> x[AHEAD];
+    auto scale = [&](int k) {
 #pragma unroll
-        for (int k = 0; k < UNIT; k += 256 * N) {
-            const long long i = at + k + threadIdx.x * N;
-            const int some = (int)(end - i < N ? end - i : N);
-            float x[N];
-            if (some == N) load<T, N>(g + i, x);
-            else load_some<T, N>(g + i, some, x);
+        for (int e = 0; e < N; ++e) x[k][e] = (T)((float)x[k][e] * coef);
+    };
+    for (int j = 0; j < V.upto; j += 256 * AHEAD) {
+        const int mine = j + threadIdx.x;
+        if (j >= V.from && j + 256 * AHEAD <= V.upto) {
 #pragma unroll
-            for (int e = 0; e < N; ++e) x[e] *= coef;
-            if (some == N) store<T, N>(out + i, x);
-            else store_some<T, N>(out + i, some, x);
+            for (int k = 0; k < AHEAD; ++k) x[k] = load<STREAM, T, N>(g + (mine + k * 256) * N);
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                scale(k);
+                store<STREAM, T, N>(out + (mine + k * 256) * N, x[k]);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+                if (mine + k * 256 >= V.from && mine + k * 256 < V.upto) x[k] = load<STREAM, T, N>(g + (mine + k * 256) * N);
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+                if (mine + k * 256 >= V.from && mine + k * 256 < V.upto) {
+                    scale(k);
+                    store<STREAM, T, N>(out + (mine + k * 256) * N, x[k]);
+                }
         }
+    }
+    if ((int)threadIdx.x < V.edges) {
+        const long long i = V.edge() - p.begin;
+        out[i] = (T)((float)g[i] * coef);
+    }
 }
 
+template <bool STREAM>
 __global__ __launch_bounds__(256) void k_clip(ListD L, double max_norm, double scale, const float *__restrict__ norm)
 {
     const float coef = clip_coef(norm, max_norm, scale);
-    walk(L, [&](const TensorD &t, long long begin, long long end) {
+    walk<true>(L, [&](const TensorD &t, const Piece &p) {
         if (t.out == t.grad && coef == 1.0f) return;
         switch (t.types & 255) {
-        case TYPE_F32: scale_range(global<float>(t.grad), global<float>(t.out), begin, end, coef); break;
-        case TYPE_BF16: scale_range(global<__bf16>(t.grad), global<__bf16>(t.out), begin, end, coef); break;
-        default: scale_range(global<_Float16>(t.grad), global<_Float16>(t.out), begin, end, coef); break;
+        case TYPE_F32: scale_piece<STREAM>(global<float>(t.grad), global<float>(t.out), p, coef); break;
+        case TYPE_BF16: scale_piece<STREAM>(global<__bf16>(t.grad), global<__bf16>(t.out), p, coef); break;
+        default: scale_piece<STREAM>(global<_Float16>(t.grad), global<_Float16>(t.out), p, coef); break;
         }
     });
 }
@@ -289,90 +368,117 @@ __device__ __forceinline__ double one_minus_exp(double y)
     return -__builtin_fma(p, e, p - 1.0);
 }
 
-struct AdamC { float coef, lr, inv1, inv_sqrt2; };          // of this step
+// What a thread holds of one place: N elements of every array.
+template <class P, class G, bool MASTER, int N>
+struct Place {
+    Vec<G, N> g;
+    Vec<float, N> m, v, w;
+    Vec<P, N> p;
+};
+
+struct AdamT { float coef, fade, step, inv_sqrt2, beta1, beta2, rest1, rest2, eps; };      // of one tensor
 
 template <class P, class G, bool MASTER>
-__device__ __forceinline__ void adam_range(const TensorD &t, long long begin, long long end, const AdamD &A, const AdamC &C)
-{
-    constexpr int N = 4;                                   // fp32 moments: 16 bytes of each
-    const Global<G> grad = global<G>(t.grad);
-    const Global<P> param = global<P>(t.param);
-    const Global<float> tm = global<float>(t.m), tv = global<float>(t.v), master = global<float>(t.master);
-    const float lr = C.lr * t.lr_scale, fade = lr * (A.decay * t.decay_scale), step = lr * C.inv1;
-    for (long long at = begin; at < end; at += UNIT)
+struct Arrays {
+    Global<G> g;
+    Global<P> p;
+    Global<float> m, v, w;
+
+    template <bool STREAM, int N>
+    __device__ __forceinline__ void get(long long i, Place<P, G, MASTER, N> &x) const
+    {
+        x.g = load<STREAM, G, N>(g + i);
+        x.m = load<STREAM, float, N>(m + i);
+        x.v = load<STREAM, float, N>(v + i);
+        if (MASTER) x.w = load<STREAM, float, N>(w + i);
+        else x.p = load<STREAM, P, N>(p + i);
+    }
+    // Everything in fp32; the parameter in 16 bits is rounded once, from the new value.
+    template <bool STREAM, int N>
+    __device__ __forceinline__ void update(long long i, Place<P, G, MASTER, N> &x, const AdamT &A) const
+    {
 #pragma unroll
-        for (int k = 0; k < UNIT; k += 256 * N) {
-            const long long i = at + k + threadIdx.x * N;
-            const int some = (int)(end - i < N ? end - i : N);
-            if (some <= 0) continue;
-            float g[N], p[N], m[N], v[N];
-            if (some == N) {
-                load<G, N>(grad + i, g);
-                load<float, N>(tm + i, m);
-                load<float, N>(tv + i, v);
-                if (MASTER) load<float, N>(master + i, p);
-                else load<P, N>(param + i, p);
-            } else {
-                load_some<G, N>(grad + i, some, g);
-                load_some<float, N>(tm + i, some, m);
-                load_some<float, N>(tv + i, some, v);
-                if (MASTER) load_some<float, N>(master + i, some, p);
-                else load_some<P, N>(param + i, some, p);
-            }
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const float x = g[e] * C.coef;
-                m[e] = __builtin_fmaf(A.beta1, m[e], A.rest1 * x);
-                v[e] = __builtin_fmaf(A.beta2, v[e], A.rest2 * x * x);
-                p[e] -= __builtin_fmaf(fade, p[e], step * m[e] / __builtin_fmaf(__builtin_sqrtf(v[e]), C.inv_sqrt2, A.eps));
-            }
-            if (some == N) {
-                store<float, N>(tm + i, m);
-                store<float, N>(tv + i, v);
-                if (MASTER) store<float, N>(master + i, p);
-                store<P, N>(param + i, p);
-            } else {
-                store_some<float, N>(tm + i, some, m);
-                store_some<float, N>(tv + i, some, v);
-                if (MASTER) store_some<float, N>(master + i, some, p);
-                store_some<P, N>(param + i, some, p);
-            }
+        for (int e = 0; e < N; ++e) {
+            const float g = (float)x.g[e] * A.coef, p = MASTER ? x.w[e] : (float)x.p[e];
+            const float m = __builtin_fmaf(A.beta1, x.m[e], A.rest1 * g), v = __builtin_fmaf(A.beta2, x.v[e], A.rest2 * g * g);
+            const float now = p - __builtin_fmaf(A.fade, p, A.step * m / __builtin_fmaf(__builtin_sqrtf(v), A.inv_sqrt2, A.eps));
+            x.m[e] = m;
+            x.v[e] = v;
+            if (MASTER) x.w[e] = now;
+            x.p[e] = (P)now;
         }
-}
+        store<STREAM, float, N>(m + i, x.m);
+        store<STREAM, float, N>(v + i, x.v);
+        if (MASTER) store<STREAM, float, N>(w + i, x.w);
+        store<STREAM, P, N>(p + i, x.p);
+    }
+};
 
-template <class P, class G>
-__device__ __forceinline__ void adam_tensor(const TensorD &t, long long begin, long long end, const AdamD &A, const AdamC &C)
+template <bool STREAM, class P, class G, bool MASTER>
+__device__ __forceinline__ void adam_piece(const TensorD &t, const Piece &piece, const AdamT &A)
 {
-    if (t.master) adam_range<P, G, true>(t, begin, end, A, C);
-    else adam_range<P, G, false>(t, begin, end, A, C);
-}
-
-template <class P>
-__device__ __forceinline__ void adam_types(const TensorD &t, long long begin, long long end, const AdamD &A, const AdamC &C)
-{
-    switch (t.types & 255) {
-    case TYPE_F32: adam_tensor<P, float>(t, begin, end, A, C); break;
-    case TYPE_BF16: adam_tensor<P, __bf16>(t, begin, end, A, C); break;
-    default: adam_tensor<P, _Float16>(t, begin, end, A, C); break;
+    constexpr int N = 4, AHEAD = AHEAD_A;
+    const Vectors<N> V(piece);
+    const long long at = piece.begin;
+    const Arrays<P, G, MASTER> a = {global<G>(t.grad) + at, global<P>(t.param) + at, global<float>(t.m) + at, global<float>(t.v) + at, global<float>(t.master) + at};
+    Place<P, G, MASTER, N> x[AHEAD];
+    for (int j = 0; j < V.upto; j += 256 * AHEAD) {
+        const int mine = j + threadIdx.x;
+        if (j >= V.from && j + 256 * AHEAD <= V.upto) {
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) a.template get<STREAM>((mine + k * 256) * N, x[k]);
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) a.template update<STREAM>((mine + k * 256) * N, x[k], A);
+        } else {
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+                if (mine + k * 256 >= V.from && mine + k * 256 < V.upto) {
+                    a.template get<STREAM>((mine + k * 256) * N, x[k]);
+                    a.template update<STREAM>((mine + k * 256) * N, x[k], A);
+                }
+        }
+    }
+    if ((int)threadIdx.x < V.edges) {
+        Place<P, G, MASTER, 1> y;
+        a.template get<false>(V.edge() - at, y);
+        a.template update<false>(V.edge() - at, y, A);
     }
 }
 
-__global__ __launch_bounds__(256) void k_adamw(ListD L, AdamD A, const float *__restrict__ lr, const float *__restrict__ norm,
+template <bool STREAM, class P, class G>
+__device__ __forceinline__ void adam_master(const TensorD &t, const Piece &p, const AdamT &A)
+{
+    if (t.master) adam_piece<STREAM, P, G, true>(t, p, A);
+    else adam_piece<STREAM, P, G, false>(t, p, A);
+}
+
+template <bool STREAM, class P>
+__device__ __forceinline__ void adam_grad(const TensorD &t, const Piece &p, const AdamT &A)
+{
+    switch (t.types & 255) {
+    case TYPE_F32: adam_master<STREAM, P, float>(t, p, A); break;
+    case TYPE_BF16: adam_master<STREAM, P, __bf16>(t, p, A); break;
+    default: adam_master<STREAM, P, _Float16>(t, p, A); break;
+    }
+}
+
+template <bool STREAM>
+__global__ __launch_bounds__(256) void k_adamw(ListD L, AdamD A, const float *__restrict__ lr_word, const float *__restrict__ norm,
                                                long long *__restrict__ steps, unsigned *__restrict__ tickets)
 {
     if (A.skip_nonfinite && !(__builtin_fabsf(*norm) < __builtin_inff())) return;      // every block sees the same norm
     const long long before = *steps;
     const double time = (double)(before + 1);
-    AdamC C;
-    C.coef = clip_coef(norm, A.max_norm, A.scale);
-    C.lr = lr ? *lr : A.lr;
-    C.inv1 = (float)(1.0 / one_minus_exp(time * A.log_beta1));
-    C.inv_sqrt2 = (float)(1.0 / __builtin_sqrt(one_minus_exp(time * A.log_beta2)));
-    walk(L, [&](const TensorD &t, long long begin, long long end) {
+    const float coef = clip_coef(norm, A.max_norm, A.scale), rate = lr_word ? *lr_word : A.lr;
+    const float inv1 = (float)(1.0 / one_minus_exp(time * A.log_beta1));
+    const float inv_sqrt2 = (float)(1.0 / __builtin_sqrt(one_minus_exp(time * A.log_beta2)));
+    walk<true>(L, [&](const TensorD &t, const Piece &p) {
+        const float lr = rate * t.lr_scale;
+        const AdamT T = {coef, lr * (A.decay * t.decay_scale), lr * inv1, inv_sqrt2, A.beta1, A.beta2, A.rest1, A.rest2, A.eps};
         switch (t.types >> 8) {
-        case TYPE_F32: adam_types<float>(t, begin, end, A, C); break;
-        case TYPE_BF16: adam_types<__bf16>(t, begin, end, A, C); break;
-        default: adam_types<_Float16>(t, begin, end, A, C); break;
+        case TYPE_F32: adam_grad<STREAM, float>(t, p, T); break;
+        case TYPE_BF16: adam_grad<STREAM, __bf16>(t, p, T); break;
+        default: adam_grad<STREAM, _Float16>(t, p, T); break;
         }
     });
     // the counter moves on when every block has read it

@@ -117,12 +117,14 @@ def test_launches(tmp_path):
 h = make([])
 S.stub_clear_launches()
 assert norm(h) == OK and clip(h) == OK and adamw(h, how()) == OK
-assert [(n, g[0]) for n, g, _, _ in launched()] == [("k_norm<0>", 1), ("k_norm<0>", 1), ("k_norm<0>", 1), ("k_adamw", 1)]      # nothing to clip; the step counts
+kinds = lambda ls: [l[0].split("<")[0] for l in ls]
+ls = launched()
+assert kinds(ls) == ["k_norm", "k_norm", "k_norm", "k_adamw"] and all(l[1][0] == 1 for l in ls)      # nothing to clip; the step counts
 h = make([tensor(n=0, grad=None)] + 100 * [tensor(n=1)])
 assert [n for n in names() if n == "k_list_put"] == 3 * ["k_list_put"]       # 40 tensors at a time
 assert norm(h, 1) == OK and adamw(h, how(max_norm=math.inf), d=None) == OK and adamw(h, how(given=1)) == OK and clip(h, given=1, kind=9) == OK
 ls = launched()
-assert [l[0] for l in ls] == ["k_norm<1>", "k_adamw", "k_adamw", "k_clip"] and all(1 <= l[1][0] <= 4096 and l[2] == (256, 1, 1) for l in ls)
+assert kinds(ls) == ["k_norm", "k_adamw", "k_adamw", "k_clip"] and all(1 <= l[1][0] <= 4096 and l[2] == (256, 1, 1) for l in ls)
 a = (Tensor * 101)(*(101 * [tensor(n=5)]))
 assert L.fs_tensors_update(h, a, 101) == OK and names() == 3 * ["k_list_put"]
 # blocks never outnumber the partial sums, however long the list and large the device
