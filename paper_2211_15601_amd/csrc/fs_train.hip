@@ -20,7 +20,8 @@ struct fs_tensors {
     fs_tensor *given;         // [asked] of the last create or update
     TensorD *host;            // [asked] those with elements, as they are on the device
     // what the tensors as a whole have
-    bool params, moments;
+    bool params, moments, apart, in_place;      // in_place, apart: every `out` is, or none is, its gradient
+    double grad_bytes;
     ListD L;
     char *mem;                // device: TensorD [asked], int [asked + 1], double [TRAIN_BLOCKS], unsigned [TICKETS]
     double *partial;
@@ -128,7 +129,8 @@ int lead_of(const fs_tensor &x)
 fs_status put_list(fs_tensors *t, const char *what, const fs_tensor *list)
 {
     int count = 0, units = 0;
-    t->params = t->moments = true;
+    t->params = t->moments = t->apart = t->in_place = true;
+    t->grad_bytes = 0.0;
     for (int32_t i = 0; i < t->asked; ++i) {
         const fs_tensor &x = t->given[i] = list[i];
         if (x.n == 0) continue;
@@ -149,6 +151,9 @@ fs_status put_list(fs_tensors *t, const char *what, const fs_tensor *list)
         d.decay_scale = x.decay_scale;
         t->params = t->params && x.param;
         t->moments = t->moments && x.exp_avg && x.exp_avg_sq;
+        t->apart = t->apart && d.out != d.grad;
+        t->in_place = t->in_place && d.out == d.grad;
+        t->grad_bytes += (double)x.n * size_of(x.grad_type);
     }
     t->L.count = count;
     t->L.units = units;
@@ -178,32 +183,45 @@ fs_status on_current_device(fs_tensors *t, const char *what)
         if (begin_status != FS_OK) return begin_status;                   \
     } while (0)
 
-#ifndef BPC_N
-#define BPC_N 2
-#define BPC_C 2
-#define BPC_A 2
-#define CAP 8
-#define SN(x) true
-#define SC(x) true
-#define SA(x) true
-#endif
-// How many blocks, and how many units each takes at a time.
+// Blocks of a kernel per compute unit, and how many units each takes at a time at most.  Few blocks with their chunks side by side keep the arrays' pages
+// and channels evenly in use.  Measured for 2 / 4 / 8 blocks per unit, us: norm of 400 M fp32 230 / 234 / 241 and of 45 M bf16 in 300 tensors 23.3 / 23.1 /
+// 23.2; clipping 20 M mixed 37 / 35 / 35; AdamW of 12.6 M fp32 70.6 / 73.3 / 73.1, of 250 M mixed 1365 / 1414 / 1415.  Chunks of 3 / 6 / 8 units in AdamW:
+// 1351 / 1372 / 1384; of 1 unit 1600 (a block has too little on its way).
+struct Shape { int per_cu, most; };
+constexpr Shape NORM = {4, 8}, CLIP = {4, 4}, ADAMW = {2, 3};
+
 struct Grid { int blocks; ListD L; };
-Grid grid_for(const fs_tensors *t, int per_cu)
+Grid grid_for(const fs_tensors *t, const Shape &shape)
 {
-    Grid g = {std::max(1, std::min(t->L.units, per_cu * t->n_cus)), t->L};
-    const long long rounds = std::max(1ll, ((long long)t->L.units + (long long)CAP * g.blocks - 1) / ((long long)CAP * g.blocks));
+    Grid g = {std::max(1, std::min(t->L.units, shape.per_cu * t->n_cus)), t->L};
+    const long long most = (long long)shape.most * g.blocks, rounds = std::max(1ll, (t->L.units + most - 1) / most);
     g.L.chunk = (int)std::max(1ll, (t->L.units + g.blocks * rounds - 1) / (g.blocks * rounds));
     return g;
 }
 
+// Lists whose norm every block adds up for itself, in the kernel that needs it: two trips to memory for the 16 waves of a block.  Measured with 4 / 12 /
+// 35 units, us, this and two kernels: clipping 4.4 / 5.2 / 7.0 and 7.4 / 7.4 / 7.6, AdamW 5.8 / 6.4 / 9.7 and 10.4 / 10.4 / 10.5; the norm alone by one block and by many
+// 3.0 / 3.6 / 5.3 and 4.5 / 4.5 / 4.5.
+constexpr int SHORT_UNITS = 32;
+bool is_short(const fs_tensors *t) { return t->L.units <= SHORT_UNITS; }
+int short_blocks(const fs_tensors *t) { return std::max(1, (t->L.units * (UNIT / SHORT_PART) + SHORT_WAVES - 1) / SHORT_WAVES); }
+
+// Bytes at the end of the gradients that the norm leaves in the caches (256 MiB of them in front of the memory), for the pass behind it, which comes from that
+// end.  What is before them streams: 400 M fp32 then take 234 us, not 259.  Measured with 64 / 128 / 192 / 240 MB, clipping 250 M fp32: 512 / 490 / 497 / 492 us.
+constexpr double KEPT_BYTES = 192e6;
+
 void launch_norm(fs_tensors *t, int32_t kind, double scale, float *d_norm)
 {
-    const Grid g = grid_for(t, BPC_N);
-    const bool stream = SN(t);
-#define FS_NORM(K, S) k_norm<K, S><<<g.blocks, 256, 0, t->stream>>>(g.L, scale, t->partial, t->tickets, d_norm)
-    if (kind == FS_NORM_TWO) { if (stream) FS_NORM(KIND_TWO, true); else FS_NORM(KIND_TWO, false); }
-    else { if (stream) FS_NORM(KIND_MAX, true); else FS_NORM(KIND_MAX, false); }
+    if (is_short(t)) {
+        if (kind == FS_NORM_TWO) k_norm_short<KIND_TWO><<<1, SHORT_THREADS, 0, t->stream>>>(t->L, scale, d_norm);
+        else k_norm_short<KIND_MAX><<<1, SHORT_THREADS, 0, t->stream>>>(t->L, scale, d_norm);
+        return;
+    }
+    const Grid g = grid_for(t, NORM);
+    const double chunks = std::ceil((double)t->L.units / g.L.chunk);
+    const int streamed = t->grad_bytes > KEPT_BYTES ? (int)(chunks * (1.0 - KEPT_BYTES / t->grad_bytes)) : 0;
+    if (kind == FS_NORM_TWO) k_norm<KIND_TWO><<<g.blocks, 256, 0, t->stream>>>(g.L, streamed, scale, t->partial, t->tickets, d_norm);
+    else k_norm<KIND_MAX><<<g.blocks, 256, 0, t->stream>>>(g.L, streamed, scale, t->partial, t->tickets, d_norm);
 }
 
 bool scale_ok(double s) { return s > 0.0 && std::isfinite(s); }
@@ -237,7 +255,7 @@ fs_status fs_tensors_create(const fs_tensor *list, int32_t count, void *hip_stre
     if (s == FS_OK) {
         if (hipDeviceGetAttribute(&t->n_cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || t->n_cus < 1) t->n_cus = 256;
         (void)hipGetLastError();
-        t->n_cus = std::min(t->n_cus, TRAIN_BLOCKS / 8);
+        t->n_cus = std::min(t->n_cus, TRAIN_BLOCKS / NORM.per_cu);
         const size_t at_first = (size_t)count * sizeof(TensorD), at_partial = (at_first + ((size_t)count + 1) * sizeof(int) + 255) / 256 * 256;
         const size_t at_tickets = at_partial + TRAIN_BLOCKS * sizeof(double);
         if (hipMalloc(reinterpret_cast<void **>(&t->mem), at_tickets + TICKETS * sizeof(unsigned)) != hipSuccess) {
@@ -309,11 +327,15 @@ fs_status fs_grad_clip(fs_tensors *t, int32_t kind, double max_norm, double grad
     if (!(max_norm >= 0.0)) return fail(t, FS_E_ARG, "fs_grad_clip: max_norm must not be negative");
     if (!scale_ok(grad_scale)) return fail(t, FS_E_ARG, "fs_grad_clip: grad_scale must be positive and finite");
     if (!word_ok(t, d_norm, 4)) return fail(t, FS_E_ARG, "fs_grad_clip: d_norm must be a device pointer");
+    if (!norm_given && t->apart && is_short(t)) {
+        if (kind == FS_NORM_TWO) k_clip_short<KIND_TWO><<<short_blocks(t), SHORT_THREADS, 0, t->stream>>>(t->L, max_norm, grad_scale, d_norm);
+        else k_clip_short<KIND_MAX><<<short_blocks(t), SHORT_THREADS, 0, t->stream>>>(t->L, max_norm, grad_scale, d_norm);
+        return launch_status(t, "fs_grad_clip");
+    }
     if (!norm_given) launch_norm(t, kind, grad_scale, d_norm);
     if (t->L.units) {
-        const Grid g = grid_for(t, BPC_C);
-        if (SC(t)) k_clip<true><<<g.blocks, 256, 0, t->stream>>>(g.L, max_norm, grad_scale, d_norm);
-        else k_clip<false><<<g.blocks, 256, 0, t->stream>>>(g.L, max_norm, grad_scale, d_norm);
+        const Grid g = grid_for(t, CLIP);
+        k_clip<<<g.blocks, 256, 0, t->stream>>>(g.L, t->in_place, max_norm, grad_scale, d_norm);
     }
     return launch_status(t, "fs_grad_clip");
 }
@@ -336,7 +358,6 @@ fs_status fs_adamw_step(fs_tensors *t, const fs_adamw *how, int64_t *d_step, flo
     if (!word_ok(t, d_step, 8)) return fail(t, FS_E_ARG, "fs_adamw_step: d_step must be a device pointer");
     if (h.d_lr && !word_ok(t, h.d_lr, 4)) return fail(t, FS_E_ARG, "fs_adamw_step: d_lr must be a device pointer or NULL");
     if (!t->params || !t->moments) return fail(t, FS_E_STATE, "fs_adamw_step: tensors without param, exp_avg or exp_avg_sq");
-    if (d_norm && !h.norm_given) launch_norm(t, FS_NORM_TWO, h.grad_scale, d_norm);
     AdamD A;
     A.log_beta1 = std::log(h.beta1);
     A.log_beta2 = std::log(h.beta2);
@@ -350,9 +371,15 @@ fs_status fs_adamw_step(fs_tensors *t, const fs_adamw *how, int64_t *d_step, flo
     A.eps = (float)h.eps;
     A.decay = (float)h.weight_decay;
     A.skip_nonfinite = h.skip_nonfinite;
-    const Grid g = grid_for(t, BPC_A);
-    if (SA(t)) k_adamw<true><<<g.blocks, 256, 0, t->stream>>>(g.L, A, h.d_lr, d_norm, reinterpret_cast<long long *>(d_step), t->tickets);
-    else k_adamw<false><<<g.blocks, 256, 0, t->stream>>>(g.L, A, h.d_lr, d_norm, reinterpret_cast<long long *>(d_step), t->tickets);
+    long long *steps = reinterpret_cast<long long *>(d_step);
+    const bool computed = d_norm && !h.norm_given;
+    if (computed && is_short(t)) {
+        k_adamw_short<<<short_blocks(t), SHORT_THREADS, 0, t->stream>>>(t->L, A, h.d_lr, d_norm, steps, t->tickets);
+        return launch_status(t, "fs_adamw_step");
+    }
+    if (computed) launch_norm(t, FS_NORM_TWO, h.grad_scale, d_norm);
+    const Grid g = grid_for(t, ADAMW);
+    k_adamw<<<g.blocks, 256, 0, t->stream>>>(g.L, A, h.d_lr, d_norm, steps, t->tickets);
     return launch_status(t, "fs_adamw_step");
 }
 

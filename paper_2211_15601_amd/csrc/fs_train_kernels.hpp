@@ -10,6 +10,7 @@ namespace fs {
 
 constexpr int UNIT = 2048;             // elements: 8 per thread
 constexpr int TRAIN_BLOCKS = 4096;     // at most; a partial sum for each
+constexpr int SHORT_PART = 256;         // elements that a wave of a short list's second pass takes at a time
 constexpr int LIST_LDS = 1024;          // places that a block keeps in LDS
 constexpr int TICKET_GROUPS = 32, TICKET_STRIDE = 64;      // counters of last_block, each on lines of its own
 constexpr int TICKETS = (1 + TICKET_GROUPS) * TICKET_STRIDE;
@@ -104,8 +105,9 @@ __device__ __forceinline__ TensorD tensor_at(const ListD &L, int i)
 
 // A part of a tensor: elements [begin, end), of which those before 0 are not there (begin < 0 in a first unit with a lead).
 struct Piece { long long begin, end; };
+__device__ __forceinline__ Piece piece_of(const TensorD &t, long long from, long long upto) { return {from - t.lead, min(upto - t.lead, t.n)}; }
 
-// Calls f(tensor, piece) for what this block's chunks of units cover of every tensor.  The next piece's tensor is found and asked for before
+// Calls f(tensor, piece, chunk) for what this block's chunks of units cover of every tensor.  The next piece's tensor is found and asked for before
 // the present piece is worked on.  BACK: the last chunk first.
 template <bool BACK, class F>
 __device__ __forceinline__ void walk(const ListD &L, F f)
@@ -123,8 +125,8 @@ __device__ __forceinline__ void walk(const ListD &L, F f)
     int u = (BACK ? chunks - 1 - c : c) * L.chunk, end = min(u + L.chunk, L.units), i = find(u);
     TensorD t = tensor_at(L, i);
     for (;;) {
-        const long long upto = (long long)(end - t.first) * UNIT - t.lead;
-        const Piece p = {(long long)(u - t.first) * UNIT - t.lead, upto < t.n ? upto : t.n};
+        const Piece p = piece_of(t, (long long)(u - t.first) * UNIT, (long long)(end - t.first) * UNIT);
+        const int now = c;
         u = t.next;
         bool more = u < end;
         if (more) ++i;
@@ -138,73 +140,98 @@ __device__ __forceinline__ void walk(const ListD &L, F f)
             }
         }
         const TensorD next = more ? tensor_at(L, i) : t;
-        f(t, p);
+        f(t, p, now);
         if (!more) return;
         t = next;
     }
 }
 
-// A piece in vectors of N elements.  Those at the tensor's ends that are not whole are left out; their elements, fewer than 2 N, are `edge`'s, one to a thread.
-template <int N>
+// The same for short lists, a wave by itself: parts of PART elements, dealt out to `waves` waves of which this is number `wave`.
+template <int PART, class F>
+__device__ __forceinline__ void walk_short(const ListD &L, int wave, int waves, F f)
+{
+    constexpr int PARTS = UNIT / PART;
+    for (int c = wave; c < L.units * PARTS; c += waves) {
+        const TensorD t = tensor_at(L, find_tensor(L.first, L.count, c / PARTS));
+        const long long at = (long long)(c / PARTS - t.first) * UNIT + c % PARTS * PART;
+        const Piece p = piece_of(t, at, at + PART);
+        if (p.begin < p.end && p.end > 0) f(t, p);
+    }
+}
+
+// A piece in vectors of N elements, worked on by TEAM threads of which this is number `rank`.  Vectors at the tensor's ends that are not whole are left out;
+// their elements, fewer than 2 N, are the edges, one to a thread.
+template <int N, int TEAM>
 struct Vectors {
     int from, upto;                    // whole vectors, numbered from the piece's begin
-    int heads, edges;                  // elements before them, and in all
-    long long tail;                    // the first element behind them
-    __device__ __forceinline__ explicit Vectors(const Piece &p)
+    int rank;
+    bool edge;                         // this thread has an edge
+    int at;                            // that element, from the piece's begin
+    __device__ __forceinline__ explicit Vectors(const Piece &p) : rank(threadIdx.x & (TEAM - 1))
     {
-        const int before = p.begin < 0 ? (int)-p.begin : 0;
-        const int there = (int)(p.end - p.begin);
+        static_assert(2 * N <= TEAM, "an edge a thread");
+        const int before = p.begin < 0 ? (int)-p.begin : 0, there = (int)(p.end - p.begin);
         from = (before + N - 1) / N;
-        upto = there / N;
-        heads = min(from * N, there) - before;
-        if (upto < from) upto = from;
-        tail = p.begin + (long long)upto * N;
-        edges = heads + (tail < p.end ? (int)(p.end - tail) : 0);
+        upto = max(from, there / N);
+        const int heads = min(from * N, there) - before;
+        at = rank < heads ? before + rank : upto * N + (rank - heads);
+        edge = at < there;
     }
-    // the element of this thread, which is < edges
-    __device__ __forceinline__ long long edge() const { return (int)threadIdx.x < heads ? (long long)threadIdx.x : tail + ((int)threadIdx.x - heads); }
+    // Calls f(first vector of this thread, all of its vectors are there) for every AHEAD * TEAM vectors; it has k * TEAM more behind it, see has().
+    template <int AHEAD, class F>
+    __device__ __forceinline__ void each(F f) const
+    {
+        for (int j = 0; j < upto; j += TEAM * AHEAD) f(j + rank, j >= from && j + TEAM * AHEAD <= upto);
+    }
+    __device__ __forceinline__ bool has(int j) const { return j >= from && j < upto; }
 };
 
 // ---- sums over a block, and over the blocks ----
 __device__ __forceinline__ double join(double a, double b) { return a + b; }
 __device__ __forceinline__ unsigned join(unsigned a, unsigned b) { return a > b ? a : b; }
 
-// result in thread 0; every thread of the block calls it
-template <class S>
+// result in every thread; every thread of the block calls it
+template <int WAVES, class S>
 __device__ __forceinline__ S block_join(S s)
 {
-    __shared__ S wave[4];
+    __shared__ S wave[WAVES];
 #pragma unroll
     for (int d = 32; d; d >>= 1) s = join(s, __shfl_xor(s, d));
     if ((threadIdx.x & 63) == 0) wave[threadIdx.x >> 6] = s;
     __syncthreads();
-    return join(join(wave[0], wave[1]), join(wave[2], wave[3]));
+    s = wave[0];
+#pragma unroll
+    for (int i = 1; i < WAVES; ++i) s = join(s, wave[i]);
+    return s;
 }
 
-// True in every thread of the block that comes last, when all threads of all blocks have come here.  Blocks count themselves in groups, the last
-// of a group counts it at the top: one counter serves a block in some 10 ns, so 2048 blocks that end together would stand 20 us in line at a
-// single one.  The counters are 0 between kernels.  What a block leaves for the last one it stores with agent-scope atomics, which go past the caches;
-// they are done when vmcnt is 0.  (A release at agent scope would write the whole L2 back and an acquire drop it, some 25 ns a block of 50 us in all.)
-__device__ __forceinline__ unsigned count_in(unsigned *counter, unsigned of)
+// Which block comes last?  Blocks count themselves in groups, the last of a group counts it at the top: one counter serves a block in some 10 ns,
+// so 1024 blocks that end together would stand 10 us in line at a single one.  The counters are 0 between kernels.  A release or acquire at agent scope would
+// write the whole L2 back or drop it, 50 us with 2048 blocks; what a block leaves for the last one it stores with agent-scope atomics, which go past the
+// caches, and has done so when vmcnt is 0.
+struct Ticket { unsigned *counter; unsigned before, of; };
+
+__device__ __forceinline__ unsigned count_in(unsigned *counter) { return __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// By one thread of a block, when all that the block does before the last one goes on is done.
+__device__ __forceinline__ Ticket take_ticket(unsigned *tickets)
 {
-    const unsigned before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (before != of - 1) return 0;
-    __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return 1;
+    __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    const bool few = gridDim.x <= 2 * TICKET_GROUPS;
+    const unsigned mine = blockIdx.x % TICKET_GROUPS;
+    unsigned *counter = few ? tickets : tickets + (1 + mine) * TICKET_STRIDE;
+    return {counter, count_in(counter), few ? gridDim.x : (gridDim.x - mine + TICKET_GROUPS - 1) / TICKET_GROUPS};
 }
 
-__device__ __forceinline__ bool last_block(unsigned *tickets)
+// By the same thread, then or later: is it the last block's?
+__device__ __forceinline__ bool is_last(const Ticket &t, unsigned *tickets)
 {
-    __shared__ unsigned last;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        const unsigned groups = min((unsigned)TICKET_GROUPS, gridDim.x), mine = blockIdx.x % groups;
-        last = count_in(tickets + (1 + mine) * TICKET_STRIDE, (gridDim.x - mine + groups - 1) / groups);
-        if (last) last = count_in(tickets, groups);
-    }
-    __syncthreads();
-    return last;
+    if (t.before != t.of - 1) return false;
+    __hip_atomic_store(t.counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (t.counter == tickets) return true;
+    if (count_in(tickets) != TICKET_GROUPS - 1) return false;
+    __hip_atomic_store(tickets, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return true;
 }
 
 // ---- global norm ----
@@ -223,126 +250,156 @@ template <> struct Sum<KIND_MAX> {
     static __device__ __forceinline__ double value(unsigned s) { return (double)__uint_as_float(s); }
 };
 
-// AHEAD loads of 16 bytes in every thread on their way.
-#ifndef AHEAD_N
-#define AHEAD_N 4
-#define AHEAD_C 2
-#define AHEAD_A 1
-#endif
-template <int KIND, bool STREAM, class T, class S>
+// AHEAD: loads of 16 bytes of an array that every thread has on their way.
+constexpr int AHEAD_NORM = 4, AHEAD_CLIP = 2, AHEAD_ADAMW = 1;
+
+template <int KIND, bool STREAM, int TEAM, int AHEAD, class T, class S>
 __device__ __forceinline__ S sum_piece(Global<T> g, const Piece &p, S s)
 {
-    constexpr int N = 16 / sizeof(T), AHEAD = AHEAD_N;
-    const Vectors<N> V(p);
+    constexpr int N = 16 / sizeof(T);
+    const Vectors<N, TEAM> V(p);
     g += p.begin;
-    Vec<T, N> x[AHEAD];
-    auto add = [&](int k) {
+    float edge = 0.0f;
+    if (V.edge) edge = (float)g[V.at];
+    V.template each<AHEAD>([&](int j, bool all) {
+        Vec<T, N> x[AHEAD];
+        if (all) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) s = Sum<KIND>::add(s, (float)x[k][e]);
-    };
-    for (int j = 0; j < V.upto; j += 256 * AHEAD) {
-        const int mine = j + threadIdx.x;
-        if (j >= V.from && j + 256 * AHEAD <= V.upto) {
-#pragma unroll
-            for (int k = 0; k < AHEAD; ++k) x[k] = load<STREAM, T, N>(g + (mine + k * 256) * N);
+            for (int k = 0; k < AHEAD; ++k) x[k] = load<STREAM, T, N>(g + (j + k * TEAM) * N);
         } else {
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) {
                 x[k] = (T)0.0f;
-                if (mine + k * 256 >= V.from && mine + k * 256 < V.upto) x[k] = load<STREAM, T, N>(g + (mine + k * 256) * N);
+                if (V.has(j + k * TEAM)) x[k] = load<STREAM, T, N>(g + (j + k * TEAM) * N);
             }
         }
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) add(k);
-    }
-    if ((int)threadIdx.x < V.edges) s = Sum<KIND>::add(s, (float)g[V.edge() - p.begin]);
-    return s;
+        for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+            for (int e = 0; e < N; ++e) s = Sum<KIND>::add(s, (float)x[k][e]);
+    });
+    return Sum<KIND>::add(s, edge);
 }
 
-template <int KIND, bool STREAM>
-__global__ __launch_bounds__(256) void k_norm(ListD L, double scale, double *__restrict__ partial, unsigned *__restrict__ tickets, float *__restrict__ norm)
+template <int KIND, bool STREAM, int TEAM, int AHEAD, class S>
+__device__ __forceinline__ S sum_types(const TensorD &t, const Piece &p, S s)
+{
+    switch (t.types & 255) {
+    case TYPE_F32: return sum_piece<KIND, STREAM, TEAM, AHEAD>(global<float>(t.grad), p, s);
+    case TYPE_BF16: return sum_piece<KIND, STREAM, TEAM, AHEAD>(global<__bf16>(t.grad), p, s);
+    default: return sum_piece<KIND, STREAM, TEAM, AHEAD>(global<_Float16>(t.grad), p, s);
+    }
+}
+
+// The first `streamed` chunks are read past the caches, the others stay there for a pass that comes from the other end.
+template <int KIND>
+__global__ __launch_bounds__(256) void k_norm(ListD L, int streamed, double scale, double *__restrict__ partial, unsigned *__restrict__ tickets, float *__restrict__ norm)
 {
     using S = typename Sum<KIND>::type;
     S s = 0;
-    walk<false>(L, [&](const TensorD &t, const Piece &p) {
-        switch (t.types & 255) {
-        case TYPE_F32: s = sum_piece<KIND, STREAM>(global<float>(t.grad), p, s); break;
-        case TYPE_BF16: s = sum_piece<KIND, STREAM>(global<__bf16>(t.grad), p, s); break;
-        default: s = sum_piece<KIND, STREAM>(global<_Float16>(t.grad), p, s); break;
-        }
+    walk<false>(L, [&](const TensorD &t, const Piece &p, int c) {
+        s = c < streamed ? sum_types<KIND, true, 256, AHEAD_NORM>(t, p, s) : sum_types<KIND, false, 256, AHEAD_NORM>(t, p, s);
     });
-    s = block_join(s);
+    s = block_join<4>(s);
     S *part = reinterpret_cast<S *>(partial);
-    if (threadIdx.x == 0) __hip_atomic_store(part + blockIdx.x, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (!last_block(tickets)) return;
+    __shared__ bool last;
+    if (threadIdx.x == 0) {
+        __hip_atomic_store(part + blockIdx.x, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        last = is_last(take_ticket(tickets), tickets);
+    }
+    __syncthreads();
+    if (!last) return;
     s = 0;
     for (unsigned i = threadIdx.x; i < gridDim.x; i += 256) s = join(s, __hip_atomic_load(part + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-    s = block_join(s);
+    s = block_join<4>(s);
     if (threadIdx.x == 0) *norm = (float)(Sum<KIND>::value(s) * scale);
+}
+
+// ---- short lists ----
+// Every block adds up the whole list, the same way, and needs to hear of no other: a list of SHORT_UNITS units is two trips to memory for its 16 waves.
+constexpr int SHORT_THREADS = 1024, SHORT_WAVES = SHORT_THREADS / 64;
+template <int KIND>
+__device__ __forceinline__ float short_norm(const ListD &L, double scale)
+{
+    typename Sum<KIND>::type s = 0;
+    walk_short<UNIT>(L, threadIdx.x >> 6, SHORT_WAVES, [&](const TensorD &t, const Piece &p) { s = sum_types<KIND, false, 64, 8>(t, p, s); });
+    return (float)(Sum<KIND>::value(block_join<SHORT_WAVES>(s)) * scale);
+}
+
+template <int KIND>
+__global__ __launch_bounds__(SHORT_THREADS) void k_norm_short(ListD L, double scale, float *__restrict__ norm)
+{
+    const float n = short_norm<KIND>(L, scale);
+    if (threadIdx.x == 0) *norm = n;
 }
 
 // ---- clipping ----
 
 // s min(1, max_norm / (norm + 1e-6)), NaN for a norm that is NaN
-__device__ __forceinline__ float clip_coef(const float *norm, double max_norm, double scale)
+__device__ __forceinline__ float clip_coef(float norm, double max_norm, double scale)
 {
     if (max_norm == __builtin_inf()) return (float)scale;
-    const double q = max_norm / ((double)*norm + 1e-6);
+    const double q = max_norm / ((double)norm + 1e-6);
     return (float)((q >= 1.0 ? 1.0 : q) * scale);
 }
 
-template <bool STREAM, class T>
+template <bool STREAM, int TEAM, int AHEAD, class T>
 __device__ __forceinline__ void scale_piece(Global<T> g, Global<T> out, const Piece &p, float coef)
 {
-    constexpr int N = 16 / sizeof(T), AHEAD = AHEAD_C;
-    const Vectors<N> V(p);
+    constexpr int N = 16 / sizeof(T);
+    const Vectors<N, TEAM> V(p);
     g += p.begin;
     out += p.begin;
-    Vec<T, N> x[AHEAD];
-    auto scale = [&](int k) {
+    V.template each<AHEAD>([&](int j, bool all) {
+        Vec<T, N> x[AHEAD];
+        auto get = [&](int k) { x[k] = load<STREAM, T, N>(g + (j + k * TEAM) * N); };
+        auto put = [&](int k) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[k][e] = (T)((float)x[k][e] * coef);
-    };
-    for (int j = 0; j < V.upto; j += 256 * AHEAD) {
-        const int mine = j + threadIdx.x;
-        if (j >= V.from && j + 256 * AHEAD <= V.upto) {
+            for (int e = 0; e < N; ++e) x[k][e] = (T)((float)x[k][e] * coef);
+            store<STREAM, T, N>(out + (j + k * TEAM) * N, x[k]);
+        };
+        if (all) {
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k) x[k] = load<STREAM, T, N>(g + (mine + k * 256) * N);
+            for (int k = 0; k < AHEAD; ++k) get(k);
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k) {
-                scale(k);
-                store<STREAM, T, N>(out + (mine + k * 256) * N, x[k]);
-            }
+            for (int k = 0; k < AHEAD; ++k) put(k);
         } else {
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k)
-                if (mine + k * 256 >= V.from && mine + k * 256 < V.upto) x[k] = load<STREAM, T, N>(g + (mine + k * 256) * N);
+                if (V.has(j + k * TEAM)) get(k);
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k)
-                if (mine + k * 256 >= V.from && mine + k * 256 < V.upto) {
-                    scale(k);
-                    store<STREAM, T, N>(out + (mine + k * 256) * N, x[k]);
-                }
+                if (V.has(j + k * TEAM)) put(k);
         }
-    }
-    if ((int)threadIdx.x < V.edges) {
-        const long long i = V.edge() - p.begin;
-        out[i] = (T)((float)g[i] * coef);
+    });
+    if (V.edge) out[V.at] = (T)((float)g[V.at] * coef);
+}
+
+template <bool STREAM, int TEAM, int AHEAD>
+__device__ __forceinline__ void scale_types(const TensorD &t, const Piece &p, float coef)
+{
+    if (t.out == t.grad && coef == 1.0f) return;
+    switch (t.types & 255) {
+    case TYPE_F32: scale_piece<STREAM, TEAM, AHEAD>(global<float>(t.grad), global<float>(t.out), p, coef); break;
+    case TYPE_BF16: scale_piece<STREAM, TEAM, AHEAD>(global<__bf16>(t.grad), global<__bf16>(t.out), p, coef); break;
+    default: scale_piece<STREAM, TEAM, AHEAD>(global<_Float16>(t.grad), global<_Float16>(t.out), p, coef); break;
     }
 }
 
-template <bool STREAM>
-__global__ __launch_bounds__(256) void k_clip(ListD L, double max_norm, double scale, const float *__restrict__ norm)
+__global__ __launch_bounds__(256) void k_clip(ListD L, int all_in_place, double max_norm, double scale, const float *__restrict__ norm)
 {
-    const float coef = clip_coef(norm, max_norm, scale);
-    walk<true>(L, [&](const TensorD &t, const Piece &p) {
-        if (t.out == t.grad && coef == 1.0f) return;
-        switch (t.types & 255) {
-        case TYPE_F32: scale_piece<STREAM>(global<float>(t.grad), global<float>(t.out), p, coef); break;
-        case TYPE_BF16: scale_piece<STREAM>(global<__bf16>(t.grad), global<__bf16>(t.out), p, coef); break;
-        default: scale_piece<STREAM>(global<_Float16>(t.grad), global<_Float16>(t.out), p, coef); break;
-        }
-    });
+    const float coef = clip_coef(*norm, max_norm, scale);
+    if (all_in_place && coef == 1.0f) return;
+    walk<true>(L, [&](const TensorD &t, const Piece &p, int) { scale_types<true, 256, AHEAD_CLIP>(t, p, coef); });
+}
+
+// Not in place: a block may have written while another still adds up.
+template <int KIND>
+__global__ __launch_bounds__(SHORT_THREADS) void k_clip_short(ListD L, double max_norm, double scale, float *__restrict__ norm)
+{
+    const float n = short_norm<KIND>(L, scale), coef = clip_coef(n, max_norm, scale);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *norm = n;
+    walk_short<SHORT_PART>(L, blockIdx.x * SHORT_WAVES + (threadIdx.x >> 6), gridDim.x * SHORT_WAVES, [&](const TensorD &t, const Piece &p) { scale_types<false, 64, 1>(t, p, coef); });
 }
 
 // ---- AdamW ----
@@ -414,75 +471,129 @@ struct Arrays {
     }
 };
 
-template <bool STREAM, class P, class G, bool MASTER>
-__device__ __forceinline__ void adam_piece(const TensorD &t, const Piece &piece, const AdamT &A)
+template <bool STREAM, int TEAM, int AHEAD, class P, class G, bool MASTER>
+__device__ __forceinline__ void adam_piece(const TensorD &t, const Piece &p, const AdamT &A)
 {
-    constexpr int N = 4, AHEAD = AHEAD_A;
-    const Vectors<N> V(piece);
-    const long long at = piece.begin;
-    const Arrays<P, G, MASTER> a = {global<G>(t.grad) + at, global<P>(t.param) + at, global<float>(t.m) + at, global<float>(t.v) + at, global<float>(t.master) + at};
-    Place<P, G, MASTER, N> x[AHEAD];
-    for (int j = 0; j < V.upto; j += 256 * AHEAD) {
-        const int mine = j + threadIdx.x;
-        if (j >= V.from && j + 256 * AHEAD <= V.upto) {
+    constexpr int N = 4;                                   // 16 bytes of every fp32 array
+    const Vectors<N, TEAM> V(p);
+    const Arrays<P, G, MASTER> a = {global<G>(t.grad) + p.begin, global<P>(t.param) + p.begin, global<float>(t.m) + p.begin, global<float>(t.v) + p.begin,
+                                    global<float>(t.master) + p.begin};
+    V.template each<AHEAD>([&](int j, bool all) {
+        Place<P, G, MASTER, N> x[AHEAD];
+        if (all) {
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k) a.template get<STREAM>((mine + k * 256) * N, x[k]);
+            for (int k = 0; k < AHEAD; ++k) a.template get<STREAM>((j + k * TEAM) * N, x[k]);
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k) a.template update<STREAM>((mine + k * 256) * N, x[k], A);
+            for (int k = 0; k < AHEAD; ++k) a.template update<STREAM>((j + k * TEAM) * N, x[k], A);
         } else {
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k)
-                if (mine + k * 256 >= V.from && mine + k * 256 < V.upto) {
-                    a.template get<STREAM>((mine + k * 256) * N, x[k]);
-                    a.template update<STREAM>((mine + k * 256) * N, x[k], A);
+                if (V.has(j + k * TEAM)) {
+                    a.template get<STREAM>((j + k * TEAM) * N, x[k]);
+                    a.template update<STREAM>((j + k * TEAM) * N, x[k], A);
                 }
         }
-    }
-    if ((int)threadIdx.x < V.edges) {
+    });
+    if (V.edge) {
         Place<P, G, MASTER, 1> y;
-        a.template get<false>(V.edge() - at, y);
-        a.template update<false>(V.edge() - at, y, A);
+        a.template get<false>(V.at, y);
+        a.template update<false>(V.at, y, A);
     }
 }
 
-template <bool STREAM, class P, class G>
+template <bool STREAM, int TEAM, int AHEAD, class P, class G>
 __device__ __forceinline__ void adam_master(const TensorD &t, const Piece &p, const AdamT &A)
 {
-    if (t.master) adam_piece<STREAM, P, G, true>(t, p, A);
-    else adam_piece<STREAM, P, G, false>(t, p, A);
+    if (t.master) adam_piece<STREAM, TEAM, AHEAD, P, G, true>(t, p, A);
+    else adam_piece<STREAM, TEAM, AHEAD, P, G, false>(t, p, A);
 }
 
-template <bool STREAM, class P>
+template <bool STREAM, int TEAM, int AHEAD, class P>
 __device__ __forceinline__ void adam_grad(const TensorD &t, const Piece &p, const AdamT &A)
 {
     switch (t.types & 255) {
-    case TYPE_F32: adam_master<STREAM, P, float>(t, p, A); break;
-    case TYPE_BF16: adam_master<STREAM, P, __bf16>(t, p, A); break;
-    default: adam_master<STREAM, P, _Float16>(t, p, A); break;
+    case TYPE_F32: adam_master<STREAM, TEAM, AHEAD, P, float>(t, p, A); break;
+    case TYPE_BF16: adam_master<STREAM, TEAM, AHEAD, P, __bf16>(t, p, A); break;
+    default: adam_master<STREAM, TEAM, AHEAD, P, _Float16>(t, p, A); break;
     }
 }
 
-template <bool STREAM>
+struct AdamC { float coef, rate, inv1, inv_sqrt2; };       // of one step
+
+// What the number of the step makes of the rate, by one wave for its block: the 64-bit arithmetic would take every wave some 0.8 us.  That wave's first
+// lane also takes the ticket here, when it has read the counter, and looks at it at the end, when the answer has long come.
+struct StepD { long long before; Ticket ticket; };
+__device__ __forceinline__ StepD adam_begin(const AdamD &A, const float *lr_word, const long long *steps, unsigned *tickets, AdamC *shared)
+{
+    StepD s;
+    s.before = *steps;
+    const double time = (double)(s.before + 1);
+    const AdamC C = {0.0f, lr_word ? *lr_word : A.lr, (float)(1.0 / one_minus_exp(time * A.log_beta1)), (float)(1.0 / __builtin_sqrt(one_minus_exp(time * A.log_beta2)))};
+    if ((threadIdx.x & 63) == 0) {
+        *shared = C;
+        s.ticket = take_ticket(tickets);
+    }
+    return s;
+}
+
+// The counter moves on when every block has read it.
+__device__ __forceinline__ void adam_end(const StepD &s, long long *steps, unsigned *tickets)
+{
+    if ((threadIdx.x & 63) == 0 && is_last(s.ticket, tickets)) *steps = s.before + 1;
+}
+
+template <bool STREAM, int TEAM, int AHEAD>
+__device__ __forceinline__ void adam_types(const TensorD &t, const Piece &p, const AdamD &A, const AdamC &C)
+{
+    const float lr = C.rate * t.lr_scale;
+    const AdamT T = {C.coef, lr * (A.decay * t.decay_scale), lr * C.inv1, C.inv_sqrt2, A.beta1, A.beta2, A.rest1, A.rest2, A.eps};
+    switch (t.types >> 8) {
+    case TYPE_F32: adam_grad<STREAM, TEAM, AHEAD, float>(t, p, T); break;
+    case TYPE_BF16: adam_grad<STREAM, TEAM, AHEAD, __bf16>(t, p, T); break;
+    default: adam_grad<STREAM, TEAM, AHEAD, _Float16>(t, p, T); break;
+    }
+}
+
+__device__ __forceinline__ bool is_finite(float x) { return __builtin_fabsf(x) < __builtin_inff(); }
+
+// norm: of the gradients, or NULL where nothing asks for it
 __global__ __launch_bounds__(256) void k_adamw(ListD L, AdamD A, const float *__restrict__ lr_word, const float *__restrict__ norm,
                                                long long *__restrict__ steps, unsigned *__restrict__ tickets)
 {
-    if (A.skip_nonfinite && !(__builtin_fabsf(*norm) < __builtin_inff())) return;      // every block sees the same norm
-    const long long before = *steps;
-    const double time = (double)(before + 1);
-    const float coef = clip_coef(norm, A.max_norm, A.scale), rate = lr_word ? *lr_word : A.lr;
-    const float inv1 = (float)(1.0 / one_minus_exp(time * A.log_beta1));
-    const float inv_sqrt2 = (float)(1.0 / __builtin_sqrt(one_minus_exp(time * A.log_beta2)));
-    walk<true>(L, [&](const TensorD &t, const Piece &p) {
-        const float lr = rate * t.lr_scale;
-        const AdamT T = {coef, lr * (A.decay * t.decay_scale), lr * inv1, inv_sqrt2, A.beta1, A.beta2, A.rest1, A.rest2, A.eps};
-        switch (t.types >> 8) {
-        case TYPE_F32: adam_grad<STREAM, float>(t, p, T); break;
-        case TYPE_BF16: adam_grad<STREAM, __bf16>(t, p, T); break;
-        default: adam_grad<STREAM, _Float16>(t, p, T); break;
-        }
-    });
-    // the counter moves on when every block has read it
-    if (last_block(tickets) && threadIdx.x == 0) *steps = before + 1;
+    const float n = norm ? *norm : 0.0f;
+    if (A.skip_nonfinite && !is_finite(n)) return;         // every block sees the same norm
+    __shared__ AdamC shared;
+    StepD step;
+    const bool first = threadIdx.x < 64;
+    if (first) step = adam_begin(A, lr_word, steps, tickets, &shared);
+    __syncthreads();
+    AdamC C = shared;
+    C.coef = clip_coef(n, A.max_norm, A.scale);
+    walk<true>(L, [&](const TensorD &t, const Piece &p, int) { adam_types<true, 256, AHEAD_ADAMW>(t, p, A, C); });
+    if (first) adam_end(step, steps, tickets);
+}
+
+// With the norm in the same kernel, which is as good as the list is short.
+__global__ __launch_bounds__(SHORT_THREADS) void k_adamw_short(ListD L, AdamD A, const float *__restrict__ lr_word, float *__restrict__ norm,
+                                                               long long *__restrict__ steps, unsigned *__restrict__ tickets)
+{
+    __shared__ AdamC shared;
+    StepD step;
+    const int wave = threadIdx.x >> 6;
+    const bool last_wave = wave == SHORT_WAVES - 1;        // the one with the least to add up
+    if (last_wave) step = adam_begin(A, lr_word, steps, tickets, &shared);
+    const float n = short_norm<KIND_TWO>(L, A.scale);      // waits for all of the block
+    if (blockIdx.x == 0 && threadIdx.x == 0) *norm = n;
+    const bool skip = A.skip_nonfinite && !is_finite(n);
+    if (!skip) {
+        AdamC C = shared;
+        C.coef = clip_coef(n, A.max_norm, A.scale);
+        walk_short<SHORT_PART>(L, blockIdx.x * SHORT_WAVES + wave, gridDim.x * SHORT_WAVES, [&](const TensorD &t, const Piece &p) { adam_types<false, 64, 1>(t, p, A, C); });
+    }
+    if (last_wave) {
+        if (skip) step.before -= 1;                        // the tickets were taken; the counter keeps its value
+        adam_end(step, steps, tickets);
+    }
 }
 
 }  // namespace fs

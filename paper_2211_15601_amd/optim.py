@@ -94,14 +94,16 @@ class _Handle:
             raise binding.FsError(st, self.L.fs_tensors_error(self._h).decode())
 
     def on_stream(self):
+        # torch.cuda.current_stream makes an object, 2 us of the 7 that a call takes the host; this is what compiled code of torch's own asks
+        if torch._C._cuda_getCurrentRawStream(self.device.index) == self._raw:
+            return
         now = torch.cuda.current_stream(self.device)
-        if now.cuda_stream != self._raw:
-            # the list's scratch is one: this stream's calls come after those of the stream before.  A stream that records a graph cannot wait
-            # for work outside of it; torch.cuda.graph waits for the whole device before it records.
-            if not torch.cuda.is_current_stream_capturing():
-                now.wait_stream(self._stream)
-            self._stream, self._raw = now, now.cuda_stream
-            self.ret(self.L.fs_tensors_set_stream(self._h, self._raw))
+        # the list's scratch is one: this stream's calls come after those of the stream before.  A stream that records a graph cannot wait
+        # for work outside of it; torch.cuda.graph waits for the whole device before it records.
+        if not torch.cuda.is_current_stream_capturing():
+            now.wait_stream(self._stream)
+        self._stream, self._raw = now, now.cuda_stream
+        self.ret(self.L.fs_tensors_set_stream(self._h, self._raw))
 
     def norm(self, norm):
         """Where a call's norm goes or comes from."""
@@ -237,9 +239,7 @@ class AdamW:
         self._given = None
         if grads is not None:
             (self._given,) = _lists(n, grads=grads)
-        self._state = [t for t in self.masters + self.exp_avgs + self.exp_avg_sqs if t is not None]
-        self._written = self.params + self._state
-        _check_apart(self._written + (self._given or []))
+        _check_apart(self.params + self.masters + self.exp_avgs + self.exp_avg_sqs + (self._given or []))
         self._straight = [p.is_contiguous() for p in self.params]
         self._places = None
         self._how = binding.AdamW()
@@ -286,7 +286,7 @@ class AdamW:
         how.max_norm = math.inf if self.max_norm is None else self.max_norm
         how.norm_given, how.skip_nonfinite = norm is not None, bool(self.skip_nonfinite)
         h.ret(h.L.fs_adamw_step(h._h, ctypes.byref(how), self.step_count.data_ptr(), d.data_ptr() if asked else None))
-        torch.autograd.graph.increment_version(self._written)
+        torch.autograd.graph.increment_version(self.params)       # autograd has to notice that they have changed
         return d
 
     def zero_grad(self, set_to_none: bool = False):

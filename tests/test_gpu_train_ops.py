@@ -12,6 +12,7 @@ DEV = "cuda:0"
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
 TYPES = [F32, BF16, F16]
 # lengths around the unit of 2048 elements and the 4 and 8 elements of a load; zero and one
+# (without the last ones the list is short enough for kernels of its own)
 LENGTHS = [0, 1, 2, 3, 5, 7, 8, 9, 31, 255, 1023, 1024, 1025, 2047, 2048, 2049, 4093, 8192, 40961]
 
 
@@ -112,18 +113,19 @@ def test_norm_of_nan_and_infinity(optim, dtype):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("inplace", [False, True])
+@pytest.mark.parametrize("lengths", [LENGTHS, LENGTHS[:-2]])
 @pytest.mark.parametrize("kind,max_norm,scale", [("l2", 0.5, 1.0), ("max", 0.25, 1.0), ("l2", 3.0, 2.0 ** -7), ("l2", 1e9, 0.125), ("l2", 0.0, 1.0)])
-def test_clip(optim, dtype, inplace, kind, max_norm, scale):
+def test_clip(optim, dtype, inplace, lengths, kind, max_norm, scale):
     gen = torch.Generator().manual_seed(3)
-    grads = [_values(gen, n, dtype) for n in LENGTHS]
+    grads = [_values(gen, n, dtype) for n in lengths]
     flat, views = _packed(grads, dtype, 5)
-    flat_out, outs = _packed([torch.zeros(n) for n in LENGTHS], dtype, 5)
+    flat_out, outs = _packed([torch.zeros(n) for n in lengths], dtype, 5)
     before = flat.clone()
     got_norm = float(optim.TensorList(views, outs=None if inplace else outs).clip_grads(max_norm, kind=kind, grad_scale=scale))
     norm = ref.norm(grads, kind, scale)
     assert abs(got_norm - norm) <= norm * ref.U * ref.SLACK
     c = ref.coef(norm, max_norm, scale)
-    for n, g, out in zip(LENGTHS, grads, views if inplace else outs):
+    for n, g, out in zip(lengths, grads, views if inplace else outs):
         ref.near(out, *ref.clip(g, c), f"length {n}")
     written = flat if inplace else flat_out
     assert (written[:5] == 7).all() and (written[-5:] == 7).all()
@@ -176,10 +178,9 @@ def _adam_lists(gen, sizes, ptype, gtype, masters, fresh):
 @pytest.mark.parametrize("ptype", TYPES)
 @pytest.mark.parametrize("gtype", TYPES)
 @pytest.mark.parametrize("masters", [False, True])
-@pytest.mark.parametrize("start", [0, 1000])
-def test_adamw(optim, ptype, gtype, masters, start):
+@pytest.mark.parametrize("start,sizes", [(0, LENGTHS), (1000, LENGTHS), (0, LENGTHS[:-2])])
+def test_adamw(optim, ptype, gtype, masters, start, sizes):
     gen = torch.Generator().manual_seed(5)
-    sizes = LENGTHS
     p, g, m, v, w = _adam_lists(gen, sizes, ptype, gtype, masters, start == 0)
     lead = 3
     flats, on = {}, {}
@@ -229,9 +230,10 @@ def test_adamw_of_zero_gradients_only_decays(optim):
     assert (p == 1.5).all()
 
 
-def test_adamw_skips_a_step_that_is_not_finite(optim):
+@pytest.mark.parametrize("more", [3, 100_000])
+def test_adamw_skips_a_step_that_is_not_finite(optim, more):
     gen = torch.Generator().manual_seed(7)
-    p = [_values(gen, n, BF16).to(DEV).requires_grad_(True) for n in (7, 5000)]
+    p = [_values(gen, n, BF16).to(DEV).requires_grad_(True) for n in (7, 5000, more)]
     opt = optim.AdamW(p, lr=0.1, skip_nonfinite=True, masters=True)
     for x in p:
         x.grad = torch.ones_like(x)
@@ -356,9 +358,9 @@ def test_calls_run_on_the_current_stream(optim):
     assert abs(float(lst.grad_norm()) - want) <= want * ref.U * ref.SLACK
 
 
-def test_a_captured_step_is_replayed(optim):
+@pytest.mark.parametrize("sizes", [[70_001, 3, 2048], [5, 9001]])
+def test_a_captured_step_is_replayed(optim, sizes):
     gen = torch.Generator().manual_seed(12)
-    sizes = [70_001, 3, 2048]
     host = [_values(gen, n, BF16) for n in sizes]
 
     def make():

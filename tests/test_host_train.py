@@ -119,7 +119,7 @@ S.stub_clear_launches()
 assert norm(h) == OK and clip(h) == OK and adamw(h, how()) == OK
 kinds = lambda ls: [l[0].split("<")[0] for l in ls]
 ls = launched()
-assert kinds(ls) == ["k_norm", "k_norm", "k_norm", "k_adamw"] and all(l[1][0] == 1 for l in ls)      # nothing to clip; the step counts
+assert kinds(ls) == ["k_norm_short", "k_clip_short", "k_adamw_short"] and all(l[1][0] == 1 for l in ls)      # norm 0; the step counts
 h = make([tensor(n=0, grad=None)] + 100 * [tensor(n=1)])
 assert [n for n in names() if n == "k_list_put"] == 3 * ["k_list_put"]       # 40 tensors at a time
 assert norm(h, 1) == OK and adamw(h, how(max_norm=math.inf), d=None) == OK and adamw(h, how(given=1)) == OK and clip(h, given=1, kind=9) == OK
