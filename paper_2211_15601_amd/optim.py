@@ -16,10 +16,14 @@ import ctypes
 import math
 from typing import Optional, Sequence
 
+import numpy as np
 import torch
 
 from . import binding
 
+# an fs_tensor, for whole columns of a list at once
+_COLUMNS = np.dtype([(n, np.uint64) for n in ("grad", "out", "param", "master", "exp_avg", "exp_avg_sq")] +
+                    [("n", np.int64), ("grad_type", np.int32), ("param_type", np.int32), ("lr_scale", np.float32), ("decay_scale", np.float32)])
 _TYPES = {torch.float32: binding.FS_FLOAT_FULL, torch.bfloat16: binding.FS_FLOAT_BRAIN, torch.float16: binding.FS_FLOAT_HALF}
 _KINDS = {"l2": binding.FS_NORM_TWO, "max": binding.FS_NORM_MAX}
 
@@ -50,16 +54,18 @@ def _check(what: str, i: int, t: torch.Tensor, like: Optional[torch.Tensor], dev
     if like is None:
         if t.layout != torch.strided or not _dense(t):
             raise ValueError(f"{what}[{i}]: elements must lie one after another in memory (use .contiguous())")
-    elif t.shape != like.shape or (t.numel() and _order(t) != _order(like)):
+    elif t.shape != like.shape or not (t.is_contiguous() and like.is_contiguous()) and t.numel() and _order(t) != _order(like):
         raise ValueError(f"{what}[{i}]: shape {tuple(t.shape)} and strides {t.stride()}, expected {tuple(like.shape)} and {like.stride()}")
 
 
 def _check_apart(arrays):
     """No two of the arrays may share memory: calls write some of them, block by block in no order."""
-    spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in arrays if t is not None and t.numel())
-    for (_, end), (begin, _) in zip(spans, spans[1:]):
-        if begin < end:
-            raise ValueError("tensors of the list overlap in memory")
+    arrays = [t for t in arrays if t is not None and t.numel()]
+    begin = np.array([t.data_ptr() for t in arrays], dtype=np.uint64)
+    end = begin + np.array([t.nbytes for t in arrays], dtype=np.uint64)
+    order = np.argsort(begin)
+    if (begin[order][1:] < end[order][:-1]).any():
+        raise ValueError("tensors of the list overlap in memory")
 
 
 class _Handle:
@@ -72,6 +78,8 @@ class _Handle:
         self.device = device if device.index is not None else torch.device("cuda", torch.cuda.current_device())
         self.count = count
         self.list = (binding.Tensor * max(1, count))()
+        self.columns = np.frombuffer(self.list, dtype=_COLUMNS)[:count]
+        self.columns["lr_scale"] = self.columns["decay_scale"] = 1.0
         self._h = None
 
     def put(self):
@@ -143,6 +151,14 @@ def _places(tensors):
     return [0 if t is None else t.data_ptr() for t in tensors]
 
 
+def _sizes(tensors):
+    return [0 if t is None else t.numel() for t in tensors]
+
+
+def _types(tensors):
+    return [0 if t is None else _TYPES[t.dtype] for t in tensors]
+
+
 class TensorList:
     """A list of gradients, and where their clipped values go (`outs`; without: in place).  Entries of `grads` may be None: they
     are left out.  The list keeps references to the tensors, and notices when their memory has moved."""
@@ -157,20 +173,20 @@ class TensorList:
         self._put()
 
     def _put(self):
-        h = self._handle
+        h, c = self._handle, self._handle.columns
+        for i, g in enumerate(self._grads):
+            if g is not None:
+                _check("grads", i, g, None, h.device, _TYPES)
         for i, (g, o) in enumerate(zip(self._grads, self._outs)):
-            e = h.list[i]
-            e.n = 0
-            if g is None:
-                continue
-            _check("grads", i, g, None, h.device, _TYPES)
-            if o is not None:
+            if g is not None and o is not None:
                 _check("outs", i, o, g, h.device, [g.dtype])
-            e.grad, e.out, e.n, e.grad_type = g.data_ptr(), None if o is None else o.data_ptr(), g.numel(), _TYPES[g.dtype]
         _check_apart(self._grads + [o for o, g in zip(self._outs, self._grads) if o is not None and g is not None and o.data_ptr() != g.data_ptr()])
         self._places = None
+        places = _places(self._watched)
+        c["grad"], c["out"] = places[:h.count], _places(self._outs)
+        c["n"], c["grad_type"] = _sizes(self._grads), _types(self._grads)
         h.put()
-        self._places = _places(self._watched)
+        self._places = places
 
     def _ready(self):
         if _places(self._watched) != self._places:
@@ -226,8 +242,7 @@ class AdamW:
         zeros = lambda: [torch.zeros_like(p, dtype=torch.float32, memory_format=torch.preserve_format, requires_grad=False) for p in self.params]
         (self.masters,) = _lists(n, masters=masters or None)
         self.exp_avgs, self.exp_avg_sqs = _lists(n, exp_avgs=zeros() if exp_avgs is None else exp_avgs, exp_avg_sqs=zeros() if exp_avg_sqs is None else exp_avg_sqs)
-        self._lr_scales, self._decay_scales = _lists(n, lr_scales=[1.0] * n if lr_scales is None else lr_scales,
-                                                     decay_scales=[1.0] * n if decay_scales is None else decay_scales)
+        lr_scales, decay_scales = _lists(n, lr_scales=[1.0] * n if lr_scales is None else lr_scales, decay_scales=[1.0] * n if decay_scales is None else decay_scales)
         for name, v in (("masters", self.masters), ("exp_avgs", self.exp_avgs), ("exp_avg_sqs", self.exp_avg_sqs)):
             for i, (t, p) in enumerate(zip(v, self.params)):
                 if t is not None or name != "masters":
@@ -243,20 +258,20 @@ class AdamW:
         self._straight = [p.is_contiguous() for p in self.params]
         self._places = None
         self._how = binding.AdamW()
+        c = h.columns
+        c["master"], c["exp_avg"], c["exp_avg_sq"] = _places(self.masters), _places(self.exp_avgs), _places(self.exp_avg_sqs)
+        c["param_type"], c["lr_scale"], c["decay_scale"] = _types(self.params), lr_scales, decay_scales
+        if self._given is not None:
+            self._put(self._given, _places(self._given) + _places(self.params))
 
     def _put(self, grads, now):
-        h = self._handle
+        h, c = self._handle, self._handle.columns
         for i, (g, p) in enumerate(zip(grads, self.params)):
-            e = h.list[i]
-            e.n, e.lr_scale, e.decay_scale = 0, float(self._lr_scales[i]), float(self._decay_scales[i])
-            if g is None:
-                continue
-            _check("grads", i, g, p, h.device, _TYPES)
-            w = self.masters[i]
-            e.grad, e.param, e.master = g.data_ptr(), p.data_ptr(), None if w is None else w.data_ptr()
-            e.exp_avg, e.exp_avg_sq = self.exp_avgs[i].data_ptr(), self.exp_avg_sqs[i].data_ptr()
-            e.n, e.grad_type, e.param_type = p.numel(), _TYPES[g.dtype], _TYPES[p.dtype]
+            if g is not None:
+                _check("grads", i, g, p, h.device, _TYPES)
         self._places = None
+        c["grad"], c["param"] = now[:h.count], now[h.count:]
+        c["n"], c["grad_type"] = _sizes(grads), _types(grads)
         h.put()
         self._places = now
 
