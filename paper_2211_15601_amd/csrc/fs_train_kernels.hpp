@@ -32,8 +32,12 @@ struct ListD {
     const TensorD *tensors;
     const int *first;                  // [count] first units, ascending
     int count, units;
-    int chunk;                         // units that a block takes at a time
+    int chunks;                        // parts that blocks take in turn, alike to a unit: part c begins at unit c step / 2^STEP_BITS
+    long long step;
 };
+
+constexpr int STEP_BITS = 20;
+__host__ __device__ inline int chunk_begin(const ListD &L, int c) { const long long u = c * L.step >> STEP_BITS; return u < L.units ? (int)u : L.units; }
 
 constexpr int PUT = 40;                // tensors that one launch of k_list_put carries in its arguments (3.2 KB of 4)
 struct PutD { TensorD t[PUT]; };
@@ -112,7 +116,7 @@ __device__ __forceinline__ Piece piece_of(const TensorD &t, long long from, long
 template <bool BACK, class F>
 __device__ __forceinline__ void walk(const ListD &L, F f)
 {
-    const int chunks = (int)(((long long)L.units + L.chunk - 1) / L.chunk);
+    const int chunks = L.chunks;
     int c = blockIdx.x;
     if (c >= chunks) return;
     const bool kept = (int)gridDim.x < chunks && L.count <= LIST_LDS;      // several chunks: the places are asked for more than once
@@ -122,7 +126,8 @@ __device__ __forceinline__ void walk(const ListD &L, F f)
         __syncthreads();
     }
     auto find = [&](int u) { return kept ? find_tensor(s_first, L.count, u) : find_tensor(L.first, L.count, u); };
-    int u = (BACK ? chunks - 1 - c : c) * L.chunk, end = min(u + L.chunk, L.units), i = find(u);
+    auto place = [&](int c) { return BACK ? chunks - 1 - c : c; };
+    int u = chunk_begin(L, place(c)), end = chunk_begin(L, place(c) + 1), i = find(u);
     TensorD t = tensor_at(L, i);
     for (;;) {
         const Piece p = piece_of(t, (long long)(u - t.first) * UNIT, (long long)(end - t.first) * UNIT);
@@ -134,8 +139,8 @@ __device__ __forceinline__ void walk(const ListD &L, F f)
             c += gridDim.x;
             more = c < chunks;
             if (more) {
-                u = (BACK ? chunks - 1 - c : c) * L.chunk;
-                end = min(u + L.chunk, L.units);
+                u = chunk_begin(L, place(c));
+                end = chunk_begin(L, place(c) + 1);
                 i = find(u);
             }
         }
@@ -291,7 +296,17 @@ __device__ __forceinline__ S sum_types(const TensorD &t, const Piece &p, S s)
     }
 }
 
+// Sums that blocks have left, joined by every thread's block in the same order.
+template <class S>
+__device__ __forceinline__ S join_parts(const S *part, int n)
+{
+    S s = 0;
+    for (int i = threadIdx.x; i < n; i += 256) s = join(s, __hip_atomic_load(part + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+    return block_join<4>(s);
+}
+
 // The first `streamed` chunks are read past the caches, the others stay there for a pass that comes from the other end.
+// norm == NULL: the blocks' sums stay in `partial`, and every block of the kernel behind this one joins them for itself (see norm_value()).
 template <int KIND>
 __global__ __launch_bounds__(256) void k_norm(ListD L, int streamed, double scale, double *__restrict__ partial, unsigned *__restrict__ tickets, float *__restrict__ norm)
 {
@@ -305,14 +320,30 @@ __global__ __launch_bounds__(256) void k_norm(ListD L, int streamed, double scal
     __shared__ bool last;
     if (threadIdx.x == 0) {
         __hip_atomic_store(part + blockIdx.x, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        last = is_last(take_ticket(tickets), tickets);
+        last = norm && is_last(take_ticket(tickets), tickets);
     }
     __syncthreads();
     if (!last) return;
-    s = 0;
-    for (unsigned i = threadIdx.x; i < gridDim.x; i += 256) s = join(s, __hip_atomic_load(part + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-    s = block_join<4>(s);
+    s = join_parts(part, gridDim.x);
     if (threadIdx.x == 0) *norm = (float)(Sum<KIND>::value(s) * scale);
+}
+
+// Where a kernel gets the norm from: `parts` sums of k_norm, which it joins and writes to `norm`; or, parts == 0, from `norm` (NULL: nothing asks for it).
+struct NormD {
+    const double *partial;
+    int parts, kind;
+    double scale;
+    float *norm;
+};
+
+__device__ __forceinline__ float norm_value(const NormD &N)
+{
+    if (N.parts == 0) return N.norm ? *N.norm : 0.0f;
+    const double v = N.kind == KIND_TWO ? Sum<KIND_TWO>::value(join_parts(N.partial, N.parts))
+                                        : Sum<KIND_MAX>::value(join_parts(reinterpret_cast<const unsigned *>(N.partial), N.parts));
+    const float n = (float)(v * N.scale);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *N.norm = n;
+    return n;
 }
 
 // ---- short lists ----
@@ -386,9 +417,9 @@ __device__ __forceinline__ void scale_types(const TensorD &t, const Piece &p, fl
     }
 }
 
-__global__ __launch_bounds__(256) void k_clip(ListD L, int all_in_place, double max_norm, double scale, const float *__restrict__ norm)
+__global__ __launch_bounds__(256) void k_clip(ListD L, NormD N, int all_in_place, double max_norm, double scale)
 {
-    const float coef = clip_coef(*norm, max_norm, scale);
+    const float coef = clip_coef(norm_value(N), max_norm, scale);
     if (all_in_place && coef == 1.0f) return;
     walk<true>(L, [&](const TensorD &t, const Piece &p, int) { scale_types<true, 256, AHEAD_CLIP>(t, p, coef); });
 }
@@ -556,11 +587,9 @@ __device__ __forceinline__ void adam_types(const TensorD &t, const Piece &p, con
 
 __device__ __forceinline__ bool is_finite(float x) { return __builtin_fabsf(x) < __builtin_inff(); }
 
-// norm: of the gradients, or NULL where nothing asks for it
-__global__ __launch_bounds__(256) void k_adamw(ListD L, AdamD A, const float *__restrict__ lr_word, const float *__restrict__ norm,
-                                               long long *__restrict__ steps, unsigned *__restrict__ tickets)
+__global__ __launch_bounds__(256) void k_adamw(ListD L, AdamD A, NormD N, const float *__restrict__ lr_word, long long *__restrict__ steps, unsigned *__restrict__ tickets)
 {
-    const float n = norm ? *norm : 0.0f;
+    const float n = norm_value(N);
     if (A.skip_nonfinite && !is_finite(n)) return;         // every block sees the same norm
     __shared__ AdamC shared;
     StepD step;
