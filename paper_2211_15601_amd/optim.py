@@ -8,7 +8,7 @@ tensors, clipping, and the AdamW step.
 
 Tensors are float32, bfloat16 or float16 on one GPU, of any size and alignment, dense (any order of dimensions, without
 gaps); moments and masters are float32.  Results stay on the GPU and nothing waits for it.  Calls run on the stream that is current
-when they are made.  Argument marshalling only: the arithmetic runs in the HIP kernels.  There is no CPU fallback.
+when they are made, and can be captured into a graph (after one call outside of it).  Argument marshalling only: the arithmetic runs in the HIP kernels.  There is no CPU fallback.
 """
 from __future__ import annotations
 
@@ -69,7 +69,10 @@ def _check_apart(arrays):
 
 
 class _Handle:
-    """An fs_tensors, its host list and its stream.  Holds no tensors."""
+    """An fs_tensors, its host list and its stream.  Holds no tensors.
+
+    A captured graph reads the list's copy on the device when it is replayed.  An fs_tensors that was captured therefore keeps its list, and is never
+    destroyed: when the list changes afterwards, another takes its place."""
 
     def __init__(self, count: int, device: torch.device):
         self.L = binding.load()
@@ -81,34 +84,48 @@ class _Handle:
         self.columns = np.frombuffer(self.list, dtype=_COLUMNS)[:count]
         self.columns["lr_scale"] = self.columns["decay_scale"] = 1.0
         self._h = None
+        self.captured = False          # a graph has calls on it
+        self.recorded = False          # the last put was recorded, not run
+
+    def ready(self, put, unchanged: bool):
+        """Before a call: put() if the list has changed, and the stream."""
+        capturing = torch.cuda.is_current_stream_capturing()
+        if not unchanged or (self.recorded and not capturing):
+            put()
+        self.on_stream(capturing)
+        self.captured = self.captured or capturing
 
     def put(self):
         """Hands the list over: the first time, or after it has changed."""
-        if self._h is not None:
-            self.on_stream()
+        capturing = torch.cuda.is_current_stream_capturing()
+        if self._h is not None and not self.captured:
+            self.on_stream(capturing)
             self.ret(self.L.fs_tensors_update(self._h, self.list, self.count))
+            self.recorded = capturing
             return
+        if capturing:
+            raise RuntimeError("a list has to be made, and used with tensors that do not move from one graph to the next, before a graph is captured")
         h = ctypes.c_void_p()
         with torch.cuda.device(self.device):
-            self._stream = torch.cuda.current_stream(self.device)
-            self._raw = self._stream.cuda_stream
-            st = self.L.fs_tensors_create(self.list, self.count, self._raw, ctypes.byref(h))
+            stream = torch.cuda.current_stream(self.device)
+            st = self.L.fs_tensors_create(self.list, self.count, stream.cuda_stream, ctypes.byref(h))
         if st != binding.FS_OK:
             raise binding.FsError(st, "fs_tensors_create failed")
-        self._h = h
+        self._h, self._stream, self._raw = h, stream, stream.cuda_stream
+        self.captured = self.recorded = False
 
     def ret(self, st):
         if st != binding.FS_OK:
             raise binding.FsError(st, self.L.fs_tensors_error(self._h).decode())
 
-    def on_stream(self):
+    def on_stream(self, capturing):
         # torch.cuda.current_stream makes an object, 2 us of the 7 that a call takes the host; this is what compiled code of torch's own asks
         if torch._C._cuda_getCurrentRawStream(self.device.index) == self._raw:
             return
         now = torch.cuda.current_stream(self.device)
         # the list's scratch is one: this stream's calls come after those of the stream before.  A stream that records a graph cannot wait
         # for work outside of it; torch.cuda.graph waits for the whole device before it records.
-        if not torch.cuda.is_current_stream_capturing():
+        if not capturing:
             now.wait_stream(self._stream)
         self._stream, self._raw = now, now.cuda_stream
         self.ret(self.L.fs_tensors_set_stream(self._h, self._raw))
@@ -124,7 +141,7 @@ class _Handle:
 
     def __del__(self):
         try:
-            if self._h is not None:
+            if self._h is not None and not self.captured:
                 self.L.fs_tensors_destroy(self._h)
                 self._h = None
         except Exception:
@@ -189,9 +206,7 @@ class TensorList:
         self._places = places
 
     def _ready(self):
-        if _places(self._watched) != self._places:
-            self._put()
-        self._handle.on_stream()
+        self._handle.ready(self._put, _places(self._watched) == self._places)
 
     def grad_norm(self, kind: str = "l2", grad_scale: float = 1.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Global norm of the gradients times grad_scale, float32 [1]: "l2", or "max", the largest magnitude."""
@@ -254,13 +269,17 @@ class AdamW:
         self._given = None
         if grads is not None:
             (self._given,) = _lists(n, grads=grads)
-        _check_apart(self.params + self.masters + self.exp_avgs + self.exp_avg_sqs + (self._given or []))
         self._straight = [p.is_contiguous() for p in self.params]
         self._places = None
         self._how = binding.AdamW()
         c = h.columns
         c["master"], c["exp_avg"], c["exp_avg_sq"] = _places(self.masters), _places(self.exp_avgs), _places(self.exp_avg_sqs)
         c["param_type"], c["lr_scale"], c["decay_scale"] = _types(self.params), lr_scales, decay_scales
+        if self._given is not None:
+            for i, (g, p) in enumerate(zip(self._given, self.params)):
+                if g is not None:
+                    _check("grads", i, g, p, h.device, _TYPES)
+        _check_apart(self.params + self.masters + self.exp_avgs + self.exp_avg_sqs + (self._given or []))
         if self._given is not None:
             self._put(self._given, _places(self._given) + _places(self.params))
 
@@ -286,9 +305,7 @@ class AdamW:
         grads = self._given if self._given is not None else [p.grad for p in self.params]
         now = _places(grads) + _places(self.params)
         # gradients that are not held here may have been replaced by others at the same place
-        if now != self._places or (self._given is None and not all(self._alike(g, p, s) for g, p, s in zip(grads, self.params, self._straight))):
-            self._put(grads, now)
-        h.on_stream()
+        h.ready(lambda: self._put(grads, now), now == self._places and (self._given is not None or all(map(self._alike, grads, self.params, self._straight))))
         asked = norm is not None or self.max_norm is not None or self.skip_nonfinite
         d = h.norm(norm) if asked else None
         if isinstance(self.lr, torch.Tensor):

@@ -388,6 +388,68 @@ def test_a_captured_step_is_replayed(optim, sizes):
             assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("n", [9001, 300_001])
+def test_graphs_and_eager_steps_keep_apart(optim, n):
+    """Gradients that lie elsewhere in the graph and outside of it: neither works on the other's."""
+    p = torch.zeros(n, device=DEV, requires_grad=True)
+    opt = optim.AdamW([p], lr=1.0, betas=(0.0, 0.0), eps=0.0, weight_decay=0.0)      # p goes by the gradient's sign
+    outside = torch.ones(n, device=DEV)
+    p.grad = outside
+    opt.step()
+    graph = torch.cuda.CUDAGraph()
+    p.grad = None
+    with torch.cuda.graph(graph):
+        (p * -2.0).sum().backward()
+        inside = p.grad
+        opt.step()
+    assert inside.data_ptr() != outside.data_ptr()
+    torch.cuda.synchronize()
+    assert (p == -1).all()
+    p.grad = outside
+    opt.step()                                              # before the graph has ever run
+    assert (p == -2).all()
+    for k in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert (p == -1 - k).all()
+        opt.step(), opt.step()
+        assert (p == -3 - k).all()
+    moved = torch.full_like(outside, -1.0)
+    p.grad = moved
+    opt.step()
+    assert (p == -4).all()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert (p == -3).all() and int(opt.step_count) == 13
+
+
+def test_a_list_is_not_made_while_a_graph_is_captured(optim):
+    g = torch.ones(100, device=DEV)
+    x = torch.zeros(3, device=DEV)
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        x.add_(1.0)
+        with pytest.raises(RuntimeError, match="before a graph is captured"):
+            optim.TensorList([g])
+
+
+def test_arrays_that_are_aligned_differently(optim):
+    gen = torch.Generator().manual_seed(13)
+    n = 50_003
+    for short in (False, True):
+        m = n if not short else 5003
+        host = {"p": _values(gen, m, BF16), "g": _values(gen, m, F16), "m": _values(gen, m, F32, 0.1), "v": torch.rand(m, generator=gen), "w": _values(gen, m, F32)}
+        on = {k: _packed([x], x.dtype, 1 + 2 * i)[1] for i, (k, x) in enumerate(host.items())}
+        opt = optim.AdamW(on["p"], grads=on["g"], lr=0.01, max_norm=1.0, masters=on["w"], exp_avgs=on["m"], exp_avg_sqs=on["v"], step=torch.tensor([9], device=DEV))
+        opt.step()
+        c = ref.coef(ref.norm([host["g"]]), 1.0)
+        want = ref.adamw(host["p"], host["g"], host["m"], host["v"], 10, c, 0.01, (0.9, 0.999), 1e-8, 0.01, master=host["w"])
+        for key, name in (("exp_avg", "m"), ("exp_avg_sq", "v"), ("param", "p"), ("master", "w")):
+            ref.near(on[name][0], *want[key], key)
+        out = _packed([torch.zeros(m)], F16, 7)[1]
+        optim.TensorList(on["g"], outs=out).clip_grads(1.0)
+        ref.near(out[0], *ref.clip(host["g"], c))
+
+
 # ---- refusals that need tensors on a GPU ----
 
 def test_refusals(optim):
