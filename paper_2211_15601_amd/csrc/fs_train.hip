@@ -213,7 +213,7 @@ bool is_short(const fs_tensors *t) { return t->L.units <= SHORT_UNITS; }
 int short_blocks(const fs_tensors *t) { return std::max(1, (t->L.units * (UNIT / SHORT_PART) + SHORT_WAVES - 1) / SHORT_WAVES); }
 
 // Bytes at the end of the gradients that the norm leaves in the caches (256 MiB of them in front of the memory), for the pass behind it, which comes from that
-// end.  What is before them streams: 400 M fp32 then take 234 us, not 259.  Measured with 64 / 128 / 192 / 240 MB, clipping 250 M fp32: 512 / 490 / 497 / 492 us.
+// end (none for a norm alone).  What is before them streams: 400 M fp32 then take 234 us, not 259, and 228 where all of it streams.  Measured with 64 / 128 / 192 / 240 MB, clipping 250 M fp32: 512 / 490 / 497 / 492 us.
 constexpr double KEPT_BYTES = 192e6;
 
 // The norm into d_norm, or, d_norm == NULL, as sums for the kernel behind it: their number is returned.
@@ -225,7 +225,7 @@ int launch_norm(fs_tensors *t, int32_t kind, double scale, float *d_norm)
         return 0;
     }
     const Grid g = grid_for(t, NORM);
-    const int streamed = t->grad_bytes > KEPT_BYTES ? (int)(g.L.chunks * (1.0 - KEPT_BYTES / t->grad_bytes)) : 0;
+    const int streamed = t->grad_bytes > KEPT_BYTES ? (d_norm ? g.L.chunks : (int)(g.L.chunks * (1.0 - KEPT_BYTES / t->grad_bytes))) : 0;
     if (kind == FS_NORM_TWO) k_norm<KIND_TWO><<<g.blocks, 256, 0, t->stream>>>(g.L, streamed, scale, t->partial, t->tickets, d_norm);
     else k_norm<KIND_MAX><<<g.blocks, 256, 0, t->stream>>>(g.L, streamed, scale, t->partial, t->tickets, d_norm);
     return g.blocks;

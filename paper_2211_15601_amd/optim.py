@@ -269,12 +269,11 @@ class AdamW:
         self._given = None
         if grads is not None:
             (self._given,) = _lists(n, grads=grads)
-        self._straight = [p.is_contiguous() for p in self.params]
         self._places = None
-        self._how = binding.AdamW()
+        self._how, self._set_to = binding.AdamW(), None
         c = h.columns
         c["master"], c["exp_avg"], c["exp_avg_sq"] = _places(self.masters), _places(self.exp_avgs), _places(self.exp_avg_sqs)
-        c["param_type"], c["lr_scale"], c["decay_scale"] = _types(self.params), lr_scales, decay_scales
+        c["lr_scale"], c["decay_scale"] = lr_scales, decay_scales
         if self._given is not None:
             for i, (g, p) in enumerate(zip(self._given, self.params)):
                 if g is not None:
@@ -287,16 +286,20 @@ class AdamW:
         h, c = self._handle, self._handle.columns
         for i, (g, p) in enumerate(zip(grads, self.params)):
             if g is not None:
+                _check("params", i, p, None, h.device, _TYPES)
+                _check("exp_avgs", i, self.exp_avgs[i], p, h.device, [torch.float32])
                 _check("grads", i, g, p, h.device, _TYPES)
         self._places = None
         c["grad"], c["param"] = now[:h.count], now[h.count:]
-        c["n"], c["grad_type"] = _sizes(grads), _types(grads)
+        c["n"], c["grad_type"], c["param_type"] = _sizes(grads), _types(grads), _types(self.params)
+        self._looks = self._look(grads)
         h.put()
         self._places = now
 
     @staticmethod
-    def _alike(g, p, straight):
-        return g is None or (g.dtype == p.dtype and (g.is_contiguous() if straight else _order(g) == _order(p)))
+    def _look(grads):
+        """What gradients could have other than those before them at the same place, apart from the shape, which a parameter prescribes."""
+        return [None if g is None else (g.dtype, g.is_contiguous() or g.stride()) for g in grads]
 
     def step(self, norm: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
         """One step.  Returns the gradients' global norm, float32 [1] (None where neither max_norm nor skip_nonfinite asks for it); a
@@ -305,18 +308,25 @@ class AdamW:
         grads = self._given if self._given is not None else [p.grad for p in self.params]
         now = _places(grads) + _places(self.params)
         # gradients that are not held here may have been replaced by others at the same place
-        h.ready(lambda: self._put(grads, now), now == self._places and (self._given is not None or all(map(self._alike, grads, self.params, self._straight))))
+        h.ready(lambda: self._put(grads, now), now == self._places and (self._given is not None or self._look(grads) == self._looks))
         asked = norm is not None or self.max_norm is not None or self.skip_nonfinite
         d = h.norm(norm) if asked else None
-        if isinstance(self.lr, torch.Tensor):
-            _check("lr", 0, self.lr, None, h.device, [torch.float32])
-            how.lr, how.d_lr = 0.0, self.lr.data_ptr()
+        lr = self.lr
+        if isinstance(lr, torch.Tensor):
+            _check("lr", 0, lr, None, h.device, [torch.float32])
+            if lr.numel() != 1:
+                raise ValueError("lr must have one element")
+            how.d_lr, lr = lr.data_ptr(), 0.0
         else:
-            how.lr, how.d_lr = self.lr, None
-        how.beta1, how.beta2 = self.betas
-        how.eps, how.weight_decay, how.grad_scale = self.eps, self.weight_decay, self.grad_scale
-        how.max_norm = math.inf if self.max_norm is None else self.max_norm
-        how.norm_given, how.skip_nonfinite = norm is not None, bool(self.skip_nonfinite)
+            how.d_lr = None
+        set_to = (lr, self.betas, self.eps, self.weight_decay, self.grad_scale, self.max_norm, self.skip_nonfinite, norm is not None)
+        if set_to != self._set_to:
+            self._set_to = None
+            how.lr, (how.beta1, how.beta2) = lr, self.betas
+            how.eps, how.weight_decay, how.grad_scale = self.eps, self.weight_decay, self.grad_scale
+            how.max_norm = math.inf if self.max_norm is None else self.max_norm
+            how.norm_given, how.skip_nonfinite = norm is not None, bool(self.skip_nonfinite)
+            self._set_to = set_to
         h.ret(h.L.fs_adamw_step(h._h, ctypes.byref(how), self.step_count.data_ptr(), d.data_ptr() if asked else None))
         torch.autograd.graph.increment_version(self.params)       # autograd has to notice that they have changed
         return d

@@ -267,6 +267,14 @@ def test_adamw_reads_the_rate_and_the_norm_from_the_device(optim):
     rate.fill_(0.0)
     opt.step(norm=norm)
     assert torch.equal(now, on.cpu())
+    # settings that change between steps: a number in its place, then another, no limit
+    opt.lr, opt.weight_decay = 1.0, 0.0
+    opt.step(norm=norm)
+    first = (on.cpu() - now).abs().max()
+    opt.lr, opt.max_norm = 0.5, None
+    now = on.cpu()
+    assert opt.step() is None
+    assert 0 < (on.cpu() - now).abs().max() < first
 
 
 def test_parameters_without_gradients_and_gradients_that_move(optim):
@@ -294,6 +302,24 @@ def test_parameters_without_gradients_and_gradients_that_move(optim):
                 continue
             want = ref.adamw(before[i], p[i].grad.cpu(), *state[i], t, 1.0, 0.1, (0.9, 0.999), 1e-8, 0.0)
             ref.near(p[i], *want["param"], f"tensor {i}, step {t}")
+
+
+def test_parameters_that_change_their_type(optim):
+    """As Module.bfloat16() does it, between two steps."""
+    gen = torch.Generator().manual_seed(14)
+    m = torch.nn.Linear(37, 53).to(DEV)
+    opt = optim.AdamW(list(m.parameters()), lr=0.1)
+    for dtype in (F32, BF16, BF16, F32):
+        m.to(dtype)
+        x = torch.randn(5, 37, generator=gen).to(DEV, dtype)
+        for p in m.parameters():
+            p.grad = None
+        m(x).square().sum().backward()
+        before = [(p.detach().cpu(), a.cpu(), b.cpu()) for p, a, b in zip(m.parameters(), opt.exp_avgs, opt.exp_avg_sqs)]
+        t = int(opt.step_count) + 1
+        opt.step()
+        for p, (old, a, b) in zip(m.parameters(), before):
+            ref.near(p, *ref.adamw(old, p.grad.cpu(), a, b, t, 1.0, 0.1, (0.9, 0.999), 1e-8, 0.01)["param"], f"{dtype}, step {t}")
 
 
 def test_state_goes_on(optim):
