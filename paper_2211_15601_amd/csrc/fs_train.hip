@@ -21,7 +21,7 @@ struct fs_tensors {
     TensorD *host;            // [asked] those with elements, as they are on the device
     // what the tensors as a whole have
     bool params, moments, apart, in_place;      // in_place, apart: every `out` is, or none is, its gradient
-    double grad_bytes;
+    double grad_bytes, adam_bytes, param_bytes;
     ListD L;
     char *mem;                // device: TensorD [asked], int [asked + 1], double [TRAIN_BLOCKS], unsigned [TICKETS]
     double *partial;
@@ -130,7 +130,7 @@ fs_status put_list(fs_tensors *t, const char *what, const fs_tensor *list)
 {
     int count = 0, units = 0;
     t->params = t->moments = t->apart = t->in_place = true;
-    t->grad_bytes = 0.0;
+    t->grad_bytes = t->adam_bytes = t->param_bytes = 0.0;
     for (int32_t i = 0; i < t->asked; ++i) {
         const fs_tensor &x = t->given[i] = list[i];
         if (x.n == 0) continue;
@@ -154,6 +154,8 @@ fs_status put_list(fs_tensors *t, const char *what, const fs_tensor *list)
         t->apart = t->apart && d.out != d.grad;
         t->in_place = t->in_place && d.out == d.grad;
         t->grad_bytes += (double)x.n * size_of(x.grad_type);
+        if (x.param) t->param_bytes += (double)x.n * size_of(x.param_type);
+        if (x.param) t->adam_bytes += (double)x.n * (size_of(x.grad_type) + 16 + (x.master ? 8 : size_of(x.param_type)) + size_of(x.param_type));
     }
     t->L.count = count;
     t->L.units = units;
@@ -215,6 +217,12 @@ int short_blocks(const fs_tensors *t) { return std::max(1, (t->L.units * (UNIT /
 // Bytes at the end of the gradients that the norm leaves in the caches (256 MiB of them in front of the memory), for the pass behind it, which comes from that
 // end (none for a norm alone).  What is before them streams: 400 M fp32 then take 234 us, not 259, and 228 where all of it streams.  Measured with 64 / 128 / 192 / 240 MB, clipping 250 M fp32: 512 / 490 / 497 / 492 us.
 constexpr double KEPT_BYTES = 192e6;
+
+// What a pass leaves in the caches, by the bytes that it reads and writes (of AdamW's parameters, by theirs alone).  Measured with three lists in turn, us.
+// Clipping, cached / past the caches: 5 M fp32 (40 MB) 15.6 / 17.1, 10 M 24.0 / 25.0, 20 M 50.6 / 43.5, 250 M 534 / 498.  AdamW, all cached / all but the
+// parameters past the caches / all of it: 5 M fp32 (140 MB, 20 of parameters) 32.2 / 34.1 / 35.5, 10 M 67 / 57 / 60, 20 M 124 / 107 / 110, 40 M 248 / 221 / 208, 160 M
+// 968 / 939 / 880; bf16 with masters 5 M 31.8 / 36.7 / 37.4, 20 M 122 / 107 / 112, 40 M (80 MB of parameters) 236 / 208 / 212, 160 M 933 / 861 / 842.
+constexpr double CLIP_CACHED_BYTES = 112e6, ADAM_CACHED_BYTES = 192e6, ADAM_PARAM_BYTES = 96e6;
 
 // The norm into d_norm, or, d_norm == NULL, as sums for the kernel behind it: their number is returned.
 int launch_norm(fs_tensors *t, int32_t kind, double scale, float *d_norm)
@@ -341,7 +349,8 @@ fs_status fs_grad_clip(fs_tensors *t, int32_t kind, double max_norm, double grad
     }
     const NormD N = {t->partial, norm_given ? 0 : launch_norm(t, kind, grad_scale, nullptr), kind, grad_scale, d_norm};
     const Grid g = grid_for(t, CLIP);
-    k_clip<<<g.blocks, 256, 0, t->stream>>>(g.L, N, t->in_place, max_norm, grad_scale);
+    if (2.0 * t->grad_bytes > CLIP_CACHED_BYTES) k_clip<true><<<g.blocks, 256, 0, t->stream>>>(g.L, N, t->in_place, max_norm, grad_scale);
+    else k_clip<false><<<g.blocks, 256, 0, t->stream>>>(g.L, N, t->in_place, max_norm, grad_scale);
     return launch_status(t, "fs_grad_clip");
 }
 
@@ -384,7 +393,9 @@ fs_status fs_adamw_step(fs_tensors *t, const fs_adamw *how, int64_t *d_step, flo
     }
     const NormD N = {t->partial, computed ? launch_norm(t, FS_NORM_TWO, h.grad_scale, nullptr) : 0, FS_NORM_TWO, h.grad_scale, d_norm};
     const Grid g = grid_for(t, ADAMW);
-    k_adamw<<<g.blocks, 256, 0, t->stream>>>(g.L, A, N, h.d_lr, steps, t->tickets);
+    if (t->param_bytes > ADAM_PARAM_BYTES) k_adamw<ADAM_STREAM><<<g.blocks, 256, 0, t->stream>>>(g.L, A, N, h.d_lr, steps, t->tickets);
+    else if (t->adam_bytes > ADAM_CACHED_BYTES) k_adamw<ADAM_PARAM><<<g.blocks, 256, 0, t->stream>>>(g.L, A, N, h.d_lr, steps, t->tickets);
+    else k_adamw<ADAM_CACHED><<<g.blocks, 256, 0, t->stream>>>(g.L, A, N, h.d_lr, steps, t->tickets);
     return launch_status(t, "fs_adamw_step");
 }
 

@@ -417,11 +417,12 @@ __device__ __forceinline__ void scale_types(const TensorD &t, const Piece &p, fl
     }
 }
 
+template <bool STREAM>
 __global__ __launch_bounds__(256) void k_clip(ListD L, NormD N, int all_in_place, double max_norm, double scale)
 {
     const float coef = clip_coef(norm_value(N), max_norm, scale);
     if (all_in_place && coef == 1.0f) return;
-    walk<true>(L, [&](const TensorD &t, const Piece &p, int) { scale_types<true, 256, AHEAD_CLIP>(t, p, coef); });
+    walk<true>(L, [&](const TensorD &t, const Piece &p, int) { scale_types<STREAM, 256, AHEAD_CLIP>(t, p, coef); });
 }
 
 // Not in place: a block may have written while another still adds up.
@@ -464,6 +465,9 @@ struct Place {
     Vec<P, N> p;
 };
 
+// What goes past the caches: nothing; all but the parameters, which the next forward pass reads; or all.
+enum { ADAM_CACHED, ADAM_PARAM, ADAM_STREAM };
+
 struct AdamT { float coef, fade, step, inv_sqrt2, beta1, beta2, rest1, rest2, eps; };      // of one tensor
 
 template <class P, class G, bool MASTER>
@@ -472,9 +476,10 @@ struct Arrays {
     Global<P> p;
     Global<float> m, v, w;
 
-    template <bool STREAM, int N>
+    template <int MODE, int N>
     __device__ __forceinline__ void get(long long i, Place<P, G, MASTER, N> &x) const
     {
+        constexpr bool STREAM = MODE != ADAM_CACHED;
         x.g = load<STREAM, G, N>(g + i);
         x.m = load<STREAM, float, N>(m + i);
         x.v = load<STREAM, float, N>(v + i);
@@ -482,7 +487,7 @@ struct Arrays {
         else x.p = load<STREAM, P, N>(p + i);
     }
     // Everything in fp32; the parameter in 16 bits is rounded once, from the new value.
-    template <bool STREAM, int N>
+    template <int MODE, int N>
     __device__ __forceinline__ void update(long long i, Place<P, G, MASTER, N> &x, const AdamT &A) const
     {
 #pragma unroll
@@ -495,14 +500,15 @@ struct Arrays {
             if (MASTER) x.w[e] = now;
             x.p[e] = (P)now;
         }
+        constexpr bool STREAM = MODE != ADAM_CACHED;
         store<STREAM, float, N>(m + i, x.m);
         store<STREAM, float, N>(v + i, x.v);
         if (MASTER) store<STREAM, float, N>(w + i, x.w);
-        store<STREAM, P, N>(p + i, x.p);
+        store<MODE == ADAM_STREAM, P, N>(p + i, x.p);
     }
 };
 
-template <bool STREAM, int TEAM, int AHEAD, class P, class G, bool MASTER>
+template <int MODE, int TEAM, int AHEAD, class P, class G, bool MASTER>
 __device__ __forceinline__ void adam_piece(const TensorD &t, const Piece &p, const AdamT &A)
 {
     constexpr int N = 4;                                   // 16 bytes of every fp32 array
@@ -513,39 +519,39 @@ __device__ __forceinline__ void adam_piece(const TensorD &t, const Piece &p, con
         Place<P, G, MASTER, N> x[AHEAD];
         if (all) {
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k) a.template get<STREAM>((j + k * TEAM) * N, x[k]);
+            for (int k = 0; k < AHEAD; ++k) a.template get<MODE>((j + k * TEAM) * N, x[k]);
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k) a.template update<STREAM>((j + k * TEAM) * N, x[k], A);
+            for (int k = 0; k < AHEAD; ++k) a.template update<MODE>((j + k * TEAM) * N, x[k], A);
         } else {
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k)
                 if (V.has(j + k * TEAM)) {
-                    a.template get<STREAM>((j + k * TEAM) * N, x[k]);
-                    a.template update<STREAM>((j + k * TEAM) * N, x[k], A);
+                    a.template get<MODE>((j + k * TEAM) * N, x[k]);
+                    a.template update<MODE>((j + k * TEAM) * N, x[k], A);
                 }
         }
     });
     if (V.edge) {
         Place<P, G, MASTER, 1> y;
-        a.template get<false>(V.at, y);
-        a.template update<false>(V.at, y, A);
+        a.template get<ADAM_CACHED>(V.at, y);
+        a.template update<ADAM_CACHED>(V.at, y, A);
     }
 }
 
-template <bool STREAM, int TEAM, int AHEAD, class P, class G>
+template <int MODE, int TEAM, int AHEAD, class P, class G>
 __device__ __forceinline__ void adam_master(const TensorD &t, const Piece &p, const AdamT &A)
 {
-    if (t.master) adam_piece<STREAM, TEAM, AHEAD, P, G, true>(t, p, A);
-    else adam_piece<STREAM, TEAM, AHEAD, P, G, false>(t, p, A);
+    if (t.master) adam_piece<MODE, TEAM, AHEAD, P, G, true>(t, p, A);
+    else adam_piece<MODE, TEAM, AHEAD, P, G, false>(t, p, A);
 }
 
-template <bool STREAM, int TEAM, int AHEAD, class P>
+template <int MODE, int TEAM, int AHEAD, class P>
 __device__ __forceinline__ void adam_grad(const TensorD &t, const Piece &p, const AdamT &A)
 {
     switch (t.types & 255) {
-    case TYPE_F32: adam_master<STREAM, TEAM, AHEAD, P, float>(t, p, A); break;
-    case TYPE_BF16: adam_master<STREAM, TEAM, AHEAD, P, __bf16>(t, p, A); break;
-    default: adam_master<STREAM, TEAM, AHEAD, P, _Float16>(t, p, A); break;
+    case TYPE_F32: adam_master<MODE, TEAM, AHEAD, P, float>(t, p, A); break;
+    case TYPE_BF16: adam_master<MODE, TEAM, AHEAD, P, __bf16>(t, p, A); break;
+    default: adam_master<MODE, TEAM, AHEAD, P, _Float16>(t, p, A); break;
     }
 }
 
@@ -573,20 +579,21 @@ __device__ __forceinline__ void adam_end(const StepD &s, long long *steps, unsig
     if ((threadIdx.x & 63) == 0 && is_last(s.ticket, tickets)) *steps = s.before + 1;
 }
 
-template <bool STREAM, int TEAM, int AHEAD>
+template <int MODE, int TEAM, int AHEAD>
 __device__ __forceinline__ void adam_types(const TensorD &t, const Piece &p, const AdamD &A, const AdamC &C)
 {
     const float lr = C.rate * t.lr_scale;
     const AdamT T = {C.coef, lr * (A.decay * t.decay_scale), lr * C.inv1, C.inv_sqrt2, A.beta1, A.beta2, A.rest1, A.rest2, A.eps};
     switch (t.types >> 8) {
-    case TYPE_F32: adam_grad<STREAM, TEAM, AHEAD, float>(t, p, T); break;
-    case TYPE_BF16: adam_grad<STREAM, TEAM, AHEAD, __bf16>(t, p, T); break;
-    default: adam_grad<STREAM, TEAM, AHEAD, _Float16>(t, p, T); break;
+    case TYPE_F32: adam_grad<MODE, TEAM, AHEAD, float>(t, p, T); break;
+    case TYPE_BF16: adam_grad<MODE, TEAM, AHEAD, __bf16>(t, p, T); break;
+    default: adam_grad<MODE, TEAM, AHEAD, _Float16>(t, p, T); break;
     }
 }
 
 __device__ __forceinline__ bool is_finite(float x) { return __builtin_fabsf(x) < __builtin_inff(); }
 
+template <int MODE>
 __global__ __launch_bounds__(256) void k_adamw(ListD L, AdamD A, NormD N, const float *__restrict__ lr_word, long long *__restrict__ steps, unsigned *__restrict__ tickets)
 {
     const float n = norm_value(N);
@@ -598,7 +605,7 @@ __global__ __launch_bounds__(256) void k_adamw(ListD L, AdamD A, NormD N, const 
     __syncthreads();
     AdamC C = shared;
     C.coef = clip_coef(n, A.max_norm, A.scale);
-    walk<true>(L, [&](const TensorD &t, const Piece &p, int) { adam_types<true, 256, AHEAD_ADAMW>(t, p, A, C); });
+    walk<true>(L, [&](const TensorD &t, const Piece &p, int) { adam_types<MODE, 256, AHEAD_ADAMW>(t, p, A, C); });
     if (first) adam_end(step, steps, tickets);
 }
 
@@ -617,7 +624,7 @@ __global__ __launch_bounds__(SHORT_THREADS) void k_adamw_short(ListD L, AdamD A,
     if (!skip) {
         AdamC C = shared;
         C.coef = clip_coef(n, A.max_norm, A.scale);
-        walk_short<SHORT_PART>(L, blockIdx.x * SHORT_WAVES + wave, gridDim.x * SHORT_WAVES, [&](const TensorD &t, const Piece &p) { adam_types<false, 64, 1>(t, p, A, C); });
+        walk_short<SHORT_PART>(L, blockIdx.x * SHORT_WAVES + wave, gridDim.x * SHORT_WAVES, [&](const TensorD &t, const Piece &p) { adam_types<ADAM_CACHED, 64, 1>(t, p, A, C); });
     }
     if (last_wave) {
         if (skip) step.before -= 1;                        // the tickets were taken; the counter keeps its value

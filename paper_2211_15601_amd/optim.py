@@ -89,17 +89,22 @@ class _Handle:
 
     def ready(self, put, unchanged: bool):
         """Before a call: put() if the list has changed, and the stream."""
-        capturing = torch.cuda.is_current_stream_capturing()
+        # torch.cuda.current_stream makes an object, 2 us of the 7 that a call takes the host; this is what compiled code of torch's own asks
+        raw = torch._C._cuda_getCurrentRawStream(self.device.index)
+        capturing = raw != 0 and torch.cuda.is_current_stream_capturing()      # the default stream is none that can be captured
         if not unchanged or (self.recorded and not capturing):
             put()
-        self.on_stream(capturing)
-        self.captured = self.captured or capturing
+        if raw != self._raw:
+            self.to_stream(capturing)
+        if capturing:
+            self.captured = True
 
     def put(self):
         """Hands the list over: the first time, or after it has changed."""
         capturing = torch.cuda.is_current_stream_capturing()
         if self._h is not None and not self.captured:
-            self.on_stream(capturing)
+            if torch._C._cuda_getCurrentRawStream(self.device.index) != self._raw:
+                self.to_stream(capturing)
             self.ret(self.L.fs_tensors_update(self._h, self.list, self.count))
             self.recorded = capturing
             return
@@ -118,10 +123,7 @@ class _Handle:
         if st != binding.FS_OK:
             raise binding.FsError(st, self.L.fs_tensors_error(self._h).decode())
 
-    def on_stream(self, capturing):
-        # torch.cuda.current_stream makes an object, 2 us of the 7 that a call takes the host; this is what compiled code of torch's own asks
-        if torch._C._cuda_getCurrentRawStream(self.device.index) == self._raw:
-            return
+    def to_stream(self, capturing):
         now = torch.cuda.current_stream(self.device)
         # the list's scratch is one: this stream's calls come after those of the stream before.  A stream that records a graph cannot wait
         # for work outside of it; torch.cuda.graph waits for the whole device before it records.
