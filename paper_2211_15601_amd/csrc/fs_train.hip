@@ -26,6 +26,7 @@ struct fs_tensors {
     char *mem;                // device: TensorD [asked], int [asked + 1], double [TRAIN_BLOCKS], unsigned [TICKETS]
     double *partial;
     unsigned *tickets;
+    bool put;                 // the device's copy is that of `host`
     const void *seen[8];      // words (d_norm, d_step, d_lr) that are known to be memory of the device, by address
     char err[256];
 };
@@ -128,6 +129,7 @@ int lead_of(const fs_tensor &x)
 // Takes a checked list over: the host's copies, and the device's in the stream's order.
 fs_status put_list(fs_tensors *t, const char *what, const fs_tensor *list)
 {
+    t->put = false;
     int count = 0, units = 0;
     t->params = t->moments = t->apart = t->in_place = true;
     t->grad_bytes = t->adam_bytes = t->param_bytes = 0.0;
@@ -165,7 +167,9 @@ fs_status put_list(fs_tensors *t, const char *what, const fs_tensor *list)
         std::memcpy(p.t, t->host + at, n * sizeof(TensorD));
         k_list_put<<<1, 64, 0, t->stream>>>(p, at, n, const_cast<TensorD *>(t->L.tensors), const_cast<int *>(t->L.first));
     }
-    return launch_status(t, what);
+    const fs_status s = launch_status(t, what);
+    t->put = s == FS_OK;
+    return s;
 }
 
 fs_status on_current_device(fs_tensors *t, const char *what)
@@ -178,11 +182,12 @@ fs_status on_current_device(fs_tensors *t, const char *what)
     return FS_OK;
 }
 
-#define FS_TRAIN_BEGIN(t)                                                 \
-    do {                                                                  \
-        if (!(t)) return FS_E_ARG;                                        \
-        const fs_status begin_status = on_current_device((t), __func__);  \
-        if (begin_status != FS_OK) return begin_status;                   \
+#define FS_TRAIN_BEGIN(t, needs_list)                                                                                     \
+    do {                                                                                                                  \
+        if (!(t)) return FS_E_ARG;                                                                                        \
+        const fs_status begin_status = on_current_device((t), __func__);                                                  \
+        if (begin_status != FS_OK) return begin_status;                                                                   \
+        if ((needs_list) && !(t)->put) return fail((t), FS_E_STATE, "%s: the list has not reached the device", __func__); \
     } while (0)
 
 // Blocks of a kernel per compute unit, and how many units each takes at a time at most.  Few blocks with their chunks side by side keep the arrays' pages
@@ -310,7 +315,7 @@ fs_status fs_tensors_destroy(fs_tensors *t)
 
 fs_status fs_tensors_update(fs_tensors *t, const fs_tensor *list, int32_t count)
 {
-    FS_TRAIN_BEGIN(t);
+    FS_TRAIN_BEGIN(t, false);
     if (count != t->asked) return fail(t, FS_E_SHAPE, "fs_tensors_update: the list has %d tensors, not %d", t->asked, count);
     if (!list && count) return fail(t, FS_E_ARG, "fs_tensors_update: list is NULL");
     const fs_status s = check_list(t, "fs_tensors_update", list, count, t->given);
@@ -326,7 +331,7 @@ fs_status fs_tensors_set_stream(fs_tensors *t, void *hip_stream)
 
 fs_status fs_grad_norm(fs_tensors *t, int32_t kind, double grad_scale, float *d_norm)
 {
-    FS_TRAIN_BEGIN(t);
+    FS_TRAIN_BEGIN(t, true);
     if (kind != FS_NORM_TWO && kind != FS_NORM_MAX) return fail(t, FS_E_ARG, "fs_grad_norm: bad kind");
     if (!scale_ok(grad_scale)) return fail(t, FS_E_ARG, "fs_grad_norm: grad_scale must be positive and finite");
     if (!word_ok(t, d_norm, 4)) return fail(t, FS_E_ARG, "fs_grad_norm: d_norm must be a device pointer");
@@ -336,7 +341,7 @@ fs_status fs_grad_norm(fs_tensors *t, int32_t kind, double grad_scale, float *d_
 
 fs_status fs_grad_clip(fs_tensors *t, int32_t kind, double max_norm, double grad_scale, int32_t norm_given, float *d_norm)
 {
-    FS_TRAIN_BEGIN(t);
+    FS_TRAIN_BEGIN(t, true);
     if (norm_given != 0 && norm_given != 1) return fail(t, FS_E_ARG, "fs_grad_clip: norm_given must be 0 or 1");
     if (!norm_given && kind != FS_NORM_TWO && kind != FS_NORM_MAX) return fail(t, FS_E_ARG, "fs_grad_clip: bad kind");
     if (!(max_norm >= 0.0)) return fail(t, FS_E_ARG, "fs_grad_clip: max_norm must not be negative");
@@ -356,7 +361,7 @@ fs_status fs_grad_clip(fs_tensors *t, int32_t kind, double max_norm, double grad
 
 fs_status fs_adamw_step(fs_tensors *t, const fs_adamw *how, int64_t *d_step, float *d_norm)
 {
-    FS_TRAIN_BEGIN(t);
+    FS_TRAIN_BEGIN(t, true);
     if (!how) return fail(t, FS_E_ARG, "fs_adamw_step: how is NULL");
     const fs_adamw &h = *how;
     if (!std::isfinite(h.lr) || !std::isfinite(h.weight_decay)) return fail(t, FS_E_ARG, "fs_adamw_step: lr and weight_decay must be finite");

@@ -344,6 +344,68 @@ def test_results_do_not_change_from_call_to_call(optim):
     assert len({float(lst.grad_norm()) for _ in range(5)}) == 1
 
 
+def test_many_tensors_are_clipped_and_updated(optim):
+    """More than a block keeps the places of, several to a chunk."""
+    gen = torch.Generator().manual_seed(15)
+    sizes = torch.randint(0, 60, (3000,), generator=gen).tolist()
+    sizes[1500] = 400_003
+    p, g, m, v, _ = _adam_lists(gen, sizes, F32, F32, False, False)
+    on = {k: _packed(x, F32)[1] for k, x in (("p", p), ("g", g), ("m", m), ("v", v))}
+    outs = _packed([torch.zeros(n) for n in sizes], F32)[1]
+    optim.TensorList(on["g"], outs=outs).clip_grads(1.0)
+    opt = optim.AdamW(on["p"], grads=on["g"], lr=0.01, max_norm=1.0, exp_avgs=on["m"], exp_avg_sqs=on["v"], step=torch.tensor([3], device=DEV))
+    opt.step()
+    c = ref.coef(ref.norm(g), 1.0)
+    g, p, m, v = (torch.cat(x) for x in (g, p, m, v))
+    ref.near(torch.cat(outs), *ref.clip(g, c))
+    want = ref.adamw(p, g, m, v, 4, c, 0.01, (0.9, 0.999), 1e-8, 0.01)
+    for key, name in (("exp_avg", "m"), ("exp_avg_sq", "v"), ("param", "p")):
+        ref.near(torch.cat(on[name]), *want[key], key)
+
+
+@pytest.mark.parametrize("dtype,total", [(BF16, 4_000_000), (F32, 9_000_000), (BF16, 30_000_000), (F32, 60_000_000), (F16, 130_000_000)])
+def test_large_lists(optim, dtype, total):
+    """Sizes that differ in what stays in the caches and in how chunks are dealt out; the reference on the GPU, in 64 bits."""
+    gen = torch.Generator(device=DEV).manual_seed(total)
+    sizes = [total // 2 + 1, total // 5, 12_345, 1, total // 7 + 3]
+    new = lambda n, scale=1.0: torch.randn(n, generator=gen, device=DEV) * scale
+    g = [(new(n) * 10.0 ** -i).to(dtype) for i, n in enumerate(sizes)]
+    norm = ref.norm(g)
+    c = ref.coef(norm, 0.1)
+    outs = [torch.zeros_like(x) for x in g]
+    lst = optim.TensorList(g, outs=outs)
+    assert abs(float(lst.clip_grads(0.1)) - norm) <= norm * ref.U * ref.SLACK
+    assert abs(float(lst.grad_norm()) - norm) <= norm * ref.U * ref.SLACK
+    for x, y in zip(g, outs):
+        ref.near(y, *ref.clip(x, c))
+    del outs, lst, y
+    p, m, v = [new(n).to(dtype) for n in sizes], [new(n, 0.1) for n in sizes], [new(n).square() for n in sizes]
+    w = [x.float() + 0.01 for x in p] if dtype != F32 else None
+    before = [[x.clone() for x in t] for t in (p, m, v)] + [[x.clone() for x in w] if w else None]
+    opt = optim.AdamW(p, grads=g, lr=0.01, max_norm=0.1, masters=w, exp_avgs=m, exp_avg_sqs=v, step=torch.tensor([99], device=DEV))
+    opt.step()
+    for i in range(len(sizes)):
+        want = ref.adamw(before[0][i], g[i], before[1][i], before[2][i], 100, c, 0.01, (0.9, 0.999), 1e-8, 0.01, master=before[3][i] if w else None)
+        ref.near(p[i], *want["param"], "param")
+        ref.near(m[i], *want["exp_avg"], "exp_avg")
+        ref.near(v[i], *want["exp_avg_sq"], "exp_avg_sq")
+        if w:
+            ref.near(w[i], *want["master"], "master")
+
+
+def test_a_long_norm_streams_its_beginning(optim):
+    gen = torch.Generator(device=DEV).manual_seed(16)
+    g = [torch.randn(n, generator=gen, device=DEV) for n in (150_000_001, 140_000_000, 3)]
+    want = ref.norm(g)
+    out = [torch.empty_like(x) for x in g]
+    lst = optim.TensorList(g, outs=out)
+    for got in (lst.grad_norm(), lst.clip_grads(want / 4)):
+        assert abs(float(got) - want) <= want * ref.U * ref.SLACK
+    assert float(lst.grad_norm(kind="max")) == ref.norm(g, "max")
+    for x, y in zip(g, out):
+        ref.near(y, *ref.clip(x, ref.coef(want, want / 4)))
+
+
 # ---- more than 2^31 elements; streams; graphs ----
 
 def test_more_elements_than_32_bits_count(optim):

@@ -158,6 +158,16 @@ for call in (norm, clip, lambda h: adamw(h, how())):
     S.stub_fail_launch(-1)
     assert call(h) == OK
 assert S.stub_memsets() == 0
+# a list that has not reached the device is not worked on
+a = (Tensor * 1)(tensor(n=7))
+S.stub_fail_launch(0)
+assert L.fs_tensors_update(h, a, 1) == E_DEVICE
+S.stub_fail_launch(-1)
+S.stub_clear_launches()
+for call in (norm, clip, lambda h: adamw(h, how())):
+    assert call(h) == E_STATE and "reached" in error(h)
+assert names() == []
+assert L.fs_tensors_update(h, a, 1) == OK and norm(h) == OK
 """, tmp_path)
 
 

@@ -14,7 +14,7 @@ TINY = {t: torch.finfo(t).smallest_normal * torch.finfo(t).eps / 2 for t in HALF
 
 
 def norm(grads, kind="l2", scale=1.0):
-    """Of tensors on the CPU, as a Python float."""
+    """As a Python float."""
     flat = [g.double().reshape(-1) for g in grads if g is not None and g.numel()]
     if kind == "max":
         return max([float(f.abs().max()) for f in flat], default=0.0) * scale
@@ -63,12 +63,14 @@ def adamw(p, g, m, v, t, c, lr, betas, eps, decay, lr_scale=1.0, decay_scale=1.0
     off_p = off_up + 6 * U * fade.abs() + U * change.abs() + U * new_p.abs() + low
     out = {"exp_avg": (new_m, off_m * SLACK), "exp_avg_sq": (new_v, off_v * SLACK), "master": (new_p, off_p * SLACK)}
     more = HALF[dtype] * (new_p.abs() + off_p) + TINY[dtype] if dtype != torch.float32 else 0.0
-    return out | {"param": (new_p, (off_p + more) * SLACK)}
+    # beyond the type's range the rounding gives infinity
+    stored = torch.where(new_p.abs() >= torch.finfo(dtype).max * (1 + HALF[dtype]), torch.copysign(torch.full_like(new_p, math.inf), new_p), new_p)
+    return out | {"param": (stored, (off_p + more) * SLACK)}
 
 
 def near(got, want, bound, what=""):
-    got = got.detach().cpu().double()
-    bad = ~((got - want).abs() <= bound)
+    got = got.detach().to(want.device).double()
+    bad = ~((got == want) | ((got - want).abs() <= bound))
     if bad.any():
         i = int(torch.nonzero(bad.reshape(-1))[0])
         raise AssertionError(f"{what}: {int(bad.sum())} of {bad.numel()} outside; [{i}] {got.reshape(-1)[i]} for {want.reshape(-1)[i]}, bound {bound.reshape(-1)[i]}")
