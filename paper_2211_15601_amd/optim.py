@@ -170,6 +170,11 @@ def _places(tensors):
     return [0 if t is None else t.data_ptr() for t in tensors]
 
 
+def _aliases(tensors):
+    """The same memory, which stays theirs whatever becomes of the tensors."""
+    return [None if t is None else t.detach() for t in tensors]
+
+
 def _sizes(tensors):
     return [0 if t is None else t.numel() for t in tensors]
 
@@ -180,35 +185,28 @@ def _types(tensors):
 
 class TensorList:
     """A list of gradients, and where their clipped values go (`outs`; without: in place).  Entries of `grads` may be None: they
-    are left out.  The list keeps references to the tensors, and notices when their memory has moved."""
+    are left out.  The list is of the memory that the tensors have when it is made, and keeps it alive: a tensor that gets other memory later
+    (`.grad` made anew, `.data` replaced) needs another list."""
 
     def __init__(self, grads: Sequence[Optional[torch.Tensor]], outs: Optional[Sequence[Optional[torch.Tensor]]] = None, device=None):
-        self._grads = list(grads)
-        (self._outs,) = _lists(len(self._grads), outs=outs)
-        self._handle = _Handle(len(self._grads), _device_of(self._grads, device))
-        self._written = [o if o is not None else g for o, g in zip(self._outs, self._grads) if g is not None]
-        self._watched = self._grads + [o for o in self._outs if o is not None]
-        self._places = None
-        self._put()
-
-    def _put(self):
-        h, c = self._handle, self._handle.columns
-        for i, g in enumerate(self._grads):
+        grads = list(grads)
+        (outs,) = _lists(len(grads), outs=outs)
+        h = self._handle = _Handle(len(grads), _device_of(grads, device))
+        for i, g in enumerate(grads):
             if g is not None:
                 _check("grads", i, g, None, h.device, _TYPES)
-        for i, (g, o) in enumerate(zip(self._grads, self._outs)):
+        for i, (g, o) in enumerate(zip(grads, outs)):
             if g is not None and o is not None:
                 _check("outs", i, o, g, h.device, [g.dtype])
-        _check_apart(self._grads + [o for o, g in zip(self._outs, self._grads) if o is not None and g is not None and o.data_ptr() != g.data_ptr()])
-        self._places = None
-        places = _places(self._watched)
-        c["grad"], c["out"] = places[:h.count], _places(self._outs)
-        c["n"], c["grad_type"] = _sizes(self._grads), _types(self._grads)
+        grads, outs = _aliases(grads), _aliases([None if g is None else o for g, o in zip(grads, outs)])
+        _check_apart(grads + [o for o, g in zip(outs, grads) if o is not None and o.data_ptr() != g.data_ptr()])
+        self._grads, self._written = grads, [o if o is not None else g for o, g in zip(outs, grads) if g is not None]
+        c = h.columns
+        c["grad"], c["out"], c["n"], c["grad_type"] = _places(grads), _places(outs), _sizes(grads), _types(grads)
         h.put()
-        self._places = places
 
     def _ready(self):
-        self._handle.ready(self._put, _places(self._watched) == self._places)
+        self._handle.ready(self._handle.put, True)
 
     def grad_norm(self, kind: str = "l2", grad_scale: float = 1.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Global norm of the gradients times grad_scale, float32 [1]: "l2", or "max", the largest magnitude."""
@@ -233,7 +231,8 @@ class AdamW:
     """AdamW with decoupled weight decay over a list of parameters, one or two launches a step whatever their number.
 
       params       float32, bfloat16 or float16 tensors on one GPU
-      grads        their gradients; without: each parameter's .grad at the time of the step (None: the parameter stays as it is)
+      grads        their gradients, by the memory that they have now; without: each parameter's .grad at the time of the step (None: the
+                   parameter stays as it is)
       lr           a number, or a float32 tensor of one element on the GPU that is read at every step (a schedule under graph capture)
       max_norm     limit of the gradients' global 2-norm; None: no clipping
       grad_scale   factor on all gradients before anything else (the inverse of a loss scale)
@@ -270,19 +269,19 @@ class AdamW:
             raise ValueError("step must have one element")
         self._given = None
         if grads is not None:
-            (self._given,) = _lists(n, grads=grads)
-        self._places = None
+            (given,) = _lists(n, grads=grads)
+            for i, (g, p) in enumerate(zip(given, self.params)):
+                if g is not None:
+                    _check("grads", i, g, p, h.device, _TYPES)
+            self._given = _aliases(given)
+        self._places = self._looks = None
         self._how, self._set_to = binding.AdamW(), None
         c = h.columns
         c["master"], c["exp_avg"], c["exp_avg_sq"] = _places(self.masters), _places(self.exp_avgs), _places(self.exp_avg_sqs)
         c["lr_scale"], c["decay_scale"] = lr_scales, decay_scales
-        if self._given is not None:
-            for i, (g, p) in enumerate(zip(self._given, self.params)):
-                if g is not None:
-                    _check("grads", i, g, p, h.device, _TYPES)
         _check_apart(self.params + self.masters + self.exp_avgs + self.exp_avg_sqs + (self._given or []))
         if self._given is not None:
-            self._put(self._given, _places(self._given) + _places(self.params))
+            self._put(self._given, _places(self.params))
 
     def _put(self, grads, now):
         h, c = self._handle, self._handle.columns
@@ -292,7 +291,7 @@ class AdamW:
                 _check("exp_avgs", i, self.exp_avgs[i], p, h.device, [torch.float32])
                 _check("grads", i, g, p, h.device, _TYPES)
         self._places = None
-        c["grad"], c["param"] = now[:h.count], now[h.count:]
+        c["grad"], c["param"] = _places(grads), now[:h.count]
         c["n"], c["grad_type"], c["param_type"] = _sizes(grads), _types(grads), _types(self.params)
         self._looks = self._look(grads)
         h.put()
@@ -307,10 +306,13 @@ class AdamW:
         """One step.  Returns the gradients' global norm, float32 [1] (None where neither max_norm nor skip_nonfinite asks for it); a
         `norm` that is given is taken as it is (one over several GPUs, say)."""
         h, how = self._handle, self._how
-        grads = self._given if self._given is not None else [p.grad for p in self.params]
-        now = _places(grads) + _places(self.params)
-        # gradients that are not held here may have been replaced by others at the same place
-        h.ready(lambda: self._put(grads, now), now == self._places and (self._given is not None or self._look(grads) == self._looks))
+        now, grads, unchanged = _places(self.params), self._given, True
+        if grads is None:
+            # gradients that are not held here may lie elsewhere, or have been replaced by others at the same place
+            grads = [p.grad for p in self.params]
+            now += _places(grads)
+            unchanged = self._look(grads) == self._looks
+        h.ready(lambda: self._put(grads, now), unchanged and now == self._places)
         asked = norm is not None or self.max_norm is not None or self.skip_nonfinite
         d = h.norm(norm) if asked else None
         lr = self.lr
