@@ -64,7 +64,7 @@ typedef struct {
 
 /* Make a list of `count` tensors (0 .. FS_MAX_TENSORS) on the current device.  `list` is host memory and is not kept; the
  * tensors' memory stays the caller's and has to stay where it is while calls on the list are made.  Tensors that a call writes must
- * not overlap one another or what it reads otherwise.  Allocates 96 bytes per tensor and 33 KiB.  On failure *out is NULL. */
+ * not overlap one another or what it reads otherwise.  Allocates 84 bytes per tensor and 25 KiB.  On failure *out is NULL. */
 fs_status fs_tensors_create(const fs_tensor *list, int32_t count, void *hip_stream, fs_tensors **out);
 
 /* Free what the list owns.  Synchronises its stream first.  NULL is allowed. */
