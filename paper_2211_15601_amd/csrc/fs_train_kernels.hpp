@@ -309,8 +309,8 @@ __device__ __forceinline__ S join_parts(const S *part, int n)
 }
 
 // s sqrt(sum g^2) or s max |g|: each thread adds up what it reads, a block's waves join by shuffles and LDS, the block that comes last joins the blocks' sums, every
-// time in the same order.  Bound by reading: 400 M fp32 in 226 us (7.1 TB/s), 45 M bf16 in 300 tensors 20.5 us (4.4, of which some 5 us are the two ends).  64-bit sums
-// cost two instructions an element, a quarter of the time of the loads.
+// time in the same order.  Bound by reading: 400 M fp32 in 226 us (7.1 TB/s), 45 M bf16 in 300 tensors 20.5 us (4.4, of which some 5 us are the two ends).  With the
+// 64-bit sums it issues 3 instructions an element in fp32 and 5 in 16 bits, a seventh and a quarter of the time.
 // The first `streamed` chunks are read past the caches, the others stay there for a pass that comes from the other end.
 // norm == NULL: the blocks' sums stay in `partial`, and every block of the kernel behind this one joins them for itself (see norm_value()).
 template <int KIND>
@@ -603,7 +603,7 @@ __device__ __forceinline__ void adam_types(const TensorD &t, const Piece &p, con
 __device__ __forceinline__ bool is_finite(float x) { return __builtin_fabsf(x) < __builtin_inff(); }
 
 // Reads four arrays and writes three (of 16-bit parameters with masters, four and four), 28 bytes an element, once each; the counters say that no more is moved.
-// 250 M elements in 1253 us (7.0 GB, 5.6 TB/s), 12.6 M fp32 in 57.5 (6.1).  Vector instructions, 11 a byte of a wave, take a quarter of that.  Four elements a thread, so
+// 250 M elements in 1253 us (7.0 GB, 5.6 TB/s), 12.6 M fp32 in 57.5 (6.1).  Its 44 vector instructions an element take a quarter of that.  Four elements a thread, so
 // that fp32 arrays are read 16 bytes at a time; more on its way per thread, or more blocks, makes no difference or costs pages in use (see grid_for).
 template <int MODE>
 __global__ __launch_bounds__(256) void k_adamw(ListD L, AdamD A, NormD N, const float *__restrict__ lr_word, long long *__restrict__ steps, unsigned *__restrict__ tickets)
