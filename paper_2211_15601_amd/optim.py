@@ -1,7 +1,7 @@
 """What a training program does with its gradients, over the C ABI of include/fastsnarf_train.h: the global norm of a list of
 tensors, clipping, and the AdamW step.
 
-    norm = TensorList([p.grad for p in params]).clip_grads(1.0)          # as torch.nn.utils.clip_grad_norm_
+    norm = TensorList([p.grad for p in params]).clip_grads(1.0)          # scales the gradients where they are
 
     opt = AdamW(params, lr=1e-3, weight_decay=0.01, max_norm=1.0)        # clips inside the step: no gradient is rewritten
     loss.backward(); norm = opt.step(); opt.zero_grad()
@@ -89,7 +89,7 @@ class _Handle:
 
     def ready(self, put, unchanged: bool):
         """Before a call: put() if the list has changed, and the stream."""
-        # torch.cuda.current_stream makes an object, 2 us of the 7 that a call takes the host; this is what compiled code of torch's own asks
+        # the current stream's number; asking for the stream itself makes an object, 2 us of the 7 that a call then takes the host
         raw = torch._C._cuda_getCurrentRawStream(self.device.index)
         capturing = raw != 0 and torch.cuda.is_current_stream_capturing()      # the default stream is none that can be captured
         if not unchanged or (self.recorded and not capturing):
