@@ -193,9 +193,10 @@ fs_status on_current_device(fs_tensors *t, const char *what)
 // Blocks of a kernel per compute unit, and how many units each takes at a time at most.  Few blocks with their chunks side by side keep the arrays' pages
 // and channels evenly in use.  Measured for 2 / 4 / 8 blocks per unit, us: norm of 400 M fp32 226 / 234 / 241 and of 45 M bf16 in 300 tensors 23.5 / 20.9 /
 // 21.2 (where a block's start is not hidden by what it has to do); clipping 20 M mixed 37 / 35 / 35; AdamW of 12.6 M fp32 70.6 / 73.3 / 73.1, of 250 M mixed 1365 / 1414 / 1415.  Chunks of 3 / 6 / 8 units in AdamW:
-// 1351 / 1372 / 1384; of 1 unit 1600 (a block has too little on its way).
+// 1351 / 1372 / 1384; of 1 unit 1600 (a block has too little on its way); of 6 / 8 / 32 in the
+// norm of 45 M bf16 22.2 / 20.6 / 20.2, of 180 M 62.3 / 62.3 / 59.6.
 struct Shape { int per_cu, most; };
-constexpr Shape NORM = {4, 8}, NORM_LONG = {2, 8}, CLIP = {4, 4}, ADAMW = {2, 3};
+constexpr Shape NORM = {4, 32}, NORM_LONG = {2, 8}, CLIP = {4, 4}, ADAMW = {2, 3};
 
 // Long lists mostly in fp32, where two blocks a unit read what they can: norm of 450 M fp32 254 us, with four 262; 900 M bf16, twice the arithmetic a byte, 296 and 263.
 bool norm_is_long(const fs_tensors *t) { return t->L.units >= 1 << 16 && t->grad_bytes >= 3.0 * UNIT * t->L.units; }
