@@ -309,7 +309,7 @@ __device__ __forceinline__ S join_parts(const S *part, int n)
 }
 
 // s sqrt(sum g^2) or s max |g|: each thread adds up what it reads, a block's waves join by shuffles and LDS, the block that comes last joins the blocks' sums, every
-// time in the same order.  Bound by reading: 400 M fp32 in 226 us (7.1 TB/s), 45 M bf16 in 300 tensors 20.5 us (4.4, of which some 5 us are the two ends).  With the
+// time in the same order.  Bound by reading: 400 M fp32 in 226 us (7.1 TB/s), 45 M bf16 in 300 tensors 20 us (4.5, of which some 5 us are the two ends).  With the
 // 64-bit sums it issues 3 instructions an element in fp32 and 5 in 16 bits, a seventh and a quarter of the time.
 // The first `streamed` chunks are read past the caches, the others stay there for a pass that comes from the other end.
 // norm == NULL: the blocks' sums stay in `partial`, and every block of the kernel behind this one joins them for itself (see norm_value()).

@@ -285,14 +285,17 @@ class AdamW:
 
     def _put(self, grads, now):
         h, c = self._handle, self._handle.columns
-        for i, (g, p) in enumerate(zip(grads, self.params)):
-            if g is not None:
+        if self._places is None or self._places[:h.count] != now[:h.count]:
+            for i, p in enumerate(self.params):              # they may have another type or order now
                 _check("params", i, p, None, h.device, _TYPES)
                 _check("exp_avgs", i, self.exp_avgs[i], p, h.device, [torch.float32])
+            c["param_type"] = _types(self.params)
+        for i, (g, p) in enumerate(zip(grads, self.params)):
+            if g is not None:
                 _check("grads", i, g, p, h.device, _TYPES)
         self._places = None
         c["grad"], c["param"] = _places(grads), now[:h.count]
-        c["n"], c["grad_type"], c["param_type"] = _sizes(grads), _types(grads), _types(self.params)
+        c["n"], c["grad_type"] = _sizes(grads), _types(grads)
         self._looks = self._look(grads)
         h.put()
         self._places = now
