@@ -13,8 +13,8 @@
  *
  * Magnitudes are squared and added in 64 bits, so the norm of any finite fp32 gradients is finite before it is rounded to
  * fp32; the coefficient and the bias corrections are computed in 64 bits, the update in fp32.  16-bit results are rounded
- * once, to nearest even.  Sums run in an order that depends on the list and on the device only: results are the same
- * from call to call.  NaN and infinities go through as the formulas say.
+ * once, to nearest even.  Sums run in an order that depends on the list (with its addresses) and on the device only: results are the
+ * same from call to call.  NaN and infinities go through as the formulas say.
  *
  * Conventions of fastsnarf.h hold (device pointers, nothing synchronises, status codes, no exceptions or aborts), with one
  * difference: the pointers of a list are aligned to their own element type, no more, so tensors may be views into a packed buffer.
