@@ -71,7 +71,9 @@ fs_status fs_tensors_create(const fs_tensor *list, int32_t count, void *hip_stre
 fs_status fs_tensors_destroy(fs_tensors *t);
 
 /* Other addresses, sizes or types for the same number of tensors, for the calls after this one (a program whose gradients move from
- * step to step).  On an error nothing has changed. */
+ * step to step).  A list that is refused changes nothing; after FS_E_DEVICE, calls return FS_E_STATE until another update has succeeded.
+ * A stream that records a graph records the update.  A graph's calls read the list as it is on the device when they are replayed: a list that a
+ * graph uses is neither updated nor destroyed while the graph is. */
 fs_status fs_tensors_update(fs_tensors *t, const fs_tensor *list, int32_t count);
 
 /* The stream of the calls after this one.  The list's scratch is shared by all its calls: the caller orders this stream behind the one before. */
@@ -84,7 +86,7 @@ fs_status fs_grad_norm(fs_tensors *t, int32_t kind, double grad_scale, float *d_
  * norm_given = 0: d_norm [1] is computed as by fs_grad_norm; 1: it is read (kind is then not looked at). */
 fs_status fs_grad_clip(fs_tensors *t, int32_t kind, double max_norm, double grad_scale, int32_t norm_given, float *d_norm);
 
-/* One AdamW step.  d_step [1]: steps done before, one more after.  d_norm [1] may be NULL if max_norm is INFINITY and
+/* One AdamW step.  d_step [1]: steps done before, one more after (8-byte aligned).  d_norm [1] may be NULL if max_norm is INFINITY and
  * skip_nonfinite 0: then no norm is computed. */
 fs_status fs_adamw_step(fs_tensors *t, const fs_adamw *how, int64_t *d_step, float *d_norm);
 
