@@ -192,9 +192,9 @@ fs_status on_current_device(fs_tensors *t, const char *what)
 
 // Blocks of a kernel per compute unit, and how many units each takes at a time at most.  Few blocks with their chunks side by side keep the arrays' pages
 // and channels evenly in use.  Measured for 2 / 4 / 8 blocks per unit, us: norm of 400 M fp32 226 / 234 / 241 and of 45 M bf16 in 300 tensors 23.5 / 20.9 /
-// 21.2 (where a block's start is not hidden by what it has to do); clipping 20 M mixed 37 / 35 / 35; AdamW of 12.6 M fp32 70.6 / 73.3 / 73.1, of 250 M mixed 1365 / 1414 / 1415.  Chunks of 3 / 6 / 8 units in AdamW:
-// 1351 / 1372 / 1384; of 1 unit 1600 (a block has too little on its way); of 6 / 8 / 32 in the
-// norm of 45 M bf16 22.2 / 20.6 / 20.2, of 180 M 62.3 / 62.3 / 59.6.
+// 21.2 (where a block's start is not hidden by what it has to do); clipping 20 M mixed 37 / 35 / 35; AdamW of 12.6 M fp32 70.6 / 73.3 / 73.1, of 250 M mixed
+// 1365 / 1414 / 1415.  Chunks of 3 / 6 / 8 units in AdamW: 1351 / 1372 / 1384; of 1 unit 1600 (a block has too little on its way); of 6 / 8 / 32 in the norm of 45 M
+// bf16 22.2 / 20.6 / 20.2, of 180 M 62.3 / 62.3 / 59.6.
 struct Shape { int per_cu, most; };
 constexpr Shape NORM = {4, 32}, NORM_LONG = {2, 8}, CLIP = {4, 4}, ADAMW = {2, 3};
 
@@ -224,7 +224,8 @@ bool is_short(const fs_tensors *t) { return t->L.units <= SHORT_UNITS; }
 int short_blocks(const fs_tensors *t) { return std::max(1, (t->L.units * (UNIT / SHORT_PART) + SHORT_WAVES - 1) / SHORT_WAVES); }
 
 // Bytes at the end of the gradients that the norm leaves in the caches (256 MiB of them in front of the memory), for the pass behind it, which comes from that
-// end (none for a norm alone).  What is before them streams: 400 M fp32 then take 234 us, not 259, and 228 where all of it streams.  Measured with 64 / 128 / 192 / 240 MB, clipping 250 M fp32: 512 / 490 / 497 / 492 us.
+// end (none for a norm alone).  What is before them streams: 400 M fp32 then take 234 us, not 259, and 228 where all of it streams.  Measured with 64 / 128 / 192 / 240
+// MB, clipping 250 M fp32: 512 / 490 / 497 / 492 us.
 constexpr double KEPT_BYTES = 192e6;
 
 // What a pass leaves in the caches, by the bytes that it reads and writes (of AdamW's parameters, by theirs alone).  Measured with three lists in turn, us.
