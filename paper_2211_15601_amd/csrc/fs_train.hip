@@ -194,8 +194,8 @@ fs_status on_current_device(fs_tensors *t, const char *what)
 // and channels evenly in use.  Measured for 2 / 4 / 8 blocks per unit, us: norm of 400 M fp32 226 / 234 / 241 and of 45 M bf16 in 300 tensors 23.5 / 20.9 /
 // 21.2 (where a block's start is not hidden by what it has to do); clipping 20 M mixed 37 / 35 / 35; AdamW of 12.6 M fp32 70.6 / 73.3 / 73.1, of 250 M mixed
 // 1365 / 1414 / 1415.  Chunks of 3 / 6 / 8 units in AdamW: 1351 / 1372 / 1384; of 1 unit 1600 (a block has too little on its way); of 6 / 8 / 32 in the norm of 45 M
-// bf16 22.2 / 20.6 / 20.2, of 180 M 62.3 / 62.3 / 59.6.  Where there are fewer units than `least` for every block, one block a compute unit: a norm that is short
-// has fewer blocks to wait for at its end, 2 M fp32 5.7 / 6.5, 4 M bf16 6.1 / 7.7, 16 M 11.2 / 11.1.
+// bf16 22.2 / 20.6 / 20.2, of 180 M 62.3 / 62.3 / 59.6.  Where that leaves less than `least` units a block, blocks are fewer, down to one a compute unit: a
+// norm has fewer of them to wait for at its end, 2 M fp32 5.7 / 6.5, 4 M bf16 6.1 / 7.7, 16 M 11.2 / 11.1.
 struct Shape { int per_cu, most, least; };
 constexpr Shape NORM = {4, 32, 8}, NORM_LONG = {2, 8, 1}, CLIP = {4, 4, 1}, ADAMW = {2, 3, 1};
 

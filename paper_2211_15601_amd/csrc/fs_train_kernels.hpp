@@ -114,45 +114,55 @@ __device__ __forceinline__ TensorD tensor_at(const ListD &L, int i)
 struct Piece { long long begin, end; };
 __device__ __forceinline__ Piece piece_of(const TensorD &t, long long from, long long upto) { return {from - t.lead, min(upto - t.lead, t.n)}; }
 
-// Calls f(tensor, piece, chunk) for what this block's chunks of units cover of every tensor.  The next piece's tensor is found and asked for before
-// the present piece is worked on.  BACK: the last chunk first.
-template <bool BACK, class F>
-__device__ __forceinline__ void walk(const ListD &L, F f)
-{
-    const int chunks = L.chunks;
-    int c = blockIdx.x;
-    if (c >= chunks) return;
-    const bool kept = (int)gridDim.x < chunks && L.count <= LIST_LDS;      // several chunks: the places are asked for more than once
-    __shared__ int s_first[LIST_LDS];
-    if (kept) {
-        for (int i = threadIdx.x; i < L.count; i += 256) s_first[i] = L.first[i];
-        __syncthreads();
-    }
-    auto find = [&](int u) { return kept ? find_tensor(s_first, L.count, u) : find_tensor(L.first, L.count, u); };
-    auto place = [&](int c) { return BACK ? chunks - 1 - c : c; };
-    int u = chunk_begin(L, place(c)), end = chunk_begin(L, place(c) + 1), i = find(u);
-    TensorD t = tensor_at(L, i);
-    for (;;) {
-        const Piece p = piece_of(t, (long long)(u - t.first) * UNIT, (long long)(end - t.first) * UNIT);
-        const int now = c;
-        u = t.next;
-        bool more = u < end;
-        if (more) ++i;
-        else {
-            c += gridDim.x;
-            more = c < chunks;
-            if (more) {
-                u = chunk_begin(L, place(c));
-                end = chunk_begin(L, place(c) + 1);
-                i = find(u);
-            }
+// This block's way through the list: chunk after chunk, tensor after tensor.  Made early, so that the first tensor is on its way while the kernel gets its norm.
+// BACK: the last chunk first.
+template <bool BACK>
+struct Walk {
+    const ListD &L;
+    const int *kept;                   // the places in LDS, where they are asked for more than once
+    int c, u, end, i;                  // chunk, unit, first unit behind the chunk, tensor
+    TensorD t;
+
+    __device__ __forceinline__ explicit Walk(const ListD &list) : L(list), kept(nullptr), c(blockIdx.x)
+    {
+        __shared__ int s_first[LIST_LDS];
+        if ((int)gridDim.x < L.chunks && L.count <= LIST_LDS) {
+            for (int k = threadIdx.x; k < L.count; k += 256) s_first[k] = L.first[k];
+            __syncthreads();
+            kept = s_first;
         }
-        const TensorD next = more ? tensor_at(L, i) : t;
-        f(t, p, now);
-        if (!more) return;
-        t = next;
+        if (c < L.chunks) {
+            go();
+            t = tensor_at(L, i);
+        }
     }
-}
+    __device__ __forceinline__ void go()
+    {
+        const int at = BACK ? L.chunks - 1 - c : c;
+        u = chunk_begin(L, at);
+        end = chunk_begin(L, at + 1);
+        i = kept ? find_tensor((const __attribute__((address_space(3))) int *)kept, L.count, u) : find_tensor(L.first, L.count, u);
+    }
+    // Calls f(tensor, piece, chunk) for what the block's chunks cover of every tensor.  The next piece's tensor is found and asked for before the present
+    // piece is worked on.
+    template <class F>
+    __device__ __forceinline__ void each(F f)
+    {
+        while (c < L.chunks) {
+            const Piece p = piece_of(t, (long long)(u - t.first) * UNIT, (long long)(end - t.first) * UNIT);
+            const int now = c;
+            u = t.next;
+            if (u < end) ++i;
+            else {
+                c += gridDim.x;
+                if (c < L.chunks) go();
+            }
+            const TensorD next = c < L.chunks ? tensor_at(L, i) : t;
+            f(t, p, now);
+            t = next;
+        }
+    }
+};
 
 // The same for short lists, a wave by itself: parts of PART elements, dealt out to `waves` waves of which this is number `wave`.
 template <int PART, class F>
@@ -318,7 +328,7 @@ __global__ __launch_bounds__(256) void k_norm(ListD L, int streamed, double scal
 {
     using S = typename Sum<KIND>::type;
     S s = 0;
-    walk<false>(L, [&](const TensorD &t, const Piece &p, int c) {
+    Walk<false>(L).each([&](const TensorD &t, const Piece &p, int c) {
         s = c < streamed ? sum_types<KIND, true, 256, AHEAD_NORM>(t, p, s) : sum_types<KIND, false, 256, AHEAD_NORM>(t, p, s);
     });
     s = block_join<4>(s);
@@ -430,8 +440,8 @@ template <bool STREAM>
 __global__ __launch_bounds__(256) void k_clip(ListD L, NormD N, int all_in_place, double max_norm, double scale)
 {
     const float coef = clip_coef(norm_value(N), max_norm, scale);
-    if (all_in_place && coef == 1.0f) return;
-    walk<true>(L, [&](const TensorD &t, const Piece &p, int) { scale_types<STREAM, 256, AHEAD_CLIP>(t, p, coef); });
+    if (all_in_place && coef == 1.0f) return;              // what most steps end with: nothing is asked for before it is known
+    Walk<true>(L).each([&](const TensorD &t, const Piece &p, int) { scale_types<STREAM, 256, AHEAD_CLIP>(t, p, coef); });
 }
 
 // Not in place: a block may have written while another still adds up.
@@ -582,10 +592,10 @@ __device__ __forceinline__ StepD adam_begin(const AdamD &A, const float *lr_word
     return s;
 }
 
-// The counter moves on when every block has read it.
-__device__ __forceinline__ void adam_end(const StepD &s, long long *steps, unsigned *tickets)
+// The counter moves on when every block has read it, unless the step was skipped.
+__device__ __forceinline__ void adam_end(const StepD &s, bool skip, long long *steps, unsigned *tickets)
 {
-    if ((threadIdx.x & 63) == 0 && is_last(s.ticket, tickets)) *steps = s.before + 1;
+    if ((threadIdx.x & 63) == 0 && is_last(s.ticket, tickets) && !skip) *steps = s.before + 1;
 }
 
 template <int MODE, int TEAM, int AHEAD>
@@ -603,22 +613,25 @@ __device__ __forceinline__ void adam_types(const TensorD &t, const Piece &p, con
 __device__ __forceinline__ bool is_finite(float x) { return __builtin_fabsf(x) < __builtin_inff(); }
 
 // Reads four arrays and writes three (of 16-bit parameters with masters, four and four), 28 bytes an element, once each; the counters say that no more is moved.
-// 250 M elements in 1253 us (7.0 GB, 5.6 TB/s), 12.6 M fp32 in 57.5 (6.1).  Its 44 vector instructions an element take a quarter of that.  Four elements a thread, so
+// 250 M elements in 1251 us (7.0 GB, 5.6 TB/s), 12.6 M fp32 in 57 (6.2).  Its 44 vector instructions an element take a quarter of that.  Four elements a thread, so
 // that fp32 arrays are read 16 bytes at a time; more on its way per thread, or more blocks, makes no difference or costs pages in use (see grid_for).
 template <int MODE>
 __global__ __launch_bounds__(256) void k_adamw(ListD L, AdamD A, NormD N, const float *__restrict__ lr_word, long long *__restrict__ steps, unsigned *__restrict__ tickets)
 {
-    const float n = norm_value(N);
-    if (A.skip_nonfinite && !is_finite(n)) return;         // every block sees the same norm
+    Walk<true> walk(L);
     __shared__ AdamC shared;
     StepD step;
     const bool first = threadIdx.x < 64;
     if (first) step = adam_begin(A, lr_word, steps, tickets, &shared);
+    const float n = norm_value(N);
     __syncthreads();
-    AdamC C = shared;
-    C.coef = clip_coef(n, A.max_norm, A.scale);
-    walk<true>(L, [&](const TensorD &t, const Piece &p, int) { adam_types<MODE, 256, AHEAD_ADAMW>(t, p, A, C); });
-    if (first) adam_end(step, steps, tickets);
+    const bool skip = A.skip_nonfinite && !is_finite(n);   // every block sees the same norm
+    if (!skip) {
+        AdamC C = shared;
+        C.coef = clip_coef(n, A.max_norm, A.scale);
+        walk.each([&](const TensorD &t, const Piece &p, int) { adam_types<MODE, 256, AHEAD_ADAMW>(t, p, A, C); });
+    }
+    if (first) adam_end(step, skip, steps, tickets);
 }
 
 // With the norm in the same kernel, which is as good as the list is short.
@@ -638,10 +651,7 @@ __global__ __launch_bounds__(SHORT_THREADS) void k_adamw_short(ListD L, AdamD A,
         C.coef = clip_coef(n, A.max_norm, A.scale);
         walk_short<SHORT_PART>(L, blockIdx.x * SHORT_WAVES + wave, gridDim.x * SHORT_WAVES, [&](const TensorD &t, const Piece &p) { adam_types<ADAM_CACHED, 64, 1>(t, p, A, C); });
     }
-    if (last_wave) {
-        if (skip) step.before -= 1;                        // the tickets were taken; the counter keeps its value
-        adam_end(step, steps, tickets);
-    }
+    if (last_wave) adam_end(step, skip, steps, tickets);
 }
 
 }  // namespace fs
