@@ -326,7 +326,7 @@ class AdamW:
             how.d_lr, lr = lr.data_ptr(), 0.0
         else:
             how.d_lr = None
-        set_to = (lr, self.betas, self.eps, self.weight_decay, self.grad_scale, self.max_norm, self.skip_nonfinite, norm is not None)
+        set_to = (lr, *self.betas, self.eps, self.weight_decay, self.grad_scale, self.max_norm, self.skip_nonfinite, norm is not None)
         if set_to != self._set_to:
             self._set_to = None
             how.lr, (how.beta1, how.beta2) = lr, self.betas
