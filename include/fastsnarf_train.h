@@ -72,8 +72,9 @@ fs_status fs_tensors_destroy(fs_tensors *t);
 
 /* Other addresses, sizes or types for the same number of tensors, for the calls after this one (a program whose gradients move from
  * step to step).  A list that is refused changes nothing; after FS_E_DEVICE, calls return FS_E_STATE until another update has succeeded.
- * A stream that records a graph records the update.  A graph's calls read the list as it is on the device when they are replayed: a list that a
- * graph uses is neither updated nor destroyed while the graph is. */
+ * A stream that records a graph records the update: it is for the calls behind it in the same graph, and any other call returns FS_E_STATE until
+ * another update has succeeded where that call is made.  A graph's calls read the list as it is on the device when they are replayed: a list that
+ * a graph uses is neither updated outside of it nor destroyed while the graph is. */
 fs_status fs_tensors_update(fs_tensors *t, const fs_tensor *list, int32_t count);
 
 /* The stream of the calls after this one.  The list's scratch is shared by all its calls: the caller orders this stream behind the one before. */

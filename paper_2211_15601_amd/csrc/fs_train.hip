@@ -13,6 +13,9 @@
 
 using namespace fs;
 
+// The capture that a stream records for; `active` false: it records none.
+struct Capture { bool active; unsigned long long id; };
+
 struct fs_tensors {
     hipStream_t stream;
     int device, n_cus;
@@ -26,7 +29,8 @@ struct fs_tensors {
     char *mem;                // device: TensorD [asked], int [asked + 1], double [TRAIN_BLOCKS], unsigned [TICKETS]
     double *partial;
     unsigned *tickets;
-    bool put;                 // the device's copy is that of `host`
+    bool put;                 // the device's copy is that of `host`, for calls in the capture `put_in`; elsewhere too if that is none
+    Capture put_in;
     const void *seen[8];      // words (d_norm, d_step, d_lr) that are known to be memory of the device, by address
     char err[256];
 };
@@ -46,6 +50,25 @@ fs_status launch_status(fs_tensors *t, const char *what)
 {
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? FS_OK : fail(t, FS_E_DEVICE, "%s: %s", what, hipGetErrorString(e));
+}
+
+Capture capture_of(hipStream_t stream)
+{
+    Capture c = {false, 0};
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    if (!stream) return c;                                  // the default stream cannot be captured
+    if (hipStreamGetCaptureInfo(stream, &status, &c.id) != hipSuccess) (void)hipGetLastError();
+    else c.active = status == hipStreamCaptureStatusActive;
+    return c;
+}
+
+// Is the device's list that of `host` where the next call on the list's stream runs?  A graph's update runs when the graph does, so until then, and
+// for all that is no part of the graph, the device has another list.
+bool there(const fs_tensors *t)
+{
+    if (!t->put || !t->put_in.active) return t->put;
+    const Capture now = capture_of(t->stream);
+    return now.active && now.id == t->put_in.id;
 }
 
 bool on_device(const fs_tensors *t, const void *p)
@@ -169,6 +192,7 @@ fs_status put_list(fs_tensors *t, const char *what, const fs_tensor *list)
     }
     const fs_status s = launch_status(t, what);
     t->put = s == FS_OK;
+    t->put_in = capture_of(t->stream);
     return s;
 }
 
@@ -187,7 +211,9 @@ fs_status on_current_device(fs_tensors *t, const char *what)
         if (!(t)) return FS_E_ARG;                                                                                        \
         const fs_status begin_status = on_current_device((t), __func__);                                                  \
         if (begin_status != FS_OK) return begin_status;                                                                   \
-        if ((needs_list) && !(t)->put) return fail((t), FS_E_STATE, "%s: the list has not reached the device", __func__); \
+        if ((needs_list) && !there(t))                                                                                    \
+            return fail((t), FS_E_STATE, "%s: the list has not reached the device%s", __func__,                           \
+                        (t)->put ? ": its last update is part of a graph" : "");                                          \
     } while (0)
 
 // Blocks of a kernel per compute unit, and how many units each takes at a time at most.  Few blocks with their chunks side by side keep the arrays' pages

@@ -1,0 +1,69 @@
+"""Host code of the calls on a list of tensors beside graphs that are captured, and on devices of other sizes, without a GPU: host_path.py on
+host_capture_stub.c."""
+import os
+import subprocess
+import sys
+
+import host_path
+from test_host_train import CHILD
+
+STREAMS = """
+A, B = ctypes.c_void_p(0x1000), ctypes.c_void_p(0x2000)
+def capture(stream, number, failed=0):
+    S.stub_capture(stream, ctypes.c_ulonglong(number), failed)
+def array(*tensors):
+    return (Tensor * len(tensors))(*tensors)
+calls = (norm, clip, lambda h: adamw(h, how()))
+"""
+
+
+def run(code, tmp_path):
+    stub = os.path.join(str(tmp_path), "host_stub.so")
+    subprocess.check_call(["gcc", "-shared", "-fPIC", "-O1", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include",
+                           os.path.join(host_path.HERE, "host_capture_stub.c"), "-o", stub])
+    env = dict(os.environ, FS_HOST_STUB=stub, PYTHONPATH=host_path.HERE)
+    r = subprocess.run([sys.executable, "-c", "from host_path import *\n" + CHILD + STREAMS + code + "\nprint('CHILD-OK')"], env=env,
+                       capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and "CHILD-OK" in r.stdout, (r.stdout + r.stderr)[-3000:]
+
+
+def test_a_recorded_update_is_of_its_graph_alone(tmp_path):
+    """Until the graph is replayed the device has another list than the host: neither eager calls nor other graphs may go by it."""
+    run("""
+h = make([tensor(n=1 << 20), tensor()])
+other = array(tensor(n=5), tensor(n=0, grad=None))
+assert L.fs_tensors_set_stream(h, A) == OK and norm(h) == OK
+capture(A, 7)
+assert norm(h) == OK                                        # recorded, with the list as it was
+assert L.fs_tensors_update(h, other, 2) == OK
+for call in calls:
+    assert call(h) == OK
+capture(A, 0)                                               # the capture has ended
+S.stub_clear_launches()
+for call in calls:
+    assert call(h) == E_STATE and "graph" in error(h)
+capture(A, 8)                                               # another one
+for call in calls:
+    assert call(h) == E_STATE and "graph" in error(h)
+assert names() == []
+assert L.fs_tensors_update(h, other, 2) == OK and names() == ["k_list_put"]
+for call in calls:
+    assert call(h) == OK
+capture(B, 8)                                               # a second stream of the same capture
+assert L.fs_tensors_set_stream(h, B) == OK
+for call in calls:
+    assert call(h) == OK
+capture(A, 8, 1), capture(B, 8, 1)                          # it has failed
+for call in calls:
+    assert call(h) == E_STATE
+capture(A, 0), capture(B, 0)
+S.stub_clear_launches()
+for call in calls:
+    assert call(h) == E_STATE
+assert names() == []
+# an update that runs makes all calls right again, whatever the stream
+for stream in (A, None):
+    assert L.fs_tensors_set_stream(h, stream) == OK and L.fs_tensors_update(h, other, 2) == OK
+    for call in calls:
+        assert call(h) == OK
+""", tmp_path)
