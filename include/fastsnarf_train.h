@@ -77,6 +77,9 @@ fs_status fs_tensors_destroy(fs_tensors *t);
  * a graph uses is neither updated outside of it nor destroyed while the graph is. */
 fs_status fs_tensors_update(fs_tensors *t, const fs_tensor *list, int32_t count);
 
+/* FS_OK if a call on the list would find it on the device now, FS_E_STATE if another update is needed before. */
+fs_status fs_tensors_ready(fs_tensors *t);
+
 /* The stream of the calls after this one.  The list's scratch is shared by all its calls: the caller orders this stream behind the one before. */
 fs_status fs_tensors_set_stream(fs_tensors *t, void *hip_stream);
 

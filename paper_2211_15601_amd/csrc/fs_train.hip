@@ -362,6 +362,12 @@ fs_status fs_tensors_set_stream(fs_tensors *t, void *hip_stream)
     return FS_OK;
 }
 
+fs_status fs_tensors_ready(fs_tensors *t)
+{
+    FS_TRAIN_BEGIN(t, true);
+    return FS_OK;
+}
+
 fs_status fs_grad_norm(fs_tensors *t, int32_t kind, double grad_scale, float *d_norm)
 {
     FS_TRAIN_BEGIN(t, true);

@@ -92,17 +92,20 @@ class _Handle:
         # the current stream's number; asking for the stream itself makes an object, 2 us of the 7 that a call then takes the host
         raw = torch._C._cuda_getCurrentRawStream(self.device.index)
         capturing = raw != 0 and torch.cuda.is_current_stream_capturing()      # the default stream is none that can be captured
-        if not unchanged or (self.recorded and not capturing):
+        if not unchanged:
             put()
         if raw != self._raw:
             self.to_stream(capturing)
+        # a put that was recorded is for the calls behind it in the same graph: others, which may run before it or without it, need their own
+        if self.recorded and (not capturing or self.L.fs_tensors_ready(self._h) != binding.FS_OK):
+            self.put(again=True)
         if capturing:
             self.captured = True
 
-    def put(self):
-        """Hands the list over: the first time, or after it has changed."""
+    def put(self, again=False):
+        """Hands the list over: the first time, after it has changed, or, `again`, as it is."""
         capturing = torch.cuda.is_current_stream_capturing()
-        if self._h is not None and not self.captured:
+        if self._h is not None and (not self.captured or again and capturing):
             if torch._C._cuda_getCurrentRawStream(self.device.index) != self._raw:
                 self.to_stream(capturing)
             self.ret(self.L.fs_tensors_update(self._h, self.list, self.count))

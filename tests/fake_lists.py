@@ -110,6 +110,10 @@ class Machine:
         self.lists[h.value]["stream"] = stream
         return self.binding.FS_OK
 
+    def fs_tensors_ready(self, h):
+        x = self.lists[h.value]
+        return self.binding.FS_E_STATE if x["put_in"] and x["put_in"] != self.here(h.value) else self.binding.FS_OK
+
     def fs_tensors_destroy(self, h):
         self.destroyed.append(h.value)
         return self.binding.FS_OK

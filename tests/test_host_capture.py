@@ -67,3 +67,26 @@ for stream in (A, None):
     for call in calls:
         assert call(h) == OK
 """, tmp_path)
+
+
+def test_a_list_says_whether_calls_would_find_it(tmp_path):
+    run("""
+h = make([tensor()])
+other = array(tensor(n=5))
+ready = L.fs_tensors_ready
+assert ready(h) == OK and ready(None) == E_ARG
+assert L.fs_tensors_set_stream(h, A) == OK
+capture(A, 7)
+assert ready(h) == OK and L.fs_tensors_update(h, other, 1) == OK and ready(h) == OK
+assert L.fs_tensors_set_stream(h, B) == OK and ready(h) == E_STATE and "graph" in error(h)
+capture(B, 7)
+assert ready(h) == OK
+capture(B, 8)
+assert ready(h) == E_STATE
+capture(B, 0)
+assert ready(h) == E_STATE and L.fs_tensors_update(h, other, 1) == OK and ready(h) == OK
+S.stub_fail_launch(0)
+assert L.fs_tensors_update(h, other, 1) == E_DEVICE
+S.stub_fail_launch(-1)
+assert ready(h) == E_STATE and "graph" not in error(h)
+""", tmp_path)

@@ -18,3 +18,24 @@ def test_settings_that_are_changed_in_place(gpu):
     opt.betas[1] = 0.25
     opt.step()
     assert [(r["args"][0]["beta1"], r["args"][0]["beta2"]) for r in gpu.ran] == [(0.9, 0.999), (0.5, 0.999), (0.5, 0.25)]
+
+
+def test_every_graph_brings_the_list_that_it_needs(gpu):
+    """Gradients that moved between the eager call and the captures: whichever graph is replayed first, or alone, works on them."""
+    params = gpu.params(10, 20)
+    opt = gpu.adamw(params)
+    gpu.grads(params)
+    opt.step()
+    moved = [g.data_ptr() for g in gpu.grads(params)]
+    graphs = []
+    for _ in range(3):
+        with gpu.capture() as g:
+            opt.step(), opt.step()
+        graphs.append(g)
+    for g in reversed(graphs):                              # the first one last
+        gpu.ran.clear()
+        g.replay()
+        assert len(gpu.ran) == 2 and all(r["fits"] and r["list"]["grad"].tolist() == moved for r in gpu.ran)
+    gpu.ran.clear()
+    opt.step()
+    assert gpu.ran[0]["fits"] and gpu.ran[0]["list"]["grad"].tolist() == moved
