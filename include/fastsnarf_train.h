@@ -67,7 +67,13 @@ typedef struct {
  * not overlap one another or what it reads otherwise.  Allocates 84 bytes per tensor and 25 KiB.  On failure *out is NULL. */
 fs_status fs_tensors_create(const fs_tensor *list, int32_t count, void *hip_stream, fs_tensors **out);
 
-/* Free what the list owns.  Synchronises its stream first.  NULL is allowed. */
+/* The same in memory of the caller's, for callers that cannot allocate (graph capture): fs_tensors_bytes(count) bytes (0 for a count out of range) of the current
+ * device, aligned to 256.  The memory stays the caller's, and has to be there until the calls on the list are done, those of graphs that are replayed included.
+ * On a stream that records a graph, the list is brought to the device whenever the graph runs. */
+int64_t fs_tensors_bytes(int32_t count);
+fs_status fs_tensors_create_noalloc(const fs_tensor *list, int32_t count, void *hip_stream, void *workspace, int64_t bytes, fs_tensors **out);
+
+/* Free what the list owns.  Where it owns memory of the device, its stream is synchronised first.  NULL is allowed. */
 fs_status fs_tensors_destroy(fs_tensors *t);
 
 /* Other addresses, sizes or types for the same number of tensors, for the calls after this one (a program whose gradients move from
@@ -80,7 +86,8 @@ fs_status fs_tensors_update(fs_tensors *t, const fs_tensor *list, int32_t count)
 /* FS_OK if a call on the list would find it on the device now, FS_E_STATE if another update is needed before. */
 fs_status fs_tensors_ready(fs_tensors *t);
 
-/* The stream of the calls after this one.  The list's scratch is shared by all its calls: the caller orders this stream behind the one before. */
+/* The stream of the calls after this one.  The list's scratch is shared by all its calls, fs_grad_norm's included: the caller orders this stream behind the
+ * one before.  A graph that may be replayed beside other calls needs a list of its own. */
 fs_status fs_tensors_set_stream(fs_tensors *t, void *hip_stream);
 
 /* d_norm [1] = norm of all gradients (kind: FS_NORM_TWO or FS_NORM_MAX); of an empty list 0. */

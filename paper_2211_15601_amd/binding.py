@@ -23,7 +23,7 @@ FS_GRAD_BROYDEN_J, FS_GRAD_EXACT_J = 0, 1
 EXPORTS = ["fs_create", "fs_destroy", "fs_set_params", "fs_set_tuning", "fs_set_list_order", "fs_set_spin_limit", "fs_precompute", "fs_init", "fs_solve", "fs_grad",
            "fs_dedupe", "fs_dedupe_noalloc", "fs_get_transforms", "fs_get_corr", "fs_microbench", "fs_set_timing", "fs_get_timing", "fs_last_error",
            "fs_version",
-           "fs_tensors_create", "fs_tensors_destroy", "fs_tensors_update", "fs_tensors_ready", "fs_tensors_set_stream", "fs_tensors_error",
+           "fs_tensors_create", "fs_tensors_create_noalloc", "fs_tensors_bytes", "fs_tensors_destroy", "fs_tensors_update", "fs_tensors_ready", "fs_tensors_set_stream", "fs_tensors_error",
            "fs_grad_norm", "fs_grad_clip", "fs_adamw_step"]
 FS_FLOAT_FULL, FS_FLOAT_BRAIN, FS_FLOAT_HALF = 0, 1, 2
 FS_NORM_TWO, FS_NORM_MAX = 0, 1
@@ -96,6 +96,8 @@ def load():
     L.fs_dedupe.argtypes = [vp, vp, vp, i64, i32, ctypes.c_float, vp, vp, vp, vp, i64]
     L.fs_dedupe_noalloc.argtypes = L.fs_dedupe.argtypes
     L.fs_tensors_create.argtypes = [ctypes.POINTER(Tensor), i32, vp, ctypes.POINTER(vp)]
+    L.fs_tensors_create_noalloc.argtypes = [ctypes.POINTER(Tensor), i32, vp, vp, i64, ctypes.POINTER(vp)]
+    L.fs_tensors_bytes.argtypes = [i32]
     L.fs_tensors_destroy.argtypes = [vp]
     L.fs_tensors_update.argtypes = [vp, ctypes.POINTER(Tensor), i32]
     L.fs_tensors_ready.argtypes = [vp]
@@ -108,6 +110,7 @@ def load():
     for name in EXPORTS:
         if name not in ("fs_last_error", "fs_version", "fs_tensors_error"):
             getattr(L, name).restype = ctypes.c_int
+    L.fs_tensors_bytes.restype = i64
     _lib = L
     return L
 

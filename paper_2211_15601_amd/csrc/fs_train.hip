@@ -26,7 +26,8 @@ struct fs_tensors {
     bool params, moments, apart, in_place;      // in_place, apart: every `out` is, or none is, its gradient
     double grad_bytes, adam_bytes, param_bytes;
     ListD L;
-    char *mem;                // device: TensorD [asked], int [asked + 1], double [TRAIN_BLOCKS], unsigned [TICKETS]
+    char *mem;                // device, see Places
+    bool owned;               // `mem` was allocated here
     double *partial;
     unsigned *tickets;
     bool put;                 // the device's copy is that of `host`, for calls in the capture `put_in`; elsewhere too if that is none
@@ -277,15 +278,22 @@ int launch_norm(fs_tensors *t, int32_t kind, double scale, float *d_norm)
     return g.blocks;
 }
 
+// Where things lie in a list's memory: TensorD [count], int [count + 1], double [TRAIN_BLOCKS], unsigned [TICKETS].
+struct Places { size_t first, partial, tickets, end; };
+Places places_for(int32_t count)
+{
+    Places p;
+    p.first = (size_t)count * sizeof(TensorD);
+    p.partial = (p.first + ((size_t)count + 1) * sizeof(int) + 255) / 256 * 256;
+    p.tickets = p.partial + TRAIN_BLOCKS * sizeof(double);
+    p.end = p.tickets + TICKETS * sizeof(unsigned);
+    return p;
+}
+
 bool scale_ok(double s) { return s > 0.0 && std::isfinite(s); }
 
-}  // namespace
-
-extern "C" {
-
-const char *fs_tensors_error(const fs_tensors *t) { return t ? t->err : "null list"; }
-
-fs_status fs_tensors_create(const fs_tensor *list, int32_t count, void *hip_stream, fs_tensors **out)
+// A list in memory of the caller's, or, workspace == NULL, of its own.
+fs_status create(const fs_tensor *list, int32_t count, void *hip_stream, void *workspace, fs_tensors **out)
 {
     if (out) *out = nullptr;
     if (!out || (!list && count > 0)) return FS_E_ARG;
@@ -305,27 +313,29 @@ fs_status fs_tensors_create(const fs_tensor *list, int32_t count, void *hip_stre
     t->host = new (std::nothrow) TensorD[count + 1];
     fs_status s = t->given && t->host ? FS_OK : FS_E_ALLOC;
     if (s == FS_OK) s = check_list(t, "fs_tensors_create", list, count, nullptr);
+    if (s == FS_OK && workspace && !on_device(t, workspace)) s = FS_E_ARG;
     if (s == FS_OK) {
         if (hipDeviceGetAttribute(&t->n_cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || t->n_cus < 1) t->n_cus = 256;
         (void)hipGetLastError();
         t->n_cus = std::min(t->n_cus, TRAIN_BLOCKS / NORM.per_cu);
-        const size_t at_first = (size_t)count * sizeof(TensorD), at_partial = (at_first + ((size_t)count + 1) * sizeof(int) + 255) / 256 * 256;
-        const size_t at_tickets = at_partial + TRAIN_BLOCKS * sizeof(double);
-        if (hipMalloc(reinterpret_cast<void **>(&t->mem), at_tickets + TICKETS * sizeof(unsigned)) != hipSuccess) {
+        const Places at = places_for(count);
+        t->mem = static_cast<char *>(workspace);
+        t->owned = !workspace;
+        if (t->owned && hipMalloc(reinterpret_cast<void **>(&t->mem), at.end) != hipSuccess) {
             (void)hipGetLastError();
             t->mem = nullptr;
             s = FS_E_ALLOC;
         } else {
             t->L.tensors = reinterpret_cast<TensorD *>(t->mem);
-            t->L.first = reinterpret_cast<int *>(t->mem + at_first);
-            t->partial = reinterpret_cast<double *>(t->mem + at_partial);
-            t->tickets = reinterpret_cast<unsigned *>(t->mem + at_tickets);
+            t->L.first = reinterpret_cast<int *>(t->mem + at.first);
+            t->partial = reinterpret_cast<double *>(t->mem + at.partial);
+            t->tickets = reinterpret_cast<unsigned *>(t->mem + at.tickets);
             k_tickets_clear<<<1, 256, 0, t->stream>>>(t->tickets);
             s = put_list(t, "fs_tensors_create", list);
         }
     }
     if (s != FS_OK) {
-        if (t->mem) (void)hipFree(t->mem);
+        if (t->mem && t->owned) (void)hipFree(t->mem);
         delete[] t->given;
         delete[] t->host;
         delete t;
@@ -335,11 +345,30 @@ fs_status fs_tensors_create(const fs_tensor *list, int32_t count, void *hip_stre
     return FS_OK;
 }
 
+}  // namespace
+
+extern "C" {
+
+const char *fs_tensors_error(const fs_tensors *t) { return t ? t->err : "null list"; }
+
+int64_t fs_tensors_bytes(int32_t count) { return count < 0 || count > FS_MAX_TENSORS ? 0 : (int64_t)places_for(count).end; }
+
+fs_status fs_tensors_create(const fs_tensor *list, int32_t count, void *hip_stream, fs_tensors **out) { return create(list, count, hip_stream, nullptr, out); }
+
+fs_status fs_tensors_create_noalloc(const fs_tensor *list, int32_t count, void *hip_stream, void *workspace, int64_t bytes, fs_tensors **out)
+{
+    if (out) *out = nullptr;
+    if (count >= 0 && count <= FS_MAX_TENSORS && (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 || bytes < fs_tensors_bytes(count))) return FS_E_ARG;
+    return create(list, count, hip_stream, workspace, out);
+}
+
 fs_status fs_tensors_destroy(fs_tensors *t)
 {
     if (!t) return FS_OK;
-    (void)hipStreamSynchronize(t->stream);
-    (void)hipFree(t->mem);
+    if (t->owned) {
+        (void)hipStreamSynchronize(t->stream);
+        (void)hipFree(t->mem);
+    }
     delete[] t->given;
     delete[] t->host;
     delete t;

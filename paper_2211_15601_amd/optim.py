@@ -68,11 +68,24 @@ def _check_apart(arrays):
         raise ValueError("tensors of the list overlap in memory")
 
 
-class _Handle:
-    """An fs_tensors, its host list and its stream.  Holds no tensors.
+class _OnDevice:
+    """An fs_tensors: the list on the device, the scratch of its calls, their stream."""
 
-    A captured graph reads the list's copy on the device when it is replayed.  An fs_tensors that was captured therefore keeps its list, and is never
-    destroyed: when the list changes afterwards, another takes its place."""
+    def __init__(self, L, h, version, stream, workspace=None):
+        self.L, self.h, self.version, self.stream, self.raw, self.workspace = L, h, version, stream, stream.cuda_stream, workspace
+
+    def __del__(self):
+        try:
+            self.L.fs_tensors_destroy(self.h)
+        except Exception:
+            pass
+
+
+class _Handle:
+    """A list on the host, and on the device once for eager calls and once for the graph that is captured now, or was last.  Holds no tensors.
+
+    A graph is replayed where and when its owner likes, so its calls have a list and scratch of their own, in memory of the graph's pool, and
+    the graph brings the list there whenever it runs: what other calls and other graphs use, it neither reads nor writes."""
 
     def __init__(self, count: int, device: torch.device):
         self.L = binding.load()
@@ -83,57 +96,77 @@ class _Handle:
         self.list = (binding.Tensor * max(1, count))()
         self.columns = np.frombuffer(self.list, dtype=_COLUMNS)[:count]
         self.columns["lr_scale"] = self.columns["decay_scale"] = 1.0
-        self._h = None
-        self.captured = False          # a graph has calls on it
-        self.recorded = False          # the last put was recorded, not run
+        self.version = 0               # of the columns; who changes them counts it up
+        self.eager = self.graph = None
+        self._h = None                 # of the call being made
 
-    def ready(self, put, unchanged: bool):
-        """Before a call: put() if the list has changed, and the stream."""
+    def ready(self):
+        """Before a call: the list where the current stream's calls find it."""
         # the current stream's number; asking for the stream itself makes an object, 2 us of the 7 that a call then takes the host
         raw = torch._C._cuda_getCurrentRawStream(self.device.index)
-        capturing = raw != 0 and torch.cuda.is_current_stream_capturing()      # the default stream is none that can be captured
-        if not unchanged:
-            put()
-        if raw != self._raw:
-            self.to_stream(capturing)
-        # a put that was recorded is for the calls behind it in the same graph: others, which may run before it or without it, need their own
-        if self.recorded and (not capturing or self.L.fs_tensors_ready(self._h) != binding.FS_OK):
-            self.put(again=True)
-        if capturing:
-            self.captured = True
+        if raw != 0 and torch.cuda.is_current_stream_capturing():              # the default stream is none that can be captured
+            x = self.in_graph(raw)
+        else:
+            x = self.eager
+            if x is None or x.version != self.version:
+                x = self.put()
+            elif raw != x.raw:
+                self.to_stream(x)
+        self._h = x.h
 
-    def put(self, again=False):
-        """Hands the list over: the first time, after it has changed, or, `again`, as it is."""
-        capturing = torch.cuda.is_current_stream_capturing()
-        if self._h is not None and (not self.captured or again and capturing):
-            if torch._C._cuda_getCurrentRawStream(self.device.index) != self._raw:
-                self.to_stream(capturing)
-            self.ret(self.L.fs_tensors_update(self._h, self.list, self.count))
-            self.recorded = capturing
-            return
-        if capturing:
-            raise RuntimeError("a list has to be made, and used with tensors that do not move from one graph to the next, before a graph is captured")
+    def put(self):
+        """Hands the list over for eager calls: the first time, or after it has changed."""
+        x = self.eager
+        if x is None:
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("a list has to be made, or used once, before a graph is captured")
+            x = self.eager = self.make()
+        else:
+            if torch._C._cuda_getCurrentRawStream(self.device.index) != x.raw:
+                self.to_stream(x)
+            self._h = x.h
+            self.ret(self.L.fs_tensors_update(x.h, self.list, self.count))
+            x.version = self.version
+        return x
+
+    def in_graph(self, raw):
+        x = self.graph
+        if self.eager is None:
+            raise RuntimeError("a list has to be made, or used once, before a graph is captured")
+        if x is not None and raw != x.raw:
+            self.to_stream(x)
+        if x is None or self.L.fs_tensors_ready(x.h) != binding.FS_OK:         # none yet, or of an earlier graph
+            workspace = torch.empty(self.L.fs_tensors_bytes(self.count), dtype=torch.uint8, device=self.device)
+            x = self.graph = self.make(workspace)
+        elif x.version != self.version:
+            self._h = x.h
+            self.ret(self.L.fs_tensors_update(x.h, self.list, self.count))
+            x.version = self.version
+        return x
+
+    def make(self, workspace=None):
         h = ctypes.c_void_p()
         with torch.cuda.device(self.device):
             stream = torch.cuda.current_stream(self.device)
-            st = self.L.fs_tensors_create(self.list, self.count, stream.cuda_stream, ctypes.byref(h))
+            if workspace is None:
+                st = self.L.fs_tensors_create(self.list, self.count, stream.cuda_stream, ctypes.byref(h))
+            else:
+                st = self.L.fs_tensors_create_noalloc(self.list, self.count, stream.cuda_stream, workspace.data_ptr(), workspace.nbytes, ctypes.byref(h))
         if st != binding.FS_OK:
             raise binding.FsError(st, "fs_tensors_create failed")
-        self._h, self._stream, self._raw = h, stream, stream.cuda_stream
-        self.captured = self.recorded = False
+        return _OnDevice(self.L, h, self.version, stream, workspace)
 
     def ret(self, st):
         if st != binding.FS_OK:
             raise binding.FsError(st, self.L.fs_tensors_error(self._h).decode())
 
-    def to_stream(self, capturing):
+    def to_stream(self, x):
         now = torch.cuda.current_stream(self.device)
-        # the list's scratch is one: this stream's calls come after those of the stream before.  A stream that records a graph cannot wait
-        # for work outside of it; torch.cuda.graph waits for the whole device before it records.
-        if not capturing:
-            now.wait_stream(self._stream)
-        self._stream, self._raw = now, now.cuda_stream
-        self.ret(self.L.fs_tensors_set_stream(self._h, self._raw))
+        if x is self.eager:
+            now.wait_stream(x.stream)          # the scratch is one: this stream's calls come after those of the stream before
+        x.stream, x.raw = now, now.cuda_stream
+        self._h = x.h
+        self.ret(self.L.fs_tensors_set_stream(x.h, x.raw))
 
     def norm(self, norm):
         """Where a call's norm goes or comes from."""
@@ -143,14 +176,6 @@ class _Handle:
         if norm.numel() != 1:
             raise ValueError("norm must have one element")
         return norm
-
-    def __del__(self):
-        try:
-            if self._h is not None and not self.captured:
-                self.L.fs_tensors_destroy(self._h)
-                self._h = None
-        except Exception:
-            pass
 
 
 def _lists(n: int, **lists):
@@ -208,14 +233,11 @@ class TensorList:
         c["grad"], c["out"], c["n"], c["grad_type"] = _places(grads), _places(outs), _sizes(grads), _types(grads)
         h.put()
 
-    def _ready(self):
-        self._handle.ready(self._handle.put, True)
-
     def grad_norm(self, kind: str = "l2", grad_scale: float = 1.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Global norm of the gradients times grad_scale, float32 [1]: "l2", or "max", the largest magnitude."""
         h = self._handle
         out = h.norm(out)
-        self._ready()
+        h.ready()
         h.ret(h.L.fs_grad_norm(h._h, _kind(kind), grad_scale, out.data_ptr()))
         return out
 
@@ -224,7 +246,7 @@ class TensorList:
         spread over several GPUs, say) is taken as it is."""
         h = self._handle
         d = h.norm(norm)
-        self._ready()
+        h.ready()
         h.ret(h.L.fs_grad_clip(h._h, _kind(kind), max_norm, grad_scale, norm is not None, d.data_ptr()))
         torch.autograd.graph.increment_version(self._written)
         return d
@@ -285,6 +307,7 @@ class AdamW:
         _check_apart(self.params + self.masters + self.exp_avgs + self.exp_avg_sqs + (self._given or []))
         if self._given is not None:
             self._put(self._given, _places(self.params))
+            h.put()
 
     def _put(self, grads, now):
         h, c = self._handle, self._handle.columns
@@ -299,9 +322,8 @@ class AdamW:
         self._places = None
         c["grad"], c["param"] = _places(grads), now[:h.count]
         c["n"], c["grad_type"] = _sizes(grads), _types(grads)
-        self._looks = self._look(grads)
-        h.put()
-        self._places = now
+        h.version += 1
+        self._looks, self._places = self._look(grads), now
 
     @staticmethod
     def _look(grads):
@@ -318,7 +340,9 @@ class AdamW:
             grads = [p.grad for p in self.params]
             now += _places(grads)
             unchanged = self._look(grads) == self._looks
-        h.ready(lambda: self._put(grads, now), unchanged and now == self._places)
+        if not unchanged or now != self._places:
+            self._put(grads, now)
+        h.ready()
         asked = norm is not None or self.max_norm is not None or self.skip_nonfinite
         d = h.norm(norm) if asked else None
         lr = self.lr

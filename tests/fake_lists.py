@@ -55,6 +55,8 @@ class Machine:
         monkeypatch.setattr(torch.cuda, "current_device", lambda: self.device)
         monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: self.device)
         monkeypatch.setattr(torch.cuda, "device", self.on_device)
+        empty = torch.empty
+        monkeypatch.setattr(torch, "empty", lambda *size, device=None, **k: on_gpu(empty(*size, **k)) if device == GPU else empty(*size, device=device, **k))
 
     @contextlib.contextmanager
     def on_device(self, device):
@@ -102,6 +104,12 @@ class Machine:
 
     def fs_tensors_create(self, array, count, stream, out):
         return self._new(array, count, stream, out, None)
+
+    def fs_tensors_create_noalloc(self, array, count, stream, workspace, size, out):
+        return self._new(array, count, stream, out, ("workspace", workspace))
+
+    def fs_tensors_bytes(self, count):
+        return 100 + count
 
     def fs_tensors_update(self, h, array, count):
         return self._put(h.value, array, count)

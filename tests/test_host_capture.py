@@ -90,3 +90,42 @@ assert L.fs_tensors_update(h, other, 1) == E_DEVICE
 S.stub_fail_launch(-1)
 assert ready(h) == E_STATE and "graph" not in error(h)
 """, tmp_path)
+
+
+def test_a_list_in_memory_of_the_callers(tmp_path):
+    run("""
+L.fs_tensors_bytes.restype = ctypes.c_int64
+need = L.fs_tensors_bytes
+assert need(-1) == need((1 << 20) + 1) == 0 and 0 < need(0) <= 27000 and need(1000) <= need(0) + 1000 * 84 + 256
+
+def noalloc(tensors, status=OK, at=buf(20), size=None, count=None):
+    h = ctypes.c_void_p(77)
+    n = len(tensors) if count is None else count
+    st = L.fs_tensors_create_noalloc(array(*tensors, tensor()), n, A, at, ctypes.c_int64(need(n) if size is None else size), ctypes.byref(h))
+    assert st == status and (h.value is None) == (status != OK), st
+    return h
+
+one = [tensor()]
+noalloc(one, E_ARG, at=None), noalloc(one, E_ARG, at=ctypes.c_void_p(buf(20).value + 128)), noalloc(one, E_ARG, size=need(1) - 1), noalloc(one, E_ARG, size=-1)
+noalloc([], E_SHAPE, count=-1), noalloc([], E_SHAPE, count=(1 << 20) + 1), noalloc([tensor(n=-1)], E_SHAPE), noalloc([tensor(grad=None)], E_ARG)
+h = ctypes.c_void_p(77)
+assert L.fs_tensors_create_noalloc(None, 1, A, buf(20), ctypes.c_int64(1 << 20), ctypes.byref(h)) == E_ARG and h.value is None
+assert L.fs_tensors_create_noalloc(array(tensor()), 1, A, buf(20), ctypes.c_int64(1 << 20), None) == E_ARG
+assert names() == []
+S.stub_fail_allocation(0)                                   # it asks for none
+capture(A, 3)
+for tensors in ([], one, 101 * one):
+    h = noalloc(tensors)
+    assert names() == ["k_tickets_clear"] + -(-len(tensors) // 40) * ["k_list_put"]
+    assert norm(h) == OK and clip(h) == OK and adamw(h, how()) == OK
+    capture(A, 4)
+    assert norm(h) == E_STATE and "graph" in error(h)
+    capture(A, 3)
+    S.stub_clear_launches()
+    assert L.fs_tensors_destroy(h) == OK
+for n in range(2):
+    S.stub_fail_launch(n)
+    noalloc(one, E_DEVICE)
+    S.stub_fail_launch(-1)
+assert S.stub_live_blocks() == 0 and S.stub_bad_frees() == 0
+""", tmp_path)

@@ -1,5 +1,6 @@
 """Host code of optim.py without a GPU (fake_lists.py): what it hands to the library, and when."""
 import pytest
+import torch
 
 import fake_lists
 
@@ -39,3 +40,29 @@ def test_every_graph_brings_the_list_that_it_needs(gpu):
     gpu.ran.clear()
     opt.step()
     assert gpu.ran[0]["fits"] and gpu.ran[0]["list"]["grad"].tolist() == moved
+
+
+def test_graphs_have_scratch_of_their_own(gpu):
+    """Replays are ordered behind nothing that optim.py knows of: beside an eager call, or another graph's replay, they must not share counters."""
+    lst = gpu.optim.TensorList([fake_lists.on_gpu(g) for g in (torch.ones(10), torch.ones(20))])
+    out = fake_lists.on_gpu(torch.zeros(1))
+    params = gpu.params(10, 20)
+    opt = gpu.adamw(params, grads=gpu.grads(params))
+    for call in (lambda: lst.grad_norm(out=out), lambda: lst.clip_grads(1.0, norm=out), opt.step):
+        gpu.ran.clear()
+        call()
+        graphs = []
+        for _ in range(2):
+            with gpu.capture() as g:
+                call(), call()
+            graphs.append(g)
+        with gpu.on(6):
+            call()
+        for g in graphs[::-1]:
+            g.replay()
+        call()
+        assert all(r["fits"] for r in gpu.ran)
+        eager, one, two = ({r["scratch"] for r in gpu.ran[a:b]} for a, b in ((0, 2), (2, 4), (4, 6)))
+        assert len(eager) == len(one) == len(two) == 1 and len(eager | one | two) == 3 and gpu.ran[6]["scratch"] in eager
+        graphs[0].replay()
+        assert gpu.ran[-1]["scratch"] in two and gpu.ran[-1]["fits"]
