@@ -150,8 +150,8 @@ int lead_of(const fs_tensor &x)
     return (int)(at % MAX_LEAD);
 }
 
-// Takes a checked list over: the host's copies, and the device's in the stream's order.
-fs_status put_list(fs_tensors *t, const char *what, const fs_tensor *list)
+// Takes a checked list over: the host's copies, and the device's in the stream's order, with counters that are cleared (NULL: they are).
+fs_status put_list(fs_tensors *t, const char *what, const fs_tensor *list, unsigned *tickets)
 {
     t->put = false;
     int count = 0, units = 0;
@@ -185,11 +185,11 @@ fs_status put_list(fs_tensors *t, const char *what, const fs_tensor *list)
     }
     t->L.count = count;
     t->L.units = units;
-    for (int at = 0; at < count; at += PUT) {
+    for (int at = 0; at < count || tickets; at += PUT, tickets = nullptr) {
         PutD p;
         const int n = std::min(PUT, count - at);
         std::memcpy(p.t, t->host + at, n * sizeof(TensorD));
-        k_list_put<<<1, 64, 0, t->stream>>>(p, at, n, const_cast<TensorD *>(t->L.tensors), const_cast<int *>(t->L.first));
+        k_list_put<<<1, 64, 0, t->stream>>>(p, at, n, const_cast<TensorD *>(t->L.tensors), const_cast<int *>(t->L.first), tickets);
     }
     const fs_status s = launch_status(t, what);
     t->put = s == FS_OK;
@@ -330,8 +330,8 @@ fs_status create(const fs_tensor *list, int32_t count, void *hip_stream, void *w
             t->L.first = reinterpret_cast<int *>(t->mem + at.first);
             t->partial = reinterpret_cast<double *>(t->mem + at.partial);
             t->tickets = reinterpret_cast<unsigned *>(t->mem + at.tickets);
-            k_tickets_clear<<<1, 256, 0, t->stream>>>(t->tickets);
-            s = put_list(t, "fs_tensors_create", list);
+            if (t->owned) k_tickets_clear<<<1, 256, 0, t->stream>>>(t->tickets);
+            s = put_list(t, "fs_tensors_create", list, t->owned ? nullptr : t->tickets);
         }
     }
     if (s != FS_OK) {
@@ -381,7 +381,7 @@ fs_status fs_tensors_update(fs_tensors *t, const fs_tensor *list, int32_t count)
     if (count != t->asked) return fail(t, FS_E_SHAPE, "fs_tensors_update: the list has %d tensors, not %d", t->asked, count);
     if (!list && count) return fail(t, FS_E_ARG, "fs_tensors_update: list is NULL");
     const fs_status s = check_list(t, "fs_tensors_update", list, count, t->given);
-    return s == FS_OK ? put_list(t, "fs_tensors_update", list) : s;
+    return s == FS_OK ? put_list(t, "fs_tensors_update", list, nullptr) : s;
 }
 
 fs_status fs_tensors_set_stream(fs_tensors *t, void *hip_stream)

@@ -46,9 +46,12 @@ constexpr int PUT = 40;                // tensors that one launch of k_list_put 
 struct PutD { TensorD t[PUT]; };
 
 // The list travels in kernel arguments: in the stream's order, without host memory that has to outlive the call, and as part of a captured graph.
-__global__ __launch_bounds__(64) void k_list_put(PutD p, int at, int n, TensorD *__restrict__ tensors, int *__restrict__ first)
+// There it runs at every replay, and so does the clearing of the counters (`tickets`, or NULL), which would take a launch of its own some 2 us.
+__global__ __launch_bounds__(64) void k_list_put(PutD p, int at, int n, TensorD *__restrict__ tensors, int *__restrict__ first, unsigned *__restrict__ tickets)
 {
     const int i = threadIdx.x;
+    if (tickets)
+        for (int k = i; k < TICKETS; k += 64) tickets[k] = 0u;
     if (i >= n) return;
     tensors[at + i] = p.t[i];
     first[at + i] = p.t[i].first;

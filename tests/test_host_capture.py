@@ -116,16 +116,15 @@ S.stub_fail_allocation(0)                                   # it asks for none
 capture(A, 3)
 for tensors in ([], one, 101 * one):
     h = noalloc(tensors)
-    assert names() == ["k_tickets_clear"] + -(-len(tensors) // 40) * ["k_list_put"]
+    assert names() == max(1, -(-len(tensors) // 40)) * ["k_list_put"]      # the first one clears the counters
     assert norm(h) == OK and clip(h) == OK and adamw(h, how()) == OK
     capture(A, 4)
     assert norm(h) == E_STATE and "graph" in error(h)
     capture(A, 3)
     S.stub_clear_launches()
     assert L.fs_tensors_destroy(h) == OK
-for n in range(2):
-    S.stub_fail_launch(n)
-    noalloc(one, E_DEVICE)
-    S.stub_fail_launch(-1)
+S.stub_fail_launch(0)
+noalloc(one, E_DEVICE)
+S.stub_fail_launch(-1)
 assert S.stub_live_blocks() == 0 and S.stub_bad_frees() == 0
 """, tmp_path)
