@@ -133,12 +133,17 @@ class _Handle:
         x = self.graph
         if self.eager is None:
             raise RuntimeError("a list has to be made, or used once, before a graph is captured")
+        before = None
         if x is not None and raw != x.raw:
+            before = x.stream
             self.to_stream(x)
         if x is None or self.L.fs_tensors_ready(x.h) != binding.FS_OK:         # none yet, or of an earlier graph
             workspace = torch.empty(self.L.fs_tensors_bytes(self.count), dtype=torch.uint8, device=self.device)
             x = self.graph = self.make(workspace)
-        elif x.version != self.version:
+            return x
+        if before is not None:
+            x.stream.wait_stream(before)       # another stream of the same graph
+        if x.version != self.version:
             self._h = x.h
             self.ret(self.L.fs_tensors_update(x.h, self.list, self.count))
             x.version = self.version

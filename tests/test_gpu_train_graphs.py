@@ -95,3 +95,25 @@ def test_one_graph_on_two_streams(optim):
         torch.cuda.synchronize()
         assert [float(x) for x in (a, b, c)] == [want, 2 * want, 4 * want]
         assert float(lst.grad_norm()) == want
+
+
+def test_branches_of_one_graph(optim):
+    """Calls that the graph itself leaves unordered: the list's scratch orders them."""
+    g = torch.full((3_000_001,), 2.0, device=DEV)
+    lst = optim.TensorList([g])
+    want = float(lst.grad_norm())
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        main = torch.cuda.current_stream()
+        side.wait_stream(main)
+        a = lst.grad_norm()
+        with torch.cuda.stream(side):
+            b = lst.grad_norm(grad_scale=2.0)
+        c = lst.grad_norm(grad_scale=4.0)
+        main.wait_stream(side)
+    for _ in range(5):
+        for x in (a, b, c):
+            x.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert [float(x) for x in (a, b, c)] == [want, 2 * want, 4 * want]

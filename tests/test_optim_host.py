@@ -66,3 +66,25 @@ def test_graphs_have_scratch_of_their_own(gpu):
         assert len(eager) == len(one) == len(two) == 1 and len(eager | one | two) == 3 and gpu.ran[6]["scratch"] in eager
         graphs[0].replay()
         assert gpu.ran[-1]["scratch"] in two and gpu.ran[-1]["fits"]
+
+
+def test_calls_of_one_graph_on_several_streams_come_one_after_another(gpu):
+    params = gpu.params(10)
+    opt = gpu.adamw(params, grads=gpu.grads(params))
+    opt.step()
+    with gpu.capture(9) as g:
+        opt.step()
+        gpu.captures[11] = gpu.captures[9]                  # a stream that has joined the capture
+        gpu.waits.clear()
+        with gpu.on(11):
+            opt.step()
+        assert gpu.waits == [(11, 9)]
+        opt.step()
+        assert gpu.waits == [(11, 9), (9, 11)]
+        del gpu.captures[11]
+    g.replay()
+    assert all(r["fits"] for r in gpu.ran) and len({r["scratch"] for r in gpu.ran[1:]}) == 1
+    # the stream of the capture is no stream to wait for outside of it
+    gpu.waits.clear()
+    opt.step()
+    assert gpu.waits == []
