@@ -304,49 +304,53 @@ class AdamW:
                 if g is not None:
                     _check("grads", i, g, p, h.device, _TYPES)
             self._given = _aliases(given)
-        self._places = self._looks = None
+        self._params_look = self._grads_look = None
         self._how, self._set_to = binding.AdamW(), None
         c = h.columns
         c["master"], c["exp_avg"], c["exp_avg_sq"] = _places(self.masters), _places(self.exp_avgs), _places(self.exp_avg_sqs)
         c["lr_scale"], c["decay_scale"] = lr_scales, decay_scales
         _check_apart(self.params + self.masters + self.exp_avgs + self.exp_avg_sqs + (self._given or []))
         if self._given is not None:
-            self._put(self._given, _places(self.params))
+            self._put(self._given, self._look_at_params(self.params), None)
             h.put()
 
-    def _put(self, grads, now):
+    def _put(self, grads, params_look, grads_look):
         h, c = self._handle, self._handle.columns
-        if self._places is None or self._places[:h.count] != now[:h.count]:
-            for i, p in enumerate(self.params):              # they may have another type or order now
+        # parameters may have another type or size now; or another order, and then their gradients have, too
+        anew = params_look != self._params_look or grads_look and grads_look[2] != self._grads_look[2]
+        for i, (g, p) in enumerate(zip(grads, self.params)):
+            if anew:
                 _check("params", i, p, None, h.device, _TYPES)
                 _check("exp_avgs", i, self.exp_avgs[i], p, h.device, [torch.float32])
-            c["param_type"] = _types(self.params)
-        for i, (g, p) in enumerate(zip(grads, self.params)):
             if g is not None:
                 _check("grads", i, g, p, h.device, _TYPES)
-        self._places = None
-        c["grad"], c["param"] = _places(grads), now[:h.count]
-        c["n"], c["grad_type"] = _sizes(grads), _types(grads)
+        c["param"], c["param_type"] = params_look[0], _types(self.params)
+        c["grad"], c["n"], c["grad_type"] = _places(grads), _sizes(grads), _types(grads)
         h.version += 1
-        self._looks, self._places = self._look(grads), now
+        self._params_look, self._grads_look = params_look, grads_look
 
     @staticmethod
-    def _look(grads):
-        """What gradients could have other than those before them at the same place, apart from the shape, which a parameter prescribes."""
-        return [None if g is None else (g.dtype, g.is_contiguous() or g.stride()) for g in grads]
+    def _look_at_params(params):
+        """What parameters could have other than those before them: the place, and at the same place (memory that was freed and taken again, another
+        view of it) the type and the size."""
+        return list(map(torch.Tensor.data_ptr, params)), [p.dtype for p in params], list(map(torch.Tensor.numel, params))
+
+    @staticmethod
+    def _look_at_grads(grads):
+        """The same of gradients that are not held here; their shape is prescribed by the parameters."""
+        look = [(0, None, None) if g is None else (g.data_ptr(), g.dtype, g.is_contiguous() or g.stride()) for g in grads]
+        return list(zip(*look)) or [(), (), ()]
 
     def step(self, norm: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
         """One step.  Returns the gradients' global norm, float32 [1] (None where neither max_norm nor skip_nonfinite asks for it); a
         `norm` that is given is taken as it is (one over several GPUs, say)."""
         h, how = self._handle, self._how
-        now, grads, unchanged = _places(self.params), self._given, True
+        params_look, grads, grads_look = self._look_at_params(self.params), self._given, None
         if grads is None:
-            # gradients that are not held here may lie elsewhere, or have been replaced by others at the same place
             grads = [p.grad for p in self.params]
-            now += _places(grads)
-            unchanged = self._look(grads) == self._looks
-        if not unchanged or now != self._places:
-            self._put(grads, now)
+            grads_look = self._look_at_grads(grads)
+        if params_look != self._params_look or grads_look != self._grads_look:
+            self._put(grads, params_look, grads_look)
         h.ready()
         asked = norm is not None or self.max_norm is not None or self.skip_nonfinite
         d = h.norm(norm) if asked else None

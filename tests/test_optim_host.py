@@ -88,3 +88,58 @@ def test_calls_of_one_graph_on_several_streams_come_one_after_another(gpu):
     gpu.waits.clear()
     opt.step()
     assert gpu.waits == []
+
+
+def _other_type_at_the_same_place(p, dtype):
+    at = p.data_ptr()
+    p.data = fake_lists.on_gpu(p.detach().as_subclass(torch.Tensor).view(dtype).reshape(-1)[:p.numel()].view(p.shape))
+    assert p.data_ptr() == at and p.dtype == dtype
+
+
+@pytest.mark.parametrize("given", [False, True])
+def test_parameters_of_another_type_at_the_same_place(gpu, given):
+    """A block that was freed and taken again, or a view of it in 16 bits: four bytes an element would go past its end."""
+    params = gpu.params(10, 20)
+    grads = gpu.grads(params)
+    opt = gpu.adamw(params, grads=grads if given else None)
+    opt.step()
+    for dtype, code in ((torch.bfloat16, gpu.binding.FS_FLOAT_BRAIN), (torch.float16, gpu.binding.FS_FLOAT_HALF)):
+        params[1].grad = None
+        _other_type_at_the_same_place(params[1], dtype)
+        if not given:
+            params[1].grad = fake_lists.on_gpu(torch.ones(20, dtype=dtype))
+        opt.step()
+        assert gpu.ran[-1]["fits"] and gpu.ran[-1]["list"]["param_type"].tolist() == [gpu.binding.FS_FLOAT_FULL, code]
+
+
+@pytest.mark.parametrize("given", [False, True])
+def test_parameters_of_another_size_at_the_same_place_are_refused(gpu, given):
+    params = gpu.params(10, 20)
+    opt = gpu.adamw(params, grads=gpu.grads(params) if given else None)
+    opt.step()
+    at, whole, grad = params[1].data_ptr(), params[1].data, params[1].grad
+    params[1].grad = None
+    params[1].data = whole[:5]
+    assert params[1].data_ptr() == at
+    if not given:
+        params[1].grad = fake_lists.on_gpu(torch.ones(5))
+    for _ in range(2):
+        with pytest.raises(ValueError, match=r"\[1\]: shape"):
+            opt.step()
+    assert len(gpu.ran) == 1
+    params[1].grad = None
+    params[1].data = whole
+    params[1].grad = grad
+    opt.step()
+    assert len(gpu.ran) == 2 and gpu.ran[-1]["fits"]
+
+
+def test_parameters_in_another_order_at_the_same_place_are_refused(gpu):
+    p = fake_lists.on_gpu(torch.ones(4, 6)).requires_grad_(True)
+    opt = gpu.adamw([p])
+    gpu.grads([p])
+    opt.step()
+    p.grad, p.data = None, p.data.as_strided((4, 6), (1, 4))
+    p.grad = fake_lists.on_gpu(torch.ones(6, 4)).t()
+    with pytest.raises(ValueError, match=r"exp_avgs\[0\]"):
+        opt.step()
