@@ -271,7 +271,8 @@ class AdamW:
       lr_scales, decay_scales   factors per parameter on lr and weight_decay
       exp_avgs, exp_avg_sqs, step   state to go on from: float32 tensors like the parameters, and an int64 tensor of one element
 
-    State: .masters, .exp_avgs, .exp_avg_sqs, .step_count (updated in place), see state_dict()."""
+    State: .step_count, and .masters, .exp_avgs, .exp_avg_sqs, by the memory that they have now (updated in place; other values come
+    by load_state_dict())."""
 
     def __init__(self, params: Sequence[torch.Tensor], grads=None, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2,
                  max_norm: Optional[float] = None, grad_scale: float = 1.0, skip_nonfinite: bool = False, masters=None, lr_scales=None,
@@ -286,17 +287,18 @@ class AdamW:
         if masters is True:
             masters = [p.detach().to(torch.float32, memory_format=torch.preserve_format) if p.dtype != torch.float32 else None for p in self.params]
         zeros = lambda: [torch.zeros_like(p, dtype=torch.float32, memory_format=torch.preserve_format, requires_grad=False) for p in self.params]
-        (self.masters,) = _lists(n, masters=masters or None)
-        self.exp_avgs, self.exp_avg_sqs = _lists(n, exp_avgs=zeros() if exp_avgs is None else exp_avgs, exp_avg_sqs=zeros() if exp_avg_sqs is None else exp_avg_sqs)
+        (masters,) = _lists(n, masters=masters or None)
+        moments = _lists(n, exp_avgs=zeros() if exp_avgs is None else exp_avgs, exp_avg_sqs=zeros() if exp_avg_sqs is None else exp_avg_sqs)
         lr_scales, decay_scales = _lists(n, lr_scales=[1.0] * n if lr_scales is None else lr_scales, decay_scales=[1.0] * n if decay_scales is None else decay_scales)
-        for name, v in (("masters", self.masters), ("exp_avgs", self.exp_avgs), ("exp_avg_sqs", self.exp_avg_sqs)):
+        for name, v in (("masters", masters), ("exp_avgs", moments[0]), ("exp_avg_sqs", moments[1])):
             for i, (t, p) in enumerate(zip(v, self.params)):
                 if t is not None or name != "masters":
                     _check(name, i, t, p, h.device, [torch.float32])
+        # not the tensors themselves: whoever has them may give them other memory, and the list goes on with this
+        self._masters, self._exp_avgs, self._exp_avg_sqs = _aliases(masters), _aliases(moments[0]), _aliases(moments[1])
         self.step_count = step if step is not None else torch.zeros(1, dtype=torch.int64, device=h.device)
-        _check("step", 0, self.step_count, None, h.device, [torch.int64])
-        if self.step_count.numel() != 1:
-            raise ValueError("step must have one element")
+        self._counter = None
+        self._check_counter()
         self._given = None
         if grads is not None:
             (given,) = _lists(n, grads=grads)
@@ -307,12 +309,22 @@ class AdamW:
         self._params_look = self._grads_look = None
         self._how, self._set_to = binding.AdamW(), None
         c = h.columns
-        c["master"], c["exp_avg"], c["exp_avg_sq"] = _places(self.masters), _places(self.exp_avgs), _places(self.exp_avg_sqs)
+        c["master"], c["exp_avg"], c["exp_avg_sq"] = _places(self._masters), _places(self._exp_avgs), _places(self._exp_avg_sqs)
         c["lr_scale"], c["decay_scale"] = lr_scales, decay_scales
-        _check_apart(self.params + self.masters + self.exp_avgs + self.exp_avg_sqs + (self._given or []))
+        _check_apart(self.params + self._masters + self._exp_avgs + self._exp_avg_sqs + (self._given or []))
         if self._given is not None:
             self._put(self._given, self._look_at_params(self.params), None)
             h.put()
+
+    masters = property(lambda self: _aliases(self._masters))
+    exp_avgs = property(lambda self: _aliases(self._exp_avgs))
+    exp_avg_sqs = property(lambda self: _aliases(self._exp_avg_sqs))
+
+    def _check_counter(self):
+        _check("step", 0, self.step_count, None, self._handle.device, [torch.int64])
+        if self.step_count.numel() != 1:
+            raise ValueError("step must have one element")
+        self._counter = self.step_count
 
     def _put(self, grads, params_look, grads_look):
         h, c = self._handle, self._handle.columns
@@ -321,7 +333,7 @@ class AdamW:
         for i, (g, p) in enumerate(zip(grads, self.params)):
             if anew:
                 _check("params", i, p, None, h.device, _TYPES)
-                _check("exp_avgs", i, self.exp_avgs[i], p, h.device, [torch.float32])
+                _check("exp_avgs", i, self._exp_avgs[i], p, h.device, [torch.float32])
             if g is not None:
                 _check("grads", i, g, p, h.device, _TYPES)
         c["param"], c["param_type"] = params_look[0], _types(self.params)
@@ -370,6 +382,8 @@ class AdamW:
             how.max_norm = math.inf if self.max_norm is None else self.max_norm
             how.norm_given, how.skip_nonfinite = norm is not None, bool(self.skip_nonfinite)
             self._set_to = set_to
+        if self.step_count is not self._counter:
+            self._check_counter()
         h.ret(h.L.fs_adamw_step(h._h, ctypes.byref(how), self.step_count.data_ptr(), d.data_ptr() if asked else None))
         torch.autograd.graph.increment_version(self.params)       # autograd has to notice that they have changed
         return d
@@ -389,11 +403,11 @@ class AdamW:
     def load_state_dict(self, state):
         """Copies a state in; the parameters are the caller's to load."""
         new = [state["masters"], state["exp_avgs"], state["exp_avg_sqs"]]
-        for name, mine, theirs in zip(("masters", "exp_avgs", "exp_avg_sqs"), (self.masters, self.exp_avgs, self.exp_avg_sqs), new):
+        for name, mine, theirs in zip(("masters", "exp_avgs", "exp_avg_sqs"), (self._masters, self._exp_avgs, self._exp_avg_sqs), new):
             if len(theirs) != len(mine) or any((a is None) != (b is None) or (a is not None and a.shape != b.shape) for a, b in zip(mine, theirs)):
                 raise ValueError(f"{name} do not fit")
         with torch.no_grad():
-            for mine, theirs in zip((self.masters, self.exp_avgs, self.exp_avg_sqs), new):
+            for mine, theirs in zip((self._masters, self._exp_avgs, self._exp_avg_sqs), new):
                 for a, b in zip(mine, theirs):
                     if a is not None:
                         a.copy_(b)

@@ -143,3 +143,41 @@ def test_parameters_in_another_order_at_the_same_place_are_refused(gpu):
     p.grad = fake_lists.on_gpu(torch.ones(6, 4)).t()
     with pytest.raises(ValueError, match=r"exp_avgs\[0\]"):
         opt.step()
+
+
+def test_state_is_not_exchanged_behind_the_list(gpu):
+    """The list has the addresses of the state: what is put in its place later would be ignored, and its memory written to after it was freed."""
+    params = gpu.params(10, 20, dtype=torch.bfloat16)
+    opt = gpu.adamw(params, grads=gpu.grads(params), masters=[fake_lists.on_gpu(torch.ones(n)) for n in (10, 20)])
+    opt.step()
+    for name in ("masters", "exp_avgs", "exp_avg_sqs"):
+        before = getattr(opt, name)
+        at = [t.data_ptr() for t in before]
+        assert gpu.ran[-1]["list"][name[:-1]].tolist() == at
+        with pytest.raises(AttributeError):
+            setattr(opt, name, [torch.zeros_like(t) for t in before])
+        changed = getattr(opt, name)
+        changed[0] = torch.zeros_like(before[0])
+        assert [t.data_ptr() for t in getattr(opt, name)] == at == [t.data_ptr() for t in opt.state_dict()[name]]
+        # other memory for the same tensor object: the list goes on with what it has, which is kept
+        before[1].data = torch.zeros(20)
+    old = [gpu.ran[-1]["list"][name].tolist() for name in ("master", "exp_avg", "exp_avg_sq")]
+    new = [fake_lists.on_gpu(torch.ones(20)) for _ in range(16)]
+    opt.step()
+    assert [gpu.ran[-1]["list"][name].tolist() for name in ("master", "exp_avg", "exp_avg_sq")] == old
+    assert not {t.data_ptr() for t in new} & {a for at in old for a in at}
+
+
+def test_the_step_counter_is_checked_when_it_is_exchanged(gpu):
+    params = gpu.params(10)
+    opt = gpu.adamw(params, grads=gpu.grads(params))
+    opt.step()
+    for bad, error in ((fake_lists.on_gpu(torch.zeros(1, dtype=torch.int32)), TypeError), (fake_lists.on_gpu(torch.zeros(2, dtype=torch.int64)), ValueError),
+                       (torch.zeros(1, dtype=torch.int64), ValueError), (3, TypeError)):
+        opt.step_count = bad
+        with pytest.raises(error, match="step"):
+            opt.step()
+    assert len(gpu.ran) == 1
+    opt.step_count = fake_lists.on_gpu(torch.full((1,), 7, dtype=torch.int64))
+    opt.step()
+    assert gpu.ran[-1]["args"][1] == opt.step_count.data_ptr()
