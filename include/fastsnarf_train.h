@@ -11,9 +11,9 @@
  *             m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2
  *             p = p (1 - l weight_decay decay_scale_i) - l / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps)
  *
- * Magnitudes are squared and added in 64 bits, so the norm of any finite fp32 gradients is finite before it is rounded to
- * fp32; the coefficient and the bias corrections are computed in 64 bits, the update in fp32.  16-bit results are rounded
- * once, to nearest even.  Sums run in an order that depends on the list (with its addresses) and on the device only: results are the
+ * Magnitudes are squared and added in 64 bits, and the norm stays in 64 bits until it is written: for the coefficient, and for whether it is
+ * finite.  The norm of any finite fp32 gradients is, also where the fp32 that is written is infinity.  A norm that is given has 32 bits.  The
+ * coefficient and the bias corrections are computed in 64 bits, the update in fp32.  16-bit results are rounded once, to nearest even.  Sums run in an order that depends on the list (with its addresses) and on the device only: results are the
  * same from call to call.  NaN and infinities go through as the formulas say.
  *
  * Conventions of fastsnarf.h hold (device pointers, nothing synchronises, status codes, no exceptions or aborts), with one
@@ -58,7 +58,7 @@ typedef struct {
     double max_norm;      /* >= 0, INFINITY: no clipping                                                         */
     double grad_scale;    /* > 0, finite                                                                         */
     int32_t norm_given;   /* 0: d_norm is computed (2-norm) and written.  1: it is read (a norm over several GPUs, say)  */
-    int32_t skip_nonfinite; /* 1: where the norm is NaN or infinite nothing is written but the norm: no update, no step */
+    int32_t skip_nonfinite; /* 1: where the norm is NaN or infinite (in 64 bits) nothing is written but the norm: no update, no step */
     const float *d_lr;    /* a word on the device that is read in place of lr (a schedule under graph capture), or NULL */
 } fs_adamw;
 

@@ -355,13 +355,14 @@ struct NormD {
     float *norm;
 };
 
-__device__ __forceinline__ float norm_value(const NormD &N)
+// In 64 bits for what is made of it; only what is written out is rounded.
+__device__ __forceinline__ double norm_value(const NormD &N)
 {
-    if (N.parts == 0) return N.norm ? *N.norm : 0.0f;
+    if (N.parts == 0) return N.norm ? (double)*N.norm : 0.0;
     const double v = N.kind == KIND_TWO ? Sum<KIND_TWO>::value(join_parts(N.partial, N.parts))
                                         : Sum<KIND_MAX>::value(join_parts(reinterpret_cast<const unsigned *>(N.partial), N.parts));
-    const float n = (float)(v * N.scale);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *N.norm = n;
+    const double n = v * N.scale;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *N.norm = (float)n;
     return n;
 }
 
@@ -370,27 +371,28 @@ __device__ __forceinline__ float norm_value(const NormD &N)
 // place of two, and no counters: bound by the launch and the chain of loads (place, tensor, elements).  8 k elements: norm 3.0 us, clipping 4.4, AdamW 5.8.
 constexpr int SHORT_THREADS = 1024, SHORT_WAVES = SHORT_THREADS / 64;
 template <int KIND>
-__device__ __forceinline__ float short_norm(const ListD &L, double scale)
+__device__ __forceinline__ double short_norm(const ListD &L, double scale)
 {
     typename Sum<KIND>::type s = 0;
     walk_short<UNIT>(L, threadIdx.x >> 6, SHORT_WAVES, [&](const TensorD &t, const Piece &p) { s = sum_types<KIND, false, 64, 8>(t, p, s); });
-    return (float)(Sum<KIND>::value(block_join<SHORT_WAVES>(s)) * scale);
+    return Sum<KIND>::value(block_join<SHORT_WAVES>(s)) * scale;
 }
 
 template <int KIND>
 __global__ __launch_bounds__(SHORT_THREADS) void k_norm_short(ListD L, double scale, float *__restrict__ norm)
 {
-    const float n = short_norm<KIND>(L, scale);
-    if (threadIdx.x == 0) *norm = n;
+    const double n = short_norm<KIND>(L, scale);
+    if (threadIdx.x == 0) *norm = (float)n;
 }
 
 // ---- clipping ----
 
-// s min(1, max_norm / (norm + 1e-6)), NaN for a norm that is NaN
-__device__ __forceinline__ float clip_coef(float norm, double max_norm, double scale)
+// s min(1, max_norm / (norm + 1e-6)), NaN for a norm that is NaN; rounded once.  (From a norm of 32 bits its largest error would be 2.6 times that, and gradients
+// whose norm 32 bits cannot hold would become zeros.)
+__device__ __forceinline__ float clip_coef(double norm, double max_norm, double scale)
 {
     if (max_norm == __builtin_inf()) return (float)scale;
-    const double q = max_norm / ((double)norm + 1e-6);
+    const double q = max_norm / (norm + 1e-6);
     return (float)((q >= 1.0 ? 1.0 : q) * scale);
 }
 
@@ -451,8 +453,9 @@ __global__ __launch_bounds__(256) void k_clip(ListD L, NormD N, int all_in_place
 template <int KIND>
 __global__ __launch_bounds__(SHORT_THREADS) void k_clip_short(ListD L, double max_norm, double scale, float *__restrict__ norm)
 {
-    const float n = short_norm<KIND>(L, scale), coef = clip_coef(n, max_norm, scale);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *norm = n;
+    const double n = short_norm<KIND>(L, scale);
+    const float coef = clip_coef(n, max_norm, scale);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
     walk_short<SHORT_PART>(L, blockIdx.x * SHORT_WAVES + (threadIdx.x >> 6), gridDim.x * SHORT_WAVES, [&](const TensorD &t, const Piece &p) { scale_types<false, 64, 1>(t, p, coef); });
 }
 
@@ -613,7 +616,7 @@ __device__ __forceinline__ void adam_types(const TensorD &t, const Piece &p, con
     }
 }
 
-__device__ __forceinline__ bool is_finite(float x) { return __builtin_fabsf(x) < __builtin_inff(); }
+__device__ __forceinline__ bool is_finite(double x) { return __builtin_fabs(x) < __builtin_inf(); }
 
 // Reads four arrays and writes three (of 16-bit parameters with masters, four and four), 28 bytes an element, once each; the counters say that no more is moved.
 // 250 M elements in 1251 us (7.0 GB, 5.6 TB/s), 12.6 M fp32 in 57 (6.2).  Its 44 vector instructions an element take a quarter of that.  Four elements a thread, so
@@ -626,7 +629,7 @@ __global__ __launch_bounds__(256) void k_adamw(ListD L, AdamD A, NormD N, const 
     StepD step;
     const bool first = threadIdx.x < 64;
     if (first) step = adam_begin(A, lr_word, steps, tickets, &shared);
-    const float n = norm_value(N);
+    const double n = norm_value(N);
     __syncthreads();
     const bool skip = A.skip_nonfinite && !is_finite(n);   // every block sees the same norm
     if (!skip) {
@@ -646,8 +649,8 @@ __global__ __launch_bounds__(SHORT_THREADS) void k_adamw_short(ListD L, AdamD A,
     const int wave = threadIdx.x >> 6;
     const bool last_wave = wave == SHORT_WAVES - 1;        // the one with the least to add up
     if (last_wave) step = adam_begin(A, lr_word, steps, tickets, &shared);
-    const float n = short_norm<KIND_TWO>(L, A.scale);      // waits for all of the block
-    if (blockIdx.x == 0 && threadIdx.x == 0) *norm = n;
+    const double n = short_norm<KIND_TWO>(L, A.scale);     // waits for all of the block
+    if (blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
     const bool skip = A.skip_nonfinite && !is_finite(n);
     if (!skip) {
         AdamC C = shared;
