@@ -208,6 +208,15 @@ def _aliases(tensors):
     return [None if t is None else t.detach() for t in tensors]
 
 
+_PLACE, _SIZE, _TYPE = torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.dtype.__get__
+
+
+def _look_at_params(params):
+    """What parameters could have other than those before them: the place; and at the same place (memory that was freed and taken again, another view
+    of it) the size and the type."""
+    return [*map(_PLACE, params), *map(_SIZE, params), *map(_TYPE, params)]
+
+
 def _sizes(tensors):
     return [0 if t is None else t.numel() for t in tensors]
 
@@ -313,7 +322,7 @@ class AdamW:
         c["lr_scale"], c["decay_scale"] = lr_scales, decay_scales
         _check_apart(self.params + self._masters + self._exp_avgs + self._exp_avg_sqs + (self._given or []))
         if self._given is not None:
-            self._put(self._given, self._look_at_params(self.params), None)
+            self._put(self._given, _look_at_params(self.params), None)
             h.put()
 
     masters = property(lambda self: _aliases(self._masters))
@@ -328,39 +337,30 @@ class AdamW:
 
     def _put(self, grads, params_look, grads_look):
         h, c = self._handle, self._handle.columns
+        _lists(h.count, params=self.params)
         # parameters may have another type or size now; or another order, and then their gradients have, too
-        anew = params_look != self._params_look or grads_look and grads_look[2] != self._grads_look[2]
+        order = lambda look: look and [x and x[2] for x in look]
+        anew = params_look != self._params_look or order(grads_look) != order(self._grads_look)
         for i, (g, p) in enumerate(zip(grads, self.params)):
             if anew:
                 _check("params", i, p, None, h.device, _TYPES)
                 _check("exp_avgs", i, self._exp_avgs[i], p, h.device, [torch.float32])
             if g is not None:
                 _check("grads", i, g, p, h.device, _TYPES)
-        c["param"], c["param_type"] = params_look[0], _types(self.params)
+        c["param"], c["param_type"] = params_look[:h.count], _types(self.params)
         c["grad"], c["n"], c["grad_type"] = _places(grads), _sizes(grads), _types(grads)
         h.version += 1
         self._params_look, self._grads_look = params_look, grads_look
-
-    @staticmethod
-    def _look_at_params(params):
-        """What parameters could have other than those before them: the place, and at the same place (memory that was freed and taken again, another
-        view of it) the type and the size."""
-        return list(map(torch.Tensor.data_ptr, params)), [p.dtype for p in params], list(map(torch.Tensor.numel, params))
-
-    @staticmethod
-    def _look_at_grads(grads):
-        """The same of gradients that are not held here; their shape is prescribed by the parameters."""
-        look = [(0, None, None) if g is None else (g.data_ptr(), g.dtype, g.is_contiguous() or g.stride()) for g in grads]
-        return list(zip(*look)) or [(), (), ()]
 
     def step(self, norm: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
         """One step.  Returns the gradients' global norm, float32 [1] (None where neither max_norm nor skip_nonfinite asks for it); a
         `norm` that is given is taken as it is (one over several GPUs, say)."""
         h, how = self._handle, self._how
-        params_look, grads, grads_look = self._look_at_params(self.params), self._given, None
+        params_look, grads, grads_look = _look_at_params(self.params), self._given, None
         if grads is None:
+            # the same of gradients that are not held here; their shape is prescribed by the parameters
             grads = [p.grad for p in self.params]
-            grads_look = self._look_at_grads(grads)
+            grads_look = [None if g is None else (g.data_ptr(), g.dtype, g.is_contiguous() or g.stride()) for g in grads]
         if params_look != self._params_look or grads_look != self._grads_look:
             self._put(grads, params_look, grads_look)
         h.ready()
@@ -385,7 +385,7 @@ class AdamW:
         if self.step_count is not self._counter:
             self._check_counter()
         h.ret(h.L.fs_adamw_step(h._h, ctypes.byref(how), self.step_count.data_ptr(), d.data_ptr() if asked else None))
-        torch.autograd.graph.increment_version(self.params)       # autograd has to notice that they have changed
+        torch._C._increment_version(self.params)                  # autograd has to notice that they have changed
         return d
 
     def zero_grad(self, set_to_none: bool = False):

@@ -181,3 +181,17 @@ def test_the_step_counter_is_checked_when_it_is_exchanged(gpu):
     opt.step_count = fake_lists.on_gpu(torch.full((1,), 7, dtype=torch.int64))
     opt.step()
     assert gpu.ran[-1]["args"][1] == opt.step_count.data_ptr()
+
+
+@pytest.mark.parametrize("given", [False, True])
+def test_a_number_of_parameters_that_changes_is_refused(gpu, given):
+    params = gpu.params(10, 20)
+    opt = gpu.adamw(params, grads=gpu.grads(params) if given else None)
+    opt.step()
+    for change in (lambda: opt.params.pop(), lambda: opt.params.extend(2 * gpu.params(20))):
+        change()
+        with pytest.raises(ValueError, match="params: . entries, expected 2"):
+            opt.step()
+    opt.params[:] = params
+    opt.step()
+    assert len(gpu.ran) == 2 and gpu.ran[0]["list"].tolist() == gpu.ran[1]["list"].tolist()
