@@ -25,6 +25,7 @@ from . import binding
 _COLUMNS = np.dtype([(n, np.uint64) for n in ("grad", "out", "param", "master", "exp_avg", "exp_avg_sq")] +
                     [("n", np.int64), ("grad_type", np.int32), ("param_type", np.int32), ("lr_scale", np.float32), ("decay_scale", np.float32)])
 _TYPES = {torch.float32: binding.FS_FLOAT_FULL, torch.bfloat16: binding.FS_FLOAT_BRAIN, torch.float16: binding.FS_FLOAT_HALF}
+_BYTES = np.array([4, 2, 2], dtype=np.uint64)          # of an element, by type
 _KINDS = {"l2": binding.FS_NORM_TWO, "max": binding.FS_NORM_MAX}
 
 
@@ -58,14 +59,35 @@ def _check(what: str, i: int, t: torch.Tensor, like: Optional[torch.Tensor], dev
         raise ValueError(f"{what}[{i}]: shape {tuple(t.shape)} and strides {t.stride()}, expected {tuple(like.shape)} and {like.stride()}")
 
 
+def _overlap():
+    raise ValueError("tensors of the list overlap in memory")
+
+
+def _apart(begin, size):
+    """No two of these arrays may share memory: calls write them, block by block in no order.  Returns where they lie, for _untouched()."""
+    begin, size = begin[size > 0], size[size > 0]
+    order = begin.argsort()
+    begin = begin[order]
+    end = begin + size[order]
+    if (begin[1:] < end[:-1]).any():
+        _overlap()
+    # with an array of nothing at either end, so that every place has one before it (the one before the first is the last)
+    return np.concatenate([_ENDS[:1], begin, _ENDS[1:]]), np.concatenate([_ENDS[:1], end, _ENDS[:1]])
+
+
+_ENDS = np.array([0, 2 ** 64 - 1], dtype=np.uint64)
+
+
+def _untouched(begin, size, written):
+    """None of these arrays, which may share memory with one another, may share any with the written ones."""
+    last = written[0].searchsorted(begin + size) - 1             # the last one that begins before this one's end
+    if (written[1][last] > begin).any():
+        _overlap()
+
+
 def _check_apart(arrays):
-    """No two of the arrays may share memory: calls write some of them, block by block in no order."""
-    arrays = [t for t in arrays if t is not None and t.numel()]
-    begin = np.array([t.data_ptr() for t in arrays], dtype=np.uint64)
-    end = begin + np.array([t.nbytes for t in arrays], dtype=np.uint64)
-    order = np.argsort(begin)
-    if (begin[order][1:] < end[order][:-1]).any():
-        raise ValueError("tensors of the list overlap in memory")
+    arrays = [t for t in arrays if t is not None]
+    _apart(np.array(_places(arrays), dtype=np.uint64), np.array([t.nbytes for t in arrays], dtype=np.uint64))
 
 
 class _OnDevice:
@@ -347,8 +369,17 @@ class AdamW:
                 _check("exp_avgs", i, self._exp_avgs[i], p, h.device, [torch.float32])
             if g is not None:
                 _check("grads", i, g, p, h.device, _TYPES)
-        c["param"], c["param_type"] = params_look[:h.count], _types(self.params)
-        c["grad"], c["n"], c["grad_type"] = _places(grads), _sizes(grads), _types(grads)
+        place, n, kind = np.array(_places(grads), dtype=np.uint64), np.array(_sizes(grads), dtype=np.uint64), np.array(_types(grads), dtype=np.int32)
+        kinds = np.array(_types(self.params), dtype=np.int32) if anew else c["param_type"]
+        if anew:
+            written = (np.array(params_look[:h.count], dtype=np.uint64), n * _BYTES[kinds]), *((c[name], n * (c[name] > 0) * _BYTES[0]) for name in ("master", "exp_avg", "exp_avg_sq"))
+            written = _apart(*(np.concatenate(x) for x in zip(*written)))
+        else:
+            written = self._written
+        _untouched(place, n * _BYTES[kind], written)
+        self._written = written
+        c["param"], c["param_type"] = params_look[:h.count], kinds
+        c["grad"], c["n"], c["grad_type"] = place, n, kind
         h.version += 1
         updated = [i for i, g in enumerate(grads) if g is not None]
         self._updated = None if len(updated) == h.count else updated

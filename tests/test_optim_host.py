@@ -213,3 +213,34 @@ def test_parameters_that_are_not_updated_stay_valid_for_autograd(gpu, given):
         params[1].grad = fake_lists.on_gpu(params[1].grad)
         opt.step()
         assert params[1]._version == before[1] + 1
+
+
+def test_memory_that_comes_to_overlap_is_refused(gpu):
+    """Parameters and gradients may move between steps; what a step writes must not be what it reads or writes elsewhere."""
+    params = gpu.params(10, 20)
+    opt = gpu.adamw(params)
+    gpu.grads(params)
+    opt.step()
+    good = [p.grad for p in params]
+    state = opt.exp_avgs[1]
+    for p, bad in ((0, params[1].data[3:13]), (0, opt.exp_avg_sqs[0]), (1, state), (1, params[1].data)):
+        params[p].grad = bad.as_subclass(torch.Tensor).as_subclass(fake_lists.OnGpu)
+        assert params[p].grad.data_ptr() == bad.data_ptr()
+        for _ in range(2):
+            with pytest.raises(ValueError, match="overlap"):
+                opt.step()
+        params[p].grad = good[p]
+    opt.step()
+    # tied by their memory
+    before = params[0].data
+    params[0].data = params[1].data[5:15]
+    with pytest.raises(ValueError, match="overlap"):
+        opt.step()
+    params[0].grad = None                                   # not updated: nothing is written twice
+    opt.step()
+    params[0].data, params[0].grad = before, good[0]
+    # gradients are read only, and may share memory
+    whole = fake_lists.on_gpu(torch.ones(20))
+    params[0].grad, params[1].grad = whole[:10], whole
+    opt.step()
+    assert all(r["fits"] for r in gpu.ran) and len(gpu.ran) == 4
