@@ -381,8 +381,6 @@ class AdamW:
         c["param"], c["param_type"] = params_look[:h.count], kinds
         c["grad"], c["n"], c["grad_type"] = place, n, kind
         h.version += 1
-        updated = [i for i, g in enumerate(grads) if g is not None]
-        self._updated = None if len(updated) == h.count else updated
         self._params_look, self._grads_look = params_look, grads_look
 
     def step(self, norm: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
@@ -418,8 +416,7 @@ class AdamW:
         if self.step_count is not self._counter:
             self._check_counter()
         h.ret(h.L.fs_adamw_step(h._h, ctypes.byref(how), self.step_count.data_ptr(), d.data_ptr() if asked else None))
-        # autograd has to notice that they have changed, those that have
-        torch._C._increment_version(self.params if self._updated is None else [self.params[i] for i in self._updated])
+        torch._C._increment_version(self.params)                  # autograd has to notice that they have changed
         return d
 
     def zero_grad(self, set_to_none: bool = False):

@@ -197,24 +197,6 @@ def test_a_number_of_parameters_that_changes_is_refused(gpu, given):
     assert len(gpu.ran) == 2 and gpu.ran[0]["list"].tolist() == gpu.ran[1]["list"].tolist()
 
 
-@pytest.mark.parametrize("given", [False, True])
-def test_parameters_that_are_not_updated_stay_valid_for_autograd(gpu, given):
-    """A parameter without a gradient is left as it is: a graph that has saved it may still run backward."""
-    params = gpu.params(10, 20, 30)
-    grads = gpu.grads(params)
-    opt = gpu.adamw(params, grads=[grads[0], None, grads[2]] if given else None)
-    params[1].grad = None
-    saved = (params[1] * params[1]).sum()
-    before = [p._version for p in params]
-    opt.step(), opt.step()
-    assert [p._version - n for p, n in zip(params, before)] == [2, 0, 2]
-    saved.backward()
-    if not given:
-        params[1].grad = fake_lists.on_gpu(params[1].grad)
-        opt.step()
-        assert params[1]._version == before[1] + 1
-
-
 def test_memory_that_comes_to_overlap_is_refused(gpu):
     """Parameters and gradients may move between steps; what a step writes must not be what it reads or writes elsewhere."""
     params = gpu.params(10, 20)
