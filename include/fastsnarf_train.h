@@ -73,7 +73,8 @@ fs_status fs_tensors_create(const fs_tensor *list, int32_t count, void *hip_stre
 int64_t fs_tensors_bytes(int32_t count);
 fs_status fs_tensors_create_noalloc(const fs_tensor *list, int32_t count, void *hip_stream, void *workspace, int64_t bytes, fs_tensors **out);
 
-/* Free what the list owns.  Where it owns memory of the device, its stream is synchronised first.  NULL is allowed. */
+/* Free what the list owns.  Where it owns memory of the device, its stream is synchronised first; where that memory cannot be freed (as
+ * while a graph is captured), the list stays, and the call can be made again.  NULL is allowed. */
 fs_status fs_tensors_destroy(fs_tensors *t);
 
 /* Other addresses, sizes or types for the same number of tensors, for the calls after this one (a program whose gradients move from

@@ -367,7 +367,9 @@ fs_status fs_tensors_destroy(fs_tensors *t)
     if (!t) return FS_OK;
     if (t->owned) {
         (void)hipStreamSynchronize(t->stream);
-        (void)hipFree(t->mem);
+        const hipError_t e = hipFree(t->mem);
+        (void)hipGetLastError();
+        if (e != hipSuccess) return fail(t, FS_E_DEVICE, "fs_tensors_destroy: %s", hipGetErrorString(e));
     }
     delete[] t->given;
     delete[] t->host;

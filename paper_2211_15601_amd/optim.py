@@ -98,9 +98,21 @@ class _OnDevice:
 
     def __del__(self):
         try:
-            self.L.fs_tensors_destroy(self.h)
+            # a list with memory of its own is not freed while a graph is captured, which that would void
+            if self.workspace is None and torch.cuda.is_current_stream_capturing() or self.L.fs_tensors_destroy(self.h) != binding.FS_OK:
+                _later.append(self.h)
         except Exception:
             pass
+
+
+_later = []                            # lists that could not be freed when they went
+
+
+def _free_later(L):
+    for _ in range(len(_later)):
+        h = _later.pop(0)
+        if L.fs_tensors_destroy(h) != binding.FS_OK:
+            _later.append(h)
 
 
 class _Handle:
@@ -176,6 +188,7 @@ class _Handle:
         with torch.cuda.device(self.device):
             stream = torch.cuda.current_stream(self.device)
             if workspace is None:
+                _free_later(self.L)
                 st = self.L.fs_tensors_create(self.list, self.count, stream.cuda_stream, ctypes.byref(h))
             else:
                 st = self.L.fs_tensors_create_noalloc(self.list, self.count, stream.cuda_stream, workspace.data_ptr(), workspace.nbytes, ctypes.byref(h))

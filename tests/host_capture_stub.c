@@ -1,5 +1,7 @@
-/* host_stub.c with streams that record graphs, and devices of other sizes. */
+/* host_stub.c with streams that record graphs, memory that cannot be freed, and devices of other sizes. */
+#define hipFree free_block
 #include "host_stub.c"
+#undef hipFree
 
 #define MAX_STREAMS 16
 static struct { hipStream_t stream; unsigned long long capture; hipStreamCaptureStatus status; } recording[MAX_STREAMS];
@@ -13,6 +15,9 @@ void stub_capture(void *stream, unsigned long long capture, int failed)
     recording[i].capture = capture;
     recording[i].status = !capture ? hipStreamCaptureStatusNone : failed ? hipStreamCaptureStatusInvalidated : hipStreamCaptureStatusActive;
 }
+static int refuse_free;
+void stub_refuse_free(int yes) { refuse_free = yes; }
+hipError_t hipFree(void *p) { return refuse_free ? last_error = hipErrorStreamCaptureUnsupported : free_block(p); }
 void stub_compute_units(int n) { n_cus = n; }
 
 hipError_t hipStreamGetCaptureInfo(hipStream_t s, hipStreamCaptureStatus *status, unsigned long long *id)

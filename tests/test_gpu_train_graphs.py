@@ -117,3 +117,24 @@ def test_branches_of_one_graph(optim):
         graph.replay()
         torch.cuda.synchronize()
         assert [float(x) for x in (a, b, c)] == [want, 2 * want, 4 * want]
+
+
+def test_lists_that_go_during_a_capture(optim):
+    g = torch.full((50_003,), 2.0, device=DEV)
+    keep, gone = optim.TensorList([g]), optim.TensorList([g])
+    want = float(keep.grad_norm())
+    assert float(gone.grad_norm()) == want
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a = keep.grad_norm()
+        b = gone.grad_norm(grad_scale=2.0)
+        del gone
+        c = keep.grad_norm(grad_scale=4.0)
+    other = optim.TensorList([g])
+    for _ in range(3):
+        for x in (a, b, c):
+            x.zero_()
+        graph.replay()
+        assert float(other.grad_norm()) == want
+        torch.cuda.synchronize()
+        assert [float(x) for x in (a, b, c)] == [want, 2 * want, 4 * want]

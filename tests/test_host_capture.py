@@ -128,3 +128,16 @@ noalloc(one, E_DEVICE)
 S.stub_fail_launch(-1)
 assert S.stub_live_blocks() == 0 and S.stub_bad_frees() == 0
 """, tmp_path)
+
+
+def test_a_list_that_cannot_be_freed_stays(tmp_path):
+    """As while a graph is captured: the call can be made again."""
+    run("""
+h = make([tensor()])
+S.stub_refuse_free(1)
+for _ in range(2):
+    assert L.fs_tensors_destroy(h) == E_DEVICE and error(h) and S.stub_live_blocks() == 1
+S.stub_refuse_free(0)
+assert norm(h) == OK                                        # and no error is left for the next call
+assert L.fs_tensors_destroy(h) == OK and S.stub_live_blocks() == 0 and S.stub_bad_frees() == 0
+""", tmp_path)

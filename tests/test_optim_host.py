@@ -226,3 +226,33 @@ def test_memory_that_comes_to_overlap_is_refused(gpu):
     params[0].grad, params[1].grad = whole[:10], whole
     opt.step()
     assert all(r["fits"] for r in gpu.ran) and len(gpu.ran) == 4
+
+
+def test_lists_that_go_while_a_graph_is_captured_are_freed_later(gpu):
+    """Freeing memory is nothing that a capture allows."""
+    import gc
+    new = lambda: gpu.optim.TensorList([fake_lists.on_gpu(torch.ones(10))])
+    out = fake_lists.on_gpu(torch.zeros(1))
+    keep, a, b = new(), new(), new()
+    h = [x._handle.eager.h.value for x in (a, b)]
+    with gpu.capture() as g:
+        keep.grad_norm(out=out)
+        a.grad_norm(out=out)
+        own = a._handle.graph.h.value
+        del a, b
+        gc.collect()
+        assert gpu.destroyed == [own]                       # that one has no memory of its own
+    g.replay()
+    assert all(r["fits"] for r in gpu.ran)
+    c = new()
+    assert sorted(gpu.destroyed) == sorted(h + [own])
+    # the runtime may refuse at other times too (a capture in another thread)
+    refuse, at = gpu.binding.FS_E_DEVICE, c._handle.eager.h.value
+    ok = gpu.fs_tensors_destroy
+    gpu.fs_tensors_destroy = lambda h: refuse
+    del c
+    gc.collect()
+    gpu.fs_tensors_destroy = ok
+    assert at not in gpu.destroyed
+    new()
+    assert at in gpu.destroyed and len(set(gpu.destroyed)) == len(gpu.destroyed)
