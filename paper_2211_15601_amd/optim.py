@@ -23,7 +23,7 @@ from . import binding
 
 # an fs_tensor, for whole columns of a list at once
 _COLUMNS = np.dtype([(n, np.uint64) for n in ("grad", "out", "param", "master", "exp_avg", "exp_avg_sq")] +
-                    [("n", np.int64), ("grad_type", np.int32), ("param_type", np.int32), ("lr_scale", np.float32), ("decay_scale", np.float32)])
+                    [("n", np.uint64), ("grad_type", np.int32), ("param_type", np.int32), ("lr_scale", np.float32), ("decay_scale", np.float32)])
 _TYPES = {torch.float32: binding.FS_FLOAT_FULL, torch.bfloat16: binding.FS_FLOAT_BRAIN, torch.float16: binding.FS_FLOAT_HALF}
 _BYTES = np.array([4, 2, 2], dtype=np.uint64)          # of an element, by type
 _KINDS = {"l2": binding.FS_NORM_TWO, "max": binding.FS_NORM_MAX}
@@ -350,7 +350,7 @@ class AdamW:
                 if g is not None:
                     _check("grads", i, g, p, h.device, _TYPES)
             self._given = _aliases(given)
-        self._params_look = self._grads_look = None
+        self._params_look = self._grads_look = self._orders = None
         self._how, self._set_to = binding.AdamW(), None
         c = h.columns
         c["master"], c["exp_avg"], c["exp_avg_sq"] = _places(self._masters), _places(self._exp_avgs), _places(self._exp_avg_sqs)
@@ -374,27 +374,24 @@ class AdamW:
         h, c = self._handle, self._handle.columns
         _lists(h.count, params=self.params)
         # parameters may have another type or size now; or another order, and then their gradients have, too
-        order = lambda look: look and [x and x[2] for x in look]
-        anew = params_look != self._params_look or order(grads_look) != order(self._grads_look)
+        orders = [x and x[2] for x in grads_look] if grads_look is not None else None
+        anew = params_look != self._params_look or orders != self._orders
+        self._params_look = None
         for i, (g, p) in enumerate(zip(grads, self.params)):
             if anew:
                 _check("params", i, p, None, h.device, _TYPES)
                 _check("exp_avgs", i, self._exp_avgs[i], p, h.device, [torch.float32])
             if g is not None:
                 _check("grads", i, g, p, h.device, _TYPES)
-        place, n, kind = np.array(_places(grads), dtype=np.uint64), np.array(_sizes(grads), dtype=np.uint64), np.array(_types(grads), dtype=np.int32)
-        kinds = np.array(_types(self.params), dtype=np.int32) if anew else c["param_type"]
+        c["grad"], c["n"], c["grad_type"] = _places(grads), _sizes(grads), _types(grads)
         if anew:
-            written = (np.array(params_look[:h.count], dtype=np.uint64), n * _BYTES[kinds]), *((c[name], n * (c[name] > 0) * _BYTES[0]) for name in ("master", "exp_avg", "exp_avg_sq"))
-            written = _apart(*(np.concatenate(x) for x in zip(*written)))
-        else:
-            written = self._written
-        _untouched(place, n * _BYTES[kind], written)
-        self._written = written
-        c["param"], c["param_type"] = params_look[:h.count], kinds
-        c["grad"], c["n"], c["grad_type"] = place, n, kind
+            c["param"], c["param_type"] = params_look[:h.count], _types(self.params)
+            n, kind = c["n"], c["param_type"]
+            written = [c["param"], *(c[name] for name in ("master", "exp_avg", "exp_avg_sq"))]
+            self._written = _apart(np.concatenate(written), np.concatenate([n * _BYTES[kind]] + [n * (at > 0) * _BYTES[0] for at in written[1:]]))
+        _untouched(c["grad"], c["n"] * _BYTES[c["grad_type"]], self._written)
         h.version += 1
-        self._params_look, self._grads_look = params_look, grads_look
+        self._params_look, self._grads_look, self._orders = params_look, grads_look, orders
 
     def step(self, norm: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
         """One step.  Returns the gradients' global norm, float32 [1] (None where neither max_norm nor skip_nonfinite asks for it); a
