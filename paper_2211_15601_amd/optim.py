@@ -126,18 +126,20 @@ class _Handle:
         if device.type != "cuda":
             raise ValueError(f"tensors must be on a GPU, got {device}")
         self.device = device if device.index is not None else torch.device("cuda", torch.cuda.current_device())
-        self.count = count
+        self.count, self.index = count, self.device.index
         self.list = (binding.Tensor * max(1, count))()
         self.columns = np.frombuffer(self.list, dtype=_COLUMNS)[:count]
         self.columns["lr_scale"] = self.columns["decay_scale"] = 1.0
         self.version = 0               # of the columns; who changes them counts it up
         self.eager = self.graph = None
-        self._h = None                 # of the call being made
 
-    def ready(self):
-        """Before a call: the list where the current stream's calls find it."""
+    def call(self, f, *args):
+        """A call on the list, on its device's current stream."""
+        if torch._C._cuda_getDevice() != self.index:
+            with torch.cuda.device(self.device):
+                return self.call(f, *args)
         # the current stream's number; asking for the stream itself makes an object, 2 us of the 7 that a call then takes the host
-        raw = torch._C._cuda_getCurrentRawStream(self.device.index)
+        raw = torch._C._cuda_getCurrentRawStream(self.index)
         if raw != 0 and torch.cuda.is_current_stream_capturing():              # the default stream is none that can be captured
             x = self.in_graph(raw)
         else:
@@ -146,7 +148,13 @@ class _Handle:
                 x = self.put()
             elif raw != x.raw:
                 self.to_stream(x)
-        self._h = x.h
+        st = f(x.h, *args)
+        if st != binding.FS_OK:
+            self.fail(x, st)
+
+    def first(self):
+        with torch.cuda.device(self.device):
+            self.put()
 
     def put(self):
         """Hands the list over for eager calls: the first time, or after it has changed."""
@@ -156,11 +164,9 @@ class _Handle:
                 raise RuntimeError("a list has to be made, or used once, before a graph is captured")
             x = self.eager = self.make()
         else:
-            if torch._C._cuda_getCurrentRawStream(self.device.index) != x.raw:
+            if torch._C._cuda_getCurrentRawStream(self.index) != x.raw:
                 self.to_stream(x)
-            self._h = x.h
-            self.ret(self.L.fs_tensors_update(x.h, self.list, self.count))
-            x.version = self.version
+            self.update(x)
         return x
 
     def in_graph(self, raw):
@@ -178,35 +184,36 @@ class _Handle:
         if before is not None:
             x.stream.wait_stream(before)       # another stream of the same graph
         if x.version != self.version:
-            self._h = x.h
-            self.ret(self.L.fs_tensors_update(x.h, self.list, self.count))
-            x.version = self.version
+            self.update(x)
         return x
+
+    def update(self, x):
+        st = self.L.fs_tensors_update(x.h, self.list, self.count)
+        if st != binding.FS_OK:
+            self.fail(x, st)
+        x.version = self.version
 
     def make(self, workspace=None):
         h = ctypes.c_void_p()
-        with torch.cuda.device(self.device):
-            stream = torch.cuda.current_stream(self.device)
-            if workspace is None:
-                _free_later(self.L)
-                st = self.L.fs_tensors_create(self.list, self.count, stream.cuda_stream, ctypes.byref(h))
-            else:
-                st = self.L.fs_tensors_create_noalloc(self.list, self.count, stream.cuda_stream, workspace.data_ptr(), workspace.nbytes, ctypes.byref(h))
+        stream = torch.cuda.current_stream(self.device)
+        if workspace is None:
+            _free_later(self.L)
+            st = self.L.fs_tensors_create(self.list, self.count, stream.cuda_stream, ctypes.byref(h))
+        else:
+            st = self.L.fs_tensors_create_noalloc(self.list, self.count, stream.cuda_stream, workspace.data_ptr(), workspace.nbytes, ctypes.byref(h))
         if st != binding.FS_OK:
             raise binding.FsError(st, "fs_tensors_create failed")
         return _OnDevice(self.L, h, self.version, stream, workspace)
 
-    def ret(self, st):
-        if st != binding.FS_OK:
-            raise binding.FsError(st, self.L.fs_tensors_error(self._h).decode())
+    def fail(self, x, st):
+        raise binding.FsError(st, self.L.fs_tensors_error(x.h).decode())
 
     def to_stream(self, x):
         now = torch.cuda.current_stream(self.device)
         if x is self.eager:
             now.wait_stream(x.stream)          # the scratch is one: this stream's calls come after those of the stream before
         x.stream, x.raw = now, now.cuda_stream
-        self._h = x.h
-        self.ret(self.L.fs_tensors_set_stream(x.h, x.raw))
+        self.L.fs_tensors_set_stream(x.h, x.raw)
 
     def norm(self, norm):
         """Where a call's norm goes or comes from."""
@@ -280,14 +287,13 @@ class TensorList:
         self._grads, self._written = grads, [o if o is not None else g for o, g in zip(outs, grads) if g is not None]
         c = h.columns
         c["grad"], c["out"], c["n"], c["grad_type"] = _places(grads), _places(outs), _sizes(grads), _types(grads)
-        h.put()
+        h.first()
 
     def grad_norm(self, kind: str = "l2", grad_scale: float = 1.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Global norm of the gradients times grad_scale, float32 [1]: "l2", or "max", the largest magnitude."""
         h = self._handle
         out = h.norm(out)
-        h.ready()
-        h.ret(h.L.fs_grad_norm(h._h, _kind(kind), grad_scale, out.data_ptr()))
+        h.call(h.L.fs_grad_norm, _kind(kind), grad_scale, out.data_ptr())
         return out
 
     def clip_grads(self, max_norm: float, kind: str = "l2", grad_scale: float = 1.0, norm: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -295,8 +301,7 @@ class TensorList:
         spread over several GPUs, say) is taken as it is."""
         h = self._handle
         d = h.norm(norm)
-        h.ready()
-        h.ret(h.L.fs_grad_clip(h._h, _kind(kind), max_norm, grad_scale, norm is not None, d.data_ptr()))
+        h.call(h.L.fs_grad_clip, _kind(kind), max_norm, grad_scale, norm is not None, d.data_ptr())
         torch.autograd.graph.increment_version(self._written)
         return d
 
@@ -352,13 +357,14 @@ class AdamW:
             self._given = _aliases(given)
         self._params_look = self._grads_look = self._orders = None
         self._how, self._set_to = binding.AdamW(), None
+        self._how_at = ctypes.byref(self._how)
         c = h.columns
         c["master"], c["exp_avg"], c["exp_avg_sq"] = _places(self._masters), _places(self._exp_avgs), _places(self._exp_avg_sqs)
         c["lr_scale"], c["decay_scale"] = lr_scales, decay_scales
         _check_apart(self.params + self._masters + self._exp_avgs + self._exp_avg_sqs + (self._given or []))
         if self._given is not None:
             self._put(self._given, _look_at_params(self.params), None)
-            h.put()
+            h.first()
 
     masters = property(lambda self: _aliases(self._masters))
     exp_avgs = property(lambda self: _aliases(self._exp_avgs))
@@ -404,7 +410,6 @@ class AdamW:
             grads_look = [None if g is None else (g.data_ptr(), g.dtype, g.is_contiguous() or g.stride()) for g in grads]
         if params_look != self._params_look or grads_look != self._grads_look:
             self._put(grads, params_look, grads_look)
-        h.ready()
         asked = norm is not None or self.max_norm is not None or self.skip_nonfinite
         d = h.norm(norm) if asked else None
         lr = self.lr
@@ -425,7 +430,7 @@ class AdamW:
             self._set_to = set_to
         if self.step_count is not self._counter:
             self._check_counter()
-        h.ret(h.L.fs_adamw_step(h._h, ctypes.byref(how), self.step_count.data_ptr(), d.data_ptr() if asked else None))
+        h.call(h.L.fs_adamw_step, self._how_at, self.step_count.data_ptr(), d.data_ptr() if asked else None)
         torch._C._increment_version(self.params)                  # autograd has to notice that they have changed
         return d
 

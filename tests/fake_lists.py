@@ -112,7 +112,7 @@ class Machine:
         return 100 + count
 
     def fs_tensors_update(self, h, array, count):
-        return self._put(h.value, array, count)
+        return self._put(h.value, array, count) if self.device == GPU.index else self.binding.FS_E_DEVICE
 
     def fs_tensors_set_stream(self, h, stream):
         self.lists[h.value]["stream"] = stream

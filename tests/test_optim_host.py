@@ -256,3 +256,20 @@ def test_lists_that_go_while_a_graph_is_captured_are_freed_later(gpu):
     assert at not in gpu.destroyed
     new()
     assert at in gpu.destroyed and len(set(gpu.destroyed)) == len(gpu.destroyed)
+
+
+def test_calls_on_a_list_of_another_gpu_than_the_current_one(gpu):
+    params = gpu.params(10, 20)
+    out = fake_lists.on_gpu(torch.zeros(1))
+    gpu.device = 1
+    lst = gpu.optim.TensorList([fake_lists.on_gpu(torch.ones(10))], device="cuda:0")
+    opt = gpu.adamw(params)
+    lst.grad_norm(out=out)
+    for _ in range(2):
+        gpu.grads(params)
+        opt.step()
+    with gpu.capture() as g:
+        lst.clip_grads(1.0, norm=out)
+        opt.step()
+    g.replay()
+    assert [r["call"] for r in gpu.ran] == ["norm", "adamw", "adamw", "clip", "adamw"] and all(r["fits"] for r in gpu.ran) and gpu.device == 1
