@@ -9,6 +9,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <limits>
 #include <new>
 
 using namespace fs;
@@ -457,7 +458,7 @@ fs_status fs_adamw_step(fs_tensors *t, const fs_adamw *how, int64_t *d_step, flo
     A.beta2 = (float)h.beta2;
     A.rest1 = (float)(1.0 - h.beta1);
     A.rest2 = (float)(1.0 - h.beta2);
-    A.eps = (float)h.eps;
+    A.eps = h.eps > 0.0 ? std::max((float)h.eps, std::numeric_limits<float>::denorm_min()) : 0.0f;      // 0 / (0 + eps) stays 0, not NaN
     A.decay = (float)h.weight_decay;
     A.skip_nonfinite = h.skip_nonfinite;
     long long *steps = reinterpret_cast<long long *>(d_step);
