@@ -141,3 +141,40 @@ S.stub_refuse_free(0)
 assert norm(h) == OK                                        # and no error is left for the next call
 assert L.fs_tensors_destroy(h) == OK and S.stub_live_blocks() == 0 and S.stub_bad_frees() == 0
 """, tmp_path)
+
+
+def test_blocks_never_outnumber_the_partial_sums(tmp_path):
+    """Whatever the device and the list: 2048 of them lie in front of the counters, and a block of the norm writes one."""
+    run("""
+sizes = (40 * 2048, 300 * 2048, 4100 * 2048, 20000 * 2048, 66000 * 2048, 1 << 40)
+most = 0
+for units in (1, 64, 256, 304, 512, 513, 1000, 4096):
+    S.stub_compute_units(units)
+    for n in sizes:
+        for gt in (0, 1):
+            h = make([tensor(n=n, gt=gt, out=None)])
+            S.stub_clear_launches()
+            assert norm(h) == OK and norm(h, 1) == OK and clip(h) == OK and adamw(h, how()) == OK
+            ls = launched()
+            assert [l[0].split("<")[0] for l in ls] == ["k_norm", "k_norm", "k_norm", "k_clip", "k_norm", "k_adamw"]
+            blocks = [l[1][0] for l in ls if l[0].startswith("k_norm")]
+            assert all(1 <= b <= 2048 for b in blocks) and all(l[2] == (256, 1, 1) for l in ls), (units, n, blocks)
+            most = max([most] + blocks)
+            L.fs_tensors_destroy(h)
+assert most == 2048                                         # the bound is reached
+""", tmp_path)
+
+
+def test_every_refusal_names_its_reason(tmp_path):
+    run("""
+h = make([tensor(), tensor(out=None)])
+for call, what in ((lambda: norm(h, 2), "kind"), (lambda: norm(h, scale=0.0), "grad_scale"), (lambda: norm(h, d=None), "d_norm"), (lambda: clip(h, kind=-1), "kind"),
+                   (lambda: clip(h, max_norm=-1.0), "max_norm"), (lambda: clip(h, scale=math.inf), "grad_scale"), (lambda: clip(h, given=2), "norm_given"),
+                   (lambda: clip(h, d=None), "d_norm"), (lambda: adamw(h, None), "how"), (lambda: adamw(h, how(lr=math.nan)), "lr"), (lambda: adamw(h, how(wd=math.inf)), "weight_decay"),
+                   (lambda: adamw(h, how(b1=1.0)), "betas"), (lambda: adamw(h, how(b2=math.nan)), "betas"), (lambda: adamw(h, how(eps=-1.0)), "eps"),
+                   (lambda: adamw(h, how(max_norm=-0.5)), "max_norm"), (lambda: adamw(h, how(scale=-1.0)), "grad_scale"), (lambda: adamw(h, how(given=5)), "norm_given"),
+                   (lambda: adamw(h, how(skip=2)), "skip_nonfinite"), (lambda: adamw(h, how(), d=None), "d_norm"), (lambda: adamw(h, how(), step=None), "d_step"),
+                   (lambda: adamw(h, how(d_lr=at(9) + 1)), "d_lr")):
+    S.stub_clear_launches()
+    assert call() == E_ARG and what in error(h) and names() == [], (what, error(h))
+""", tmp_path)
