@@ -13,8 +13,9 @@
  *
  * Magnitudes are squared and added in 64 bits, and the norm stays in 64 bits until it is written: for the coefficient, and for whether it is
  * finite.  The norm of any finite fp32 gradients is, also where the fp32 that is written is infinity.  A norm that is given has 32 bits.  The
- * coefficient and the bias corrections are computed in 64 bits, the update in fp32.  16-bit results are rounded once, to nearest even.  Sums run in an order that depends on the list (with its addresses) and on the device only: results are the
- * same from call to call.  NaN and infinities go through as the formulas say.
+ * coefficient and the bias corrections are computed in 64 bits, the update in fp32 (an eps that fp32 rounds to 0 is its smallest number).  16-bit
+ * results are rounded once, to nearest even.  Sums run in an order that depends on the list (with its addresses) and on the device only: results
+ * are the same from call to call.  NaN and infinities go through as the formulas say.
  *
  * Conventions of fastsnarf.h hold (device pointers, nothing synchronises, status codes, no exceptions or aborts), with one
  * difference: the pointers of a list are aligned to their own element type, no more, so tensors may be views into a packed buffer.

@@ -8,7 +8,8 @@ tensors, clipping, and the AdamW step.
 
 Tensors are float32, bfloat16 or float16 on one GPU, of any size and alignment, dense (any order of dimensions, without
 gaps); moments and masters are float32.  Results stay on the GPU and nothing waits for it.  Calls run on the stream that is current
-when they are made, and can be captured into a graph (after one call outside of it).  Argument marshalling only: the arithmetic runs in the HIP kernels.  There is no CPU fallback.
+when they are made, and can be captured into graphs of torch.cuda (after the list was made, or used once, outside of them), which may be replayed in any order,
+beside one another and beside eager calls.  Argument marshalling only: the arithmetic runs in the HIP kernels.  There is no CPU fallback.
 """
 from __future__ import annotations
 
@@ -315,7 +316,7 @@ class AdamW:
       lr           a number, or a float32 tensor of one element on the GPU that is read at every step (a schedule under graph capture)
       max_norm     limit of the gradients' global 2-norm; None: no clipping
       grad_scale   factor on all gradients before anything else (the inverse of a loss scale)
-      skip_nonfinite  a step whose norm is NaN or infinite changes nothing but the norm, and is not counted
+      skip_nonfinite  a step whose norm (in 64 bits, where it is computed here) is NaN or infinite changes nothing but the norm, and is not counted
       masters      True: 16-bit parameters get float32 masters, which are what is updated; or a list (None: no master)
       lr_scales, decay_scales   factors per parameter on lr and weight_decay
       exp_avgs, exp_avg_sqs, step   state to go on from: float32 tensors like the parameters, and an int64 tensor of one element
