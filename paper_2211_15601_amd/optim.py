@@ -184,6 +184,7 @@ class _Handle:
             return x
         if before is not None:
             x.stream.wait_stream(before)       # another stream of the same graph
+            x.workspace.record_stream(x.stream)
         if x.version != self.version:
             self.update(x)
         return x

@@ -15,6 +15,10 @@ GPU = torch.device("cuda", 0)
 class OnGpu(torch.Tensor):
     """A CPU tensor that is taken for one on the GPU."""
     device = property(lambda self: GPU)
+    used_on = []                                 # (address, stream), of all of them
+
+    def record_stream(self, stream):
+        OnGpu.used_on.append((self.data_ptr(), stream.cuda_stream))
 
 
 def on_gpu(t):

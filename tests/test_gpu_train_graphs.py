@@ -138,3 +138,25 @@ def test_lists_that_go_during_a_capture(optim):
         assert float(other.grad_norm()) == want
         torch.cuda.synchronize()
         assert [float(x) for x in (a, b, c)] == [want, 2 * want, 4 * want]
+
+
+def test_a_list_that_goes_during_a_capture_with_branches(optim):
+    g = torch.full((3_000_001,), 2.0, device=DEV)
+    lst = optim.TensorList([g])
+    want = float(lst.grad_norm())
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        main = torch.cuda.current_stream()
+        a = lst.grad_norm()
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            b = lst.grad_norm(grad_scale=2.0)
+        del lst
+        rest = [torch.full((26_000,), 7, dtype=torch.uint8, device=DEV) for _ in range(8)]      # of the size of its memory, on the other branch
+        main.wait_stream(side)
+    for _ in range(5):
+        for x in [a, b] + rest:
+            x.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert [float(x) for x in (a, b)] == [want, 2 * want] and all((x == 7).all() for x in rest)

@@ -273,3 +273,17 @@ def test_calls_on_a_list_of_another_gpu_than_the_current_one(gpu):
         opt.step()
     g.replay()
     assert [r["call"] for r in gpu.ran] == ["norm", "adamw", "adamw", "clip", "adamw"] and all(r["fits"] for r in gpu.ran) and gpu.device == 1
+
+
+def test_a_graphs_memory_is_known_to_be_used_on_each_of_its_streams(gpu):
+    """A list that goes during the capture leaves its memory to what the capture allocates next: not while another branch is still at it."""
+    lst = gpu.optim.TensorList([fake_lists.on_gpu(torch.ones(10))])
+    out = fake_lists.on_gpu(torch.zeros(1))
+    fake_lists.OnGpu.used_on.clear()
+    with gpu.capture(9):
+        lst.grad_norm(out=out)
+        gpu.captures[11] = gpu.captures[9]
+        with gpu.on(11):
+            lst.grad_norm(out=out)
+        assert fake_lists.OnGpu.used_on == [(lst._handle.graph.workspace.data_ptr(), 11)]
+        del gpu.captures[11]
