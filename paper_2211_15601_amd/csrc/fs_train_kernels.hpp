@@ -387,8 +387,8 @@ __global__ __launch_bounds__(SHORT_THREADS) void k_norm_short(ListD L, double sc
 
 // ---- clipping ----
 
-// s min(1, max_norm / (norm + 1e-6)), NaN for a norm that is NaN; rounded once.  (From a norm of 32 bits its largest error would be 2.6 times that, and gradients
-// whose norm 32 bits cannot hold would become zeros.)
+// s min(1, max_norm / (norm + 1e-6)), NaN for a norm that is NaN; rounded once.  (From a norm of 32 bits it would be off by about twice as much, and
+// gradients whose norm 32 bits cannot hold would become zeros.)
 __device__ __forceinline__ float clip_coef(double norm, double max_norm, double scale)
 {
     if (max_norm == __builtin_inf()) return (float)scale;
