@@ -24,9 +24,11 @@ EXPORTS = ["fs_create", "fs_destroy", "fs_set_params", "fs_set_tuning", "fs_set_
            "fs_dedupe", "fs_dedupe_noalloc", "fs_get_transforms", "fs_get_corr", "fs_microbench", "fs_set_timing", "fs_get_timing", "fs_last_error",
            "fs_version",
            "fs_tensors_create", "fs_tensors_create_noalloc", "fs_tensors_bytes", "fs_tensors_destroy", "fs_tensors_update", "fs_tensors_ready", "fs_tensors_set_stream", "fs_tensors_error",
-           "fs_grad_norm", "fs_grad_clip", "fs_adamw_step"]
+           "fs_grad_norm", "fs_grad_clip", "fs_adamw_step",
+           "fs_linear_bytes", "fs_linear_forward", "fs_linear_backward", "fs_dropout", "fs_net_error"]
 FS_FLOAT_FULL, FS_FLOAT_BRAIN, FS_FLOAT_HALF = 0, 1, 2
 FS_NORM_TWO, FS_NORM_MAX = 0, 1
+FS_ACT_NONE, FS_ACT_RELU, FS_ACT_GELU, FS_ACT_SILU, FS_ACT_SOFTPLUS = range(5)
 
 
 class GridDesc(ctypes.Structure):
@@ -53,6 +55,17 @@ class AdamW(ctypes.Structure):
     """fs_adamw of include/fastsnarf_train.h"""
     _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay", "max_norm", "grad_scale")] + \
                [("norm_given", ctypes.c_int32), ("skip_nonfinite", ctypes.c_int32), ("d_lr", ctypes.c_void_p)]
+
+
+class Drop(ctypes.Structure):
+    """fs_drop of include/fastsnarf_net.h"""
+    _fields_ = [("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64), ("d_seed", ctypes.c_void_p)]
+
+
+class Linear(ctypes.Structure):
+    """fs_linear of include/fastsnarf_net.h"""
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "inputs", "outputs")] + [(n, ctypes.c_int32) for n in ("type", "bias_type", "act")] + \
+               [("beta", ctypes.c_float), ("drop", Drop)]
 
 
 class FsError(RuntimeError):
@@ -107,10 +120,17 @@ def load():
     L.fs_grad_norm.argtypes = [vp, i32, ctypes.c_double, vp]
     L.fs_grad_clip.argtypes = [vp, i32, ctypes.c_double, ctypes.c_double, i32, vp]
     L.fs_adamw_step.argtypes = [vp, ctypes.POINTER(AdamW), vp, vp]
+    layer, drop = ctypes.POINTER(Linear), ctypes.POINTER(Drop)
+    L.fs_linear_bytes.argtypes = [layer, i32]
+    L.fs_linear_forward.argtypes = [layer, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+    L.fs_linear_backward.argtypes = [layer, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i64, vp]
+    L.fs_dropout.argtypes = [i32, i64, i64, drop, vp, i64, vp, i64, vp, i64, vp]
+    L.fs_net_error.argtypes = []
+    L.fs_net_error.restype = ctypes.c_char_p
     for name in EXPORTS:
-        if name not in ("fs_last_error", "fs_version", "fs_tensors_error"):
+        if name not in ("fs_last_error", "fs_version", "fs_tensors_error", "fs_net_error"):
             getattr(L, name).restype = ctypes.c_int
-    L.fs_tensors_bytes.restype = i64
+    L.fs_tensors_bytes.restype = L.fs_linear_bytes.restype = i64
     _lib = L
     return L
 

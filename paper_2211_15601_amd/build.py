@@ -9,7 +9,7 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(CSRC, "libfastsnarf.so")
-SOURCES = ["fastsnarf.hip", "fs_train.hip", "fs_microbench.hip"]
+SOURCES = ["fastsnarf.hip", "fs_train.hip", "fs_net.hip", "fs_microbench.hip"]
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-ffp-contract=off",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -1,0 +1,424 @@
+// C ABI of the networks' layers (see include/fastsnarf_net.h): argument checks, shapes of launches, launches.  gfx950 only.
+#include "../../include/fastsnarf_net.h"
+#include "fs_net_kernels.hpp"
+
+#include <hip/hip_runtime.h>
+#include <algorithm>
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+
+using namespace fs;
+
+static_assert(int(FS_FLOAT_FULL) == NET_F32 && int(FS_FLOAT_BRAIN) == NET_BF16 && int(FS_FLOAT_HALF) == NET_F16, "types");
+static_assert(int(FS_ACT_NONE) == ACT_NONE && int(FS_ACT_RELU) == ACT_RELU && int(FS_ACT_GELU) == ACT_GELU && int(FS_ACT_SILU) == ACT_SILU &&
+              int(FS_ACT_SOFTPLUS) == ACT_SOFTPLUS, "activations");
+
+namespace {
+
+thread_local char net_err[256];
+
+fs_status fail(fs_status s, const char *fmt, ...)
+{
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(net_err, sizeof net_err, fmt, ap);
+    va_end(ap);
+    return s;
+}
+
+fs_status launch_status(const char *what)
+{
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? FS_OK : fail(FS_E_DEVICE, "%s: %s", what, hipGetErrorString(e));
+}
+
+bool type_ok(int32_t type) { return type == FS_FLOAT_FULL || type == FS_FLOAT_BRAIN || type == FS_FLOAT_HALF; }
+int size_of(int32_t type) { return type == FS_FLOAT_FULL ? 4 : 2; }
+
+// Memory of the current device?  The lookup in the runtime takes as long as a launch, and a program passes the same addresses again and again,
+// so a thread remembers those it has confirmed, as fastsnarf.hip does.
+bool on_device(int device, const void *p)
+{
+    static thread_local struct { const void *p; int device; } seen[64];
+    const uintptr_t u = reinterpret_cast<uintptr_t>(p);
+    const int h = (int)((u >> 9 ^ u >> 15 ^ u >> 21) & 63);
+    if (seen[h].p == p && seen[h].device == device) return true;
+    hipPointerAttribute_t a;
+    if (hipPointerGetAttributes(&a, p) != hipSuccess) {
+        (void)hipGetLastError();
+        return false;
+    }
+    if ((a.type != hipMemoryTypeDevice && a.type != hipMemoryTypeManaged) || a.device != device) return false;
+    seen[h] = {p, device};
+    return true;
+}
+
+// An array of a call: `rows` rows of `cols` elements of `size` bytes, `ld` elements apart.
+struct Array { const char *name; const void *at; int64_t rows, cols, ld; int size; bool written; };
+
+bool empty(const Array &a) { return a.rows == 0 || a.cols == 0; }
+uintptr_t begin_of(const Array &a) { return reinterpret_cast<uintptr_t>(a.at); }
+unsigned __int128 extent(const Array &a) { return ((unsigned __int128)(a.rows - 1) * (uint64_t)a.ld + (uint64_t)a.cols) * a.size; }
+
+// `same`: a written array may be that one itself.  Arrays whose address is NULL are left out by the caller where they may be.
+fs_status check_arrays(const char *what, int device, const Array *a, int count, int y = -1, int same = -1)
+{
+    for (int i = 0; i < count; ++i) {
+        if (empty(a[i]) || !a[i].at) continue;
+        if (a[i].ld < 0 || (a[i].written && a[i].rows > 1 && a[i].ld < a[i].cols)) return fail(FS_E_SHAPE, "%s: rows of %s are %lld elements apart", what, a[i].name, (long long)a[i].ld);
+        if (extent(a[i]) >> 56) return fail(FS_E_SHAPE, "%s: %s is too large", what, a[i].name);
+        if (begin_of(a[i]) % a[i].size || !on_device(device, a[i].at)) return fail(FS_E_ARG, "%s: %s must be a device pointer aligned to its elements", what, a[i].name);
+    }
+    for (int i = 0; i < count; ++i) {
+        if (!a[i].written || empty(a[i]) || !a[i].at) continue;
+        for (int j = 0; j < count; ++j) {
+            if (i == j || empty(a[j]) || !a[j].at || (a[j].written && j < i)) continue;
+            if (i == y && j == same && a[i].at == a[j].at && (a[i].ld == a[j].ld || a[i].rows == 1)) continue;
+            if (begin_of(a[i]) < begin_of(a[j]) + (uint64_t)extent(a[j]) && begin_of(a[j]) < begin_of(a[i]) + (uint64_t)extent(a[i]))
+                return fail(FS_E_ARG, "%s: %s overlaps %s", what, a[i].name, a[j].name);
+        }
+    }
+    return FS_OK;
+}
+
+fs_status check_drop(const char *what, const fs_drop &d)
+{
+    if (!(d.p >= 0.0 && d.p <= 1.0)) return fail(FS_E_ARG, "%s: the chance of dropping must be in 0 .. 1", what);
+    return FS_OK;
+}
+
+// With the device known: where the seed lies.
+fs_status check_seed(const char *what, int device, const fs_drop &d)
+{
+    if (d.p > 0.0 && d.d_seed && (reinterpret_cast<uintptr_t>(d.d_seed) % 8 || !on_device(device, d.d_seed)))
+        return fail(FS_E_ARG, "%s: d_seed must be a device pointer aligned to 8 bytes", what);
+    return FS_OK;
+}
+
+DropD drop_of(const fs_drop &d)
+{
+    DropD r = {};
+    const double least = std::floor(d.p * 4294967296.0 + 0.5);
+    r.mode = d.p == 0.0 ? 0 : least >= 4294967296.0 ? 2 : 1;
+    if (r.mode != 1) return r;
+    r.at = reinterpret_cast<const long long *>(d.d_seed);
+    r.seed = d.seed;
+    r.offset = d.offset;
+    r.least = (unsigned)least;
+    r.scale = (float)(1.0 / (1.0 - d.p));
+    return r;
+}
+
+fs_status check_layer(const char *what, const fs_linear *l)
+{
+    if (!l) return fail(FS_E_ARG, "%s: layer is NULL", what);
+    if (l->rows < 0 || l->rows > 1000000000ll || l->inputs < 0 || l->inputs > 1 << 24 || l->outputs < 0 || l->outputs > 1 << 24) return fail(FS_E_SHAPE, "%s: sizes out of range", what);
+    if (!type_ok(l->type) || (l->bias_type != l->type && l->bias_type != FS_FLOAT_FULL)) return fail(FS_E_ARG, "%s: bad type", what);
+    if (l->act < FS_ACT_NONE || l->act > FS_ACT_SOFTPLUS) return fail(FS_E_ARG, "%s: bad act", what);
+    if (l->act == FS_ACT_SOFTPLUS && !(l->beta > 0.0f && std::isfinite(l->beta))) return fail(FS_E_ARG, "%s: beta must be positive and finite", what);
+    return check_drop(what, l->drop);
+}
+
+int cus_of(int device)
+{
+    int n = 0;
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess || n < 1) n = 256;
+    (void)hipGetLastError();
+    return n;
+}
+
+// ---------------------------------------------------------------------------------------------------------------- products
+
+// How a product is launched: tiles of `tile` squared, `parts` parts of the range of t, each t_part long.
+struct Plan {
+    int tile, parts;
+    long long t_part, tiles_p, tiles_q, ldp;
+    int64_t part_bytes() const { return parts > 1 ? (int64_t)parts * part_stride * 4 : 0; }
+    long long part_stride;
+};
+
+constexpr long long MAX_TILES = (1ll << 24) - 1;        // of 256 threads each: a launch has less than 2^32
+
+// Parts: enough for two blocks a compute unit, none shorter than 256.
+Plan plan_product(int type, int64_t np, int64_t nq, int64_t nt, int cus)
+{
+    Plan p = {};
+    const long long bt = type == FS_FLOAT_FULL ? 32 : 64;
+    auto tiles = [&](int64_t n, int b) { return (long long)((n + b - 1) / b); };
+    p.tile = tiles(np, 128) * tiles(nq, 128) >= cus && np > 64 && nq > 64 ? 128 : 64;
+    p.tiles_p = tiles(np, p.tile);
+    p.tiles_q = tiles(nq, p.tile);
+    const long long all = std::max(1ll, p.tiles_p * p.tiles_q);
+    const long long wanted = std::min((2ll * cus + all - 1) / all, std::max<long long>(1, nt / 256));
+    p.t_part = std::max(bt, ((long long)nt + wanted - 1) / wanted);
+    p.t_part = (p.t_part + bt - 1) / bt * bt;
+    p.parts = (int)std::max<long long>(1, (nt + p.t_part - 1) / p.t_part);
+    p.ldp = (np + 3) / 4 * 4;
+    p.part_stride = p.ldp * nq;
+    return p;
+}
+
+template <int TYPE, bool PCOL, bool QCOL>
+void launch_product(const Plan &p, const MatD &P, const MatD &Q, int64_t np, int64_t nq, int64_t nt, const EpiD &E, hipStream_t stream)
+{
+    const TilesD tiles = {(int)p.tiles_p, (int)p.tiles_q, p.parts};
+    const dim3 grid((unsigned)(p.tiles_p * p.tiles_q), (unsigned)p.parts);
+    if (p.tile == 128) k_product<TYPE, PCOL, QCOL, 128, 128, 2, 2><<<grid, 256, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
+    else k_product<TYPE, PCOL, QCOL, 64, 64, 2, 2><<<grid, 256, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
+}
+
+template <int TYPE>
+void launch_parts(const Plan &p, const float *part, int64_t np, int64_t nq, const EpiD &E, hipStream_t stream)
+{
+    const long long all = (np + 255) / 256 * nq;
+    k_parts<TYPE><<<(unsigned)std::min<long long>(all, 1 << 16), 256, 0, stream>>>(part, p.part_stride, p.ldp, p.parts, np, nq, E);
+}
+
+enum { NT, NN, TN };                   // forward, dX, dweight
+
+// One product with its epilogue; `work`: part_bytes() of the plan.
+void product(int type, int kind, const Plan &p, const MatD &P, const MatD &Q, int64_t np, int64_t nq, int64_t nt, const EpiD &E, void *work, hipStream_t stream)
+{
+    if (np == 0 || nq == 0) return;
+    EpiD part = E;
+    if (p.parts > 1) {
+        part = {};
+        part.mode = EPI_PART;
+        part.out = work;
+        part.ldo = p.ldp;
+        part.part_stride = p.part_stride;
+    }
+#define FS_NET_KIND(TYPE)                                                                              \
+    do {                                                                                               \
+        if (kind == NT) launch_product<TYPE, false, false>(p, P, Q, np, nq, nt, part, stream);         \
+        else if (kind == NN) launch_product<TYPE, true, false>(p, P, Q, np, nq, nt, part, stream);     \
+        else launch_product<TYPE, true, true>(p, P, Q, np, nq, nt, part, stream);                      \
+        if (p.parts > 1) launch_parts<TYPE>(p, static_cast<const float *>(work), np, nq, E, stream);   \
+    } while (0)
+    if (type == FS_FLOAT_FULL) FS_NET_KIND(NET_F32);
+    else if (type == FS_FLOAT_BRAIN) FS_NET_KIND(NET_BF16);
+    else FS_NET_KIND(NET_F16);
+#undef FS_NET_KIND
+}
+
+// ---------------------------------------------------------------------------------------------------------------- elementwise
+
+struct RowsPlan { RowsD n; unsigned gx, gy; };
+
+RowsPlan plan_rows(int type, int64_t rows, int64_t cols, long long blocks)
+{
+    RowsPlan p;
+    const int v = type == FS_FLOAT_FULL ? 4 : 8;
+    const long long units = (cols + v - 1) / v;
+    p.n.rows = rows;
+    p.n.cols = cols;
+    p.n.tx_bits = 0;
+    while (p.n.tx_bits < 8 && 1ll << p.n.tx_bits < units) ++p.n.tx_bits;
+    p.gx = (unsigned)std::min<long long>(1 << 16, std::max<long long>(1, (units + (1 << p.n.tx_bits) - 1) >> p.n.tx_bits));
+    const long long at_once = 256 >> p.n.tx_bits, passes = std::max<long long>(1, (rows + at_once - 1) / at_once);
+    const long long gy = std::max(1ll, std::min(passes, blocks / p.gx));
+    const long long each = (passes + gy - 1) / gy;
+    p.gy = (unsigned)((passes + each - 1) / each);
+    p.n.per_block = each * at_once;
+    return p;
+}
+
+constexpr long long ROW_BLOCKS = 2048;
+
+template <int TYPE> void launch_dz(const RowsPlan &p, const MatD &G, const MatD &Z, const fs_linear &l, void *dz, float *sums, hipStream_t stream)
+{
+    k_dz<TYPE, TYPE == NET_F32 ? 4 : 8><<<dim3(p.gx, p.gy), 256, 0, stream>>>(p.n, G, Z, l.bias_type == FS_FLOAT_FULL, l.act, l.beta, drop_of(l.drop), dz, l.outputs, sums);
+}
+
+int64_t up(int64_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// The backward pass's workspace: dZ (where it is not G itself), the sums of its columns, parts of either product.
+struct Backward {
+    Plan dx, dw;
+    RowsPlan dz;
+    bool has_dz;
+    int64_t sums, part, end;
+};
+
+Backward plan_backward(const fs_linear &l, int cus)
+{
+    Backward b;
+    b.dx = plan_product(l.type, l.inputs, l.rows, l.outputs, cus);
+    b.dw = plan_product(l.type, l.inputs, l.outputs, l.rows, cus);
+    b.dz = plan_rows(l.type, l.rows, l.outputs, ROW_BLOCKS);
+    b.has_dz = l.act != FS_ACT_NONE || l.drop.p > 0.0;
+    b.sums = b.has_dz ? up(l.rows * l.outputs * size_of(l.type)) : 0;
+    b.part = b.sums + up((int64_t)b.dz.gy * l.outputs * 4);
+    b.end = b.part + up(std::max(b.dx.part_bytes(), b.dw.part_bytes()));
+    return b;
+}
+
+bool too_many(const Plan &p) { return (unsigned __int128)p.tiles_p * p.tiles_q > MAX_TILES; }
+
+fs_status current_device(const char *what, int *device)
+{
+    if (hipGetDevice(device) == hipSuccess) return FS_OK;
+    (void)hipGetLastError();
+    return fail(FS_E_DEVICE, "%s: no device", what);
+}
+
+fs_status check_work(const char *what, int device, const void *work, int64_t bytes, int64_t needed)
+{
+    if (needed == 0) return FS_OK;
+    if (!work || bytes < needed) return fail(FS_E_ARG, "%s: needs %lld bytes of workspace", what, (long long)needed);
+    if (reinterpret_cast<uintptr_t>(work) % 256 || !on_device(device, work)) return fail(FS_E_ARG, "%s: the workspace must be a device pointer aligned to 256 bytes", what);
+    return FS_OK;
+}
+
+#define FS_NET_TRY(x)                           \
+    do {                                        \
+        const fs_status try_status = (x);       \
+        if (try_status != FS_OK) return try_status; \
+    } while (0)
+
+}  // namespace
+
+extern "C" {
+
+const char *fs_net_error(void) { return net_err; }
+
+int64_t fs_linear_bytes(const fs_linear *layer, int32_t backward)
+{
+    if (check_layer("fs_linear_bytes", layer) != FS_OK) return -1;
+    int device = 0;
+    if (current_device("fs_linear_bytes", &device) != FS_OK) return -1;
+    const int cus = cus_of(device);
+    if (!backward) return up(plan_product(layer->type, layer->outputs, layer->rows, layer->inputs, cus).part_bytes());
+    return plan_backward(*layer, cus).end;
+}
+
+fs_status fs_linear_forward(const fs_linear *layer, const void *d_x, int64_t ldx, const void *d_w, int64_t ldw, const void *d_bias, const void *d_r, int64_t ldr,
+                            void *d_y, int64_t ldy, void *d_z, int64_t ldz, void *d_work, int64_t work_bytes, void *hip_stream)
+{
+    const char *what = "fs_linear_forward";
+    FS_NET_TRY(check_layer(what, layer));
+    const fs_linear &l = *layer;
+    int device = 0;
+    FS_NET_TRY(current_device(what, &device));
+    const int64_t m = l.rows, n = l.outputs, k = l.inputs;
+    const Plan p = plan_product(l.type, n, m, k, cus_of(device));
+    if (too_many(p)) return fail(FS_E_SHAPE, "%s: too many results", what);
+    if (m > 0 && n > 0) {
+        const int s = size_of(l.type);
+        if (!d_y || (k > 0 && (!d_x || !d_w))) return fail(FS_E_ARG, "%s: d_x, d_w and d_y must not be NULL", what);
+        const Array a[] = {{"d_x", d_x, m, k, ldx, s, false}, {"d_w", d_w, n, k, ldw, s, false}, {"d_bias", d_bias, 1, n, 0, size_of(l.bias_type), false},
+                           {"d_r", d_r, m, n, ldr, s, false}, {"d_y", d_y, m, n, ldy, s, true}, {"d_z", d_z, m, n, ldz, size_of(l.bias_type), true},
+                           {"d_work", d_work, 1, p.part_bytes(), 0, 1, true}};
+        FS_NET_TRY(check_arrays(what, device, a, 7, 4, 3));
+        FS_NET_TRY(check_seed(what, device, l.drop));
+        FS_NET_TRY(check_work(what, device, d_work, work_bytes, p.part_bytes()));
+    }
+    EpiD E = {};
+    E.mode = EPI_LAYER;
+    E.act = l.act;
+    E.beta = l.beta;
+    E.bias = d_bias;
+    E.bias_f32 = l.bias_type == FS_FLOAT_FULL;
+    E.r = d_r;
+    E.ldr = ldr;
+    E.out = d_y;
+    E.ldo = ldy;
+    E.z = d_z;
+    E.ldz = ldz;
+    E.drop = drop_of(l.drop);
+    product(l.type, NT, p, {d_w, ldw, n, k}, {d_x, ldx, m, k}, n, m, k, E, d_work, static_cast<hipStream_t>(hip_stream));
+    return launch_status(what);
+}
+
+fs_status fs_linear_backward(const fs_linear *layer, const void *d_g, int64_t ldg, const void *d_x, int64_t ldx, const void *d_w, int64_t ldw, const void *d_z, int64_t ldz,
+                             void *d_dx, int64_t lddx, void *d_dw, int64_t lddw, void *d_dbias, void *d_work, int64_t work_bytes, void *hip_stream)
+{
+    const char *what = "fs_linear_backward";
+    FS_NET_TRY(check_layer(what, layer));
+    const fs_linear &l = *layer;
+    int device = 0;
+    FS_NET_TRY(current_device(what, &device));
+    const int64_t m = l.rows, n = l.outputs, k = l.inputs;
+    const Backward b = plan_backward(l, cus_of(device));
+    if (too_many(b.dx) || too_many(b.dw)) return fail(FS_E_SHAPE, "%s: too many results", what);
+    const int s = size_of(l.type);
+    const bool act = l.act != FS_ACT_NONE;
+    if (m > 0 && n > 0 && (d_dbias || (k > 0 && (d_dx || d_dw)))) {
+        if (!d_g || (act && !d_z) || (k > 0 && ((d_dx && !d_w) || (d_dw && !d_x)))) return fail(FS_E_ARG, "%s: an array that is needed is NULL", what);
+    }
+    const Array a[] = {{"d_g", d_g, m, n, ldg, s, false}, {"d_x", d_dw ? d_x : nullptr, m, k, ldx, s, false}, {"d_w", d_dx ? d_w : nullptr, n, k, ldw, s, false},
+                       {"d_z", act ? d_z : nullptr, m, n, ldz, size_of(l.bias_type), false}, {"d_dx", d_dx, m, k, lddx, s, true}, {"d_dw", d_dw, n, k, lddw, s, true},
+                       {"d_dbias", d_dbias, 1, n, 0, size_of(l.bias_type), true}, {"d_work", d_work, 1, b.end, 0, 1, true}};
+    FS_NET_TRY(check_arrays(what, device, a, 8));
+    FS_NET_TRY(check_seed(what, device, l.drop));
+    FS_NET_TRY(check_work(what, device, d_work, work_bytes, b.end));
+
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    char *work = static_cast<char *>(d_work);
+    float *sums = d_dbias ? reinterpret_cast<float *>(work + b.sums) : nullptr;
+    const MatD G = {d_g, ldg, m, n}, Z = {d_z, ldz, m, n};
+    const MatD dZ = b.has_dz ? MatD{work, n, m, n} : G;
+    void *dz = b.has_dz && (d_dx || d_dw) ? work : nullptr;
+    if ((dz || sums) && n > 0) {
+        if (l.type == FS_FLOAT_FULL) launch_dz<NET_F32>(b.dz, G, Z, l, dz, sums, stream);
+        else if (l.type == FS_FLOAT_BRAIN) launch_dz<NET_BF16>(b.dz, G, Z, l, dz, sums, stream);
+        else launch_dz<NET_F16>(b.dz, G, Z, l, dz, sums, stream);
+        if (sums) {
+            const unsigned blocks = (unsigned)((n + 63) / 64);
+            if (l.bias_type == FS_FLOAT_FULL) k_dbias<NET_F32><<<blocks, 256, 0, stream>>>(sums, (int)b.dz.gy, n, d_dbias);
+            else if (l.bias_type == FS_FLOAT_BRAIN) k_dbias<NET_BF16><<<blocks, 256, 0, stream>>>(sums, (int)b.dz.gy, n, d_dbias);
+            else k_dbias<NET_F16><<<blocks, 256, 0, stream>>>(sums, (int)b.dz.gy, n, d_dbias);
+        }
+    }
+    EpiD E = {};
+    E.mode = EPI_STORE;
+    if (d_dx) {
+        E.out = d_dx;
+        E.ldo = lddx;
+        product(l.type, NN, b.dx, {d_w, ldw, n, k}, dZ, k, m, n, E, work + b.part, stream);
+    }
+    if (d_dw) {
+        E.out = d_dw;
+        E.ldo = lddw;
+        product(l.type, TN, b.dw, {d_x, ldx, m, k}, dZ, k, n, m, E, work + b.part, stream);
+    }
+    return launch_status(what);
+}
+
+fs_status fs_dropout(int32_t type, int64_t rows, int64_t columns, const fs_drop *drop, const void *d_x, int64_t ldx, const void *d_r, int64_t ldr, void *d_y, int64_t ldy,
+                     void *hip_stream)
+{
+    const char *what = "fs_dropout";
+    if (!drop) return fail(FS_E_ARG, "%s: drop is NULL", what);
+    if (!type_ok(type)) return fail(FS_E_ARG, "%s: bad type", what);
+    if (rows < 0 || columns < 0 || rows > 1ll << 36 || columns > 1ll << 36 || (unsigned __int128)rows * columns > (1ull << 40)) return fail(FS_E_SHAPE, "%s: sizes out of range", what);
+    FS_NET_TRY(check_drop(what, *drop));
+    if (rows == 0 || columns == 0) return FS_OK;
+    int device = 0;
+    FS_NET_TRY(current_device(what, &device));
+    const int s = size_of(type);
+    if (!d_x || !d_y) return fail(FS_E_ARG, "%s: d_x and d_y must not be NULL", what);
+    const Array a[] = {{"d_x", d_x, rows, columns, ldx, s, false}, {"d_r", d_r, rows, columns, ldr, s, false}, {"d_y", d_y, rows, columns, ldy, s, true}};
+    // Y may be either of what it is made from, element by element
+    const Array xy[] = {a[0], a[2]}, ry[] = {a[1], a[2]};
+    FS_NET_TRY(check_arrays(what, device, xy, 2, 1, 0));
+    FS_NET_TRY(check_arrays(what, device, ry, 2, 1, 0));
+    FS_NET_TRY(check_seed(what, device, *drop));
+    // rows without gaps are one
+    if (ldx == columns && ldy == columns && (!d_r || ldr == columns)) {
+        columns *= rows;
+        rows = 1;
+    }
+    const RowsPlan p = plan_rows(type, rows, columns, ROW_BLOCKS);
+    const MatD X = {d_x, ldx, rows, columns}, R = {d_r, ldr, rows, columns};
+    const dim3 grid(p.gx, p.gy);
+    const DropD D = drop_of(*drop);
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    if (type == FS_FLOAT_FULL) k_dropout<NET_F32, 4><<<grid, 256, 0, stream>>>(p.n, X, R, d_y, ldy, D);
+    else if (type == FS_FLOAT_BRAIN) k_dropout<NET_BF16, 8><<<grid, 256, 0, stream>>>(p.n, X, R, d_y, ldy, D);
+    else k_dropout<NET_F16, 8><<<grid, 256, 0, stream>>>(p.n, X, R, d_y, ldy, D);
+    return launch_status(what);
+}
+
+}  // extern "C"

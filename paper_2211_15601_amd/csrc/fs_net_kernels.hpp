@@ -1,0 +1,606 @@
+// Kernels of the networks' layers: products with their epilogue, the backward pass, dropout (see include/fastsnarf_net.h).
+//
+// Every product is D[p][q] = sum over t of P[p][t] Q[q][t], with p along the rows of the result in memory.  As operands of the matrix instructions P has their
+// rows and Q their columns, so a lane's results are four neighbours p: a vector to store, and the words of one Philox call.
+//   forward  p = outputs, q = rows,    t = inputs     P = weight (t along its rows), Q = X  (t along its rows)
+//   dX       p = inputs,  q = rows,    t = outputs    P = weight (p along its rows), Q = dZ (t along its rows)
+//   dweight  p = inputs,  q = outputs, t = rows       P = X      (p along its rows), Q = dZ (q along its rows)
+// A matrix with t along its rows lies in LDS as it lies in memory and is read 16 bytes a lane; one with p or q along its rows, too, and is turned on the way
+// to the registers by the LDS's transposing reads.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace fs {
+
+enum { NET_F32, NET_BF16, NET_F16 };
+enum { ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU, ACT_SOFTPLUS };
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// A matrix in memory, `ld` elements from row to row.
+struct MatD { const void *at; long long ld, rows, cols; };
+
+struct DropD {
+    const long long *at;               // seed and offset on the device, or NULL:
+    unsigned long long seed, offset;
+    unsigned least;                    // words from here on are kept
+    int mode;                          // 0: nothing is dropped, 1: by the words, 2: everything is
+    float scale;
+};
+
+// ---------------------------------------------------------------------------------------------------------------- elements
+
+template <int TYPE> struct ElemOf { typedef unsigned short type; };
+template <> struct ElemOf<NET_F32> { typedef float type; };
+
+template <int TYPE> __device__ inline float widen(typename ElemOf<TYPE>::type v)
+{
+    if constexpr (TYPE == NET_F32) return v;
+    else if constexpr (TYPE == NET_BF16) return __uint_as_float((unsigned)v << 16);
+    else return (float)__builtin_bit_cast(_Float16, v);
+}
+
+template <int TYPE> __device__ inline typename ElemOf<TYPE>::type narrow(float v)
+{
+    if constexpr (TYPE == NET_F32) return v;
+    else if constexpr (TYPE == NET_BF16) return __builtin_bit_cast(unsigned short, (__bf16)v);
+    else return __builtin_bit_cast(unsigned short, (_Float16)v);
+}
+
+// N elements in memory, at any address that is a multiple of one: the vector instructions take those.
+template <int TYPE, int N> struct __attribute__((packed, aligned(TYPE == NET_F32 ? 4 : 2))) Packed { typename ElemOf<TYPE>::type v[N]; };
+
+// The first `n` (1 .. N) of N elements, zeros behind them.
+template <int TYPE, int N> __device__ inline Packed<TYPE, N> load_some(const typename ElemOf<TYPE>::type *at, int n)
+{
+    Packed<TYPE, N> r;
+    if (n >= N) return *reinterpret_cast<const Packed<TYPE, N> *>(at);
+#pragma unroll
+    for (int i = 0; i < N; ++i) r.v[i] = i < n ? at[i] : typename ElemOf<TYPE>::type(0);
+    return r;
+}
+
+template <int TYPE, int N> __device__ inline void load_wide(float *v, const typename ElemOf<TYPE>::type *at, int n)
+{
+    const auto x = load_some<TYPE, N>(at, n);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = widen<TYPE>(x.v[i]);
+}
+
+template <int TYPE, int N> __device__ inline void store_some(typename ElemOf<TYPE>::type *at, const float *v, int n)
+{
+    Packed<TYPE, N> r;
+#pragma unroll
+    for (int i = 0; i < N; ++i) r.v[i] = narrow<TYPE>(v[i]);
+    if (n >= N) {
+        *reinterpret_cast<Packed<TYPE, N> *>(at) = r;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (i < n) at[i] = r.v[i];
+}
+
+// ---------------------------------------------------------------------------------------------------------------- dropout
+
+// Philox4x32-10.  Ten rounds take a large bf16 dropout 7 % longer than none at all: 512 MB read and 512 MB written in 205 and 190 us (seven rounds: 196).
+__device__ inline uint4 philox(unsigned long long block, unsigned long long offset, unsigned long long seed)
+{
+    unsigned a = (unsigned)block, b = (unsigned)(block >> 32), c = (unsigned)offset, d = (unsigned)(offset >> 32);
+    unsigned k0 = (unsigned)seed, k1 = (unsigned)(seed >> 32);
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const unsigned long long p = 0xD2511F53ull * a, q = 0xCD9E8D57ull * c;
+        a = (unsigned)(q >> 32) ^ b ^ k0;
+        b = (unsigned)q;
+        c = (unsigned)(p >> 32) ^ d ^ k1;
+        d = (unsigned)p;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return make_uint4(a, b, c, d);
+}
+
+struct Seed { unsigned long long seed, offset; };
+__device__ inline Seed seed_of(const DropD &d)
+{
+    Seed s = {d.seed, d.offset};
+    if (d.mode == 1 && d.at) {
+        s.seed = (unsigned long long)d.at[0];
+        s.offset = (unsigned long long)d.at[1];
+    }
+    return s;
+}
+
+// drop() of N (4 or 8) elements from element e on.
+template <int N> __device__ inline void drop(float *v, unsigned long long e, const DropD &d, const Seed &s)
+{
+    if (d.mode == 0) return;
+    if (d.mode == 2) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = 0.0f;
+        return;
+    }
+    const int shift = (int)(e & 3);
+    unsigned w[N + 4];
+#pragma unroll
+    for (int b = 0; b < N / 4; ++b) {
+        const uint4 x = philox((e >> 2) + b, s.offset, s.seed);
+        w[4 * b] = x.x; w[4 * b + 1] = x.y; w[4 * b + 2] = x.z; w[4 * b + 3] = x.w;
+    }
+    if (shift) {                       // the elements begin inside a call's words
+        const uint4 x = philox((e >> 2) + N / 4, s.offset, s.seed);
+        w[N] = x.x; w[N + 1] = x.y; w[N + 2] = x.z; w[N + 3] = x.w;
+        if (shift & 1)
+#pragma unroll
+            for (int i = 0; i < N + 3; ++i) w[i] = w[i + 1];
+        if (shift & 2)
+#pragma unroll
+            for (int i = 0; i < N + 2; ++i) w[i] = w[i + 2];
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = w[i] >= d.least ? v[i] * d.scale : 0.0f;
+}
+
+// ---------------------------------------------------------------------------------------------------------------- activations
+
+__device__ inline float act_of(float z, int act, float beta)
+{
+    switch (act) {
+    case ACT_RELU: return z < 0.0f ? 0.0f : z;                                     // NaN stays
+    case ACT_GELU: return 0.5f * z * erfcf(z * -0.70710678f);
+    case ACT_SILU: return z / (1.0f + expf(-z));
+    case ACT_SOFTPLUS: return (z < 0.0f ? 0.0f : z) + log1pf(expf(-fabsf(z * beta))) / beta;
+    default: return z;
+    }
+}
+
+__device__ inline float slope_of(float z, int act, float beta)
+{
+    switch (act) {
+    case ACT_RELU: return z <= 0.0f ? 0.0f : 1.0f;
+    case ACT_GELU: return __builtin_fmaf(z * 0.39894228f, expf(-0.5f * z * z), 0.5f * erfcf(z * -0.70710678f));
+    case ACT_SILU: {
+        const float s = 1.0f / (1.0f + expf(-z));
+        return s * __builtin_fmaf(z, 1.0f - s, 1.0f);
+    }
+    case ACT_SOFTPLUS: return 1.0f / (1.0f + expf(-z * beta));
+    default: return 1.0f;
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------- epilogue
+
+enum { EPI_LAYER, EPI_STORE, EPI_PART };
+
+// What becomes of D.  EPI_LAYER: the layer's Y (and Z), EPI_STORE: out = D in the type, EPI_PART: fp32 sums of one part of the range of t
+// into out, `part_stride` floats from part to part.
+struct EpiD {
+    int mode, act, bias_f32;
+    float beta;
+    const void *bias, *r;
+    void *out, *z;
+    long long ldr, ldo, ldz, part_stride;
+    DropD drop;
+};
+
+template <int TYPE> __device__ inline void load_bias(float *b, const EpiD &E, long long p, int n)
+{
+    if (E.mode != EPI_LAYER || !E.bias || n <= 0) {
+        b[0] = b[1] = b[2] = b[3] = 0.0f;
+    } else if (E.bias_f32) {
+        load_wide<NET_F32, 4>(b, static_cast<const float *>(E.bias) + p, n);
+    } else {
+        load_wide<TYPE, 4>(b, static_cast<const typename ElemOf<TYPE>::type *>(E.bias) + p, n);
+    }
+}
+
+// Four results of row q from p on, of which n (1 .. 4) are in the matrix; cols: of the matrix.
+template <int TYPE> __device__ inline void finish4(float *v, const float *bias, const EpiD &E, const Seed &seed, long long q, long long p, int n, long long cols, int part)
+{
+    typedef typename ElemOf<TYPE>::type T;
+    if (E.mode == EPI_PART) {
+        store_some<NET_F32, 4>(static_cast<float *>(E.out) + part * E.part_stride + q * E.ldo + p, v, n);
+        return;
+    }
+    if (E.mode == EPI_LAYER) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += bias[i];
+        if (E.z) {
+            if (E.bias_f32) store_some<NET_F32, 4>(static_cast<float *>(E.z) + q * E.ldz + p, v, n);
+            else store_some<TYPE, 4>(static_cast<T *>(E.z) + q * E.ldz + p, v, n);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = act_of(v[i], E.act, E.beta);
+        drop<4>(v, (unsigned long long)q * cols + p, E.drop, seed);
+        if (E.r) {
+            const auto r = load_some<TYPE, 4>(static_cast<const T *>(E.r) + q * E.ldr + p, n);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] += widen<TYPE>(r.v[i]);
+        }
+    }
+    store_some<TYPE, 4>(static_cast<T *>(E.out) + q * E.ldo + p, v, n);
+}
+
+// ---------------------------------------------------------------------------------------------------------------- products
+
+// Where chunks of 8 elements lie in an LDS tile, so that the 16 lanes that are served together find theirs in 16 different places of 16 bytes.
+// t along the rows: chunk c of row r; RP rows fill the 256 bytes of all banks.
+template <int BT> __device__ inline int place_row(int r, int c)
+{
+    constexpr int RP = 128 / BT;
+    return r * BT + ((c ^ ((r / RP) & (BT / 8 - 1))) * 8);
+}
+// p along the rows: a transposing read takes 32 bytes from each of four rows t, and its other half-wave's neighbours the next 32.
+template <int B> __device__ inline int place_col(int t, int c)
+{
+    constexpr int RP = B >= 128 ? 1 : 128 / B;
+    const int turn = B >= 64 ? 4 * ((t / RP) & (4 / RP - 1)) : 0;
+    return t * B + ((c ^ turn) * 8);
+}
+
+template <int TYPE> __device__ inline f32x16 mfma(s16x8 a, s16x8 b, f32x16 c)
+{
+    if constexpr (TYPE == NET_F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+// The operand of one matrix instruction: 32 rows from p0, t = 16 step + 8 (lane / 32) + 0 .. 7.
+template <bool COL, int B, int BT> __device__ inline s16x8 operand(const short *tile, int p0, int step, int lane)
+{
+    if constexpr (!COL) {
+        const int r = p0 + (lane & 31);
+        return *reinterpret_cast<const s16x8 *>(tile + place_row<BT>(r, 2 * step + (lane >> 5)));
+    } else {
+        // lane i of 16 hands in 4 elements of row t + i / 4 and gets those of column i
+        const int i = lane & 15, t = 16 * step + 8 * (lane >> 5) + (i >> 2), p = p0 + (lane & 16) + 4 * (i & 3);
+        const short *lo = tile + place_col<B>(t, p >> 3) + (p & 7), *hi = tile + place_col<B>(t + 4, p >> 3) + (p & 7);
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)lo), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)hi);
+        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+}
+
+// Three bf16 parts of fp32 numbers: x = h + m + l to 24 bits and more, each part the rounded rest of those before it.  A rest that is no number
+// (of infinities) gives results that are none either, which k_product computes again.
+__device__ inline void split8(const float *x, s16x8 *part)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const __bf16 h = (__bf16)x[i];
+        const float rest = x[i] - (float)h;
+        const __bf16 m = (__bf16)rest;
+        const __bf16 l = (__bf16)(rest - (float)m);
+        part[0][i] = __builtin_bit_cast(short, h);
+        part[1][i] = __builtin_bit_cast(short, m);
+        part[2][i] = __builtin_bit_cast(short, l);
+    }
+}
+
+// One operand's tile on its way from memory to LDS: B rows (p or q) by BT, in chunks of 8.
+template <int TYPE, bool COL, int B, int BT, int THREADS> struct Stage {
+    typedef typename ElemOf<TYPE>::type T;
+    static constexpr int PLANES = TYPE == NET_F32 ? 3 : 1;
+    static constexpr int ROWS = COL ? BT : B, COLS = COL ? B : BT, PER_ROW = COLS / 8, N = ROWS * PER_ROW / THREADS;
+    static constexpr int LDS = PLANES * B * BT;            // 16-bit elements
+    static_assert(ROWS * PER_ROW % THREADS == 0 && N >= 1, "tile");
+    Packed<TYPE, 8> chunk[N];
+
+    // b0: first row or column p; t0: first t; t1: end of the range of t
+    __device__ inline void load(const MatD &M, long long b0, long long t0, long long t1, int tid)
+    {
+        const T *at = static_cast<const T *>(M.at);
+        const long long r0 = COL ? t0 : b0, c0 = COL ? b0 : t0, rows = COL ? t1 : M.rows, cols = COL ? M.cols : t1;
+        const bool inside = r0 + ROWS <= rows && c0 + COLS <= cols;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int u = tid + i * THREADS;
+            const long long r = r0 + u / PER_ROW, c = c0 + u % PER_ROW * 8;
+            if (inside) {
+                chunk[i] = *reinterpret_cast<const Packed<TYPE, 8> *>(at + r * M.ld + c);
+            } else if (r < rows && c < cols) {
+                const long long left = cols - c;
+                chunk[i] = load_some<TYPE, 8>(at + r * M.ld + c, left < 8 ? (int)left : 8);
+            } else {
+                for (int k = 0; k < 8; ++k) chunk[i].v[k] = T(0);
+            }
+        }
+    }
+
+    __device__ inline void store(short *tile, int tid) const
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int u = tid + i * THREADS, r = u / PER_ROW, c = u % PER_ROW;
+            short *at = tile + (COL ? place_col<B>(r, c) : place_row<BT>(r, c));
+            if constexpr (TYPE == NET_F32) {
+                s16x8 part[3];
+                split8(chunk[i].v, part);
+#pragma unroll
+                for (int k = 0; k < 3; ++k) *reinterpret_cast<s16x8 *>(at + k * B * BT) = part[k];
+            } else {
+                s16x8 v;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = (short)chunk[i].v[k];
+                *reinterpret_cast<s16x8 *>(at) = v;
+            }
+        }
+    }
+};
+
+// Tiles of D in turn: blocks of one XCD (they are dealt round the 8 of them) get neighbouring tiles, whose operands then meet in its L2; among those,
+// stripes of 8 tiles along q.
+struct TilesD { int p, q, parts; };
+__device__ inline void tile_of(const TilesD &N, int block, int &tp, int &tq)
+{
+    const int all = N.p * N.q, even = all / 8 * 8;
+    int i = block < even ? (block & 7) * (all / 8) + (block >> 3) : block;
+    const int stripe = 8 * N.p, s = i / stripe, first = 8 * s, high = N.q - first < 8 ? N.q - first : 8;
+    i -= s * stripe;
+    tq = first + i % high;
+    tp = i / high;
+}
+
+// D = P Q^T and what becomes of it.  BP x BQ results a block, WP x WQ waves; blockIdx.y: the part of the range of t, `t_part` long.
+template <int TYPE, bool PCOL, bool QCOL, int BP, int BQ, int WP, int WQ>
+__global__ __launch_bounds__(64 * WP * WQ) void k_product(MatD P, MatD Q, long long np, long long nq, long long nt, long long t_part, TilesD tiles, EpiD E)
+{
+    constexpr int THREADS = 64 * WP * WQ, BT = TYPE == NET_F32 ? 32 : 64, MT = BP / WP / 32, NT = BQ / WQ / 32, PW = 32 * MT, PITCH = PW + 4;
+    typedef Stage<TYPE, PCOL, BP, BT, THREADS> StageP;
+    typedef Stage<TYPE, QCOL, BQ, BT, THREADS> StageQ;
+    constexpr int BUFFERS = TYPE == NET_F32 ? 1 : 2, TILE = StageP::LDS + StageQ::LDS;      // 16-bit elements
+    constexpr int BYTES = BUFFERS * TILE * 2 > WP * WQ * 32 * PITCH * 4 ? BUFFERS * TILE * 2 : WP * WQ * 32 * PITCH * 4;
+    __shared__ __attribute__((aligned(1024))) char s_mem[BYTES];
+    short *lds = reinterpret_cast<short *>(s_mem);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave % WP, wq = wave / WP;
+    int tp, tq;
+    tile_of(tiles, blockIdx.x, tp, tq);
+    const long long p0 = (long long)tp * BP, q0 = (long long)tq * BQ;
+    const int part = blockIdx.y;
+    const long long t0 = part * t_part, t1 = t0 + t_part < nt ? t0 + t_part : nt;
+
+    f32x16 acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.0f;
+
+    StageP sp;
+    StageQ sq;
+    if (t0 < t1) {
+        sp.load(P, p0, t0, t1, tid);
+        sq.load(Q, q0, t0, t1, tid);
+        sp.store(lds, tid);
+        sq.store(lds + StageP::LDS, tid);
+    }
+    __syncthreads();
+    int buffer = 0;
+    for (long long t = t0; t < t1; t += BT) {
+        const bool more = t + BT < t1;
+        if (more) {
+            sp.load(P, p0, t + BT, t1, tid);
+            sq.load(Q, q0, t + BT, t1, tid);
+        }
+        const short *bp = lds + buffer * TILE, *bq = bp + StageP::LDS;
+#pragma unroll
+        for (int s = 0; s < BT / 16; ++s) {
+            constexpr int PL = StageP::PLANES;
+            s16x8 a[MT][PL], b[NT][PL];
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int k = 0; k < PL; ++k) a[i][k] = operand<PCOL, BP, BT>(bp + k * BP * BT, (wp * MT + i) * 32, s, lane);
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int k = 0; k < PL; ++k) b[j][k] = operand<QCOL, BQ, BT>(bq + k * BQ * BT, (wq * NT + j) * 32, s, lane);
+            if constexpr (PL == 1) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) acc[i][j] = mfma<TYPE>(a[i][0], b[j][0], acc[i][j]);
+            } else {
+                // the six products of parts that reach 2^-16 of the largest, the small ones first
+#pragma unroll
+                for (int u = 0; u < 6; ++u) {
+                    constexpr int PA[6] = {0, 1, 2, 0, 1, 0}, PB[6] = {2, 1, 0, 1, 0, 0};
+#pragma unroll
+                    for (int i = 0; i < MT; ++i)
+#pragma unroll
+                        for (int j = 0; j < NT; ++j) acc[i][j] = mfma<TYPE>(a[i][PA[u]], b[j][PB[u]], acc[i][j]);
+                }
+            }
+        }
+        if (BUFFERS == 1) __syncthreads();
+        if (BUFFERS == 2) buffer ^= 1;
+        if (more) {
+            sp.store(lds + buffer * TILE, tid);
+            sq.store(lds + buffer * TILE + StageP::LDS, tid);
+        }
+        __syncthreads();
+    }
+
+    if constexpr (TYPE == NET_F32) {
+        // a result that is no finite number may be one of the parts' making (of inf - inf, or a part of the largest numbers rounded up): plainly, then
+        const float *x = static_cast<const float *>(P.at), *y = static_cast<const float *>(Q.at);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int k = 0; k < 16; ++k)
+                    if (!(fabsf(acc[i][j][k]) < INFINITY)) {
+                        const long long p = p0 + (wp * MT + i) * 32 + 8 * (k >> 2) + 4 * (lane >> 5) + (k & 3), q = q0 + (wq * NT + j) * 32 + (lane & 31);
+                        float sum = 0.0f;
+                        if (p < np && q < nq)
+                            for (long long t = t0; t < t1; ++t) sum = __builtin_fmaf(x[PCOL ? t * P.ld + p : p * P.ld + t], y[QCOL ? t * Q.ld + q : q * Q.ld + t], sum);
+                        acc[i][j][k] = sum;
+                    }
+    }
+
+    // through LDS, a wave's 32 rows q at a time, so that rows leave in whole lines
+    float *out = reinterpret_cast<float *>(s_mem) + wave * 32 * PITCH;
+    const int col = 4 * (lane % (PW / 4));
+    const long long p = p0 + wp * PW + col;
+    const int n = np - p < 4 ? (int)(np - p) : 4;
+    const Seed seed = seed_of(E.drop);
+    float bias[4];
+    load_bias<TYPE>(bias, E, p, n);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                f32x4 v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+                *reinterpret_cast<f32x4 *>(out + (lane & 31) * PITCH + 32 * i + 8 * g + 4 * (lane >> 5)) = v;
+            }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        if (n > 0) {
+            constexpr int STEP = 64 / (PW / 4);
+#pragma unroll 2
+            for (int r = lane / (PW / 4); r < 32; r += STEP) {
+                const long long q = q0 + (wq * NT + j) * 32 + r;
+                if (q >= nq) break;
+                const f32x4 x = *reinterpret_cast<const f32x4 *>(out + r * PITCH + col);
+                float v[4] = {x[0], x[1], x[2], x[3]};
+                finish4<TYPE>(v, bias, E, seed, q, p, n, np, part);
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+}
+
+// The parts' sums and what becomes of them: a wave adds every 4th part of 256 neighbours p of one row q, the block's first wave those four sums.
+template <int TYPE> __global__ __launch_bounds__(256) void k_parts(const float *__restrict__ part, long long part_stride, long long ldp, int parts, long long np, long long nq, EpiD E)
+{
+    __shared__ float s_sum[3][256];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long long strips = (np + 255) / 256, all = strips * nq;
+    const Seed seed = seed_of(E.drop);
+    for (long long b = blockIdx.x; b < all; b += gridDim.x) {
+        const long long q = b / strips, p = b % strips * 256 + 4 * lane;
+        const int n = np - p < 4 ? (int)(np - p) : 4;
+        f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (n > 0) {
+            const float *at = part + q * ldp + p;              // ldp is a multiple of 4
+#pragma unroll 4
+            for (int i = wave; i < parts; i += 4) sum += *reinterpret_cast<const f32x4 *>(at + i * part_stride);
+        }
+        if (wave) *reinterpret_cast<f32x4 *>(s_sum[wave - 1] + 4 * lane) = sum;
+        __syncthreads();
+        if (wave == 0 && n > 0) {
+            for (int w = 0; w < 3; ++w) sum += *reinterpret_cast<const f32x4 *>(s_sum[w] + 4 * lane);
+            float v[4] = {sum[0], sum[1], sum[2], sum[3]}, bias[4];
+            load_bias<TYPE>(bias, E, p, n);
+            finish4<TYPE>(v, bias, E, seed, q, p, n, np, 0);
+        }
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------- elementwise
+
+// A block's rows: `tx` threads (a power of 2) side by side, each with V neighbours of a row, 256 / tx rows at a time.
+struct RowsD { long long rows, cols; int tx_bits; long long per_block; };
+
+// Y = R + drop(X)
+template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dropout(RowsD N, MatD X, MatD R, void *y, long long ldy, DropD D)
+{
+    typedef typename ElemOf<TYPE>::type T;
+    const int x = threadIdx.x & ((1 << N.tx_bits) - 1), ty = threadIdx.x >> N.tx_bits, rows = 256 >> N.tx_bits;
+    const Seed seed = seed_of(D);
+    const long long first = blockIdx.y * N.per_block, end = first + N.per_block < N.rows ? first + N.per_block : N.rows;
+    for (long long c = (((long long)blockIdx.x << N.tx_bits) + x) * V; c < N.cols; c += ((long long)gridDim.x << N.tx_bits) * V) {
+        const int n = N.cols - c < V ? (int)(N.cols - c) : V;
+#pragma unroll 2
+        for (long long q = first + ty; q < end; q += rows) {
+            const auto a = load_some<TYPE, V>(static_cast<const T *>(X.at) + q * X.ld + c, n);
+            float v[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = widen<TYPE>(a.v[i]);
+            drop<V>(v, (unsigned long long)q * N.cols + c, D, seed);
+            if (R.at) {
+                const auto r = load_some<TYPE, V>(static_cast<const T *>(R.at) + q * R.ld + c, n);
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[i] += widen<TYPE>(r.v[i]);
+            }
+            store_some<TYPE, V>(static_cast<T *>(y) + q * ldy + c, v, n);
+        }
+    }
+}
+
+// dZ = drop(G act'(Z)), and the sums of its columns over a block's rows (either may be NULL)
+template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dz(RowsD N, MatD G, MatD Z, int z_f32, int act, float beta, DropD D, void *dz, long long lddz, float *__restrict__ sums)
+{
+    typedef typename ElemOf<TYPE>::type T;
+    __shared__ float s_sum[256 * V];
+    const int tx = 1 << N.tx_bits, x = threadIdx.x & (tx - 1), ty = threadIdx.x >> N.tx_bits, rows = 256 >> N.tx_bits;
+    const long long c = (((long long)blockIdx.x << N.tx_bits) + x) * V;
+    const int n = N.cols - c < V ? (int)(N.cols - c) : V;
+    const Seed seed = seed_of(D);
+    const long long first = blockIdx.y * N.per_block, end = first + N.per_block < N.rows ? first + N.per_block : N.rows;
+    float sum[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) sum[i] = 0.0f;
+    if (n > 0) {
+#pragma unroll 2
+        for (long long q = first + ty; q < end; q += rows) {
+            const auto g = load_some<TYPE, V>(static_cast<const T *>(G.at) + q * G.ld + c, n);
+            float v[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = widen<TYPE>(g.v[i]);
+            if (act != ACT_NONE) {
+                float z[V];
+                if (z_f32) load_wide<NET_F32, V>(z, static_cast<const float *>(Z.at) + q * Z.ld + c, n);
+                else load_wide<TYPE, V>(z, static_cast<const T *>(Z.at) + q * Z.ld + c, n);
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[i] *= slope_of(z[i], act, beta);
+            }
+            drop<V>(v, (unsigned long long)q * N.cols + c, D, seed);
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum[i] += v[i];
+            if (dz) store_some<TYPE, V>(static_cast<T *>(dz) + q * lddz + c, v, n);
+        }
+    }
+    if (!sums) return;
+#pragma unroll
+    for (int i = 0; i < V; ++i) s_sum[threadIdx.x * V + i] = sum[i];
+    __syncthreads();
+    for (int i = threadIdx.x; i < tx * V; i += 256) {
+        float all = 0.0f;
+        for (int r = 0; r < rows; ++r) all += s_sum[r * tx * V + i];
+        const long long k = ((long long)blockIdx.x << N.tx_bits) * V + i;
+        if (k < N.cols) sums[blockIdx.y * N.cols + k] = all;
+    }
+}
+
+// dbias from the blocks' sums: 64 columns a block, every 4th sum a wave
+template <int TYPE> __global__ __launch_bounds__(256) void k_dbias(const float *__restrict__ sums, int blocks, long long cols, void *out)
+{
+    __shared__ float s_sum[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long long c = blockIdx.x * 64ll + lane;
+    float all = 0.0f;
+    if (c < cols)
+#pragma unroll 4
+        for (int b = wave; b < blocks; b += 4) all += sums[b * cols + c];
+    s_sum[wave][lane] = all;
+    __syncthreads();
+    if (wave == 0 && c < cols) static_cast<typename ElemOf<TYPE>::type *>(out)[c] = narrow<TYPE>((s_sum[0][lane] + s_sum[1][lane]) + (s_sum[2][lane] + s_sum[3][lane]));
+}
+
+}  // namespace fs

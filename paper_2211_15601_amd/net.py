@@ -1,0 +1,241 @@
+"""The layers of the networks on either side of the search (the skinning network, the occupancy network), over the C ABI of
+include/fastsnarf_net.h: matrix products with bias, activation, dropout and residual in one pass, and dropout alone, both with gradients.
+
+    y = linear(x, weight, bias, activation="softplus", beta=100.0)                  # x [..., inputs], weight [outputs, inputs]
+    y = linear(y, weight, bias, residual=y, activation="gelu", dropout=0.1, seed=words)
+    y = dropout(y, 0.1, words)
+
+Tensors are float32, bfloat16 or float16 on one GPU, all of one type but the bias, which may be float32.  Dropout draws its numbers from a counter:
+`seed` is a pair of integers (seed, offset), or an int64 tensor of those two words on the GPU, which is read when the kernels run (a captured graph that
+counts the offset up drops other elements at each replay).  The same words drop the same elements, so every call of a step gets an offset of its own.
+The mask is not stored: the backward pass makes it anew.
+
+Calls run on the stream that is current when they are made, wait for nothing, keep nothing but what autograd saves, and can be captured into graphs of torch.cuda.
+A captured backward pass needs its forward pass in the same capture, and no eager graph of the same leaves alive.  There is no CPU fallback."""
+from __future__ import annotations
+
+import ctypes
+import math
+from typing import Optional, Sequence, Tuple, Union
+
+import torch
+
+from . import binding
+
+_TYPES = {torch.float32: binding.FS_FLOAT_FULL, torch.bfloat16: binding.FS_FLOAT_BRAIN, torch.float16: binding.FS_FLOAT_HALF}
+_ACTS = {"none": binding.FS_ACT_NONE, "relu": binding.FS_ACT_RELU, "gelu": binding.FS_ACT_GELU, "silu": binding.FS_ACT_SILU, "softplus": binding.FS_ACT_SOFTPLUS}
+
+Seed = Union[torch.Tensor, Tuple[int, int]]
+
+
+def _check(what: str, t: torch.Tensor, like: torch.Tensor, types):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{what}: expected a tensor, got {type(t).__name__}")
+    if t.dtype not in types:
+        raise TypeError(f"{what}: {t.dtype} is not supported here, expected {' or '.join(str(k) for k in types)}")
+    if t.device != like.device:
+        raise ValueError(f"{what}: on {t.device}, expected {like.device}")
+    if t.layout != torch.strided:
+        raise ValueError(f"{what}: expected a dense tensor, got {t.layout}")
+
+
+def _check_input(x):
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"x: expected a tensor, got {type(x).__name__}")
+    if x.dtype not in _TYPES:
+        raise TypeError(f"x: {x.dtype} is not supported here, expected {' or '.join(str(k) for k in _TYPES)}")
+    if not x.is_cuda:
+        raise ValueError(f"tensors must be on a GPU, got {x.device}")
+    if x.layout != torch.strided:
+        raise ValueError(f"x: expected a dense tensor, got {x.layout}")
+
+
+def _check_p(what, p):
+    if not 0.0 <= p <= 1.0:
+        raise ValueError(f"{what} must be in 0 .. 1, got {p}")
+
+
+def _check_seed(seed, x):
+    if isinstance(seed, torch.Tensor):
+        _check("seed", seed, x, [torch.int64])
+        if seed.shape != (2,) or not seed.is_contiguous():
+            raise ValueError("seed must hold two words, one after another")
+        if seed.requires_grad:
+            raise ValueError("seed cannot require a gradient")
+    elif not (isinstance(seed, Sequence) and len(seed) == 2 and all(isinstance(v, int) and 0 <= v < 2 ** 64 for v in seed)):
+        raise ValueError("dropout needs a seed: two integers in 0 .. 2^64 - 1, or an int64 tensor of two words on the GPU")
+
+
+def _rows(t: torch.Tensor) -> torch.Tensor:
+    """[rows, columns] with a row's elements one after another: a view where the strides allow one, else a copy."""
+    if t.dim() != 2:
+        t = t.reshape(1, -1) if t.dim() < 2 else t.reshape(math.prod(t.shape[:-1]), t.shape[-1])
+    return t if t.stride(1) == 1 or t.shape[1] <= 1 else t.contiguous()
+
+
+def _at(t: Optional[torch.Tensor]):
+    """Address and row stride."""
+    return (None, 0) if t is None else (t.data_ptr(), t.stride(0))
+
+
+def _drop(p, seed) -> binding.Drop:
+    if p == 0.0:
+        return binding.Drop()
+    if isinstance(seed, torch.Tensor):
+        return binding.Drop(p, 0, 0, seed.data_ptr())
+    return binding.Drop(p, seed[0], seed[1], None)
+
+
+def _call(device, f, *args):
+    """A call on the device's current stream."""
+    if torch._C._cuda_getDevice() != device.index:
+        with torch.cuda.device(device):
+            return _call(device, f, *args)
+    st = f(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    if st != binding.FS_OK:
+        raise binding.FsError(st, binding.load().fs_net_error().decode())
+
+
+def _workspace(layer, backward, device):
+    with torch.cuda.device(device):
+        n = binding.load().fs_linear_bytes(ctypes.byref(layer), backward)
+    if n < 0:
+        raise binding.FsError(binding.FS_E_SHAPE, binding.load().fs_net_error().decode())
+    return (torch.empty(n, dtype=torch.uint8, device=device) if n else None), n
+
+
+def _forward(layer, shape, x, weight, bias, residual, keep_z):
+    """x, residual [rows, ...] and weight as _rows() gives them.  Y (of `shape`: no view, so that a program may change it in place), and Z where it is kept."""
+    L, device = binding.load(), x.device
+    y = torch.empty(shape, dtype=x.dtype, device=device)
+    z = torch.empty(shape, dtype=x.dtype if bias is None else bias.dtype, device=device) if keep_z else None
+    work, n = _workspace(layer, 0, device)
+    _call(device, L.fs_linear_forward, ctypes.byref(layer), *_at(x), *_at(weight), None if bias is None else bias.data_ptr(), *_at(residual), y.data_ptr(), layer.outputs, None if z is None else z.data_ptr(), layer.outputs,
+          None if work is None else work.data_ptr(), n)
+    return y, z
+
+
+def _layer(x, weight, bias, act, beta, p, seed):
+    kind = _TYPES[x.dtype]
+    return binding.Linear(x.shape[0], x.shape[1], weight.shape[0], kind, kind if bias is None else _TYPES[bias.dtype], act, beta, _drop(p, seed))
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, residual, act, beta, p, seed):
+        rows, w, r = _rows(x), _rows(weight), None if residual is None else _rows(residual)
+        b = None if bias is None else bias.contiguous()
+        y, z = _forward(_layer(rows, w, b, act, beta, p, seed), (*x.shape[:-1], weight.shape[0]), rows, w, b, r, act != binding.FS_ACT_NONE)
+        need = ctx.needs_input_grad
+        ctx.how, ctx.shape, ctx.bias_type = (act, beta, p, None if isinstance(seed, torch.Tensor) else seed), x.shape, None if bias is None else bias.dtype
+        ctx.save_for_backward(x if need[1] else None, weight, z, seed if isinstance(seed, torch.Tensor) else None)
+        ctx.set_materialize_grads(False)
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, g):
+        if g is None:
+            return (None,) * 8
+        x, weight, z, words = ctx.saved_tensors
+        act, beta, p, seed = ctx.how
+        need_x, need_w, need_b, need_r = ctx.needs_input_grad[:4]
+        dx = dw = db = None
+        if need_x or need_w or need_b:
+            L, device = binding.load(), g.device
+            G, w = _rows(g), _rows(weight)
+            X = None if x is None else _rows(x)
+            rows, (outputs, inputs), kind = math.prod(ctx.shape[:-1]), w.shape, _TYPES[g.dtype]
+            layer = binding.Linear(rows, inputs, outputs, kind, kind if ctx.bias_type is None else _TYPES[ctx.bias_type], act, beta, _drop(p, seed if words is None else words))
+            dx = torch.empty(ctx.shape, dtype=g.dtype, device=device) if need_x else None
+            dw = torch.empty(outputs, inputs, dtype=g.dtype, device=device) if need_w else None
+            db = torch.empty(outputs, dtype=ctx.bias_type, device=device) if need_b else None
+            work, n = _workspace(layer, 1, device)
+            _call(device, L.fs_linear_backward, ctypes.byref(layer), *_at(G), *_at(X), *_at(w), None if z is None else z.data_ptr(), outputs,
+                  None if dx is None else dx.data_ptr(), inputs, None if dw is None else dw.data_ptr(), inputs, None if db is None else db.data_ptr(), None if work is None else work.data_ptr(), n)
+        return dx, dw, db, g if need_r else None, None, None, None, None
+
+
+def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, activation: str = "none",
+           beta: float = 1.0, dropout: float = 0.0, seed: Optional[Seed] = None) -> torch.Tensor:
+    """residual + drop(act(x weight^T + bias)), [..., outputs], with gradients for x, weight, bias and residual.
+
+      x            [..., inputs], of any strides (rows whose elements do not lie one after another are copied)
+      weight       [outputs, inputs];  bias [outputs], float32 or of the tensors' type;  residual [..., outputs]
+      activation   "none", "relu", "gelu", "silu", or "softplus": ln(1 + e^(beta z)) / beta
+      dropout      the chance of an activation to be dropped (those that are kept are divided by 1 - dropout), of the numbers that `seed` gives"""
+    _check_input(x)
+    if x.dim() < 1:
+        raise ValueError("x needs a dimension")
+    _check("weight", weight, x, [x.dtype])
+    if weight.dim() != 2 or weight.shape[1] != x.shape[-1]:
+        raise ValueError(f"weight: shape {tuple(weight.shape)}, expected [outputs, {x.shape[-1]}]")
+    outputs = weight.shape[0]
+    if bias is not None:
+        _check("bias", bias, x, [x.dtype] if x.dtype == torch.float32 else [x.dtype, torch.float32])
+        if bias.shape != (outputs,):
+            raise ValueError(f"bias: shape {tuple(bias.shape)}, expected ({outputs},)")
+    if residual is not None:
+        _check("residual", residual, x, [x.dtype])
+        if residual.shape[-1:] != (outputs,) or residual.shape[:-1] != x.shape[:-1]:
+            raise ValueError(f"residual: shape {tuple(residual.shape)}, expected {(*x.shape[:-1], outputs)}")
+    if activation not in _ACTS:
+        raise ValueError(f"activation must be one of {', '.join(_ACTS)}, got {activation!r}")
+    act = _ACTS[activation]
+    if act == binding.FS_ACT_SOFTPLUS and not (beta > 0.0 and math.isfinite(beta)):
+        raise ValueError(f"beta must be positive and finite, got {beta}")
+    _check_p("dropout", dropout)
+    if dropout > 0.0:
+        _check_seed(seed, x)
+    else:
+        seed = None
+    if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or bias is not None and bias.requires_grad or residual is not None and residual.requires_grad):
+        return _Linear.apply(x, weight, bias, residual, act, beta, dropout, seed)
+    rows, w = _rows(x), _rows(weight)
+    b = None if bias is None else bias.contiguous()
+    return _forward(_layer(rows, w, b, act, beta, dropout, seed), (*x.shape[:-1], outputs), rows, w, b, None if residual is None else _rows(residual), False)[0]
+
+
+def _dropped(x, residual, p, seed):
+    L, drop = binding.load(), _drop(p, seed)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    x, r = _rows(x), None if residual is None else _rows(residual)
+    _call(x.device, L.fs_dropout, _TYPES[x.dtype], *x.shape, ctypes.byref(drop), *_at(x), *_at(r), y.data_ptr(), x.shape[1])
+    return y
+
+
+class _Dropout(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, p, seed):
+        ctx.how = p, None if isinstance(seed, torch.Tensor) else seed
+        ctx.save_for_backward(seed if isinstance(seed, torch.Tensor) else None)
+        ctx.set_materialize_grads(False)
+        return _dropped(x, residual, p, seed)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, g):
+        if g is None:
+            return None, None, None, None
+        (words,) = ctx.saved_tensors
+        p, seed = ctx.how
+        dx = _dropped(g, None, p, seed if words is None else words) if ctx.needs_input_grad[0] else None
+        return dx, g if ctx.needs_input_grad[1] else None, None, None
+
+
+def dropout(x: torch.Tensor, p: float, seed: Optional[Seed] = None, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """residual + drop(x), with gradients for both: elements of x are dropped with a chance of p, those that are kept divided by 1 - p.  Which
+    ones goes by their place in the tensor's order and by `seed`: linear(..., dropout=p, seed=seed) drops the same."""
+    _check_input(x)
+    _check_p("p", p)
+    if p > 0.0:
+        _check_seed(seed, x)
+    else:
+        seed = None
+    if residual is not None:
+        _check("residual", residual, x, [x.dtype])
+        if residual.shape != x.shape:
+            raise ValueError(f"residual: shape {tuple(residual.shape)}, expected {tuple(x.shape)}")
+    if torch.is_grad_enabled() and (x.requires_grad or residual is not None and residual.requires_grad):
+        return _Dropout.apply(x, residual, p, seed)
+    return _dropped(x, residual, p, seed)

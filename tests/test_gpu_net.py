@@ -1,0 +1,343 @@
+"""The networks' layers on the GPU against their definitions in 64 bits (net_ref.py)."""
+import itertools
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import net_ref as ref
+
+pytestmark = pytest.mark.gpu
+F64 = torch.float64
+SEED = (0x0123456789ABCDEF, 0xFEDCBA9876543210)
+# rows, inputs, outputs: single ones, none, a tile and its neighbours, thin and wide, split ranges
+SIZES = [(1, 1, 1), (0, 8, 8), (5, 0, 7), (3, 7, 0), (64, 64, 64), (65, 63, 66), (129, 65, 131), (3, 1000, 2), (1000, 24, 257), (257, 1000, 24),
+         (2, 9, 700), (16, 2048, 40), (130, 3, 128), (1, 777, 1001), (4100, 20, 36), (31, 129, 33)]
+
+
+@pytest.fixture(scope="module")
+def net(gpu_lib):
+    from paper_2211_15601_amd import net
+    return net
+
+
+def make(rows, inputs, outputs, dtype, seed=0, pad=0, whole=False):
+    """x, weight, bias, residual, g on the GPU; rows `pad` elements further apart than they are long."""
+    gen = torch.Generator().manual_seed(seed)
+
+    def one(m, n, scale):
+        v = torch.randint(-2, 3, (m, n), generator=gen).float() if whole else torch.randn(m, n, generator=gen) * scale
+        wide = torch.full((m, n + pad), math.nan, dtype=dtype, device="cuda")
+        wide[:, :n] = v.to(dtype)
+        return wide[:, :n]
+
+    return (one(rows, inputs, 1.0), one(outputs, inputs, 1.0 / math.sqrt(max(1, inputs))), one(1, outputs, 0.5)[0], one(rows, outputs, 1.0), one(rows, outputs, 1.0))
+
+
+def run(net, x, w, b, r, g, kind, beta, p, seed):
+    leaves = [t.detach().requires_grad_(True) if t is not None else None for t in (x, w, b, r)]
+    y = net.linear(leaves[0], leaves[1], leaves[2], residual=leaves[3], activation=kind, beta=beta, dropout=p, seed=seed)
+    wanted = [t for t in leaves if t is not None]
+    grads = iter(torch.autograd.grad(y, wanted, g))
+    out = {"y": y}
+    for name, t in zip(("dx", "dweight", "dbias", "dresidual"), leaves):
+        if t is not None:
+            out[name] = next(grads)
+    return out
+
+
+def check(out, x, w, b, r, g, kind, beta, p, seed):
+    want = ref.linear(x, w, b, r, g, kind, beta, p, seed)
+    for name, v in want.items():
+        ref.assert_close(name, out[name], v)
+    if r is not None:
+        assert torch.equal(out["dresidual"], g)
+
+
+@pytest.mark.parametrize("dtype", list(ref.TYPES))
+@pytest.mark.parametrize("size", SIZES, ids=str)
+def test_sizes(net, size, dtype):
+    t = make(*size, ref.TYPES[dtype], seed=sum(size))
+    for kind, p in (("none", 0.0), ("gelu", 0.25)):
+        check(run(net, *t, kind, 1.0, p, SEED), *t, kind, 1.0, p, SEED)
+
+
+@pytest.mark.parametrize("dtype", list(ref.TYPES))
+@pytest.mark.parametrize("size", SIZES, ids=str)
+def test_whole_numbers_are_exact(net, size, dtype):
+    """Small whole numbers: every sum is exact in fp32, so results are the definition's, rounded once."""
+    T = ref.TYPES[dtype]
+    x, w, b, r, g = make(*size, T, seed=1 + sum(size), pad=3, whole=True)
+    out = run(net, x, w, b, r, g, "none", 1.0, 0.5, SEED)
+    X, W, B, R, G = (t.cpu().to(F64) for t in (x, w, b, r, g))
+    f = ref.factor(R.shape, 0.5, SEED)
+    dz = G * f
+    for name, want in (("y", (X @ W.T + B) * f + R), ("dx", dz @ W), ("dweight", dz.T @ X), ("dbias", dz.sum(0))):
+        assert torch.equal(out[name].cpu(), want.to(T)), name
+
+
+@pytest.mark.parametrize("dtype", list(ref.TYPES))
+@pytest.mark.parametrize("kind", ref.ACTS)
+@pytest.mark.parametrize("pad", [0, 1, 8])
+def test_activations(net, kind, dtype, pad):
+    T = ref.TYPES[dtype]
+    for beta in ((1.0, 100.0) if kind == "softplus" else (1.0,)):
+        x, w, b, r, g = make(200, 72, 136, T, seed=7, pad=pad)
+        for bias, residual in ((b, r), (None, r), (b.float(), None), (None, None)):
+            for p in (0.0, 0.1):
+                check(run(net, x, w, bias, residual, g, kind, beta, p, SEED), x, w, bias, residual, g, kind, beta, p, SEED)
+
+
+@pytest.mark.parametrize("dtype", list(ref.TYPES))
+@pytest.mark.parametrize("size", [(1500, 1200, 1100), (9000, 130, 140), (300, 5000, 300)], ids=str)
+def test_larger(net, size, dtype):
+    t = make(*size, ref.TYPES[dtype], seed=3)
+    check(run(net, *t, "silu", 1.0, 0.1, SEED), *t, "silu", 1.0, 0.1, SEED)
+
+
+def test_inference_is_the_same(net):
+    for dtype in ref.TYPES.values():
+        x, w, b, r, _ = make(100, 70, 90, dtype)
+        kw = dict(residual=r, activation="gelu", dropout=0.3, seed=SEED)
+        y = net.linear(x, w, b, **kw)
+        assert not y.requires_grad and torch.equal(y, net.linear(x, w.detach().requires_grad_(True), b, **kw))
+        with torch.no_grad():
+            assert torch.equal(y, net.linear(x.detach().requires_grad_(True), w, b, **kw))
+
+
+def test_gradients_against_differences(net):
+    """Central differences of the definition in 64 bits, at the operator's own inputs."""
+    x, w, b, r, g = make(6, 5, 7, torch.float32, seed=11)
+    for kind, beta in (("gelu", 1.0), ("silu", 1.0), ("softplus", 3.0), ("none", 1.0)):
+        out = run(net, x, w, b, r, g, kind, beta, 0.4, SEED)
+        wide = [t.cpu().to(F64) for t in (x, w, b, r)]
+        f, G = ref.factor((6, 7), 0.4, SEED), g.cpu().to(F64)
+        loss = lambda v: float((G * (ref.act(v[0] @ v[1].T + v[2], kind, beta) * f + v[3])).sum())
+        for k, name in enumerate(("dx", "dweight", "dbias", "dresidual")):
+            got = out[name].cpu().flatten()
+            for i in range(wide[k].numel()):
+                h, two = 1e-4, []
+                for sign in (1, -1):
+                    v = [t.clone() for t in wide]
+                    v[k].view(-1)[i] += sign * h
+                    two.append(loss(v))
+                # third derivatives of these sums are below 1e3: h^2 1e3 / 6 < 2e-6; fp32 sums of 7 terms below 10
+                assert abs((two[0] - two[1]) / (2 * h) - float(got[i])) < 2e-5, (kind, name, i)
+
+
+def test_shapes_and_strides(net):
+    T = torch.bfloat16
+    x, w, b, r, g = make(60, 24, 40, T, seed=5)
+    want = net.linear(x, w, b, residual=r, activation="silu")
+    same = lambda y, shape=(60, 40): torch.equal(y.reshape(60, 40), want) and y.shape == shape
+    assert same(net.linear(x.view(3, 4, 5, 24), w, b, residual=r.view(3, 4, 5, 40), activation="silu"), (3, 4, 5, 40))
+    assert same(net.linear(x.t().contiguous().t(), w.t().contiguous().t(), b, residual=r.t().contiguous().t(), activation="silu"))
+    assert same(net.linear(x[:, None].expand(60, 2, 24)[:, 1], w, b, residual=r, activation="silu"))
+    one = net.linear(x[3], w, b, residual=r[3], activation="silu")
+    assert one.shape == (40,) and torch.equal(one, net.linear(x[3:4], w, b, residual=r[3:4], activation="silu")[0])
+    # results are no views: a program may change them
+    y = net.linear(x.detach().requires_grad_(True).view(3, 20, 24), w, b)
+    assert torch.equal(y.mul_(2.0).detach(), net.linear(x, w, b).view(3, 20, 40) * 2)
+    # a row that is broadcast, and a residual that is: their gradients are sums over the rows
+    row, res = x[:1].detach().requires_grad_(True), r[:1].detach().requires_grad_(True)
+    y = net.linear(row.expand(60, 24), w, b, residual=res.expand(60, 40))
+    assert torch.equal(y, net.linear(x[:1].repeat(60, 1), w, b, residual=r[:1].repeat(60, 1)))
+    drow, dres = torch.autograd.grad(y, [row, res], g)
+    full = net.linear(x[:1].repeat(60, 1).requires_grad_(True), w, b)
+    assert torch.equal(dres, g.sum(0, keepdim=True)) and drow.shape == (1, 24)
+    # the same weight twice; a sum as the loss, whose gradient is one number seen 2400 times
+    weight = w.detach()[:24].clone().requires_grad_(True)
+    y = net.linear(net.linear(x, weight, activation="relu"), weight).sum()
+    (d,) = torch.autograd.grad(y, weight)
+    W = weight.detach().double().requires_grad_(True)
+    (D,) = torch.autograd.grad(((x.double() @ W.T).clamp(min=0) @ W.T).sum(), W)
+    assert float((d.double() - D).norm() / D.norm()) < 0.01
+
+
+def test_only_what_is_asked_for(net):
+    x, w, b, r, g = make(70, 33, 50, torch.float32)
+    every = run(net, x, w, b, r, g, "silu", 1.0, 0.2, SEED)
+    for wanted in itertools.product((False, True), repeat=4):
+        if not any(wanted):
+            continue
+        leaves = [t.detach().requires_grad_(n) for t, n in zip((x, w, b, r), wanted)]
+        y = net.linear(leaves[0], leaves[1], leaves[2], residual=leaves[3], activation="silu", dropout=0.2, seed=SEED)
+        grads = torch.autograd.grad(y, [t for t in leaves if t.requires_grad], g)
+        names = [n for n, k in zip(("dx", "dweight", "dbias", "dresidual"), wanted) if k]
+        assert torch.equal(y, every["y"]) and all(torch.equal(d, every[n]) for d, n in zip(grads, names))
+
+
+def test_values_that_are_not_finite(net):
+    """Of a row that holds NaN or infinities, that row's results; of every row, those columns of the weight's gradient."""
+    for dtype in ref.TYPES.values():
+        x, w, b, r, g = make(140, 40, 70, dtype, seed=2)
+        clean = run(net, x, w, b, r, g, "none", 1.0, 0.0, None)
+        bad = x.clone()
+        bad[3, 5], bad[77, 0], bad[100, 39] = math.inf, math.nan, -math.inf
+        out = run(net, bad, w, b, r, g, "none", 1.0, 0.0, None)
+        rows = [i for i in range(140) if i not in (3, 77, 100)]
+        assert torch.equal(out["y"][rows], clean["y"][rows]) and torch.equal(out["dx"], clean["dx"])
+        assert out["y"][77].isnan().all()
+        assert torch.equal(out["y"][3], torch.where(w[:, 5] > 0, math.inf, -math.inf).to(dtype)), dtype
+        assert torch.equal(out["y"][100], torch.where(w[:, 39] > 0, -math.inf, math.inf).to(dtype))
+        cols = [i for i in range(40) if i not in (0, 5, 39)]
+        assert torch.equal(out["dweight"][:, cols], clean["dweight"][:, cols]) and out["dweight"][:, 0].isnan().all() and out["dweight"][:, 5].isinf().all()
+        # dropped elements are 0 whatever they were
+        y = net.linear(bad, w, b, dropout=1.0, seed=SEED)
+        assert torch.equal(y, torch.zeros_like(y))
+    big = torch.full((2, 3), 3.4e38, device="cuda")
+    y = net.linear(big, torch.tensor([[1.0, -1.0, 1.0], [0.0, 0.0, 0.25], [1.0, 1.0, 0.0]], device="cuda"))
+    assert torch.equal(y[0], torch.tensor([3.4e38, 3.4e38 * 0.25, math.inf], device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", list(ref.TYPES))
+@pytest.mark.parametrize("shape", [(1,), (0, 5), (7,), (3, 5, 7), (33, 1), (1, 1000), (257, 777), (64, 2048), ()], ids=str)
+def test_dropout(net, shape, dtype):
+    T = ref.TYPES[dtype]
+    gen = torch.Generator().manual_seed(4)
+    for p, pad in ((0.0, 0), (0.1, 0), (0.5, 3), (0.999, 1), (1.0, 0)):
+        def one():
+            v = torch.randn(shape, generator=gen).to(T).cuda()
+            if pad and v.dim() > 1:
+                v = torch.cat([v, torch.full((*shape[:-1], pad), math.nan, dtype=T, device="cuda")], -1)[..., :shape[-1]]
+            return v
+        x, r, g = one(), one(), one()
+        f = ref.factor(shape, p, SEED)
+        fp32 = (x.cpu().float() * torch.tensor(1.0 / (1.0 - p) if p < 1 else 0.0, dtype=torch.float32)) * (f != 0)
+        for residual in (None, r):
+            leaf, res = x.detach().requires_grad_(True), None if residual is None else r.detach().requires_grad_(True)
+            y = net.dropout(leaf, p, SEED, residual=res)
+            want = fp32 if residual is None else fp32 + r.cpu().float()
+            assert y.shape == tuple(shape) and torch.equal(y.cpu(), want.to(T)), (p, pad)
+            assert torch.equal(net.dropout(x, p, SEED, residual=residual), y)
+            grads = torch.autograd.grad(y, [leaf] if res is None else [leaf, res], g)
+            want = (g.cpu().float() * torch.tensor(1.0 / (1.0 - p) if p < 1 else 0.0, dtype=torch.float32)) * (f != 0)
+            assert torch.equal(grads[0].cpu(), want.to(T))
+            assert res is None or torch.equal(grads[1], g)
+
+
+def test_dropout_and_linear_draw_the_same(net):
+    words = torch.tensor([77, -5], dtype=torch.int64, device="cuda")
+    seed = (77, 2 ** 64 - 5)
+    for n in (64, 77):
+        x, w, b, r, g = make(90, 50, n, torch.float32)
+        y = net.linear(x, w, b, activation="silu", dropout=0.3, seed=words)
+        assert torch.equal(y, net.dropout(net.linear(x, w, b, activation="silu"), 0.3, seed))
+        assert torch.equal(net.linear(x, w, b, residual=r, dropout=0.3, seed=seed), net.linear(x, w, b, residual=r, dropout=0.3, seed=words))
+        assert torch.equal(y == 0, ref.factor((90, n), 0.3, seed).cuda() == 0)
+    share = float((net.dropout(torch.ones(1 << 20, device="cuda"), 0.3, words) == 0).float().mean())
+    assert abs(share - 0.3) < 6 * math.sqrt(0.3 * 0.7 / 2 ** 20)
+    words[1] += 1
+    assert not torch.equal(y, net.linear(x, w, b, activation="silu", dropout=0.3, seed=words))
+
+
+def test_a_seed_that_changes_is_noticed(net):
+    x, w, *_ = make(8, 8, 8, torch.float32)
+    words = torch.tensor([1, 2], device="cuda")
+    for f in (lambda t: net.linear(t, w, dropout=0.5, seed=words), lambda t: net.dropout(t, 0.5, words)):
+        y = f(x.detach().requires_grad_(True))
+        words += 1
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.sum().backward()
+
+
+def test_same_results_from_call_to_call(net):
+    for dtype in ref.TYPES.values():
+        t = make(3000, 200, 100, dtype)
+        a, b = (run(net, *t, "gelu", 1.0, 0.1, SEED) for _ in range(2))
+        assert all(torch.equal(a[k], b[k]) for k in a)
+
+
+def test_other_streams(net):
+    t = make(500, 300, 200, torch.bfloat16)
+    want = run(net, *t, "gelu", 1.0, 0.1, SEED)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    got = []
+    for _ in range(4):
+        for s in streams:
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                got.append(run(net, *t, "gelu", 1.0, 0.1, SEED))
+    torch.cuda.synchronize()
+    assert all(torch.equal(g[k], want[k]) for g in got for k in want)
+
+
+def test_graphs(net):
+    """A captured step of layers and dropout, replayed between eager work, with its words counted up by the graph."""
+    x, w, b, r, g = make(300, 64, 64, torch.bfloat16)
+    words = torch.tensor([5, 0], device="cuda")
+
+    def step(words):
+        leaves = [t.detach().requires_grad_(True) for t in (x, w, b)]
+        h = net.linear(leaves[0], leaves[1], leaves[2], residual=leaves[0], activation="gelu", dropout=0.2, seed=words)
+        y = net.dropout(net.linear(h, leaves[1]), 0.1, words, residual=h)
+        return [y.detach(), *torch.autograd.grad(y, leaves, g)]
+
+    step(words)
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            now = words.clone()
+            out = step(now)
+            words += 3
+        graphs.append((graph, out))
+    for k in range(6):
+        graph, out = graphs[k % 2]
+        before = words.clone()
+        want = step(before)
+        graph.replay()
+        torch.cuda.synchronize() if k % 3 == 0 else None
+        assert torch.equal(words, before + 3)
+        assert all(torch.equal(a, b) for a, b in zip(out, want)), k
+
+
+def test_two_graphs_beside_one_another(net):
+    t = make(700, 500, 90, torch.float32)
+    want = run(net, *t, "silu", 1.0, 0.0, None)
+    pairs = []
+    for _ in range(2):
+        graph, s = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        with torch.cuda.graph(graph, stream=s):
+            out = run(net, *t, "silu", 1.0, 0.0, None)
+        pairs.append((graph, out, s))
+    for _ in range(3):
+        for graph, out, s in pairs:
+            for name in ("y", "dx", "dweight", "dbias"):
+                out[name].detach().zero_()
+        torch.cuda.synchronize()
+        for graph, _, s in pairs:
+            with torch.cuda.stream(s):
+                graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(out[k], want[k]) for _, out, _ in pairs for k in want)
+
+
+def test_more_than_32_bits_of_elements(net):
+    rows, n = (1 << 32) // 56 + 1000, 56
+    x = torch.zeros(rows, 3, dtype=torch.bfloat16, device="cuda")
+    x[-5:] = torch.randn(5, 3).to(torch.bfloat16).cuda()
+    w = torch.randn(n, 3).to(torch.bfloat16).cuda()
+    y = net.linear(x, w, dropout=0.25, seed=SEED)
+    assert y.numel() > 1 << 32
+    f = ref.factor((5, n), 0.25, SEED, first=(rows - 5) * n)
+    want = (x[-5:].cpu().to(F64) @ w.cpu().to(F64).T) * f
+    ref.assert_close("y", y[-5:], (want, ref.rounded(want, torch.bfloat16) * 1.01 + 1e-6))
+    assert int(y[:-5].count_nonzero()) == 0
+    leaf = w.detach().requires_grad_(True)
+    g = y
+    dx, dw = torch.autograd.grad(net.linear(x.requires_grad_(True), leaf), [x, leaf], g)
+    X, G = x.detach()[-5:].cpu().to(F64), g[-5:].cpu().to(F64)
+    want = G.T @ X
+    ref.assert_close("dweight", dw, (want, ref.rounded(want, torch.bfloat16) * 1.01 + 1e-5))
+    ref.assert_close("dx", dx[-5:], (G @ w.cpu().to(F64), ref.rounded(G @ w.cpu().to(F64), torch.bfloat16) * 1.01 + 1e-4))
+    assert int(dx[:-5].count_nonzero()) == 0
+    del dx, dw, x
+    z = net.dropout(g, 0.25, SEED)                     # without gaps: one long row
+    assert torch.equal(z[-5:].cpu(), (g[-5:].cpu().float() * torch.tensor(1 / 0.75) * (f != 0)).to(torch.bfloat16))
+    wide = g.view(-1)[: g.numel() - 56].view(-1, 56)[:, :55]
+    z = net.dropout(wide, 0.25, SEED)                  # rows with gaps
+    f = ref.factor((4, 55), 0.25, SEED, first=(wide.shape[0] - 4) * 55)
+    assert torch.equal(z[-4:].cpu(), (wide[-4:].cpu().float() * torch.tensor(1 / 0.75) * (f != 0)).to(torch.bfloat16))
