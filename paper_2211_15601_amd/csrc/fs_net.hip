@@ -171,8 +171,9 @@ void launch_product(const Plan &p, const MatD &P, const MatD &Q, int64_t np, int
 template <int TYPE>
 void launch_parts(const Plan &p, const float *part, int64_t np, int64_t nq, const EpiD &E, hipStream_t stream)
 {
-    const long long all = (np + 255) / 256 * nq;
-    k_parts<TYPE><<<(unsigned)std::min<long long>(all, 1 << 16), 256, 0, stream>>>(part, p.part_stride, p.ldp, p.parts, np, nq, E);
+    const long long all = (np + 255) / 256 * nq, blocks = p.parts >= 8 ? all : (all + 3) / 4;
+    if (p.parts >= 8) k_parts<TYPE, true><<<(unsigned)std::min<long long>(blocks, 1 << 16), 256, 0, stream>>>(part, p.part_stride, p.ldp, p.parts, np, nq, E);
+    else k_parts<TYPE, false><<<(unsigned)std::min<long long>(blocks, 1 << 16), 256, 0, stream>>>(part, p.part_stride, p.ldp, p.parts, np, nq, E);
 }
 
 enum { NT, NN, TN };                   // forward, dX, dweight
@@ -224,7 +225,7 @@ RowsPlan plan_rows(int type, int64_t rows, int64_t cols, long long blocks)
     return p;
 }
 
-constexpr long long ROW_BLOCKS = 2048;
+constexpr long long ROW_BLOCKS = 2048, DZ_BLOCKS = 1024;
 
 template <int TYPE> void launch_dz(const RowsPlan &p, const MatD &G, const MatD &Z, const fs_linear &l, void *dz, float *sums, hipStream_t stream)
 {
@@ -246,7 +247,7 @@ Backward plan_backward(const fs_linear &l, int cus)
     Backward b;
     b.dx = plan_product(l.type, l.inputs, l.rows, l.outputs, cus);
     b.dw = plan_product(l.type, l.inputs, l.outputs, l.rows, cus);
-    b.dz = plan_rows(l.type, l.rows, l.outputs, ROW_BLOCKS);
+    b.dz = plan_rows(l.type, l.rows, l.outputs, DZ_BLOCKS);
     b.has_dz = l.act != FS_ACT_NONE || l.drop.p > 0.0;
     b.sums = b.has_dz ? up(l.rows * l.outputs * size_of(l.type)) : 0;
     b.part = b.sums + up((int64_t)b.dz.gy * l.outputs * 4);
@@ -318,6 +319,7 @@ fs_status fs_linear_forward(const fs_linear *layer, const void *d_x, int64_t ldx
     E.mode = EPI_LAYER;
     E.act = l.act;
     E.beta = l.beta;
+    E.over_beta = 1.0f / l.beta;
     E.bias = d_bias;
     E.bias_f32 = l.bias_type == FS_FLOAT_FULL;
     E.r = d_r;
@@ -366,9 +368,9 @@ fs_status fs_linear_backward(const fs_linear *layer, const void *d_g, int64_t ld
         else launch_dz<NET_F16>(b.dz, G, Z, l, dz, sums, stream);
         if (sums) {
             const unsigned blocks = (unsigned)((n + 63) / 64);
-            if (l.bias_type == FS_FLOAT_FULL) k_dbias<NET_F32><<<blocks, 256, 0, stream>>>(sums, (int)b.dz.gy, n, d_dbias);
-            else if (l.bias_type == FS_FLOAT_BRAIN) k_dbias<NET_BF16><<<blocks, 256, 0, stream>>>(sums, (int)b.dz.gy, n, d_dbias);
-            else k_dbias<NET_F16><<<blocks, 256, 0, stream>>>(sums, (int)b.dz.gy, n, d_dbias);
+            if (l.bias_type == FS_FLOAT_FULL) k_dbias<NET_F32><<<blocks, 1024, 0, stream>>>(sums, (int)b.dz.gy, n, d_dbias);
+            else if (l.bias_type == FS_FLOAT_BRAIN) k_dbias<NET_BF16><<<blocks, 1024, 0, stream>>>(sums, (int)b.dz.gy, n, d_dbias);
+            else k_dbias<NET_F16><<<blocks, 1024, 0, stream>>>(sums, (int)b.dz.gy, n, d_dbias);
         }
     }
     EpiD E = {};

@@ -150,28 +150,68 @@ template <int N> __device__ inline void drop(float *v, unsigned long long e, con
 
 // ---------------------------------------------------------------------------------------------------------------- activations
 
-__device__ inline float act_of(float z, int act, float beta)
+// The hardware's 2^x, log2 and 1/x are good to a unit of the last place; what is built on them here is off by some units, of e^x |x| more (the rounding of x log2 e).
+// The library's functions take 5 times the instructions, and an epilogue is bound by those: 65536 x 128 softplus took 33 us with them beside 35 for the product.
+__device__ inline float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+__device__ inline float fast_rcp(float x) { return __builtin_amdgcn_rcpf(x); }
+
+// ln(1 + u) of 0 <= u <= 1: with w the rounded 1 + u, ln(w) u / (w - 1); the quotient takes out what rounding changed in w.
+__device__ inline float log_of_one_more(float u)
 {
-    switch (act) {
-    case ACT_RELU: return z < 0.0f ? 0.0f : z;                                     // NaN stays
-    case ACT_GELU: return 0.5f * z * erfcf(z * -0.70710678f);
-    case ACT_SILU: return z / (1.0f + expf(-z));
-    case ACT_SOFTPLUS: return (z < 0.0f ? 0.0f : z) + log1pf(expf(-fabsf(z * beta))) / beta;
-    default: return z;
-    }
+    const float w = 1.0f + u, d = w - 1.0f;
+    return d == 0.0f ? u : __builtin_amdgcn_logf(w) * 0.693147181f * (u * fast_rcp(d));
 }
 
-__device__ inline float slope_of(float z, int act, float beta)
+// Phi(z), and e^(-z^2/2), which it is made from: with u = |z| and t = 1 / (1 + 0.3 u), Phi(-u) = e^(-u^2/2) (t c0 + t^2 c1 + .. + t^10 c9), a polynomial fitted to
+// the least relative error, 1e-7 (4e-7 in fp32 arithmetic).
+__device__ inline float normal_of(float z, float &bell)
+{
+    constexpr float C[10] = {0.119682692f, 0.119680032f, 0.109011605f, 0.0859197751f, 0.068387121f, -0.0155361798f, 0.0995843709f, -0.147240862f, 0.0729390979f, -0.0124276103f};
+    const float t = fast_rcp(__builtin_fmaf(fabsf(z), 0.3f, 1.0f));
+    bell = fast_exp(-0.5f * z * z);
+    float p = C[9];
+#pragma unroll
+    for (int i = 8; i >= 0; --i) p = __builtin_fmaf(p, t, C[i]);
+    p *= t * bell;
+    return z < 0.0f ? p : 1.0f - p;
+}
+
+template <int ACT> __device__ inline float act_of(float z, float beta, float over_beta)
+{
+    if constexpr (ACT == ACT_RELU) return z < 0.0f ? 0.0f : z;                                     // NaN stays
+    else if constexpr (ACT == ACT_GELU) {
+        float bell;
+        return z * normal_of(z, bell);
+    } else if constexpr (ACT == ACT_SILU) return z * fast_rcp(1.0f + fast_exp(-z));
+    else if constexpr (ACT == ACT_SOFTPLUS) return __builtin_fmaf(log_of_one_more(fast_exp(-fabsf(z * beta))), over_beta, z < 0.0f ? 0.0f : z);
+    else return z;
+}
+
+template <int ACT> __device__ inline float slope_of(float z, float beta)
+{
+    if constexpr (ACT == ACT_RELU) return z <= 0.0f ? 0.0f : 1.0f;
+    else if constexpr (ACT == ACT_GELU) {
+        float bell;
+        const float n = normal_of(z, bell);
+        return __builtin_fmaf(z * 0.39894228f, bell, n);
+    } else if constexpr (ACT == ACT_SILU) {
+        const float s = fast_rcp(1.0f + fast_exp(-z));
+        return s * __builtin_fmaf(z, 1.0f - s, 1.0f);
+    } else if constexpr (ACT == ACT_SOFTPLUS) return fast_rcp(1.0f + fast_exp(-z * beta));
+    else return 1.0f;
+}
+
+template <int N> struct Int { static constexpr int value = N; };
+
+// f(Int<act>()), the branch outside of the loops
+template <class F> __device__ inline void with_act(int act, F f)
 {
     switch (act) {
-    case ACT_RELU: return z <= 0.0f ? 0.0f : 1.0f;
-    case ACT_GELU: return __builtin_fmaf(z * 0.39894228f, expf(-0.5f * z * z), 0.5f * erfcf(z * -0.70710678f));
-    case ACT_SILU: {
-        const float s = 1.0f / (1.0f + expf(-z));
-        return s * __builtin_fmaf(z, 1.0f - s, 1.0f);
-    }
-    case ACT_SOFTPLUS: return 1.0f / (1.0f + expf(-z * beta));
-    default: return 1.0f;
+    case ACT_RELU: return f(Int<ACT_RELU>());
+    case ACT_GELU: return f(Int<ACT_GELU>());
+    case ACT_SILU: return f(Int<ACT_SILU>());
+    case ACT_SOFTPLUS: return f(Int<ACT_SOFTPLUS>());
+    default: return f(Int<ACT_NONE>());
     }
 }
 
@@ -183,7 +223,7 @@ enum { EPI_LAYER, EPI_STORE, EPI_PART };
 // into out, `part_stride` floats from part to part.
 struct EpiD {
     int mode, act, bias_f32;
-    float beta;
+    float beta, over_beta;
     const void *bias, *r;
     void *out, *z;
     long long ldr, ldo, ldz, part_stride;
@@ -201,31 +241,36 @@ template <int TYPE> __device__ inline void load_bias(float *b, const EpiD &E, lo
     }
 }
 
-// Four results of row q from p on, of which n (1 .. 4) are in the matrix; cols: of the matrix.
-template <int TYPE> __device__ inline void finish4(float *v, const float *bias, const EpiD &E, const Seed &seed, long long q, long long p, int n, long long cols, int part)
+// Four results of row q from p on, of which n (1 .. 4) are in the matrix; cols: of the matrix; r: their residual.
+template <int TYPE, int ACT> __device__ inline void finish4(float *v, const float *bias, const Packed<TYPE, 4> &r, const EpiD &E, const Seed &seed, long long q, long long p, int n, long long cols)
 {
     typedef typename ElemOf<TYPE>::type T;
-    if (E.mode == EPI_PART) {
-        store_some<NET_F32, 4>(static_cast<float *>(E.out) + part * E.part_stride + q * E.ldo + p, v, n);
-        return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] += bias[i];
+    if (E.z) {
+        if (E.bias_f32) store_some<NET_F32, 4>(static_cast<float *>(E.z) + q * E.ldz + p, v, n);
+        else store_some<TYPE, 4>(static_cast<T *>(E.z) + q * E.ldz + p, v, n);
     }
-    if (E.mode == EPI_LAYER) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] += bias[i];
-        if (E.z) {
-            if (E.bias_f32) store_some<NET_F32, 4>(static_cast<float *>(E.z) + q * E.ldz + p, v, n);
-            else store_some<TYPE, 4>(static_cast<T *>(E.z) + q * E.ldz + p, v, n);
-        }
+    for (int i = 0; i < 4; ++i) v[i] = act_of<ACT>(v[i], E.beta, E.over_beta);
+    drop<4>(v, (unsigned long long)q * cols + p, E.drop, seed);
+    if (E.r)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = act_of(v[i], E.act, E.beta);
-        drop<4>(v, (unsigned long long)q * cols + p, E.drop, seed);
-        if (E.r) {
-            const auto r = load_some<TYPE, 4>(static_cast<const T *>(E.r) + q * E.ldr + p, n);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] += widen<TYPE>(r.v[i]);
-        }
-    }
+        for (int i = 0; i < 4; ++i) v[i] += widen<TYPE>(r.v[i]);
     store_some<TYPE, 4>(static_cast<T *>(E.out) + q * E.ldo + p, v, n);
+}
+
+template <int TYPE> __device__ inline Packed<TYPE, 4> residual4(const EpiD &E, long long q, long long p, int n)
+{
+    Packed<TYPE, 4> r = {};
+    if (E.r) r = load_some<TYPE, 4>(static_cast<const typename ElemOf<TYPE>::type *>(E.r) + q * E.ldr + p, n);
+    return r;
+}
+
+template <int TYPE> __device__ inline void plain4(const float *v, const EpiD &E, long long q, long long p, int n, int part)
+{
+    if (E.mode == EPI_PART) store_some<NET_F32, 4>(static_cast<float *>(E.out) + part * E.part_stride + q * E.ldo + p, v, n);
+    else store_some<TYPE, 4>(static_cast<typename ElemOf<TYPE>::type *>(E.out) + q * E.ldo + p, v, n);
 }
 
 // ---------------------------------------------------------------------------------------------------------------- products
@@ -455,60 +500,88 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_product(MatD P, MatD Q, long l
     const Seed seed = seed_of(E.drop);
     float bias[4];
     load_bias<TYPE>(bias, E, p, n);
-#pragma unroll
+#pragma unroll 1
     for (int j = 0; j < NT; ++j) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int k = 0; k < NT; ++k)           // a register's number is fixed
+            if (k == j)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                f32x4 v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-                *reinterpret_cast<f32x4 *>(out + (lane & 31) * PITCH + 32 * i + 8 * g + 4 * (lane >> 5)) = v;
-            }
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        f32x4 v = {acc[i][k][4 * g], acc[i][k][4 * g + 1], acc[i][k][4 * g + 2], acc[i][k][4 * g + 3]};
+                        *reinterpret_cast<f32x4 *>(out + (lane & 31) * PITCH + 32 * i + 8 * g + 4 * (lane >> 5)) = v;
+                    }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        if (n > 0) {
-            constexpr int STEP = 64 / (PW / 4);
-#pragma unroll 2
-            for (int r = lane / (PW / 4); r < 32; r += STEP) {
-                const long long q = q0 + (wq * NT + j) * 32 + r;
-                if (q >= nq) break;
-                const f32x4 x = *reinterpret_cast<const f32x4 *>(out + r * PITCH + col);
-                float v[4] = {x[0], x[1], x[2], x[3]};
-                finish4<TYPE>(v, bias, E, seed, q, p, n, np, part);
-            }
-        }
+        constexpr int STEP = 64 / (PW / 4), PASSES = 32 / STEP, AHEAD = 4;
+        const long long q1 = q0 + (wq * NT + j) * 32 + lane / (PW / 4);
+        const float *in = out + lane / (PW / 4) * PITCH + col;
+        if (n > 0 && !PCOL && E.mode == EPI_LAYER)
+            with_act(E.act, [&](auto act) {
+#pragma unroll 1
+                for (int r = 0; r < PASSES; r += AHEAD) {
+                    Packed<TYPE, 4> res[AHEAD];
+#pragma unroll
+                    for (int a = 0; a < AHEAD; ++a)
+                        if (q1 + (r + a) * STEP < nq) res[a] = residual4<TYPE>(E, q1 + (r + a) * STEP, p, n);
+#pragma unroll
+                    for (int a = 0; a < AHEAD; ++a)
+                        if (q1 + (r + a) * STEP < nq) {
+                            const f32x4 x = *reinterpret_cast<const f32x4 *>(in + (r + a) * STEP * PITCH);
+                            float v[4] = {x[0], x[1], x[2], x[3]};
+                            finish4<TYPE, decltype(act)::value>(v, bias, res[a], E, seed, q1 + (r + a) * STEP, p, n, np);
+                        }
+                }
+            });
+        else if (n > 0)
+#pragma unroll
+            for (int r = 0; r < PASSES; ++r)
+                if (q1 + r * STEP < nq) {
+                    const f32x4 x = *reinterpret_cast<const f32x4 *>(in + r * STEP * PITCH);
+                    const float v[4] = {x[0], x[1], x[2], x[3]};
+                    plain4<TYPE>(v, E, q1 + r * STEP, p, n, part);
+                }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     }
 }
 
-// The parts' sums and what becomes of them: a wave adds every 4th part of 256 neighbours p of one row q, the block's first wave those four sums.
-template <int TYPE> __global__ __launch_bounds__(256) void k_parts(const float *__restrict__ part, long long part_stride, long long ldp, int parts, long long np, long long nq, EpiD E)
+// The parts' sums and what becomes of them, 256 neighbours p of one row q at a time.  SPLIT: a block's four waves add every fourth part each and the first of
+// them finishes; else each wave has a strip of its own.
+template <int TYPE, bool SPLIT> __global__ __launch_bounds__(256) void k_parts(const float *__restrict__ part, long long part_stride, long long ldp, int parts, long long np, long long nq, EpiD E)
 {
-    __shared__ float s_sum[3][256];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long strips = (np + 255) / 256, all = strips * nq;
+    __shared__ float s_sum[SPLIT ? 3 : 1][256];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = SPLIT ? wave : 0, step = SPLIT ? 4 : 1;
+    const long long strips = (np + 255) / 256, all = strips * nq, each = SPLIT ? 1 : 4;
     const Seed seed = seed_of(E.drop);
-    for (long long b = blockIdx.x; b < all; b += gridDim.x) {
+    for (long long b = blockIdx.x * each + (SPLIT ? 0 : wave); b < all; b += gridDim.x * each) {
         const long long q = b / strips, p = b % strips * 256 + 4 * lane;
         const int n = np - p < 4 ? (int)(np - p) : 4;
         f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        Packed<TYPE, 4> r = {};
         if (n > 0) {
+            if (!SPLIT || wave == 0) r = residual4<TYPE>(E, q, p, n);
             const float *at = part + q * ldp + p;              // ldp is a multiple of 4
-#pragma unroll 4
-            for (int i = wave; i < parts; i += 4) sum += *reinterpret_cast<const f32x4 *>(at + i * part_stride);
+#pragma unroll 8
+            for (int i = first; i < parts; i += step) sum += *reinterpret_cast<const f32x4 *>(at + i * part_stride);
         }
-        if (wave) *reinterpret_cast<f32x4 *>(s_sum[wave - 1] + 4 * lane) = sum;
-        __syncthreads();
-        if (wave == 0 && n > 0) {
-            for (int w = 0; w < 3; ++w) sum += *reinterpret_cast<const f32x4 *>(s_sum[w] + 4 * lane);
+        if constexpr (SPLIT) {
+            if (wave) *reinterpret_cast<f32x4 *>(s_sum[wave - 1] + 4 * lane) = sum;
+            __syncthreads();
+        }
+        if (first == 0 && n > 0) {
+            if constexpr (SPLIT)
+                for (int w = 0; w < 3; ++w) sum += *reinterpret_cast<const f32x4 *>(s_sum[w] + 4 * lane);
             float v[4] = {sum[0], sum[1], sum[2], sum[3]}, bias[4];
-            load_bias<TYPE>(bias, E, p, n);
-            finish4<TYPE>(v, bias, E, seed, q, p, n, np, 0);
+            if (E.mode == EPI_LAYER) {
+                load_bias<TYPE>(bias, E, p, n);
+                with_act(E.act, [&](auto act) { finish4<TYPE, decltype(act)::value>(v, bias, r, E, seed, q, p, n, np); });
+            } else plain4<TYPE>(v, E, q, p, n, 0);
         }
-        __syncthreads();
+        if constexpr (SPLIT) __syncthreads();
     }
 }
 
@@ -556,26 +629,27 @@ template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dz(RowsD N, 
     float sum[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) sum[i] = 0.0f;
-    if (n > 0) {
+    if (n > 0) with_act(act, [&](auto kind) {
+        constexpr int ACT = decltype(kind)::value;
 #pragma unroll 2
         for (long long q = first + ty; q < end; q += rows) {
             const auto g = load_some<TYPE, V>(static_cast<const T *>(G.at) + q * G.ld + c, n);
             float v[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) v[i] = widen<TYPE>(g.v[i]);
-            if (act != ACT_NONE) {
+            if constexpr (ACT != ACT_NONE) {
                 float z[V];
                 if (z_f32) load_wide<NET_F32, V>(z, static_cast<const float *>(Z.at) + q * Z.ld + c, n);
                 else load_wide<TYPE, V>(z, static_cast<const T *>(Z.at) + q * Z.ld + c, n);
 #pragma unroll
-                for (int i = 0; i < V; ++i) v[i] *= slope_of(z[i], act, beta);
+                for (int i = 0; i < V; ++i) v[i] *= slope_of<ACT>(z[i], beta);
             }
             drop<V>(v, (unsigned long long)q * N.cols + c, D, seed);
 #pragma unroll
             for (int i = 0; i < V; ++i) sum[i] += v[i];
             if (dz) store_some<TYPE, V>(static_cast<T *>(dz) + q * lddz + c, v, n);
         }
-    }
+    });
     if (!sums) return;
 #pragma unroll
     for (int i = 0; i < V; ++i) s_sum[threadIdx.x * V + i] = sum[i];
@@ -588,19 +662,22 @@ template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dz(RowsD N, 
     }
 }
 
-// dbias from the blocks' sums: 64 columns a block, every 4th sum a wave
-template <int TYPE> __global__ __launch_bounds__(256) void k_dbias(const float *__restrict__ sums, int blocks, long long cols, void *out)
+// dbias from the blocks' sums: 64 columns a block, every 16th sum a wave
+template <int TYPE> __global__ __launch_bounds__(1024) void k_dbias(const float *__restrict__ sums, int blocks, long long cols, void *out)
 {
-    __shared__ float s_sum[4][64];
+    __shared__ float s_sum[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const long long c = blockIdx.x * 64ll + lane;
     float all = 0.0f;
     if (c < cols)
-#pragma unroll 4
-        for (int b = wave; b < blocks; b += 4) all += sums[b * cols + c];
+#pragma unroll 16
+        for (int b = wave; b < blocks; b += 16) all += sums[b * cols + c];
     s_sum[wave][lane] = all;
     __syncthreads();
-    if (wave == 0 && c < cols) static_cast<typename ElemOf<TYPE>::type *>(out)[c] = narrow<TYPE>((s_sum[0][lane] + s_sum[1][lane]) + (s_sum[2][lane] + s_sum[3][lane]));
+    if (wave == 0 && c < cols) {
+        for (int w = 1; w < 16; ++w) all += s_sum[w][lane];
+        static_cast<typename ElemOf<TYPE>::type *>(out)[c] = narrow<TYPE>(all);
+    }
 }
 
 }  // namespace fs
