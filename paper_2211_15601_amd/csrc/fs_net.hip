@@ -146,11 +146,13 @@ Plan plan_product(int type, int64_t np, int64_t nq, int64_t nt, int cus)
     Plan p = {};
     const long long bt = type == FS_FLOAT_FULL ? 32 : 64;
     auto tiles = [&](int64_t n, int b) { return (long long)((n + b - 1) / b); };
+    auto area = [&](int b) { return tiles(np, b) * tiles(nq, b) * b * b; };
     p.tile = tiles(np, 128) * tiles(nq, 128) >= cus && np > 64 && nq > 64 ? 128 : 64;
+    if (type != FS_FLOAT_FULL && tiles(np, 256) * tiles(nq, 256) >= cus && area(256) <= area(128) / 4 * 5) p.tile = 256;
     p.tiles_p = tiles(np, p.tile);
     p.tiles_q = tiles(nq, p.tile);
     const long long all = std::max(1ll, p.tiles_p * p.tiles_q);
-    const long long wanted = std::min((2ll * cus + all - 1) / all, std::max<long long>(1, nt / 256));
+    const long long wanted = p.tile == 256 ? 1 : std::min((2ll * cus + all - 1) / all, std::max<long long>(1, nt / 256));
     p.t_part = std::max(bt, ((long long)nt + wanted - 1) / wanted);
     p.t_part = (p.t_part + bt - 1) / bt * bt;
     p.parts = (int)std::max<long long>(1, (nt + p.t_part - 1) / p.t_part);
@@ -159,12 +161,26 @@ Plan plan_product(int type, int64_t np, int64_t nq, int64_t nt, int cus)
     return p;
 }
 
+// May k_product_big read this operand?  Whole chunks of 16 bytes, and offsets in a tile that 32 bits hold.
+bool direct_ok(const MatD &M, bool col) { return reinterpret_cast<uintptr_t>(M.at) % 16 == 0 && M.ld % 8 == 0 && M.ld <= 1 << 22 && (!col || M.cols % 8 == 0); }
+
 template <int TYPE, bool PCOL, bool QCOL>
 void launch_product(const Plan &p, const MatD &P, const MatD &Q, int64_t np, int64_t nq, int64_t nt, const EpiD &E, hipStream_t stream)
 {
-    const TilesD tiles = {(int)p.tiles_p, (int)p.tiles_q, p.parts};
-    const dim3 grid((unsigned)(p.tiles_p * p.tiles_q), (unsigned)p.parts);
-    if (p.tile == 128) k_product<TYPE, PCOL, QCOL, 128, 128, 2, 2><<<grid, 256, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
+    long long tiles_p = p.tiles_p, tiles_q = p.tiles_q;
+    if constexpr (TYPE != NET_F32)
+        if (p.tile == 256) {
+            if (direct_ok(P, PCOL) && direct_ok(Q, QCOL)) {
+                const TilesD tiles = {(int)tiles_p, (int)tiles_q};
+                k_product_big<TYPE, PCOL, QCOL, 2, 4><<<dim3((unsigned)(tiles_p * tiles_q), (unsigned)p.parts), 512, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
+                return;
+            }
+            tiles_p = (np + 127) / 128;
+            tiles_q = (nq + 127) / 128;
+        }
+    const TilesD tiles = {(int)tiles_p, (int)tiles_q};
+    const dim3 grid((unsigned)(tiles_p * tiles_q), (unsigned)p.parts);
+    if (p.tile >= 128) k_product<TYPE, PCOL, QCOL, 128, 128, 2, 2><<<grid, 256, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
     else k_product<TYPE, PCOL, QCOL, 64, 64, 2, 2><<<grid, 256, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
 }
 
@@ -255,7 +271,7 @@ Backward plan_backward(const fs_linear &l, int cus)
     return b;
 }
 
-bool too_many(const Plan &p) { return (unsigned __int128)p.tiles_p * p.tiles_q > MAX_TILES; }
+bool too_many(const Plan &p) { return (unsigned __int128)p.tiles_p * p.tiles_q * (p.tile == 256 ? 4 : 1) > MAX_TILES; }
 
 fs_status current_device(const char *what, int *device)
 {

@@ -348,49 +348,126 @@ template <int TYPE, bool COL, int B, int BT, int THREADS> struct Stage {
         for (int i = 0; i < N; ++i) {
             const int u = tid + i * THREADS;
             const long long r = r0 + u / PER_ROW, c = c0 + u % PER_ROW * 8;
-            if (inside) {
-                chunk[i] = *reinterpret_cast<const Packed<TYPE, 8> *>(at + r * M.ld + c);
-            } else if (r < rows && c < cols) {
-                const long long left = cols - c;
-                chunk[i] = load_some<TYPE, 8>(at + r * M.ld + c, left < 8 ? (int)left : 8);
-            } else {
-                for (int k = 0; k < 8; ++k) chunk[i].v[k] = T(0);
-            }
+            if (inside) chunk[i] = *reinterpret_cast<const Packed<TYPE, 8> *>(at + r * M.ld + c);
+            else chunk[i] = guarded(at, M.ld, r, c, rows, cols);
+        }
+    }
+
+    // zeros where the matrix has nothing
+    static __device__ inline Packed<TYPE, 8> guarded(const T *at, long long ld, long long r, long long c, long long rows, long long cols)
+    {
+        Packed<TYPE, 8> x = {};
+        if (r < rows && c < cols) {
+            const long long left = cols - c;
+            x = load_some<TYPE, 8>(at + r * ld + c, left < 8 ? (int)left : 8);
+        }
+        return x;
+    }
+
+    static __device__ inline void put(const Packed<TYPE, 8> &x, short *tile, int u)
+    {
+        const int r = u / PER_ROW, c = u % PER_ROW;
+        short *at = tile + (COL ? place_col<B>(r, c) : place_row<BT>(r, c));
+        if constexpr (TYPE == NET_F32) {
+            s16x8 part[3];
+            split8(x.v, part);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) *reinterpret_cast<s16x8 *>(at + k * B * BT) = part[k];
+        } else {
+            s16x8 v;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = (short)x.v[k];
+            *reinterpret_cast<s16x8 *>(at) = v;
         }
     }
 
     __device__ inline void store(short *tile, int tid) const
     {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int u = tid + i * THREADS, r = u / PER_ROW, c = u % PER_ROW;
-            short *at = tile + (COL ? place_col<B>(r, c) : place_row<BT>(r, c));
-            if constexpr (TYPE == NET_F32) {
-                s16x8 part[3];
-                split8(chunk[i].v, part);
-#pragma unroll
-                for (int k = 0; k < 3; ++k) *reinterpret_cast<s16x8 *>(at + k * B * BT) = part[k];
-            } else {
-                s16x8 v;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = (short)chunk[i].v[k];
-                *reinterpret_cast<s16x8 *>(at) = v;
-            }
-        }
+        for (int i = 0; i < N; ++i) put(chunk[i], tile, tid + i * THREADS);
+    }
+
+    // the whole way at once, chunk by chunk: few registers
+    static __device__ inline void bring(const MatD &M, long long b0, long long t0, long long t1, short *tile, int tid)
+    {
+#pragma unroll 1
+        for (int u = tid; u < ROWS * PER_ROW; u += THREADS)
+            put(guarded(static_cast<const T *>(M.at), M.ld, (COL ? t0 : b0) + u / PER_ROW, (COL ? b0 : t0) + u % PER_ROW * 8, COL ? t1 : M.rows, COL ? M.cols : t1), tile, u);
     }
 };
 
+// The end of a product: a wave's results, MT by NT squares from (p0, q0) on, go through LDS (32 * (32 MT + 4) floats of its own), 32 rows q at a time, so that
+// rows leave in whole lines.
+template <int TYPE, bool LAYER, int MT, int NT>
+__device__ inline void product_end(const f32x16 (&acc)[MT][NT], float *out, int lane, long long p0, long long q0, long long np, long long nq, int part, const EpiD &E)
+{
+    constexpr int PW = 32 * MT, PITCH = PW + 4;
+    const int col = 4 * (lane % (PW / 4));
+    const long long p = p0 + col;
+    const int n = np - p < 4 ? (int)(np - p) : 4;
+    const Seed seed = seed_of(E.drop);
+    float bias[4];
+    load_bias<TYPE>(bias, E, p, n);
+#pragma unroll 1
+    for (int j = 0; j < NT; ++j) {
+#pragma unroll
+        for (int k = 0; k < NT; ++k)           // a register's number is fixed
+            if (k == j)
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        f32x4 v = {acc[i][k][4 * g], acc[i][k][4 * g + 1], acc[i][k][4 * g + 2], acc[i][k][4 * g + 3]};
+                        *reinterpret_cast<f32x4 *>(out + (lane & 31) * PITCH + 32 * i + 8 * g + 4 * (lane >> 5)) = v;
+                    }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        constexpr int STEP = 64 / (PW / 4), PASSES = 32 / STEP, AHEAD = MT == 4 ? 2 : 4;
+        const long long q1 = q0 + j * 32 + lane / (PW / 4);
+        const float *in = out + lane / (PW / 4) * PITCH + col;
+        if (n > 0 && LAYER && E.mode == EPI_LAYER)
+            with_act(E.act, [&](auto act) {
+#pragma unroll 1
+                for (int r = 0; r < PASSES; r += AHEAD) {
+                    Packed<TYPE, 4> res[AHEAD];
+#pragma unroll
+                    for (int a = 0; a < AHEAD; ++a)
+                        if (q1 + (r + a) * STEP < nq) res[a] = residual4<TYPE>(E, q1 + (r + a) * STEP, p, n);
+#pragma unroll
+                    for (int a = 0; a < AHEAD; ++a)
+                        if (q1 + (r + a) * STEP < nq) {
+                            const f32x4 x = *reinterpret_cast<const f32x4 *>(in + (r + a) * STEP * PITCH);
+                            float v[4] = {x[0], x[1], x[2], x[3]};
+                            finish4<TYPE, decltype(act)::value>(v, bias, res[a], E, seed, q1 + (r + a) * STEP, p, n, np);
+                        }
+                }
+            });
+        else if (n > 0)
+#pragma unroll
+            for (int r = 0; r < PASSES; ++r)
+                if (q1 + r * STEP < nq) {
+                    const f32x4 x = *reinterpret_cast<const f32x4 *>(in + r * STEP * PITCH);
+                    const float v[4] = {x[0], x[1], x[2], x[3]};
+                    plain4<TYPE>(v, E, q1 + r * STEP, p, n, part);
+                }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+}
+
 // Tiles of D in turn: blocks of one XCD (they are dealt round the 8 of them) get neighbouring tiles, whose operands then meet in its L2; among those,
 // stripes of 8 tiles along q.
-struct TilesD { int p, q, parts; };
+struct TilesD { int p, q; };
 __device__ inline void tile_of(const TilesD &N, int block, int &tp, int &tq)
 {
     const int all = N.p * N.q, even = all / 8 * 8;
     int i = block < even ? (block & 7) * (all / 8) + (block >> 3) : block;
     const int stripe = 8 * N.p, s = i / stripe, first = 8 * s, high = N.q - first < 8 ? N.q - first : 8;
     i -= s * stripe;
-    tq = first + i % high;
-    tp = i / high;
+    tq = __builtin_amdgcn_readfirstlane(first + i % high);
+    tp = __builtin_amdgcn_readfirstlane(i / high);
 }
 
 // D = P Q^T and what becomes of it.  BP x BQ results a block, WP x WQ waves; blockIdx.y: the part of the range of t, `t_part` long.
@@ -428,48 +505,69 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_product(MatD P, MatD Q, long l
         sq.store(lds + StageP::LDS, tid);
     }
     __syncthreads();
+    if (BUFFERS == 2 && t0 + BT < t1) {
+        sp.load(P, p0, t0 + BT, t1, tid);
+        sq.load(Q, q0, t0 + BT, t1, tid);
+    }
     int buffer = 0;
-    for (long long t = t0; t < t1; t += BT) {
-        const bool more = t + BT < t1;
-        if (more) {
-            sp.load(P, p0, t + BT, t1, tid);
-            sq.load(Q, q0, t + BT, t1, tid);
-        }
+    auto compute = [&](int s) {
         const short *bp = lds + buffer * TILE, *bq = bp + StageP::LDS;
+        constexpr int PL = StageP::PLANES;
+        s16x8 a[MT][PL], b[NT][PL];
 #pragma unroll
-        for (int s = 0; s < BT / 16; ++s) {
-            constexpr int PL = StageP::PLANES;
-            s16x8 a[MT][PL], b[NT][PL];
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int k = 0; k < PL; ++k) a[i][k] = operand<PCOL, BP, BT>(bp + k * BP * BT, (wp * MT + i) * 32, s, lane);
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int k = 0; k < PL; ++k) b[j][k] = operand<QCOL, BQ, BT>(bq + k * BQ * BT, (wq * NT + j) * 32, s, lane);
+        if constexpr (PL == 1) {
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
-                for (int k = 0; k < PL; ++k) a[i][k] = operand<PCOL, BP, BT>(bp + k * BP * BT, (wp * MT + i) * 32, s, lane);
+                for (int j = 0; j < NT; ++j) acc[i][j] = mfma<TYPE>(a[i][0], b[j][0], acc[i][j]);
+        } else {
+            // the six products of parts that reach 2^-16 of the largest, the small ones first
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int k = 0; k < PL; ++k) b[j][k] = operand<QCOL, BQ, BT>(bq + k * BQ * BT, (wq * NT + j) * 32, s, lane);
-            if constexpr (PL == 1) {
+            for (int u = 0; u < 6; ++u) {
+                constexpr int PA[6] = {0, 1, 2, 0, 1, 0}, PB[6] = {2, 1, 0, 1, 0, 0};
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
 #pragma unroll
-                    for (int j = 0; j < NT; ++j) acc[i][j] = mfma<TYPE>(a[i][0], b[j][0], acc[i][j]);
-            } else {
-                // the six products of parts that reach 2^-16 of the largest, the small ones first
-#pragma unroll
-                for (int u = 0; u < 6; ++u) {
-                    constexpr int PA[6] = {0, 1, 2, 0, 1, 0}, PB[6] = {2, 1, 0, 1, 0, 0};
-#pragma unroll
-                    for (int i = 0; i < MT; ++i)
-#pragma unroll
-                        for (int j = 0; j < NT; ++j) acc[i][j] = mfma<TYPE>(a[i][PA[u]], b[j][PB[u]], acc[i][j]);
-                }
+                    for (int j = 0; j < NT; ++j) acc[i][j] = mfma<TYPE>(a[i][PA[u]], b[j][PB[u]], acc[i][j]);
             }
         }
-        if (BUFFERS == 1) __syncthreads();
-        if (BUFFERS == 2) buffer ^= 1;
-        if (more) {
-            sp.store(lds + buffer * TILE, tid);
-            sq.store(lds + buffer * TILE + StageP::LDS, tid);
+    };
+    for (long long t = t0; t < t1; t += BT) {
+        const bool more = t + BT < t1;
+        if constexpr (BUFFERS == 2) {
+            // the next tile's writes to LDS and the loads of the one behind it among the products of this one
+#pragma unroll
+            for (int s = 0; s < BT / 32; ++s) compute(s);
+            if (more) {
+                sp.store(lds + (buffer ^ 1) * TILE, tid);
+                sq.store(lds + (buffer ^ 1) * TILE + StageP::LDS, tid);
+            }
+            if (t + 2 * BT < t1) {
+                sp.load(P, p0, t + 2 * BT, t1, tid);
+                sq.load(Q, q0, t + 2 * BT, t1, tid);
+            }
+#pragma unroll
+            for (int s = BT / 32; s < BT / 16; ++s) compute(s);
+            buffer ^= 1;
+        } else {
+            if (more) {
+                sp.load(P, p0, t + BT, t1, tid);
+                sq.load(Q, q0, t + BT, t1, tid);
+            }
+#pragma unroll
+            for (int s = 0; s < BT / 16; ++s) compute(s);
+            __syncthreads();
+            if (more) {
+                sp.store(lds, tid);
+                sq.store(lds + StageP::LDS, tid);
+            }
         }
         __syncthreads();
     }
@@ -492,61 +590,138 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_product(MatD P, MatD Q, long l
                     }
     }
 
-    // through LDS, a wave's 32 rows q at a time, so that rows leave in whole lines
-    float *out = reinterpret_cast<float *>(s_mem) + wave * 32 * PITCH;
-    const int col = 4 * (lane % (PW / 4));
-    const long long p = p0 + wp * PW + col;
-    const int n = np - p < 4 ? (int)(np - p) : 4;
-    const Seed seed = seed_of(E.drop);
-    float bias[4];
-    load_bias<TYPE>(bias, E, p, n);
-#pragma unroll 1
-    for (int j = 0; j < NT; ++j) {
+    product_end<TYPE, !PCOL, MT, NT>(acc, reinterpret_cast<float *>(s_mem) + wave * 32 * PITCH, lane, p0 + wp * PW, q0 + wq * NT * 32, np, nq, part, E);
+}
+
+// The same for large products of 16-bit matrices whose rows lie at multiples of 16 bytes: 256 x 256 results a block, tiles of 64 t that go from memory to LDS
+// directly while the ones before them are multiplied.
+typedef __attribute__((address_space(1))) const void glob_void;
+typedef __attribute__((address_space(3))) void lds_void;
+
+// Along p or q in memory they are multiples of 8 wide.  One operand's part of that: 256 rows (or, COL, columns) by 64 t are 32 KB, 1 KB an instruction.  A lane's chunk goes where the wave's place and its number say, so it
+// is the chunk that is chosen: the one that place_row() or place_col() keep there.
+template <bool COL, int WAVES> struct Direct {
+    static constexpr int N = 32 / WAVES;
+    unsigned offset[N];                // bytes from the tile's first element
+    const char *at;
+    long long step;
+
+    __device__ inline void begin(const MatD &M, long long b0, long long t0, int wave, int lane)
+    {
+        at = static_cast<const char *>(M.at) + (COL ? t0 * M.ld + b0 : b0 * M.ld + t0) * 2;
+        step = (COL ? 64 * M.ld : 64) * 2;
 #pragma unroll
-        for (int k = 0; k < NT; ++k)           // a register's number is fixed
-            if (k == j)
-#pragma unroll
-                for (int i = 0; i < MT; ++i)
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        f32x4 v = {acc[i][k][4 * g], acc[i][k][4 * g + 1], acc[i][k][4 * g + 2], acc[i][k][4 * g + 3]};
-                        *reinterpret_cast<f32x4 *>(out + (lane & 31) * PITCH + 32 * i + 8 * g + 4 * (lane >> 5)) = v;
-                    }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        constexpr int STEP = 64 / (PW / 4), PASSES = 32 / STEP, AHEAD = 4;
-        const long long q1 = q0 + (wq * NT + j) * 32 + lane / (PW / 4);
-        const float *in = out + lane / (PW / 4) * PITCH + col;
-        if (n > 0 && !PCOL && E.mode == EPI_LAYER)
-            with_act(E.act, [&](auto act) {
-#pragma unroll 1
-                for (int r = 0; r < PASSES; r += AHEAD) {
-                    Packed<TYPE, 4> res[AHEAD];
-#pragma unroll
-                    for (int a = 0; a < AHEAD; ++a)
-                        if (q1 + (r + a) * STEP < nq) res[a] = residual4<TYPE>(E, q1 + (r + a) * STEP, p, n);
-#pragma unroll
-                    for (int a = 0; a < AHEAD; ++a)
-                        if (q1 + (r + a) * STEP < nq) {
-                            const f32x4 x = *reinterpret_cast<const f32x4 *>(in + (r + a) * STEP * PITCH);
-                            float v[4] = {x[0], x[1], x[2], x[3]};
-                            finish4<TYPE, decltype(act)::value>(v, bias, res[a], E, seed, q1 + (r + a) * STEP, p, n, np);
-                        }
-                }
-            });
-        else if (n > 0)
-#pragma unroll
-            for (int r = 0; r < PASSES; ++r)
-                if (q1 + r * STEP < nq) {
-                    const f32x4 x = *reinterpret_cast<const f32x4 *>(in + r * STEP * PITCH);
-                    const float v[4] = {x[0], x[1], x[2], x[3]};
-                    plain4<TYPE>(v, E, q1 + r * STEP, p, n, part);
-                }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        for (int i = 0; i < N; ++i) {
+            const int u = wave * N + i;
+            if constexpr (COL) {
+                const int t = 2 * u + (lane >> 5), slot = lane & 31;
+                long long c = (slot ^ (4 * (t & 3))) * 8;
+                if (b0 + c >= M.cols) c = 0;                               // beyond the matrix: something of it, whose results go nowhere
+                offset[i] = (unsigned)((t * M.ld + c) * 2);
+            } else {
+                const int r = 8 * u + (lane >> 3), slot = lane & 7;
+                long long row = r;
+                if (b0 + row >= M.rows) row = M.rows - 1 - b0;
+                offset[i] = (unsigned)((row * M.ld + (slot ^ ((r >> 1) & 7)) * 8) * 2);
+            }
+        }
     }
+
+    __device__ inline void load(short *tile, int wave)
+    {
+        asm volatile("" : "+s"(at));           // one scalar address and the lanes' 32-bit offsets, not an address of 64 bits for each load
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            __builtin_amdgcn_global_load_lds((glob_void *)(at + offset[i]), (lds_void *)(tile + (wave * N + i) * 512), 16, 0, 0);
+        at += step;
+    }
+};
+
+template <int TYPE, bool PCOL, bool QCOL, int WP, int WQ>
+__global__ __launch_bounds__(64 * WP * WQ) void k_product_big(MatD P, MatD Q, long long np, long long nq, long long nt, long long t_part, TilesD tiles, EpiD E)
+{
+    constexpr int WAVES = WP * WQ, MT = 8 / WP, NT = 8 / WQ, PITCH = 32 * MT + 4, TILE = 256 * 64;
+    __shared__ __attribute__((aligned(1024))) short s_p0[TILE], s_q0[TILE], s_p1[TILE], s_q1[TILE];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave % WP, wq = wave / WP;
+    int tp, tq;
+    tile_of(tiles, blockIdx.x, tp, tq);
+    const long long p0 = (long long)tp * 256, q0 = (long long)tq * 256;
+    const int part = blockIdx.y;
+    const long long t0 = part * t_part, t1 = t0 + t_part < nt ? t0 + t_part : nt;
+    f32x16 acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.0f;
+    Direct<PCOL, WAVES> dp;
+    Direct<QCOL, WAVES> dq;
+    dp.begin(P, p0, t0, wave, lane);
+    dq.begin(Q, q0, t0, wave, lane);
+    auto compute = [&](const short *bp, const short *bq) {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            s16x8 a[MT], b[NT];
+#pragma unroll
+            for (int i = 0; i < MT; ++i) a[i] = operand<PCOL, 256, 64>(bp, (wp * MT + i) * 32, s, lane);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) b[j] = operand<QCOL, 256, 64>(bq, (wq * NT + j) * 32, s, lane);
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = mfma<TYPE>(a[i], b[j], acc[i][j]);
+        }
+        // the next step's reads among this one's products
+        constexpr int READS = MT * (PCOL ? 2 : 1) + NT * (QCOL ? 2 : 1), MFMAS = MT * NT, EACH = (READS + MFMAS - 1) / MFMAS;
+        __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+#pragma unroll
+        for (int s = 0; s < 3; ++s) {
+#pragma unroll
+            for (int i = 0; i < MFMAS; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
+            }
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, MFMAS, 0);
+    };
+    auto arrived = [&] {
+        __builtin_amdgcn_s_waitcnt(0x0F70);            // every load of this wave
+        __syncthreads();
+    };
+    const int whole = (int)((t1 - t0) / 64);
+    if (whole > 0) {
+        dp.load(s_p0, wave);
+        dq.load(s_q0, wave);
+        arrived();
+        for (int k = 0;;) {
+            if (k + 1 < whole) {
+                dp.load(s_p1, wave);
+                dq.load(s_q1, wave);
+            }
+            compute(s_p0, s_q0);
+            if (++k == whole) break;
+            arrived();
+            if (k + 1 < whole) {
+                dp.load(s_p0, wave);
+                dq.load(s_q0, wave);
+            }
+            compute(s_p1, s_q1);
+            if (++k == whole) break;
+            arrived();
+        }
+        __syncthreads();
+    }
+    if (t0 + whole * 64ll < t1) {                      // what is left of t
+        Stage<TYPE, PCOL, 256, 64, 64 * WAVES>::bring(P, p0, t0 + whole * 64ll, t1, s_p0, tid);
+        Stage<TYPE, QCOL, 256, 64, 64 * WAVES>::bring(Q, q0, t0 + whole * 64ll, t1, s_q0, tid);
+        __syncthreads();
+        compute(s_p0, s_q0);
+        __syncthreads();
+    }
+    // 67.6 KB for 4 waves of 32 x 132 floats, 69.6 KB for 8 of 32 x 68 or 132
+    product_end<TYPE, !PCOL, MT, NT>(acc, reinterpret_cast<float *>(wave < WAVES / 2 ? (wave < WAVES / 4 ? s_p0 : s_q0) : (wave < 3 * WAVES / 4 ? s_p1 : s_q1)) + wave % (WAVES / 4) * 32 * PITCH,
+                                     lane, p0 + wp * MT * 32, q0 + wq * NT * 32, np, nq, part, E);
 }
 
 // The parts' sums and what becomes of them, 256 neighbours p of one row q at a time.  SPLIT: a block's four waves add every fourth part each and the first of
