@@ -172,7 +172,7 @@ void launch_product(const Plan &p, const MatD &P, const MatD &Q, int64_t np, int
         if (p.tile == 256) {
             if (direct_ok(P, PCOL) && direct_ok(Q, QCOL)) {
                 const TilesD tiles = {(int)tiles_p, (int)tiles_q};
-                k_product_big<TYPE, PCOL, QCOL, 2, 4><<<dim3((unsigned)(tiles_p * tiles_q), (unsigned)p.parts), 512, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
+                k_product_big<TYPE, PCOL, QCOL><<<dim3((unsigned)(tiles_p * tiles_q), (unsigned)p.parts), 512, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
                 return;
             }
             tiles_p = (np + 127) / 128;

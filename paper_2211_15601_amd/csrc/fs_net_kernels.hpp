@@ -53,16 +53,60 @@ template <int TYPE> __device__ inline typename ElemOf<TYPE>::type narrow(float v
     else return __builtin_bit_cast(unsigned short, (_Float16)v);
 }
 
-// N elements in memory, at any address that is a multiple of one: the vector instructions take those.
-template <int TYPE, int N> struct __attribute__((packed, aligned(TYPE == NET_F32 ? 4 : 2))) Packed { typename ElemOf<TYPE>::type v[N]; };
+// N elements (a multiple of 16 bytes, or 8), as words.  In memory they lie at any address that is a multiple of one: the vector instructions take those.
+template <int TYPE, int N> struct Packed {
+    static constexpr int SIZE = TYPE == NET_F32 ? 4 : 2, WORDS = N * SIZE / 4;
+    unsigned w[WORDS];
+    typedef typename ElemOf<TYPE>::type T;
+
+    __device__ inline T at(int i) const
+    {
+        if constexpr (TYPE == NET_F32) return __uint_as_float(w[i]);
+        else return (T)(w[i / 2] >> (i & 1) * 16);
+    }
+    __device__ inline float wide(int i) const
+    {
+        if constexpr (TYPE == NET_BF16) return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+        else return widen<TYPE>(at(i));
+    }
+};
+
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+template <int SIZE> struct Loose;      // vectors at any address that is a multiple of SIZE
+template <> struct Loose<2> { typedef u32x2 two __attribute__((aligned(2))); typedef u32x4 four __attribute__((aligned(2))); };
+template <> struct Loose<4> { typedef u32x2 two __attribute__((aligned(4))); typedef u32x4 four __attribute__((aligned(4))); };
+
+template <int TYPE, int N> __device__ inline Packed<TYPE, N> load_all(const typename ElemOf<TYPE>::type *at)
+{
+    typedef Packed<TYPE, N> R;
+    R r;
+    if constexpr (R::WORDS == 2) {
+        const u32x2 v = *reinterpret_cast<const typename Loose<R::SIZE>::two *>(at);
+        r.w[0] = v.x; r.w[1] = v.y;
+    } else {
+#pragma unroll
+        for (int k = 0; k < R::WORDS; k += 4) {
+            const u32x4 v = *reinterpret_cast<const typename Loose<R::SIZE>::four *>(at + k * 4 / R::SIZE);
+            r.w[k] = v.x; r.w[k + 1] = v.y; r.w[k + 2] = v.z; r.w[k + 3] = v.w;
+        }
+    }
+    return r;
+}
 
 // The first `n` (1 .. N) of N elements, zeros behind them.
 template <int TYPE, int N> __device__ inline Packed<TYPE, N> load_some(const typename ElemOf<TYPE>::type *at, int n)
 {
+    if (n >= N) return load_all<TYPE, N>(at);
     Packed<TYPE, N> r;
-    if (n >= N) return *reinterpret_cast<const Packed<TYPE, N> *>(at);
 #pragma unroll
-    for (int i = 0; i < N; ++i) r.v[i] = i < n ? at[i] : typename ElemOf<TYPE>::type(0);
+    for (int k = 0; k < r.WORDS; ++k) {
+        if constexpr (TYPE == NET_F32) r.w[k] = k < n ? __float_as_uint(at[k]) : 0u;
+        else {
+            const unsigned lo = 2 * k < n ? at[2 * k] : 0u, hi = 2 * k + 1 < n ? at[2 * k + 1] : 0u;
+            r.w[k] = lo | hi << 16;
+        }
+    }
     return r;
 }
 
@@ -70,21 +114,28 @@ template <int TYPE, int N> __device__ inline void load_wide(float *v, const type
 {
     const auto x = load_some<TYPE, N>(at, n);
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = widen<TYPE>(x.v[i]);
+    for (int i = 0; i < N; ++i) v[i] = x.wide(i);
 }
 
 template <int TYPE, int N> __device__ inline void store_some(typename ElemOf<TYPE>::type *at, const float *v, int n)
 {
-    Packed<TYPE, N> r;
+    typedef Packed<TYPE, N> R;
+    if (n < N) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) r.v[i] = narrow<TYPE>(v[i]);
-    if (n >= N) {
-        *reinterpret_cast<Packed<TYPE, N> *>(at) = r;
+        for (int i = 0; i < N; ++i)
+            if (i < n) at[i] = narrow<TYPE>(v[i]);
         return;
     }
+    unsigned w[R::WORDS];
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-        if (i < n) at[i] = r.v[i];
+    for (int k = 0; k < R::WORDS; ++k) {
+        if constexpr (TYPE == NET_F32) w[k] = __float_as_uint(v[k]);
+        else w[k] = (unsigned)narrow<TYPE>(v[2 * k]) | (unsigned)narrow<TYPE>(v[2 * k + 1]) << 16;
+    }
+    if constexpr (R::WORDS == 2) *reinterpret_cast<typename Loose<R::SIZE>::two *>(at) = u32x2{w[0], w[1]};
+    else
+#pragma unroll
+        for (int k = 0; k < R::WORDS; k += 4) *reinterpret_cast<typename Loose<R::SIZE>::four *>(at + k * 4 / R::SIZE) = u32x4{w[k], w[k + 1], w[k + 2], w[k + 3]};
 }
 
 // ---------------------------------------------------------------------------------------------------------------- dropout
@@ -256,7 +307,7 @@ template <int TYPE, int ACT> __device__ inline void finish4(float *v, const floa
     drop<4>(v, (unsigned long long)q * cols + p, E.drop, seed);
     if (E.r)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] += widen<TYPE>(r.v[i]);
+        for (int i = 0; i < 4; ++i) v[i] += r.wide(i);
     store_some<TYPE, 4>(static_cast<T *>(E.out) + q * E.ldo + p, v, n);
 }
 
@@ -315,12 +366,12 @@ template <bool COL, int B, int BT> __device__ inline s16x8 operand(const short *
 
 // Three bf16 parts of fp32 numbers: x = h + m + l to 24 bits and more, each part the rounded rest of those before it.  A rest that is no number
 // (of infinities) gives results that are none either, which k_product computes again.
-__device__ inline void split8(const float *x, s16x8 *part)
+__device__ inline void split8(const Packed<NET_F32, 8> &x, s16x8 *part)
 {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const __bf16 h = (__bf16)x[i];
-        const float rest = x[i] - (float)h;
+        const __bf16 h = (__bf16)x.wide(i);
+        const float rest = x.wide(i) - (float)h;
         const __bf16 m = (__bf16)rest;
         const __bf16 l = (__bf16)(rest - (float)m);
         part[0][i] = __builtin_bit_cast(short, h);
@@ -348,7 +399,7 @@ template <int TYPE, bool COL, int B, int BT, int THREADS> struct Stage {
         for (int i = 0; i < N; ++i) {
             const int u = tid + i * THREADS;
             const long long r = r0 + u / PER_ROW, c = c0 + u % PER_ROW * 8;
-            if (inside) chunk[i] = *reinterpret_cast<const Packed<TYPE, 8> *>(at + r * M.ld + c);
+            if (inside) chunk[i] = load_all<TYPE, 8>(at + r * M.ld + c);
             else chunk[i] = guarded(at, M.ld, r, c, rows, cols);
         }
     }
@@ -370,14 +421,11 @@ template <int TYPE, bool COL, int B, int BT, int THREADS> struct Stage {
         short *at = tile + (COL ? place_col<B>(r, c) : place_row<BT>(r, c));
         if constexpr (TYPE == NET_F32) {
             s16x8 part[3];
-            split8(x.v, part);
+            split8(x, part);
 #pragma unroll
             for (int k = 0; k < 3; ++k) *reinterpret_cast<s16x8 *>(at + k * B * BT) = part[k];
         } else {
-            s16x8 v;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = (short)x.v[k];
-            *reinterpret_cast<s16x8 *>(at) = v;
+            *reinterpret_cast<u32x4 *>(at) = u32x4{x.w[0], x.w[1], x.w[2], x.w[3]};
         }
     }
 
@@ -396,37 +444,40 @@ template <int TYPE, bool COL, int B, int BT, int THREADS> struct Stage {
     }
 };
 
-// The end of a product: a wave's results, MT by NT squares from (p0, q0) on, go through LDS (32 * (32 MT + 4) floats of its own), 32 rows q at a time, so that
-// rows leave in whole lines.
+// The end of a product: a wave's results, MT by NT squares from (p0, q0) on, go through LDS (end_floats(MT) of its own), 32 rows q and up to 64 p at a time,
+// so that rows leave in whole lines.
+constexpr __host__ __device__ int end_floats(int mt) { return 32 * ((mt > 1 ? 64 : 32) + 4); }
+
 template <int TYPE, bool LAYER, int MT, int NT>
 __device__ inline void product_end(const f32x16 (&acc)[MT][NT], float *out, int lane, long long p0, long long q0, long long np, long long nq, int part, const EpiD &E)
 {
-    constexpr int PW = 32 * MT, PITCH = PW + 4;
+    constexpr int MG = MT > 1 ? 2 : 1, PW = 32 * MG, PITCH = PW + 4;
+    static_assert(MT % MG == 0, "squares");
     const int col = 4 * (lane % (PW / 4));
-    const long long p = p0 + col;
-    const int n = np - p < 4 ? (int)(np - p) : 4;
     const Seed seed = seed_of(E.drop);
-    float bias[4];
-    load_bias<TYPE>(bias, E, p, n);
 #pragma unroll 1
-    for (int j = 0; j < NT; ++j) {
+    for (int h = 0; h < NT * (MT / MG); ++h) {
 #pragma unroll
-        for (int k = 0; k < NT; ++k)           // a register's number is fixed
-            if (k == j)
+        for (int k = 0; k < NT * (MT / MG); ++k)           // a register's number is fixed
+            if (k == h)
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
+                for (int i = 0; i < MG; ++i)
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
-                        f32x4 v = {acc[i][k][4 * g], acc[i][k][4 * g + 1], acc[i][k][4 * g + 2], acc[i][k][4 * g + 3]};
+                        const f32x16 &x = acc[k / NT * MG + i][k % NT];
+                        f32x4 v = {x[4 * g], x[4 * g + 1], x[4 * g + 2], x[4 * g + 3]};
                         *reinterpret_cast<f32x4 *>(out + (lane & 31) * PITCH + 32 * i + 8 * g + 4 * (lane >> 5)) = v;
                     }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        constexpr int STEP = 64 / (PW / 4), PASSES = 32 / STEP, AHEAD = MT == 4 ? 2 : 4;
-        const long long q1 = q0 + j * 32 + lane / (PW / 4);
+        constexpr int STEP = 64 / (PW / 4), PASSES = 32 / STEP, AHEAD = 4;
+        const long long p = p0 + h / NT * PW + col, q1 = q0 + h % NT * 32 + lane / (PW / 4);
+        const int n = np - p < 4 ? (int)(np - p) : 4;
         const float *in = out + lane / (PW / 4) * PITCH + col;
-        if (n > 0 && LAYER && E.mode == EPI_LAYER)
+        if (n > 0 && LAYER && E.mode == EPI_LAYER) {
+            float bias[4];
+            load_bias<TYPE>(bias, E, p, n);
             with_act(E.act, [&](auto act) {
 #pragma unroll 1
                 for (int r = 0; r < PASSES; r += AHEAD) {
@@ -443,7 +494,7 @@ __device__ inline void product_end(const f32x16 (&acc)[MT][NT], float *out, int 
                         }
                 }
             });
-        else if (n > 0)
+        } else if (n > 0)
 #pragma unroll
             for (int r = 0; r < PASSES; ++r)
                 if (q1 + r * STEP < nq) {
@@ -474,11 +525,11 @@ __device__ inline void tile_of(const TilesD &N, int block, int &tp, int &tq)
 template <int TYPE, bool PCOL, bool QCOL, int BP, int BQ, int WP, int WQ>
 __global__ __launch_bounds__(64 * WP * WQ) void k_product(MatD P, MatD Q, long long np, long long nq, long long nt, long long t_part, TilesD tiles, EpiD E)
 {
-    constexpr int THREADS = 64 * WP * WQ, BT = TYPE == NET_F32 ? 32 : 64, MT = BP / WP / 32, NT = BQ / WQ / 32, PW = 32 * MT, PITCH = PW + 4;
+    constexpr int THREADS = 64 * WP * WQ, BT = TYPE == NET_F32 ? 32 : 64, MT = BP / WP / 32, NT = BQ / WQ / 32;
     typedef Stage<TYPE, PCOL, BP, BT, THREADS> StageP;
     typedef Stage<TYPE, QCOL, BQ, BT, THREADS> StageQ;
     constexpr int BUFFERS = TYPE == NET_F32 ? 1 : 2, TILE = StageP::LDS + StageQ::LDS;      // 16-bit elements
-    constexpr int BYTES = BUFFERS * TILE * 2 > WP * WQ * 32 * PITCH * 4 ? BUFFERS * TILE * 2 : WP * WQ * 32 * PITCH * 4;
+    constexpr int END = WP * WQ * end_floats(MT) * 4, BYTES = BUFFERS * TILE * 2 > END ? BUFFERS * TILE * 2 : END;
     __shared__ __attribute__((aligned(1024))) char s_mem[BYTES];
     short *lds = reinterpret_cast<short *>(s_mem);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave % WP, wq = wave / WP;
@@ -590,58 +641,60 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_product(MatD P, MatD Q, long l
                     }
     }
 
-    product_end<TYPE, !PCOL, MT, NT>(acc, reinterpret_cast<float *>(s_mem) + wave * 32 * PITCH, lane, p0 + wp * PW, q0 + wq * NT * 32, np, nq, part, E);
+    product_end<TYPE, !PCOL, MT, NT>(acc, reinterpret_cast<float *>(s_mem) + wave * end_floats(MT), lane, p0 + wp * MT * 32, q0 + wq * NT * 32, np, nq, part, E);
 }
 
-// The same for large products of 16-bit matrices whose rows lie at multiples of 16 bytes: 256 x 256 results a block, tiles of 64 t that go from memory to LDS
-// directly while the ones before them are multiplied.
+// The same for large products of 16-bit matrices whose rows lie at multiples of 16 bytes (and are, along p or q, a multiple of 8 long): 256 x 256 results a
+// block of 8 waves.  Tiles of 32 t go from memory to LDS directly, into the four buffers in turn, three tiles ahead of the one that is multiplied: with one
+// tile of 64 ahead a third of the time went by in waiting for it.
 typedef __attribute__((address_space(1))) const void glob_void;
 typedef __attribute__((address_space(3))) void lds_void;
 
-// Along p or q in memory they are multiples of 8 wide.  One operand's part of that: 256 rows (or, COL, columns) by 64 t are 32 KB, 1 KB an instruction.  A lane's chunk goes where the wave's place and its number say, so it
-// is the chunk that is chosen: the one that place_row() or place_col() keep there.
-template <bool COL, int WAVES> struct Direct {
-    static constexpr int N = 32 / WAVES;
-    unsigned offset[N];                // bytes from the tile's first element
+// One operand's part of that: 256 rows (or, COL, columns) by 32 t are 16 KB, 1 KB an instruction, two instructions a wave.  A lane's chunk goes where the wave's place
+// and its number say, so it is the chunk that is chosen: the one that place_row() or place_col() keep there.
+template <bool COL> struct Direct {
+    unsigned offset[2];                // bytes from the tile's first element
     const char *at;
     long long step;
 
     __device__ inline void begin(const MatD &M, long long b0, long long t0, int wave, int lane)
     {
         at = static_cast<const char *>(M.at) + (COL ? t0 * M.ld + b0 : b0 * M.ld + t0) * 2;
-        step = (COL ? 64 * M.ld : 64) * 2;
+        step = (COL ? 32 * M.ld : 32) * 2;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int u = wave * N + i;
+        for (int i = 0; i < 2; ++i) {
+            const int u = wave * 2 + i;
             if constexpr (COL) {
                 const int t = 2 * u + (lane >> 5), slot = lane & 31;
                 long long c = (slot ^ (4 * (t & 3))) * 8;
                 if (b0 + c >= M.cols) c = 0;                               // beyond the matrix: something of it, whose results go nowhere
                 offset[i] = (unsigned)((t * M.ld + c) * 2);
             } else {
-                const int r = 8 * u + (lane >> 3), slot = lane & 7;
+                const int r = 16 * u + (lane >> 2), slot = lane & 3;
                 long long row = r;
                 if (b0 + row >= M.rows) row = M.rows - 1 - b0;
-                offset[i] = (unsigned)((row * M.ld + (slot ^ ((r >> 1) & 7)) * 8) * 2);
+                offset[i] = (unsigned)((row * M.ld + (slot ^ ((r >> 2) & 3)) * 8) * 2);
             }
         }
     }
 
-    __device__ inline void load(short *tile, int wave)
+    __device__ inline void load(short *tile, int wave, bool more)
     {
         asm volatile("" : "+s"(at));           // one scalar address and the lanes' 32-bit offsets, not an address of 64 bits for each load
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            __builtin_amdgcn_global_load_lds((glob_void *)(at + offset[i]), (lds_void *)(tile + (wave * N + i) * 512), 16, 0, 0);
-        at += step;
+        for (int i = 0; i < 2; ++i)
+            __builtin_amdgcn_global_load_lds((glob_void *)(at + offset[i]), (lds_void *)(tile + (wave * 2 + i) * 512), 16, 0, 0);
+        at += more ? step : 0;
     }
 };
 
-template <int TYPE, bool PCOL, bool QCOL, int WP, int WQ>
-__global__ __launch_bounds__(64 * WP * WQ) void k_product_big(MatD P, MatD Q, long long np, long long nq, long long nt, long long t_part, TilesD tiles, EpiD E)
+template <int TYPE, bool PCOL, bool QCOL>
+__global__ __launch_bounds__(512) void k_product_big(MatD P, MatD Q, long long np, long long nq, long long nt, long long t_part, TilesD tiles, EpiD E)
 {
-    constexpr int WAVES = WP * WQ, MT = 8 / WP, NT = 8 / WQ, PITCH = 32 * MT + 4, TILE = 256 * 64;
-    __shared__ __attribute__((aligned(1024))) short s_p0[TILE], s_q0[TILE], s_p1[TILE], s_q1[TILE];
+    constexpr int WP = 2, WAVES = 8, MT = 4, NT = 2, TILE = 256 * 32;
+    static_assert(end_floats(MT) * 4 <= TILE * 2, "a wave's results go through a buffer");
+    // arrays of their own, by which the compiler sees that reads of one buffer need not wait for loads into another
+    __shared__ __attribute__((aligned(1024))) short s_0[2 * TILE], s_1[2 * TILE], s_2[2 * TILE], s_3[2 * TILE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave % WP, wq = wave / WP;
     int tp, tq;
     tile_of(tiles, blockIdx.x, tp, tq);
@@ -655,73 +708,81 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_product_big(MatD P, MatD Q, lo
         for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.0f;
-    Direct<PCOL, WAVES> dp;
-    Direct<QCOL, WAVES> dq;
-    dp.begin(P, p0, t0, wave, lane);
-    dq.begin(Q, q0, t0, wave, lane);
-    auto compute = [&](const short *bp, const short *bq) {
+    auto compute = [&](const short *bp) {
+        const short *bq = bp + TILE;
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
+        for (int s = 0; s < 2; ++s) {
             s16x8 a[MT], b[NT];
 #pragma unroll
-            for (int i = 0; i < MT; ++i) a[i] = operand<PCOL, 256, 64>(bp, (wp * MT + i) * 32, s, lane);
+            for (int i = 0; i < MT; ++i) a[i] = operand<PCOL, 256, 32>(bp, (wp * MT + i) * 32, s, lane);
 #pragma unroll
-            for (int j = 0; j < NT; ++j) b[j] = operand<QCOL, 256, 64>(bq, (wq * NT + j) * 32, s, lane);
+            for (int j = 0; j < NT; ++j) b[j] = operand<QCOL, 256, 32>(bq, (wq * NT + j) * 32, s, lane);
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
                 for (int j = 0; j < NT; ++j) acc[i][j] = mfma<TYPE>(a[i], b[j], acc[i][j]);
         }
-        // the next step's reads among this one's products
+        // the second step's reads among the first one's products
         constexpr int READS = MT * (PCOL ? 2 : 1) + NT * (QCOL ? 2 : 1), MFMAS = MT * NT, EACH = (READS + MFMAS - 1) / MFMAS;
         __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
 #pragma unroll
-        for (int s = 0; s < 3; ++s) {
-#pragma unroll
-            for (int i = 0; i < MFMAS; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
-            }
+        for (int i = 0; i < MFMAS; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
         }
         __builtin_amdgcn_sched_group_barrier(0x008, MFMAS, 0);
     };
-    auto arrived = [&] {
-        __builtin_amdgcn_s_waitcnt(0x0F70);            // every load of this wave
-        __syncthreads();
-    };
-    const int whole = (int)((t1 - t0) / 64);
+    const int whole = (int)((t1 - t0) / 32);
     if (whole > 0) {
-        dp.load(s_p0, wave);
-        dq.load(s_q0, wave);
-        arrived();
+        Direct<PCOL> dp;
+        Direct<QCOL> dq;
+        dp.begin(P, p0, t0, wave, lane);
+        dq.begin(Q, q0, t0, wave, lane);
+        int asked = 0;
+        auto ask = [&](short *bp) {         // behind the last tile: that one again, so that the count of loads on their way stays the same
+            ++asked;
+            dp.load(bp, wave, asked < whole);
+            dq.load(bp + TILE, wave, asked < whole);
+        };
+        auto arrived = [&] {                           // this wave's reads are done, and its loads but the last 8: those of the two tiles behind the next
+            __builtin_amdgcn_s_waitcnt(0x0078);
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        ask(s_0);
+        ask(s_1);
+        ask(s_2);
         for (int k = 0;;) {
-            if (k + 1 < whole) {
-                dp.load(s_p1, wave);
-                dq.load(s_q1, wave);
-            }
-            compute(s_p0, s_q0);
+            arrived();
+            ask(s_3);
+            compute(s_0);
             if (++k == whole) break;
             arrived();
-            if (k + 1 < whole) {
-                dp.load(s_p0, wave);
-                dq.load(s_q0, wave);
-            }
-            compute(s_p1, s_q1);
+            ask(s_0);
+            compute(s_1);
             if (++k == whole) break;
             arrived();
+            ask(s_1);
+            compute(s_2);
+            if (++k == whole) break;
+            arrived();
+            ask(s_2);
+            compute(s_3);
+            if (++k == whole) break;
         }
+        __builtin_amdgcn_s_waitcnt(0x0070);            // everything
         __syncthreads();
     }
-    if (t0 + whole * 64ll < t1) {                      // what is left of t
-        Stage<TYPE, PCOL, 256, 64, 64 * WAVES>::bring(P, p0, t0 + whole * 64ll, t1, s_p0, tid);
-        Stage<TYPE, QCOL, 256, 64, 64 * WAVES>::bring(Q, q0, t0 + whole * 64ll, t1, s_q0, tid);
+    if (t0 + whole * 32ll < t1) {                      // what is left of t
+        Stage<TYPE, PCOL, 256, 32, 64 * WAVES>::bring(P, p0, t0 + whole * 32ll, t1, s_0, tid);
+        Stage<TYPE, QCOL, 256, 32, 64 * WAVES>::bring(Q, q0, t0 + whole * 32ll, t1, s_0 + TILE, tid);
         __syncthreads();
-        compute(s_p0, s_q0);
+        compute(s_0);
         __syncthreads();
     }
-    // 67.6 KB for 4 waves of 32 x 132 floats, 69.6 KB for 8 of 32 x 68 or 132
-    product_end<TYPE, !PCOL, MT, NT>(acc, reinterpret_cast<float *>(wave < WAVES / 2 ? (wave < WAVES / 4 ? s_p0 : s_q0) : (wave < 3 * WAVES / 4 ? s_p1 : s_q1)) + wave % (WAVES / 4) * 32 * PITCH,
-                                     lane, p0 + wp * MT * 32, q0 + wq * NT * 32, np, nq, part, E);
+    float *out = reinterpret_cast<float *>((wave < 4 ? (wave < 2 ? s_0 : s_1) : (wave < 6 ? s_2 : s_3)) + (wave & 1) * TILE);
+    product_end<TYPE, !PCOL, MT, NT>(acc, out, lane, p0 + wp * MT * 32, q0 + wq * NT * 32, np, nq, part, E);
 }
 
 // The parts' sums and what becomes of them, 256 neighbours p of one row q at a time.  SPLIT: a block's four waves add every fourth part each and the first of
@@ -779,12 +840,12 @@ template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dropout(Rows
             const auto a = load_some<TYPE, V>(static_cast<const T *>(X.at) + q * X.ld + c, n);
             float v[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = widen<TYPE>(a.v[i]);
+            for (int i = 0; i < V; ++i) v[i] = a.wide(i);
             drop<V>(v, (unsigned long long)q * N.cols + c, D, seed);
             if (R.at) {
                 const auto r = load_some<TYPE, V>(static_cast<const T *>(R.at) + q * R.ld + c, n);
 #pragma unroll
-                for (int i = 0; i < V; ++i) v[i] += widen<TYPE>(r.v[i]);
+                for (int i = 0; i < V; ++i) v[i] += r.wide(i);
             }
             store_some<TYPE, V>(static_cast<T *>(y) + q * ldy + c, v, n);
         }
@@ -811,7 +872,7 @@ template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dz(RowsD N, 
             const auto g = load_some<TYPE, V>(static_cast<const T *>(G.at) + q * G.ld + c, n);
             float v[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = widen<TYPE>(g.v[i]);
+            for (int i = 0; i < V; ++i) v[i] = g.wide(i);
             if constexpr (ACT != ACT_NONE) {
                 float z[V];
                 if (z_f32) load_wide<NET_F32, V>(z, static_cast<const float *>(Z.at) + q * Z.ld + c, n);
