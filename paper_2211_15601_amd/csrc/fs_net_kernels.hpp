@@ -680,10 +680,13 @@ template <bool COL> struct Direct {
 
     __device__ inline void load(short *tile, int wave, bool more)
     {
-        asm volatile("" : "+s"(at));           // one scalar address and the lanes' 32-bit offsets, not an address of 64 bits for each load
+        // By hand, since the compiler waits for all loads before it reads what such a load into the same array wrote once; who calls this waits.  (A change of m0
+        // needs a cycle before it is used here.)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            __builtin_amdgcn_global_load_lds((glob_void *)(at + offset[i]), (lds_void *)(tile + (wave * 2 + i) * 512), 16, 0, 0);
+        for (int i = 0; i < 2; ++i) {
+            const unsigned to = (unsigned)(unsigned long long)(lds_void *)(tile + (wave * 2 + i) * 512);
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(offset[i]), "s"(at) : "memory");
+        }
         at += more ? step : 0;
     }
 };
