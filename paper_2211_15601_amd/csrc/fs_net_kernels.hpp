@@ -645,46 +645,44 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_product(MatD P, MatD Q, long l
 }
 
 // The same for large products of 16-bit matrices whose rows lie at multiples of 16 bytes (and are, along p or q, a multiple of 8 long): 256 x 256 results a
-// block of 8 waves.  Tiles of 32 t go from memory to LDS directly, into the four buffers in turn, three tiles ahead of the one that is multiplied: with one
-// tile of 64 ahead a third of the time went by in waiting for it.
-typedef __attribute__((address_space(1))) const void glob_void;
+// block of 8 waves.  Tiles of 64 t (whole lines of 128 bytes: with 32 the L2 has twice the requests) go from memory to LDS directly, into two buffers in turn.
 typedef __attribute__((address_space(3))) void lds_void;
 
-// One operand's part of that: 256 rows (or, COL, columns) by 32 t are 16 KB, 1 KB an instruction, two instructions a wave.  A lane's chunk goes where the wave's place
+// One operand's part of that: 256 rows (or, COL, columns) by 64 t are 32 KB, 1 KB an instruction, four instructions a wave.  A lane's chunk goes where the wave's place
 // and its number say, so it is the chunk that is chosen: the one that place_row() or place_col() keep there.
 template <bool COL> struct Direct {
-    unsigned offset[2];                // bytes from the tile's first element
+    unsigned offset[4];                // bytes from the tile's first element
     const char *at;
     long long step;
 
     __device__ inline void begin(const MatD &M, long long b0, long long t0, int wave, int lane)
     {
         at = static_cast<const char *>(M.at) + (COL ? t0 * M.ld + b0 : b0 * M.ld + t0) * 2;
-        step = (COL ? 32 * M.ld : 32) * 2;
+        step = (COL ? 64 * M.ld : 64) * 2;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int u = wave * 2 + i;
+        for (int i = 0; i < 4; ++i) {
+            const int u = wave * 4 + i;
             if constexpr (COL) {
                 const int t = 2 * u + (lane >> 5), slot = lane & 31;
                 long long c = (slot ^ (4 * (t & 3))) * 8;
                 if (b0 + c >= M.cols) c = 0;                               // beyond the matrix: something of it, whose results go nowhere
                 offset[i] = (unsigned)((t * M.ld + c) * 2);
             } else {
-                const int r = 16 * u + (lane >> 2), slot = lane & 3;
+                const int r = 8 * u + (lane >> 3), slot = lane & 7;
                 long long row = r;
                 if (b0 + row >= M.rows) row = M.rows - 1 - b0;
-                offset[i] = (unsigned)((row * M.ld + (slot ^ ((r >> 2) & 3)) * 8) * 2);
+                offset[i] = (unsigned)((row * M.ld + (slot ^ ((r >> 1) & 7)) * 8) * 2);
             }
         }
     }
 
+    // By hand, since the compiler waits for all loads before it reads what such a load into the same array wrote once; who calls this waits.  (A change of m0
+    // needs a cycle before it is used here.)
     __device__ inline void load(short *tile, int wave, bool more)
     {
-        // By hand, since the compiler waits for all loads before it reads what such a load into the same array wrote once; who calls this waits.  (A change of m0
-        // needs a cycle before it is used here.)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const unsigned to = (unsigned)(unsigned long long)(lds_void *)(tile + (wave * 2 + i) * 512);
+        for (int i = 0; i < 4; ++i) {
+            const unsigned to = (unsigned)(unsigned long long)(lds_void *)(tile + (wave * 4 + i) * 512);
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(offset[i]), "s"(at) : "memory");
         }
         at += more ? step : 0;
@@ -694,10 +692,9 @@ template <bool COL> struct Direct {
 template <int TYPE, bool PCOL, bool QCOL>
 __global__ __launch_bounds__(512) void k_product_big(MatD P, MatD Q, long long np, long long nq, long long nt, long long t_part, TilesD tiles, EpiD E)
 {
-    constexpr int WP = 2, WAVES = 8, MT = 4, NT = 2, TILE = 256 * 32;
-    static_assert(end_floats(MT) * 4 <= TILE * 2, "a wave's results go through a buffer");
-    // arrays of their own, by which the compiler sees that reads of one buffer need not wait for loads into another
-    __shared__ __attribute__((aligned(1024))) short s_0[2 * TILE], s_1[2 * TILE], s_2[2 * TILE], s_3[2 * TILE];
+    constexpr int WP = 2, WAVES = 8, MT = 4, NT = 2, TILE = 256 * 64;
+    static_assert(WAVES * end_floats(MT) * 4 <= 4 * TILE * 2, "results go through the buffers");
+    __shared__ __attribute__((aligned(1024))) short s_mem[4 * TILE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave % WP, wq = wave / WP;
     int tp, tq;
     tile_of(tiles, blockIdx.x, tp, tq);
@@ -711,81 +708,83 @@ __global__ __launch_bounds__(512) void k_product_big(MatD P, MatD Q, long long n
         for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.0f;
-    auto compute = [&](const short *bp) {
-        const short *bq = bp + TILE;
+    struct Step { s16x8 a[MT], b[NT]; };
+    auto read = [&](Step &x, const short *bp, int s) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            s16x8 a[MT], b[NT];
+        for (int i = 0; i < MT; ++i) x.a[i] = operand<PCOL, 256, 64>(bp, (wp * MT + i) * 32, s, lane);
 #pragma unroll
-            for (int i = 0; i < MT; ++i) a[i] = operand<PCOL, 256, 32>(bp, (wp * MT + i) * 32, s, lane);
-#pragma unroll
-            for (int j = 0; j < NT; ++j) b[j] = operand<QCOL, 256, 32>(bq, (wq * NT + j) * 32, s, lane);
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = mfma<TYPE>(a[i], b[j], acc[i][j]);
-        }
-        // the second step's reads among the first one's products
-        constexpr int READS = MT * (PCOL ? 2 : 1) + NT * (QCOL ? 2 : 1), MFMAS = MT * NT, EACH = (READS + MFMAS - 1) / MFMAS;
-        __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
-#pragma unroll
-        for (int i = 0; i < MFMAS; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
-        }
-        __builtin_amdgcn_sched_group_barrier(0x008, MFMAS, 0);
+        for (int j = 0; j < NT; ++j) x.b[j] = operand<QCOL, 256, 64>(bp + TILE, (wq * NT + j) * 32, s, lane);
     };
-    const int whole = (int)((t1 - t0) / 32);
+    auto multiply = [&](const Step &x) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[i][j] = mfma<TYPE>(x.a[i], x.b[j], acc[i][j]);
+    };
+    constexpr int READS = MT * (PCOL ? 2 : 1) + NT * (QCOL ? 2 : 1), MFMAS = MT * NT, EACH = (READS + MFMAS - 1) / MFMAS;
+    auto mixed = [&](int steps) {                      // a step's reads among the products of the one before
+#pragma unroll
+        for (int i = 0; i < steps * MFMAS; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        }
+    };
+    const int whole = (int)((t1 - t0) / 64);
     if (whole > 0) {
         Direct<PCOL> dp;
         Direct<QCOL> dq;
         dp.begin(P, p0, t0, wave, lane);
         dq.begin(Q, q0, t0, wave, lane);
         int asked = 0;
-        auto ask = [&](short *bp) {         // behind the last tile: that one again, so that the count of loads on their way stays the same
+        auto ask = [&](short *bp) {                    // behind the last tile: that one again, into a buffer that nobody reads
             ++asked;
             dp.load(bp, wave, asked < whole);
             dq.load(bp + TILE, wave, asked < whole);
         };
-        auto arrived = [&] {                           // this wave's reads are done, and its loads but the last 8: those of the two tiles behind the next
-            __builtin_amdgcn_s_waitcnt(0x0078);
+        auto arrived = [&] {                           // this wave's reads are done, and its loads
             __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_waitcnt(0x0070);
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
         };
-        ask(s_0);
-        ask(s_1);
-        ask(s_2);
-        for (int k = 0;;) {
-            arrived();
-            ask(s_3);
-            compute(s_0);
-            if (++k == whole) break;
-            arrived();
-            ask(s_0);
-            compute(s_1);
-            if (++k == whole) break;
-            arrived();
-            ask(s_1);
-            compute(s_2);
-            if (++k == whole) break;
-            arrived();
-            ask(s_2);
-            compute(s_3);
-            if (++k == whole) break;
+        Step x, y;
+        ask(s_mem);
+        arrived();
+        ask(s_mem + 2 * TILE);
+        read(x, s_mem, 0);
+        int at = 0;
+        for (int k = 0; k < whole; ++k) {
+            short *now = s_mem + at;
+            at ^= 2 * TILE;
+            read(y, now, 1);
+            multiply(x);
+            read(x, now, 2);
+            multiply(y);
+            read(y, now, 3);
+            multiply(x);
+            mixed(3);
+            arrived();                                 // the next tile is there, and this one's buffer is read out
+            ask(now);
+            read(x, s_mem + at, 0);
+            multiply(y);
+            mixed(1);
         }
-        __builtin_amdgcn_s_waitcnt(0x0070);            // everything
+        __builtin_amdgcn_s_waitcnt(0x0070);
         __syncthreads();
     }
-    if (t0 + whole * 32ll < t1) {                      // what is left of t
-        Stage<TYPE, PCOL, 256, 32, 64 * WAVES>::bring(P, p0, t0 + whole * 32ll, t1, s_0, tid);
-        Stage<TYPE, QCOL, 256, 32, 64 * WAVES>::bring(Q, q0, t0 + whole * 32ll, t1, s_0 + TILE, tid);
+    if (t0 + whole * 64ll < t1) {                      // what is left of t
+        Stage<TYPE, PCOL, 256, 64, 64 * WAVES>::bring(P, p0, t0 + whole * 64ll, t1, s_mem, tid);
+        Stage<TYPE, QCOL, 256, 64, 64 * WAVES>::bring(Q, q0, t0 + whole * 64ll, t1, s_mem + TILE, tid);
         __syncthreads();
-        compute(s_0);
+#pragma unroll 1
+        for (int s = 0; s < 4; ++s) {
+            Step x;
+            read(x, s_mem, s);
+            multiply(x);
+        }
         __syncthreads();
     }
-    float *out = reinterpret_cast<float *>((wave < 4 ? (wave < 2 ? s_0 : s_1) : (wave < 6 ? s_2 : s_3)) + (wave & 1) * TILE);
-    product_end<TYPE, !PCOL, MT, NT>(acc, out, lane, p0 + wp * MT * 32, q0 + wq * NT * 32, np, nq, part, E);
+    product_end<TYPE, !PCOL, MT, NT>(acc, reinterpret_cast<float *>(s_mem) + wave * end_floats(MT), lane, p0 + wp * MT * 32, q0 + wq * NT * 32, np, nq, part, E);
 }
 
 // The parts' sums and what becomes of them, 256 neighbours p of one row q at a time.  SPLIT: a block's four waves add every fourth part each and the first of
