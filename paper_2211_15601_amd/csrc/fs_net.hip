@@ -148,11 +148,12 @@ Plan plan_product(int type, int64_t np, int64_t nq, int64_t nt, int cus)
     auto tiles = [&](int64_t n, int b) { return (long long)((n + b - 1) / b); };
     auto area = [&](int b) { return tiles(np, b) * tiles(nq, b) * b * b; };
     p.tile = tiles(np, 128) * tiles(nq, 128) >= cus && np > 64 && nq > 64 ? 128 : 64;
-    if (type != FS_FLOAT_FULL && tiles(np, 256) * tiles(nq, 256) >= cus && area(256) <= area(128) / 4 * 5) p.tile = 256;
+    // a block of the 256 tile has a compute unit for itself: one each, parts of 512 at least
+    if (type != FS_FLOAT_FULL && tiles(np, 256) * tiles(nq, 256) * std::max<long long>(1, nt / 512) >= cus && area(256) <= area(128) / 4 * 5) p.tile = 256;
     p.tiles_p = tiles(np, p.tile);
     p.tiles_q = tiles(nq, p.tile);
     const long long all = std::max(1ll, p.tiles_p * p.tiles_q);
-    const long long wanted = p.tile == 256 ? 1 : std::min((2ll * cus + all - 1) / all, std::max<long long>(1, nt / 256));
+    const long long wanted = p.tile == 256 ? std::max(1ll, cus / all) : std::min((2ll * cus + all - 1) / all, std::max<long long>(1, nt / 256));
     p.t_part = std::max(bt, ((long long)nt + wanted - 1) / wanted);
     p.t_part = (p.t_part + bt - 1) / bt * bt;
     p.parts = (int)std::max<long long>(1, (nt + p.t_part - 1) / p.t_part);
