@@ -130,6 +130,9 @@ int cus_of(int device)
 
 // ---------------------------------------------------------------------------------------------------------------- products
 
+// Forward with so many rows at most is k_few's.
+constexpr int FEW_ROWS = 32;
+
 // How a product is launched: tiles of `tile` squared, `parts` parts of the range of t, each t_part long.
 struct Plan {
     int tile, parts;
@@ -162,6 +165,13 @@ Plan plan_product(int type, int64_t np, int64_t nq, int64_t nt, int cus)
     return p;
 }
 
+Plan plan_forward(const fs_linear &l, int cus)
+{
+    Plan p = plan_product(l.type, l.outputs, l.rows, l.inputs, cus);
+    if (l.rows <= FEW_ROWS) p.parts = 1;
+    return p;
+}
+
 // May k_product_big read this operand?  Whole chunks of 16 bytes, and offsets in a tile that 32 bits hold.
 bool direct_ok(const MatD &M, bool col) { return reinterpret_cast<uintptr_t>(M.at) % 16 == 0 && M.ld % 8 == 0 && M.ld <= 1 << 22 && (!col || M.cols % 8 == 0); }
 
@@ -191,6 +201,15 @@ void launch_parts(const Plan &p, const float *part, int64_t np, int64_t nq, cons
     const long long all = (np + 255) / 256 * nq, blocks = p.parts >= 8 ? all : (all + 3) / 4;
     if (p.parts >= 8) k_parts<TYPE, true><<<(unsigned)std::min<long long>(blocks, 1 << 16), 256, 0, stream>>>(part, p.part_stride, p.ldp, p.parts, np, nq, E);
     else k_parts<TYPE, false><<<(unsigned)std::min<long long>(blocks, 1 << 16), 256, 0, stream>>>(part, p.part_stride, p.ldp, p.parts, np, nq, E);
+}
+
+// Waves a block: enough that every compute unit has some 16, and each a step or more.
+template <int TYPE> void launch_few(const MatD &W, const MatD &X, int64_t np, int64_t nq, int64_t nt, const EpiD &E, int cus, hipStream_t stream)
+{
+    const long long blocks = (np + 15) / 16, ahead = TYPE == NET_F32 ? (nq > 16 ? 2 : 4) : 8, steps = std::max<long long>(1, ((nt + 31) / 32 + ahead - 1) / ahead);
+    const int waves = (int)std::max(nq > 16 ? 2ll : 1ll, std::min(std::min(16ll, steps), std::max(4ll, 16ll * cus / blocks)));
+    if (nq > 16) k_few<TYPE, 2><<<(unsigned)blocks, 64 * waves, 0, stream>>>(W, X, np, nq, nt, E);
+    else k_few<TYPE, 1><<<(unsigned)blocks, 64 * waves, 0, stream>>>(W, X, np, nq, nt, E);
 }
 
 enum { NT, NN, TN };                   // forward, dX, dweight
@@ -251,13 +270,32 @@ template <int TYPE> void launch_dz(const RowsPlan &p, const MatD &G, const MatD 
 
 int64_t up(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// The backward pass's workspace: dZ (where it is not G itself), the sums of its columns, parts of either product.
+// The backward pass's workspace: dZ (where it is not G itself), the sums of its columns, parts of either product.  narrow: k_narrow's, by
+// `blocks` blocks.
+constexpr int NARROW = 128;            // inputs and outputs of a layer whose backward pass is k_narrow's
+
 struct Backward {
     Plan dx, dw;
     RowsPlan dz;
     bool has_dz;
+    bool narrow;
+    int blocks;
     int64_t sums, part, end;
 };
+
+int64_t narrow_ld(const fs_linear &l) { return (l.inputs + 3) / 4 * 4; }
+int64_t narrow_sums(const fs_linear &l, const Backward &b) { return b.narrow ? up((int64_t)b.blocks * l.outputs * narrow_ld(l) * 4) : 0; }
+
+template <int TYPE>
+void launch_narrow(const fs_linear &l, const Backward &b, const DzD &D, const MatD &X, const MatD &W, void *dx, int64_t lddx, void *dw, int64_t lddw, void *dbias, char *work, hipStream_t stream)
+{
+    float *part = dw ? reinterpret_cast<float *>(work) : nullptr, *sums = dbias ? reinterpret_cast<float *>(work + narrow_sums(l, b)) : nullptr;
+    const int64_t ld = narrow_ld(l);
+    constexpr int WAVES = TYPE == NET_F32 ? 8 : 4;
+    k_narrow<TYPE, NARROW, WAVES><<<b.blocks, 64 * WAVES, 0, stream>>>(D, X, W, dx, lddx, part, ld, sums);
+    const int blocks_dw = dw ? (int)((l.outputs * ld + 255) / 256) : 0, blocks_db = dbias ? (int)((l.outputs + 63) / 64) : 0;
+    if (blocks_dw + blocks_db > 0) k_narrow_end<TYPE><<<blocks_dw + blocks_db, 1024, 0, stream>>>(part, ld, b.blocks, l.inputs, l.outputs, dw, lddw, sums, dbias, l.bias_type == FS_FLOAT_FULL, blocks_dw);
+}
 
 Backward plan_backward(const fs_linear &l, int cus)
 {
@@ -266,9 +304,13 @@ Backward plan_backward(const fs_linear &l, int cus)
     b.dw = plan_product(l.type, l.inputs, l.outputs, l.rows, cus);
     b.dz = plan_rows(l.type, l.rows, l.outputs, DZ_BLOCKS);
     b.has_dz = l.act != FS_ACT_NONE || l.drop.p > 0.0;
+    b.narrow = std::max(l.inputs, l.outputs) <= NARROW;
+    const long long per_cu = l.type != FS_FLOAT_FULL ? 3 : 1;
+    b.blocks = (int)std::max<long long>(1, std::min<long long>(per_cu * cus, (l.rows + 31) / 32));
     b.sums = b.has_dz ? up(l.rows * l.outputs * size_of(l.type)) : 0;
     b.part = b.sums + up((int64_t)b.dz.gy * l.outputs * 4);
     b.end = b.part + up(std::max(b.dx.part_bytes(), b.dw.part_bytes()));
+    b.end = std::max(b.end, narrow_sums(l, b) + up((int64_t)b.blocks * l.outputs * 4));
     return b;
 }
 
@@ -307,7 +349,7 @@ int64_t fs_linear_bytes(const fs_linear *layer, int32_t backward)
     int device = 0;
     if (current_device("fs_linear_bytes", &device) != FS_OK) return -1;
     const int cus = cus_of(device);
-    if (!backward) return up(plan_product(layer->type, layer->outputs, layer->rows, layer->inputs, cus).part_bytes());
+    if (!backward) return up(plan_forward(*layer, cus).part_bytes());
     return plan_backward(*layer, cus).end;
 }
 
@@ -320,7 +362,8 @@ fs_status fs_linear_forward(const fs_linear *layer, const void *d_x, int64_t ldx
     int device = 0;
     FS_NET_TRY(current_device(what, &device));
     const int64_t m = l.rows, n = l.outputs, k = l.inputs;
-    const Plan p = plan_product(l.type, n, m, k, cus_of(device));
+    const int cus = cus_of(device);
+    const Plan p = plan_forward(l, cus);
     if (too_many(p)) return fail(FS_E_SHAPE, "%s: too many results", what);
     if (m > 0 && n > 0) {
         const int s = size_of(l.type);
@@ -346,7 +389,13 @@ fs_status fs_linear_forward(const fs_linear *layer, const void *d_x, int64_t ldx
     E.z = d_z;
     E.ldz = ldz;
     E.drop = drop_of(l.drop);
-    product(l.type, NT, p, {d_w, ldw, n, k}, {d_x, ldx, m, k}, n, m, k, E, d_work, static_cast<hipStream_t>(hip_stream));
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    const MatD W = {d_w, ldw, n, k}, X = {d_x, ldx, m, k};
+    if (m == 0 || n == 0) return FS_OK;
+    if (m > FEW_ROWS) product(l.type, NT, p, W, X, n, m, k, E, d_work, stream);
+    else if (l.type == FS_FLOAT_FULL) launch_few<NET_F32>(W, X, n, m, k, E, cus, stream);
+    else if (l.type == FS_FLOAT_BRAIN) launch_few<NET_BF16>(W, X, n, m, k, E, cus, stream);
+    else launch_few<NET_F16>(W, X, n, m, k, E, cus, stream);
     return launch_status(what);
 }
 
@@ -377,6 +426,14 @@ fs_status fs_linear_backward(const fs_linear *layer, const void *d_g, int64_t ld
     char *work = static_cast<char *>(d_work);
     float *sums = d_dbias ? reinterpret_cast<float *>(work + b.sums) : nullptr;
     const MatD G = {d_g, ldg, m, n}, Z = {d_z, ldz, m, n};
+    if (b.narrow && m > 0 && n > 0 && k > 0 && (d_dx || d_dw || d_dbias)) {
+        const DzD D = {G, Z, l.bias_type == FS_FLOAT_FULL, l.act, l.beta, drop_of(l.drop)};
+        const MatD X = {d_x, ldx, m, k}, W = {d_w, ldw, n, k};
+        if (l.type == FS_FLOAT_FULL) launch_narrow<NET_F32>(l, b, D, X, W, d_dx, lddx, d_dw, lddw, d_dbias, work, stream);
+        else if (l.type == FS_FLOAT_BRAIN) launch_narrow<NET_BF16>(l, b, D, X, W, d_dx, lddx, d_dw, lddw, d_dbias, work, stream);
+        else launch_narrow<NET_F16>(l, b, D, X, W, d_dx, lddx, d_dw, lddw, d_dbias, work, stream);
+        return launch_status(what);
+    }
     const MatD dZ = b.has_dz ? MatD{work, n, m, n} : G;
     void *dz = b.has_dz && (d_dx || d_dw) ? work : nullptr;
     if ((dz || sums) && n > 0) {

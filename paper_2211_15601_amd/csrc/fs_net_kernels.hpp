@@ -148,9 +148,9 @@ __device__ inline uint4 philox(unsigned long long block, unsigned long long offs
 #pragma unroll
     for (int r = 0; r < 10; ++r) {
         const unsigned long long p = 0xD2511F53ull * a, q = 0xCD9E8D57ull * c;
-        a = (unsigned)(q >> 32) ^ b ^ k0;
+        a = __builtin_amdgcn_bitop3_b32((unsigned)(q >> 32), b, k0, 0x96);             // a ^ b ^ c
         b = (unsigned)q;
-        c = (unsigned)(p >> 32) ^ d ^ k1;
+        c = __builtin_amdgcn_bitop3_b32((unsigned)(p >> 32), d, k1, 0x96);
         d = (unsigned)p;
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
@@ -349,19 +349,21 @@ template <int TYPE> __device__ inline f32x16 mfma(s16x8 a, s16x8 b, f32x16 c)
 
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-// The operand of one matrix instruction: 32 rows from p0, t = 16 step + 8 (lane / 32) + 0 .. 7.
+// The operand of one matrix instruction from a tile with p along its rows: 32 of those from p0 on, t = 16 step + 8 (lane / 32) + 0 .. 7.
+template <class Place> __device__ inline s16x8 turned(Place place, const short *tile, int p0, int step, int lane)
+{
+    // lane i of 16 hands in 4 elements of row t + i / 4 and gets those of column i
+    const int i = lane & 15, t = 16 * step + 8 * (lane >> 5) + (i >> 2), p = p0 + (lane & 16) + 4 * (i & 3);
+    const short *lo = tile + place(t, p >> 3) + (p & 7), *hi = tile + place(t + 4, p >> 3) + (p & 7);
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)lo), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)hi);
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// The same from either kind of tile.
 template <bool COL, int B, int BT> __device__ inline s16x8 operand(const short *tile, int p0, int step, int lane)
 {
-    if constexpr (!COL) {
-        const int r = p0 + (lane & 31);
-        return *reinterpret_cast<const s16x8 *>(tile + place_row<BT>(r, 2 * step + (lane >> 5)));
-    } else {
-        // lane i of 16 hands in 4 elements of row t + i / 4 and gets those of column i
-        const int i = lane & 15, t = 16 * step + 8 * (lane >> 5) + (i >> 2), p = p0 + (lane & 16) + 4 * (i & 3);
-        const short *lo = tile + place_col<B>(t, p >> 3) + (p & 7), *hi = tile + place_col<B>(t + 4, p >> 3) + (p & 7);
-        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)lo), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)hi);
-        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-    }
+    if constexpr (COL) return turned([](int t, int c) { return place_col<B>(t, c); }, tile, p0, step, lane);
+    else return *reinterpret_cast<const s16x8 *>(tile + place_row<BT>(p0 + (lane & 31), 2 * step + (lane >> 5)));
 }
 
 // Three bf16 parts of fp32 numbers: x = h + m + l to 24 bits and more, each part the rounded rest of those before it.  A rest that is no number
@@ -380,6 +382,14 @@ __device__ inline void split8(const Packed<NET_F32, 8> &x, s16x8 *part)
     }
 }
 
+// A result that is no finite number may be one of the parts' making (inf - inf, or a part of the largest numbers rounded up to infinity): it is computed plainly, then.
+__device__ __attribute__((noinline)) float plain_dot(const float *x, long long step_x, const float *y, long long step_y, long long n)
+{
+    float sum = 0.0f;
+    for (long long t = 0; t < n; ++t) sum = __builtin_fmaf(x[t * step_x], y[t * step_y], sum);
+    return sum;
+}
+
 // One operand's tile on its way from memory to LDS: B rows (p or q) by BT, in chunks of 8.
 template <int TYPE, bool COL, int B, int BT, int THREADS> struct Stage {
     typedef typename ElemOf<TYPE>::type T;
@@ -387,20 +397,26 @@ template <int TYPE, bool COL, int B, int BT, int THREADS> struct Stage {
     static constexpr int ROWS = COL ? BT : B, COLS = COL ? B : BT, PER_ROW = COLS / 8, N = ROWS * PER_ROW / THREADS;
     static constexpr int LDS = PLANES * B * BT;            // 16-bit elements
     static_assert(ROWS * PER_ROW % THREADS == 0 && N >= 1, "tile");
+    static constexpr int APART = THREADS / PER_ROW;        // rows between a thread's chunks
+    static_assert(THREADS % PER_ROW == 0, "tile");
     Packed<TYPE, 8> chunk[N];
 
-    // b0: first row or column p; t0: first t; t1: end of the range of t
+    // b0: first row or column p; t0: first t; t1: end of the range of t.  Addresses are a wave's and a lane's part, of which the latter stays the same.
     __device__ inline void load(const MatD &M, long long b0, long long t0, long long t1, int tid)
     {
-        const T *at = static_cast<const T *>(M.at);
         const long long r0 = COL ? t0 : b0, c0 = COL ? b0 : t0, rows = COL ? t1 : M.rows, cols = COL ? M.cols : t1;
-        const bool inside = r0 + ROWS <= rows && c0 + COLS <= cols;
+        const T *at = static_cast<const T *>(M.at) + r0 * M.ld + c0;
+        const long long own = tid / PER_ROW * M.ld + tid % PER_ROW * 8;
+        if (r0 + ROWS <= rows && c0 + COLS <= cols) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) chunk[i] = load_all<TYPE, 8>(at + i * APART * M.ld + own);
+            return;
+        }
+        const long long c = c0 + tid % PER_ROW * 8, left = cols - c;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int u = tid + i * THREADS;
-            const long long r = r0 + u / PER_ROW, c = c0 + u % PER_ROW * 8;
-            if (inside) chunk[i] = load_all<TYPE, 8>(at + r * M.ld + c);
-            else chunk[i] = guarded(at, M.ld, r, c, rows, cols);
+            chunk[i] = Packed<TYPE, 8>();
+            if (r0 + tid / PER_ROW + i * APART < rows && left > 0) chunk[i] = load_some<TYPE, 8>(at + i * APART * M.ld + own, left < 8 ? (int)left : 8);
         }
     }
 
@@ -418,7 +434,9 @@ template <int TYPE, bool COL, int B, int BT, int THREADS> struct Stage {
     static __device__ inline void put(const Packed<TYPE, 8> &x, short *tile, int u)
     {
         const int r = u / PER_ROW, c = u % PER_ROW;
-        short *at = tile + (COL ? place_col<B>(r, c) : place_row<BT>(r, c));
+        short *at = tile;
+        if constexpr (COL) at += place_col<B>(r, c);
+        else at += place_row<BT>(r, c);
         if constexpr (TYPE == NET_F32) {
             s16x8 part[3];
             split8(x, part);
@@ -624,7 +642,7 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_product(MatD P, MatD Q, long l
     }
 
     if constexpr (TYPE == NET_F32) {
-        // a result that is no finite number may be one of the parts' making (of inf - inf, or a part of the largest numbers rounded up): plainly, then
+        // a result that is no finite number may be one of the parts' making (see plain_dot)
         const float *x = static_cast<const float *>(P.at), *y = static_cast<const float *>(Q.at);
 #pragma unroll
         for (int i = 0; i < MT; ++i)
@@ -634,10 +652,7 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_product(MatD P, MatD Q, long l
                 for (int k = 0; k < 16; ++k)
                     if (!(fabsf(acc[i][j][k]) < INFINITY)) {
                         const long long p = p0 + (wp * MT + i) * 32 + 8 * (k >> 2) + 4 * (lane >> 5) + (k & 3), q = q0 + (wq * NT + j) * 32 + (lane & 31);
-                        float sum = 0.0f;
-                        if (p < np && q < nq)
-                            for (long long t = t0; t < t1; ++t) sum = __builtin_fmaf(x[PCOL ? t * P.ld + p : p * P.ld + t], y[QCOL ? t * Q.ld + q : q * Q.ld + t], sum);
-                        acc[i][j][k] = sum;
+                        acc[i][j][k] = p < np && q < nq ? plain_dot(x + (PCOL ? t0 * P.ld + p : p * P.ld + t0), PCOL ? P.ld : 1, y + (QCOL ? t0 * Q.ld + q : q * Q.ld + t0), QCOL ? Q.ld : 1, t1 - t0) : 0.0f;
                     }
     }
 
@@ -821,6 +836,373 @@ template <int TYPE, bool SPLIT> __global__ __launch_bounds__(256) void k_parts(c
         }
         if constexpr (SPLIT) __syncthreads();
     }
+}
+
+// ---------------------------------------------------------------------------------------------------------------- few rows
+
+template <int TYPE> __device__ inline f32x4 mfma16(s16x8 a, s16x8 b, f32x4 c)
+{
+    if constexpr (TYPE == NET_F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// Forward with few rows: the weights are read once, past LDS, straight into the operands (16 outputs by 64 bytes an instruction), and that is all the time it takes.
+// A block has 16 outputs and all rows (NQ times 16); its waves take stretches of t in turn and add up in LDS.
+template <int TYPE, int NQ>
+__global__ __launch_bounds__(1024) void k_few(MatD W, MatD X, long long np, long long nq, long long nt, EpiD E)
+{
+    typedef typename ElemOf<TYPE>::type T;
+    constexpr int PL = TYPE == NET_F32 ? 3 : 1, AHEAD = (TYPE == NET_F32 ? 4 : 8) / NQ;      // loads of the weights on their way, a lane
+    __shared__ __attribute__((aligned(16))) float s_sum[16][NQ][64][4];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const long long p0 = blockIdx.x * 16ll;
+    const long long row = p0 + (lane & 15) < np ? p0 + (lane & 15) : np - 1;
+    const T *w = static_cast<const T *>(W.at) + row * W.ld;
+    // what the end needs, of the threads that take part in it
+    const int j = threadIdx.x >> 6;
+    const long long q = 16 * j + (lane & 15), p = p0 + 4 * (lane >> 4);
+    const int n = j < NQ && q < nq ? (np - p < 4 ? (int)(np - p) : 4) : 0;
+    const Seed seed = seed_of(E.drop);
+    float bias[4];
+    load_bias<TYPE>(bias, E, p, n);
+    Packed<TYPE, 4> r = {};
+    if (n > 0) r = residual4<TYPE>(E, q, p, n);
+    f32x4 acc[NQ];
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const long long steps = (nt + 31) / 32;
+    for (long long s = (long long)wave * AHEAD; s < steps; s += waves * AHEAD) {
+        Packed<TYPE, 8> a[AHEAD], b[AHEAD][NQ];
+        const bool inside = (s + AHEAD) * 32 <= nt;
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const long long t = (s + k) * 32 + (lane >> 4) * 8, left = nt - t;
+            a[k] = Packed<TYPE, 8>();
+            if (inside) a[k] = load_all<TYPE, 8>(w + t);
+            else if (left > 0) a[k] = load_some<TYPE, 8>(w + t, left < 8 ? (int)left : 8);
+#pragma unroll
+            for (int j = 0; j < NQ; ++j) {
+                const long long q = 16 * j + (lane & 15);
+                b[k][j] = Packed<TYPE, 8>();
+                const T *x = static_cast<const T *>(X.at) + q * X.ld + t;
+                if (q < nq) {
+                    if (inside) b[k][j] = load_all<TYPE, 8>(x);
+                    else if (left > 0) b[k][j] = load_some<TYPE, 8>(x, left < 8 ? (int)left : 8);
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            s16x8 u[PL], v[PL];
+            if constexpr (PL == 3) split8(a[k], u);
+            else u[0] = __builtin_bit_cast(s16x8, u32x4{a[k].w[0], a[k].w[1], a[k].w[2], a[k].w[3]});
+#pragma unroll
+            for (int j = 0; j < NQ; ++j) {
+                if constexpr (PL == 3) {
+                    split8(b[k][j], v);
+                    constexpr int PA[6] = {0, 1, 2, 0, 1, 0}, PB[6] = {2, 1, 0, 1, 0, 0};
+#pragma unroll
+                    for (int n = 0; n < 6; ++n) acc[j] = mfma16<TYPE>(u[PA[n]], v[PB[n]], acc[j]);
+                } else {
+                    v[0] = __builtin_bit_cast(s16x8, u32x4{b[k][j].w[0], b[k][j].w[1], b[k][j].w[2], b[k][j].w[3]});
+                    acc[j] = mfma16<TYPE>(u[0], v[0], acc[j]);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) *reinterpret_cast<f32x4 *>(s_sum[wave][j][lane]) = acc[j];
+    __syncthreads();
+    if (n <= 0) return;
+    f32x4 sum = *reinterpret_cast<const f32x4 *>(s_sum[0][j][lane]);
+    for (int i = 1; i < waves; ++i) sum += *reinterpret_cast<const f32x4 *>(s_sum[i][j][lane]);
+    float v[4] = {sum[0], sum[1], sum[2], sum[3]};
+    if constexpr (TYPE == NET_F32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < n && !(fabsf(v[i]) < INFINITY)) v[i] = plain_dot(static_cast<const float *>(W.at) + (p + i) * W.ld, 1, static_cast<const float *>(X.at) + q * X.ld, 1, nt);
+    }
+    with_act(E.act, [&](auto act) { finish4<TYPE, decltype(act)::value>(v, bias, r, E, seed, q, p, n, np); });
+}
+
+// ---------------------------------------------------------------------------------------------------------------- narrow layers
+
+// Chunks of 8 elements of dZ in LDS, [rows][B]: read along the rows as an operand of dX, and turned as one of dweight.  16 rows have one chunk in 16 different places,
+// and four rows 32 neighbours in 8.
+template <int B> __device__ inline int place_both(int t, int c) { return t * B + ((c ^ 4 * (t & 3) ^ (t >> 2 & 3)) * 8); }
+
+// What dZ is made from.
+struct DzD { MatD G, Z; int z_f32, act; float beta; DropD drop; };
+
+// One element of it, in fp32
+__device__ inline float dz_at(const DzD &D, const Seed &seed, long long q, long long n)
+{
+    float g = static_cast<const float *>(D.G.at)[q * D.G.ld + n];
+    if (D.act != ACT_NONE) {
+        const float z = static_cast<const float *>(D.Z.at)[q * D.Z.ld + n];
+        float s = 1.0f;
+        with_act(D.act, [&](auto kind) { s = slope_of<decltype(kind)::value>(z, D.beta); });
+        g *= s;
+    }
+    if (D.drop.mode == 0) return g;
+    if (D.drop.mode == 2) return 0.0f;
+    const unsigned long long e = (unsigned long long)q * D.G.cols + n;
+    const uint4 w = philox(e >> 2, seed.offset, seed.seed);
+    const unsigned word = e & 2 ? (e & 1 ? w.w : w.z) : (e & 1 ? w.y : w.x);
+    return word >= D.drop.least ? g * D.drop.scale : 0.0f;
+}
+
+// The backward pass of a layer of at most B inputs and B outputs, in one pass over its rows: G, Z and X are read once, dX is written, dweight stays in registers and the
+// sums for dbias too, a part for each block.  The weights lie in LDS.  A block takes 32 rows at a time, the next ones on their way meanwhile.
+//   dweight: WP x WQ waves share the B x B results, t = rows.  dX: 32 inputs a wave, t = outputs; where there are twice the waves, two share those.
+template <int TYPE, int B, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void k_narrow(DzD D, MatD X, MatD W, void *dx, long long lddx, float *__restrict__ dw, long long ldw, float *__restrict__ sums)
+{
+    typedef typename ElemOf<TYPE>::type T;
+    constexpr int THREADS = 64 * WAVES, R = 32, PL = TYPE == NET_F32 ? 3 : 1, WP = WAVES / 2, WQ = 2, MT = B / WP / 32, NT = B / WQ / 32;
+    constexpr int HALVES = WAVES * 32 / B, STEPS = B / 16 / HALVES, UNITS = R * B / 8 / THREADS, PER_ROW = B / 8;
+    static_assert(MT >= 1 && (HALVES == 1 || HALVES == 2) && THREADS % PER_ROW == 0, "shape");
+    __shared__ __attribute__((aligned(1024))) short s_w[PL * B * B];
+    __shared__ __attribute__((aligned(1024))) short s_in[2 * PL * R * B];
+    static_assert(HALVES * R * B * 4 <= 2 * PL * R * B * 2, "dX goes through the inputs' place");
+    short *s_dz = s_in, *s_x = s_in + PL * R * B;
+    float *s_out = reinterpret_cast<float *>(s_in);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave % WP, wq = wave / WP;
+    const long long rows = D.G.rows, outputs = D.G.cols, inputs = X.cols;
+    const Seed seed = seed_of(D.drop);
+    if (dx) Stage<TYPE, true, B, B, THREADS>::bring(W, 0, 0, outputs, s_w, tid);
+
+    f32x16 acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.0f;
+    float db[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) db[i] = 0.0f;
+
+    Packed<TYPE, 8> g[UNITS];
+    unsigned z[UNITS][8];
+    Stage<TYPE, true, B, R, THREADS> sx;
+    const int c8 = tid % PER_ROW * 8, left = outputs - c8 < 8 ? (int)(outputs - c8) : 8;
+    constexpr int APART = THREADS / PER_ROW;
+    const int r0 = tid / PER_ROW;
+    const long long own_g = r0 * D.G.ld + c8, own_z = r0 * D.Z.ld + c8;
+    auto load = [&](long long q0) {
+        const T *at_g = static_cast<const T *>(D.G.at) + q0 * D.G.ld;
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+            g[i] = Packed<TYPE, 8>();
+#pragma unroll
+            for (int k = 0; k < 8; ++k) z[i][k] = 0u;
+            if (q0 + r0 + i * APART < rows && left > 0) {
+                g[i] = load_some<TYPE, 8>(at_g + i * APART * D.G.ld + own_g, left);
+                if (D.act == ACT_NONE) continue;
+                if (D.z_f32) {
+                    const auto x = load_some<NET_F32, 8>(static_cast<const float *>(D.Z.at) + (q0 + i * APART) * D.Z.ld + own_z, left);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) z[i][k] = x.w[k];
+                } else {
+                    const auto x = load_some<TYPE, 8>(static_cast<const T *>(D.Z.at) + (q0 + i * APART) * D.Z.ld + own_z, left);
+#pragma unroll
+                    for (int k = 0; k < x.WORDS; ++k) z[i][k] = x.w[k];
+                }
+            }
+        }
+        if (dw) sx.load(X, 0, q0, rows, tid);
+    };
+
+    const long long stride = (long long)gridDim.x * R;
+    long long q0 = (long long)blockIdx.x * R;
+    load(q0);
+    for (; q0 < rows; q0 += stride) {
+        with_act(D.act, [&](auto kind) {
+#pragma unroll
+            for (int i = 0; i < UNITS; ++i) {
+                const int u = tid + i * THREADS, r = u / PER_ROW;
+                float v[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    v[k] = g[i].wide(k);
+                    if constexpr (decltype(kind)::value != ACT_NONE) {
+                        float zk;
+                        if (TYPE == NET_F32 || D.z_f32) zk = __uint_as_float(z[i][k]);
+                        else {
+                            Packed<TYPE, 8> x;
+#pragma unroll
+                            for (int m = 0; m < x.WORDS; ++m) x.w[m] = z[i][m];
+                            zk = x.wide(k);
+                        }
+                        v[k] *= slope_of<decltype(kind)::value>(zk, D.beta);
+                    }
+                }
+                drop<8>(v, (unsigned long long)(q0 + r) * outputs + c8, D.drop, seed);
+                Packed<TYPE, 8> x;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) db[k] += v[k];
+                if constexpr (TYPE == NET_F32) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) x.w[k] = __float_as_uint(v[k]);
+                    s16x8 part[3];
+                    split8(x, part);
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) *reinterpret_cast<s16x8 *>(s_dz + k * R * B + place_both<B>(r, u % PER_ROW)) = part[k];
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) x.w[k] = (unsigned)narrow<TYPE>(v[2 * k]) | (unsigned)narrow<TYPE>(v[2 * k + 1]) << 16;
+                    *reinterpret_cast<u32x4 *>(s_dz + place_both<B>(r, u % PER_ROW)) = u32x4{x.w[0], x.w[1], x.w[2], x.w[3]};
+                }
+            }
+        });
+        if (dw) sx.store(s_x, tid);
+        if (q0 + stride < rows) load(q0 + stride);
+        __syncthreads();
+
+        constexpr int PA[6] = {0, 1, 2, 0, 1, 0}, PB[6] = {2, 1, 0, 1, 0, 0};
+        if (dw)
+#pragma unroll
+        for (int s = 0; s < R / 16; ++s) {
+            s16x8 a[MT][PL], b[NT][PL];
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int k = 0; k < PL; ++k) a[i][k] = operand<true, B, R>(s_x + k * R * B, (wp * MT + i) * 32, s, lane);
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int k = 0; k < PL; ++k) b[j][k] = turned([](int t, int c) { return place_both<B>(t, c); }, s_dz + k * R * B, (wq * NT + j) * 32, s, lane);
+#pragma unroll
+            for (int u = 0; u < (PL == 1 ? 1 : 6); ++u)
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) acc[i][j] = mfma<TYPE>(a[i][PL == 1 ? 0 : PA[u]], b[j][PL == 1 ? 0 : PB[u]], acc[i][j]);
+        }
+        if (!dx) {
+            __syncthreads();
+            continue;
+        }
+        f32x16 d;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) d[k] = 0.0f;
+        const int pb = wave % (B / 32) * 32, half = wave / (B / 32);
+#pragma unroll 4
+        for (int s = 0; s < STEPS; ++s) {
+            const int step = half * STEPS + s;
+            s16x8 a[PL], b[PL];
+#pragma unroll
+            for (int k = 0; k < PL; ++k) a[k] = operand<true, B, B>(s_w + k * B * B, pb, step, lane);
+#pragma unroll
+            for (int k = 0; k < PL; ++k) b[k] = *reinterpret_cast<const s16x8 *>(s_dz + k * R * B + place_both<B>(lane & 31, 2 * step + (lane >> 5)));
+#pragma unroll
+            for (int u = 0; u < (PL == 1 ? 1 : 6); ++u) d = mfma<TYPE>(a[PL == 1 ? 0 : PA[u]], b[PL == 1 ? 0 : PB[u]], d);
+        }
+        __syncthreads();
+        // row q of dX: B floats, its quarters of 16 bytes turned by q so that the lanes' writes spread over the banks
+#pragma unroll
+        for (int gq = 0; gq < 4; ++gq) {
+            const int q = lane & 31, quad = (pb + 8 * gq + 4 * (lane >> 5)) / 4;
+            *reinterpret_cast<f32x4 *>(s_out + half * R * B + q * B + ((quad ^ (q & 15)) * 4)) = f32x4{d[4 * gq], d[4 * gq + 1], d[4 * gq + 2], d[4 * gq + 3]};
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < R * B / 4 / THREADS; ++i) {
+            const int u = tid + i * THREADS, r = u / (B / 4), quad = u % (B / 4);
+            const long long q = q0 + r, p = 4 * quad;
+            f32x4 x = *reinterpret_cast<const f32x4 *>(s_out + r * B + ((quad ^ (r & 15)) * 4));
+            if constexpr (HALVES == 2) x += *reinterpret_cast<const f32x4 *>(s_out + R * B + r * B + ((quad ^ (r & 15)) * 4));
+            if (q < rows && p < inputs) {
+                const int n = inputs - p < 4 ? (int)(inputs - p) : 4;
+                float v[4] = {x[0], x[1], x[2], x[3]};
+                if constexpr (TYPE == NET_F32)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (k < n && !(fabsf(v[k]) < INFINITY)) {              // as in k_product
+                            float sum = 0.0f;
+                            for (long long m = 0; m < outputs; ++m) sum = __builtin_fmaf(dz_at(D, seed, q, m), static_cast<const float *>(W.at)[m * W.ld + p + k], sum);
+                            v[k] = sum;
+                        }
+                store_some<TYPE, 4>(static_cast<T *>(dx) + q * lddx + p, v, n);
+            }
+        }
+        __syncthreads();
+    }
+
+    // dweight's part, [outputs][ldw]
+    float *part = dw + (long long)blockIdx.x * outputs * ldw;
+    if (dw)
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int gq = 0; gq < 4; ++gq) {
+                const long long p = (wp * MT + i) * 32 + 8 * gq + 4 * (lane >> 5), q = (wq * NT + j) * 32 + (lane & 31);
+                if (p >= inputs || q >= outputs) continue;
+                *reinterpret_cast<f32x4 *>(part + q * ldw + p) = f32x4{acc[i][j][4 * gq], acc[i][j][4 * gq + 1], acc[i][j][4 * gq + 2], acc[i][j][4 * gq + 3]};
+            }
+    if constexpr (TYPE == NET_F32)
+        if (dw) {                      // results that are no finite numbers, plainly
+            __syncthreads();
+            for (long long e = tid; e < outputs * inputs; e += THREADS) {
+                const long long q = e / inputs, p = e % inputs;
+                float sum = part[q * ldw + p];
+                if (fabsf(sum) < INFINITY) continue;
+                sum = 0.0f;
+                for (long long m0 = (long long)blockIdx.x * R; m0 < rows; m0 += stride)
+                    for (long long m = m0; m < m0 + R && m < rows; ++m) sum = __builtin_fmaf(dz_at(D, seed, m, q), static_cast<const float *>(X.at)[m * X.ld + p], sum);
+                part[q * ldw + p] = sum;
+            }
+        }
+    if (!sums) return;
+    // dbias' part: a thread's columns are those of every PER_ROW-th other
+    __syncthreads();
+    float *s_db = reinterpret_cast<float *>(s_in);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s_db[tid / PER_ROW * B + c8 + k] = db[k];
+    __syncthreads();
+    for (int n = tid; n < outputs; n += THREADS) {
+        float all = 0.0f;
+        for (int r = 0; r < THREADS / PER_ROW; ++r) all += s_db[r * B + n];
+        sums[blockIdx.x * outputs + n] = all;
+    }
+}
+
+// The parts of k_narrow added up, dweight (of 256 neighbours by a block) and behind it dbias (of 64).
+template <int TYPE> __global__ __launch_bounds__(1024) void k_narrow_end(const float *__restrict__ dw, long long ldp, int parts, long long inputs, long long outputs, void *out, long long ldo,
+                                                                         const float *__restrict__ sums, void *dbias, int bias_f32, int blocks_dw)
+{
+    __shared__ __attribute__((aligned(16))) float s_sum[16][256];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if ((int)blockIdx.x < blocks_dw) {
+        // rows of ldp floats, a multiple of 4, one after another
+        const long long e = blockIdx.x * 256ll + 4 * lane, all = outputs * ldp;
+        f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (e < all)
+#pragma unroll 8
+            for (int i = wave; i < parts; i += 16) sum += *reinterpret_cast<const f32x4 *>(dw + i * all + e);
+        *reinterpret_cast<f32x4 *>(s_sum[wave] + 4 * lane) = sum;
+        __syncthreads();
+        if (wave || e >= all) return;
+        for (int w = 1; w < 16; ++w) sum += *reinterpret_cast<const f32x4 *>(s_sum[w] + 4 * lane);
+        const long long q = e / ldp, p = e % ldp;
+        const float v[4] = {sum[0], sum[1], sum[2], sum[3]};
+        store_some<TYPE, 4>(static_cast<typename ElemOf<TYPE>::type *>(out) + q * ldo + p, v, inputs - p < 4 ? (int)(inputs - p) : 4);
+        return;
+    }
+    const long long c = (blockIdx.x - blocks_dw) * 64ll + lane;
+    float all = 0.0f;
+    if (c < outputs)
+#pragma unroll 16
+        for (int b = wave; b < parts; b += 16) all += sums[b * outputs + c];
+    s_sum[wave][lane] = all;
+    __syncthreads();
+    if (wave || c >= outputs) return;
+    for (int w = 1; w < 16; ++w) all += s_sum[w][lane];
+    if (bias_f32) static_cast<float *>(dbias)[c] = all;
+    else static_cast<typename ElemOf<TYPE>::type *>(dbias)[c] = narrow<TYPE>(all);
 }
 
 // ---------------------------------------------------------------------------------------------------------------- elementwise

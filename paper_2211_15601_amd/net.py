@@ -15,6 +15,7 @@ A captured backward pass needs its forward pass in the same capture, and no eage
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 from typing import Optional, Sequence, Tuple, Union
 
@@ -57,7 +58,7 @@ def _check_p(what, p):
 
 def _check_seed(seed, x):
     if isinstance(seed, torch.Tensor):
-        _check("seed", seed, x, [torch.int64])
+        _check("seed", seed, x, (torch.int64,))
         if seed.shape != (2,) or not seed.is_contiguous():
             raise ValueError("seed must hold two words, one after another")
         if seed.requires_grad:
@@ -73,11 +74,6 @@ def _rows(t: torch.Tensor) -> torch.Tensor:
     return t if t.stride(1) == 1 or t.shape[1] <= 1 else t.contiguous()
 
 
-def _at(t: Optional[torch.Tensor]):
-    """Address and row stride."""
-    return (None, 0) if t is None else (t.data_ptr(), t.stride(0))
-
-
 def _drop(p, seed) -> binding.Drop:
     if p == 0.0:
         return binding.Drop()
@@ -86,49 +82,61 @@ def _drop(p, seed) -> binding.Drop:
     return binding.Drop(p, seed[0], seed[1], None)
 
 
-def _call(device, f, *args):
-    """A call on the device's current stream."""
-    if torch._C._cuda_getDevice() != device.index:
-        with torch.cuda.device(device):
-            return _call(device, f, *args)
-    st = f(*args, torch._C._cuda_getCurrentRawStream(device.index))
+def _call(index, f, *args):
+    """A call on a device's current stream."""
+    if torch._C._cuda_getDevice() != index:
+        with torch.cuda.device(index):
+            return _call(index, f, *args)
+    st = f(*args, torch._C._cuda_getCurrentRawStream(index))
     if st != binding.FS_OK:
         raise binding.FsError(st, binding.load().fs_net_error().decode())
 
 
-def _workspace(layer, backward, device):
-    with torch.cuda.device(device):
-        n = binding.load().fs_linear_bytes(ctypes.byref(layer), backward)
-    if n < 0:
-        raise binding.FsError(binding.FS_E_SHAPE, binding.load().fs_net_error().decode())
-    return (torch.empty(n, dtype=torch.uint8, device=device) if n else None), n
+class _Plan:
+    """What calls of the same sizes share: the layer as the library takes it, without a seed, and the bytes that its calls work in."""
+
+    def __init__(self, index, rows, inputs, outputs, kind, bias_kind, act, beta, p):
+        L = binding.load()
+        self.index, self.bare = index, binding.Linear(rows, inputs, outputs, kind, bias_kind, act, beta, binding.Drop(p, 0, 0, None))
+        self.at = ctypes.byref(self.bare)
+        self.forward, self.backward = L.fs_linear_forward, L.fs_linear_backward
+        with torch.cuda.device(index):
+            self.bytes = L.fs_linear_bytes(self.at, 0), L.fs_linear_bytes(self.at, 1)
+        if min(self.bytes) < 0:
+            raise binding.FsError(binding.FS_E_SHAPE, L.fs_net_error().decode())
+
+    def layer(self, seed):
+        if seed is None:
+            return self.at
+        b = self.bare
+        return ctypes.byref(binding.Linear(b.rows, b.inputs, b.outputs, b.type, b.bias_type, b.act, b.beta, _drop(b.drop.p, seed)))
 
 
-def _forward(layer, shape, x, weight, bias, residual, keep_z):
-    """x, residual [rows, ...] and weight as _rows() gives them.  Y (of `shape`: no view, so that a program may change it in place), and Z where it is kept."""
-    L, device = binding.load(), x.device
-    y = torch.empty(shape, dtype=x.dtype, device=device)
-    z = torch.empty(shape, dtype=x.dtype if bias is None else bias.dtype, device=device) if keep_z else None
-    work, n = _workspace(layer, 0, device)
-    _call(device, L.fs_linear_forward, ctypes.byref(layer), *_at(x), *_at(weight), None if bias is None else bias.data_ptr(), *_at(residual), y.data_ptr(), layer.outputs, None if z is None else z.data_ptr(), layer.outputs,
+_plan = functools.lru_cache(maxsize=1024)(_Plan)
+
+
+def _forward(plan, shape, x, weight, bias, residual, keep_z, seed):
+    """Y (of `shape`: no view, so that a program may change it in place), and Z where it is kept."""
+    x, w = _rows(x), _rows(weight)
+    r = None if residual is None else _rows(residual)
+    y = x.new_empty(shape)
+    z = x.new_empty(shape, dtype=x.dtype if bias is None else bias.dtype) if keep_z else None
+    n, outputs = plan.bytes[0], w.shape[0]
+    work = x.new_empty(n, dtype=torch.uint8) if n else None
+    b = bias if bias is None or bias.is_contiguous() else bias.contiguous()
+    _call(plan.index, plan.forward, plan.layer(seed), x.data_ptr(), x.stride(0), w.data_ptr(), w.stride(0), None if b is None else b.data_ptr(),
+          None if r is None else r.data_ptr(), 0 if r is None else r.stride(0), y.data_ptr(), outputs, None if z is None else z.data_ptr(), outputs,
           None if work is None else work.data_ptr(), n)
     return y, z
 
 
-def _layer(x, weight, bias, act, beta, p, seed):
-    kind = _TYPES[x.dtype]
-    return binding.Linear(x.shape[0], x.shape[1], weight.shape[0], kind, kind if bias is None else _TYPES[bias.dtype], act, beta, _drop(p, seed))
-
-
 class _Linear(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, bias, residual, act, beta, p, seed):
-        rows, w, r = _rows(x), _rows(weight), None if residual is None else _rows(residual)
-        b = None if bias is None else bias.contiguous()
-        y, z = _forward(_layer(rows, w, b, act, beta, p, seed), (*x.shape[:-1], weight.shape[0]), rows, w, b, r, act != binding.FS_ACT_NONE)
-        need = ctx.needs_input_grad
-        ctx.how, ctx.shape, ctx.bias_type = (act, beta, p, None if isinstance(seed, torch.Tensor) else seed), x.shape, None if bias is None else bias.dtype
-        ctx.save_for_backward(x if need[1] else None, weight, z, seed if isinstance(seed, torch.Tensor) else None)
+    def forward(ctx, x, weight, bias, residual, plan, shape, seed):
+        y, z = _forward(plan, shape, x, weight, bias, residual, plan.bare.act != binding.FS_ACT_NONE, seed)
+        words = seed if isinstance(seed, torch.Tensor) else None
+        ctx.plan, ctx.seed, ctx.shape, ctx.bias_type = plan, None if words is not None else seed, x.shape, None if bias is None else bias.dtype
+        ctx.save_for_backward(x if ctx.needs_input_grad[1] else None, weight, z, words)
         ctx.set_materialize_grads(False)
         return y
 
@@ -136,24 +144,23 @@ class _Linear(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, g):
         if g is None:
-            return (None,) * 8
-        x, weight, z, words = ctx.saved_tensors
-        act, beta, p, seed = ctx.how
+            return (None,) * 7
         need_x, need_w, need_b, need_r = ctx.needs_input_grad[:4]
         dx = dw = db = None
         if need_x or need_w or need_b:
-            L, device = binding.load(), g.device
-            G, w = _rows(g), _rows(weight)
-            X = None if x is None else _rows(x)
-            rows, (outputs, inputs), kind = math.prod(ctx.shape[:-1]), w.shape, _TYPES[g.dtype]
-            layer = binding.Linear(rows, inputs, outputs, kind, kind if ctx.bias_type is None else _TYPES[ctx.bias_type], act, beta, _drop(p, seed if words is None else words))
-            dx = torch.empty(ctx.shape, dtype=g.dtype, device=device) if need_x else None
-            dw = torch.empty(outputs, inputs, dtype=g.dtype, device=device) if need_w else None
-            db = torch.empty(outputs, dtype=ctx.bias_type, device=device) if need_b else None
-            work, n = _workspace(layer, 1, device)
-            _call(device, L.fs_linear_backward, ctypes.byref(layer), *_at(G), *_at(X), *_at(w), None if z is None else z.data_ptr(), outputs,
-                  None if dx is None else dx.data_ptr(), inputs, None if dw is None else dw.data_ptr(), inputs, None if db is None else db.data_ptr(), None if work is None else work.data_ptr(), n)
-        return dx, dw, db, g if need_r else None, None, None, None, None
+            x, weight, z, words = ctx.saved_tensors
+            plan = ctx.plan
+            G, w, X = _rows(g), _rows(weight), None if x is None else _rows(x)
+            outputs, inputs = weight.shape
+            dx = g.new_empty(ctx.shape) if need_x else None
+            dw = g.new_empty((outputs, inputs)) if need_w else None
+            db = g.new_empty(outputs, dtype=ctx.bias_type) if need_b else None
+            n = plan.bytes[1]
+            work = g.new_empty(n, dtype=torch.uint8) if n else None
+            _call(plan.index, plan.backward, plan.layer(ctx.seed if words is None else words), G.data_ptr(), G.stride(0), None if X is None else X.data_ptr(),
+                  0 if X is None else X.stride(0), w.data_ptr(), w.stride(0), None if z is None else z.data_ptr(), outputs, None if dx is None else dx.data_ptr(), inputs,
+                  None if dw is None else dw.data_ptr(), inputs, None if db is None else db.data_ptr(), None if work is None else work.data_ptr(), n)
+        return dx, dw, db, g if need_r else None, None, None, None
 
 
 def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, activation: str = "none",
@@ -165,42 +172,47 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] =
       activation   "none", "relu", "gelu", "silu", or "softplus": ln(1 + e^(beta z)) / beta
       dropout      the chance of an activation to be dropped (those that are kept are divided by 1 - dropout), of the numbers that `seed` gives"""
     _check_input(x)
-    if x.dim() < 1:
+    kind, device, shape = x.dtype, x.device, x.shape
+    if not shape:
         raise ValueError("x needs a dimension")
-    _check("weight", weight, x, [x.dtype])
-    if weight.dim() != 2 or weight.shape[1] != x.shape[-1]:
-        raise ValueError(f"weight: shape {tuple(weight.shape)}, expected [outputs, {x.shape[-1]}]")
+    _check("weight", weight, x, (kind,))
+    if weight.dim() != 2 or weight.shape[1] != shape[-1]:
+        raise ValueError(f"weight: shape {tuple(weight.shape)}, expected [outputs, {shape[-1]}]")
     outputs = weight.shape[0]
+    bias_kind, y_shape = kind, (*shape[:-1], outputs)
     if bias is not None:
-        _check("bias", bias, x, [x.dtype] if x.dtype == torch.float32 else [x.dtype, torch.float32])
+        _check("bias", bias, x, (kind, torch.float32))
         if bias.shape != (outputs,):
             raise ValueError(f"bias: shape {tuple(bias.shape)}, expected ({outputs},)")
+        bias_kind = bias.dtype
     if residual is not None:
-        _check("residual", residual, x, [x.dtype])
-        if residual.shape[-1:] != (outputs,) or residual.shape[:-1] != x.shape[:-1]:
-            raise ValueError(f"residual: shape {tuple(residual.shape)}, expected {(*x.shape[:-1], outputs)}")
-    if activation not in _ACTS:
+        _check("residual", residual, x, (kind,))
+        if residual.shape != y_shape:
+            raise ValueError(f"residual: shape {tuple(residual.shape)}, expected {y_shape}")
+    act = _ACTS.get(activation)
+    if act is None:
         raise ValueError(f"activation must be one of {', '.join(_ACTS)}, got {activation!r}")
-    act = _ACTS[activation]
-    if act == binding.FS_ACT_SOFTPLUS and not (beta > 0.0 and math.isfinite(beta)):
+    if act != binding.FS_ACT_SOFTPLUS:
+        beta = 1.0
+    elif not (beta > 0.0 and math.isfinite(beta)):
         raise ValueError(f"beta must be positive and finite, got {beta}")
     _check_p("dropout", dropout)
     if dropout > 0.0:
         _check_seed(seed, x)
     else:
         seed = None
+    plan = _plan(device.index, math.prod(shape[:-1]), shape[-1], outputs, _TYPES[kind], _TYPES[bias_kind], act, float(beta), float(dropout))
     if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or bias is not None and bias.requires_grad or residual is not None and residual.requires_grad):
-        return _Linear.apply(x, weight, bias, residual, act, beta, dropout, seed)
-    rows, w = _rows(x), _rows(weight)
-    b = None if bias is None else bias.contiguous()
-    return _forward(_layer(rows, w, b, act, beta, dropout, seed), (*x.shape[:-1], outputs), rows, w, b, None if residual is None else _rows(residual), False)[0]
+        return _Linear.apply(x, weight, bias, residual, plan, y_shape, seed)
+    return _forward(plan, y_shape, x, weight, bias, residual, False, seed)[0]
 
 
 def _dropped(x, residual, p, seed):
-    L, drop = binding.load(), _drop(p, seed)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    y, drop = x.new_empty(x.shape), _drop(p, seed)
     x, r = _rows(x), None if residual is None else _rows(residual)
-    _call(x.device, L.fs_dropout, _TYPES[x.dtype], *x.shape, ctypes.byref(drop), *_at(x), *_at(r), y.data_ptr(), x.shape[1])
+    rows, columns = x.shape
+    _call(x.device.index, binding.load().fs_dropout, _TYPES[x.dtype], rows, columns, ctypes.byref(drop), x.data_ptr(), x.stride(0), None if r is None else r.data_ptr(),
+          0 if r is None else r.stride(0), y.data_ptr(), columns)
     return y
 
 
@@ -233,7 +245,7 @@ def dropout(x: torch.Tensor, p: float, seed: Optional[Seed] = None, residual: Op
     else:
         seed = None
     if residual is not None:
-        _check("residual", residual, x, [x.dtype])
+        _check("residual", residual, x, (x.dtype,))
         if residual.shape != x.shape:
             raise ValueError(f"residual: shape {tuple(residual.shape)}, expected {tuple(x.shape)}")
     if torch.is_grad_enabled() and (x.requires_grad or residual is not None and residual.requires_grad):
