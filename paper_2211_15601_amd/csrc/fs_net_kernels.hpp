@@ -540,13 +540,13 @@ __device__ inline void tile_of(const TilesD &N, int block, int &tp, int &tq)
 }
 
 // D = P Q^T and what becomes of it.  BP x BQ results a block, WP x WQ waves; blockIdx.y: the part of the range of t, `t_part` long.
-template <int TYPE, bool PCOL, bool QCOL, int BP, int BQ, int WP, int WQ>
+template <int TYPE, bool PCOL, bool QCOL, int BP, int BQ, int WP, int WQ, int BUFFERS>
 __global__ __launch_bounds__(64 * WP * WQ) void k_product(MatD P, MatD Q, long long np, long long nq, long long nt, long long t_part, TilesD tiles, EpiD E)
 {
     constexpr int THREADS = 64 * WP * WQ, BT = TYPE == NET_F32 ? 32 : 64, MT = BP / WP / 32, NT = BQ / WQ / 32;
     typedef Stage<TYPE, PCOL, BP, BT, THREADS> StageP;
     typedef Stage<TYPE, QCOL, BQ, BT, THREADS> StageQ;
-    constexpr int BUFFERS = TYPE == NET_F32 ? 1 : 2, TILE = StageP::LDS + StageQ::LDS;      // 16-bit elements
+    constexpr int TILE = StageP::LDS + StageQ::LDS;       // 16-bit elements
     constexpr int END = WP * WQ * end_floats(MT) * 4, BYTES = BUFFERS * TILE * 2 > END ? BUFFERS * TILE * 2 : END;
     __shared__ __attribute__((aligned(1024))) char s_mem[BYTES];
     short *lds = reinterpret_cast<short *>(s_mem);

@@ -2,8 +2,10 @@
 step in one training loop.
 
     python -m paper_2211_15601_amd.fit --steps 100
+    python -m paper_2211_15601_amd.fit --steps 100 --field network --dropout 0.05
 
-The weight grid is a softmax over the bones of a grid of logits (as the paper's skinning network ends); each pose's bones also get a
+The weight grid is a softmax over the bones of logits: a grid of them that is learned itself, or (paper, Sec. 3.2, "Distilling Smooth Skinning Fields") what a
+network, evaluated at the grid's nodes in every step, adds to the field that learning starts from.  Each pose's bones also get a
 learned shift, as where poses come from an estimate.  Every step poses a batch of points with the true field, searches their canonical
 correspondences with the learned one, and pulls the nearest root of each point to where the point came from.  A root near a fold has a
 large inverse Jacobian and a gradient to match: hence the limit on the global norm, which the step applies by itself, and one on each pose's shift
@@ -15,7 +17,7 @@ import argparse
 import numpy as np
 import torch
 
-from . import binding, optim, workloads as wl
+from . import binding, net, optim, workloads as wl
 from .autograd import CorrespondenceSearch
 
 
@@ -32,24 +34,41 @@ def poses(seed, dims, n_points, n_poses):
     return up(wl.weight_grid(dims, a, b)), out
 
 
-def train(steps=100, dims=(16, 16, 4), n_points=4096, n_poses=4, lr=0.05, max_norm=0.01, shift_norm=0.01, seed=0):
+def nodes(dims):
+    """The grid's nodes in -1 .. 1 along each axis, [nx, ny, nz, 3]."""
+    return torch.stack(torch.meshgrid(*[torch.linspace(-1.0, 1.0, n, device="cuda") for n in dims], indexing="ij"), dim=-1).contiguous()
+
+
+def train(steps=100, dims=(16, 16, 4), n_points=4096, n_poses=4, lr=None, max_norm=0.01, shift_norm=0.01, seed=0, field="grid", width=64, hidden=3, dropout=0.0):
     """Returns the losses (mean squared distance of the nearest roots), the gradients' norms, their largest entries, and the optimizer."""
+    if field not in ("grid", "network"):
+        raise ValueError(f"field must be grid or network, got {field!r}")
+    lr = {"grid": 0.05, "network": 2e-3}[field] if lr is None else lr
     W_true, data = poses(seed, dims, n_points, n_poses)
-    logits = (0.25 * (W_true + 1e-4).log()).requires_grad_(True)          # a field that is far too smooth
+    start = 0.25 * (W_true + 1e-4).log()                                   # a field that is far too smooth
+    if field == "grid":
+        learned = [start.requires_grad_(True)]
+        logits_now = lambda: start
+    else:
+        network, at = net.Network(3, width, hidden, wl.N_BONES, dropout=dropout, seed=seed), nodes(dims)
+        learned = network.params
+        # a seed for the run; the offset counts calls of the generator, one for every hidden layer in every step
+        words = torch.tensor([[seed, i] for i in range(hidden)], dtype=torch.int64, device="cuda") if dropout > 0.0 else None
+        logits_now = lambda: start + network(at, words)
     shift = [torch.zeros(wl.N_BONES, 3, device="cuda", requires_grad=True) for _ in data]
-    params = [logits, *shift]
+    params = [*learned, *shift]
     for p in params:                                                       # gradients stay where they are: backward adds, zero_grad clears
         p.grad = torch.zeros_like(p)
     grads, shift_grads = optim.TensorList([p.grad for p in params]), [optim.TensorList([s.grad]) for s in shift]
     fs = binding.Context(dims, wl.N_BONES, wl.BOX_LO, wl.BOX_HI)
     # the shifts go by a fraction of the rate and do not decay; a batch that spoils the gradients is left out
     opt = optim.AdamW(params, lr=lr, weight_decay=0.0, max_norm=max_norm, skip_nonfinite=True,
-                      lr_scales=[1.0] + [0.02] * n_poses, decay_scales=[1.0] + [0.0] * n_poses)
+                      lr_scales=[1.0] * len(learned) + [0.001 / lr] * n_poses, decay_scales=[1.0] * len(learned) + [0.0] * n_poses)
     losses, norms, peaks = [], [], []
     for step in range(steps):
         p = step % n_poses
         B, xq, x = data[p]
-        W = torch.softmax(logits, dim=-1)
+        W = torch.softmax(logits_now(), dim=-1)
         moved = torch.cat([B.view(wl.N_BONES, 3, 4)[..., :3], B.view(wl.N_BONES, 3, 4)[..., 3:] + shift[p][..., None]], dim=-1)
         roots, conv = CorrespondenceSearch.apply(fs, W, moved.reshape(1, wl.N_BONES, 12), xq, None)
         far = ((roots - x) ** 2).sum(1).masked_fill(conv == 0, torch.inf)  # [K,N]
@@ -61,6 +80,8 @@ def train(steps=100, dims=(16, 16, 4), n_points=4096, n_poses=4, lr=0.05, max_no
         shift_grads[p].clip_grads(shift_norm)
         norms.append(opt.step())
         opt.zero_grad()
+        if field == "network" and words is not None:
+            words[:, 1] += hidden
         losses.append(loss.detach())
     return torch.stack(losses).tolist(), torch.cat(norms).tolist(), torch.cat(peaks).tolist(), opt
 
@@ -70,8 +91,10 @@ def main():
     ap.add_argument("--steps", type=int, default=100)
     ap.add_argument("--points", type=int, default=4096)
     ap.add_argument("--max-norm", type=float, default=0.01)
+    ap.add_argument("--field", choices=("grid", "network"), default="grid")
+    ap.add_argument("--dropout", type=float, default=0.0, help="chance of a hidden unit of the network to be dropped")
     args = ap.parse_args()
-    losses, norms, peaks, opt = train(args.steps, n_points=args.points, max_norm=args.max_norm)
+    losses, norms, peaks, opt = train(args.steps, n_points=args.points, max_norm=args.max_norm, field=args.field, dropout=args.dropout)
     for i in range(0, len(losses), max(1, len(losses) // 10)):
         print(f"step {i:4d}: loss {losses[i]:.3e}, gradient norm {norms[i]:.3e}, largest {peaks[i]:.3e}")
     print(f"last: loss {losses[-1]:.3e}; {sum(n > args.max_norm for n in norms)} of {len(norms)} steps clipped, {int(opt.step_count)} taken")

@@ -5,6 +5,9 @@ include/fastsnarf_net.h: matrix products with bias, activation, dropout and resi
     y = linear(y, weight, bias, residual=y, activation="gelu", dropout=0.1, seed=words)
     y = dropout(y, 0.1, words)
 
+    field = Network(3, 64, 2, n_bones, dropout=0.1)                                 # layers of them: the skinning network of fit.py
+    logits = field(nodes, words)
+
 Tensors are float32, bfloat16 or float16 on one GPU, all of one type but the bias, which may be float32.  Dropout draws its numbers from a counter:
 `seed` is a pair of integers (seed, offset), or an int64 tensor of those two words on the GPU, which is read when the kernels run (a captured graph that
 counts the offset up drops other elements at each replay).  The same words drop the same elements, so every call of a step gets an offset of its own.
@@ -251,3 +254,33 @@ def dropout(x: torch.Tensor, p: float, seed: Optional[Seed] = None, residual: Op
     if torch.is_grad_enabled() and (x.requires_grad or residual is not None and residual.requires_grad):
         return _Dropout.apply(x, residual, p, seed)
     return _dropped(x, residual, p, seed)
+
+
+class Network:
+    """Layers of linear(): `inputs` to `width`, `hidden` - 1 times `width` to `width` with the layer's input as residual, then `width` to `outputs` without an
+    activation.  .params: weights and biases in turn, leaves that require gradients; the last weight starts at zero, so that the network does.
+
+    network(x, words): x [..., inputs]; words: with dropout, where it is wanted, one row of two words (seed, offset) for every hidden layer (an int64
+    tensor [hidden, 2] on the GPU); None: nothing is dropped."""
+
+    def __init__(self, inputs: int, width: int, hidden: int, outputs: int, activation: str = "softplus", beta: float = 10.0, dropout: float = 0.0,
+                 dtype: torch.dtype = torch.float32, device="cuda", seed: int = 0):
+        if min(inputs, width, hidden, outputs) < 1:
+            raise ValueError("a network needs a hidden layer or more, and sizes of 1 or more")
+        if activation not in _ACTS:
+            raise ValueError(f"activation must be one of {', '.join(_ACTS)}, got {activation!r}")
+        _check_p("dropout", dropout)
+        gen = torch.Generator().manual_seed(seed)
+        self.hidden, self.how, self.dropout, self.params = hidden, dict(activation=activation, beta=beta), dropout, []
+        sizes = [inputs] + [width] * hidden + [outputs]
+        for i, (k, n) in enumerate(zip(sizes, sizes[1:])):
+            w = torch.randn(n, k, generator=gen) * (math.sqrt(2.0 / k) if i < hidden else 0.0)
+            self.params += [w.to(device, dtype).requires_grad_(True), torch.zeros(n, dtype=dtype, device=device, requires_grad=True)]
+
+    def __call__(self, x: torch.Tensor, words: Optional[torch.Tensor] = None) -> torch.Tensor:
+        if words is not None and self.dropout > 0.0 and tuple(words.shape) != (self.hidden, 2):
+            raise ValueError(f"words: shape {tuple(words.shape)}, expected ({self.hidden}, 2)")
+        p = 0.0 if words is None else self.dropout
+        for i in range(self.hidden):
+            x = linear(x, *self.params[2 * i:2 * i + 2], residual=x if i else None, dropout=p, seed=words[i] if p > 0.0 else None, **self.how)
+        return linear(x, *self.params[-2:])
