@@ -160,7 +160,7 @@ Plan plan_product(int type, int64_t np, int64_t nq, int64_t nt, int cus, bool la
     p.tiles_p = tiles(np, p.tile);
     p.tiles_q = tiles(nq, p.tile);
     const long long all = std::max(1ll, p.tiles_p * p.tiles_q);
-    const long long wanted = p.tile == 256 ? std::max(1ll, cus / all) : std::min((2ll * cus + all - 1) / all, std::max<long long>(1, nt / 256));
+    const long long wanted = p.tile == 256 ? std::max(1ll, cus / all) : 4 * all >= 3 * cus ? 1 : std::min((2ll * cus + all - 1) / all, std::max<long long>(1, nt / 256));
     p.t_part = std::max(bt, ((long long)nt + wanted - 1) / wanted);
     p.t_part = (p.t_part + bt - 1) / bt * bt;
     p.parts = (int)std::max<long long>(1, (nt + p.t_part - 1) / p.t_part);
@@ -197,15 +197,15 @@ void launch_product(const Plan &p, const MatD &P, const MatD &Q, int64_t np, int
     const dim3 grid((unsigned)(tiles_p * tiles_q), (unsigned)p.parts);
     constexpr int BUFFERS = TYPE == NET_F32 ? 1 : 2;
     if (p.tile < 128) {
-        k_product<TYPE, PCOL, QCOL, 64, 64, 2, 2, BUFFERS><<<grid, 256, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
+        k_product<TYPE, PCOL, QCOL, 64, 64, 2, 2, 2, TYPE == NET_F32 ? 2 : 4><<<grid, 256, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
         return;
     }
     if constexpr (BUFFERS == 2 && !PCOL)
         if (nt <= SHORT_T) {
-            k_product<TYPE, PCOL, QCOL, 128, 128, 2, 2, 1><<<grid, 256, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
+            k_product<TYPE, PCOL, QCOL, 128, 128, 2, 2, 1, 1><<<grid, 256, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
             return;
         }
-    k_product<TYPE, PCOL, QCOL, 128, 128, 2, 2, BUFFERS><<<grid, 256, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
+    k_product<TYPE, PCOL, QCOL, 128, 128, 2, 2, BUFFERS, 1><<<grid, 256, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
 }
 
 template <int TYPE>

@@ -401,22 +401,37 @@ template <int TYPE, bool COL, int B, int BT, int THREADS> struct Stage {
     static_assert(THREADS % PER_ROW == 0, "tile");
     Packed<TYPE, 8> chunk[N];
 
-    // b0: first row or column p; t0: first t; t1: end of the range of t.  Addresses are a wave's and a lane's part, of which the latter stays the same.
+    // Where a thread's chunks of the tile that begins at row or column b0 lie, from its first element on.  Rows beyond the matrix: the last one, whose results go nowhere.
+    struct Own { long long at[COL ? 1 : N]; };
+    static __device__ inline Own own(const MatD &M, long long b0, int tid)
+    {
+        Own o;
+        const int r = tid / PER_ROW, c = tid % PER_ROW * 8;
+        if constexpr (COL) o.at[0] = r * M.ld + c;
+        else
+#pragma unroll
+            for (int i = 0; i < N; ++i) o.at[i] = (b0 + r + i * APART < M.rows ? r + i * APART : M.rows - 1 - b0) * M.ld + c;
+        return o;
+    }
+
+    // A tile of whole t, and, COL, whole chunks.  Addresses are a wave's and a lane's part, of which the latter stays the same.
+    __device__ inline void fast(const MatD &M, long long b0, long long t0, const Own &o)
+    {
+        const T *at = static_cast<const T *>(M.at) + (COL ? t0 * M.ld + b0 : b0 * M.ld + t0);
+#pragma unroll
+        for (int i = 0; i < N; ++i) chunk[i] = load_all<TYPE, 8>(COL ? at + i * APART * M.ld + o.at[0] : at + o.at[COL ? 0 : i]);
+    }
+
+    // Any tile.  b0: first row or column p; t0: first t; t1: end of the range of t.
     __device__ inline void load(const MatD &M, long long b0, long long t0, long long t1, int tid)
     {
         const long long r0 = COL ? t0 : b0, c0 = COL ? b0 : t0, rows = COL ? t1 : M.rows, cols = COL ? M.cols : t1;
-        const T *at = static_cast<const T *>(M.at) + r0 * M.ld + c0;
-        const long long own = tid / PER_ROW * M.ld + tid % PER_ROW * 8;
-        if (r0 + ROWS <= rows && c0 + COLS <= cols) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) chunk[i] = load_all<TYPE, 8>(at + i * APART * M.ld + own);
-            return;
-        }
-        const long long c = c0 + tid % PER_ROW * 8, left = cols - c;
+        const T *at = static_cast<const T *>(M.at) + r0 * M.ld + c0 + (tid / PER_ROW * M.ld + tid % PER_ROW * 8);
+        const long long left = cols - (c0 + tid % PER_ROW * 8);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             chunk[i] = Packed<TYPE, 8>();
-            if (r0 + tid / PER_ROW + i * APART < rows && left > 0) chunk[i] = load_some<TYPE, 8>(at + i * APART * M.ld + own, left < 8 ? (int)left : 8);
+            if (r0 + tid / PER_ROW + i * APART < rows && left > 0) chunk[i] = load_some<TYPE, 8>(at + i * APART * M.ld, left < 8 ? (int)left : 8);
         }
     }
 
@@ -540,7 +555,7 @@ __device__ inline void tile_of(const TilesD &N, int block, int &tp, int &tq)
 }
 
 // D = P Q^T and what becomes of it.  BP x BQ results a block, WP x WQ waves; blockIdx.y: the part of the range of t, `t_part` long.
-template <int TYPE, bool PCOL, bool QCOL, int BP, int BQ, int WP, int WQ, int BUFFERS>
+template <int TYPE, bool PCOL, bool QCOL, int BP, int BQ, int WP, int WQ, int BUFFERS, int AHEAD>
 __global__ __launch_bounds__(64 * WP * WQ) void k_product(MatD P, MatD Q, long long np, long long nq, long long nt, long long t_part, TilesD tiles, EpiD E)
 {
     constexpr int THREADS = 64 * WP * WQ, BT = TYPE == NET_F32 ? 32 : 64, MT = BP / WP / 32, NT = BQ / WQ / 32;
@@ -565,19 +580,6 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_product(MatD P, MatD Q, long l
 #pragma unroll
             for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.0f;
 
-    StageP sp;
-    StageQ sq;
-    if (t0 < t1) {
-        sp.load(P, p0, t0, t1, tid);
-        sq.load(Q, q0, t0, t1, tid);
-        sp.store(lds, tid);
-        sq.store(lds + StageP::LDS, tid);
-    }
-    __syncthreads();
-    if (BUFFERS == 2 && t0 + BT < t1) {
-        sp.load(P, p0, t0 + BT, t1, tid);
-        sq.load(Q, q0, t0 + BT, t1, tid);
-    }
     int buffer = 0;
     auto compute = [&](int s) {
         const short *bp = lds + buffer * TILE, *bq = bp + StageP::LDS;
@@ -608,36 +610,79 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_product(MatD P, MatD Q, long l
             }
         }
     };
-    for (long long t = t0; t < t1; t += BT) {
-        const bool more = t + BT < t1;
-        if constexpr (BUFFERS == 2) {
-            // the next tile's writes to LDS and the loads of the one behind it among the products of this one
+    const int whole = (int)((t1 - t0) / BT);
+    const bool rest = t0 + (long long)whole * BT < t1;
+    constexpr bool EARLY = BP * BQ <= 64 * 64;          // what is left of t is asked for first, where registers allow, and used last
+    StageP rest_p;
+    StageQ rest_q;
+    if (EARLY && rest) {
+        rest_p.load(P, p0, t0 + (long long)whole * BT, t1, tid);
+        rest_q.load(Q, q0, t0 + (long long)whole * BT, t1, tid);
+    }
+    // AHEAD tiles on their way to registers, one or two in LDS.  EDGE: tiles that lie partly beyond the matrix along p or q in memory
+    auto run = [&](auto edge) {
+        constexpr bool EDGE = decltype(edge)::value;
+        StageP sp[AHEAD];
+        StageQ sq[AHEAD];
+        const auto own_p = StageP::own(P, p0, tid);
+        const auto own_q = StageQ::own(Q, q0, tid);
+        // without a condition, so that the compiler can count the loads on their way: behind the last tile that one again, for nobody
+        auto ask = [&](int k, StageP &x, StageQ &y) {
+            const long long t = t0 + (long long)(k < whole ? k : whole - 1) * BT;
+            if constexpr (EDGE && PCOL) x.load(P, p0, t, t1, tid);
+            else x.fast(P, p0, t, own_p);
+            if constexpr (EDGE && QCOL) y.load(Q, q0, t, t1, tid);
+            else y.fast(Q, q0, t, own_q);
+        };
+        auto put = [&](int k, StageP &x, StageQ &y, int to) {
+            x.store(lds + to * TILE, tid);
+            y.store(lds + to * TILE + StageP::LDS, tid);
+            ask(k + AHEAD, x, y);
+        };
 #pragma unroll
-            for (int s = 0; s < BT / 32; ++s) compute(s);
-            if (more) {
-                sp.store(lds + (buffer ^ 1) * TILE, tid);
-                sq.store(lds + (buffer ^ 1) * TILE + StageP::LDS, tid);
-            }
-            if (t + 2 * BT < t1) {
-                sp.load(P, p0, t + 2 * BT, t1, tid);
-                sq.load(Q, q0, t + 2 * BT, t1, tid);
-            }
+        for (int k = 0; k < AHEAD; ++k) ask(k, sp[k], sq[k]);
+        put(0, sp[0], sq[0], 0);
+        __syncthreads();
+        for (int k0 = 0; k0 < whole; k0 += AHEAD) {
 #pragma unroll
-            for (int s = BT / 32; s < BT / 16; ++s) compute(s);
-            buffer ^= 1;
-        } else {
-            if (more) {
-                sp.load(P, p0, t + BT, t1, tid);
-                sq.load(Q, q0, t + BT, t1, tid);
-            }
+            for (int j = 0; j < AHEAD; ++j) {
+                const int k = k0 + j;
+                if (k >= whole) break;
+                StageP &np = sp[(j + 1) % AHEAD];
+                StageQ &nq = sq[(j + 1) % AHEAD];
+                if constexpr (BUFFERS == 2) {
+                    // the next tile's writes to LDS among the products of this one
 #pragma unroll
-            for (int s = 0; s < BT / 16; ++s) compute(s);
-            __syncthreads();
-            if (more) {
-                sp.store(lds, tid);
-                sq.store(lds + StageP::LDS, tid);
+                    for (int s = 0; s < BT / 32; ++s) compute(s);
+                    put(k + 1, np, nq, buffer ^ 1);
+#pragma unroll
+                    for (int s = BT / 32; s < BT / 16; ++s) compute(s);
+                    buffer ^= 1;
+                } else {
+#pragma unroll
+                    for (int s = 0; s < BT / 16; ++s) compute(s);
+                    __syncthreads();
+                    put(k + 1, np, nq, 0);
+                }
+                __syncthreads();
             }
         }
+    };
+    if (whole > 0) {
+        if ((PCOL && p0 + BP > P.cols) || (QCOL && q0 + BQ > Q.cols)) run(Int<1>());
+        else run(Int<0>());
+    }
+    if (rest) {
+        if (!EARLY) {
+            rest_p.load(P, p0, t0 + (long long)whole * BT, t1, tid);
+            rest_q.load(Q, q0, t0 + (long long)whole * BT, t1, tid);
+        }
+        buffer = 0;
+        rest_p.store(lds, tid);
+        rest_q.store(lds + StageP::LDS, tid);
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < BT / 16; ++s) compute(s);
         __syncthreads();
     }
 
