@@ -206,11 +206,12 @@ template <int N> __device__ inline void drop(float *v, unsigned long long e, con
 __device__ inline float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 __device__ inline float fast_rcp(float x) { return __builtin_amdgcn_rcpf(x); }
 
-// ln(1 + u) of 0 <= u <= 1: with w the rounded 1 + u, ln(w) u / (w - 1); the quotient takes out what rounding changed in w.
+// ln(1 + u) of 0 <= u <= 1: ln of the rounded 1 + u, and what that rounding left out, at most 2^-24, times the slope 1 / (1 + u), for which 1 - u / 2 is near
+// enough: it is off by u / 4 of that at most, 2^-26 of the result.
 __device__ inline float log_of_one_more(float u)
 {
     const float w = 1.0f + u, d = w - 1.0f;
-    return d == 0.0f ? u : __builtin_amdgcn_logf(w) * 0.693147181f * (u * fast_rcp(d));
+    return __builtin_fmaf(__builtin_amdgcn_logf(w), 0.693147181f, (u - d) * __builtin_fmaf(d, -0.5f, 1.0f));
 }
 
 // Phi(z), and e^(-z^2/2), which it is made from: with u = |z| and t = 1 / (1 + 0.3 u), Phi(-u) = e^(-u^2/2) (t c0 + t^2 c1 + .. + t^10 c9), a polynomial fitted to
@@ -292,36 +293,60 @@ template <int TYPE> __device__ inline void load_bias(float *b, const EpiD &E, lo
     }
 }
 
-// Four results of row q from p on, of which n (1 .. 4) are in the matrix; cols: of the matrix; r: their residual.
-template <int TYPE, int ACT> __device__ inline void finish4(float *v, const float *bias, const Packed<TYPE, 4> &r, const EpiD &E, const Seed &seed, long long q, long long p, int n, long long cols)
+// Where a lane's results go, and what joins them there: addresses of one row, and of others by whole numbers of rows.
+template <int TYPE> struct Place {
+    typedef typename ElemOf<TYPE>::type T;
+    T *out;
+    char *z;
+    const T *r;
+    long long ldo, ldz, ldr;
+    int zs;
+
+    __device__ inline Place(const EpiD &E, long long q, long long p, int part)
+    {
+        zs = TYPE == NET_F32 || E.bias_f32 ? 4 : 2;
+        ldo = E.ldo;
+        ldz = E.ldz * zs;
+        ldr = E.ldr;
+        if (E.mode == EPI_PART) out = reinterpret_cast<T *>(static_cast<float *>(E.out) + part * E.part_stride + q * E.ldo + p);
+        else out = static_cast<T *>(E.out) + q * E.ldo + p;
+        z = E.z ? static_cast<char *>(E.z) + q * ldz + p * zs : nullptr;
+        r = E.r ? static_cast<const T *>(E.r) + q * E.ldr + p : nullptr;
+    }
+};
+
+// Four results, of which n (1 .. 4) are in the matrix, `rows` rows behind the place; e: the first one's number for drop(); r: their residual.
+template <int TYPE, int ACT>
+__device__ inline void finish4(float *v, const float *bias, const Packed<TYPE, 4> &r, const EpiD &E, const Seed &seed, const Place<TYPE> &at, int rows, unsigned long long e, int n)
 {
     typedef typename ElemOf<TYPE>::type T;
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] += bias[i];
     if (E.z) {
-        if (E.bias_f32) store_some<NET_F32, 4>(static_cast<float *>(E.z) + q * E.ldz + p, v, n);
-        else store_some<TYPE, 4>(static_cast<T *>(E.z) + q * E.ldz + p, v, n);
+        char *z = at.z + rows * at.ldz;
+        if (E.bias_f32) store_some<NET_F32, 4>(reinterpret_cast<float *>(z), v, n);
+        else store_some<TYPE, 4>(reinterpret_cast<T *>(z), v, n);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = act_of<ACT>(v[i], E.beta, E.over_beta);
-    drop<4>(v, (unsigned long long)q * cols + p, E.drop, seed);
+    drop<4>(v, e, E.drop, seed);
     if (E.r)
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] += r.wide(i);
-    store_some<TYPE, 4>(static_cast<T *>(E.out) + q * E.ldo + p, v, n);
+    store_some<TYPE, 4>(at.out + rows * at.ldo, v, n);
 }
 
-template <int TYPE> __device__ inline Packed<TYPE, 4> residual4(const EpiD &E, long long q, long long p, int n)
+template <int TYPE> __device__ inline Packed<TYPE, 4> residual4(const EpiD &E, const Place<TYPE> &at, int rows, int n)
 {
     Packed<TYPE, 4> r = {};
-    if (E.r) r = load_some<TYPE, 4>(static_cast<const typename ElemOf<TYPE>::type *>(E.r) + q * E.ldr + p, n);
+    if (E.r) r = load_some<TYPE, 4>(at.r + rows * at.ldr, n);
     return r;
 }
 
-template <int TYPE> __device__ inline void plain4(const float *v, const EpiD &E, long long q, long long p, int n, int part)
+template <int TYPE> __device__ inline void plain4(const float *v, const EpiD &E, const Place<TYPE> &at, int rows, int n)
 {
-    if (E.mode == EPI_PART) store_some<NET_F32, 4>(static_cast<float *>(E.out) + part * E.part_stride + q * E.ldo + p, v, n);
-    else store_some<TYPE, 4>(static_cast<typename ElemOf<TYPE>::type *>(E.out) + q * E.ldo + p, v, n);
+    if (E.mode == EPI_PART) store_some<NET_F32, 4>(reinterpret_cast<float *>(at.out) + rows * at.ldo, v, n);
+    else store_some<TYPE, 4>(at.out + rows * at.ldo, v, n);
 }
 
 // ---------------------------------------------------------------------------------------------------------------- products
@@ -506,34 +531,36 @@ __device__ inline void product_end(const f32x16 (&acc)[MT][NT], float *out, int 
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         constexpr int STEP = 64 / (PW / 4), PASSES = 32 / STEP, AHEAD = 4;
         const long long p = p0 + h / NT * PW + col, q1 = q0 + h % NT * 32 + lane / (PW / 4);
-        const int n = np - p < 4 ? (int)(np - p) : 4;
+        const int n = np - p < 4 ? (int)(np - p) : 4, rows = nq - q1 < 32 ? (int)(nq - q1) : 32;      // of which this lane has every STEP-th
         const float *in = out + lane / (PW / 4) * PITCH + col;
+        const Place<TYPE> at(E, q1, p, part);
         if (n > 0 && LAYER && E.mode == EPI_LAYER) {
             float bias[4];
             load_bias<TYPE>(bias, E, p, n);
+            const unsigned long long e = (unsigned long long)q1 * np + p;
             with_act(E.act, [&](auto act) {
 #pragma unroll 1
                 for (int r = 0; r < PASSES; r += AHEAD) {
                     Packed<TYPE, 4> res[AHEAD];
 #pragma unroll
                     for (int a = 0; a < AHEAD; ++a)
-                        if (q1 + (r + a) * STEP < nq) res[a] = residual4<TYPE>(E, q1 + (r + a) * STEP, p, n);
+                        if ((r + a) * STEP < rows) res[a] = residual4<TYPE>(E, at, (r + a) * STEP, n);
 #pragma unroll
                     for (int a = 0; a < AHEAD; ++a)
-                        if (q1 + (r + a) * STEP < nq) {
+                        if ((r + a) * STEP < rows) {
                             const f32x4 x = *reinterpret_cast<const f32x4 *>(in + (r + a) * STEP * PITCH);
                             float v[4] = {x[0], x[1], x[2], x[3]};
-                            finish4<TYPE, decltype(act)::value>(v, bias, res[a], E, seed, q1 + (r + a) * STEP, p, n, np);
+                            finish4<TYPE, decltype(act)::value>(v, bias, res[a], E, seed, at, (r + a) * STEP, e + (unsigned long long)((r + a) * STEP) * np, n);
                         }
                 }
             });
         } else if (n > 0)
 #pragma unroll
             for (int r = 0; r < PASSES; ++r)
-                if (q1 + r * STEP < nq) {
+                if (r * STEP < rows) {
                     const f32x4 x = *reinterpret_cast<const f32x4 *>(in + r * STEP * PITCH);
                     const float v[4] = {x[0], x[1], x[2], x[3]};
-                    plain4<TYPE>(v, E, q1 + r * STEP, p, n, part);
+                    plain4<TYPE>(v, E, at, r * STEP, n);
                 }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -858,10 +885,11 @@ template <int TYPE, bool SPLIT> __global__ __launch_bounds__(256) void k_parts(c
     for (long long b = blockIdx.x * each + (SPLIT ? 0 : wave); b < all; b += gridDim.x * each) {
         const long long q = b / strips, p = b % strips * 256 + 4 * lane;
         const int n = np - p < 4 ? (int)(np - p) : 4;
+        const Place<TYPE> to(E, q, p, 0);
         f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
         Packed<TYPE, 4> r = {};
         if (n > 0) {
-            if (!SPLIT || wave == 0) r = residual4<TYPE>(E, q, p, n);
+            if (!SPLIT || wave == 0) r = residual4<TYPE>(E, to, 0, n);
             const float *at = part + q * ldp + p;              // ldp is a multiple of 4
 #pragma unroll 8
             for (int i = first; i < parts; i += step) sum += *reinterpret_cast<const f32x4 *>(at + i * part_stride);
@@ -876,8 +904,8 @@ template <int TYPE, bool SPLIT> __global__ __launch_bounds__(256) void k_parts(c
             float v[4] = {sum[0], sum[1], sum[2], sum[3]}, bias[4];
             if (E.mode == EPI_LAYER) {
                 load_bias<TYPE>(bias, E, p, n);
-                with_act(E.act, [&](auto act) { finish4<TYPE, decltype(act)::value>(v, bias, r, E, seed, q, p, n, np); });
-            } else plain4<TYPE>(v, E, q, p, n, 0);
+                with_act(E.act, [&](auto act) { finish4<TYPE, decltype(act)::value>(v, bias, r, E, seed, to, 0, (unsigned long long)q * np + p, n); });
+            } else plain4<TYPE>(v, E, to, 0, n);
         }
         if constexpr (SPLIT) __syncthreads();
     }
@@ -911,7 +939,8 @@ __global__ __launch_bounds__(1024) void k_few(MatD W, MatD X, long long np, long
     float bias[4];
     load_bias<TYPE>(bias, E, p, n);
     Packed<TYPE, 4> r = {};
-    if (n > 0) r = residual4<TYPE>(E, q, p, n);
+    const Place<TYPE> to(E, q, p, 0);
+    if (n > 0) r = residual4<TYPE>(E, to, 0, n);
     f32x4 acc[NQ];
 #pragma unroll
     for (int j = 0; j < NQ; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -967,7 +996,7 @@ __global__ __launch_bounds__(1024) void k_few(MatD W, MatD X, long long np, long
         for (int i = 0; i < 4; ++i)
             if (i < n && !(fabsf(v[i]) < INFINITY)) v[i] = plain_dot(static_cast<const float *>(W.at) + (p + i) * W.ld, 1, static_cast<const float *>(X.at) + q * X.ld, 1, nt);
     }
-    with_act(E.act, [&](auto act) { finish4<TYPE, decltype(act)::value>(v, bias, r, E, seed, q, p, n, np); });
+    with_act(E.act, [&](auto act) { finish4<TYPE, decltype(act)::value>(v, bias, r, E, seed, to, 0, (unsigned long long)q * np + p, n); });
 }
 
 // ---------------------------------------------------------------------------------------------------------------- narrow layers
