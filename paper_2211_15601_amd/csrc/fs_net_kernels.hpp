@@ -393,22 +393,26 @@ template <bool COL, int B, int BT> __device__ inline s16x8 operand(const short *
 
 // Three bf16 parts of fp32 numbers: x = h + m + l to 24 bits and more, each part the rounded rest of those before it.  A rest that is no number
 // (of infinities) gives results that are none either, which k_product computes again.
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 __device__ inline void split8(const Packed<NET_F32, 8> &x, s16x8 *part)
 {
+    unsigned w[3][4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const __bf16 h = (__bf16)x.wide(i);
-        const float rest = x.wide(i) - (float)h;
-        const __bf16 m = (__bf16)rest;
-        const __bf16 l = (__bf16)(rest - (float)m);
-        part[0][i] = __builtin_bit_cast(short, h);
-        part[1][i] = __builtin_bit_cast(short, m);
-        part[2][i] = __builtin_bit_cast(short, l);
+    for (int i = 0; i < 4; ++i) {                      // two at a time, as the conversion does them
+        f32x2 v = {x.wide(2 * i), x.wide(2 * i + 1)};
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            w[k][i] = __builtin_bit_cast(unsigned, __builtin_convertvector(v, bf16x2));
+            v = f32x2{v.x - __uint_as_float(w[k][i] << 16), v.y - __uint_as_float(w[k][i] & 0xFFFF0000u)};
+        }
     }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) part[k] = __builtin_bit_cast(s16x8, u32x4{w[k][0], w[k][1], w[k][2], w[k][3]});
 }
 
 // A result that is no finite number may be one of the parts' making (inf - inf, or a part of the largest numbers rounded up to infinity): it is computed plainly, then.
-__device__ __attribute__((noinline)) float plain_dot(const float *x, long long step_x, const float *y, long long step_y, long long n)
+__device__ inline float plain_dot(const float *x, long long step_x, const float *y, long long step_y, long long n)
 {
     float sum = 0.0f;
     for (long long t = 0; t < n; ++t) sum = __builtin_fmaf(x[t * step_x], y[t * step_y], sum);
@@ -503,11 +507,11 @@ template <int TYPE, bool COL, int B, int BT, int THREADS> struct Stage {
 };
 
 // The end of a product: a wave's results, MT by NT squares from (p0, q0) on, go through LDS (end_floats(MT) of its own), 32 rows q and up to 64 p at a time,
-// so that rows leave in whole lines.
+// so that rows leave in whole lines.  fp32: a result that is no finite number is what again(q, p) says.
 constexpr __host__ __device__ int end_floats(int mt) { return 32 * ((mt > 1 ? 64 : 32) + 4); }
 
-template <int TYPE, bool LAYER, int MT, int NT>
-__device__ inline void product_end(const f32x16 (&acc)[MT][NT], float *out, int lane, long long p0, long long q0, long long np, long long nq, int part, const EpiD &E)
+template <int TYPE, bool LAYER, int MT, int NT, class Again>
+__device__ inline void product_end(const f32x16 (&acc)[MT][NT], float *out, int lane, long long p0, long long q0, long long np, long long nq, int part, const EpiD &E, Again again)
 {
     constexpr int MG = MT > 1 ? 2 : 1, PW = 32 * MG, PITCH = PW + 4;
     static_assert(MT % MG == 0, "squares");
@@ -515,6 +519,7 @@ __device__ inline void product_end(const f32x16 (&acc)[MT][NT], float *out, int 
     const Seed seed = seed_of(E.drop);
 #pragma unroll 1
     for (int h = 0; h < NT * (MT / MG); ++h) {
+        bool bad = false;
 #pragma unroll
         for (int k = 0; k < NT * (MT / MG); ++k)           // a register's number is fixed
             if (k == h)
@@ -525,7 +530,16 @@ __device__ inline void product_end(const f32x16 (&acc)[MT][NT], float *out, int 
                         const f32x16 &x = acc[k / NT * MG + i][k % NT];
                         f32x4 v = {x[4 * g], x[4 * g + 1], x[4 * g + 2], x[4 * g + 3]};
                         *reinterpret_cast<f32x4 *>(out + (lane & 31) * PITCH + 32 * i + 8 * g + 4 * (lane >> 5)) = v;
+                        if constexpr (TYPE == NET_F32)
+#pragma unroll
+                            for (int m = 0; m < 4; ++m) bad |= !(fabsf(v[m]) < INFINITY);
                     }
+        if (TYPE == NET_F32 && __any(bad))
+            for (int i = 0; i < 16 * MG; ++i) {        // each lane those that it wrote
+                float *x = out + (lane & 31) * PITCH + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3);
+                const long long q = q0 + h % NT * 32 + (lane & 31), p = p0 + h / NT * PW + (x - out - (lane & 31) * PITCH);
+                if (!(fabsf(*x) < INFINITY) && p < np && q < nq) *x = again(q, p);
+            }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
@@ -555,7 +569,7 @@ __device__ inline void product_end(const f32x16 (&acc)[MT][NT], float *out, int 
                 }
             });
         } else if (n > 0)
-#pragma unroll
+#pragma unroll 2
             for (int r = 0; r < PASSES; ++r)
                 if (r * STEP < rows) {
                     const f32x4 x = *reinterpret_cast<const f32x4 *>(in + r * STEP * PITCH);
@@ -583,7 +597,7 @@ __device__ inline void tile_of(const TilesD &N, int block, int &tp, int &tq)
 
 // D = P Q^T and what becomes of it.  BP x BQ results a block, WP x WQ waves; blockIdx.y: the part of the range of t, `t_part` long.
 template <int TYPE, bool PCOL, bool QCOL, int BP, int BQ, int WP, int WQ, int BUFFERS, int AHEAD>
-__global__ __launch_bounds__(64 * WP * WQ) void k_product(MatD P, MatD Q, long long np, long long nq, long long nt, long long t_part, TilesD tiles, EpiD E)
+__global__ __launch_bounds__(64 * WP * WQ, TYPE == NET_F32 && BP * BQ == 128 * 128 ? 3 : 1) void k_product(MatD P, MatD Q, long long np, long long nq, long long nt, long long t_part, TilesD tiles, EpiD E)
 {
     constexpr int THREADS = 64 * WP * WQ, BT = TYPE == NET_F32 ? 32 : 64, MT = BP / WP / 32, NT = BQ / WQ / 32;
     typedef Stage<TYPE, PCOL, BP, BT, THREADS> StageP;
@@ -611,30 +625,23 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_product(MatD P, MatD Q, long l
     auto compute = [&](int s) {
         const short *bp = lds + buffer * TILE, *bq = bp + StageP::LDS;
         constexpr int PL = StageP::PLANES;
-        s16x8 a[MT][PL], b[NT][PL];
+        s16x8 a[MT][PL];
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int k = 0; k < PL; ++k) a[i][k] = operand<PCOL, BP, BT>(bp + k * BP * BT, (wp * MT + i) * 32, s, lane);
+        // of three parts each the six products that reach 2^-16 of the largest, the smaller parts of Q first
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+        for (int y = PL - 1; y >= 0; --y) {
+            s16x8 b[NT];
 #pragma unroll
-            for (int k = 0; k < PL; ++k) b[j][k] = operand<QCOL, BQ, BT>(bq + k * BQ * BT, (wq * NT + j) * 32, s, lane);
-        if constexpr (PL == 1) {
+            for (int j = 0; j < NT; ++j) b[j] = operand<QCOL, BQ, BT>(bq + y * BQ * BT, (wq * NT + j) * 32, s, lane);
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = mfma<TYPE>(a[i][0], b[j][0], acc[i][j]);
-        } else {
-            // the six products of parts that reach 2^-16 of the largest, the small ones first
-#pragma unroll
-            for (int u = 0; u < 6; ++u) {
-                constexpr int PA[6] = {0, 1, 2, 0, 1, 0}, PB[6] = {2, 1, 0, 1, 0, 0};
+            for (int x = PL - 1 - y; x >= 0; --x)
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
 #pragma unroll
-                    for (int j = 0; j < NT; ++j) acc[i][j] = mfma<TYPE>(a[i][PA[u]], b[j][PB[u]], acc[i][j]);
-            }
+                    for (int j = 0; j < NT; ++j) acc[i][j] = mfma<TYPE>(a[i][x], b[j], acc[i][j]);
         }
     };
     const int whole = (int)((t1 - t0) / BT);
@@ -700,35 +707,26 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_product(MatD P, MatD Q, long l
         else run(Int<0>());
     }
     if (rest) {
-        if (!EARLY) {
-            rest_p.load(P, p0, t0 + (long long)whole * BT, t1, tid);
-            rest_q.load(Q, q0, t0 + (long long)whole * BT, t1, tid);
-        }
         buffer = 0;
-        rest_p.store(lds, tid);
-        rest_q.store(lds + StageP::LDS, tid);
+        if (EARLY) {
+            rest_p.store(lds, tid);
+            rest_q.store(lds + StageP::LDS, tid);
+        } else {
+            StageP::bring(P, p0, t0 + (long long)whole * BT, t1, lds, tid);
+            StageQ::bring(Q, q0, t0 + (long long)whole * BT, t1, lds + StageP::LDS, tid);
+        }
         __syncthreads();
 #pragma unroll
         for (int s = 0; s < BT / 16; ++s) compute(s);
         __syncthreads();
     }
 
-    if constexpr (TYPE == NET_F32) {
-        // a result that is no finite number may be one of the parts' making (see plain_dot)
-        const float *x = static_cast<const float *>(P.at), *y = static_cast<const float *>(Q.at);
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int k = 0; k < 16; ++k)
-                    if (!(fabsf(acc[i][j][k]) < INFINITY)) {
-                        const long long p = p0 + (wp * MT + i) * 32 + 8 * (k >> 2) + 4 * (lane >> 5) + (k & 3), q = q0 + (wq * NT + j) * 32 + (lane & 31);
-                        acc[i][j][k] = p < np && q < nq ? plain_dot(x + (PCOL ? t0 * P.ld + p : p * P.ld + t0), PCOL ? P.ld : 1, y + (QCOL ? t0 * Q.ld + q : q * Q.ld + t0), QCOL ? Q.ld : 1, t1 - t0) : 0.0f;
-                    }
-    }
-
-    product_end<TYPE, !PCOL, MT, NT>(acc, reinterpret_cast<float *>(s_mem) + wave * end_floats(MT), lane, p0 + wp * MT * 32, q0 + wq * NT * 32, np, nq, part, E);
+    // (see plain_dot)
+    auto again = [&](long long q, long long p) {
+        return plain_dot(static_cast<const float *>(P.at) + (PCOL ? t0 * P.ld + p : p * P.ld + t0), PCOL ? P.ld : 1, static_cast<const float *>(Q.at) + (QCOL ? t0 * Q.ld + q : q * Q.ld + t0),
+                         QCOL ? Q.ld : 1, t1 - t0);
+    };
+    product_end<TYPE, !PCOL, MT, NT>(acc, reinterpret_cast<float *>(s_mem) + wave * end_floats(MT), lane, p0 + wp * MT * 32, q0 + wq * NT * 32, np, nq, part, E, again);
 }
 
 // The same for large products of 16-bit matrices whose rows lie at multiples of 16 bytes (and are, along p or q, a multiple of 8 long): 256 x 256 results a
@@ -871,7 +869,7 @@ __global__ __launch_bounds__(512) void k_product_big(MatD P, MatD Q, long long n
         }
         __syncthreads();
     }
-    product_end<TYPE, !PCOL, MT, NT>(acc, reinterpret_cast<float *>(s_mem) + wave * end_floats(MT), lane, p0 + wp * MT * 32, q0 + wq * NT * 32, np, nq, part, E);
+    product_end<TYPE, !PCOL, MT, NT>(acc, reinterpret_cast<float *>(s_mem) + wave * end_floats(MT), lane, p0 + wp * MT * 32, q0 + wq * NT * 32, np, nq, part, E, [](long long, long long) { return 0.0f; });
 }
 
 // The parts' sums and what becomes of them, 256 neighbours p of one row q at a time.  SPLIT: a block's four waves add every fourth part each and the first of
