@@ -132,6 +132,7 @@ int cus_of(int device)
 
 // Forward with so many rows at most is k_few's.
 constexpr int FEW_ROWS = 32;
+constexpr long long FEW_WAVES = 16;
 
 // A layer's epilogue behind a range of t that is not longer: smaller blocks, one buffer, so that more of them are there to load while others end (524288 x 256 x 256
 // bf16 with residual and dropout 375 us, with the large tile 420; without an epilogue 228 and 169).
@@ -216,13 +217,18 @@ void launch_parts(const Plan &p, const float *part, int64_t np, int64_t nq, cons
     else k_parts<TYPE, false><<<(unsigned)std::min<long long>(blocks, 1 << 16), 256, 0, stream>>>(part, p.part_stride, p.ldp, p.parts, np, nq, E);
 }
 
-// Waves a block: enough that every compute unit has some 16, and each a step or more.
+// Waves a block: enough that every compute unit has some 16, and each a group of steps or more.
 template <int TYPE> void launch_few(const MatD &W, const MatD &X, int64_t np, int64_t nq, int64_t nt, const EpiD &E, int cus, hipStream_t stream)
 {
-    const long long blocks = (np + 15) / 16, ahead = TYPE == NET_F32 ? (nq > 16 ? 2 : 4) : 8, steps = std::max<long long>(1, ((nt + 31) / 32 + ahead - 1) / ahead);
-    const int waves = (int)std::max(nq > 16 ? 2ll : 1ll, std::min(std::min(16ll, steps), std::max(4ll, 16ll * cus / blocks)));
-    if (nq > 16) k_few<TYPE, 2><<<(unsigned)blocks, 64 * waves, 0, stream>>>(W, X, np, nq, nt, E);
-    else k_few<TYPE, 1><<<(unsigned)blocks, 64 * waves, 0, stream>>>(W, X, np, nq, nt, E);
+    // two times 16 outputs a block where that leaves a block for every unit: the rows are read half as often
+    const int mp = nq > 4 && np > 16ll * cus ? 2 : 1, many = nq > 16 ? 2 : 1;
+    const long long blocks = (np + 16 * mp - 1) / (16 * mp), groups = std::max<long long>(1, nt / 32 / few_ahead(TYPE == NET_F32, mp, many));
+    const int waves = (int)std::max<long long>(mp * many, std::min(std::min(16ll, groups), std::max(4ll, FEW_WAVES * cus / blocks)));
+    const dim3 grid((unsigned)blocks), block(64 * waves);
+    if (mp == 1 && many == 1) k_few<TYPE, 1, 1><<<grid, block, 0, stream>>>(W, X, np, nq, nt, E);
+    else if (mp == 1) k_few<TYPE, 1, 2><<<grid, block, 0, stream>>>(W, X, np, nq, nt, E);
+    else if (many == 1) k_few<TYPE, 2, 1><<<grid, block, 0, stream>>>(W, X, np, nq, nt, E);
+    else k_few<TYPE, 2, 2><<<grid, block, 0, stream>>>(W, X, np, nq, nt, E);
 }
 
 enum { NT, NN, TN };                   // forward, dX, dweight

@@ -94,17 +94,19 @@ template <int TYPE, int N> __device__ inline Packed<TYPE, N> load_all(const type
     return r;
 }
 
-// The first `n` (1 .. N) of N elements, zeros behind them.
+// The first `n` (1 .. N) of N elements, zeros behind them.  Single elements are loaded without conditions, so that all are on their way at once.
 template <int TYPE, int N> __device__ inline Packed<TYPE, N> load_some(const typename ElemOf<TYPE>::type *at, int n)
 {
     if (n >= N) return load_all<TYPE, N>(at);
     Packed<TYPE, N> r;
 #pragma unroll
     for (int k = 0; k < r.WORDS; ++k) {
-        if constexpr (TYPE == NET_F32) r.w[k] = k < n ? __float_as_uint(at[k]) : 0u;
-        else {
-            const unsigned lo = 2 * k < n ? at[2 * k] : 0u, hi = 2 * k + 1 < n ? at[2 * k + 1] : 0u;
-            r.w[k] = lo | hi << 16;
+        if constexpr (TYPE == NET_F32) {
+            const unsigned x = __float_as_uint(at[k < n ? k : n - 1]);
+            r.w[k] = k < n ? x : 0u;
+        } else {
+            const unsigned lo = at[2 * k < n ? 2 * k : n - 1], hi = at[2 * k + 1 < n ? 2 * k + 1 : n - 1];
+            r.w[k] = (2 * k < n ? lo : 0u) | (2 * k + 1 < n ? hi : 0u) << 16;
         }
     }
     return r;
@@ -597,7 +599,7 @@ __device__ inline void tile_of(const TilesD &N, int block, int &tp, int &tq)
 
 // D = P Q^T and what becomes of it.  BP x BQ results a block, WP x WQ waves; blockIdx.y: the part of the range of t, `t_part` long.
 template <int TYPE, bool PCOL, bool QCOL, int BP, int BQ, int WP, int WQ, int BUFFERS, int AHEAD>
-__global__ __launch_bounds__(64 * WP * WQ, TYPE == NET_F32 && BP * BQ == 128 * 128 ? 3 : 1) void k_product(MatD P, MatD Q, long long np, long long nq, long long nt, long long t_part, TilesD tiles, EpiD E)
+__global__ __launch_bounds__(64 * WP * WQ, TYPE == NET_F32 && BP * BQ == 128 * 128 && !QCOL ? 3 : 1) void k_product(MatD P, MatD Q, long long np, long long nq, long long nt, long long t_part, TilesD tiles, EpiD E)
 {
     constexpr int THREADS = 64 * WP * WQ, BT = TYPE == NET_F32 ? 32 : 64, MT = BP / WP / 32, NT = BQ / WQ / 32;
     typedef Stage<TYPE, PCOL, BP, BT, THREADS> StageP;
@@ -667,6 +669,7 @@ __global__ __launch_bounds__(64 * WP * WQ, TYPE == NET_F32 && BP * BQ == 128 * 1
             else x.fast(P, p0, t, own_p);
             if constexpr (EDGE && QCOL) y.load(Q, q0, t, t1, tid);
             else y.fast(Q, q0, t, own_q);
+            __builtin_amdgcn_sched_barrier(0);         // in this order, which the waits go by
         };
         auto put = [&](int k, StageP &x, StageQ &y, int to) {
             x.store(lds + to * TILE, tid);
@@ -677,30 +680,30 @@ __global__ __launch_bounds__(64 * WP * WQ, TYPE == NET_F32 && BP * BQ == 128 * 1
         for (int k = 0; k < AHEAD; ++k) ask(k, sp[k], sq[k]);
         put(0, sp[0], sq[0], 0);
         __syncthreads();
-        for (int k0 = 0; k0 < whole; k0 += AHEAD) {
+        auto turn = [&](int k, StageP &np, StageQ &nq) {
+            if constexpr (BUFFERS == 2) {
+                // the next tile's writes to LDS among the products of this one
 #pragma unroll
-            for (int j = 0; j < AHEAD; ++j) {
-                const int k = k0 + j;
-                if (k >= whole) break;
-                StageP &np = sp[(j + 1) % AHEAD];
-                StageQ &nq = sq[(j + 1) % AHEAD];
-                if constexpr (BUFFERS == 2) {
-                    // the next tile's writes to LDS among the products of this one
+                for (int s = 0; s < BT / 32; ++s) compute(s);
+                put(k + 1, np, nq, buffer ^ 1);
 #pragma unroll
-                    for (int s = 0; s < BT / 32; ++s) compute(s);
-                    put(k + 1, np, nq, buffer ^ 1);
+                for (int s = BT / 32; s < BT / 16; ++s) compute(s);
+                buffer ^= 1;
+            } else {
 #pragma unroll
-                    for (int s = BT / 32; s < BT / 16; ++s) compute(s);
-                    buffer ^= 1;
-                } else {
-#pragma unroll
-                    for (int s = 0; s < BT / 16; ++s) compute(s);
-                    __syncthreads();
-                    put(k + 1, np, nq, 0);
-                }
+                for (int s = 0; s < BT / 16; ++s) compute(s);
                 __syncthreads();
+                put(k + 1, np, nq, 0);
             }
-        }
+            __syncthreads();
+        };
+        int k = 0;
+        for (; k + AHEAD <= whole; k += AHEAD)
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) turn(k + j, sp[(j + 1) % AHEAD], sq[(j + 1) % AHEAD]);
+#pragma unroll
+        for (int j = 0; j < AHEAD - 1; ++j)
+            if (k + j < whole) turn(k + j, sp[(j + 1) % AHEAD], sq[(j + 1) % AHEAD]);
     };
     if (whole > 0) {
         if ((PCOL && p0 + BP > P.cols) || (QCOL && q0 + BQ > Q.cols)) run(Int<1>());
@@ -917,80 +920,115 @@ template <int TYPE> __device__ inline f32x4 mfma16(s16x8 a, s16x8 b, f32x4 c)
     else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
+constexpr __host__ __device__ int few_ahead(bool f32, int mp, int nq) { return (f32 ? 2 : 4) * (mp * nq == 1 ? 2 : 1) / (f32 && mp * nq == 4 ? 2 : 1); }
+
 // Forward with few rows: the weights are read once, past LDS, straight into the operands (16 outputs by 64 bytes an instruction), and that is all the time it takes.
-// A block has 16 outputs and all rows (NQ times 16); its waves take stretches of t in turn and add up in LDS.
-template <int TYPE, int NQ>
+// A block has MP times 16 outputs and all rows (NQ times 16); its waves have a stretch of t each and add up in LDS.
+template <int TYPE, int MP, int NQ>
 __global__ __launch_bounds__(1024) void k_few(MatD W, MatD X, long long np, long long nq, long long nt, EpiD E)
 {
     typedef typename ElemOf<TYPE>::type T;
-    constexpr int PL = TYPE == NET_F32 ? 3 : 1, AHEAD = (TYPE == NET_F32 ? 4 : 8) / NQ;      // loads of the weights on their way, a lane
-    __shared__ __attribute__((aligned(16))) float s_sum[16][NQ][64][4];
+    constexpr int PL = TYPE == NET_F32 ? 3 : 1, AHEAD = few_ahead(TYPE == NET_F32, MP, NQ);     // steps of 32 t on their way, a wave
+    __shared__ __attribute__((aligned(16))) float s_sum[16][MP * NQ][64][4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-    const long long p0 = blockIdx.x * 16ll;
-    const long long row = p0 + (lane & 15) < np ? p0 + (lane & 15) : np - 1;
-    const T *w = static_cast<const T *>(W.at) + row * W.ld;
-    // what the end needs, of the threads that take part in it
+    const long long p0 = blockIdx.x * (16ll * MP);
+    // what the end needs, of the threads that take part in it: wave j has the results of outputs j / NQ and rows j % NQ
     const int j = threadIdx.x >> 6;
-    const long long q = 16 * j + (lane & 15), p = p0 + 4 * (lane >> 4);
-    const int n = j < NQ && q < nq ? (np - p < 4 ? (int)(np - p) : 4) : 0;
+    const long long q = 16 * (j % NQ) + (lane & 15), p = p0 + 16 * (j / NQ) + 4 * (lane >> 4);
+    const int n = j < MP * NQ && q < nq ? (np - p < 4 ? (int)(np - p) : 4) : 0;
     const Seed seed = seed_of(E.drop);
     float bias[4];
     load_bias<TYPE>(bias, E, p, n);
     Packed<TYPE, 4> r = {};
     const Place<TYPE> to(E, q, p, 0);
     if (n > 0) r = residual4<TYPE>(E, to, 0, n);
-    f32x4 acc[NQ];
+
+    // outputs and rows beyond the last: the last one, whose results go nowhere
+    const T *w[MP], *x[NQ];
 #pragma unroll
-    for (int j = 0; j < NQ; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    const long long steps = (nt + 31) / 32;
-    for (long long s = (long long)wave * AHEAD; s < steps; s += waves * AHEAD) {
-        Packed<TYPE, 8> a[AHEAD], b[AHEAD][NQ];
-        const bool inside = (s + AHEAD) * 32 <= nt;
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            const long long t = (s + k) * 32 + (lane >> 4) * 8, left = nt - t;
-            a[k] = Packed<TYPE, 8>();
-            if (inside) a[k] = load_all<TYPE, 8>(w + t);
-            else if (left > 0) a[k] = load_some<TYPE, 8>(w + t, left < 8 ? (int)left : 8);
-#pragma unroll
-            for (int j = 0; j < NQ; ++j) {
-                const long long q = 16 * j + (lane & 15);
-                b[k][j] = Packed<TYPE, 8>();
-                const T *x = static_cast<const T *>(X.at) + q * X.ld + t;
-                if (q < nq) {
-                    if (inside) b[k][j] = load_all<TYPE, 8>(x);
-                    else if (left > 0) b[k][j] = load_some<TYPE, 8>(x, left < 8 ? (int)left : 8);
-                }
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            s16x8 u[PL], v[PL];
-            if constexpr (PL == 3) split8(a[k], u);
-            else u[0] = __builtin_bit_cast(s16x8, u32x4{a[k].w[0], a[k].w[1], a[k].w[2], a[k].w[3]});
-#pragma unroll
-            for (int j = 0; j < NQ; ++j) {
-                if constexpr (PL == 3) {
-                    split8(b[k][j], v);
-                    constexpr int PA[6] = {0, 1, 2, 0, 1, 0}, PB[6] = {2, 1, 0, 1, 0, 0};
-#pragma unroll
-                    for (int n = 0; n < 6; ++n) acc[j] = mfma16<TYPE>(u[PA[n]], v[PB[n]], acc[j]);
-                } else {
-                    v[0] = __builtin_bit_cast(s16x8, u32x4{b[k][j].w[0], b[k][j].w[1], b[k][j].w[2], b[k][j].w[3]});
-                    acc[j] = mfma16<TYPE>(u[0], v[0], acc[j]);
-                }
-            }
-        }
+    for (int k = 0; k < MP; ++k) {
+        const long long row = p0 + 16 * k + (lane & 15);
+        w[k] = static_cast<const T *>(W.at) + (row < np ? row : np - 1) * W.ld + (lane >> 4) * 8;
     }
 #pragma unroll
-    for (int j = 0; j < NQ; ++j) *reinterpret_cast<f32x4 *>(s_sum[wave][j][lane]) = acc[j];
+    for (int k = 0; k < NQ; ++k) {
+        const long long row = 16 * k + (lane & 15);
+        x[k] = static_cast<const T *>(X.at) + (row < nq ? row : nq - 1) * X.ld + (lane >> 4) * 8;
+    }
+    f32x4 acc[MP][NQ];
+#pragma unroll
+    for (int i = 0; i < MP; ++i)
+#pragma unroll
+        for (int k = 0; k < NQ; ++k) acc[i][k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    struct Step { Packed<TYPE, 8> a[MP], b[NQ]; };
+    auto multiply = [&](const Step &c) {
+        s16x8 u[MP][PL], v[PL];
+#pragma unroll
+        for (int i = 0; i < MP; ++i)
+            if constexpr (PL == 3) split8(c.a[i], u[i]);
+            else u[i][0] = __builtin_bit_cast(s16x8, u32x4{c.a[i].w[0], c.a[i].w[1], c.a[i].w[2], c.a[i].w[3]});
+#pragma unroll
+        for (int k = 0; k < NQ; ++k) {
+            if constexpr (PL == 3) split8(c.b[k], v);
+            else v[0] = __builtin_bit_cast(s16x8, u32x4{c.b[k].w[0], c.b[k].w[1], c.b[k].w[2], c.b[k].w[3]});
+#pragma unroll
+            for (int y = PL - 1; y >= 0; --y)
+#pragma unroll
+                for (int z = PL - 1 - y; z >= 0; --z)
+#pragma unroll
+                    for (int i = 0; i < MP; ++i) acc[i][k] = mfma16<TYPE>(u[i][z], v[y], acc[i][k]);
+        }
+    };
+    auto ask = [&](Step &y, long long s) {
+#pragma unroll
+        for (int k = 0; k < MP; ++k) y.a[k] = load_all<TYPE, 8>(w[k] + s * 32);
+#pragma unroll
+        for (int k = 0; k < NQ; ++k) y.b[k] = load_all<TYPE, 8>(x[k] + s * 32);
+        __builtin_amdgcn_sched_barrier(0);             // in this order, which the waits go by
+    };
+    // a wave's stretch of groups of AHEAD steps, a group on its way; single steps behind them to one wave each
+    const long long whole = nt / 32, groups = whole / AHEAD, first = groups * wave / waves * AHEAD, end = groups * (wave + 1) / waves * AHEAD;
+    if (first < end) {
+        Step c[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) ask(c[k], first + k);
+        for (long long s = first + AHEAD; s < end; s += AHEAD)
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                multiply(c[k]);
+                ask(c[k], s + k);
+            }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) multiply(c[k]);
+    }
+    for (long long s = groups * AHEAD + wave; s < whole; s += waves) {
+        Step c;
+        ask(c, s);
+        multiply(c);
+    }
+    if (whole * 32 < nt && wave == waves - 1) {
+        Step c = {};
+        const long long left = nt - whole * 32 - (lane >> 4) * 8;
+        if (left > 0) {
+#pragma unroll
+            for (int k = 0; k < MP; ++k) c.a[k] = load_some<TYPE, 8>(w[k] + whole * 32, left < 8 ? (int)left : 8);
+#pragma unroll
+            for (int k = 0; k < NQ; ++k) c.b[k] = load_some<TYPE, 8>(x[k] + whole * 32, left < 8 ? (int)left : 8);
+        }
+        multiply(c);
+    }
+#pragma unroll
+    for (int i = 0; i < MP; ++i)
+#pragma unroll
+        for (int k = 0; k < NQ; ++k) *reinterpret_cast<f32x4 *>(s_sum[wave][i * NQ + k][lane]) = acc[i][k];
     __syncthreads();
     if (n <= 0) return;
     f32x4 sum = *reinterpret_cast<const f32x4 *>(s_sum[0][j][lane]);
+#pragma unroll 4
     for (int i = 1; i < waves; ++i) sum += *reinterpret_cast<const f32x4 *>(s_sum[i][j][lane]);
     float v[4] = {sum[0], sum[1], sum[2], sum[3]};
     if constexpr (TYPE == NET_F32) {
-#pragma unroll
+#pragma unroll 1
         for (int i = 0; i < 4; ++i)
             if (i < n && !(fabsf(v[i]) < INFINITY)) v[i] = plain_dot(static_cast<const float *>(W.at) + (p + i) * W.ld, 1, static_cast<const float *>(X.at) + q * X.ld, 1, nt);
     }
