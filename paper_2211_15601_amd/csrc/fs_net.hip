@@ -198,7 +198,7 @@ void launch_product(const Plan &p, const MatD &P, const MatD &Q, int64_t np, int
     const dim3 grid((unsigned)(tiles_p * tiles_q), (unsigned)p.parts);
     constexpr int BUFFERS = TYPE == NET_F32 ? 1 : 2;
     if (p.tile < 128) {
-        k_product<TYPE, PCOL, QCOL, 64, 64, 2, 2, 2, TYPE == NET_F32 ? 2 : 4><<<grid, 256, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
+        k_product<TYPE, PCOL, QCOL, 64, 64, 2, 2, 2, 2><<<grid, 256, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
         return;
     }
     if constexpr (BUFFERS == 2 && !PCOL)
