@@ -262,21 +262,17 @@ void product(int type, int kind, const Plan &p, const MatD &P, const MatD &Q, in
 
 struct RowsPlan { RowsD n; unsigned gx, gy; };
 
-RowsPlan plan_rows(int type, int64_t rows, int64_t cols, long long blocks)
+// last: elements of the last row
+RowsPlan plan_rows(int type, int64_t rows, int64_t cols, int64_t last, long long blocks)
 {
     RowsPlan p;
     const int v = type == FS_FLOAT_FULL ? 4 : 8;
     const long long units = (cols + v - 1) / v;
-    p.n.rows = rows;
-    p.n.cols = cols;
-    p.n.tx_bits = 0;
+    p.n = {rows, cols, last, 0};
     while (p.n.tx_bits < 8 && 1ll << p.n.tx_bits < units) ++p.n.tx_bits;
     p.gx = (unsigned)std::min<long long>(1 << 16, std::max<long long>(1, (units + (1 << p.n.tx_bits) - 1) >> p.n.tx_bits));
     const long long at_once = 256 >> p.n.tx_bits, passes = std::max<long long>(1, (rows + at_once - 1) / at_once);
-    const long long gy = std::max(1ll, std::min(passes, blocks / p.gx));
-    const long long each = (passes + gy - 1) / gy;
-    p.gy = (unsigned)((passes + each - 1) / each);
-    p.n.per_block = each * at_once;
+    p.gy = (unsigned)std::max(1ll, std::min(passes, blocks / p.gx));
     return p;
 }
 
@@ -321,7 +317,7 @@ Backward plan_backward(const fs_linear &l, int cus)
     Backward b;
     b.dx = plan_product(l.type, l.inputs, l.rows, l.outputs, cus);
     b.dw = plan_product(l.type, l.inputs, l.outputs, l.rows, cus);
-    b.dz = plan_rows(l.type, l.rows, l.outputs, DZ_BLOCKS);
+    b.dz = plan_rows(l.type, l.rows, l.outputs, l.outputs, DZ_BLOCKS);
     b.has_dz = l.act != FS_ACT_NONE || l.drop.p > 0.0;
     b.narrow = std::max(l.inputs, l.outputs) <= NARROW;
     const long long per_cu = l.type != FS_FLOAT_FULL ? 3 : 1;
@@ -500,12 +496,16 @@ fs_status fs_dropout(int32_t type, int64_t rows, int64_t columns, const fs_drop 
     FS_NET_TRY(check_arrays(what, device, xy, 2, 1, 0));
     FS_NET_TRY(check_arrays(what, device, ry, 2, 1, 0));
     FS_NET_TRY(check_seed(what, device, *drop));
-    // rows without gaps are one
+    // memory without gaps: rows of a block's width, whatever they were
+    int64_t last = columns;
     if (ldx == columns && ldy == columns && (!d_r || ldr == columns)) {
-        columns *= rows;
-        rows = 1;
+        const int64_t all = rows * columns, width = type == FS_FLOAT_FULL ? 1024 : 2048;
+        columns = std::min(all, width);
+        rows = (all + columns - 1) / columns;
+        last = all - (rows - 1) * columns;
+        ldx = ldy = ldr = columns;
     }
-    const RowsPlan p = plan_rows(type, rows, columns, ROW_BLOCKS);
+    const RowsPlan p = plan_rows(type, rows, columns, last, ROW_BLOCKS);
     const MatD X = {d_x, ldx, rows, columns}, R = {d_r, ldr, rows, columns};
     const dim3 grid(p.gx, p.gy);
     const DropD D = drop_of(*drop);
