@@ -130,9 +130,14 @@ int cus_of(int device)
 
 // ---------------------------------------------------------------------------------------------------------------- products
 
-// Forward with so many rows at most is k_few's.
-constexpr int FEW_ROWS = 32;
+// Forward by k_few?  Up to 32 rows, where every wave has a stretch or two (few outputs with many inputs are better off in parts: 12 x 11000 x 300 bf16 takes it 16.2 us,
+// the tiles 10.0), and where many weights do not make many blocks read the rows (4096 x 16384, 12 and 32 rows: 30.3 and 36.2 us, tiles 26.7 and 27.6; 8 rows 29; 4096 x 4096, 12
+// and 32 rows: 10.4 and 14.3, tiles 13.0 and 13.6; 1024 x 1024: 4.5 and 5.6, tiles 8.0 and 8.3).
 constexpr long long FEW_WAVES = 16;
+bool is_few(int64_t rows, int64_t outputs, int64_t inputs, int cus)
+{
+    return rows <= 32 && (outputs >= 16ll * cus || inputs <= 4096) && (rows <= 8 || outputs * inputs <= 1 << 25);
+}
 
 // A layer's epilogue behind a range of t that is not longer: smaller blocks, one buffer, so that more of them are there to load while others end (524288 x 256 x 256
 // bf16 with residual and dropout 375 us, with the large tile 420; without an epilogue 228 and 169).
@@ -148,7 +153,10 @@ struct Plan {
 
 constexpr long long MAX_TILES = (1ll << 24) - 1;        // of 256 threads each: a launch has less than 2^32
 
-// Parts: enough for two blocks a compute unit, none shorter than 256.
+// 64 squared unless there is a tile of 128 squared for every compute unit (bf16, us, 64 and 128: 2048 x 1024 x 1024 14.9 and 24.7, 4096 x 512 x 4096 49 and 37, 65536 x 128 x 128
+// 18.9 and 15.8; fp32: 1024 cubed 25 and 30, 4096 x 1024 x 2048 130 and 103).  Parts, for two blocks a compute unit and none shorter than 256, where there are
+// fewer tiles than three for four units (300 x 4096 x 300 bf16 12.7, without parts 22.1; dweight of 65536 x 256 x 256 85 and 372; with 288 tiles of 1536 x 1024 x 768
+// fp16 17 in two parts, 12 in one).
 Plan plan_product(int type, int64_t np, int64_t nq, int64_t nt, int cus, bool layer = false)
 {
     Plan p = {};
@@ -156,8 +164,9 @@ Plan plan_product(int type, int64_t np, int64_t nq, int64_t nt, int cus, bool la
     auto tiles = [&](int64_t n, int b) { return (long long)((n + b - 1) / b); };
     auto area = [&](int b) { return tiles(np, b) * tiles(nq, b) * b * b; };
     p.tile = tiles(np, 128) * tiles(nq, 128) >= cus && np > 64 && nq > 64 ? 128 : 64;
-    // a block of the 256 tile has a compute unit for itself: one each, parts of 512 at least
-    if (type != FS_FLOAT_FULL && !(layer && nt <= SHORT_T) && tiles(np, 256) * tiles(nq, 256) * std::max<long long>(1, nt / 512) >= cus && area(256) <= area(128) / 4 * 5) p.tile = 256;
+    // a block of the 256 tile has a compute unit for itself: one each, in parts where t is long (dweight of 524288 x 256 x 256 bf16 132 us, with 64 squared 250 to 550;
+    // of 8192 x 1024 x 1024 in two parts 110 with dX, with 128 squared 91)
+    if (type != FS_FLOAT_FULL && !(layer && nt <= SHORT_T) && tiles(np, 256) * tiles(nq, 256) * std::max<long long>(1, nt / 2048) >= cus && area(256) <= area(128) / 4 * 5) p.tile = 256;
     p.tiles_p = tiles(np, p.tile);
     p.tiles_q = tiles(nq, p.tile);
     const long long all = std::max(1ll, p.tiles_p * p.tiles_q);
@@ -173,7 +182,7 @@ Plan plan_product(int type, int64_t np, int64_t nq, int64_t nt, int cus, bool la
 Plan plan_forward(const fs_linear &l, int cus)
 {
     Plan p = plan_product(l.type, l.outputs, l.rows, l.inputs, cus, true);
-    if (l.rows <= FEW_ROWS) p.parts = 1;
+    if (is_few(l.rows, l.outputs, l.inputs, cus)) p.parts = 1;
     return p;
 }
 
@@ -287,7 +296,11 @@ int64_t up(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
 // The backward pass's workspace: dZ (where it is not G itself), the sums of its columns, parts of either product.  narrow: k_narrow's, by
 // `blocks` blocks.
-constexpr int NARROW = 128;            // inputs and outputs of a layer whose backward pass is k_narrow's
+// Inputs and outputs of a layer whose backward pass is k_narrow's: two launches instead of five or six, 7 us each on the thread that runs backward passes.  Kernels, us, this and
+// the others: fp32 1024 x 64 x 64 13.4 and 20.0, 65536 x 128 x 128 66 and 77, 524288 x 32 x 128 252 and 341; bf16 9.6 and 15.6, 51 and 49, 187 and 169: long ones
+// of 16 bits take the others.
+constexpr int NARROW = 128;
+constexpr int64_t NARROW_ROWS = 131072;
 
 struct Backward {
     Plan dx, dw;
@@ -319,7 +332,7 @@ Backward plan_backward(const fs_linear &l, int cus)
     b.dw = plan_product(l.type, l.inputs, l.outputs, l.rows, cus);
     b.dz = plan_rows(l.type, l.rows, l.outputs, l.outputs, DZ_BLOCKS);
     b.has_dz = l.act != FS_ACT_NONE || l.drop.p > 0.0;
-    b.narrow = std::max(l.inputs, l.outputs) <= NARROW;
+    b.narrow = std::max(l.inputs, l.outputs) <= NARROW && (l.type == FS_FLOAT_FULL || l.rows <= NARROW_ROWS);
     const long long per_cu = l.type != FS_FLOAT_FULL ? 3 : 1;
     b.blocks = (int)std::max<long long>(1, std::min<long long>(per_cu * cus, (l.rows + 31) / 32));
     b.sums = b.has_dz ? up(l.rows * l.outputs * size_of(l.type)) : 0;
@@ -407,7 +420,7 @@ fs_status fs_linear_forward(const fs_linear *layer, const void *d_x, int64_t ldx
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const MatD W = {d_w, ldw, n, k}, X = {d_x, ldx, m, k};
     if (m == 0 || n == 0) return FS_OK;
-    if (m > FEW_ROWS) product(l.type, NT, p, W, X, n, m, k, E, d_work, stream);
+    if (!is_few(m, n, k, cus)) product(l.type, NT, p, W, X, n, m, k, E, d_work, stream);
     else if (l.type == FS_FLOAT_FULL) launch_few<NET_F32>(W, X, n, m, k, E, cus, stream);
     else if (l.type == FS_FLOAT_BRAIN) launch_few<NET_BF16>(W, X, n, m, k, E, cus, stream);
     else launch_few<NET_F16>(W, X, n, m, k, E, cus, stream);

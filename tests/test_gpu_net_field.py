@@ -42,6 +42,7 @@ def test_network(gpu_lib):
         # Every layer adds errors of 8 sqrt(6 64) 2^-24 = 1e-5 of its products' magnitudes at most (net_ref.product), which are about 8 times their sums
         # of 64 terms of either sign; there and back through 4 layers: 8 8e-5 = 6.4e-4 of the norm at most, softplus' slope at 10 z adding 2.5 times its argument's.
         for got, want in zip([y, *grads], [Y, *wanted]):
+            want = want.detach()
             off = (got.detach().cpu().to(F64) - want).norm() / want.norm()
             assert float(off) < 2e-3, float(off)
     with pytest.raises(ValueError, match="words"):

@@ -124,9 +124,12 @@ def launches(call, l, **k):
 
 ends = lambda x: [n.split("<")[0] for n, g, b in x]
 # few rows: the weights are read once, by one launch
-for rows in (1, 16, 17, 32):
+for rows in (1, 4, 5, 8, 17, 32):
     ((n, g, b),) = launches(forward, layer(rows=rows, inputs=4096, outputs=1000))
     assert n.startswith("k_few") and g == (63, 1, 1) and b[0] % 64 == 0 and b[0] <= 1024
+for l in (layer(rows=33, inputs=4096, outputs=1000), layer(rows=9, inputs=4096, outputs=16384), layer(rows=2, inputs=11000, outputs=300)):
+    assert ends(launches(forward, l))[0] == "k_product"
+assert ends(launches(forward, layer(rows=8, inputs=11000, outputs=16384, type=1))) == ["k_few"]
 # large ones of 16 bits: the large tile, where the rows lie at multiples of 16 bytes; smaller ones where they do not
 big = layer(rows=8192, inputs=4096, outputs=4096, type=1)
 ((n, g, b),) = launches(forward, big)
