@@ -598,6 +598,9 @@ __device__ inline void tile_of(const TilesD &N, int block, int &tp, int &tq)
 }
 
 // D = P Q^T and what becomes of it.  BP x BQ results a block, WP x WQ waves; blockIdx.y: the part of the range of t, `t_part` long.
+// 16 bits: bound by latency (1536 x 1024 x 768 fp16 12 us) and, at odd addresses, by the loads (8192 x 4096 x 4096 at odd elements 400 us).  fp32: by the arithmetic beside the matrix
+// instructions, the parts (5.7 instructions an element) and the epilogue: 200003 x 256 x 256 with softplus 183 us, 143 TFLOP/s.  Three blocks a compute unit, whose
+// phases mix: two took 247 (with 7.6 instructions an element).
 template <int TYPE, bool PCOL, bool QCOL, int BP, int BQ, int WP, int WQ, int BUFFERS, int AHEAD>
 __global__ __launch_bounds__(64 * WP * WQ, TYPE == NET_F32 && BP * BQ == 128 * 128 && !QCOL ? 3 : 1) void k_product(MatD P, MatD Q, long long np, long long nq, long long nt, long long t_part, TilesD tiles, EpiD E)
 {
@@ -734,6 +737,9 @@ __global__ __launch_bounds__(64 * WP * WQ, TYPE == NET_F32 && BP * BQ == 128 * 1
 
 // The same for large products of 16-bit matrices whose rows lie at multiples of 16 bytes (and are, along p or q, a multiple of 8 long): 256 x 256 results a
 // block of 8 waves.  Tiles of 64 t (whole lines of 128 bytes: with 32 the L2 has twice the requests) go from memory to LDS directly, into two buffers in turn.
+// Bound by the matrix instructions and, with data that are not zeros, by power: 8192 x 4096 x 16384 bf16 932 us (1180 TFLOP/s; of zeros 826, the library's product
+// 788).  128 squared through registers took 1736, tiles read straight before their products 1024; reads of a step among the products of the one before, over
+// the barrier too, made it 932.
 typedef __attribute__((address_space(3))) void lds_void;
 
 // One operand's part of that: 256 rows (or, COL, columns) by 64 t are 32 KB, 1 KB an instruction, four instructions a wave.  A lane's chunk goes where the wave's place
@@ -764,8 +770,8 @@ template <bool COL> struct Direct {
         }
     }
 
-    // By hand, since the compiler waits for all loads before it reads what such a load into the same array wrote once; who calls this waits.  (A change of m0
-    // needs a cycle before it is used here.)
+    // By hand, since the compiler waits for all loads before it reads what such a load into the same array wrote once; who calls this waits.  A change of m0
+    // needs a cycle before it is used here; nothing else in the kernel uses m0, which the compiler keeps no value in.
     __device__ inline void load(short *tile, int wave, bool more)
     {
 #pragma unroll
@@ -923,7 +929,9 @@ template <int TYPE> __device__ inline f32x4 mfma16(s16x8 a, s16x8 b, f32x4 c)
 constexpr __host__ __device__ int few_ahead(bool f32, int mp, int nq) { return (f32 ? 2 : 4) * (mp * nq == 1 ? 2 : 1) / (f32 && mp * nq == 4 ? 2 : 1); }
 
 // Forward with few rows: the weights are read once, past LDS, straight into the operands (16 outputs by 64 bytes an instruction), and that is all the time it takes.
-// A block has MP times 16 outputs and all rows (NQ times 16); its waves have a stretch of t each and add up in LDS.
+// A block has MP times 16 outputs and all rows (NQ times 16); its waves have a stretch of t each and add up in LDS.  1 x 4096 x 16384 bf16 26.4 us where no cache holds the
+// weights (5.1 TB/s), through the tiles 51.  Loads of steps that there are not cost as much as others: with a group too many a wave 31 us, and 8 x 1003 x 777
+// 16.7 in place of 6.0.
 template <int TYPE, int MP, int NQ>
 __global__ __launch_bounds__(1024) void k_few(MatD W, MatD X, long long np, long long nq, long long nt, EpiD E)
 {
@@ -1065,6 +1073,8 @@ __device__ inline float dz_at(const DzD &D, const Seed &seed, long long q, long 
 // The backward pass of a layer of at most B inputs and B outputs, in one pass over its rows: G, Z and X are read once, dX is written, dweight stays in registers and the
 // sums for dbias too, a part for each block.  The weights lie in LDS.  A block takes 32 rows at a time, the next ones on their way meanwhile.
 //   dweight: WP x WQ waves share the B x B results, t = rows.  dX: 32 inputs a wave, t = outputs; where there are twice the waves, two share those.
+// 65536 x 128 x 128 fp32 58 us (134 MB, 2.3 TB/s): four barriers every 32 rows, between which loads, parts and products follow one another.  For 256 x 256 in 16 bits, one
+// block a compute unit, that took 624 us against 556 of the other kernels, so B is 128.
 template <int TYPE, int B, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void k_narrow(DzD D, MatD X, MatD W, void *dx, long long lddx, float *__restrict__ dw, long long ldw, float *__restrict__ sums)
 {
@@ -1339,7 +1349,8 @@ template <int TYPE, int V, bool WHOLE> __device__ inline Packed<TYPE, V> load_ro
     else return load_some<TYPE, V>(at, n);
 }
 
-// Y = R + drop(X).  Two rows' loads before the first one's store, which might be to the same memory.
+// Y = R + drop(X).  Two rows' loads before the first one's store, which might be to the same memory.  134 M bf16 with and without residual 136 us each (5.9 and 3.9 TB/s): Philox's
+// multiplications keep the arithmetic busy for 41 issue slots an element.
 template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dropout(RowsD N, MatD X, MatD R, void *y, long long ldy, DropD D)
 {
     typedef typename ElemOf<TYPE>::type T;
@@ -1374,7 +1385,7 @@ template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dropout(Rows
         });
 }
 
-// dZ = drop(G act'(Z)), and the sums of its columns over a block's rows (either may be NULL)
+// dZ = drop(G act'(Z)), and the sums of its columns over a block's rows (either may be NULL).  134 M bf16 with Z in fp32 239 us (1.07 GB, 4.5 TB/s), beside Philox's arithmetic.
 template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dz(RowsD N, MatD G, MatD Z, int z_f32, int act, float beta, DropD D, void *dz, long long lddz, float *__restrict__ sums)
 {
     typedef typename ElemOf<TYPE>::type T;

@@ -341,3 +341,114 @@ def test_more_than_32_bits_of_elements(net):
     z = net.dropout(wide, 0.25, SEED)                  # rows with gaps
     f = ref.factor((4, 55), 0.25, SEED, first=(wide.shape[0] - 4) * 55)
     assert torch.equal(z[-4:].cpu(), (wide[-4:].cpu().float() * torch.tensor(1 / 0.75) * (f != 0)).to(torch.bfloat16))
+
+
+def whole(rows, cols, dtype, gen, pad=0):
+    v = torch.randint(-2, 3, (rows, cols + pad), generator=gen, device="cuda", dtype=torch.int8).to(dtype)
+    return v[:, :cols]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("size", [(4100, 584, 4104), (4100, 4104, 584), (584, 4104, 4096), (4096, 1024, 4096), (4099, 600, 4101)], ids=str)
+@pytest.mark.parametrize("pad", [0, 8, 3])
+def test_large_whole_numbers_are_exact(net, size, pad, dtype):
+    """The large tiles, with edges along p, q and t, in each of the three products; 64-bit sums on the GPU."""
+    rows, inputs, outputs = size
+    T, gen = ref.TYPES[dtype], torch.Generator(device="cuda").manual_seed(rows)
+    x, w, g = (whole(m, n, T, gen, pad).requires_grad_(True) for m, n in ((rows, inputs), (outputs, inputs), (rows, outputs)))
+    g = g.detach()
+    y = net.linear(x, w)
+    dx, dw = torch.autograd.grad(y, [x, w], g)
+    X, W, G = (t.detach().to(F64) for t in (x, w, g))
+    for name, got, want in (("y", y, X @ W.t()), ("dx", dx, G @ W), ("dweight", dw, G.t() @ X)):
+        off = got.detach() != want.to(T)
+        assert not bool(off.any()), (name, int(off.sum()), off.nonzero()[:4].tolist())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_long_contractions_in_parts(net, dtype):
+    rows, T, gen = 530001, ref.TYPES[dtype], torch.Generator(device="cuda").manual_seed(1)
+    x, w, g = (whole(m, n, T, gen).requires_grad_(True) for m, n in ((rows, 256), (256, 256), (rows, 256)))
+    b = torch.zeros(256, device="cuda", requires_grad=True)
+    # partial sums of whole numbers below 2^24 are exact in fp32
+    dw, db = torch.autograd.grad(net.linear(x, w, b, activation="relu"), [w, b], g.detach())
+    X, W, G = (t.detach().to(F64) for t in (x, w, g))
+    dz = G * (X @ W.t() > 0)
+    assert float((dz.t().abs() @ X.abs()).max()) < 2 ** 24
+    assert torch.equal(dw, (dz.t() @ X).to(T)) and torch.equal(db, dz.sum(0).float())
+
+
+def test_every_digit_of_fp32(net):
+    """Through a matrix of ones on the diagonal every fp32 number comes as it is: its three parts hold all of it, small, large or infinite."""
+    gen = torch.Generator().manual_seed(9)
+    for rows, n in ((1, 64), (3, 128), (20, 160), (200, 64), (300, 128), (300, 200), (1100, 1100)):
+        v = torch.randn(rows, n, generator=gen) * 2.0 ** torch.randint(-90, 120, (rows, n), generator=gen).float()
+        v[0, :4] = torch.tensor([3.4028235e38, -3.4028235e38, math.inf, 2.0 ** -100 * (1 + 2.0 ** -23)])
+        x, w = v.cuda().requires_grad_(True), torch.eye(n, device="cuda").requires_grad_(True)
+        y = net.linear(x, w)
+        # beside an infinity stands 0 times it
+        clean = torch.ones(rows, n, dtype=torch.bool)
+        clean[0] = False
+        assert torch.equal(y.detach().cpu()[clean], v[clean])
+        dx, dw = torch.autograd.grad(y, [x, w], torch.eye(rows, n, device="cuda") * 1.2345678)
+        assert torch.equal(dx, torch.eye(rows, n, device="cuda") * 1.2345678)
+        few = torch.autograd.grad(net.linear(w, w), w, v.cuda()[:n] if rows >= n else torch.cat([v, v.new_zeros(n - rows, n)]).cuda())[0]
+        assert few.shape == (n, n)
+    v = v[1:]
+    x = v.cuda().requires_grad_(True)
+    (dx,) = torch.autograd.grad(net.linear(x, torch.eye(1100, device="cuda")), x, v.cuda())
+    assert torch.equal(dx.cpu(), v)
+
+
+def test_small_numbers_of_16_bits(net):
+    for T, small in ((torch.float16, 2.0 ** -24), (torch.bfloat16, 2.0 ** -126)):
+        for rows in (2, 100):
+            x = torch.full((rows, 64), small, dtype=T, device="cuda") * torch.arange(64, device="cuda").to(T)
+            y = net.linear(x, torch.eye(64, dtype=T, device="cuda"))
+            assert torch.equal(y, x), T
+
+
+@pytest.mark.parametrize("dtype", list(ref.TYPES))
+def test_odd_addresses(net, dtype):
+    """Tensors that begin between the multiples of their vectors, rows as well."""
+    T, gen = ref.TYPES[dtype], torch.Generator(device="cuda").manual_seed(2)
+    for size in ((3, 70, 40), (150, 130, 90), (1500, 640, 1100)):
+        rows, inputs, outputs = size
+
+        def odd(m, n):
+            flat = torch.randint(-2, 3, (m * (n + 1) + 1,), generator=gen, device="cuda", dtype=torch.int8).to(T)
+            return flat[1:].view(m, n + 1)[:, :n]
+
+        x, w, r, g = odd(rows, inputs), odd(outputs, inputs), odd(rows, outputs), odd(rows, outputs)
+        b = odd(1, outputs)[0]
+        out = run(net, x, w, b, r, g, "none", 1.0, 0.5, SEED)
+        X, W, B, R, G = (t.to(F64) for t in (x, w, b, r, g))
+        f = ref.factor((rows, outputs), 0.5, SEED).cuda()
+        for name, want in (("y", (X @ W.t() + B) * f + R), ("dx", (G * f) @ W), ("dweight", (G * f).t() @ X), ("dbias", (G * f).sum(0))):
+            assert torch.equal(out[name].detach(), want.to(T)), (size, name)
+        assert torch.equal(net.dropout(x, 0.5, SEED, residual=x), (X * ref.factor((rows, inputs), 0.5, SEED).cuda() + X).to(T))
+
+
+def test_in_place(gpu_lib):
+    """The C calls with Y in the residual's place, or in X's."""
+    import ctypes
+    L, T = gpu_lib.load(), torch.bfloat16
+    s = torch.cuda.current_stream().cuda_stream
+    for rows, inputs, outputs in ((5, 40, 72), (300, 72, 90), (90, 3000, 64)):
+        x, w, b, r, _ = make(rows, inputs, outputs, T)
+        layer = gpu_lib.Linear(rows, inputs, outputs, 1, 1, gpu_lib.FS_ACT_SILU, 1.0, gpu_lib.Drop(0.3, 1, 2, None))
+        n = L.fs_linear_bytes(ctypes.byref(layer), 0)
+        work = torch.empty(max(n, 1), dtype=torch.uint8, device="cuda")
+        want, z = torch.empty_like(r), torch.empty_like(r)
+        go = lambda y, res: L.fs_linear_forward(ctypes.byref(layer), x.data_ptr(), inputs, w.data_ptr(), inputs, b.data_ptr(), res.data_ptr(), outputs, y.data_ptr(), outputs, z.data_ptr(),
+                                                outputs, work.data_ptr() if n else None, n, s)
+        assert go(want, r) == 0
+        same = r.clone()
+        assert go(same, same) == 0 and torch.equal(same, want)
+    drop = gpu_lib.Drop(0.4, 3, 4, None)
+    for shape in ((7, 33), (64, 4096)):
+        x, r = torch.randn(shape, device="cuda"), torch.randn(shape, device="cuda")
+        want, a, c = torch.empty_like(x), x.clone(), r.clone()
+        go = lambda x, r, y: L.fs_dropout(0, *shape, ctypes.byref(drop), x.data_ptr(), shape[1], r.data_ptr(), shape[1], y.data_ptr(), shape[1], s)
+        assert go(x, r, want) == 0 and go(a, r, a) == 0 and go(x, c, c) == 0
+        assert torch.equal(a, want) and torch.equal(c, want)

@@ -143,3 +143,24 @@ def test_errors_are_raised(fake):
     fake.fs_linear_bytes = lambda *a: -1
     with pytest.raises(fake.binding.FsError, match="FS_E_SHAPE: no"):
         net.linear(on_gpu(4, 6), on_gpu(8, 6))
+
+
+def test_another_device_than_the_current_one(fake, monkeypatch):
+    """The call is made with the tensors' device current, on that device's stream, and the other one is current again afterwards."""
+    from paper_2211_15601_amd import net
+    now, seen = [3], []
+
+    @contextlib.contextmanager
+    def device(d):
+        before, now[0] = now[0], d if isinstance(d, int) else d.index
+        yield
+        now[0] = before
+
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: now[0], raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: 100 + i, raising=False)
+    monkeypatch.setattr(torch.cuda, "device", device)
+    fake.fs_linear_forward = lambda *a: seen.append((now[0], a[-1])) or 0
+    fake.fs_dropout = lambda *a: seen.append((now[0], a[-1])) or 0
+    net.linear(on_gpu(4, 6), on_gpu(8, 6))
+    net.dropout(on_gpu(4, 6), 0.5, (1, 2))
+    assert seen == [(0, 100), (0, 100)] and now == [3]
