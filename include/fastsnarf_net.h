@@ -50,7 +50,7 @@ typedef struct {
 } fs_drop;
 
 typedef struct {
-    int64_t rows;           /* 0 .. 10^9 */
+    int64_t rows;           /* 0 .. 5 10^8 */
     int64_t inputs;         /* 0 .. 2^24 */
     int64_t outputs;        /* 0 .. 2^24 */
     int32_t type;           /* FS_FLOAT_*: X, weight, residual, Y, and their gradients */
@@ -60,7 +60,7 @@ typedef struct {
     fs_drop drop;
 } fs_linear;
 
-/* A product of more than 2^24 tiles of its result (of 128 by 128; 64 by 64 where there are few, or either side is at most 64) is refused: FS_E_SHAPE. */
+/* A product of 2^23 tiles of its result or more (of 128 by 128; 64 by 64 where there are few, or either side is at most 64) is refused: FS_E_SHAPE. */
 
 /* Bytes of workspace that fs_linear_forward (backward = 0) or fs_linear_backward (1) needs on the current device; -1 if `layer` is refused.
  * Depends on the layer alone, not on seeds or addresses. */

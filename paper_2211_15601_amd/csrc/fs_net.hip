@@ -113,7 +113,7 @@ DropD drop_of(const fs_drop &d)
 fs_status check_layer(const char *what, const fs_linear *l)
 {
     if (!l) return fail(FS_E_ARG, "%s: layer is NULL", what);
-    if (l->rows < 0 || l->rows > 1000000000ll || l->inputs < 0 || l->inputs > 1 << 24 || l->outputs < 0 || l->outputs > 1 << 24) return fail(FS_E_SHAPE, "%s: sizes out of range", what);
+    if (l->rows < 0 || l->rows > 500000000ll || l->inputs < 0 || l->inputs > 1 << 24 || l->outputs < 0 || l->outputs > 1 << 24) return fail(FS_E_SHAPE, "%s: sizes out of range", what);
     if (!type_ok(l->type) || (l->bias_type != l->type && l->bias_type != FS_FLOAT_FULL)) return fail(FS_E_ARG, "%s: bad type", what);
     if (l->act < FS_ACT_NONE || l->act > FS_ACT_SOFTPLUS) return fail(FS_E_ARG, "%s: bad act", what);
     if (l->act == FS_ACT_SOFTPLUS && !(l->beta > 0.0f && std::isfinite(l->beta))) return fail(FS_E_ARG, "%s: beta must be positive and finite", what);
@@ -140,7 +140,7 @@ bool is_few(int64_t rows, int64_t outputs, int64_t inputs, int cus)
 }
 
 // A layer's epilogue behind a range of t that is not longer: smaller blocks, one buffer, so that more of them are there to load while others end (524288 x 256 x 256
-// bf16 with residual and dropout 375 us, with the large tile 420; without an epilogue 228 and 169).
+// bf16 with residual and dropout 354 us, with the large tile 420; without an epilogue 228 and 169).
 constexpr long long SHORT_T = 512;
 
 // How a product is launched: tiles of `tile` squared, `parts` parts of the range of t, each t_part long.
@@ -151,7 +151,7 @@ struct Plan {
     long long part_stride;
 };
 
-constexpr long long MAX_TILES = (1ll << 24) - 1;        // of 256 threads each: a launch has less than 2^32
+constexpr long long MAX_TILES = (1ll << 23) - 1;        // of 512 threads each at most: a launch has less than 2^32
 
 // 64 squared unless there is a tile of 128 squared for every compute unit (bf16, us, 64 and 128: 2048 x 1024 x 1024 14.9 and 24.7, 4096 x 512 x 4096 49 and 37, 65536 x 128 x 128
 // 18.9 and 15.8; fp32: 1024 cubed 25 and 30, 4096 x 1024 x 2048 130 and 103).  Parts, for two blocks a compute unit and none shorter than 256, where there are
@@ -205,17 +205,11 @@ void launch_product(const Plan &p, const MatD &P, const MatD &Q, int64_t np, int
         }
     const TilesD tiles = {(int)tiles_p, (int)tiles_q};
     const dim3 grid((unsigned)(tiles_p * tiles_q), (unsigned)p.parts);
-    constexpr int BUFFERS = TYPE == NET_F32 ? 1 : 2;
-    if (p.tile < 128) {
-        k_product<TYPE, PCOL, QCOL, 64, 64, 2, 2, 2, 2><<<grid, 256, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
-        return;
-    }
-    if constexpr (BUFFERS == 2 && !PCOL)
-        if (nt <= SHORT_T) {
-            k_product<TYPE, PCOL, QCOL, 128, 128, 2, 2, 1, 1><<<grid, 256, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
-            return;
-        }
-    k_product<TYPE, PCOL, QCOL, 128, 128, 2, 2, BUFFERS, 1><<<grid, 256, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
+    // Forward by 8 waves and one buffer (fp32 200003 x 256 x 256 174 us, by 4 waves 188; bf16 8192 x 1024 x 1024 26 and 30).  Backward in fp32 by 4 (200003 x 256 x 256 474 us, by 8 503), in 16 bits by 8 and two buffers (8192 x 4095 x 4095 1117 us, with one 1229, by 4 1232).
+    if (p.tile < 128) k_product<TYPE, PCOL, QCOL, 64, 64, 2, 2, 2, 2><<<grid, 256, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
+    else if constexpr (!PCOL) k_product<TYPE, PCOL, QCOL, 128, 128, 2, 4, 1, 1><<<grid, 512, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
+    else if constexpr (TYPE == NET_F32) k_product<TYPE, PCOL, QCOL, 128, 128, 2, 2, 1, 1><<<grid, 256, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
+    else k_product<TYPE, PCOL, QCOL, 128, 128, 2, 4, 2, 1><<<grid, 512, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
 }
 
 template <int TYPE>

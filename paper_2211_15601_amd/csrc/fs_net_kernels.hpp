@@ -599,8 +599,8 @@ __device__ inline void tile_of(const TilesD &N, int block, int &tp, int &tq)
 
 // D = P Q^T and what becomes of it.  BP x BQ results a block, WP x WQ waves; blockIdx.y: the part of the range of t, `t_part` long.
 // 16 bits: bound by latency (1536 x 1024 x 768 fp16 12 us) and, at odd addresses, by the loads (8192 x 4096 x 4096 at odd elements 400 us).  fp32: by the arithmetic beside the matrix
-// instructions, the parts (5.7 instructions an element) and the epilogue: 200003 x 256 x 256 with softplus 183 us, 143 TFLOP/s.  Three blocks a compute unit, whose
-// phases mix: two took 247 (with 7.6 instructions an element).
+// instructions, the parts (5.7 instructions an element) and the epilogue: 200003 x 256 x 256 with silu 174 us, 151 TFLOP/s, 8192 x 4096 x 4096 1303 us, 211 TFLOP/s (the library's
+// 1822).  Two blocks of eight waves a compute unit, whose phases mix: three of four took 188, two of four (with 7.6 instructions an element) 247.
 template <int TYPE, bool PCOL, bool QCOL, int BP, int BQ, int WP, int WQ, int BUFFERS, int AHEAD>
 __global__ __launch_bounds__(64 * WP * WQ, TYPE == NET_F32 && BP * BQ == 128 * 128 && !QCOL ? 3 : 1) void k_product(MatD P, MatD Q, long long np, long long nq, long long nt, long long t_part, TilesD tiles, EpiD E)
 {

@@ -53,7 +53,7 @@ def run(code, tmp_path):
 
 def test_layers_that_are_refused(tmp_path):
     run("""
-for bad, status in ((dict(rows=-1), E_SHAPE), (dict(rows=10 ** 9 + 1), E_SHAPE), (dict(inputs=-1), E_SHAPE), (dict(inputs=(1 << 24) + 1), E_SHAPE), (dict(outputs=-1), E_SHAPE),
+for bad, status in ((dict(rows=-1), E_SHAPE), (dict(rows=5 * 10 ** 8 + 1), E_SHAPE), (dict(inputs=-1), E_SHAPE), (dict(inputs=(1 << 24) + 1), E_SHAPE), (dict(outputs=-1), E_SHAPE),
                     (dict(outputs=(1 << 24) + 1), E_SHAPE), (dict(type=3), E_ARG), (dict(type=-1), E_ARG), (dict(type=0, bias_type=1), E_ARG), (dict(type=1, bias_type=2), E_ARG),
                     (dict(act=5), E_ARG), (dict(act=-1), E_ARG), (dict(act=4, beta=0.0), E_ARG), (dict(act=4, beta=math.inf), E_ARG), (dict(act=4, beta=math.nan), E_ARG),
                     (dict(p=-0.1), E_ARG), (dict(p=1.1), E_ARG), (dict(p=math.nan), E_ARG)):
@@ -64,7 +64,7 @@ for bad, status in ((dict(rows=-1), E_SHAPE), (dict(rows=10 ** 9 + 1), E_SHAPE),
         assert "fs_linear" in error()
 assert L.fs_linear_bytes(None, 0) == -1
 assert L.fs_linear_forward(*[None] * 15) == E_ARG and L.fs_linear_backward(*[None] * 17) == E_ARG
-assert forward(layer(rows=10 ** 9, outputs=1 << 24)) == E_SHAPE and "too many" in error()      # more tiles than a launch has blocks
+assert forward(layer(rows=5 * 10 ** 8, outputs=1 << 24)) == E_SHAPE and "too many" in error()      # more tiles than a launch has blocks
 assert names() == []
 for good in (dict(act=0, beta=math.nan), dict(type=1, bias_type=0), dict(type=2), dict(p=1.0), dict(p=0.0), dict(rows=0), dict(inputs=0), dict(outputs=0)):
     assert forward(layer(**good)) == OK and backward(layer(**good)) == OK, (good, error())
@@ -148,7 +148,7 @@ assert ends(launches(backward, layer(rows=50000, inputs=300, outputs=200), dw=No
 assert launches(forward, layer(rows=0)) == [] and launches(forward, layer(outputs=0)) == []
 assert [n for n, g, b in launches(backward, layer(rows=0))] and launches(backward, layer(rows=0, inputs=0, outputs=0)) == []
 # every grid is within what a launch may have
-for l in (layer(rows=10 ** 9, inputs=1, outputs=1), layer(rows=10 ** 9, inputs=300, outputs=200, type=1), layer(rows=1, inputs=1 << 20, outputs=1 << 18, type=1), layer(rows=100, inputs=1 << 24, outputs=3)):
+for l in (layer(rows=5 * 10 ** 8, inputs=1, outputs=1), layer(rows=5 * 10 ** 8, inputs=300, outputs=200, type=1), layer(rows=1, inputs=1 << 20, outputs=1 << 18, type=1), layer(rows=100, inputs=1 << 24, outputs=3)):
     for call in (forward, backward):
         st = call(l)
         assert st in (OK, E_SHAPE), error()

@@ -39,7 +39,9 @@ def test_registers(tmp_path):
     for n, k in ks.items():
         if n.startswith("k_few<"):                      # blocks of up to 16 waves
             assert waves(k) >= 4, (n, k)
-        if re.match(r"k_product<0,\w+,false,128,128", n):         # fp32, forward and dX: three blocks of four waves
+        if re.match(r"k_product<0,true,false,128,128,2,2", n):     # fp32, dX: three blocks of four waves
             assert waves(k) >= 3 and 3 * k["group_segment_fixed_size"] <= 160 << 10, (n, k)
+        if re.match(r"k_product<\d,false,false,128,128,2,4", n):   # forward: two blocks of eight
+            assert waves(k) >= 3 and 2 * k["group_segment_fixed_size"] <= 160 << 10, (n, k)
         if n.startswith(("k_product_big<", "k_narrow<0")):        # eight waves
             assert waves(k) >= 2, (n, k)
