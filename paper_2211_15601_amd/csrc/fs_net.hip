@@ -139,8 +139,8 @@ bool is_few(int64_t rows, int64_t outputs, int64_t inputs, int cus)
     return rows <= 32 && (outputs >= 16ll * cus || inputs <= 4096) && (rows <= 8 || outputs * inputs <= 1 << 25);
 }
 
-// A layer's epilogue behind a range of t that is not longer: smaller blocks, one buffer, so that more of them are there to load while others end (524288 x 256 x 256
-// bf16 with residual and dropout 354 us, with the large tile 420; without an epilogue 228 and 169).
+// A layer's epilogue behind a range of t that is not longer: smaller blocks, of which some load while others end (524288 x 256 x 256 bf16 with residual and dropout 316 us, with
+// the large tile 420; without an epilogue 228 and 169).
 constexpr long long SHORT_T = 512;
 
 // How a product is launched: tiles of `tile` squared, `parts` parts of the range of t, each t_part long.
@@ -205,11 +205,12 @@ void launch_product(const Plan &p, const MatD &P, const MatD &Q, int64_t np, int
         }
     const TilesD tiles = {(int)tiles_p, (int)tiles_q};
     const dim3 grid((unsigned)(tiles_p * tiles_q), (unsigned)p.parts);
-    // Forward by 8 waves and one buffer (fp32 200003 x 256 x 256 174 us, by 4 waves 188; bf16 8192 x 1024 x 1024 26 and 30).  Backward in fp32 by 4 (200003 x 256 x 256 474 us, by 8 503), in 16 bits by 8 and two buffers (8192 x 4095 x 4095 1117 us, with one 1229, by 4 1232).
+    // By 8 waves (bf16 8192 x 1024 x 1024 forward 26 us, by 4 waves 30; backward 8192 x 4095 x 4095 1117 us, by 4 1232), fp32 backward by 4 (200003 x 256 x 256 474 us, by 8 503).
+    // 16 bits have two buffers (524288 x 256 x 256 bf16 with residual and dropout 316 us, with one 337), fp32 one (200003 x 256 x 256 with residual and Z 254 us, with two 294).
+    constexpr bool F32 = TYPE == NET_F32;
     if (p.tile < 128) k_product<TYPE, PCOL, QCOL, 64, 64, 2, 2, 2, 2><<<grid, 256, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
-    else if constexpr (!PCOL) k_product<TYPE, PCOL, QCOL, 128, 128, 2, 4, 1, 1><<<grid, 512, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
-    else if constexpr (TYPE == NET_F32) k_product<TYPE, PCOL, QCOL, 128, 128, 2, 2, 1, 1><<<grid, 256, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
-    else k_product<TYPE, PCOL, QCOL, 128, 128, 2, 4, 2, 1><<<grid, 512, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
+    else if constexpr (F32 && PCOL) k_product<TYPE, PCOL, QCOL, 128, 128, 2, 2, 1, 1><<<grid, 256, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
+    else k_product<TYPE, PCOL, QCOL, 128, 128, 2, 4, F32 ? 1 : 2, 1><<<grid, 512, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
 }
 
 template <int TYPE>
