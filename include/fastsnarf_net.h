@@ -18,7 +18,8 @@
  * No mask is stored: the backward pass makes it anew.  Philox4x32-10: Salmon et al., "Parallel random numbers: as easy as 1, 2, 3" (2011).
  *
  * Arithmetic: sums in fp32; results rounded once, to nearest even.  Where the type has 16 bits, dZ is rounded to it for the products that read it (not
- * for dbias, which is summed before that); and Z is kept for the backward pass in the bias's type: an fp32 bias gets a gradient that is good to fp32.  fp32 operands of the products go in as three bf16 parts
+ * for dbias, which is summed before that; and not in layers of at most 128 inputs, 128 outputs and 131072 values of dZ, where few values would not average that out); and Z is
+ * kept for the backward pass in the bias's type, or in fp32 by FS_Z_FULL: an fp32 bias gets a gradient that is good to fp32.  fp32 operands of the products go in as three bf16 parts
  * each (24 bits together), of whose nine products the six largest are added: what is left out is below 2^-23 of |x w|, as fp32 rounds a product to 2^-24.
  * Operands below 2^-102 lose digits (the parts are normal numbers no more).  Results are the same from call to call on a device: no atomics.
  * NaN and infinities go through as the formulas say.
@@ -41,7 +42,7 @@
 extern "C" {
 #endif
 
-enum { FS_ACT_NONE = 0, FS_ACT_RELU = 1, FS_ACT_GELU = 2, FS_ACT_SILU = 3, FS_ACT_SOFTPLUS = 4 };
+enum { FS_ACT_NONE = 0, FS_ACT_RELU = 1, FS_ACT_GELU = 2, FS_ACT_SILU = 3, FS_ACT_SOFTPLUS = 4, FS_Z_FULL = 256 };
 
 typedef struct {
     double p;               /* 0 .. 1: the chance of being dropped; 0: nothing is, and the rest is not looked at */
@@ -55,7 +56,7 @@ typedef struct {
     int64_t outputs;        /* 0 .. 2^24 */
     int32_t type;           /* FS_FLOAT_*: X, weight, residual, Y, and their gradients */
     int32_t bias_type;      /* that type or FS_FLOAT_FULL: bias, dbias and Z */
-    int32_t act;            /* FS_ACT_* */
+    int32_t act;            /* FS_ACT_*; + FS_Z_FULL: Z is fp32 whatever the bias is */
     float beta;             /* of softplus: > 0, finite */
     fs_drop drop;
 } fs_linear;

@@ -29,6 +29,7 @@ EXPORTS = ["fs_create", "fs_destroy", "fs_set_params", "fs_set_tuning", "fs_set_
 FS_FLOAT_FULL, FS_FLOAT_BRAIN, FS_FLOAT_HALF = 0, 1, 2
 FS_NORM_TWO, FS_NORM_MAX = 0, 1
 FS_ACT_NONE, FS_ACT_RELU, FS_ACT_GELU, FS_ACT_SILU, FS_ACT_SOFTPLUS = range(5)
+FS_Z_FULL = 256
 
 
 class GridDesc(ctypes.Structure):

@@ -110,13 +110,16 @@ DropD drop_of(const fs_drop &d)
     return r;
 }
 
+int act_kind(const fs_linear &l) { return l.act & FS_Z_FULL && l.act > 0 ? l.act - FS_Z_FULL : l.act; }
+bool z_full(const fs_linear &l) { return (l.act & FS_Z_FULL) != 0 || l.bias_type == FS_FLOAT_FULL; }
+
 fs_status check_layer(const char *what, const fs_linear *l)
 {
     if (!l) return fail(FS_E_ARG, "%s: layer is NULL", what);
     if (l->rows < 0 || l->rows > 500000000ll || l->inputs < 0 || l->inputs > 1 << 24 || l->outputs < 0 || l->outputs > 1 << 24) return fail(FS_E_SHAPE, "%s: sizes out of range", what);
     if (!type_ok(l->type) || (l->bias_type != l->type && l->bias_type != FS_FLOAT_FULL)) return fail(FS_E_ARG, "%s: bad type", what);
-    if (l->act < FS_ACT_NONE || l->act > FS_ACT_SOFTPLUS) return fail(FS_E_ARG, "%s: bad act", what);
-    if (l->act == FS_ACT_SOFTPLUS && !(l->beta > 0.0f && std::isfinite(l->beta))) return fail(FS_E_ARG, "%s: beta must be positive and finite", what);
+    if (act_kind(*l) < FS_ACT_NONE || act_kind(*l) > FS_ACT_SOFTPLUS) return fail(FS_E_ARG, "%s: bad act", what);
+    if (act_kind(*l) == FS_ACT_SOFTPLUS && !(l->beta > 0.0f && std::isfinite(l->beta))) return fail(FS_E_ARG, "%s: beta must be positive and finite", what);
     return check_drop(what, l->drop);
 }
 
@@ -284,7 +287,7 @@ constexpr long long ROW_BLOCKS = 2048, DZ_BLOCKS = 1024;
 
 template <int TYPE> void launch_dz(const RowsPlan &p, const MatD &G, const MatD &Z, const fs_linear &l, void *dz, float *sums, hipStream_t stream)
 {
-    k_dz<TYPE, TYPE == NET_F32 ? 4 : 8><<<dim3(p.gx, p.gy), 256, 0, stream>>>(p.n, G, Z, l.bias_type == FS_FLOAT_FULL, l.act, l.beta, drop_of(l.drop), dz, l.outputs, sums);
+    k_dz<TYPE, TYPE == NET_F32 ? 4 : 8><<<dim3(p.gx, p.gy), 256, 0, stream>>>(p.n, G, Z, z_full(l), act_kind(l), l.beta, drop_of(l.drop), dz, l.outputs, sums);
 }
 
 int64_t up(int64_t bytes) { return (bytes + 255) / 256 * 256; }
@@ -296,6 +299,9 @@ int64_t up(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 // of 16 bits take the others.
 constexpr int NARROW = 128;
 constexpr int64_t NARROW_ROWS = 131072;
+// Values of dZ up to which those of 16 bits keep what its rounding leaves.  The results' own rounding and dZ's make 1.41 times the error of the first alone; of few values
+// by chance more (2 x 27 x 2 fp16, silu: 3.2 times), and of one output, whose rows may cancel (87983 x 1 x 1 fp16: 21): all of those that k_narrow takes are below this.
+constexpr int64_t NARROW_RESTS = 1 << 17;
 
 struct Backward {
     Plan dx, dw;
@@ -315,7 +321,8 @@ void launch_narrow(const fs_linear &l, const Backward &b, const DzD &D, const Ma
     float *part = dw ? reinterpret_cast<float *>(work) : nullptr, *sums = dbias ? reinterpret_cast<float *>(work + narrow_sums(l, b)) : nullptr;
     const int64_t ld = narrow_ld(l);
     constexpr int WAVES = TYPE == NET_F32 ? 8 : 4;
-    k_narrow<TYPE, NARROW, WAVES><<<b.blocks, 64 * WAVES, 0, stream>>>(D, X, W, dx, lddx, part, ld, sums);
+    if (TYPE == NET_F32 || l.rows * l.outputs > NARROW_RESTS) k_narrow<TYPE, NARROW, WAVES, false><<<b.blocks, 64 * WAVES, 0, stream>>>(D, X, W, dx, lddx, part, ld, sums);
+    else k_narrow<TYPE, NARROW, WAVES, TYPE != NET_F32><<<b.blocks, 64 * WAVES, 0, stream>>>(D, X, W, dx, lddx, part, ld, sums);
     const int blocks_dw = dw ? (int)((l.outputs * ld + 255) / 256) : 0, blocks_db = dbias ? (int)((l.outputs + 63) / 64) : 0;
     if (blocks_dw + blocks_db > 0) k_narrow_end<TYPE><<<blocks_dw + blocks_db, 1024, 0, stream>>>(part, ld, b.blocks, l.inputs, l.outputs, dw, lddw, sums, dbias, l.bias_type == FS_FLOAT_FULL, blocks_dw);
 }
@@ -326,7 +333,7 @@ Backward plan_backward(const fs_linear &l, int cus)
     b.dx = plan_product(l.type, l.inputs, l.rows, l.outputs, cus);
     b.dw = plan_product(l.type, l.inputs, l.outputs, l.rows, cus);
     b.dz = plan_rows(l.type, l.rows, l.outputs, l.outputs, DZ_BLOCKS);
-    b.has_dz = l.act != FS_ACT_NONE || l.drop.p > 0.0;
+    b.has_dz = act_kind(l) != FS_ACT_NONE || l.drop.p > 0.0;
     b.narrow = std::max(l.inputs, l.outputs) <= NARROW && (l.type == FS_FLOAT_FULL || l.rows <= NARROW_ROWS);
     const long long per_cu = l.type != FS_FLOAT_FULL ? 3 : 1;
     b.blocks = (int)std::max<long long>(1, std::min<long long>(per_cu * cus, (l.rows + 31) / 32));
@@ -392,7 +399,7 @@ fs_status fs_linear_forward(const fs_linear *layer, const void *d_x, int64_t ldx
         const int s = size_of(l.type);
         if (!d_y || (k > 0 && (!d_x || !d_w))) return fail(FS_E_ARG, "%s: d_x, d_w and d_y must not be NULL", what);
         const Array a[] = {{"d_x", d_x, m, k, ldx, s, false}, {"d_w", d_w, n, k, ldw, s, false}, {"d_bias", d_bias, 1, n, 0, size_of(l.bias_type), false},
-                           {"d_r", d_r, m, n, ldr, s, false}, {"d_y", d_y, m, n, ldy, s, true}, {"d_z", d_z, m, n, ldz, size_of(l.bias_type), true},
+                           {"d_r", d_r, m, n, ldr, s, false}, {"d_y", d_y, m, n, ldy, s, true}, {"d_z", d_z, m, n, ldz, z_full(l) ? 4 : s, true},
                            {"d_work", d_work, 1, p.part_bytes(), 0, 1, true}};
         FS_NET_TRY(check_arrays(what, device, a, 7, 4, 3));
         FS_NET_TRY(check_seed(what, device, l.drop));
@@ -400,11 +407,12 @@ fs_status fs_linear_forward(const fs_linear *layer, const void *d_x, int64_t ldx
     }
     EpiD E = {};
     E.mode = EPI_LAYER;
-    E.act = l.act;
+    E.act = act_kind(l);
     E.beta = l.beta;
     E.over_beta = 1.0f / l.beta;
     E.bias = d_bias;
     E.bias_f32 = l.bias_type == FS_FLOAT_FULL;
+    E.z_f32 = z_full(l);
     E.r = d_r;
     E.ldr = ldr;
     E.out = d_y;
@@ -434,12 +442,12 @@ fs_status fs_linear_backward(const fs_linear *layer, const void *d_g, int64_t ld
     const Backward b = plan_backward(l, cus_of(device));
     if (too_many(b.dx) || too_many(b.dw)) return fail(FS_E_SHAPE, "%s: too many results", what);
     const int s = size_of(l.type);
-    const bool act = l.act != FS_ACT_NONE;
+    const bool act = act_kind(l) != FS_ACT_NONE;
     if (m > 0 && n > 0 && (d_dbias || (k > 0 && (d_dx || d_dw)))) {
         if (!d_g || (act && !d_z) || (k > 0 && ((d_dx && !d_w) || (d_dw && !d_x)))) return fail(FS_E_ARG, "%s: an array that is needed is NULL", what);
     }
     const Array a[] = {{"d_g", d_g, m, n, ldg, s, false}, {"d_x", d_dw ? d_x : nullptr, m, k, ldx, s, false}, {"d_w", d_dx ? d_w : nullptr, n, k, ldw, s, false},
-                       {"d_z", act ? d_z : nullptr, m, n, ldz, size_of(l.bias_type), false}, {"d_dx", d_dx, m, k, lddx, s, true}, {"d_dw", d_dw, n, k, lddw, s, true},
+                       {"d_z", act ? d_z : nullptr, m, n, ldz, z_full(l) ? 4 : s, false}, {"d_dx", d_dx, m, k, lddx, s, true}, {"d_dw", d_dw, n, k, lddw, s, true},
                        {"d_dbias", d_dbias, 1, n, 0, size_of(l.bias_type), true}, {"d_work", d_work, 1, b.end, 0, 1, true}};
     FS_NET_TRY(check_arrays(what, device, a, 8));
     FS_NET_TRY(check_seed(what, device, l.drop));
@@ -450,7 +458,7 @@ fs_status fs_linear_backward(const fs_linear *layer, const void *d_g, int64_t ld
     float *sums = d_dbias ? reinterpret_cast<float *>(work + b.sums) : nullptr;
     const MatD G = {d_g, ldg, m, n}, Z = {d_z, ldz, m, n};
     if (b.narrow && m > 0 && n > 0 && k > 0 && (d_dx || d_dw || d_dbias)) {
-        const DzD D = {G, Z, l.bias_type == FS_FLOAT_FULL, l.act, l.beta, drop_of(l.drop)};
+        const DzD D = {G, Z, z_full(l), act_kind(l), l.beta, drop_of(l.drop)};
         const MatD X = {d_x, ldx, m, k}, W = {d_w, ldw, n, k};
         if (l.type == FS_FLOAT_FULL) launch_narrow<NET_F32>(l, b, D, X, W, d_dx, lddx, d_dw, lddw, d_dbias, work, stream);
         else if (l.type == FS_FLOAT_BRAIN) launch_narrow<NET_BF16>(l, b, D, X, W, d_dx, lddx, d_dw, lddw, d_dbias, work, stream);

@@ -276,7 +276,7 @@ enum { EPI_LAYER, EPI_STORE, EPI_PART };
 // What becomes of D.  EPI_LAYER: the layer's Y (and Z), EPI_STORE: out = D in the type, EPI_PART: fp32 sums of one part of the range of t
 // into out, `part_stride` floats from part to part.
 struct EpiD {
-    int mode, act, bias_f32;
+    int mode, act, bias_f32, z_f32;
     float beta, over_beta;
     const void *bias, *r;
     void *out, *z;
@@ -306,7 +306,7 @@ template <int TYPE> struct Place {
 
     __device__ inline Place(const EpiD &E, long long q, long long p, int part)
     {
-        zs = TYPE == NET_F32 || E.bias_f32 ? 4 : 2;
+        zs = TYPE == NET_F32 || E.z_f32 ? 4 : 2;
         ldo = E.ldo;
         ldz = E.ldz * zs;
         ldr = E.ldr;
@@ -326,7 +326,7 @@ __device__ inline void finish4(float *v, const float *bias, const Packed<TYPE, 4
     for (int i = 0; i < 4; ++i) v[i] += bias[i];
     if (E.z) {
         char *z = at.z + rows * at.ldz;
-        if (E.bias_f32) store_some<NET_F32, 4>(reinterpret_cast<float *>(z), v, n);
+        if (E.z_f32) store_some<NET_F32, 4>(reinterpret_cast<float *>(z), v, n);
         else store_some<TYPE, 4>(reinterpret_cast<T *>(z), v, n);
     }
 #pragma unroll
@@ -1053,11 +1053,13 @@ template <int B> __device__ inline int place_both(int t, int c) { return t * B +
 struct DzD { MatD G, Z; int z_f32, act; float beta; DropD drop; };
 
 // One element of it, in fp32
-__device__ inline float dz_at(const DzD &D, const Seed &seed, long long q, long long n)
+template <int TYPE> __device__ inline float dz_at(const DzD &D, const Seed &seed, long long q, long long n)
 {
-    float g = static_cast<const float *>(D.G.at)[q * D.G.ld + n];
+    typedef typename ElemOf<TYPE>::type T;
+    float g = widen<TYPE>(static_cast<const T *>(D.G.at)[q * D.G.ld + n]);
     if (D.act != ACT_NONE) {
-        const float z = static_cast<const float *>(D.Z.at)[q * D.Z.ld + n];
+        const long long at = q * D.Z.ld + n;
+        const float z = TYPE == NET_F32 || D.z_f32 ? static_cast<const float *>(D.Z.at)[at] : widen<TYPE>(static_cast<const T *>(D.Z.at)[at]);
         float s = 1.0f;
         with_act(D.act, [&](auto kind) { s = slope_of<decltype(kind)::value>(z, D.beta); });
         g *= s;
@@ -1073,19 +1075,23 @@ __device__ inline float dz_at(const DzD &D, const Seed &seed, long long q, long 
 // The backward pass of a layer of at most B inputs and B outputs, in one pass over its rows: G, Z and X are read once, dX is written, dweight stays in registers and the
 // sums for dbias too, a part for each block.  The weights lie in LDS.  A block takes 32 rows at a time, the next ones on their way meanwhile.
 //   dweight: WP x WQ waves share the B x B results, t = rows.  dX: 32 inputs a wave, t = outputs; where there are twice the waves, two share those.
-// 65536 x 128 x 128 fp32 58 us (134 MB, 2.3 TB/s): four barriers every 32 rows, between which loads, parts and products follow one another.  For 256 x 256 in 16 bits, one
+// RESTS (16 bits): dZ goes in as two parts, itself rounded and what that leaves, for layers whose dZ has too few values to average its rounding out.  A rest of 0 would make
+// a NaN of another operand's infinity: dX has sums of its own for the rests, and leaves them out where the others' are no finite numbers; dweight (whose second sums would
+// take 437 registers, one block a compute unit) makes such results again, plainly.  Forward and backward of 1024 x 64 x 64 bf16, gelu, 21.5 us, by one part 17.1; of
+// 65536 x 128 x 128 87, by one 67: there one part is taken.
+// 65536 x 128 x 128 fp32 56 us (134 MB, 2.3 TB/s): four barriers every 32 rows, between which loads, parts and products follow one another.  For 256 x 256 in 16 bits, one
 // block a compute unit, that took 624 us against 556 of the other kernels, so B is 128.
-template <int TYPE, int B, int WAVES>
+template <int TYPE, int B, int WAVES, bool RESTS>
 __global__ __launch_bounds__(64 * WAVES, 2) void k_narrow(DzD D, MatD X, MatD W, void *dx, long long lddx, float *__restrict__ dw, long long ldw, float *__restrict__ sums)
 {
     typedef typename ElemOf<TYPE>::type T;
-    constexpr int THREADS = 64 * WAVES, R = 32, PL = TYPE == NET_F32 ? 3 : 1, WP = WAVES / 2, WQ = 2, MT = B / WP / 32, NT = B / WQ / 32;
+    constexpr int THREADS = 64 * WAVES, R = 32, PL = TYPE == NET_F32 ? 3 : 1, PZ = TYPE == NET_F32 ? 3 : RESTS ? 2 : 1, WP = WAVES / 2, WQ = 2, MT = B / WP / 32, NT = B / WQ / 32;
     constexpr int HALVES = WAVES * 32 / B, STEPS = B / 16 / HALVES, UNITS = R * B / 8 / THREADS, PER_ROW = B / 8;
     static_assert(MT >= 1 && (HALVES == 1 || HALVES == 2) && THREADS % PER_ROW == 0, "shape");
     __shared__ __attribute__((aligned(1024))) short s_w[PL * B * B];
-    __shared__ __attribute__((aligned(1024))) short s_in[2 * PL * R * B];
-    static_assert(HALVES * R * B * 4 <= 2 * PL * R * B * 2, "dX goes through the inputs' place");
-    short *s_dz = s_in, *s_x = s_in + PL * R * B;
+    __shared__ __attribute__((aligned(1024))) short s_in[(PZ + PL) * R * B];
+    static_assert(HALVES * R * B * 4 <= (PZ + PL) * R * B * 2, "dX goes through the inputs' place");
+    short *s_dz = s_in, *s_x = s_in + PZ * R * B;
     float *s_out = reinterpret_cast<float *>(s_in);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave % WP, wq = wave / WP;
     const long long rows = D.G.rows, outputs = D.G.cols, inputs = X.cols;
@@ -1173,6 +1179,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_narrow(DzD D, MatD X, MatD W,
 #pragma unroll
                     for (int k = 0; k < 4; ++k) x.w[k] = (unsigned)narrow<TYPE>(v[2 * k]) | (unsigned)narrow<TYPE>(v[2 * k + 1]) << 16;
                     *reinterpret_cast<u32x4 *>(s_dz + place_both<B>(r, u % PER_ROW)) = u32x4{x.w[0], x.w[1], x.w[2], x.w[3]};
+                    if constexpr (RESTS) {             // and what that leaves, none where it is no finite number
+                        float rest[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) rest[k] = fabsf(x.wide(k)) < INFINITY ? v[k] - x.wide(k) : 0.0f;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) x.w[k] = (unsigned)narrow<TYPE>(rest[2 * k]) | (unsigned)narrow<TYPE>(rest[2 * k + 1]) << 16;
+                        *reinterpret_cast<u32x4 *>(s_dz + R * B + place_both<B>(r, u % PER_ROW)) = u32x4{x.w[0], x.w[1], x.w[2], x.w[3]};
+                    }
                 }
             }
         });
@@ -1184,7 +1198,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_narrow(DzD D, MatD X, MatD W,
         if (dw)
 #pragma unroll
         for (int s = 0; s < R / 16; ++s) {
-            s16x8 a[MT][PL], b[NT][PL];
+            s16x8 a[MT][PL], b[NT][PZ];
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -1192,33 +1206,37 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_narrow(DzD D, MatD X, MatD W,
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
-                for (int k = 0; k < PL; ++k) b[j][k] = turned([](int t, int c) { return place_both<B>(t, c); }, s_dz + k * R * B, (wq * NT + j) * 32, s, lane);
+                for (int k = 0; k < PZ; ++k) b[j][k] = turned([](int t, int c) { return place_both<B>(t, c); }, s_dz + k * R * B, (wq * NT + j) * 32, s, lane);
 #pragma unroll
-            for (int u = 0; u < (PL == 1 ? 1 : 6); ++u)
+            for (int u = 0; u < (PL == 1 ? PZ : 6); ++u)
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
 #pragma unroll
-                    for (int j = 0; j < NT; ++j) acc[i][j] = mfma<TYPE>(a[i][PL == 1 ? 0 : PA[u]], b[j][PL == 1 ? 0 : PB[u]], acc[i][j]);
+                    for (int j = 0; j < NT; ++j) acc[i][j] = mfma<TYPE>(a[i][PL == 1 ? 0 : PA[u]], b[j][PL == 1 ? PZ - 1 - u : PB[u]], acc[i][j]);
         }
         if (!dx) {
             __syncthreads();
             continue;
         }
-        f32x16 d;
+        f32x16 d, rest;
 #pragma unroll
-        for (int k = 0; k < 16; ++k) d[k] = 0.0f;
+        for (int k = 0; k < 16; ++k) d[k] = rest[k] = 0.0f;
         const int pb = wave % (B / 32) * 32, half = wave / (B / 32);
 #pragma unroll 4
         for (int s = 0; s < STEPS; ++s) {
             const int step = half * STEPS + s;
-            s16x8 a[PL], b[PL];
+            s16x8 a[PL], b[PZ];
 #pragma unroll
             for (int k = 0; k < PL; ++k) a[k] = operand<true, B, B>(s_w + k * B * B, pb, step, lane);
 #pragma unroll
-            for (int k = 0; k < PL; ++k) b[k] = *reinterpret_cast<const s16x8 *>(s_dz + k * R * B + place_both<B>(lane & 31, 2 * step + (lane >> 5)));
+            for (int k = 0; k < PZ; ++k) b[k] = *reinterpret_cast<const s16x8 *>(s_dz + k * R * B + place_both<B>(lane & 31, 2 * step + (lane >> 5)));
 #pragma unroll
             for (int u = 0; u < (PL == 1 ? 1 : 6); ++u) d = mfma<TYPE>(a[PL == 1 ? 0 : PA[u]], b[PL == 1 ? 0 : PB[u]], d);
+            if constexpr (RESTS) rest = mfma<TYPE>(a[0], b[1], rest);
         }
+        if constexpr (RESTS)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) d[k] = fabsf(d[k]) < INFINITY ? d[k] + rest[k] : d[k];
         __syncthreads();
         // row q of dX: B floats, its quarters of 16 bytes turned by q so that the lanes' writes spread over the banks
 #pragma unroll
@@ -1241,7 +1259,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_narrow(DzD D, MatD X, MatD W,
                     for (int k = 0; k < 4; ++k)
                         if (k < n && !(fabsf(v[k]) < INFINITY)) {              // as in k_product
                             float sum = 0.0f;
-                            for (long long m = 0; m < outputs; ++m) sum = __builtin_fmaf(dz_at(D, seed, q, m), static_cast<const float *>(W.at)[m * W.ld + p + k], sum);
+                            for (long long m = 0; m < outputs; ++m) sum = __builtin_fmaf(dz_at<TYPE>(D, seed, q, m), static_cast<const float *>(W.at)[m * W.ld + p + k], sum);
                             v[k] = sum;
                         }
                 store_some<TYPE, 4>(static_cast<T *>(dx) + q * lddx + p, v, n);
@@ -1263,19 +1281,18 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_narrow(DzD D, MatD X, MatD W,
                 if (p >= inputs || q >= outputs) continue;
                 *reinterpret_cast<f32x4 *>(part + q * ldw + p) = f32x4{acc[i][j][4 * gq], acc[i][j][4 * gq + 1], acc[i][j][4 * gq + 2], acc[i][j][4 * gq + 3]};
             }
-    if constexpr (TYPE == NET_F32)
-        if (dw) {                      // results that are no finite numbers, plainly
-            __syncthreads();
-            for (long long e = tid; e < outputs * inputs; e += THREADS) {
-                const long long q = e / inputs, p = e % inputs;
-                float sum = part[q * ldw + p];
-                if (fabsf(sum) < INFINITY) continue;
-                sum = 0.0f;
-                for (long long m0 = (long long)blockIdx.x * R; m0 < rows; m0 += stride)
-                    for (long long m = m0; m < m0 + R && m < rows; ++m) sum = __builtin_fmaf(dz_at(D, seed, m, q), static_cast<const float *>(X.at)[m * X.ld + p], sum);
-                part[q * ldw + p] = sum;
-            }
+    if ((TYPE == NET_F32 || RESTS) && dw) {       // results that are no finite numbers, plainly
+        __syncthreads();
+        for (long long e = tid; e < outputs * inputs; e += THREADS) {
+            const long long q = e / inputs, p = e % inputs;
+            float sum = part[q * ldw + p];
+            if (fabsf(sum) < INFINITY) continue;
+            sum = 0.0f;
+            for (long long m0 = (long long)blockIdx.x * R; m0 < rows; m0 += stride)
+                for (long long m = m0; m < m0 + R && m < rows; ++m) sum = __builtin_fmaf(dz_at<TYPE>(D, seed, m, q), widen<TYPE>(static_cast<const T *>(X.at)[m * X.ld + p]), sum);
+            part[q * ldw + p] = sum;
         }
+    }
     if (!sums) return;
     // dbias' part: a thread's columns are those of every PER_ROW-th other
     __syncthreads();

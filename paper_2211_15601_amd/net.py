@@ -95,12 +95,20 @@ def _call(index, f, *args):
         raise binding.FsError(st, binding.load().fs_net_error().decode())
 
 
+# Activations whose slope changes with Z.  Up to _Z_FULL values Z is kept in float32 for them: few values do not average out what 16 bits round off, and the
+# bytes, 8 MB more at most, are few beside the calls themselves.
+_BENT = (binding.FS_ACT_GELU, binding.FS_ACT_SILU, binding.FS_ACT_SOFTPLUS)
+_Z_FULL = 1 << 22
+
+
 class _Plan:
     """What calls of the same sizes share: the layer as the library takes it, without a seed, and the bytes that its calls work in."""
 
     def __init__(self, index, rows, inputs, outputs, kind, bias_kind, act, beta, p):
         L = binding.load()
-        self.index, self.bare = index, binding.Linear(rows, inputs, outputs, kind, bias_kind, act, beta, binding.Drop(p, 0, 0, None))
+        keep = binding.FS_Z_FULL if act in _BENT and bias_kind != binding.FS_FLOAT_FULL and rows * outputs <= _Z_FULL else 0
+        self.z_full = bool(keep)
+        self.index, self.bare = index, binding.Linear(rows, inputs, outputs, kind, bias_kind, act | keep, beta, binding.Drop(p, 0, 0, None))
         self.at = ctypes.byref(self.bare)
         self.forward, self.backward = L.fs_linear_forward, L.fs_linear_backward
         with torch.cuda.device(index):
@@ -123,7 +131,7 @@ def _forward(plan, shape, x, weight, bias, residual, keep_z, seed):
     x, w = _rows(x), _rows(weight)
     r = None if residual is None else _rows(residual)
     y = x.new_empty(shape)
-    z = x.new_empty(shape, dtype=x.dtype if bias is None else bias.dtype) if keep_z else None
+    z = x.new_empty(shape, dtype=torch.float32 if plan.z_full else x.dtype if bias is None else bias.dtype) if keep_z else None
     n, outputs = plan.bytes[0], w.shape[0]
     work = x.new_empty(n, dtype=torch.uint8) if n else None
     b = bias if bias is None or bias.is_contiguous() else bias.contiguous()

@@ -452,3 +452,22 @@ def test_in_place(gpu_lib):
         go = lambda x, r, y: L.fs_dropout(0, *shape, ctypes.byref(drop), x.data_ptr(), shape[1], r.data_ptr(), shape[1], y.data_ptr(), shape[1], s)
         assert go(x, r, want) == 0 and go(a, r, a) == 0 and go(x, c, c) == 0
         assert torch.equal(a, want) and torch.equal(c, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("kind", ["none", "gelu", "silu", "softplus"])
+@pytest.mark.parametrize("size", [(40, 10, 1), (1, 10, 40), (2, 27, 2), (1899, 10, 1), (70, 128, 128), (1, 1, 1), (87983, 1, 1)], ids=str)
+def test_small_layers_round_their_gradients_once(net, size, kind, dtype):
+    """Neither dZ nor Z is rounded to 16 bits in small layers.  Bounds: those of the same numbers in fp32; what two parts of dZ leave, half a step of half a step of it, and
+    half of fp16's least number (2^-25); the result's own rounding."""
+    T = ref.TYPES[dtype]
+    t = make(*size, T, seed=9 + sum(size), pad=1)
+    out = run(net, *t, kind, 1.0, 0.25, SEED)
+    x, w, b, r, g = (v.float() for v in t)
+    want = ref.linear(x, w, b, r, g, kind, 1.0, 0.25, SEED)
+    X, W, B, G = (v.cpu().to(F64) for v in (x, w, b, g))
+    dz = (G * ref.slope(X @ W.T + B, kind, 1.0) * ref.factor(G.shape, 0.25, SEED)).abs()
+    left = dz * 1.1 * (torch.finfo(T).eps / 2) ** 2 + 2.0 ** -25
+    for name, more in (("dx", left @ W.abs()), ("dweight", left.T @ X.abs())):
+        value, bound = want[name]
+        ref.assert_close(name, out[name], (value, bound + more + ref.rounded(value, T) * 1.01))

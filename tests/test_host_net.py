@@ -163,3 +163,18 @@ assert forward(layer()) == E_DEVICE and "fs_linear_forward" in error()
 assert forward(layer()) == OK
 assert S.stub_live_blocks() == 0                        # nothing is allocated
 """, tmp_path)
+
+
+def test_z_in_fp32(tmp_path):
+    """FS_Z_FULL goes with every act, and changes what Z's elements are aligned to."""
+    run("""
+for act in range(5):
+    for type in range(3):
+        l = layer(act=act + 256, type=type)
+        assert forward(l) == OK and backward(l) == OK, (act, type, error())
+for act in (256 + 5, 256 - 1, 512, 768, -256, -1):
+    assert forward(layer(act=act)) == E_ARG and "bad act" in error(), act
+assert forward(layer(act=2, type=1), z=at(Z, 2)) == OK
+assert forward(layer(act=2 + 256, type=1), z=at(Z, 2)) == E_ARG and "d_z" in error()
+assert backward(layer(act=2 + 256, type=1), z=at(Z, 2)) == E_ARG and "d_z" in error()
+""", tmp_path)

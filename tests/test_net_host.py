@@ -164,3 +164,13 @@ def test_another_device_than_the_current_one(fake, monkeypatch):
     net.linear(on_gpu(4, 6), on_gpu(8, 6))
     net.dropout(on_gpu(4, 6), 0.5, (1, 2))
     assert seen == [(0, 100), (0, 100)] and now == [3]
+
+
+@pytest.mark.parametrize("rows, act, kind, bias_kind, full", [
+    (6, "gelu", torch.bfloat16, torch.bfloat16, True), (6, "silu", torch.float16, None, True), (1 << 19, "softplus", torch.float16, None, True),
+    ((1 << 19) + 1, "softplus", torch.float16, None, False), (6, "relu", torch.bfloat16, None, False), (6, "none", torch.bfloat16, None, False),
+    (6, "gelu", torch.float32, None, False), (6, "gelu", torch.bfloat16, torch.float32, False)])
+def test_where_z_is_kept_in_fp32(fake, rows, act, kind, bias_kind, full):
+    net = __import__("paper_2211_15601_amd.net", fromlist=["net"])
+    plan = net._plan(0, rows, 6, 8, net._TYPES[kind], net._TYPES[bias_kind or kind], net._ACTS[act], 1.0, 0.0)
+    assert plan.z_full == full and plan.bare.act == net._ACTS[act] + 256 * full
