@@ -471,3 +471,34 @@ def test_small_layers_round_their_gradients_once(net, size, kind, dtype):
     for name, more in (("dx", left @ W.abs()), ("dweight", left.T @ X.abs())):
         value, bound = want[name]
         ref.assert_close(name, out[name], (value, bound + more + ref.rounded(value, T) * 1.01))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("size", [(65, 63, 66), (1100, 128, 128), (2000, 17, 97), (300, 200, 130)], ids=str)
+def test_z_in_16_bits(net, monkeypatch, size, dtype):
+    """As layers of more than 2^22 values keep it; the second and third have more values of dZ than go in as two parts."""
+    T = ref.TYPES[dtype]
+    monkeypatch.setattr(net, "_Z_FULL", 0)
+    net._plan.cache_clear()
+    try:
+        for kind in ("gelu", "silu", "softplus"):
+            t = make(*size, T, seed=3 + sum(size), pad=2)
+            check(run(net, *t, kind, 1.0, 0.25, SEED), *t, kind, 1.0, 0.25, SEED)
+    finally:
+        net._plan.cache_clear()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("rows", [70, 1100])
+def test_infinities_in_small_layers(net, rows, dtype):
+    """One infinity in weight, x or g reaches the results that the formulas send it to, and no others; dZ's parts make no NaN of it."""
+    T = ref.TYPES[dtype]
+    for where in range(3):
+        x, w, b, r, g = make(rows, 24, 128, T, seed=rows + where, whole=True)
+        x, w, g = (t.abs() + 1 for t in (x, w, g))
+        (x, w, g)[where][1, 2] = math.inf
+        leaves = [t.detach().requires_grad_(True) for t in (x, w, b)]
+        dx, dw, db = torch.autograd.grad(net.linear(leaves[0], leaves[1], leaves[2]), leaves, g)
+        X, W, G = (t.cpu().to(F64) for t in (x, w, g))
+        for name, got, want in (("dx", dx, G @ W), ("dweight", dw, G.T @ X), ("dbias", db, G.sum(0))):
+            assert torch.equal(got.cpu(), want.to(T)), (name, where)
