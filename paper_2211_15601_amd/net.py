@@ -14,7 +14,8 @@ counts the offset up drops other elements at each replay).  The same words drop 
 The mask is not stored: the backward pass makes it anew.
 
 Calls run on the stream that is current when they are made, wait for nothing, keep nothing but what autograd saves, and can be captured into graphs of torch.cuda.
-A captured backward pass needs its forward pass in the same capture, and no eager graph of the same leaves alive.  There is no CPU fallback."""
+A captured backward pass needs its forward pass in the same capture, and no eager graph of the same leaves alive.  Forward-mode derivatives, second derivatives and
+traces are refused (torch.compile goes round the calls).  There is no CPU fallback."""
 from __future__ import annotations
 
 import ctypes
@@ -23,6 +24,7 @@ import math
 from typing import Optional, Sequence, Tuple, Union
 
 import torch
+import torch.autograd.forward_ad as forward_ad
 
 from . import binding
 
@@ -44,6 +46,9 @@ def _check(what: str, t: torch.Tensor, like: torch.Tensor, types):
 
 
 def _check_input(x):
+    # The library writes through addresses: a trace would hold a result that nothing computes.
+    if torch._C._is_tracing() or torch._C._len_torch_dispatch_stack() and torch._C._get_dispatch_mode(torch._C._TorchDispatchModeKey.PROXY) is not None:
+        raise RuntimeError("layers cannot be traced (torch.jit.trace, make_fx, torch.export): their calls leave no operations behind")
     if not isinstance(x, torch.Tensor):
         raise TypeError(f"x: expected a tensor, got {type(x).__name__}")
     if x.dtype not in _TYPES:
@@ -52,6 +57,12 @@ def _check_input(x):
         raise ValueError(f"tensors must be on a GPU, got {x.device}")
     if x.layout != torch.strided:
         raise ValueError(f"x: expected a dense tensor, got {x.layout}")
+
+
+def _check_tangents(*tensors):
+    """Those of forward mode would be lost in a call."""
+    if any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        raise NotImplementedError("layers have no forward-mode derivatives (jvp)")
 
 
 def _check_p(what, p):
@@ -213,6 +224,8 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] =
     else:
         seed = None
     plan = _plan(device.index, math.prod(shape[:-1]), shape[-1], outputs, _TYPES[kind], _TYPES[bias_kind], act, float(beta), float(dropout))
+    if forward_ad._current_level >= 0:
+        _check_tangents(x, weight, bias, residual)
     if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or bias is not None and bias.requires_grad or residual is not None and residual.requires_grad):
         return _Linear.apply(x, weight, bias, residual, plan, y_shape, seed)
     return _forward(plan, y_shape, x, weight, bias, residual, False, seed)[0]
@@ -259,6 +272,8 @@ def dropout(x: torch.Tensor, p: float, seed: Optional[Seed] = None, residual: Op
         _check("residual", residual, x, (x.dtype,))
         if residual.shape != x.shape:
             raise ValueError(f"residual: shape {tuple(residual.shape)}, expected {tuple(x.shape)}")
+    if forward_ad._current_level >= 0:
+        _check_tangents(x, residual)
     if torch.is_grad_enabled() and (x.requires_grad or residual is not None and residual.requires_grad):
         return _Dropout.apply(x, residual, p, seed)
     return _dropped(x, residual, p, seed)

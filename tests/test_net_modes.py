@@ -1,0 +1,47 @@
+"""net.py where PyTorch looks on: forward-mode derivatives and traces, which the calls do not offer, are refused and not lost."""
+import pytest
+import torch
+import torch.autograd.forward_ad as forward_ad
+
+from test_net_host import OnGpu, fake, on_gpu  # noqa: F401
+
+CALLS = (lambda net, x: net.linear(x, on_gpu(6, 6)), lambda net, x: net.linear(on_gpu(4, 6), on_gpu(6, 6), residual=x, activation="silu"), lambda net, x: net.dropout(x, 0.5, (1, 2)),
+         lambda net, x: net.dropout(on_gpu(4, 6), 0.5, (1, 2), residual=x))
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_tangents_are_not_lost(fake, call):  # noqa: F811
+    from paper_2211_15601_amd import net
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(torch.zeros(4, 6), torch.ones(4, 6)).as_subclass(OnGpu)
+        for enabled in (True, False):
+            with torch.set_grad_enabled(enabled), pytest.raises(NotImplementedError, match="jvp"):
+                call(net, dual)
+        assert not fake.calls
+        call(net, on_gpu(4, 6))                          # without a tangent it is a call as any other
+    assert len(fake.calls) == 1
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_traces_are_refused(fake, call):  # noqa: F811
+    from torch.fx.experimental.proxy_tensor import make_fx
+    from paper_2211_15601_amd import net
+    with pytest.raises(RuntimeError, match="cannot be traced"):
+        make_fx(lambda t: call(net, t))(on_gpu(4, 6))
+    with pytest.raises(RuntimeError, match="cannot be traced"):
+        torch.jit.trace(lambda t: call(net, t), (on_gpu(4, 6),), check_trace=False)
+    assert not fake.calls
+
+
+def test_other_modes_are_none_of_its_business(fake):  # noqa: F811
+    """A mode that only looks on (a counter of operations, a log) sees the call run."""
+    from torch.utils._python_dispatch import TorchDispatchMode
+    from paper_2211_15601_amd import net
+
+    class Log(TorchDispatchMode):
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            return func(*args, **(kwargs or {}))
+
+    with Log():
+        net.dropout(on_gpu(4, 6), 0.5, (1, 2))
+    assert len(fake.calls) == 1
