@@ -83,6 +83,8 @@ def _check_seed(seed, x):
 
 def _rows(t: torch.Tensor) -> torch.Tensor:
     """[rows, columns] with a row's elements one after another: a view where the strides allow one, else a copy."""
+    if t.is_neg():                     # its sign stands beside the tensor: the imaginary part of a conjugate
+        t = t.resolve_neg()
     if t.dim() != 2:
         t = t.reshape(1, -1) if t.dim() < 2 else t.reshape(math.prod(t.shape[:-1]), t.shape[-1])
     return t if t.stride(1) == 1 or t.shape[1] <= 1 else t.contiguous()
@@ -145,7 +147,7 @@ def _forward(plan, shape, x, weight, bias, residual, keep_z, seed):
     z = x.new_empty(shape, dtype=torch.float32 if plan.z_full else x.dtype if bias is None else bias.dtype) if keep_z else None
     n, outputs = plan.bytes[0], w.shape[0]
     work = x.new_empty(n, dtype=torch.uint8) if n else None
-    b = bias if bias is None or bias.is_contiguous() else bias.contiguous()
+    b = None if bias is None else bias.resolve_neg().contiguous()
     _call(plan.index, plan.forward, plan.layer(seed), x.data_ptr(), x.stride(0), w.data_ptr(), w.stride(0), None if b is None else b.data_ptr(),
           None if r is None else r.data_ptr(), 0 if r is None else r.stride(0), y.data_ptr(), outputs, None if z is None else z.data_ptr(), outputs,
           None if work is None else work.data_ptr(), n)

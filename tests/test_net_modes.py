@@ -45,3 +45,19 @@ def test_other_modes_are_none_of_its_business(fake):  # noqa: F811
     with Log():
         net.dropout(on_gpu(4, 6), 0.5, (1, 2))
     assert len(fake.calls) == 1
+
+
+def test_values_that_are_negated_lazily(fake):  # noqa: F811
+    """The imaginary part of a conjugate has its sign kept beside the tensor; what the library reads has to have it."""
+    import ctypes
+    from paper_2211_15601_amd import net
+    read = lambda p: ctypes.c_float.from_address(p).value
+    seen = []
+    fake.fs_linear_forward = lambda layer, x, ldx, w, ldw, b, r, ldr, y, *a: seen.append([read(p) for p in (x, w, b, r)]) or 0
+    fake.fs_dropout = lambda kind, rows, columns, drop, x, ldx, r, ldr, *a: seen.append([read(p) for p in (x, r)]) or 0
+    negated = lambda *shape: torch.complex(torch.zeros(shape), torch.ones(shape)).conj().imag.as_subclass(OnGpu)
+    assert negated(3, 1).is_neg() and negated(3, 1).stride(0) == 2
+    net.linear(negated(3, 1), negated(1, 1), negated(1), residual=negated(3, 1))
+    net.dropout(negated(3, 1), 0.5, (1, 2), residual=negated(3, 1))
+    net.dropout(negated(3, 2), 0.5, (1, 2), residual=negated(3, 2))
+    assert seen == [[-1.0] * 4, [-1.0] * 2, [-1.0] * 2]
