@@ -157,10 +157,12 @@ def _forward(plan, shape, x, weight, bias, residual, keep_z, seed):
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, residual, plan, shape, seed):
-        y, z = _forward(plan, shape, x, weight, bias, residual, plan.bare.act != binding.FS_ACT_NONE, seed)
+        need_x, need_w, need_b = ctx.needs_input_grad[:3]
+        own = need_x or need_w or need_b               # the residual's gradient is y's
+        y, z = _forward(plan, shape, x, weight, bias, residual, own and plan.bare.act != binding.FS_ACT_NONE, seed)
         words = seed if isinstance(seed, torch.Tensor) else None
         ctx.plan, ctx.seed, ctx.shape, ctx.bias_type = plan, None if words is not None else seed, x.shape, None if bias is None else bias.dtype
-        ctx.save_for_backward(x if ctx.needs_input_grad[1] else None, weight, z, words)
+        ctx.save_for_backward(x if need_w else None, weight if need_x else None, z, words if own else None)
         ctx.set_materialize_grads(False)
         return y
 
@@ -174,15 +176,15 @@ class _Linear(torch.autograd.Function):
         if need_x or need_w or need_b:
             x, weight, z, words = ctx.saved_tensors
             plan = ctx.plan
-            G, w, X = _rows(g), _rows(weight), None if x is None else _rows(x)
-            outputs, inputs = weight.shape
+            G, w, X = _rows(g), None if weight is None else _rows(weight), None if x is None else _rows(x)
+            outputs, inputs = plan.bare.outputs, plan.bare.inputs
             dx = g.new_empty(ctx.shape) if need_x else None
             dw = g.new_empty((outputs, inputs)) if need_w else None
             db = g.new_empty(outputs, dtype=ctx.bias_type) if need_b else None
             n = plan.bytes[1]
             work = g.new_empty(n, dtype=torch.uint8) if n else None
             _call(plan.index, plan.backward, plan.layer(ctx.seed if words is None else words), G.data_ptr(), G.stride(0), None if X is None else X.data_ptr(),
-                  0 if X is None else X.stride(0), w.data_ptr(), w.stride(0), None if z is None else z.data_ptr(), outputs, None if dx is None else dx.data_ptr(), inputs,
+                  0 if X is None else X.stride(0), None if w is None else w.data_ptr(), 0 if w is None else w.stride(0), None if z is None else z.data_ptr(), outputs, None if dx is None else dx.data_ptr(), inputs,
                   None if dw is None else dw.data_ptr(), inputs, None if db is None else db.data_ptr(), None if work is None else work.data_ptr(), n)
         return dx, dw, db, g if need_r else None, None, None, None
 
@@ -246,7 +248,7 @@ class _Dropout(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, residual, p, seed):
         ctx.how = p, None if isinstance(seed, torch.Tensor) else seed
-        ctx.save_for_backward(seed if isinstance(seed, torch.Tensor) else None)
+        ctx.save_for_backward(seed if isinstance(seed, torch.Tensor) and ctx.needs_input_grad[0] else None)
         ctx.set_materialize_grads(False)
         return _dropped(x, residual, p, seed)
 

@@ -1,0 +1,47 @@
+"""What a layer keeps for its backward pass: what that reads, and nothing else."""
+import pytest
+import torch
+
+from test_net_host import fake, on_gpu  # noqa: F401
+
+
+def leaf(*shape, wanted=True):
+    return on_gpu(*shape).requires_grad_(wanted)
+
+
+def test_a_weight_is_kept_for_the_gradient_of_x_alone(fake):  # noqa: F811
+    from paper_2211_15601_amd import net
+    for needs_x in (False, True):
+        x, w = leaf(4, 6, wanted=needs_x), leaf(8, 6)
+        y = net.linear(x, w)
+        with torch.no_grad():
+            w.add_(1.0)
+        if needs_x:
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                torch.autograd.grad(y, w, on_gpu(4, 8))
+        else:
+            torch.autograd.grad(y, w, on_gpu(4, 8))
+            assert fake.calls[-1][0] == "backward" and fake.calls[-1][2][4] is None                 # no weight
+
+
+@pytest.mark.parametrize("wanted, kept", [("x", True), ("weight", True), ("bias", True), ("residual", False)])
+def test_z_is_kept_where_the_backward_pass_reads_it(fake, wanted, kept):  # noqa: F811
+    from paper_2211_15601_amd import net
+    t = {n: leaf(*shape, wanted=n == wanted) for n, shape in (("x", (4, 6)), ("weight", (8, 6)), ("bias", (8,)), ("residual", (4, 8)))}
+    words = on_gpu(2, dtype=torch.int64)
+    y = net.linear(**t, activation="gelu", dropout=0.5, seed=words)
+    assert (fake.calls[-1][2][9] is not None) == kept
+    g = on_gpu(4, 8)
+    if not kept:
+        words += 1                                     # nobody's business any more
+    (d,) = torch.autograd.grad(y, t[wanted], g)
+    assert d.shape == t[wanted].shape and len(fake.calls) == 1 + kept
+
+
+def test_words_are_kept_where_dropout_is_made_anew(fake):  # noqa: F811
+    from paper_2211_15601_amd import net
+    words, r = on_gpu(2, dtype=torch.int64), leaf(4, 6)
+    y = net.dropout(on_gpu(4, 6), 0.5, words, residual=r)
+    words += 1
+    torch.autograd.grad(y, r, on_gpu(4, 6))
+    assert len(fake.calls) == 1
