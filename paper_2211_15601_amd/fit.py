@@ -43,7 +43,9 @@ def train(steps=100, dims=(16, 16, 4), n_points=4096, n_poses=4, lr=None, max_no
     """Returns the losses (mean squared distance of the nearest roots), the gradients' norms, their largest entries, and the optimizer."""
     if field not in ("grid", "network"):
         raise ValueError(f"field must be grid or network, got {field!r}")
-    lr = {"grid": 0.05, "network": 2e-3}[field] if lr is None else lr
+    # the rate where none is given, and the shifts' share of the rate
+    given, share = {"grid": (0.05, 0.02), "network": (2e-3, 0.5)}[field]
+    lr = given if lr is None else lr
     W_true, data = poses(seed, dims, n_points, n_poses)
     start = 0.25 * (W_true + 1e-4).log()                                   # a field that is far too smooth
     if field == "grid":
@@ -63,7 +65,7 @@ def train(steps=100, dims=(16, 16, 4), n_points=4096, n_poses=4, lr=None, max_no
     fs = binding.Context(dims, wl.N_BONES, wl.BOX_LO, wl.BOX_HI)
     # the shifts go by a fraction of the rate and do not decay; a batch that spoils the gradients is left out
     opt = optim.AdamW(params, lr=lr, weight_decay=0.0, max_norm=max_norm, skip_nonfinite=True,
-                      lr_scales=[1.0] * len(learned) + [0.001 / lr] * n_poses, decay_scales=[1.0] * len(learned) + [0.0] * n_poses)
+                      lr_scales=[1.0] * len(learned) + [share] * n_poses, decay_scales=[1.0] * len(learned) + [0.0] * n_poses)
     losses, norms, peaks = [], [], []
     for step in range(steps):
         p = step % n_poses
