@@ -292,8 +292,8 @@ template <int TYPE> void launch_dz(const RowsPlan &p, const MatD &G, const MatD 
 
 int64_t up(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// The backward pass's workspace: dZ (where it is not G itself), the sums of its columns, parts of either product.  narrow: k_narrow's, by
-// `blocks` blocks.
+// The backward pass's workspace: dZ (where it is not G itself), the sums of its columns, parts of either product.  narrow: k_narrow's, parts of dweight and of dbias by
+// `blocks` blocks, and nothing else.
 // Inputs and outputs of a layer whose backward pass is k_narrow's: two launches instead of five or six, 7 us each on the thread that runs backward passes.  Kernels, us, this and
 // the others: fp32 1024 x 64 x 64 13.4 and 20.0, 65536 x 128 x 128 66 and 77, 524288 x 32 x 128 252 and 341; bf16 9.6 and 15.6, 51 and 49, 187 and 169: long ones
 // of 16 bits take the others.
@@ -313,7 +313,7 @@ struct Backward {
 };
 
 int64_t narrow_ld(const fs_linear &l) { return (l.inputs + 3) / 4 * 4; }
-int64_t narrow_sums(const fs_linear &l, const Backward &b) { return b.narrow ? up((int64_t)b.blocks * l.outputs * narrow_ld(l) * 4) : 0; }
+int64_t narrow_sums(const fs_linear &l, const Backward &b) { return up((int64_t)b.blocks * l.outputs * narrow_ld(l) * 4); }
 
 template <int TYPE>
 void launch_narrow(const fs_linear &l, const Backward &b, const DzD &D, const MatD &X, const MatD &W, void *dx, int64_t lddx, void *dw, int64_t lddw, void *dbias, char *work, hipStream_t stream)
@@ -329,18 +329,21 @@ void launch_narrow(const fs_linear &l, const Backward &b, const DzD &D, const Ma
 
 Backward plan_backward(const fs_linear &l, int cus)
 {
-    Backward b;
+    Backward b = {};
     b.dx = plan_product(l.type, l.inputs, l.rows, l.outputs, cus);
     b.dw = plan_product(l.type, l.inputs, l.outputs, l.rows, cus);
     b.dz = plan_rows(l.type, l.rows, l.outputs, l.outputs, DZ_BLOCKS);
     b.has_dz = act_kind(l) != FS_ACT_NONE || l.drop.p > 0.0;
-    b.narrow = std::max(l.inputs, l.outputs) <= NARROW && (l.type == FS_FLOAT_FULL || l.rows <= NARROW_ROWS);
+    b.narrow = std::min({l.rows, l.inputs, l.outputs}) > 0 && std::max(l.inputs, l.outputs) <= NARROW && (l.type == FS_FLOAT_FULL || l.rows <= NARROW_ROWS);
     const long long per_cu = l.type != FS_FLOAT_FULL ? 3 : 1;
     b.blocks = (int)std::max<long long>(1, std::min<long long>(per_cu * cus, (l.rows + 31) / 32));
+    if (b.narrow) {                    // no dZ, and no products' parts
+        b.end = narrow_sums(l, b) + up((int64_t)b.blocks * l.outputs * 4);
+        return b;
+    }
     b.sums = b.has_dz ? up(l.rows * l.outputs * size_of(l.type)) : 0;
     b.part = b.sums + up((int64_t)b.dz.gy * l.outputs * 4);
     b.end = b.part + up(std::max(b.dx.part_bytes(), b.dw.part_bytes()));
-    b.end = std::max(b.end, narrow_sums(l, b) + up((int64_t)b.blocks * l.outputs * 4));
     return b;
 }
 
@@ -457,7 +460,7 @@ fs_status fs_linear_backward(const fs_linear *layer, const void *d_g, int64_t ld
     char *work = static_cast<char *>(d_work);
     float *sums = d_dbias ? reinterpret_cast<float *>(work + b.sums) : nullptr;
     const MatD G = {d_g, ldg, m, n}, Z = {d_z, ldz, m, n};
-    if (b.narrow && m > 0 && n > 0 && k > 0 && (d_dx || d_dw || d_dbias)) {
+    if (b.narrow && (d_dx || d_dw || d_dbias)) {
         const DzD D = {G, Z, z_full(l), act_kind(l), l.beta, drop_of(l.drop)};
         const MatD X = {d_x, ldx, m, k}, W = {d_w, ldw, n, k};
         if (l.type == FS_FLOAT_FULL) launch_narrow<NET_F32>(l, b, D, X, W, d_dx, lddx, d_dw, lddw, d_dbias, work, stream);
