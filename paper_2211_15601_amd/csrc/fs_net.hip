@@ -285,14 +285,16 @@ RowsPlan plan_rows(int type, int64_t rows, int64_t cols, int64_t last, long long
 
 constexpr long long ROW_BLOCKS = 2048, DZ_BLOCKS = 1024;
 
-template <int TYPE> void launch_dz(const RowsPlan &p, const MatD &G, const MatD &Z, const fs_linear &l, void *dz, float *sums, hipStream_t stream)
+// most, factor: of fp16, where dz is wanted (see k_dz)
+template <int TYPE> void launch_dz(const RowsPlan &p, const MatD &G, const MatD &Z, const fs_linear &l, void *dz, float *sums, unsigned *most, float *factor, hipStream_t stream)
 {
-    k_dz<TYPE, TYPE == NET_F32 ? 4 : 8><<<dim3(p.gx, p.gy), 256, 0, stream>>>(p.n, G, Z, z_full(l), act_kind(l), l.beta, drop_of(l.drop), dz, l.outputs, sums);
+    if (most) k_largest<<<LARGEST_BLOCKS, 256, 0, stream>>>(p.n, G, most);
+    k_dz<TYPE, TYPE == NET_F32 ? 4 : 8><<<dim3(p.gx, p.gy), 256, 0, stream>>>(p.n, G, Z, z_full(l), act_kind(l), l.beta, drop_of(l.drop), dz, l.outputs, sums, most, factor);
 }
 
 int64_t up(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// The backward pass's workspace: dZ (where it is not G itself), the sums of its columns, parts of either product.  narrow: k_narrow's, parts of dweight and of dbias by
+// The backward pass's workspace: dZ (where it is not G itself), the sums of its columns, parts of either product, and of fp16 the factor and its numbers.  narrow: k_narrow's, parts of dweight and of dbias by
 // `blocks` blocks, and nothing else.
 // Inputs and outputs of a layer whose backward pass is k_narrow's: two launches instead of five or six, 7 us each on the thread that runs backward passes.  Kernels, us, this and
 // the others: fp32 1024 x 64 x 64 13.4 and 20.0, 65536 x 128 x 128 66 and 77, 524288 x 32 x 128 252 and 341; bf16 9.6 and 15.6, 51 and 49, 187 and 169: long ones
@@ -309,7 +311,7 @@ struct Backward {
     bool has_dz;
     bool narrow;
     int blocks;
-    int64_t sums, part, end;
+    int64_t sums, part, factor, most, end;
 };
 
 int64_t narrow_ld(const fs_linear &l) { return (l.inputs + 3) / 4 * 4; }
@@ -343,7 +345,10 @@ Backward plan_backward(const fs_linear &l, int cus)
     }
     b.sums = b.has_dz ? up(l.rows * l.outputs * size_of(l.type)) : 0;
     b.part = b.sums + up((int64_t)b.dz.gy * l.outputs * 4);
-    b.end = b.part + up(std::max(b.dx.part_bytes(), b.dw.part_bytes()));
+    b.factor = b.part + up(std::max(b.dx.part_bytes(), b.dw.part_bytes()));
+    const bool scaled = b.has_dz && l.type == FS_FLOAT_HALF;
+    b.most = b.factor + (scaled ? 256 : 0);
+    b.end = b.most + (scaled ? up(LARGEST_BLOCKS * sizeof(unsigned)) : 0);
     return b;
 }
 
@@ -470,10 +475,11 @@ fs_status fs_linear_backward(const fs_linear *layer, const void *d_g, int64_t ld
     }
     const MatD dZ = b.has_dz ? MatD{work, n, m, n} : G;
     void *dz = b.has_dz && (d_dx || d_dw) ? work : nullptr;
+    float *factor = dz && n > 0 && l.type == FS_FLOAT_HALF ? reinterpret_cast<float *>(work + b.factor) : nullptr;
     if ((dz || sums) && n > 0) {
-        if (l.type == FS_FLOAT_FULL) launch_dz<NET_F32>(b.dz, G, Z, l, dz, sums, stream);
-        else if (l.type == FS_FLOAT_BRAIN) launch_dz<NET_BF16>(b.dz, G, Z, l, dz, sums, stream);
-        else launch_dz<NET_F16>(b.dz, G, Z, l, dz, sums, stream);
+        if (l.type == FS_FLOAT_FULL) launch_dz<NET_F32>(b.dz, G, Z, l, dz, sums, nullptr, nullptr, stream);
+        else if (l.type == FS_FLOAT_BRAIN) launch_dz<NET_BF16>(b.dz, G, Z, l, dz, sums, nullptr, nullptr, stream);
+        else launch_dz<NET_F16>(b.dz, G, Z, l, dz, sums, factor ? reinterpret_cast<unsigned *>(work + b.most) : nullptr, factor, stream);
         if (sums) {
             const unsigned blocks = (unsigned)((n + 63) / 64);
             if (l.bias_type == FS_FLOAT_FULL) k_dbias<NET_F32><<<blocks, 1024, 0, stream>>>(sums, (int)b.dz.gy, n, d_dbias);
@@ -483,6 +489,7 @@ fs_status fs_linear_backward(const fs_linear *layer, const void *d_g, int64_t ld
     }
     EpiD E = {};
     E.mode = EPI_STORE;
+    E.factor = factor;
     if (d_dx) {
         E.out = d_dx;
         E.ldo = lddx;

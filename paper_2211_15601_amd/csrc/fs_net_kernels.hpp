@@ -201,6 +201,46 @@ template <int N> __device__ inline void drop(float *v, unsigned long long e, con
     for (int i = 0; i < N; ++i) v[i] = w[i] >= d.least ? v[i] * d.scale : 0.0f;
 }
 
+// ---------------------------------------------------------------------------------------------------------------- fp16's range
+
+// dZ goes into 16 bits for the products.  fp16 has 40 powers of two, and dZ may lie below its least (gradients of a mean) or, divided by 1 - p, above its largest number: so it goes
+// in times the power of two that takes the largest finite |G| / (1 - p) to 2^14 .. 2^15 (slopes are 1.13 at most), and the results are divided by that, both exactly.  What
+// rounds to fp16's least steps is then below 2^-28 of the largest.  bf16 has fp32's range, and needs nothing.
+struct Power { float to, back; };
+__device__ inline Power power_of(unsigned most, const DropD &d)
+{
+    const float f = widen<NET_F16>((unsigned short)most) * (d.mode == 1 ? d.scale : 1.0f);
+    if (!(f > 0.0f)) return {1.0f, 1.0f};
+    const int e = (int)(__float_as_uint(f) >> 23) - 127;          // -24 .. 47
+    return {__uint_as_float((unsigned)(127 + 14 - e) << 23), __uint_as_float((unsigned)(127 - 14 + e) << 23)};
+}
+
+// The largest finite of 8 fp16 numbers and `most`, without signs, as bits
+__device__ inline unsigned largest(const Packed<NET_F16, 8> &x, unsigned most)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const unsigned h = x.at(i) & 0x7FFFu;
+        most = h < 0x7C00u && h > most ? h : most;
+    }
+    return most;
+}
+
+// ... of a block's threads, of WAVES waves
+template <int WAVES> __device__ inline unsigned largest_of(unsigned most, unsigned *s_most)
+{
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) {
+        const unsigned other = __shfl_xor(most, m);
+        most = other > most ? other : most;
+    }
+    if ((threadIdx.x & 63) == 0) s_most[threadIdx.x >> 6] = most;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) most = s_most[w] > most ? s_most[w] : most;
+    return most;
+}
+
 // ---------------------------------------------------------------------------------------------------------------- activations
 
 // The hardware's 2^x, log2 and 1/x are good to a unit of the last place; what is built on them here is off by some units, of e^x |x| more (the rounding of x log2 e).
@@ -273,14 +313,15 @@ template <class F> __device__ inline void with_act(int act, F f)
 
 enum { EPI_LAYER, EPI_STORE, EPI_PART };
 
-// What becomes of D.  EPI_LAYER: the layer's Y (and Z), EPI_STORE: out = D in the type, EPI_PART: fp32 sums of one part of the range of t
-// into out, `part_stride` floats from part to part.
+// What becomes of D.  EPI_LAYER: the layer's Y (and Z), EPI_STORE: out = D in the type (fp16: times *factor, where that is not NULL), EPI_PART: fp32 sums of one part of the
+// range of t into out, `part_stride` floats from part to part.
 struct EpiD {
     int mode, act, bias_f32, z_f32;
     float beta, over_beta;
     const void *bias, *r;
     void *out, *z;
     long long ldr, ldo, ldz, part_stride;
+    const float *factor;
     DropD drop;
 };
 
@@ -345,8 +386,17 @@ template <int TYPE> __device__ inline Packed<TYPE, 4> residual4(const EpiD &E, c
     return r;
 }
 
-template <int TYPE> __device__ inline void plain4(const float *v, const EpiD &E, const Place<TYPE> &at, int rows, int n)
+template <int TYPE> __device__ inline float factor_of(const EpiD &E)
 {
+    if constexpr (TYPE == NET_F16) return E.factor ? *E.factor : 1.0f;
+    else return 1.0f;
+}
+
+template <int TYPE> __device__ inline void plain4(float *v, float factor, const EpiD &E, const Place<TYPE> &at, int rows, int n)
+{
+    if constexpr (TYPE == NET_F16)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] *= factor;
     if (E.mode == EPI_PART) store_some<NET_F32, 4>(reinterpret_cast<float *>(at.out) + rows * at.ldo, v, n);
     else store_some<TYPE, 4>(at.out + rows * at.ldo, v, n);
 }
@@ -519,6 +569,7 @@ __device__ inline void product_end(const f32x16 (&acc)[MT][NT], float *out, int 
     static_assert(MT % MG == 0, "squares");
     const int col = 4 * (lane % (PW / 4));
     const Seed seed = seed_of(E.drop);
+    const float factor = factor_of<TYPE>(E);
 #pragma unroll 1
     for (int h = 0; h < NT * (MT / MG); ++h) {
         bool bad = false;
@@ -575,8 +626,8 @@ __device__ inline void product_end(const f32x16 (&acc)[MT][NT], float *out, int 
             for (int r = 0; r < PASSES; ++r)
                 if (r * STEP < rows) {
                     const f32x4 x = *reinterpret_cast<const f32x4 *>(in + r * STEP * PITCH);
-                    const float v[4] = {x[0], x[1], x[2], x[3]};
-                    plain4<TYPE>(v, E, at, r * STEP, n);
+                    float v[4] = {x[0], x[1], x[2], x[3]};
+                    plain4<TYPE>(v, factor, E, at, r * STEP, n);
                 }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -889,6 +940,7 @@ template <int TYPE, bool SPLIT> __global__ __launch_bounds__(256) void k_parts(c
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = SPLIT ? wave : 0, step = SPLIT ? 4 : 1;
     const long long strips = (np + 255) / 256, all = strips * nq, each = SPLIT ? 1 : 4;
     const Seed seed = seed_of(E.drop);
+    const float factor = factor_of<TYPE>(E);
     for (long long b = blockIdx.x * each + (SPLIT ? 0 : wave); b < all; b += gridDim.x * each) {
         const long long q = b / strips, p = b % strips * 256 + 4 * lane;
         const int n = np - p < 4 ? (int)(np - p) : 4;
@@ -912,7 +964,7 @@ template <int TYPE, bool SPLIT> __global__ __launch_bounds__(256) void k_parts(c
             if (E.mode == EPI_LAYER) {
                 load_bias<TYPE>(bias, E, p, n);
                 with_act(E.act, [&](auto act) { finish4<TYPE, decltype(act)::value>(v, bias, r, E, seed, to, 0, (unsigned long long)q * np + p, n); });
-            } else plain4<TYPE>(v, E, to, 0, n);
+            } else plain4<TYPE>(v, factor, E, to, 0, n);
         }
         if constexpr (SPLIT) __syncthreads();
     }
@@ -1142,6 +1194,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_narrow(DzD D, MatD X, MatD W,
 
     const long long stride = (long long)gridDim.x * R;
     long long q0 = (long long)blockIdx.x * R;
+    Power power = {1.0f, 1.0f};
+    if constexpr (TYPE == NET_F16)
+        if (D.act != ACT_NONE || D.drop.mode == 1) {       // a block's own (see power_of): its rows of G are read twice, six groups of 32 at most
+            __shared__ unsigned s_most[WAVES];
+            unsigned most = 0;
+            for (long long q = q0 + r0; q < rows + r0; q += stride)
+#pragma unroll
+                for (int i = 0; i < UNITS; ++i)
+                    if (q + i * APART < rows && left > 0) most = largest(load_some<TYPE, 8>(static_cast<const T *>(D.G.at) + (q + i * APART) * D.G.ld + c8, left), most);
+            power = power_of(largest_of<WAVES>(most, s_most), D.drop);
+        }
     load(q0);
     for (; q0 < rows; q0 += stride) {
         with_act(D.act, [&](auto kind) {
@@ -1176,6 +1239,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_narrow(DzD D, MatD X, MatD W,
 #pragma unroll
                     for (int k = 0; k < 3; ++k) *reinterpret_cast<s16x8 *>(s_dz + k * R * B + place_both<B>(r, u % PER_ROW)) = part[k];
                 } else {
+                    if constexpr (TYPE == NET_F16)
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) v[k] *= power.to;
 #pragma unroll
                     for (int k = 0; k < 4; ++k) x.w[k] = (unsigned)narrow<TYPE>(v[2 * k]) | (unsigned)narrow<TYPE>(v[2 * k + 1]) << 16;
                     *reinterpret_cast<u32x4 *>(s_dz + place_both<B>(r, u % PER_ROW)) = u32x4{x.w[0], x.w[1], x.w[2], x.w[3]};
@@ -1254,6 +1320,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_narrow(DzD D, MatD X, MatD W,
             if (q < rows && p < inputs) {
                 const int n = inputs - p < 4 ? (int)(inputs - p) : 4;
                 float v[4] = {x[0], x[1], x[2], x[3]};
+                if constexpr (TYPE == NET_F16)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] *= power.back;
                 if constexpr (TYPE == NET_F32)
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
@@ -1279,7 +1348,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_narrow(DzD D, MatD X, MatD W,
             for (int gq = 0; gq < 4; ++gq) {
                 const long long p = (wp * MT + i) * 32 + 8 * gq + 4 * (lane >> 5), q = (wq * NT + j) * 32 + (lane & 31);
                 if (p >= inputs || q >= outputs) continue;
-                *reinterpret_cast<f32x4 *>(part + q * ldw + p) = f32x4{acc[i][j][4 * gq], acc[i][j][4 * gq + 1], acc[i][j][4 * gq + 2], acc[i][j][4 * gq + 3]};
+                f32x4 v = {acc[i][j][4 * gq], acc[i][j][4 * gq + 1], acc[i][j][4 * gq + 2], acc[i][j][4 * gq + 3]};
+                if constexpr (TYPE == NET_F16) v *= power.back;
+                *reinterpret_cast<f32x4 *>(part + q * ldw + p) = v;
             }
     if ((TYPE == NET_F32 || RESTS) && dw) {       // results that are no finite numbers, plainly
         __syncthreads();
@@ -1402,12 +1473,44 @@ template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dropout(Rows
         });
 }
 
+// fp16: the largest finite |G| of each of LARGEST_BLOCKS blocks, for power_of().
+constexpr int LARGEST_BLOCKS = 512;
+__global__ __launch_bounds__(256) void k_largest(RowsD N, MatD G, unsigned *__restrict__ most)
+{
+    __shared__ unsigned s_most[4];
+    const long long step = (long long)gridDim.x * (256 >> N.tx_bits), first = (long long)blockIdx.x * (256 >> N.tx_bits) + (threadIdx.x >> N.tx_bits);
+    unsigned m = 0;
+    for (long long c = (threadIdx.x & ((1 << N.tx_bits) - 1)) * 8; c < N.cols; c += 8ll << N.tx_bits) {
+        const unsigned short *at = static_cast<const unsigned short *>(G.at) + c;
+        const int n = N.cols - c < 8 ? (int)(N.cols - c) : 8;
+        if (n == 8)
+#pragma unroll 4
+            for (long long q = first; q < N.rows; q += step) m = largest(load_all<NET_F16, 8>(at + q * G.ld), m);
+        else
+            for (long long q = first; q < N.rows; q += step) m = largest(load_some<NET_F16, 8>(at + q * G.ld, n), m);
+    }
+    m = largest_of<4>(m, s_most);
+    if (threadIdx.x == 0) most[blockIdx.x] = m;
+}
+
 // dZ = drop(G act'(Z)), and the sums of its columns over a block's rows (either may be NULL).  134 M bf16 with Z in fp32 239 us (1.07 GB, 4.5 TB/s), beside Philox's arithmetic.
-template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dz(RowsD N, MatD G, MatD Z, int z_f32, int act, float beta, DropD D, void *dz, long long lddz, float *__restrict__ sums)
+// fp16: dZ is written times a power of two, which goes by k_largest's `most` (where that is not NULL) and whose inverse goes to *factor.
+template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dz(RowsD N, MatD G, MatD Z, int z_f32, int act, float beta, DropD D, void *dz, long long lddz, float *__restrict__ sums,
+                                                                       const unsigned *__restrict__ most, float *__restrict__ factor)
 {
     typedef typename ElemOf<TYPE>::type T;
     __shared__ float s_sum[256 * V];
     const int tx = 1 << N.tx_bits, x = threadIdx.x & (tx - 1), ty = threadIdx.x >> N.tx_bits;
+    float to = 1.0f;
+    if constexpr (TYPE == NET_F16)
+        if (most) {
+            __shared__ unsigned s_most[4];
+            static_assert(LARGEST_BLOCKS == 512, "two a thread");
+            const unsigned a = most[threadIdx.x], b = most[threadIdx.x + 256];
+            const Power power = power_of(largest_of<4>(a > b ? a : b, s_most), D);
+            to = power.to;
+            if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *factor = power.back;
+        }
     const long long c = (((long long)blockIdx.x << N.tx_bits) + x) * V;
     const Seed seed = seed_of(D);
     float sum[V];
@@ -1441,6 +1544,9 @@ template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dz(RowsD N, 
                             drop<V>(v, (unsigned long long)(q + u * step) * N.cols + c, D, seed);
 #pragma unroll
                             for (int i = 0; i < V; ++i) sum[i] += v[i];
+                            if constexpr (TYPE == NET_F16)
+#pragma unroll
+                                for (int i = 0; i < V; ++i) v[i] *= to;
                             if (dz) store_some<TYPE, V>(static_cast<T *>(dz) + (q + u * step) * lddz + c, v, WHOLE ? V : n);
                         }
                 }

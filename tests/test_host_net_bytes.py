@@ -28,3 +28,21 @@ for empty in (dict(rows=0), dict(inputs=0), dict(outputs=0)):
     assert backward(l) == OK, error()
     assert "k_narrow" not in [n.split("<")[0] for n in names()]
 """, tmp_path)
+
+
+def test_where_fp16_is_scaled(tmp_path):
+    """The largest |G| is looked for where dZ is made, of fp16 and by itself, in memory of the workspace behind all else."""
+    run("""
+ends = lambda: [n.split("<")[0] for n in names()]
+for type in range(3):
+    for act, p in ((0, 0.0), (1, 0.0), (0, 0.5)):
+        for rows, outputs in ((5000, 200), (0, 200), (5000, 0)):
+            l = layer(rows=rows, inputs=300, outputs=outputs, act=act, p=p, type=type)
+            dz = (act != 0 or p > 0.0) and outputs > 0
+            names()
+            assert backward(l) == OK, error()
+            assert ends().count("k_largest") == (dz and type == 2), (type, act, p, rows, outputs)
+            assert backward(l, dx=None, dw=None) == OK and "k_largest" not in ends()           # dbias is made from dZ in fp32
+sizes = [L.fs_linear_bytes(ctypes.byref(layer(rows=5000, act=1, type=t)), 1) for t in (1, 2)]
+assert sizes[1] == sizes[0] + 256 + 2048
+""", tmp_path)
