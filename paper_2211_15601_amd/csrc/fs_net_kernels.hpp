@@ -358,6 +358,13 @@ template <int TYPE> struct Place {
     }
 };
 
+// What fp16 keeps of Z: finite numbers stay finite (the slopes at an infinity would be NaN, and are 0 and 1 at 65504 already), and positive ones positive (relu's slope is 1).
+__device__ inline float half_z(float v)
+{
+    const float h = v > 0.0f && v < 0x1p-24f ? 0x1p-24f : __builtin_amdgcn_fmed3f(v, -65504.0f, 65504.0f);
+    return fabsf(v) < INFINITY ? h : v;
+}
+
 // Four results, of which n (1 .. 4) are in the matrix, `rows` rows behind the place; e: the first one's number for drop(); r: their residual.
 template <int TYPE, int ACT>
 __device__ inline void finish4(float *v, const float *bias, const Packed<TYPE, 4> &r, const EpiD &E, const Seed &seed, const Place<TYPE> &at, int rows, unsigned long long e, int n)
@@ -368,7 +375,12 @@ __device__ inline void finish4(float *v, const float *bias, const Packed<TYPE, 4
     if (E.z) {
         char *z = at.z + rows * at.ldz;
         if (E.z_f32) store_some<NET_F32, 4>(reinterpret_cast<float *>(z), v, n);
-        else store_some<TYPE, 4>(reinterpret_cast<T *>(z), v, n);
+        else if constexpr (TYPE == NET_F16) {
+            float h[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) h[i] = half_z(v[i]);
+            store_some<TYPE, 4>(reinterpret_cast<T *>(z), h, n);
+        } else store_some<TYPE, 4>(reinterpret_cast<T *>(z), v, n);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = act_of<ACT>(v[i], E.beta, E.over_beta);

@@ -112,6 +112,8 @@ def _call(index, f, *args):
 # bytes, 8 MB more at most, are few beside the calls themselves.
 _BENT = (binding.FS_ACT_GELU, binding.FS_ACT_SILU, binding.FS_ACT_SOFTPLUS)
 _Z_FULL = 1 << 22
+# float16 keeps Z within +-65504.  The slope of softplus is 0 or 1 there (to e^-32) from this beta on; below it Z is kept in float32 too, whatever its size.
+_FLAT = 2.0 ** -11
 
 
 class _Plan:
@@ -119,7 +121,8 @@ class _Plan:
 
     def __init__(self, index, rows, inputs, outputs, kind, bias_kind, act, beta, p):
         L = binding.load()
-        keep = binding.FS_Z_FULL if act in _BENT and bias_kind != binding.FS_FLOAT_FULL and rows * outputs <= _Z_FULL else 0
+        flat = kind == binding.FS_FLOAT_HALF and act == binding.FS_ACT_SOFTPLUS and beta < _FLAT
+        keep = binding.FS_Z_FULL if act in _BENT and bias_kind != binding.FS_FLOAT_FULL and (rows * outputs <= _Z_FULL or flat) else 0
         self.z_full = bool(keep)
         self.index, self.bare = index, binding.Linear(rows, inputs, outputs, kind, bias_kind, act | keep, beta, binding.Drop(p, 0, 0, None))
         self.at = ctypes.byref(self.bare)
