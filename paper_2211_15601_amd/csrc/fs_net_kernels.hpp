@@ -215,16 +215,18 @@ __device__ inline Power power_of(unsigned most, const DropD &d)
     return {__uint_as_float((unsigned)(127 + 14 - e) << 23), __uint_as_float((unsigned)(127 - 14 + e) << 23)};
 }
 
-// The largest finite of 8 fp16 numbers and `most`, without signs, as bits
-__device__ inline unsigned largest(const Packed<NET_F16, 8> &x, unsigned most)
-{
+// The largest finite fp16 numbers without signs, two columns of them, as bits and 0x0400: infinities and NaN are negative then.
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+struct Largest {
+    s16x2 most = {0x0400, 0x0400};
+
+    __device__ inline void add(const Packed<NET_F16, 8> &x)
+    {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const unsigned h = x.at(i) & 0x7FFFu;
-        most = h < 0x7C00u && h > most ? h : most;
+        for (int k = 0; k < 4; ++k) most = __builtin_elementwise_max(most, __builtin_bit_cast(s16x2, x.w[k] & 0x7FFF7FFFu) + s16x2{0x0400, 0x0400});
     }
-    return most;
-}
+    __device__ inline unsigned bits() const { return (unsigned)(most.x > most.y ? most.x : most.y) - 0x0400u; }
+};
 
 // ... of a block's threads, of WAVES waves
 template <int WAVES> __device__ inline unsigned largest_of(unsigned most, unsigned *s_most)
@@ -1210,12 +1212,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_narrow(DzD D, MatD X, MatD W,
     if constexpr (TYPE == NET_F16)
         if (D.act != ACT_NONE || D.drop.mode == 1) {       // a block's own (see power_of): its rows of G are read twice, six groups of 32 at most
             __shared__ unsigned s_most[WAVES];
-            unsigned most = 0;
+            Largest most;
             for (long long q = q0 + r0; q < rows + r0; q += stride)
 #pragma unroll
                 for (int i = 0; i < UNITS; ++i)
-                    if (q + i * APART < rows && left > 0) most = largest(load_some<TYPE, 8>(static_cast<const T *>(D.G.at) + (q + i * APART) * D.G.ld + c8, left), most);
-            power = power_of(largest_of<WAVES>(most, s_most), D.drop);
+                    if (q + i * APART < rows && left > 0) most.add(load_some<TYPE, 8>(static_cast<const T *>(D.G.at) + (q + i * APART) * D.G.ld + c8, left));
+            power = power_of(largest_of<WAVES>(most.bits(), s_most), D.drop);
         }
     load(q0);
     for (; q0 < rows; q0 += stride) {
@@ -1486,23 +1488,30 @@ template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dropout(Rows
 }
 
 // fp16: the largest finite |G| of each of LARGEST_BLOCKS blocks, for power_of().
-constexpr int LARGEST_BLOCKS = 512;
+constexpr int LARGEST_BLOCKS = 1024;
 __global__ __launch_bounds__(256) void k_largest(RowsD N, MatD G, unsigned *__restrict__ most)
 {
     __shared__ unsigned s_most[4];
-    const long long step = (long long)gridDim.x * (256 >> N.tx_bits), first = (long long)blockIdx.x * (256 >> N.tx_bits) + (threadIdx.x >> N.tx_bits);
-    unsigned m = 0;
+    constexpr int U = 4;                               // loads before the first one's use
+    const long long step = 256 >> N.tx_bits, first = blockIdx.x * U * step + (threadIdx.x >> N.tx_bits);
+    Largest m;
     for (long long c = (threadIdx.x & ((1 << N.tx_bits) - 1)) * 8; c < N.cols; c += 8ll << N.tx_bits) {
         const unsigned short *at = static_cast<const unsigned short *>(G.at) + c;
         const int n = N.cols - c < 8 ? (int)(N.cols - c) : 8;
-        if (n == 8)
-#pragma unroll 4
-            for (long long q = first; q < N.rows; q += step) m = largest(load_all<NET_F16, 8>(at + q * G.ld), m);
-        else
-            for (long long q = first; q < N.rows; q += step) m = largest(load_some<NET_F16, 8>(at + q * G.ld, n), m);
+#pragma unroll 1
+        for (long long q = first; q < N.rows; q += gridDim.x * U * step) {
+            if (n == 8 && q + (U - 1) * step < N.rows) {
+                Packed<NET_F16, 8> x[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) x[u] = load_all<NET_F16, 8>(at + (q + u * step) * G.ld);
+#pragma unroll
+                for (int u = 0; u < U; ++u) m.add(x[u]);
+            } else
+                for (int u = 0; u < U && q + u * step < N.rows; ++u) m.add(load_some<NET_F16, 8>(at + (q + u * step) * G.ld, n));
+        }
     }
-    m = largest_of<4>(m, s_most);
-    if (threadIdx.x == 0) most[blockIdx.x] = m;
+    const unsigned all = largest_of<4>(m.bits(), s_most);
+    if (threadIdx.x == 0) most[blockIdx.x] = all;
 }
 
 // dZ = drop(G act'(Z)), and the sums of its columns over a block's rows (either may be NULL).  134 M bf16 with Z in fp32 239 us (1.07 GB, 4.5 TB/s), beside Philox's arithmetic.
@@ -1517,9 +1526,13 @@ template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dz(RowsD N, 
     if constexpr (TYPE == NET_F16)
         if (most) {
             __shared__ unsigned s_most[4];
-            static_assert(LARGEST_BLOCKS == 512, "two a thread");
-            const unsigned a = most[threadIdx.x], b = most[threadIdx.x + 256];
-            const Power power = power_of(largest_of<4>(a > b ? a : b, s_most), D);
+            unsigned m = 0;
+#pragma unroll
+            for (int i = 0; i < LARGEST_BLOCKS; i += 256) {
+                const unsigned other = most[threadIdx.x + i];
+                m = other > m ? other : m;
+            }
+            const Power power = power_of(largest_of<4>(m, s_most), D);
             to = power.to;
             if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *factor = power.back;
         }

@@ -44,5 +44,5 @@ for type in range(3):
             assert ends().count("k_largest") == (dz and type == 2), (type, act, p, rows, outputs)
             assert backward(l, dx=None, dw=None) == OK and "k_largest" not in ends()           # dbias is made from dZ in fp32
 sizes = [L.fs_linear_bytes(ctypes.byref(layer(rows=5000, act=1, type=t)), 1) for t in (1, 2)]
-assert sizes[1] == sizes[0] + 256 + 2048
+assert sizes[1] == sizes[0] + 256 + 4096
 """, tmp_path)
