@@ -26,7 +26,7 @@
  *  - fp32 operands of the products go in as three bf16 parts each (24 bits together), of whose nine products the six largest are added: what is left out is
  *    below 2^-23 of |x w|, as fp32 rounds a product to 2^-24.  Operands below 2^-102 lose digits (the parts are normal numbers no more).
  *  - Results are the same from call to call on a device: no atomics.
- *  - NaN and infinities go through as the formulas say.
+ *  - NaN and infinities go through as the formulas say.  Blocks of fp32 results among which there are any are made twice: up to some ten times as long, where all are.
  *
  * Conventions of fastsnarf.h hold (device pointers, nothing synchronises, status codes, no exceptions or aborts), with these differences:
  *  - No context: the calls keep nothing.  They run on the current device and on the stream that is given, in memory that is given.  Calls that may

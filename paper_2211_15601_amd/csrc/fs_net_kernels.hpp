@@ -458,7 +458,7 @@ template <bool COL, int B, int BT> __device__ inline s16x8 operand(const short *
 }
 
 // Three bf16 parts of fp32 numbers: x = h + m + l to 24 bits and more, each part the rounded rest of those before it.  A rest that is no number
-// (of infinities) gives results that are none either, which k_product computes again.
+// (of infinities) gives results that are none either, which made_again() makes again.
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 __device__ inline void split8(const Packed<NET_F32, 8> &x, s16x8 *part)
@@ -477,12 +477,97 @@ __device__ inline void split8(const Packed<NET_F32, 8> &x, s16x8 *part)
     for (int k = 0; k < 3; ++k) part[k] = __builtin_bit_cast(s16x8, u32x4{w[k][0], w[k][1], w[k][2], w[k][3]});
 }
 
-// A result that is no finite number may be one of the parts' making (inf - inf, or a part of the largest numbers rounded up to infinity): it is computed plainly, then.
-__device__ inline float plain_dot(const float *x, long long step_x, const float *y, long long step_y, long long n)
+__device__ inline f32x16 mfma_bf16(s16x8 a, s16x8 b, f32x16 c) { return mfma<NET_BF16>(a, b, c); }
+__device__ inline f32x4 mfma_bf16(s16x8 a, s16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0); }
+
+// What eight numbers are beside infinities, as bf16: NaN, infinities and zeros themselves, 1 of the sign for all others.
+__device__ inline s16x8 kinds8(const float (&x)[8])
 {
-    float sum = 0.0f;
-    for (long long t = 0; t < n; ++t) sum = __builtin_fmaf(x[t * step_x], y[t * step_y], sum);
-    return sum;
+    unsigned w[4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const unsigned u = __float_as_uint(x[i]), size = u & 0x7FFFFFFFu, k = (u >> 16 & 0x8000u) | (size > 0x7F800000u ? 0x7FC0u : size == 0x7F800000u ? 0x7F80u : size ? 0x3F80u : 0u);
+        w[i / 2] = i & 1 ? w[i / 2] | k << 16 : k;
+    }
+    return __builtin_bit_cast(s16x8, u32x4{w[0], w[1], w[2], w[3]});
+}
+
+// A wave's results (those of one matrix instruction, get(i) and set(i, value)) that are no finite numbers, made again: they may be the parts' making (inf - inf, or a part
+// of the largest numbers rounded up to infinity).  p(x, s) and q(x, s): a lane's elements of step s of the operands, in fp32.
+//  1. A sum over the products of kinds is no finite number where NaN or infinities take part, and is then what theirs is.
+//  2. Else the products or their parts passed 2^128: the parts of operands times 2^-64 do not.  What that takes from operands below 2^-38 is below 2^-62 times the
+//     other's size, which sums beyond 2^128 do not hold.
+// Bound by latency: a step's loads, past LDS, are waited for one step after another.  A batch of NaN, us, with it and without NaN: 2048 cubed forward 960 and 94, backward of
+// 65536 x 128 x 128 270 and 50; finite sums beyond 2^128 take the second pass too (2048 cubed 1850).  A scalar sum for each result took 15200 and 7400.
+template <class V, class P, class Q, class Get, class Set> __device__ inline void made_again(long long steps, P p, Q q, Get get, Set set)
+{
+    constexpr int N = sizeof(V) / 4;
+    auto no_number = [&](int i) { return !(fabsf(get(i)) < INFINITY); };
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < N; ++i) bad |= no_number(i);
+    if (!__any(bad)) return;
+    constexpr int PA[6] = {0, 1, 2, 0, 1, 0}, PB[6] = {2, 1, 0, 1, 0, 0};
+    unsigned left = 0;                 // bits of those that are left to the second pass
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+        V sum;
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum[i] = 0.0f;
+        auto parts = [&](const float (&x)[8], s16x8 *to) {
+            if (pass == 0) {
+                to[0] = kinds8(x);
+                return;
+            }
+            Packed<NET_F32, 8> small;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) small.w[i] = __float_as_uint(x[i] * 0x1p-64f);
+            split8(small, to);
+        };
+#pragma unroll 1
+        for (long long s = 0; s < steps; ++s) {
+            s16x8 u[3], w[3];
+            float x[8];
+            p(x, s);
+            parts(x, u);
+            __builtin_amdgcn_sched_barrier(0);         // one operand after the other: few registers
+            q(x, s);
+            parts(x, w);
+            if (pass == 0) sum = mfma_bf16(u[0], w[0], sum);
+            else
+#pragma unroll
+                for (int i = 0; i < 6; ++i) sum = mfma_bf16(u[PA[i]], w[PB[i]], sum);
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (pass == 0 && no_number(i)) {
+                if (fabsf(sum[i]) < INFINITY) left |= 1u << i;
+                else set(i, sum[i]);
+            }
+            if (pass == 1 && left >> i & 1) set(i, sum[i] * 0x1p64f * 0x1p64f);
+        }
+        if (!__any(left)) return;
+    }
+}
+
+// ... of results in registers
+template <class V, class P, class Q> __device__ inline void made_again(V &v, long long steps, P p, Q q)
+{
+    made_again<V>(steps, p, q, [&](int i) { return v[i]; }, [&](int i, float x) { v[i] = x; });
+}
+
+// Eight elements of row (COL: column) r from t on, zeros from t1 on.  t1 is at least 1.
+template <int TYPE, bool COL> __device__ inline void eight(float (&x)[8], const MatD &M, long long r, long long t, long long t1)
+{
+    const typename ElemOf<TYPE>::type *at = static_cast<const typename ElemOf<TYPE>::type *>(M.at);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const long long n = t + k < t1 ? t + k : t1 - 1;
+        x[k] = widen<TYPE>(at[COL ? n * M.ld + r : r * M.ld + n]);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        if (t + k >= t1) x[k] = 0.0f;
 }
 
 // One operand's tile on its way from memory to LDS: B rows (p or q) by BT, in chunks of 8.
@@ -573,7 +658,7 @@ template <int TYPE, bool COL, int B, int BT, int THREADS> struct Stage {
 };
 
 // The end of a product: a wave's results, MT by NT squares from (p0, q0) on, go through LDS (end_floats(MT) of its own), 32 rows q and up to 64 p at a time,
-// so that rows leave in whole lines.  fp32: a result that is no finite number is what again(q, p) says.
+// so that rows leave in whole lines.  fp32: again(p, q, get, set) makes those of a square that are no finite numbers again.
 constexpr __host__ __device__ int end_floats(int mt) { return 32 * ((mt > 1 ? 64 : 32) + 4); }
 
 template <int TYPE, bool LAYER, int MT, int NT, class Again>
@@ -602,10 +687,10 @@ __device__ inline void product_end(const f32x16 (&acc)[MT][NT], float *out, int 
                             for (int m = 0; m < 4; ++m) bad |= !(fabsf(v[m]) < INFINITY);
                     }
         if (TYPE == NET_F32 && __any(bad))
-            for (int i = 0; i < 16 * MG; ++i) {        // each lane those that it wrote
-                float *x = out + (lane & 31) * PITCH + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3);
-                const long long q = q0 + h % NT * 32 + (lane & 31), p = p0 + h / NT * PW + (x - out - (lane & 31) * PITCH);
-                if (!(fabsf(*x) < INFINITY) && p < np && q < nq) *x = again(q, p);
+#pragma unroll 1
+            for (int i = 0; i < MG; ++i) {             // each lane those that it wrote
+                float *x = out + (lane & 31) * PITCH + 32 * i + 4 * (lane >> 5);
+                again(p0 + h / NT * PW + 32 * i, q0 + h % NT * 32, [&](int k) { return x[8 * (k >> 2) + (k & 3)]; }, [&](int k, float v) { x[8 * (k >> 2) + (k & 3)] = v; });
             }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -792,10 +877,14 @@ __global__ __launch_bounds__(64 * WP * WQ, TYPE == NET_F32 && BP * BQ == 128 * 1
         __syncthreads();
     }
 
-    // (see plain_dot)
-    auto again = [&](long long q, long long p) {
-        return plain_dot(static_cast<const float *>(P.at) + (PCOL ? t0 * P.ld + p : p * P.ld + t0), PCOL ? P.ld : 1, static_cast<const float *>(Q.at) + (QCOL ? t0 * Q.ld + q : q * Q.ld + t0),
-                         QCOL ? Q.ld : 1, t1 - t0);
+    auto again = [&](long long p, long long q, auto get, auto set) {            // rows beyond the last: the last one, whose results go nowhere
+        p += lane & 31;
+        q += lane & 31;
+        p = p < np ? p : np - 1;
+        q = q < nq ? q : nq - 1;
+        auto at = [&](long long s) { return t0 + 16 * s + 8 * (lane >> 5); };
+        made_again<f32x16>((t1 - t0 + 15) / 16, [&](float (&x)[8], long long s) { eight<NET_F32, PCOL>(x, P, p, at(s), t1); },
+                           [&](float (&x)[8], long long s) { eight<NET_F32, QCOL>(x, Q, q, at(s), t1); }, get, set);
     };
     product_end<TYPE, !PCOL, MT, NT>(acc, reinterpret_cast<float *>(s_mem) + wave * end_floats(MT), lane, p0 + wp * MT * 32, q0 + wq * NT * 32, np, nq, part, E, again);
 }
@@ -943,7 +1032,7 @@ __global__ __launch_bounds__(512) void k_product_big(MatD P, MatD Q, long long n
         }
         __syncthreads();
     }
-    product_end<TYPE, !PCOL, MT, NT>(acc, reinterpret_cast<float *>(s_mem) + wave * end_floats(MT), lane, p0 + wp * MT * 32, q0 + wq * NT * 32, np, nq, part, E, [](long long, long long) { return 0.0f; });
+    product_end<TYPE, !PCOL, MT, NT>(acc, reinterpret_cast<float *>(s_mem) + wave * end_floats(MT), lane, p0 + wp * MT * 32, q0 + wq * NT * 32, np, nq, part, E, [](long long, long long, auto, auto) {});
 }
 
 // The parts' sums and what becomes of them, 256 neighbours p of one row q at a time.  SPLIT: a block's four waves add every fourth part each and the first of
@@ -1091,6 +1180,22 @@ __global__ __launch_bounds__(1024) void k_few(MatD W, MatD X, long long np, long
         }
         multiply(c);
     }
+    if constexpr (TYPE == NET_F32) {
+        // of its own steps: the stretch, single ones, and the end
+        const long long rest = whole - groups * AHEAD - wave, stretch = end - first, steps = stretch + (rest > 0 ? (rest + waves - 1) / waves : 0) + (whole * 32 < nt && wave == waves - 1);
+        auto at = [&](long long s) {
+            const bool last = whole * 32 < nt && wave == waves - 1 && s == steps - 1;
+            return 32 * (s < stretch ? first + s : last ? whole : groups * AHEAD + wave + (s - stretch) * waves) + 8 * (lane >> 4);
+        };
+#pragma unroll
+        for (int i = 0; i < MP; ++i)
+#pragma unroll
+            for (int k = 0; k < NQ; ++k) {
+                const long long p = p0 + 16 * i + (lane & 15), q = 16 * k + (lane & 15);
+                made_again(acc[i][k], steps, [&](float (&x)[8], long long s) { eight<NET_F32, false>(x, W, p < np ? p : np - 1, at(s), nt); },
+                           [&](float (&x)[8], long long s) { eight<NET_F32, false>(x, X, q < nq ? q : nq - 1, at(s), nt); });
+            }
+    }
 #pragma unroll
     for (int i = 0; i < MP; ++i)
 #pragma unroll
@@ -1101,11 +1206,6 @@ __global__ __launch_bounds__(1024) void k_few(MatD W, MatD X, long long np, long
 #pragma unroll 4
     for (int i = 1; i < waves; ++i) sum += *reinterpret_cast<const f32x4 *>(s_sum[i][j][lane]);
     float v[4] = {sum[0], sum[1], sum[2], sum[3]};
-    if constexpr (TYPE == NET_F32) {
-#pragma unroll 1
-        for (int i = 0; i < 4; ++i)
-            if (i < n && !(fabsf(v[i]) < INFINITY)) v[i] = plain_dot(static_cast<const float *>(W.at) + (p + i) * W.ld, 1, static_cast<const float *>(X.at) + q * X.ld, 1, nt);
-    }
     with_act(E.act, [&](auto act) { finish4<TYPE, decltype(act)::value>(v, bias, r, E, seed, to, 0, (unsigned long long)q * np + p, n); });
 }
 
@@ -1118,24 +1218,34 @@ template <int B> __device__ inline int place_both(int t, int c) { return t * B +
 // What dZ is made from.
 struct DzD { MatD G, Z; int z_f32, act; float beta; DropD drop; };
 
-// One element of it, in fp32
-template <int TYPE> __device__ inline float dz_at(const DzD &D, const Seed &seed, long long q, long long n)
+// Eight elements of it in fp32, k of them at (q(k), n(k)); zeros where there is none.
+template <int TYPE, class Q, class N> __device__ inline void dz_eight(float (&x)[8], const DzD &D, const Seed &seed, Q q, N n)
 {
     typedef typename ElemOf<TYPE>::type T;
-    float g = widen<TYPE>(static_cast<const T *>(D.G.at)[q * D.G.ld + n]);
-    if (D.act != ACT_NONE) {
-        const long long at = q * D.Z.ld + n;
-        const float z = TYPE == NET_F32 || D.z_f32 ? static_cast<const float *>(D.Z.at)[at] : widen<TYPE>(static_cast<const T *>(D.Z.at)[at]);
-        float s = 1.0f;
-        with_act(D.act, [&](auto kind) { s = slope_of<decltype(kind)::value>(z, D.beta); });
-        g *= s;
+    const long long rows = D.G.rows, cols = D.G.cols;
+    float z[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const long long r = q(k) < rows ? q(k) : rows - 1, c = n(k) < cols ? n(k) : cols - 1;
+        x[k] = widen<TYPE>(static_cast<const T *>(D.G.at)[r * D.G.ld + c]);
+        z[k] = 0.0f;
+        if (D.act != ACT_NONE) z[k] = TYPE == NET_F32 || D.z_f32 ? static_cast<const float *>(D.Z.at)[r * D.Z.ld + c] : widen<TYPE>(static_cast<const T *>(D.Z.at)[r * D.Z.ld + c]);
     }
-    if (D.drop.mode == 0) return g;
-    if (D.drop.mode == 2) return 0.0f;
-    const unsigned long long e = (unsigned long long)q * D.G.cols + n;
-    const uint4 w = philox(e >> 2, seed.offset, seed.seed);
-    const unsigned word = e & 2 ? (e & 1 ? w.w : w.z) : (e & 1 ? w.y : w.x);
-    return word >= D.drop.least ? g * D.drop.scale : 0.0f;
+    with_act(D.act, [&](auto kind) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] *= slope_of<decltype(kind)::value>(z[k], D.beta);
+    });
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        if (D.drop.mode == 1) {
+            const unsigned long long e = (unsigned long long)q(k) * cols + n(k);
+            const uint4 w = philox(e >> 2, seed.offset, seed.seed);
+            const unsigned word = e & 2 ? (e & 1 ? w.w : w.z) : (e & 1 ? w.y : w.x);
+            x[k] = word >= D.drop.least ? x[k] * D.drop.scale : 0.0f;
+            __builtin_amdgcn_sched_barrier(0);         // one after another: few registers
+        }
+        if (D.drop.mode == 2 || q(k) >= rows || n(k) >= cols) x[k] = 0.0f;
+    }
 }
 
 // The backward pass of a layer of at most B inputs and B outputs, in one pass over its rows: G, Z and X are read once, dX is written, dweight stays in registers and the
@@ -1143,7 +1253,7 @@ template <int TYPE> __device__ inline float dz_at(const DzD &D, const Seed &seed
 //   dweight: WP x WQ waves share the B x B results, t = rows.  dX: 32 inputs a wave, t = outputs; where there are twice the waves, two share those.
 // RESTS (16 bits): dZ goes in as two parts, itself rounded and what that leaves, for layers whose dZ has too few values to average its rounding out.  A rest of 0 would make
 // a NaN of another operand's infinity: dX has sums of its own for the rests, and leaves them out where the others' are no finite numbers; dweight (whose second sums would
-// take 437 registers, one block a compute unit) makes such results again, plainly.  Forward and backward of 1024 x 64 x 64 bf16, gelu, 21.5 us, by one part 17.1; of
+// take 437 registers, one block a compute unit) makes such results again.  Forward and backward of 1024 x 64 x 64 bf16, gelu, 21.5 us, by one part 17.1; of
 // 65536 x 128 x 128 87, by one 67: there one part is taken.
 // 65536 x 128 x 128 fp32 56 us (134 MB, 2.3 TB/s): four barriers every 32 rows, between which loads, parts and products follow one another.  For 256 x 256 in 16 bits, one
 // block a compute unit, that took 624 us against 556 of the other kernels, so B is 128.
@@ -1324,6 +1434,18 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_narrow(DzD D, MatD X, MatD W,
             const int q = lane & 31, quad = (pb + 8 * gq + 4 * (lane >> 5)) / 4;
             *reinterpret_cast<f32x4 *>(s_out + half * R * B + q * B + ((quad ^ (q & 15)) * 4)) = f32x4{d[4 * gq], d[4 * gq + 1], d[4 * gq + 2], d[4 * gq + 3]};
         }
+        bool bad = false;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) bad |= !(fabsf(d[k]) < INFINITY);
+        if (TYPE == NET_F32 && __any(bad)) {
+            const long long p = pb + (lane & 31) < inputs ? pb + (lane & 31) : inputs - 1, q = q0 + (lane & 31);
+            float *row = s_out + half * R * B + (lane & 31) * B;
+            auto place = [&](int i) { return row + ((((pb + 8 * (i >> 2) + 4 * (lane >> 5)) / 4 ^ (lane & 15)) * 4) + (i & 3)); };
+            auto at = [&](long long s) { return 16 * (half * STEPS + s) + 8 * (lane >> 5); };
+            made_again<f32x16>(STEPS, [&](float (&x)[8], long long s) { eight<TYPE, true>(x, W, p, at(s), outputs); },
+                               [&](float (&x)[8], long long s) { dz_eight<TYPE>(x, D, seed, [&](int) { return q; }, [&](int k) { return at(s) + k; }); },
+                               [&](int i) { return *place(i); }, [&](int i, float v) { *place(i) = v; });
+        }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < R * B / 4 / THREADS; ++i) {
@@ -1337,14 +1459,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_narrow(DzD D, MatD X, MatD W,
                 if constexpr (TYPE == NET_F16)
 #pragma unroll
                     for (int k = 0; k < 4; ++k) v[k] *= power.back;
-                if constexpr (TYPE == NET_F32)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        if (k < n && !(fabsf(v[k]) < INFINITY)) {              // as in k_product
-                            float sum = 0.0f;
-                            for (long long m = 0; m < outputs; ++m) sum = __builtin_fmaf(dz_at<TYPE>(D, seed, q, m), static_cast<const float *>(W.at)[m * W.ld + p + k], sum);
-                            v[k] = sum;
-                        }
                 store_some<TYPE, 4>(static_cast<T *>(dx) + q * lddx + p, v, n);
             }
         }
@@ -1353,30 +1467,34 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_narrow(DzD D, MatD X, MatD W,
 
     // dweight's part, [outputs][ldw]
     float *part = dw + (long long)blockIdx.x * outputs * ldw;
-    if (dw)
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int gq = 0; gq < 4; ++gq) {
-                const long long p = (wp * MT + i) * 32 + 8 * gq + 4 * (lane >> 5), q = (wq * NT + j) * 32 + (lane & 31);
-                if (p >= inputs || q >= outputs) continue;
-                f32x4 v = {acc[i][j][4 * gq], acc[i][j][4 * gq + 1], acc[i][j][4 * gq + 2], acc[i][j][4 * gq + 3]};
-                if constexpr (TYPE == NET_F16) v *= power.back;
-                *reinterpret_cast<f32x4 *>(part + q * ldw + p) = v;
-            }
-    if ((TYPE == NET_F32 || RESTS) && dw) {       // results that are no finite numbers, plainly
-        __syncthreads();
-        for (long long e = tid; e < outputs * inputs; e += THREADS) {
-            const long long q = e / inputs, p = e % inputs;
-            float sum = part[q * ldw + p];
-            if (fabsf(sum) < INFINITY) continue;
-            sum = 0.0f;
-            for (long long m0 = (long long)blockIdx.x * R; m0 < rows; m0 += stride)
-                for (long long m = m0; m < m0 + R && m < rows; ++m) sum = __builtin_fmaf(dz_at<TYPE>(D, seed, m, q), widen<TYPE>(static_cast<const T *>(X.at)[m * X.ld + p]), sum);
-            part[q * ldw + p] = sum;
+    auto put = [&](f32x16 v, int h) {
+        if constexpr (TYPE == NET_F16) v *= power.back;
+        const long long pb = (wp * MT + h / NT) * 32, qb = (wq * NT + h % NT) * 32;
+        if constexpr (TYPE == NET_F32 || RESTS) {
+            const long long p = pb + (lane & 31) < inputs ? pb + (lane & 31) : inputs - 1, q = qb + (lane & 31), groups = (rows - (long long)blockIdx.x * R + stride - 1) / stride;
+            auto at = [&](long long s) { return (blockIdx.x + (s >> 1) * gridDim.x) * R + 16 * (s & 1) + 8 * (lane >> 5); };
+            made_again(v, 2 * groups, [&](float (&x)[8], long long s) { eight<TYPE, true>(x, X, p, at(s), rows); },
+                       [&](float (&x)[8], long long s) { dz_eight<TYPE>(x, D, seed, [&](int k) { return at(s) + k; }, [&](int) { return q; }); });
         }
+#pragma unroll
+        for (int gq = 0; gq < 4; ++gq) {
+            const long long p = pb + 8 * gq + 4 * (lane >> 5), q = qb + (lane & 31);
+            if (p < inputs && q < outputs) *reinterpret_cast<f32x4 *>(part + q * ldw + p) = f32x4{v[4 * gq], v[4 * gq + 1], v[4 * gq + 2], v[4 * gq + 3]};
+        }
+    };
+    if (dw) {
+        if constexpr (TYPE == NET_F32 || RESTS) {
+#pragma unroll 1
+            for (int h = 0; h < MT * NT; ++h) {        // one copy of the code
+                f32x16 v;
+#pragma unroll
+                for (int k = 0; k < MT * NT; ++k)
+                    if (k == h) v = acc[k / NT][k % NT];
+                put(v, h);
+            }
+        } else
+#pragma unroll
+            for (int h = 0; h < MT * NT; ++h) put(acc[h / NT][h % NT], h);
     }
     if (!sums) return;
     // dbias' part: a thread's columns are those of every PER_ROW-th other
