@@ -337,7 +337,9 @@ Backward plan_backward(const fs_linear &l, int cus)
     b.dz = plan_rows(l.type, l.rows, l.outputs, l.outputs, DZ_BLOCKS);
     b.has_dz = act_kind(l) != FS_ACT_NONE || l.drop.p > 0.0;
     b.narrow = std::min({l.rows, l.inputs, l.outputs}) > 0 && std::max(l.inputs, l.outputs) <= NARROW && (l.type == FS_FLOAT_FULL || l.rows <= NARROW_ROWS);
-    const long long per_cu = l.type != FS_FLOAT_FULL ? 3 : 1;
+    // as many as a compute unit holds: registers and LDS leave room for two blocks of 16 bits and one of fp32.  Forward and backward, us, of bf16 with two, three and four blocks:
+    // 65536 x 128 x 128 57, 65 and 70, 131072 x 10 x 9 64, 77 and 70, 30000 x 128 x 128 38, 48 and 52.
+    const long long per_cu = l.type != FS_FLOAT_FULL ? 2 : 1;
     b.blocks = (int)std::max<long long>(1, std::min<long long>(per_cu * cus, (l.rows + 31) / 32));
     if (b.narrow) {                    // no dZ, and no products' parts
         b.end = narrow_sums(l, b) + up((int64_t)b.blocks * l.outputs * 4);

@@ -1320,7 +1320,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_narrow(DzD D, MatD X, MatD W,
     long long q0 = (long long)blockIdx.x * R;
     Power power = {1.0f, 1.0f};
     if constexpr (TYPE == NET_F16)
-        if (D.act != ACT_NONE || D.drop.mode == 1) {       // a block's own (see power_of): its rows of G are read twice, six groups of 32 at most
+        if (D.act != ACT_NONE || D.drop.mode == 1) {       // a block's own (see power_of): its rows of G are read twice, eight groups of 32 at most
             __shared__ unsigned s_most[WAVES];
             Largest most;
             for (long long q = q0 + r0; q < rows + r0; q += stride)
