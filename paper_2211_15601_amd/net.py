@@ -157,6 +157,18 @@ def _forward(plan, shape, x, weight, bias, residual, keep_z, seed):
     return y, z
 
 
+class _Last(torch.autograd.Function):
+    """Gradients that have none themselves.  Who differentiates them is told so; PyTorch would take them for constants, although they depend on the tensors that were saved."""
+
+    @staticmethod
+    def forward(ctx, mark, *grads):
+        return tuple(None if g is None else g.view_as(g) for g in grads)
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("layers have no second derivatives")
+
+
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, residual, plan, shape, seed):
@@ -170,7 +182,6 @@ class _Linear(torch.autograd.Function):
         return y
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, g):
         if g is None:
             return (None,) * 7
@@ -189,6 +200,8 @@ class _Linear(torch.autograd.Function):
             _call(plan.index, plan.backward, plan.layer(ctx.seed if words is None else words), G.data_ptr(), G.stride(0), None if X is None else X.data_ptr(),
                   0 if X is None else X.stride(0), None if w is None else w.data_ptr(), 0 if w is None else w.stride(0), None if z is None else z.data_ptr(), outputs, None if dx is None else dx.data_ptr(), inputs,
                   None if dw is None else dw.data_ptr(), inputs, None if db is None else db.data_ptr(), None if work is None else work.data_ptr(), n)
+            if torch.is_grad_enabled():                # create_graph
+                dx, dw, db = _Last.apply(torch.empty(0, requires_grad=True), dx, dw, db)
         return dx, dw, db, g if need_r else None, None, None, None
 
 

@@ -61,3 +61,27 @@ def test_values_that_are_negated_lazily(fake):  # noqa: F811
     net.dropout(negated(3, 1), 0.5, (1, 2), residual=negated(3, 1))
     net.dropout(negated(3, 2), 0.5, (1, 2), residual=negated(3, 2))
     assert seen == [[-1.0] * 4, [-1.0] * 2, [-1.0] * 2]
+
+
+def test_second_derivatives_are_not_lost(fake):  # noqa: F811
+    """A penalty on a gradient (of a field's normals, say): the gradients of x, weight and bias depend on x and weight, also where the loss is a sum and its own gradient constant."""
+    from paper_2211_15601_amd import net
+    leaf = lambda *shape: on_gpu(*shape).requires_grad_(True)
+    for act in ("none", "softplus"):
+        for of in range(3):
+            leaves = [leaf(4, 6), leaf(8, 6), leaf(8)]
+            y = net.linear(*leaves, activation=act)
+            (d,) = torch.autograd.grad(y.sum(), leaves[of], create_graph=True)
+            assert d.shape == leaves[of].shape and d.requires_grad
+            with pytest.raises(RuntimeError, match="no second derivatives"):
+                (y.sum() + d.square().sum()).backward()
+    # a gradient that is only looked at, beside others; the residual's is y's own
+    leaves, r = [leaf(4, 6), leaf(8, 6), leaf(8)], leaf(4, 8)
+    y = net.linear(*leaves, residual=r)
+    g = on_gpu(4, 8, fill=3.0).requires_grad_(True)
+    grads = torch.autograd.grad(y, [*leaves, r], g, create_graph=True)
+    assert [d.shape for d in grads] == [t.shape for t in (*leaves, r)]
+    (again,) = torch.autograd.grad(grads[3].square().sum(), g)
+    assert torch.equal(again, 2 * g.detach())
+    y.sum().backward()
+    assert all(t.grad is not None and not t.grad.requires_grad for t in leaves)
