@@ -158,10 +158,11 @@ def _forward(plan, shape, x, weight, bias, residual, keep_z, seed):
 
 
 class _Last(torch.autograd.Function):
-    """Gradients that have none themselves.  Who differentiates them is told so; PyTorch would take them for constants, although they depend on the tensors that were saved."""
+    """Gradients that have none themselves.  Who differentiates them is told so; PyTorch would take them for constants, although they depend on y's gradient `g` and, by way of
+    the layer's `mark`, on its inputs."""
 
     @staticmethod
-    def forward(ctx, mark, *grads):
+    def forward(ctx, mark, g, *grads):
         return tuple(None if g is None else g.view_as(g) for g in grads)
 
     @staticmethod
@@ -177,18 +178,19 @@ class _Linear(torch.autograd.Function):
         y, z = _forward(plan, shape, x, weight, bias, residual, own and plan.bare.act != binding.FS_ACT_NONE, seed)
         words = seed if isinstance(seed, torch.Tensor) else None
         ctx.plan, ctx.seed, ctx.shape, ctx.bias_type = plan, None if words is not None else seed, x.shape, None if bias is None else bias.dtype
-        ctx.save_for_backward(x if need_w else None, weight if need_x else None, z, words if own else None)
+        mark = torch.empty(0) if own else None         # a second result, of nothing: what _Last knows the layer by
+        ctx.save_for_backward(x if need_w else None, weight if need_x else None, z, words if own else None, mark)
         ctx.set_materialize_grads(False)
-        return y
+        return y, mark
 
     @staticmethod
-    def backward(ctx, g):
+    def backward(ctx, g, _):
         if g is None:
             return (None,) * 7
         need_x, need_w, need_b, need_r = ctx.needs_input_grad[:4]
         dx = dw = db = None
         if need_x or need_w or need_b:
-            x, weight, z, words = ctx.saved_tensors
+            x, weight, z, words, mark = ctx.saved_tensors
             plan = ctx.plan
             G, w, X = _rows(g), None if weight is None else _rows(weight), None if x is None else _rows(x)
             outputs, inputs = plan.bare.outputs, plan.bare.inputs
@@ -201,7 +203,7 @@ class _Linear(torch.autograd.Function):
                   0 if X is None else X.stride(0), None if w is None else w.data_ptr(), 0 if w is None else w.stride(0), None if z is None else z.data_ptr(), outputs, None if dx is None else dx.data_ptr(), inputs,
                   None if dw is None else dw.data_ptr(), inputs, None if db is None else db.data_ptr(), None if work is None else work.data_ptr(), n)
             if torch.is_grad_enabled():                # create_graph
-                dx, dw, db = _Last.apply(torch.empty(0, requires_grad=True), dx, dw, db)
+                dx, dw, db = _Last.apply(mark, g, dx, dw, db)
         return dx, dw, db, g if need_r else None, None, None, None
 
 
@@ -247,7 +249,7 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] =
     if forward_ad._current_level >= 0:
         _check_tangents(x, weight, bias, residual)
     if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or bias is not None and bias.requires_grad or residual is not None and residual.requires_grad):
-        return _Linear.apply(x, weight, bias, residual, plan, y_shape, seed)
+        return _Linear.apply(x, weight, bias, residual, plan, y_shape, seed)[0]
     return _forward(plan, y_shape, x, weight, bias, residual, False, seed)[0]
 
 

@@ -85,3 +85,22 @@ def test_second_derivatives_are_not_lost(fake):  # noqa: F811
     assert torch.equal(again, 2 * g.detach())
     y.sum().backward()
     assert all(t.grad is not None and not t.grad.requires_grad for t in leaves)
+
+
+@pytest.mark.parametrize("act", ["none", "silu"])
+def test_second_derivatives_towards_every_input(fake, act):  # noqa: F811
+    """Also where only some inputs' derivatives are asked for, and those that are not found may be left out, as torch.autograd.functional does."""
+    from paper_2211_15601_amd import net
+    for wanted in range(1, 8):
+        leaves = [on_gpu(*shape).requires_grad_(bool(wanted >> i & 1)) for i, shape in enumerate(((4, 6), (8, 6), (8,)))]
+        asked = [t for t in leaves if t.requires_grad]
+        g = on_gpu(4, 8, fill=1.0).requires_grad_(True)
+        for first in asked:
+            for second in (*asked, g):
+                y = net.linear(*leaves, activation=act)
+                (d,) = torch.autograd.grad(y, first, g, create_graph=True)
+                with pytest.raises(RuntimeError, match="no second derivatives"):
+                    torch.autograd.grad(d.sum(), second, allow_unused=True)
+    for f in (lambda t: torch.autograd.functional.hessian(lambda v: net.linear(v, on_gpu(8, 6), activation=act).sum(), t), lambda t: torch.autograd.functional.jvp(lambda v: net.linear(v, on_gpu(8, 6), activation=act), t, t)):
+        with pytest.raises(RuntimeError, match="no second derivatives"):
+            f(on_gpu(4, 6))
