@@ -14,8 +14,8 @@ counts the offset up drops other elements at each replay).  The same words drop 
 The mask is not stored: the backward pass makes it anew.
 
 Calls run on the stream that is current when they are made, wait for nothing, keep nothing but what autograd saves, and can be captured into graphs of torch.cuda.
-A captured backward pass needs its forward pass in the same capture, and no eager graph of the same leaves alive.  Forward-mode derivatives, second derivatives and
-traces are refused (torch.compile goes round the calls).  There is no CPU fallback."""
+A captured backward pass needs its forward pass in the same capture, and no eager graph of the same leaves alive.  Forward-mode derivatives, second derivatives of
+linear() and traces are refused (torch.compile goes round the calls).  There is no CPU fallback."""
 from __future__ import annotations
 
 import ctypes
@@ -271,13 +271,15 @@ class _Dropout(torch.autograd.Function):
         return _dropped(x, residual, p, seed)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, g):
         if g is None:
             return None, None, None, None
         (words,) = ctx.saved_tensors
         p, seed = ctx.how
-        dx = _dropped(g, None, p, seed if words is None else words) if ctx.needs_input_grad[0] else None
+        seed = seed if words is None else words
+        dx = None
+        if ctx.needs_input_grad[0]:                    # dropout again, and differentiated as that where gradients of gradients are asked for
+            dx = _Dropout.apply(g, None, p, seed) if torch.is_grad_enabled() and g.requires_grad else _dropped(g, None, p, seed)
         return dx, g if ctx.needs_input_grad[1] else None, None, None
 
 

@@ -104,3 +104,27 @@ def test_second_derivatives_towards_every_input(fake, act):  # noqa: F811
     for f in (lambda t: torch.autograd.functional.hessian(lambda v: net.linear(v, on_gpu(8, 6), activation=act).sum(), t), lambda t: torch.autograd.functional.jvp(lambda v: net.linear(v, on_gpu(8, 6), activation=act), t, t)):
         with pytest.raises(RuntimeError, match="no second derivatives"):
             f(on_gpu(4, 6))
+
+
+def test_dropout_is_its_own_derivative(fake):  # noqa: F811
+    """Its gradient is dropout of y's gradient, and is differentiated as such."""
+    import ctypes
+    from paper_2211_15601_amd import net
+    words = on_gpu(2, dtype=torch.int64)
+
+    def double(kind, rows, columns, drop, x, ldx, r, ldr, y, ldy, stream):
+        """stands for drop(): twice of everything"""
+        for i in range(rows):
+            for j in range(columns):
+                at = lambda p, ld: ctypes.c_float.from_address(p + 4 * (i * ld + j))
+                at(y, ldy).value = 2.0 * at(x, ldx).value + (at(r, ldr).value if r else 0.0)
+        return 0
+
+    fake.fs_dropout = double
+    for seed in ((1, 2), words):
+        x, r = on_gpu(3, 4, fill=3.0).requires_grad_(True), on_gpu(3, 4, fill=1.0).requires_grad_(True)
+        y = net.dropout(x, 0.5, seed, residual=r)
+        dx, dr = torch.autograd.grad(y.square().sum(), [x, r], create_graph=True)     # y = 2 x + r: 4 y and 2 y
+        assert bool((dx == 28.0).all()) and bool((dr == 14.0).all())
+        assert bool((torch.autograd.grad(dx.sum() + dr.sum(), x, retain_graph=True)[0] == 8.0 + 4.0).all())
+        assert bool((torch.autograd.grad(dx.sum(), r)[0] == 4.0).all())
