@@ -294,15 +294,14 @@ template <int TYPE> void launch_dz(const RowsPlan &p, const MatD &G, const MatD 
 
 int64_t up(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// The backward pass's workspace: dZ (where it is not G itself), the sums of its columns, parts of either product, and of fp16 the factor and its numbers.  narrow: k_narrow's, parts of dweight and of dbias by
-// `blocks` blocks, and nothing else.
-// Inputs and outputs of a layer whose backward pass is k_narrow's: two launches instead of five or six, 7 us each on the thread that runs backward passes.  Kernels, us, this and
-// the others: fp32 1024 x 64 x 64 13.4 and 20.0, 65536 x 128 x 128 66 and 77, 524288 x 32 x 128 252 and 341; bf16 9.6 and 15.6, 51 and 49, 187 and 169: long ones
-// of 16 bits take the others.
+// The backward pass's workspace: dZ (where it is not G itself), the sums of its columns, parts of either product, and of fp16 the factor and its numbers.
+// narrow: k_narrow's, parts of dweight and of dbias by `blocks` blocks, and nothing else.
+// Inputs and outputs of a layer whose backward pass is k_narrow's: two launches instead of five or six, 7 us each on the thread that runs backward passes, and no dZ in memory.
+// Kernels, us, this and the others: fp32 1024 x 64 x 64 12.1 and 20.7, 65536 x 128 x 128 48 and 73, 524288 x 32 x 128 260 and 390; bf16 14.7 and 16.7, 40 and 47, 185 and 201,
+// 262144 x 128 x 128 106 and 123.
 constexpr int NARROW = 128;
-constexpr int64_t NARROW_ROWS = 131072;
 // Values of dZ up to which those of 16 bits keep what its rounding leaves.  The results' own rounding and dZ's make 1.41 times the error of the first alone; of few values
-// by chance more (2 x 27 x 2 fp16, silu: 3.2 times), and of one output, whose rows may cancel (87983 x 1 x 1 fp16: 21): all of those that k_narrow takes are below this.
+// by chance more (2 x 27 x 2 fp16, silu: 3.2 times), and of one output, whose rows may cancel (87983 x 1 x 1 fp16: 21).
 constexpr int64_t NARROW_RESTS = 1 << 17;
 
 struct Backward {
@@ -336,7 +335,7 @@ Backward plan_backward(const fs_linear &l, int cus)
     b.dw = plan_product(l.type, l.inputs, l.outputs, l.rows, cus);
     b.dz = plan_rows(l.type, l.rows, l.outputs, l.outputs, DZ_BLOCKS);
     b.has_dz = act_kind(l) != FS_ACT_NONE || l.drop.p > 0.0;
-    b.narrow = std::min({l.rows, l.inputs, l.outputs}) > 0 && std::max(l.inputs, l.outputs) <= NARROW && (l.type == FS_FLOAT_FULL || l.rows <= NARROW_ROWS);
+    b.narrow = std::min({l.rows, l.inputs, l.outputs}) > 0 && std::max(l.inputs, l.outputs) <= NARROW;
     // as many as a compute unit holds: registers and LDS leave room for two blocks of 16 bits and one of fp32.  Forward and backward, us, of bf16 with two, three and four blocks:
     // 65536 x 128 x 128 57, 65 and 70, 131072 x 10 x 9 64, 77 and 70, 30000 x 128 x 128 38, 48 and 52.
     const long long per_cu = l.type != FS_FLOAT_FULL ? 2 : 1;

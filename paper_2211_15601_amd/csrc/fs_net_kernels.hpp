@@ -142,7 +142,7 @@ template <int TYPE, int N> __device__ inline void store_some(typename ElemOf<TYP
 
 // ---------------------------------------------------------------------------------------------------------------- dropout
 
-// Philox4x32-10.  Ten rounds take a large bf16 dropout 7 % longer than none at all: 512 MB read and 512 MB written in 205 and 190 us (seven rounds: 196).
+// Philox4x32-10.  Ten rounds take a large bf16 dropout 8 % longer than none at all: 268 M elements, 537 MB read and 537 MB written, in 229 and 212 us (seven rounds: 224).
 __device__ inline uint4 philox(unsigned long long block, unsigned long long offset, unsigned long long seed)
 {
     unsigned a = (unsigned)block, b = (unsigned)(block >> 32), c = (unsigned)offset, d = (unsigned)(offset >> 32);
@@ -748,8 +748,8 @@ __device__ inline void tile_of(const TilesD &N, int block, int &tp, int &tq)
 }
 
 // D = P Q^T and what becomes of it.  BP x BQ results a block, WP x WQ waves; blockIdx.y: the part of the range of t, `t_part` long.
-// 16 bits: bound by latency (1536 x 1024 x 768 fp16 12 us) and, at odd addresses, by the loads (8192 x 4096 x 4096 at odd elements 400 us).  fp32: by the arithmetic beside the matrix
-// instructions, the parts (5.7 instructions an element) and the epilogue: 200003 x 256 x 256 with silu 174 us, 151 TFLOP/s, 8192 x 4096 x 4096 1303 us, 211 TFLOP/s (the library's
+// 16 bits: bound by latency (1536 x 1024 x 768 fp16 12.7 us) and, at odd addresses, by the loads (8192 x 4096 x 4096 at odd elements 400 us).  fp32: by the arithmetic beside the matrix
+// instructions, the parts (5.7 instructions an element) and the epilogue: 200003 x 256 x 256 with silu 177 us, 148 TFLOP/s, 8192 x 4096 x 4096 1293 us, 213 TFLOP/s (the library's
 // 1822).  Two blocks of eight waves a compute unit, whose phases mix: three of four took 188, two of four (with 7.6 instructions an element) 247.
 template <int TYPE, bool PCOL, bool QCOL, int BP, int BQ, int WP, int WQ, int BUFFERS, int AHEAD>
 __global__ __launch_bounds__(64 * WP * WQ, TYPE == NET_F32 && BP * BQ == 128 * 128 && !QCOL ? 3 : 1) void k_product(MatD P, MatD Q, long long np, long long nq, long long nt, long long t_part, TilesD tiles, EpiD E)
@@ -1253,9 +1253,10 @@ template <int TYPE, class Q, class N> __device__ inline void dz_eight(float (&x)
 //   dweight: WP x WQ waves share the B x B results, t = rows.  dX: 32 inputs a wave, t = outputs; where there are twice the waves, two share those.
 // RESTS (16 bits): dZ goes in as two parts, itself rounded and what that leaves, for layers whose dZ has too few values to average its rounding out.  A rest of 0 would make
 // a NaN of another operand's infinity: dX has sums of its own for the rests, and leaves them out where the others' are no finite numbers; dweight (whose second sums would
-// take 437 registers, one block a compute unit) makes such results again.  Forward and backward of 1024 x 64 x 64 bf16, gelu, 21.5 us, by one part 17.1; of
-// 65536 x 128 x 128 87, by one 67: there one part is taken.
-// 65536 x 128 x 128 fp32 56 us (134 MB, 2.3 TB/s): four barriers every 32 rows, between which loads, parts and products follow one another.  For 256 x 256 in 16 bits, one
+// take 437 registers, one block a compute unit) makes such results again.  Forward and backward of 1024 x 64 x 64 bf16, gelu, 20.8 us, by one part 16.6; of
+// 65536 x 128 x 128, silu, 56, by one 50: there one part is taken.
+// 65536 x 128 x 128 fp32 39 us (134 MB, 3.4 TB/s; matrix pipe busy 22 % of the time, vector instructions 26), bf16 31 (67 MB, 2.2 TB/s; 4 and 31): four barriers every 32
+// rows, between which loads, parts and products follow one another.  For 256 x 256 in 16 bits, one
 // block a compute unit, that took 624 us against 556 of the other kernels, so B is 128.
 template <int TYPE, int B, int WAVES, bool RESTS>
 __global__ __launch_bounds__(64 * WAVES, 2) void k_narrow(DzD D, MatD X, MatD W, void *dx, long long lddx, float *__restrict__ dw, long long ldw, float *__restrict__ sums)
@@ -1320,7 +1321,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_narrow(DzD D, MatD X, MatD W,
     long long q0 = (long long)blockIdx.x * R;
     Power power = {1.0f, 1.0f};
     if constexpr (TYPE == NET_F16)
-        if (D.act != ACT_NONE || D.drop.mode == 1) {       // a block's own (see power_of): its rows of G are read twice, eight groups of 32 at most
+        if (D.act != ACT_NONE || D.drop.mode == 1) {       // a block's own (see power_of): its rows of G are read twice
             __shared__ unsigned s_most[WAVES];
             Largest most;
             for (long long q = q0 + r0; q < rows + r0; q += stride)
@@ -1569,8 +1570,8 @@ template <int TYPE, int V, bool WHOLE> __device__ inline Packed<TYPE, V> load_ro
     else return load_some<TYPE, V>(at, n);
 }
 
-// Y = R + drop(X).  Two rows' loads before the first one's store, which might be to the same memory.  134 M bf16 with and without residual 136 us each (5.9 and 3.9 TB/s): Philox's
-// multiplications keep the arithmetic busy for 41 issue slots an element.
+// Y = R + drop(X).  Two rows' loads before the first one's store, which might be to the same memory.  Bound by memory: 134 M bf16 without residual 108 us (5.0 TB/s; with p = 0, a copy,
+// 101), with residual 166 (4.9 TB/s; p = 0: 164).  Beside that vector instructions, most of them Philox's, keep the SIMDs busy for 68 % of the time, with residual 43 %.
 template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dropout(RowsD N, MatD X, MatD R, void *y, long long ldy, DropD D)
 {
     typedef typename ElemOf<TYPE>::type T;

@@ -10,7 +10,7 @@ from test_gpu_net import SEED, check, make, net, run, whole  # noqa: F401
 pytestmark = pytest.mark.gpu
 F64 = torch.float64
 SIZES = [((20001, 128, 24), "f32"), ((20001, 97, 128), "f32"), ((24640, 1, 128), "f32"), ((60001, 128, 40), "bf16"), ((60001, 128, 40), "f16"), ((50000, 33, 128), "bf16"),
-         ((131072, 10, 9), "f16"), ((130999, 8, 1), "bf16")]
+         ((131072, 10, 9), "f16"), ((130999, 8, 1), "bf16"), ((300001, 128, 9), "bf16"), ((262149, 40, 24), "f16")]
 
 
 @pytest.mark.parametrize("size, dtype", SIZES, ids=str)
