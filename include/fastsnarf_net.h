@@ -18,9 +18,10 @@
  * No mask is stored: the backward pass makes it anew.  Philox4x32-10: Salmon et al., "Parallel random numbers: as easy as 1, 2, 3" (2011).
  *
  * Arithmetic: sums in fp32; results rounded once, to nearest even.
- *  - Where the type has 16 bits, dZ is rounded to it for the products that read it (not for dbias, which is summed before that).  In layers of at most 128
- *    inputs, 128 outputs and 131072 values of dZ, where few values would not average that out, dZ goes in as two parts of 16 bits.  fp16's range does not matter
- *    for it: dZ is scaled by a power of two on the way, and its rounding steps are at most 2^-38 of the largest finite |G| / (1 - p).
+ *  - Where the type has 16 bits, dZ is rounded to it for the products that read it (not for dbias, which is summed before that).  Where that would not average
+ *    out, dZ goes in as two parts of 16 bits: in products of at most 4096 results or from at most 4096 values of dZ, and in layers of at most 128 inputs, 128
+ *    outputs and 131072 values of dZ.  fp16's range does not matter for it: dZ is scaled by a power of two on the way, and its rounding steps are at most 2^-38
+ *    of the largest finite |G| / (1 - p).
  *  - Z is kept for the backward pass in the bias's type, or in fp32 by FS_Z_FULL: an fp32 bias gets a gradient that is good to fp32.  fp16 keeps finite Z
  *    within +-65504 and positive Z positive, which changes no slope but that of softplus with beta below 2^-11 (take FS_Z_FULL for that).
  *  - fp32 operands of the products go in as three bf16 parts each (24 bits together), of whose nine products the six largest are added: what is left out is

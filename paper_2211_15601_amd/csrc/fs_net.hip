@@ -146,11 +146,13 @@ bool is_few(int64_t rows, int64_t outputs, int64_t inputs, int cus)
 // the large tile 420; without an epilogue 228 and 169).
 constexpr long long SHORT_T = 512;
 
-// How a product is launched: tiles of `tile` squared, `parts` parts of the range of t, each t_part long.
+// How a product is launched: tiles of `tile` squared, `parts` parts of the range of t, each t_part long; twice, if `rests`, with Q and with what its rounding left.
 struct Plan {
     int tile, parts;
+    bool rests;
     long long t_part, tiles_p, tiles_q, ldp;
-    int64_t part_bytes() const { return parts > 1 ? (int64_t)parts * part_stride * 4 : 0; }
+    bool in_parts() const { return parts > 1 || rests; }
+    int64_t part_bytes() const { return in_parts() ? (int64_t)parts * (rests ? 2 : 1) * part_stride * 4 : 0; }
     long long part_stride;
 };
 
@@ -216,12 +218,12 @@ void launch_product(const Plan &p, const MatD &P, const MatD &Q, int64_t np, int
     else k_product<TYPE, PCOL, QCOL, 128, 128, 2, 4, F32 ? 1 : 2, 1><<<grid, 512, 0, stream>>>(P, Q, np, nq, nt, p.t_part, tiles, E);
 }
 
-template <int TYPE>
+template <int TYPE, bool RESTS>
 void launch_parts(const Plan &p, const float *part, int64_t np, int64_t nq, const EpiD &E, hipStream_t stream)
 {
     const long long all = (np + 255) / 256 * nq, blocks = p.parts >= 8 ? all : (all + 3) / 4;
-    if (p.parts >= 8) k_parts<TYPE, true><<<(unsigned)std::min<long long>(blocks, 1 << 16), 256, 0, stream>>>(part, p.part_stride, p.ldp, p.parts, np, nq, E);
-    else k_parts<TYPE, false><<<(unsigned)std::min<long long>(blocks, 1 << 16), 256, 0, stream>>>(part, p.part_stride, p.ldp, p.parts, np, nq, E);
+    if (p.parts >= 8) k_parts<TYPE, true, RESTS><<<(unsigned)std::min<long long>(blocks, 1 << 16), 256, 0, stream>>>(part, p.part_stride, p.ldp, p.parts, np, nq, E);
+    else k_parts<TYPE, false, RESTS><<<(unsigned)std::min<long long>(blocks, 1 << 16), 256, 0, stream>>>(part, p.part_stride, p.ldp, p.parts, np, nq, E);
 }
 
 // Waves a block: enough that every compute unit has some 16, and each a group of steps or more.
@@ -240,29 +242,40 @@ template <int TYPE> void launch_few(const MatD &W, const MatD &X, int64_t np, in
 
 enum { NT, NN, TN };                   // forward, dX, dweight
 
-// One product with its epilogue; `work`: part_bytes() of the plan.
-void product(int type, int kind, const Plan &p, const MatD &P, const MatD &Q, int64_t np, int64_t nq, int64_t nt, const EpiD &E, void *work, hipStream_t stream)
+// One product with its epilogue; `work`: part_bytes() of the plan; rest: of Q, where the plan has rests.
+void product(int type, int kind, const Plan &p, const MatD &P, const MatD &Q, const MatD &rest, int64_t np, int64_t nq, int64_t nt, const EpiD &E, void *work, hipStream_t stream)
 {
     if (np == 0 || nq == 0) return;
     EpiD part = E;
-    if (p.parts > 1) {
+    if (p.in_parts()) {
         part = {};
         part.mode = EPI_PART;
         part.out = work;
         part.ldo = p.ldp;
         part.part_stride = p.part_stride;
     }
-#define FS_NET_KIND(TYPE)                                                                              \
+#define FS_NET_PRODUCT(TYPE, Q)                                                                        \
     do {                                                                                               \
         if (kind == NT) launch_product<TYPE, false, false>(p, P, Q, np, nq, nt, part, stream);         \
         else if (kind == NN) launch_product<TYPE, true, false>(p, P, Q, np, nq, nt, part, stream);     \
         else launch_product<TYPE, true, true>(p, P, Q, np, nq, nt, part, stream);                      \
-        if (p.parts > 1) launch_parts<TYPE>(p, static_cast<const float *>(work), np, nq, E, stream);   \
+    } while (0)
+#define FS_NET_KIND(TYPE)                                                                              \
+    do {                                                                                               \
+        FS_NET_PRODUCT(TYPE, Q);                                                                       \
+        if (p.rests) {                                                                                 \
+            part.out = static_cast<float *>(work) + p.parts * p.part_stride;                           \
+            FS_NET_PRODUCT(TYPE, rest);                                                                \
+            launch_parts<TYPE, TYPE != NET_F32>(p, static_cast<const float *>(work), np, nq, E, stream); \
+        } else if (p.parts > 1) {                                                                      \
+            launch_parts<TYPE, false>(p, static_cast<const float *>(work), np, nq, E, stream);         \
+        }                                                                                              \
     } while (0)
     if (type == FS_FLOAT_FULL) FS_NET_KIND(NET_F32);
     else if (type == FS_FLOAT_BRAIN) FS_NET_KIND(NET_BF16);
     else FS_NET_KIND(NET_F16);
 #undef FS_NET_KIND
+#undef FS_NET_PRODUCT
 }
 
 // ---------------------------------------------------------------------------------------------------------------- elementwise
@@ -285,11 +298,11 @@ RowsPlan plan_rows(int type, int64_t rows, int64_t cols, int64_t last, long long
 
 constexpr long long ROW_BLOCKS = 2048, DZ_BLOCKS = 1024;
 
-// most, factor: of fp16, where dz is wanted (see k_dz)
-template <int TYPE> void launch_dz(const RowsPlan &p, const MatD &G, const MatD &Z, const fs_linear &l, void *dz, float *sums, unsigned *most, float *factor, hipStream_t stream)
+// most, factor: of fp16, where dz is wanted; rest: where dz is and a product takes it (see k_dz)
+template <int TYPE> void launch_dz(const RowsPlan &p, const MatD &G, const MatD &Z, const fs_linear &l, void *dz, void *rest, float *sums, unsigned *most, float *factor, hipStream_t stream)
 {
     if (most) k_largest<<<LARGEST_BLOCKS, 256, 0, stream>>>(p.n, G, most);
-    k_dz<TYPE, TYPE == NET_F32 ? 4 : 8><<<dim3(p.gx, p.gy), 256, 0, stream>>>(p.n, G, Z, z_full(l), act_kind(l), l.beta, drop_of(l.drop), dz, l.outputs, sums, most, factor);
+    k_dz<TYPE, TYPE == NET_F32 ? 4 : 8><<<dim3(p.gx, p.gy), 256, 0, stream>>>(p.n, G, Z, z_full(l), act_kind(l), l.beta, drop_of(l.drop), dz, l.outputs, sums, most, factor, rest);
 }
 
 int64_t up(int64_t bytes) { return (bytes + 255) / 256 * 256; }
@@ -300,9 +313,18 @@ int64_t up(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 // Kernels, us, this and the others: fp32 1024 x 64 x 64 12.1 and 20.7, 65536 x 128 x 128 48 and 73, 524288 x 32 x 128 260 and 390; bf16 14.7 and 16.7, 40 and 47, 185 and 201,
 // 262144 x 128 x 128 106 and 123.
 constexpr int NARROW = 128;
-// Values of dZ up to which those of 16 bits keep what its rounding leaves.  The results' own rounding and dZ's make 1.41 times the error of the first alone; of few values
-// by chance more (2 x 27 x 2 fp16, silu: 3.2 times), and of one output, whose rows may cancel (87983 x 1 x 1 fp16: 21).
-constexpr int64_t NARROW_RESTS = 1 << 17;
+// Products of 16 bits that take dZ in two parts, rounded and what that leaves.  The results' own rounding and dZ's make 1.41 times the error of the first alone, on average: of up
+// to FEW results, or from up to FEW values of dZ, by chance more (64 results, dweight of 380289 x 8 x 8 bf16: 1.6 times; 2 x 27 x 2 fp16, silu: 3.2; 4 results of 3655
+// values each, some of which cancel: 4.2).  With 4096 the squares' sums of normal results scatter by 2 %: 1.5 times is some six deviations off.
+// Narrow layers take the parts up to NARROW_RESTS values of dZ, where that takes 4 us of 21 (1024 x 64 x 64 bf16).
+// Others launch a product twice: backward of 5000 x 10 x 200 bf16 44 us, once 31, of 200000 x 300 x 8 185, once 123.
+constexpr int64_t FEW = 4096, NARROW_RESTS = 1 << 17;
+bool few_products(int64_t values, int64_t results) { return std::min(values, results) <= FEW; }
+bool narrow_rests(const fs_linear &l)
+{
+    const int64_t values = l.rows * l.outputs;
+    return l.type != FS_FLOAT_FULL && (values <= NARROW_RESTS || few_products(values, l.rows * l.inputs) || few_products(values, l.outputs * l.inputs));
+}
 
 struct Backward {
     Plan dx, dw;
@@ -310,7 +332,7 @@ struct Backward {
     bool has_dz;
     bool narrow;
     int blocks;
-    int64_t sums, part, factor, most, end;
+    int64_t rest, sums, part, factor, most, end;
 };
 
 int64_t narrow_ld(const fs_linear &l) { return (l.inputs + 3) / 4 * 4; }
@@ -322,7 +344,7 @@ void launch_narrow(const fs_linear &l, const Backward &b, const DzD &D, const Ma
     float *part = dw ? reinterpret_cast<float *>(work) : nullptr, *sums = dbias ? reinterpret_cast<float *>(work + narrow_sums(l, b)) : nullptr;
     const int64_t ld = narrow_ld(l);
     constexpr int WAVES = TYPE == NET_F32 ? 8 : 4;
-    if (TYPE == NET_F32 || l.rows * l.outputs > NARROW_RESTS) k_narrow<TYPE, NARROW, WAVES, false><<<b.blocks, 64 * WAVES, 0, stream>>>(D, X, W, dx, lddx, part, ld, sums);
+    if (!narrow_rests(l)) k_narrow<TYPE, NARROW, WAVES, false><<<b.blocks, 64 * WAVES, 0, stream>>>(D, X, W, dx, lddx, part, ld, sums);
     else k_narrow<TYPE, NARROW, WAVES, TYPE != NET_F32><<<b.blocks, 64 * WAVES, 0, stream>>>(D, X, W, dx, lddx, part, ld, sums);
     const int blocks_dw = dw ? (int)((l.outputs * ld + 255) / 256) : 0, blocks_db = dbias ? (int)((l.outputs + 63) / 64) : 0;
     if (blocks_dw + blocks_db > 0) k_narrow_end<TYPE><<<blocks_dw + blocks_db, 1024, 0, stream>>>(part, ld, b.blocks, l.inputs, l.outputs, dw, lddw, sums, dbias, l.bias_type == FS_FLOAT_FULL, blocks_dw);
@@ -344,7 +366,12 @@ Backward plan_backward(const fs_linear &l, int cus)
         b.end = narrow_sums(l, b) + up((int64_t)b.blocks * l.outputs * 4);
         return b;
     }
-    b.sums = b.has_dz ? up(l.rows * l.outputs * size_of(l.type)) : 0;
+    if (b.has_dz && l.type != FS_FLOAT_FULL) {
+        b.dx.rests = few_products(l.rows * l.outputs, l.rows * l.inputs);
+        b.dw.rests = few_products(l.rows * l.outputs, l.outputs * l.inputs);
+    }
+    b.rest = b.has_dz ? up(l.rows * l.outputs * size_of(l.type)) : 0;
+    b.sums = b.dx.rests || b.dw.rests ? 2 * b.rest : b.rest;
     b.part = b.sums + up((int64_t)b.dz.gy * l.outputs * 4);
     b.factor = b.part + up(std::max(b.dx.part_bytes(), b.dw.part_bytes()));
     const bool scaled = b.has_dz && l.type == FS_FLOAT_HALF;
@@ -432,7 +459,7 @@ fs_status fs_linear_forward(const fs_linear *layer, const void *d_x, int64_t ldx
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const MatD W = {d_w, ldw, n, k}, X = {d_x, ldx, m, k};
     if (m == 0 || n == 0) return FS_OK;
-    if (!is_few(m, n, k, cus)) product(l.type, NT, p, W, X, n, m, k, E, d_work, stream);
+    if (!is_few(m, n, k, cus)) product(l.type, NT, p, W, X, {}, n, m, k, E, d_work, stream);
     else if (l.type == FS_FLOAT_FULL) launch_few<NET_F32>(W, X, n, m, k, E, cus, stream);
     else if (l.type == FS_FLOAT_BRAIN) launch_few<NET_BF16>(W, X, n, m, k, E, cus, stream);
     else launch_few<NET_F16>(W, X, n, m, k, E, cus, stream);
@@ -476,11 +503,12 @@ fs_status fs_linear_backward(const fs_linear *layer, const void *d_g, int64_t ld
     }
     const MatD dZ = b.has_dz ? MatD{work, n, m, n} : G;
     void *dz = b.has_dz && (d_dx || d_dw) ? work : nullptr;
+    void *rest = dz && ((d_dx && b.dx.rests) || (d_dw && b.dw.rests)) ? work + b.rest : nullptr;
     float *factor = dz && n > 0 && l.type == FS_FLOAT_HALF ? reinterpret_cast<float *>(work + b.factor) : nullptr;
     if ((dz || sums) && n > 0) {
-        if (l.type == FS_FLOAT_FULL) launch_dz<NET_F32>(b.dz, G, Z, l, dz, sums, nullptr, nullptr, stream);
-        else if (l.type == FS_FLOAT_BRAIN) launch_dz<NET_BF16>(b.dz, G, Z, l, dz, sums, nullptr, nullptr, stream);
-        else launch_dz<NET_F16>(b.dz, G, Z, l, dz, sums, factor ? reinterpret_cast<unsigned *>(work + b.most) : nullptr, factor, stream);
+        if (l.type == FS_FLOAT_FULL) launch_dz<NET_F32>(b.dz, G, Z, l, dz, nullptr, sums, nullptr, nullptr, stream);
+        else if (l.type == FS_FLOAT_BRAIN) launch_dz<NET_BF16>(b.dz, G, Z, l, dz, rest, sums, nullptr, nullptr, stream);
+        else launch_dz<NET_F16>(b.dz, G, Z, l, dz, rest, sums, factor ? reinterpret_cast<unsigned *>(work + b.most) : nullptr, factor, stream);
         if (sums) {
             const unsigned blocks = (unsigned)((n + 63) / 64);
             if (l.bias_type == FS_FLOAT_FULL) k_dbias<NET_F32><<<blocks, 1024, 0, stream>>>(sums, (int)b.dz.gy, n, d_dbias);
@@ -494,12 +522,12 @@ fs_status fs_linear_backward(const fs_linear *layer, const void *d_g, int64_t ld
     if (d_dx) {
         E.out = d_dx;
         E.ldo = lddx;
-        product(l.type, NN, b.dx, {d_w, ldw, n, k}, dZ, k, m, n, E, work + b.part, stream);
+        product(l.type, NN, b.dx, {d_w, ldw, n, k}, dZ, {rest, n, m, n}, k, m, n, E, work + b.part, stream);
     }
     if (d_dw) {
         E.out = d_dw;
         E.ldo = lddw;
-        product(l.type, TN, b.dw, {d_x, ldx, m, k}, dZ, k, n, m, E, work + b.part, stream);
+        product(l.type, TN, b.dw, {d_x, ldx, m, k}, dZ, {rest, n, m, n}, k, n, m, E, work + b.part, stream);
     }
     return launch_status(what);
 }

@@ -1036,10 +1036,12 @@ __global__ __launch_bounds__(512) void k_product_big(MatD P, MatD Q, long long n
 }
 
 // The parts' sums and what becomes of them, 256 neighbours p of one row q at a time.  SPLIT: a block's four waves add every fourth part each and the first of
-// them finishes; else each wave has a strip of its own.
-template <int TYPE, bool SPLIT> __global__ __launch_bounds__(256) void k_parts(const float *__restrict__ part, long long part_stride, long long ldp, int parts, long long np, long long nq, EpiD E)
+// them finishes; else each wave has a strip of its own.  RESTS: `parts` parts more follow, of what rounding left of an operand.  They are left out where the others' sum
+// is no finite number: a rest of 0 makes NaN of an infinity.
+template <int TYPE, bool SPLIT, bool RESTS> __global__ __launch_bounds__(256) void k_parts(const float *__restrict__ part, long long part_stride, long long ldp, int parts, long long np, long long nq, EpiD E)
 {
-    __shared__ float s_sum[SPLIT ? 3 : 1][256];
+    constexpr int SUMS = RESTS ? 2 : 1;
+    __shared__ float s_sum[SPLIT ? 3 * SUMS : 1][256];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = SPLIT ? wave : 0, step = SPLIT ? 4 : 1;
     const long long strips = (np + 255) / 256, all = strips * nq, each = SPLIT ? 1 : 4;
     const Seed seed = seed_of(E.drop);
@@ -1048,21 +1050,34 @@ template <int TYPE, bool SPLIT> __global__ __launch_bounds__(256) void k_parts(c
         const long long q = b / strips, p = b % strips * 256 + 4 * lane;
         const int n = np - p < 4 ? (int)(np - p) : 4;
         const Place<TYPE> to(E, q, p, 0);
-        f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        f32x4 sums[SUMS];
         Packed<TYPE, 4> r = {};
+#pragma unroll
+        for (int k = 0; k < SUMS; ++k) sums[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         if (n > 0) {
             if (!SPLIT || wave == 0) r = residual4<TYPE>(E, to, 0, n);
-            const float *at = part + q * ldp + p;              // ldp is a multiple of 4
+#pragma unroll
+            for (int k = 0; k < SUMS; ++k) {
+                const float *at = part + k * parts * part_stride + q * ldp + p;            // ldp is a multiple of 4
 #pragma unroll 8
-            for (int i = first; i < parts; i += step) sum += *reinterpret_cast<const f32x4 *>(at + i * part_stride);
+                for (int i = first; i < parts; i += step) sums[k] += *reinterpret_cast<const f32x4 *>(at + i * part_stride);
+            }
         }
         if constexpr (SPLIT) {
-            if (wave) *reinterpret_cast<f32x4 *>(s_sum[wave - 1] + 4 * lane) = sum;
+            if (wave)
+#pragma unroll
+                for (int k = 0; k < SUMS; ++k) *reinterpret_cast<f32x4 *>(s_sum[3 * k + wave - 1] + 4 * lane) = sums[k];
             __syncthreads();
         }
         if (first == 0 && n > 0) {
             if constexpr (SPLIT)
-                for (int w = 0; w < 3; ++w) sum += *reinterpret_cast<const f32x4 *>(s_sum[w] + 4 * lane);
+#pragma unroll
+                for (int k = 0; k < SUMS; ++k)
+                    for (int w = 0; w < 3; ++w) sums[k] += *reinterpret_cast<const f32x4 *>(s_sum[3 * k + w] + 4 * lane);
+            f32x4 sum = sums[0];
+            if constexpr (RESTS)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[i] = fabsf(sum[i]) < INFINITY ? sum[i] + sums[1][i] : sum[i];
             float v[4] = {sum[0], sum[1], sum[2], sum[3]}, bias[4];
             if (E.mode == EPI_LAYER) {
                 load_bias<TYPE>(bias, E, p, n);
@@ -1635,8 +1650,9 @@ __global__ __launch_bounds__(256) void k_largest(RowsD N, MatD G, unsigned *__re
 
 // dZ = drop(G act'(Z)), and the sums of its columns over a block's rows (either may be NULL).  134 M bf16 with Z in fp32 239 us (1.07 GB, 4.5 TB/s), beside Philox's arithmetic.
 // fp16: dZ is written times a power of two, which goes by k_largest's `most` (where that is not NULL) and whose inverse goes to *factor.
+// rest (16 bits, or NULL): what the rounding leaves of dZ, none where it is no finite number.
 template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dz(RowsD N, MatD G, MatD Z, int z_f32, int act, float beta, DropD D, void *dz, long long lddz, float *__restrict__ sums,
-                                                                       const unsigned *__restrict__ most, float *__restrict__ factor)
+                                                                       const unsigned *__restrict__ most, float *__restrict__ factor, void *rest)
 {
     typedef typename ElemOf<TYPE>::type T;
     __shared__ float s_sum[256 * V];
@@ -1692,6 +1708,14 @@ template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dz(RowsD N, 
 #pragma unroll
                                 for (int i = 0; i < V; ++i) v[i] *= to;
                             if (dz) store_some<TYPE, V>(static_cast<T *>(dz) + (q + u * step) * lddz + c, v, WHOLE ? V : n);
+                            if (TYPE != NET_F32 && rest) {
+#pragma unroll
+                                for (int i = 0; i < V; ++i) {
+                                    const float high = widen<TYPE>(narrow<TYPE>(v[i]));
+                                    v[i] = fabsf(high) < INFINITY ? v[i] - high : 0.0f;
+                                }
+                                store_some<TYPE, V>(static_cast<T *>(rest) + (q + u * step) * lddz + c, v, WHOLE ? V : n);
+                            }
                         }
                 }
             };
