@@ -17,7 +17,7 @@
  *
  * No mask is stored: the backward pass makes it anew.  Philox4x32-10: Salmon et al., "Parallel random numbers: as easy as 1, 2, 3" (2011).
  *
- * Arithmetic: sums in fp32; results rounded once, to nearest even.
+ * Arithmetic: sums in fp32, dbias over the rows in 64 bits (columns may cancel); results rounded once, to nearest even.
  *  - Where the type has 16 bits, dZ is rounded to it for the products that read it (not for dbias, which is summed before that).  Where that would not average
  *    out, dZ goes in as two parts of 16 bits: in products of at most 4096 results or from at most 4096 values of dZ, and in layers of at most 128 inputs, 128
  *    outputs and 131072 values of dZ.  fp16's range does not matter for it: dZ is scaled by a power of two on the way, and its rounding steps are at most 2^-38

@@ -299,7 +299,7 @@ RowsPlan plan_rows(int type, int64_t rows, int64_t cols, int64_t last, long long
 constexpr long long ROW_BLOCKS = 2048, DZ_BLOCKS = 1024;
 
 // most, factor: of fp16, where dz is wanted; rest: where dz is and a product takes it (see k_dz)
-template <int TYPE> void launch_dz(const RowsPlan &p, const MatD &G, const MatD &Z, const fs_linear &l, void *dz, void *rest, float *sums, unsigned *most, float *factor, hipStream_t stream)
+template <int TYPE> void launch_dz(const RowsPlan &p, const MatD &G, const MatD &Z, const fs_linear &l, void *dz, void *rest, double *sums, unsigned *most, float *factor, hipStream_t stream)
 {
     if (most) k_largest<<<LARGEST_BLOCKS, 256, 0, stream>>>(p.n, G, most);
     k_dz<TYPE, TYPE == NET_F32 ? 4 : 8><<<dim3(p.gx, p.gy), 256, 0, stream>>>(p.n, G, Z, z_full(l), act_kind(l), l.beta, drop_of(l.drop), dz, l.outputs, sums, most, factor, rest);
@@ -341,7 +341,8 @@ int64_t narrow_sums(const fs_linear &l, const Backward &b) { return up((int64_t)
 template <int TYPE>
 void launch_narrow(const fs_linear &l, const Backward &b, const DzD &D, const MatD &X, const MatD &W, void *dx, int64_t lddx, void *dw, int64_t lddw, void *dbias, char *work, hipStream_t stream)
 {
-    float *part = dw ? reinterpret_cast<float *>(work) : nullptr, *sums = dbias ? reinterpret_cast<float *>(work + narrow_sums(l, b)) : nullptr;
+    float *part = dw ? reinterpret_cast<float *>(work) : nullptr;
+    double *sums = dbias ? reinterpret_cast<double *>(work + narrow_sums(l, b)) : nullptr;
     const int64_t ld = narrow_ld(l);
     constexpr int WAVES = TYPE == NET_F32 ? 8 : 4;
     if (!narrow_rests(l)) k_narrow<TYPE, NARROW, WAVES, false><<<b.blocks, 64 * WAVES, 0, stream>>>(D, X, W, dx, lddx, part, ld, sums);
@@ -363,7 +364,7 @@ Backward plan_backward(const fs_linear &l, int cus)
     const long long per_cu = l.type != FS_FLOAT_FULL ? 2 : 1;
     b.blocks = (int)std::max<long long>(1, std::min<long long>(per_cu * cus, (l.rows + 31) / 32));
     if (b.narrow) {                    // no dZ, and no products' parts
-        b.end = narrow_sums(l, b) + up((int64_t)b.blocks * l.outputs * 4);
+        b.end = narrow_sums(l, b) + up((int64_t)b.blocks * l.outputs * 8);
         return b;
     }
     if (b.has_dz && l.type != FS_FLOAT_FULL) {
@@ -372,7 +373,7 @@ Backward plan_backward(const fs_linear &l, int cus)
     }
     b.rest = b.has_dz ? up(l.rows * l.outputs * size_of(l.type)) : 0;
     b.sums = b.dx.rests || b.dw.rests ? 2 * b.rest : b.rest;
-    b.part = b.sums + up((int64_t)b.dz.gy * l.outputs * 4);
+    b.part = b.sums + up((int64_t)b.dz.gy * l.outputs * 8);
     b.factor = b.part + up(std::max(b.dx.part_bytes(), b.dw.part_bytes()));
     const bool scaled = b.has_dz && l.type == FS_FLOAT_HALF;
     b.most = b.factor + (scaled ? 256 : 0);
@@ -491,7 +492,7 @@ fs_status fs_linear_backward(const fs_linear *layer, const void *d_g, int64_t ld
 
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     char *work = static_cast<char *>(d_work);
-    float *sums = d_dbias ? reinterpret_cast<float *>(work + b.sums) : nullptr;
+    double *sums = d_dbias ? reinterpret_cast<double *>(work + b.sums) : nullptr;
     const MatD G = {d_g, ldg, m, n}, Z = {d_z, ldz, m, n};
     if (b.narrow && (d_dx || d_dw || d_dbias)) {
         const DzD D = {G, Z, z_full(l), act_kind(l), l.beta, drop_of(l.drop)};

@@ -1274,7 +1274,7 @@ template <int TYPE, class Q, class N> __device__ inline void dz_eight(float (&x)
 // rows, between which loads, parts and products follow one another.  For 256 x 256 in 16 bits, one
 // block a compute unit, that took 624 us against 556 of the other kernels, so B is 128.
 template <int TYPE, int B, int WAVES, bool RESTS>
-__global__ __launch_bounds__(64 * WAVES, 2) void k_narrow(DzD D, MatD X, MatD W, void *dx, long long lddx, float *__restrict__ dw, long long ldw, float *__restrict__ sums)
+__global__ __launch_bounds__(64 * WAVES, 2) void k_narrow(DzD D, MatD X, MatD W, void *dx, long long lddx, float *__restrict__ dw, long long ldw, double *__restrict__ sums)
 {
     typedef typename ElemOf<TYPE>::type T;
     constexpr int THREADS = 64 * WAVES, R = 32, PL = TYPE == NET_F32 ? 3 : 1, PZ = TYPE == NET_F32 ? 3 : RESTS ? 2 : 1, WP = WAVES / 2, WQ = 2, MT = B / WP / 32, NT = B / WQ / 32;
@@ -1297,9 +1297,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_narrow(DzD D, MatD X, MatD W,
         for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.0f;
-    float db[8];
+    double db[8];                      // columns may cancel
 #pragma unroll
-    for (int i = 0; i < 8; ++i) db[i] = 0.0f;
+    for (int i = 0; i < 8; ++i) db[i] = 0.0;
 
     Packed<TYPE, 8> g[UNITS];
     unsigned z[UNITS][8];
@@ -1515,12 +1515,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_narrow(DzD D, MatD X, MatD W,
     if (!sums) return;
     // dbias' part: a thread's columns are those of every PER_ROW-th other
     __syncthreads();
-    float *s_db = reinterpret_cast<float *>(s_in);
+    double *s_db = reinterpret_cast<double *>(s_in);
+    static_assert(THREADS * 8 * 8 <= (PZ + PL) * R * B * 2, "dbias goes through the inputs' place");
 #pragma unroll
     for (int k = 0; k < 8; ++k) s_db[tid / PER_ROW * B + c8 + k] = db[k];
     __syncthreads();
     for (int n = tid; n < outputs; n += THREADS) {
-        float all = 0.0f;
+        double all = 0.0;
         for (int r = 0; r < THREADS / PER_ROW; ++r) all += s_db[r * B + n];
         sums[blockIdx.x * outputs + n] = all;
     }
@@ -1528,9 +1529,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_narrow(DzD D, MatD X, MatD W,
 
 // The parts of k_narrow added up, dweight (of 256 neighbours by a block) and behind it dbias (of 64).
 template <int TYPE> __global__ __launch_bounds__(1024) void k_narrow_end(const float *__restrict__ dw, long long ldp, int parts, long long inputs, long long outputs, void *out, long long ldo,
-                                                                         const float *__restrict__ sums, void *dbias, int bias_f32, int blocks_dw)
+                                                                         const double *__restrict__ sums, void *dbias, int bias_f32, int blocks_dw)
 {
     __shared__ __attribute__((aligned(16))) float s_sum[16][256];
+    double (*s_db)[64] = reinterpret_cast<double (*)[64]>(s_sum);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if ((int)blockIdx.x < blocks_dw) {
         // rows of ldp floats, a multiple of 4, one after another
@@ -1549,16 +1551,16 @@ template <int TYPE> __global__ __launch_bounds__(1024) void k_narrow_end(const f
         return;
     }
     const long long c = (blockIdx.x - blocks_dw) * 64ll + lane;
-    float all = 0.0f;
+    double all = 0.0;
     if (c < outputs)
 #pragma unroll 16
         for (int b = wave; b < parts; b += 16) all += sums[b * outputs + c];
-    s_sum[wave][lane] = all;
+    s_db[wave][lane] = all;
     __syncthreads();
     if (wave || c >= outputs) return;
-    for (int w = 1; w < 16; ++w) all += s_sum[w][lane];
-    if (bias_f32) static_cast<float *>(dbias)[c] = all;
-    else static_cast<typename ElemOf<TYPE>::type *>(dbias)[c] = narrow<TYPE>(all);
+    for (int w = 1; w < 16; ++w) all += s_db[w][lane];
+    if (bias_f32) static_cast<float *>(dbias)[c] = (float)all;
+    else static_cast<typename ElemOf<TYPE>::type *>(dbias)[c] = narrow<TYPE>((float)all);
 }
 
 // ---------------------------------------------------------------------------------------------------------------- elementwise
@@ -1651,11 +1653,11 @@ __global__ __launch_bounds__(256) void k_largest(RowsD N, MatD G, unsigned *__re
 // dZ = drop(G act'(Z)), and the sums of its columns over a block's rows (either may be NULL).  134 M bf16 with Z in fp32 239 us (1.07 GB, 4.5 TB/s), beside Philox's arithmetic.
 // fp16: dZ is written times a power of two, which goes by k_largest's `most` (where that is not NULL) and whose inverse goes to *factor.
 // rest (16 bits, or NULL): what the rounding leaves of dZ, none where it is no finite number.
-template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dz(RowsD N, MatD G, MatD Z, int z_f32, int act, float beta, DropD D, void *dz, long long lddz, float *__restrict__ sums,
+template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dz(RowsD N, MatD G, MatD Z, int z_f32, int act, float beta, DropD D, void *dz, long long lddz, double *__restrict__ sums,
                                                                        const unsigned *__restrict__ most, float *__restrict__ factor, void *rest)
 {
     typedef typename ElemOf<TYPE>::type T;
-    __shared__ float s_sum[256 * V];
+    __shared__ double s_sum[256 * V];
     const int tx = 1 << N.tx_bits, x = threadIdx.x & (tx - 1), ty = threadIdx.x >> N.tx_bits;
     float to = 1.0f;
     if constexpr (TYPE == NET_F16)
@@ -1673,9 +1675,9 @@ template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dz(RowsD N, 
         }
     const long long c = (((long long)blockIdx.x << N.tx_bits) + x) * V;
     const Seed seed = seed_of(D);
-    float sum[V];
+    double sum[V];                     // columns may cancel
 #pragma unroll
-    for (int i = 0; i < V; ++i) sum[i] = 0.0f;
+    for (int i = 0; i < V; ++i) sum[i] = 0.0;
     with_act(act, [&](auto kind) {
         constexpr int ACT = decltype(kind)::value;
         rows_of<V>(N, c, ty, [&](long long first, long long step, long long rows, int n, auto whole) {
@@ -1728,7 +1730,7 @@ template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dz(RowsD N, 
     for (int i = 0; i < V; ++i) s_sum[threadIdx.x * V + i] = sum[i];
     __syncthreads();
     for (int i = threadIdx.x; i < tx * V; i += 256) {
-        float all = 0.0f;
+        double all = 0.0;
         for (int r = 0; r < 256 / tx; ++r) all += s_sum[r * tx * V + i];
         const long long k = ((long long)blockIdx.x << N.tx_bits) * V + i;
         if (k < N.cols) sums[blockIdx.y * N.cols + k] = all;
@@ -1736,12 +1738,12 @@ template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dz(RowsD N, 
 }
 
 // dbias from the blocks' sums: 64 columns a block, every 16th sum a wave
-template <int TYPE> __global__ __launch_bounds__(1024) void k_dbias(const float *__restrict__ sums, int blocks, long long cols, void *out)
+template <int TYPE> __global__ __launch_bounds__(1024) void k_dbias(const double *__restrict__ sums, int blocks, long long cols, void *out)
 {
-    __shared__ float s_sum[16][64];
+    __shared__ double s_sum[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const long long c = blockIdx.x * 64ll + lane;
-    float all = 0.0f;
+    double all = 0.0;
     if (c < cols)
 #pragma unroll 16
         for (int b = wave; b < blocks; b += 16) all += sums[b * cols + c];
@@ -1749,7 +1751,7 @@ template <int TYPE> __global__ __launch_bounds__(1024) void k_dbias(const float 
     __syncthreads();
     if (wave == 0 && c < cols) {
         for (int w = 1; w < 16; ++w) all += s_sum[w][lane];
-        static_cast<typename ElemOf<TYPE>::type *>(out)[c] = narrow<TYPE>(all);
+        static_cast<typename ElemOf<TYPE>::type *>(out)[c] = narrow<TYPE>((float)all);
     }
 }
 
