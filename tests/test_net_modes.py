@@ -26,8 +26,9 @@ def test_tangents_are_not_lost(fake, call):  # noqa: F811
 def test_traces_are_refused(fake, call):  # noqa: F811
     from torch.fx.experimental.proxy_tensor import make_fx
     from paper_2211_15601_amd import net
-    with pytest.raises(RuntimeError, match="cannot be traced"):
-        make_fx(lambda t: call(net, t))(on_gpu(4, 6))
+    for before in (False, True):
+        with pytest.raises(RuntimeError, match="cannot be traced"):
+            make_fx(lambda t: call(net, t), pre_dispatch=before)(on_gpu(4, 6))
     with pytest.raises(RuntimeError, match="cannot be traced"):
         torch.jit.trace(lambda t: call(net, t), (on_gpu(4, 6),), check_trace=False)
     assert not fake.calls
