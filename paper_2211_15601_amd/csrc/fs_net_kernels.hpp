@@ -748,7 +748,7 @@ __device__ inline void tile_of(const TilesD &N, int block, int &tp, int &tq)
 }
 
 // D = P Q^T and what becomes of it.  BP x BQ results a block, WP x WQ waves; blockIdx.y: the part of the range of t, `t_part` long.
-// 16 bits: bound by latency (1536 x 1024 x 768 fp16 12.7 us) and, at odd addresses, by the loads (8192 x 4096 x 4096 at odd elements 400 us).  fp32: by the arithmetic beside the matrix
+// 16 bits: bound by latency (1536 x 1024 x 768 fp16 12.7 us) and, at odd addresses, by the loads (8192 x 4096 x 4096 at odd elements 371 us).  fp32: by the arithmetic beside the matrix
 // instructions, the parts (5.7 instructions an element) and the epilogue: 200003 x 256 x 256 with silu 177 us, 148 TFLOP/s, 8192 x 4096 x 4096 1293 us, 213 TFLOP/s (the library's
 // 1822).  Two blocks of eight waves a compute unit, whose phases mix: three of four took 188, two of four (with 7.6 instructions an element) 247.
 template <int TYPE, bool PCOL, bool QCOL, int BP, int BQ, int WP, int WQ, int BUFFERS, int AHEAD>
@@ -1270,7 +1270,7 @@ template <int TYPE, class Q, class N> __device__ inline void dz_eight(float (&x)
 // a NaN of another operand's infinity: dX has sums of its own for the rests, and leaves them out where the others' are no finite numbers; dweight (whose second sums would
 // take 437 registers, one block a compute unit) makes such results again.  Forward and backward of 1024 x 64 x 64 bf16, gelu, 20.8 us, by one part 16.6; of
 // 65536 x 128 x 128, silu, 56, by one 50: there one part is taken.
-// 65536 x 128 x 128 fp32 39 us (134 MB, 3.4 TB/s; matrix pipe busy 22 % of the time, vector instructions 26), bf16 31 (67 MB, 2.2 TB/s; 4 and 31): four barriers every 32
+// 65536 x 128 x 128 fp32 40 us (134 MB, 3.3 TB/s; matrix pipe busy 21 % of the time, vector instructions 26), bf16 31 (67 MB, 2.2 TB/s; 4 and 31): four barriers every 32
 // rows, between which loads, parts and products follow one another.  For 256 x 256 in 16 bits, one
 // block a compute unit, that took 624 us against 556 of the other kernels, so B is 128.
 template <int TYPE, int B, int WAVES, bool RESTS>
@@ -1588,7 +1588,7 @@ template <int TYPE, int V, bool WHOLE> __device__ inline Packed<TYPE, V> load_ro
 }
 
 // Y = R + drop(X).  Two rows' loads before the first one's store, which might be to the same memory.  Bound by memory: 134 M bf16 without residual 108 us (5.0 TB/s; with p = 0, a copy,
-// 101), with residual 166 (4.9 TB/s; p = 0: 164).  Beside that vector instructions, most of them Philox's, keep the SIMDs busy for 68 % of the time, with residual 43 %.
+// 101), with residual 166 (4.9 TB/s; p = 0: 164).  Beside that vector instructions, most of them Philox's, keep the SIMDs busy for 65 % of the time, with residual 43 %.
 template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dropout(RowsD N, MatD X, MatD R, void *y, long long ldy, DropD D)
 {
     typedef typename ElemOf<TYPE>::type T;
@@ -1650,7 +1650,8 @@ __global__ __launch_bounds__(256) void k_largest(RowsD N, MatD G, unsigned *__re
     if (threadIdx.x == 0) most[blockIdx.x] = all;
 }
 
-// dZ = drop(G act'(Z)), and the sums of its columns over a block's rows (either may be NULL).  134 M bf16 with Z in fp32 239 us (1.07 GB, 4.5 TB/s), beside Philox's arithmetic.
+// dZ = drop(G act'(Z)), and the sums of its columns over a block's rows (either may be NULL).  134 M bf16 with Z in fp32 241 us (1.07 GB, 4.5 TB/s), vector instructions busy
+// for 46 % of that.
 // fp16: dZ is written times a power of two, which goes by k_largest's `most` (where that is not NULL) and whose inverse goes to *factor.
 // rest (16 bits, or NULL): what the rounding leaves of dZ, none where it is no finite number.
 template <int TYPE, int V> __global__ __launch_bounds__(256) void k_dz(RowsD N, MatD G, MatD Z, int z_f32, int act, float beta, DropD D, void *dz, long long lddz, double *__restrict__ sums,
