@@ -47,8 +47,9 @@ def _check(what: str, t: torch.Tensor, like: torch.Tensor, types):
 
 def _check_input(x):
     # The library writes through addresses: a trace would hold a result that nothing computes.
-    if (torch._C._is_tracing() or torch._C._dispatch_tls_is_dispatch_key_included(torch._C.DispatchKey.PreDispatch) or
-            torch._C._len_torch_dispatch_stack() and torch._C._get_dispatch_mode(torch._C._TorchDispatchModeKey.PROXY) is not None):
+    # (torch.compile stops at those addresses, and has the call made.)
+    if not torch.compiler.is_compiling() and (torch._C._is_tracing() or torch._C._dispatch_tls_is_dispatch_key_included(torch._C.DispatchKey.PreDispatch) or
+                                              torch._C._len_torch_dispatch_stack() and torch._C._get_dispatch_mode(torch._C._TorchDispatchModeKey.PROXY) is not None):
         raise RuntimeError("layers cannot be traced (torch.jit.trace, make_fx, torch.export): their calls leave no operations behind")
     if not isinstance(x, torch.Tensor):
         raise TypeError(f"x: expected a tensor, got {type(x).__name__}")

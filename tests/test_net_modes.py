@@ -133,3 +133,16 @@ def test_dropout_is_its_own_derivative(fake, monkeypatch):  # noqa: F811
         assert bool((dx == 28.0).all()) and bool((dr == 14.0).all())
         assert bool((torch.autograd.grad(dx.sum() + dr.sum(), x, retain_graph=True)[0] == 8.0 + 4.0).all())
         assert bool((torch.autograd.grad(dx.sum(), r)[0] == 4.0).all())
+
+
+@pytest.mark.parametrize("call", CALLS)
+@pytest.mark.parametrize("grad", [False, True])
+def test_compiled_programs_go_round_the_calls(fake, call, grad):  # noqa: F811
+    from paper_2211_15601_amd import net
+    x = on_gpu(4, 6).requires_grad_(grad)
+    torch.compiler.reset()
+    try:
+        y = torch.compile(lambda t: call(net, t) + 1, backend="eager")(x)
+        assert len(fake.calls) == 1 and y.shape == (4, 6) and y.requires_grad == grad
+    finally:
+        torch.compiler.reset()
