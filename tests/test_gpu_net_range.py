@@ -83,3 +83,33 @@ def test_infinities_beside_what_is_scaled(net, size):  # noqa: F811
             got = out[name].cpu().to(F64)
             assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got[want.isinf()], want[want.isinf()]), (name, v)
             assert got[want.abs() < 60000].isfinite().all(), name
+
+
+def test_graphs_of_scaled_layers(net):  # noqa: F811
+    """What dZ is scaled by is found anew at each replay; wide layers, narrow ones, and products in two parts, on gradients of other sizes each time."""
+    layers = [make(*size, T, seed=sum(size)) for size in ((300, 200, 130), (2000, 128, 128), (70, 24, 40), (4, 3, 500))]
+    gs = [t[4].clone() for t in layers]
+
+    def step():
+        out = []
+        for (x, w, b, r, _), g in zip(layers, gs):
+            leaves = [t.detach().requires_grad_(True) for t in (x, w, b)]
+            out += torch.autograd.grad(net.linear(*leaves, activation="silu", dropout=0.25, seed=SEED), leaves, g)
+        return out
+
+    step()
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = step()
+        graphs.append((graph, out))
+    for k, size in enumerate((1.0, 1e-6, 3e4, 1.0, 2.0 ** -20, 1e-3)):
+        for g, t in zip(gs, layers):
+            g.copy_(t[4].float().clamp(-2.0, 2.0) * size)
+        want = step()
+        graph, out = graphs[k % 2]
+        graph.replay()
+        torch.cuda.synchronize() if k % 3 == 0 else None
+        assert all(torch.equal(a, b) for a, b in zip(out, want)) and all(bool(v.any()) for v in want), size
